@@ -295,11 +295,11 @@ def _encode(m, v):
 
 
 def _decode(cm, sm, cv, sv):
-    t = cm.view(-1, BLOCK).float() * (1.0 / 127.0)
-    m = t * t.abs() * sm.view(-1, 1)
-    t = cv.view(-1, BLOCK).float() * (1.0 / 255.0)
-    t = t * t
-    return m, t * t * sv.view(-1, 1)
+    c = cm.view(-1, BLOCK).float()
+    m = (c * c.abs()).mul_(1.0 / 127.0 ** 2).mul_(sm.view(-1, 1))
+    c = cv.view(-1, BLOCK).float()
+    c = c * c
+    return m, (c * c).mul_(1.0 / 255.0 ** 4).mul_(sv.view(-1, 1))
 
 
 # --------------------------------------------------------------------------------------------------------
