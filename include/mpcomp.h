@@ -288,6 +288,122 @@ mpc_status mpc_quant_compress_noalloc(const float* x, int64_t rows, int64_t row_
                                       float* scale, float* minv, mpc_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* The last stage's loss over the vocabulary                                */
+/* ------------------------------------------------------------------------ */
+
+/* Element types of the calls below that take more than fp32. */
+typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
+
+/* Softmax cross entropy of a linear head, in pieces of the vocabulary, without
+ * keeping the logits:
+ *   l[t][v] = sum_d h[t][d] w[v][d];   lse[t] = log sum_v exp l[t][v];
+ *   loss[t] = lse[t] - l[t][targets[t]].
+ *   h       [tokens][hidden] of `type`, rows ldh elements apart (ldh >= hidden).
+ *   w       [vocab][hidden] of `type`, rows ldw elements apart (ldw >= hidden).
+ *   targets [tokens] int64.  A token whose target is `ignore_index` does not
+ *           count: its loss and lse are +0, its gradient is zero, and its row of
+ *           h is not used (it may hold NaN).  Any other target outside
+ *           [0, vocab) is reported by mpc_get_status as MPC_ERR_DEVICE and its
+ *           token does not count either.
+ *   loss, lse  [tokens] fp32, out.
+ *   ws      workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
+ *           hidden, vocab, type, 0, 0), 256-byte aligned.
+ * Products are summed in fp32 and fp32 inputs are not rounded to a narrower
+ * type.  tokens = 0 is a no-op.  Requires hidden >= 1, 1 <= vocab <= 2^31-1,
+ * tokens <= 2^31-1. */
+size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
+                                     int grad, int64_t piece);
+mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                                 const int64_t* targets, int64_t tokens, int64_t hidden,
+                                 int64_t vocab, mpc_dtype type, int64_t ignore_index, float* loss,
+                                 float* lse, void* ws, size_t ws_bytes, mpc_stream_t stream);
+
+/* Its gradient, from the lse of the forward call (the logits are formed again):
+ *   c[t][v] = g[t] (exp(l[t][v] - lse[t]) - [v == targets[t]]);
+ *   dh[t][d] = sum_v c[t][v] w[v][d];   dw[v][d] = sum_t c[t][v] h[t][d].
+ *   gloss  [tokens] fp32, the gradient of each token's loss; NULL for the mean
+ *          over the tokens that count (g = 1 / their number; 0 when none does).
+ *   dh     [tokens][hidden] of `type`, rows lddh elements apart, out (zero for
+ *          tokens that do not count); dw [vocab][hidden], rows lddw apart, out.
+ *   piece  vocabulary entries whose c is in the workspace at a time; 0 lets the
+ *          library choose (1 GiB of c at most).
+ *   ws     workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
+ *          hidden, vocab, type, 1, piece), 256-byte aligned.
+ * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
+ * tokens = 0 writes dw = 0. */
+mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                                  const int64_t* targets, const float* lse, const float* gloss,
+                                  int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
+                                  int64_t ignore_index, int64_t piece, void* dh, int64_t lddh,
+                                  void* dw, int64_t lddw, void* ws, size_t ws_bytes,
+                                  mpc_stream_t stream);
+
+/* Loss and gradients in one call, for a training step that knows g beforehand:
+ * the arguments and results of the two calls above. */
+mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                               const int64_t* targets, const float* gloss, int64_t tokens,
+                               int64_t hidden, int64_t vocab, mpc_dtype type, int64_t ignore_index,
+                               int64_t piece, float* loss, void* dh, int64_t lddh, void* dw,
+                               int64_t lddw, void* ws, size_t ws_bytes, mpc_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* A stage's optimiser step                                                 */
+/* ------------------------------------------------------------------------ */
+
+/* One tensor of the list that the calls below take.  The list itself is host
+ * memory, read before the call returns; its pointers are device memory. */
+typedef struct {
+    void* param;       /* [n] of the call's param_type, updated in place */
+    const void* grad;  /* [n] of the call's grad_type */
+    void* exp_avg;     /* first moment m:  [n] fp32, or int8 codes */
+    void* exp_avg_sq;  /* second moment v: [n] fp32, or uint8 codes */
+    float* scale_m;    /* 8-bit states: [ceil(n/256)] fp32, else unused */
+    float* scale_v;
+    void* copy;        /* [n] bf16 that receives the new param as well, or NULL */
+    int64_t n;         /* entries; 0 leaves the tensor out */
+    double lr_scale;   /* the tensor's factor on lr */
+    double weight_decay;
+} mpc_adamw_tensor;
+
+/* Entries of a tensor that share a scale in the 8-bit states. */
+#define MPC_ADAMW_BLOCK 256
+
+/* AdamW with decoupled weight decay over a list of tensors, step number `step`
+ * (from 1), with g = grad:
+ *   m <- beta1 m + (1-beta1) g;   v <- beta2 v + ((1-beta2) g) g;
+ *   p <- p (1 - lr' wd) - lr'/(1-beta1^step) * (m / (sqrt(v)/sqrt(1-beta2^step) + eps)),
+ * lr' = lr lr_scale; every step one fp32 round-to-nearest operation, rounded to
+ * param_type at the end.
+ *   state_bits 32: m and v are fp32.  8: codes in blocks of MPC_ADAMW_BLOCK
+ *     consecutive entries of a tensor that share one fp32 scale s, the largest
+ *     |m| (v) of the block: code c of m stands for sign(c) (c/127)^2 s, of v for
+ *     (c/255)^4 s; the nearest one is taken (of v in the square root; a v > 0
+ *     never gets code 0).  All-zero codes and scales are m = v = 0.
+ *   grad_norm  NULL, or a device fp32 (mpc_grad_norm): g is multiplied by
+ *     min(1, max_norm / (*grad_norm + 1e-6)) first when max_norm > 0, and the
+ *     step changes nothing when *grad_norm is not finite.
+ * A param, state or scale array must not overlap another array of the list. */
+mpc_status mpc_adamw_step(const mpc_adamw_tensor* tensors, int64_t count, mpc_dtype param_type,
+                          mpc_dtype grad_type, int state_bits, double lr, double beta1,
+                          double beta2, double eps, int64_t step, const float* grad_norm,
+                          double max_norm, mpc_stream_t stream);
+
+/* The fp32 values that the 8-bit states of a list stand for, e.g. for a
+ * checkpoint: m_out and v_out are host arrays of count device pointers, [n]
+ * fp32 each. */
+mpc_status mpc_adamw_decode(const mpc_adamw_tensor* tensors, int64_t count, float* const* m_out,
+                            float* const* v_out, mpc_stream_t stream);
+
+/* *norm (device fp32) = sqrt of the sum of the squares of every `grad` of the
+ * list (only `grad` and `n` are read).  Squares are summed in fp32 per thread
+ * and fp64 beyond, in a fixed order.
+ *   ws  workspace of ws_bytes >= mpc_grad_norm_workspace_bytes(count), 8-byte
+ *       aligned. */
+size_t mpc_grad_norm_workspace_bytes(int64_t count);
+mpc_status mpc_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, mpc_dtype grad_type,
+                         float* norm, void* ws, size_t ws_bytes, mpc_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Status and diagnostics                                                   */
 /* ------------------------------------------------------------------------ */
 

@@ -26,6 +26,9 @@ __all__ = [
     "mpc_aqsgd_decompress", "mpc_quant_codes_words", "mpc_quant_workspace_bytes",
     "mpc_quant_compress", "mpc_quant_decompress", "mpc_aqsgd_quant_workspace_bytes",
     "mpc_aqsgd_quant_compress", "mpc_aqsgd_quant_decompress", "mpc_get_status", "mpc_last_error",
+    "mpc_linear_ce_workspace_bytes", "mpc_linear_ce_forward", "mpc_linear_ce_backward",
+    "mpc_linear_ce_train", "mpc_adamw_step", "mpc_adamw_decode", "mpc_grad_norm_workspace_bytes",
+    "mpc_grad_norm",
     "mpc_set_knob", "MPC_KNOB_SPIN_LIMIT", "MPC_KNOB_TOPK_PATH", "MPC_KNOB_PDL", "STATUS_NAMES",
 ]
 
@@ -41,6 +44,7 @@ _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _INT = ctypes.c_int
 _U64 = ctypes.c_uint64
+_F64 = ctypes.c_double
 
 _SIGNATURES = {
     "mpc_version": ([], _INT),
@@ -67,6 +71,18 @@ _SIGNATURES = {
                                    _INT),
     "mpc_quant_compress_noalloc": ([_VP, _I64, _I64, _INT, _INT, _U64, _VP, _VP, _VP, _VP],
                                    _INT),
+    "mpc_linear_ce_workspace_bytes": ([_I64, _I64, _I64, _INT, _INT, _I64], _SZ),
+    "mpc_linear_ce_forward": ([_VP, _I64, _VP, _I64, _VP, _I64, _I64, _I64, _INT, _I64, _VP, _VP,
+                               _VP, _SZ, _VP], _INT),
+    "mpc_linear_ce_backward": ([_VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _I64, _I64, _INT, _I64,
+                                _I64, _VP, _I64, _VP, _I64, _VP, _SZ, _VP], _INT),
+    "mpc_linear_ce_train": ([_VP, _I64, _VP, _I64, _VP, _VP, _I64, _I64, _I64, _INT, _I64, _I64,
+                             _VP, _VP, _I64, _VP, _I64, _VP, _SZ, _VP], _INT),
+    "mpc_adamw_step": ([_VP, _I64, _INT, _INT, _INT, _F64, _F64, _F64, _F64, _I64, _VP, _F64,
+                        _VP], _INT),
+    "mpc_adamw_decode": ([_VP, _I64, _VP, _VP, _VP], _INT),
+    "mpc_grad_norm_workspace_bytes": ([_I64], _SZ),
+    "mpc_grad_norm": ([_VP, _I64, _INT, _VP, _VP, _SZ, _VP], _INT),
     "mpc_get_status": ([_VP], _INT),
     "mpc_last_error": ([], ctypes.c_char_p),
     "mpc_set_knob": ([_INT, _I64], _INT),
@@ -399,6 +415,193 @@ def mpc_aqsgd_quant_decompress(codes, scale, minv, buf_recv, sample_ids, bits: i
 
 
 # ---------------------------------------------------------------------------------------
+# The last stage's loss over the vocabulary
+# ---------------------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise MpcError(1, "%s must be a CUDA tensor" % name)
+    if t.dtype not in _DTYPES:
+        raise MpcError(1, "%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    return _DTYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor, name: str, cols: int | None = None, like=None) -> int:
+    """The distance between the rows of a 2-d tensor whose rows are contiguous."""
+    _dtype(t, name)
+    if t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise MpcError(1, "%s must be 2-d%s" % (name, "" if cols is None else " with %d columns" % cols))
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise MpcError(1, "%s must be %s on %s" % (name, like.dtype, like.device))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise MpcError(1, "the rows of %s must be contiguous" % name)
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise MpcError(1, "the rows of %s overlap" % name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _on(stream, *tensors):
+    """Tells the allocator that a call on `stream` uses what was allocated for it here."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _vector(t, n: int, dtype: torch.dtype, name: str, device):
+    _cuda(t, dtype, name)
+    if t.numel() != n or t.device != device:
+        raise MpcError(1, "%s must hold %d entries on %s" % (name, n, device))
+    return t
+
+
+def mpc_linear_ce_workspace_bytes(tokens: int, hidden: int, vocab: int, dtype=torch.float32,
+                                  grad: bool = False, piece: int = 0) -> int:
+    return int(lib().mpc_linear_ce_workspace_bytes(tokens, hidden, vocab, _DTYPES[dtype], grad, piece))
+
+
+def _linear_ce_args(h, w, targets, ignore_index, grad, piece, ws, stream):
+    ldh = _matrix(h, "h")
+    T, D = h.shape
+    if D == 0 or w.dim() != 2 or w.shape[0] == 0:
+        raise MpcError(1, "h [T, D] and w [V, D] must have D >= 1 and V >= 1")
+    ldw = _matrix(w, "w", D, h)
+    V = w.shape[0]
+    _vector(targets, T, torch.int64, "targets", h.device)
+    need = mpc_linear_ce_workspace_bytes(T, D, V, h.dtype, grad, piece)
+    given = ws
+    ws, wsb = _workspace(need, ws, h.device)
+    if given is None:
+        _on(stream, ws)
+    return T, D, V, ldh, ldw, ws, wsb
+
+
+def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, lse=None, ws=None,
+                          stream=None):
+    """Softmax cross entropy of the logits h [T, D] @ w [V, D].T against targets [T] (int64).
+    Returns (loss [T], lse [T]) in fp32; both are 0 for tokens whose target is ignore_index."""
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, False, 0, ws, stream)
+    new = []
+    if loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=h.device)
+        new.append(loss)
+    if lse is None:
+        lse = torch.empty(T, dtype=torch.float32, device=h.device)
+        new.append(lse)
+    _on(stream, *new)
+    _vector(loss, T, torch.float32, "loss", h.device)
+    _vector(lse, T, torch.float32, "lse", h.device)
+    _check(lib().mpc_linear_ce_forward(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), T, D, V,
+                                       _DTYPES[h.dtype], ignore_index, _ptr(loss), _ptr(lse),
+                                       _ptr(ws), wsb, _stream(stream)))
+    return loss, lse
+
+
+def _linear_ce_grads(h, w, dh, dw, stream):
+    new = []
+    if dh is None:
+        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        new.append(dh)
+    if dw is None:
+        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+        new.append(dw)
+    _on(stream, *new)
+    if dh.shape != h.shape or dw.shape != w.shape:
+        raise MpcError(1, "dh and dw must have the shapes of h and w")
+    return dh, _matrix(dh, "dh", h.shape[1], h), dw, _matrix(dw, "dw", h.shape[1], h)
+
+
+def mpc_linear_ce_backward(h, w, targets, lse, gloss=None, ignore_index: int = -100, piece: int = 0,
+                           dh=None, dw=None, ws=None, stream=None):
+    """The gradient of mpc_linear_ce_forward from its lse: (dh [T, D], dw [V, D]) in the type of h.
+    gloss [T] fp32 is the gradient of each token's loss; None means that of the mean over the
+    tokens that count.  piece: vocabulary entries held in the workspace at a time (0: automatic)."""
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, True, piece, ws, stream)
+    _vector(lse, T, torch.float32, "lse", h.device)
+    if gloss is not None:
+        _vector(gloss, T, torch.float32, "gloss", h.device)
+    dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
+    _check(lib().mpc_linear_ce_backward(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), _ptr(lse),
+                                        _ptr(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece,
+                                        _ptr(dh), lddh, _ptr(dw), lddw, _ptr(ws), wsb,
+                                        _stream(stream)))
+    return dh, dw
+
+
+def mpc_linear_ce_train(h, w, targets, gloss=None, ignore_index: int = -100, piece: int = 0,
+                        loss=None, dh=None, dw=None, ws=None, stream=None):
+    """Loss and gradient in one call: (loss [T], dh [T, D], dw [V, D]); arguments as for
+    mpc_linear_ce_forward and mpc_linear_ce_backward."""
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, True, piece, ws, stream)
+    if loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=h.device)
+        _on(stream, loss)
+    _vector(loss, T, torch.float32, "loss", h.device)
+    if gloss is not None:
+        _vector(gloss, T, torch.float32, "gloss", h.device)
+    dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
+    _check(lib().mpc_linear_ce_train(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), _ptr(gloss), T, D,
+                                     V, _DTYPES[h.dtype], ignore_index, piece, _ptr(loss), _ptr(dh),
+                                     lddh, _ptr(dw), lddw, _ptr(ws), wsb, _stream(stream)))
+    return loss, dh, dw
+
+
+# ---------------------------------------------------------------------------------------
+# A stage's optimiser step
+# ---------------------------------------------------------------------------------------
+
+def mpc_adamw_step(plan, lr: float, beta1: float, beta2: float, eps: float, step: int,
+                   grad_norm=None, max_norm: float = 0.0, stream=None) -> None:
+    """One AdamW step over the tensors of an ``AdamWPlan``, in place; ``step`` counts from 1.
+    With ``grad_norm`` (the fp32 device scalar of mpc_grad_norm) gradients are scaled by
+    min(1, max_norm / (grad_norm + 1e-6)) if max_norm > 0, and the step changes nothing when the
+    norm is not finite."""
+    if grad_norm is not None:
+        _vector(grad_norm, 1, torch.float32, "grad_norm", plan.device)
+    _check(lib().mpc_adamw_step(plan.table, plan.count, plan.param_type, plan.grad_type,
+                                plan.state_bits, lr, beta1, beta2, eps, step, _ptr(grad_norm),
+                                max_norm, _stream(stream)))
+
+
+def mpc_adamw_decode(plan, m_out, v_out, stream=None):
+    """The fp32 values that the 8-bit states of an ``AdamWPlan`` stand for, into the tensors of
+    m_out and v_out (one for each tensor of the plan)."""
+    if plan.state_bits != 8:
+        raise MpcError(1, "the plan's states are not 8-bit codes")
+    if len(m_out) != plan.count or len(v_out) != plan.count:
+        raise MpcError(1, "m_out and v_out must hold one tensor for each of the plan's %d" % plan.count)
+    for name, outs in (("m_out", m_out), ("v_out", v_out)):
+        for t, n in zip(outs, plan.sizes):
+            _vector(t, n, torch.float32, name, plan.device)
+    array = _VP * max(1, plan.count)
+    _check(lib().mpc_adamw_decode(plan.table, plan.count, array(*[t.data_ptr() for t in m_out]),
+                                  array(*[t.data_ptr() for t in v_out]), _stream(stream)))
+    return m_out, v_out
+
+
+def mpc_grad_norm_workspace_bytes(count: int) -> int:
+    return int(lib().mpc_grad_norm_workspace_bytes(count))
+
+
+def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
+    """The 2-norm of all gradients of an ``AdamWPlan`` together, as a device fp32 of one entry."""
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=plan.device)
+        _on(stream, norm)
+    _vector(norm, 1, torch.float32, "norm", plan.device)
+    given = ws
+    ws, wsb = _workspace(mpc_grad_norm_workspace_bytes(plan.count), ws, plan.device)
+    if given is None:
+        _on(stream, ws)
+    _check(lib().mpc_grad_norm(plan.table, plan.count, plan.grad_type, _ptr(norm), _ptr(ws), wsb,
+                               _stream(stream)))
+    return norm
+
+
+# ---------------------------------------------------------------------------------------
 # Status and knobs
 # ---------------------------------------------------------------------------------------
 
@@ -417,5 +620,8 @@ def mpc_set_knob(knob: int, value: int) -> None:
 
 # The compression block between pipeline stages (§2.1) built on the calls above.
 from .boundary import CompressionBoundary, Quant, Reuse, TopK, with_boundaries  # noqa: E402
+# The last stage's loss and every stage's optimiser, built on the calls above.
+from .training import AdamW, AdamWPlan, LinearCrossEntropy, linear_cross_entropy  # noqa: E402
 
+__all__ += ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
 __all__ += ["CompressionBoundary", "Quant", "TopK", "Reuse", "with_boundaries"]

@@ -585,6 +585,255 @@ mpc_status mpc_aqsgd_quant_decompress(const uint32_t* codes, const float* scale,
   return ok();
 }
 
+namespace {
+
+mpc_status check_type(int type, const char* name) {
+  if (type != MPC_F32 && type != MPC_BF16)
+    return set_error(MPC_ERR_INVALID_ARG, "%s=%d is neither MPC_F32 nor MPC_BF16", name, type);
+  return MPC_OK;
+}
+
+mpc_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, int type, const char* name) {
+  MPC_TRY(check_ptr(p, type == MPC_BF16 ? 2 : 4, name));
+  if (ld < cols)
+    return set_error(MPC_ERR_INVALID_ARG, "rows of %s are %lld elements apart, shorter than hidden=%lld",
+                     name, (long long)ld, (long long)cols);
+  if (ld > INT64_MAX / 4 / rows) return set_error(MPC_ERR_INVALID_ARG, "the size of %s overflows", name);
+  return MPC_OK;
+}
+
+bool linear_ce_sizes_ok(int64_t tokens, int64_t hidden, int64_t vocab, int64_t piece) {
+  return tokens >= 0 && tokens <= 0x7fffffffLL && hidden >= 1 && hidden <= (1 << 24) && vocab >= 1 &&
+         vocab <= 0x7fffffffLL && piece >= 0;
+}
+
+// Shared body of the three linear cross-entropy calls.
+mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size_t ws_bytes,
+                            mpc_stream_t stream) {
+  MPC_TRY(check_type(type, "type"));
+  if (!linear_ce_sizes_ok(a.T, a.D, a.V, a.piece))
+    return set_error(MPC_ERR_INVALID_ARG, "tokens=%lld hidden=%lld vocab=%lld piece=%lld", (long long)a.T,
+                     (long long)a.D, (long long)a.V, (long long)a.piece);
+  a.bf16 = type == MPC_BF16;
+  if (a.T == 0 && !grad) return ok();
+  MPC_TRY(check_matrix(a.w, a.V, a.D, a.ldw, type, "w"));
+  if (grad) MPC_TRY(check_matrix(a.dw, a.V, a.D, a.lddw, type, "dw"));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (a.T == 0) {
+    const size_t size = a.bf16 ? 2 : 4;
+    const cudaError_t e = cudaMemset2DAsync(a.dw, a.lddw * size, 0, a.D * size, a.V, s);
+    if (e != cudaSuccess) return cuda_error(e, "linear_ce clear");
+    return ok();
+  }
+  MPC_TRY(check_matrix(a.h, a.T, a.D, a.ldh, type, "h"));
+  if (grad) MPC_TRY(check_matrix(a.dh, a.T, a.D, a.lddh, type, "dh"));
+  MPC_TRY(check_ptr(a.targets, 8, "targets"));
+  if (a.gloss != nullptr) MPC_TRY(check_ptr(a.gloss, 4, "gloss"));
+  const size_t need = mpc_linear_ce_workspace_bytes(a.T, a.D, a.V, type, grad, a.piece);
+  if (a.ws == nullptr || ws_bytes < need)
+    return set_error(MPC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
+                     a.ws == nullptr ? (size_t)0 : ws_bytes);
+  if (!aligned_to(a.ws, 256)) return set_error(MPC_ERR_INVALID_ARG, "ws is not 256-byte aligned");
+  Device d;
+  MPC_TRY(current_device(&d));
+  a.spin_limit = g_spin_limit.load();
+  a.status = d.status;
+  const cudaError_t e = mpc::launch_linear_ce(a, d.num_sms, s);
+  if (e != cudaSuccess) return cuda_error(e, "linear_ce launch");
+  return ok();
+}
+
+}  // namespace
+
+size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
+                                     int grad, int64_t piece) {
+  if (tokens == 0 || !linear_ce_sizes_ok(tokens, hidden, vocab, piece)) return 0;
+  return mpc::linear_ce_workspace_bytes(tokens, hidden, vocab, type == MPC_BF16, grad, piece);
+}
+
+mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                                 const int64_t* targets, int64_t tokens, int64_t hidden,
+                                 int64_t vocab, mpc_dtype type, int64_t ignore_index, float* loss,
+                                 float* lse, void* ws, size_t ws_bytes, mpc_stream_t stream) {
+  if (tokens > 0) {
+    MPC_TRY(check_ptr(loss, 4, "loss"));
+    MPC_TRY(check_ptr(lse, 4, "lse"));
+  }
+  mpc::LinearCeArgs a = {};
+  a.h = h;
+  a.ldh = ldh;
+  a.w = w;
+  a.ldw = ldw;
+  a.targets = targets;
+  a.T = tokens;
+  a.D = hidden;
+  a.V = vocab;
+  a.ignore = ignore_index;
+  a.loss = loss;
+  a.lse = lse;
+  a.ws = ws;
+  return linear_ce_common(a, false, type, ws_bytes, stream);
+}
+
+mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                                  const int64_t* targets, const float* lse, const float* gloss,
+                                  int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
+                                  int64_t ignore_index, int64_t piece, void* dh, int64_t lddh,
+                                  void* dw, int64_t lddw, void* ws, size_t ws_bytes,
+                                  mpc_stream_t stream) {
+  if (tokens > 0) MPC_TRY(check_ptr(lse, 4, "lse"));
+  mpc::LinearCeArgs a = {};
+  a.h = h;
+  a.ldh = ldh;
+  a.w = w;
+  a.ldw = ldw;
+  a.targets = targets;
+  a.T = tokens;
+  a.D = hidden;
+  a.V = vocab;
+  a.ignore = ignore_index;
+  a.lse_in = lse;
+  a.gloss = gloss;
+  a.dh = dh;
+  a.lddh = lddh;
+  a.dw = dw;
+  a.lddw = lddw;
+  a.piece = piece;
+  a.ws = ws;
+  return linear_ce_common(a, true, type, ws_bytes, stream);
+}
+
+mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_t ldw,
+                               const int64_t* targets, const float* gloss, int64_t tokens,
+                               int64_t hidden, int64_t vocab, mpc_dtype type, int64_t ignore_index,
+                               int64_t piece, float* loss, void* dh, int64_t lddh, void* dw,
+                               int64_t lddw, void* ws, size_t ws_bytes, mpc_stream_t stream) {
+  if (tokens > 0) MPC_TRY(check_ptr(loss, 4, "loss"));
+  mpc::LinearCeArgs a = {};
+  a.h = h;
+  a.ldh = ldh;
+  a.w = w;
+  a.ldw = ldw;
+  a.targets = targets;
+  a.T = tokens;
+  a.D = hidden;
+  a.V = vocab;
+  a.ignore = ignore_index;
+  a.loss = loss;
+  a.gloss = gloss;
+  a.dh = dh;
+  a.lddh = lddh;
+  a.dw = dw;
+  a.lddw = lddw;
+  a.piece = piece;
+  a.ws = ws;
+  return linear_ce_common(a, true, type, ws_bytes, stream);
+}
+
+namespace {
+
+mpc_status check_list(const mpc_adamw_tensor* tensors, int64_t count) {
+  if (count < 0) return set_error(MPC_ERR_INVALID_ARG, "count=%lld < 0", (long long)count);
+  if (count > 0 && tensors == nullptr) return set_error(MPC_ERR_INVALID_ARG, "tensors is NULL");
+  for (int64_t i = 0; i < count; ++i)
+    if (tensors[i].n < 0 || tensors[i].n > (int64_t{1} << 40))
+      return set_error(MPC_ERR_INVALID_ARG, "tensor %lld has n=%lld", (long long)i, (long long)tensors[i].n);
+  return MPC_OK;
+}
+
+mpc_status check_states(const mpc_adamw_tensor& t, int state_bits) {
+  const uintptr_t align = state_bits == 32 ? 4 : 1;
+  MPC_TRY(check_ptr(t.exp_avg, align, "exp_avg"));
+  MPC_TRY(check_ptr(t.exp_avg_sq, align, "exp_avg_sq"));
+  if (state_bits == 8) {
+    MPC_TRY(check_ptr(t.scale_m, 4, "scale_m"));
+    MPC_TRY(check_ptr(t.scale_v, 4, "scale_v"));
+  }
+  return MPC_OK;
+}
+
+}  // namespace
+
+mpc_status mpc_adamw_step(const mpc_adamw_tensor* tensors, int64_t count, mpc_dtype param_type,
+                          mpc_dtype grad_type, int state_bits, double lr, double beta1,
+                          double beta2, double eps, int64_t step, const float* grad_norm,
+                          double max_norm, mpc_stream_t stream) {
+  MPC_TRY(check_type(param_type, "param_type"));
+  MPC_TRY(check_type(grad_type, "grad_type"));
+  if (state_bits != 32 && state_bits != 8)
+    return set_error(MPC_ERR_INVALID_ARG, "state_bits=%d is neither 32 nor 8", state_bits);
+  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0))
+    return set_error(MPC_ERR_INVALID_ARG, "beta1=%g and beta2=%g must be in [0, 1)", beta1, beta2);
+  if (!(eps >= 0.0)) return set_error(MPC_ERR_INVALID_ARG, "eps=%g < 0", eps);
+  if (step < 1) return set_error(MPC_ERR_INVALID_ARG, "step=%lld < 1", (long long)step);
+  if (grad_norm != nullptr) MPC_TRY(check_ptr(grad_norm, 4, "grad_norm"));
+  MPC_TRY(check_list(tensors, count));
+  bool any = false;
+  for (int64_t i = 0; i < count; ++i) {
+    const mpc_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    any = true;
+    MPC_TRY(check_ptr(t.param, param_type == MPC_BF16 ? 2 : 4, "param"));
+    MPC_TRY(check_ptr(t.grad, grad_type == MPC_BF16 ? 2 : 4, "grad"));
+    MPC_TRY(check_states(t, state_bits));
+    if (t.copy != nullptr) MPC_TRY(check_ptr(t.copy, 2, "copy"));
+  }
+  if (!any) return ok();
+  Device d;
+  MPC_TRY(current_device(&d));
+  const mpc::AdamwArgs a = {tensors, count, param_type == MPC_BF16, grad_type == MPC_BF16, state_bits,
+                            lr,      beta1, beta2, eps, step, grad_norm, max_norm};
+  const cudaError_t e = mpc::launch_adamw(a, d.num_sms, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "adamw launch");
+  return ok();
+}
+
+mpc_status mpc_adamw_decode(const mpc_adamw_tensor* tensors, int64_t count, float* const* m_out,
+                            float* const* v_out, mpc_stream_t stream) {
+  MPC_TRY(check_list(tensors, count));
+  if (count > 0 && (m_out == nullptr || v_out == nullptr))
+    return set_error(MPC_ERR_INVALID_ARG, "m_out or v_out is NULL");
+  bool any = false;
+  for (int64_t i = 0; i < count; ++i) {
+    if (tensors[i].n == 0) continue;
+    any = true;
+    MPC_TRY(check_states(tensors[i], 8));
+    MPC_TRY(check_ptr(m_out[i], 4, "m_out"));
+    MPC_TRY(check_ptr(v_out[i], 4, "v_out"));
+  }
+  if (!any) return ok();
+  Device d;
+  MPC_TRY(current_device(&d));
+  const cudaError_t e = mpc::launch_adamw_decode(tensors, count, m_out, v_out, d.num_sms,
+                                                 reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "adamw_decode launch");
+  return ok();
+}
+
+size_t mpc_grad_norm_workspace_bytes(int64_t count) {
+  return count < 0 ? 0 : mpc::grad_norm_workspace_bytes(count);
+}
+
+mpc_status mpc_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, mpc_dtype grad_type,
+                         float* norm, void* ws, size_t ws_bytes, mpc_stream_t stream) {
+  MPC_TRY(check_type(grad_type, "grad_type"));
+  MPC_TRY(check_list(tensors, count));
+  MPC_TRY(check_ptr(norm, 4, "norm"));
+  for (int64_t i = 0; i < count; ++i)
+    if (tensors[i].n > 0) MPC_TRY(check_ptr(tensors[i].grad, grad_type == MPC_BF16 ? 2 : 4, "grad"));
+  const size_t need = mpc::grad_norm_workspace_bytes(count);
+  if (ws == nullptr || ws_bytes < need)
+    return set_error(MPC_ERR_WORKSPACE, "workspace of %zu bytes needed", need);
+  MPC_TRY(check_ptr(ws, 8, "ws"));
+  Device d;
+  MPC_TRY(current_device(&d));
+  const cudaError_t e = mpc::launch_grad_norm(tensors, count, grad_type == MPC_BF16, norm,
+                                              static_cast<double*>(ws), d.num_sms,
+                                              reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "grad_norm launch");
+  return ok();
+}
+
 mpc_status mpc_get_status(mpc_stream_t stream) {
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaStreamSynchronize(s);

@@ -1,0 +1,521 @@
+// adamw.cu -- the optimiser step of a pipeline stage: AdamW over many tensors
+// in one launch, its states in fp32 or in 8-bit codes, and the global norm of
+// the gradients that the step clips by.
+//
+// Mathematics (decoupled weight decay; every operation one fp32 round-to-nearest
+// operation in this order, no contraction):
+//   g <- g * min(1, max_norm / (norm + 1e-6))            (when a norm is given)
+//   m <- b1 m + (1-b1) g;   v <- b2 v + ((1-b2) g) g
+//   p <- p (1 - lr wd) - (lr / (1-b1^t)) * (m / (sqrt(v) / sqrt(1-b2^t) + eps))
+// 8-bit states: blocks of 256 consecutive entries of a tensor share one fp32
+// scale s, the block's largest |m| (or v).  A code c stands for
+//   m: sign(c) (c/127)^2 s, c in -127..127;      v: (c/255)^4 s, c in 0..255.
+// The squares spend the codes on small values: the least non-zero |m| is s/16129,
+// the least non-zero sqrt(v) is sqrt(s)/65025.  The code is the nearest one, for
+// m in m/s and for v in sqrt(v/s) (what the step divides by); a v > 0 never gets
+// code 0, so that a small v cannot turn into a division by eps alone.  The step
+// itself uses the m and v of before the coding.
+//
+// What bounds it: memory.  fp32 states move 28 bytes an entry (p, m, v read and
+// written, g read).  The work is laid out over chunks of 2048 entries that never
+// straddle two tensors: a CTA of 256 threads takes a contiguous range of chunks
+// of the whole list, a warp 256 entries, a lane 8 consecutive ones (16-byte
+// loads; a warp's entries are one 8-bit block, so a block's largest is one warp
+// reduction).  The list travels as a kernel argument: no copy to the device
+// precedes the launch, and a captured graph holds it by value.
+#include <algorithm>
+#include <cmath>
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "launch_util.h"
+
+namespace mpc {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLane = 8;                   // entries a lane holds
+constexpr int kChunk = kThreads * kLane;   // entries a CTA takes at a time
+
+struct Entry {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* sm;
+  float* sv;
+  void* copy;
+  int64_t n;
+  float keep;  // 1 - lr wd
+  float step;  // lr / (1 - b1^t)
+  int first;   // the tensor's first chunk in the launch
+  int wide;    // every pointer suits 16-byte accesses
+};
+
+template <int N>
+struct Table {
+  Entry e[N];
+  int count;
+  int chunks;
+};
+
+// Table sizes: the small one keeps the kernel arguments under 4 KB (a launch
+// then costs what any other does), the large one fills the 32 KB limit.
+constexpr int kSmallTable = 48;
+constexpr int kLargeTable = 400;
+static_assert(sizeof(Table<kSmallTable>) + 64 <= 4096, "");
+static_assert(sizeof(Table<kLargeTable>) + 64 <= 32764, "");
+
+struct Scalars {
+  float b1, c1, b2, c2, rs, eps, max_norm;
+  const float* norm;
+};
+
+// The contiguous range of chunks of this CTA, and the tensor of its first one.
+template <int N>
+__device__ __forceinline__ void my_range(const Table<N>& t, int* c0, int* c1, int* at) {
+  const int64_t total = t.chunks;
+  *c0 = static_cast<int>(total * blockIdx.x / gridDim.x);
+  *c1 = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x);
+  int lo = 0, hi = t.count - 1;  // the last tensor whose first chunk is <= c0
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.e[mid].first <= *c0) lo = mid;
+    else hi = mid - 1;
+  }
+  *at = lo;
+}
+
+__device__ __forceinline__ float bf_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
+  __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  uint32_t u;
+  memcpy(&u, &p, 4);
+  return u;
+}
+
+// Eight entries from i on as floats (left = how many of them exist).
+__device__ __forceinline__ void load8(const float* p, int64_t i, int left, bool wide, float (&x)[8]) {
+  if (wide && left >= 8) {
+    const float4 a = *reinterpret_cast<const float4*>(p + i);
+    const float4 b = *reinterpret_cast<const float4*>(p + i + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < left ? p[i + j] : 0.0f;
+  }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int64_t i, int left, bool wide, float (&x)[8]) {
+  if (wide && left >= 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p + i);
+    x[0] = bf_lo(a.x); x[1] = bf_hi(a.x); x[2] = bf_lo(a.y); x[3] = bf_hi(a.y);
+    x[4] = bf_lo(a.z); x[5] = bf_hi(a.z); x[6] = bf_lo(a.w); x[7] = bf_hi(a.w);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < left ? __bfloat162float(p[i + j]) : 0.0f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int64_t i, int left, bool wide, const float (&x)[8]) {
+  if (wide && left >= 8) {
+    *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[i + j] = x[j];
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int64_t i, int left, bool wide, const float (&x)[8]) {
+  if (wide && left >= 8) {
+    *reinterpret_cast<uint4*>(p + i) = make_uint4(bf_pack(x[0], x[1]), bf_pack(x[2], x[3]),
+                                                  bf_pack(x[4], x[5]), bf_pack(x[6], x[7]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) p[i + j] = __float2bfloat16_rn(x[j]);
+  }
+}
+
+// Eight codes (one byte each, low byte first) as two words.
+__device__ __forceinline__ uint2 load_codes(const void* p, int64_t i, int left, bool wide) {
+  const uint8_t* b = static_cast<const uint8_t*>(p) + i;
+  if (wide && left >= 8) return *reinterpret_cast<const uint2*>(b);
+  uint2 u = make_uint2(0, 0);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < left) (j < 4 ? u.x : u.y) |= static_cast<uint32_t>(b[j]) << (8 * (j & 3));
+  return u;
+}
+__device__ __forceinline__ void store_codes(void* p, int64_t i, int left, bool wide, uint2 u) {
+  uint8_t* b = static_cast<uint8_t*>(p) + i;
+  if (wide && left >= 8) {
+    *reinterpret_cast<uint2*>(b) = u;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < left) b[j] = static_cast<uint8_t>((j < 4 ? u.x : u.y) >> (8 * (j & 3)));
+  }
+}
+
+// The squares of a code are exact in fp32, so a value carries three (m) or four
+// (v) roundings.
+__device__ __forceinline__ float decode_m(uint32_t u, int j, float s) {
+  const float c = static_cast<float>(static_cast<int8_t>(u >> (8 * j)));
+  return fmul(fmul(fmul(c, fabsf(c)), static_cast<float>(1.0 / (127.0 * 127.0))), s);
+}
+__device__ __forceinline__ float decode_v(uint32_t u, int j, float s) {
+  const float c = static_cast<float>((u >> (8 * j)) & 0xffu);
+  const float c2 = fmul(c, c);
+  return fmul(fmul(fmul(c2, c2), static_cast<float>(1.0 / (255.0 * 255.0 * 255.0 * 255.0))), s);
+}
+
+// 1/top, or 0 for a block without a value in the normal range (its codes are 0).
+__device__ __forceinline__ float inverse(float top) {
+  return top < 1.17549435e-38f ? 0.0f : fdiv(1.0f, top);
+}
+
+__device__ __forceinline__ float root_approx(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// The code of y in [0, 1]: how many midpoints lie at or below it.  The midpoint
+// under code c of LEVELS is K (2c(c-1) + 1), K = 1/(2 LEVELS^2), halfway between
+// the neighbouring squares, and its square for FOURTH (v).  c - 1/2 is the
+// root of LEVELS^2 y - 1/4 there, so an approximate root, lowered by 1e-3 (its
+// error in c is below 2e-4), gives the code or the one before it, and the exact
+// midpoint decides: the result does not depend on the approximation.
+template <int LEVELS, bool FOURTH>
+__device__ __forceinline__ int encode(float y) {
+  constexpr float K = static_cast<float>(1.0 / (2.0 * LEVELS * LEVELS));
+  const float s = FOURTH ? root_approx(y) : y;
+  const float z = fmaxf(__fmaf_rn(s, static_cast<float>(LEVELS * LEVELS), -0.25f), 0.0f);
+  int c = min(static_cast<int>(fadd(root_approx(z), 0.499f)), LEVELS - 1);
+  float mid = fmul(static_cast<float>(2 * c * (c + 1) + 1), K);
+  if (FOURTH) mid = fmul(mid, mid);
+  return y >= mid ? c + 1 : c;
+}
+
+__device__ __forceinline__ float warp_max(float x) {  // x >= 0 or NaN
+  return __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(x)));
+}
+
+template <typename P, typename G, int BITS, int N>
+__global__ void __launch_bounds__(kThreads)
+    adamw_kernel(const __grid_constant__ Table<N> t, const Scalars k) {
+  pdl_begin();
+  float clip = 1.0f;
+  if (k.norm != nullptr) {
+    const float norm = *k.norm;
+    if (!(norm <= 3.402823466e38f)) return;  // not finite: the step is skipped
+    if (k.max_norm > 0.0f) clip = fminf(fdiv(k.max_norm, fadd(norm, 1e-6f)), 1.0f);
+  }
+  int c0, c1, at;
+  my_range(t, &c0, &c1, &at);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int c = c0; c < c1; ++c) {
+    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
+    const Entry& e = t.e[at];
+    const int64_t base = static_cast<int64_t>(c - e.first) * kChunk + warp * (32 * kLane);
+    if (base >= e.n) continue;
+    const int64_t i = base + lane * kLane;
+    const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+    const bool wide = e.wide;
+    float p[8], g[8], m[8], v[8];
+    load8(static_cast<const G*>(e.grad), i, left, wide, g);
+    load8(static_cast<const P*>(e.param), i, left, wide, p);
+    const int64_t block = base >> 8;
+    if (BITS == 32) {
+      load8(static_cast<const float*>(e.m), i, left, wide, m);
+      load8(static_cast<const float*>(e.v), i, left, wide, v);
+    } else {
+      const uint2 um = load_codes(e.m, i, left, wide), uv = load_codes(e.v, i, left, wide);
+      const float sm = e.sm[block], sv = e.sv[block];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = decode_m(j < 4 ? um.x : um.y, j & 3, sm);
+        v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float gj = fmul(g[j], clip);
+      m[j] = fadd(fmul(m[j], k.b1), fmul(gj, k.c1));
+      v[j] = fadd(fmul(v[j], k.b2), fmul(fmul(gj, k.c2), gj));
+      const float under = fadd(fmul(__fsqrt_rn(v[j]), k.rs), k.eps);
+      p[j] = fsub(fmul(p[j], e.keep), fmul(fdiv(m[j], under), e.step));
+    }
+    store8(static_cast<P*>(e.param), i, left, wide, p);
+    if (e.copy != nullptr) store8(static_cast<__nv_bfloat16*>(e.copy), i, left, wide, p);
+    if (BITS == 32) {
+      store8(static_cast<float*>(e.m), i, left, wide, m);
+      store8(static_cast<float*>(e.v), i, left, wide, v);
+    } else {
+      float tm = 0.0f, tv = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j >= left) m[j] = v[j] = 0.0f;
+        tm = fmaxf(tm, fabsf(m[j]));
+        tv = fmaxf(tv, v[j]);
+      }
+      tm = warp_max(tm);
+      tv = warp_max(tv);
+      const float im = inverse(tm), iv = inverse(tv);
+      uint2 um = make_uint2(0, 0), uv = make_uint2(0, 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        int cm = encode<127, false>(fmul(fabsf(m[j]), im));
+        if (m[j] < 0.0f) cm = -cm;
+        const float y = fmul(v[j], iv);
+        int cv = encode<255, true>(y);
+        if (y > 0.0f) cv = max(cv, 1);
+        (j < 4 ? um.x : um.y) |= static_cast<uint32_t>(cm & 0xff) << (8 * (j & 3));
+        (j < 4 ? uv.x : uv.y) |= static_cast<uint32_t>(cv) << (8 * (j & 3));
+      }
+      store_codes(e.m, i, left, wide, um);
+      store_codes(e.v, i, left, wide, uv);
+      if (lane == 0) {
+        e.sm[block] = tm;
+        e.sv[block] = tv;
+      }
+    }
+  }
+}
+
+// The values that 8-bit states stand for: param and copy of an entry are the
+// fp32 outputs of m and v here.
+template <int N>
+__global__ void __launch_bounds__(kThreads) adamw_decode_kernel(const __grid_constant__ Table<N> t) {
+  pdl_begin();
+  int c0, c1, at;
+  my_range(t, &c0, &c1, &at);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int c = c0; c < c1; ++c) {
+    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
+    const Entry& e = t.e[at];
+    const int64_t base = static_cast<int64_t>(c - e.first) * kChunk + warp * (32 * kLane);
+    if (base >= e.n) continue;
+    const int64_t i = base + lane * kLane;
+    const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+    const uint2 um = load_codes(e.m, i, left, e.wide), uv = load_codes(e.v, i, left, e.wide);
+    const float sm = e.sm[base >> 8], sv = e.sv[base >> 8];
+    float m[8], v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = decode_m(j < 4 ? um.x : um.y, j & 3, sm);
+      v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+    }
+    store8(static_cast<float*>(e.param), i, left, e.wide, m);
+    store8(static_cast<float*>(e.copy), i, left, e.wide, v);
+  }
+}
+
+// Sum of squares of this CTA's chunks: fp32 over the entries of a thread, then
+// fp64 over the CTA.  No atomics: the sum depends on the grid alone.
+template <typename G, int N>
+__global__ void __launch_bounds__(kThreads)
+    grad_square_kernel(const __grid_constant__ Table<N> t, double* part) {
+  pdl_begin();
+  int c0, c1, at;
+  my_range(t, &c0, &c1, &at);
+  float sum = 0.0f;
+  for (int c = c0; c < c1; ++c) {
+    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
+    const Entry& e = t.e[at];
+    const int64_t i = static_cast<int64_t>(c - e.first) * kChunk + threadIdx.x * kLane;
+    if (i >= e.n) continue;
+    float g[8];
+    load8(static_cast<const G*>(e.grad), i, static_cast<int>(min64(e.n - i, kLane)), e.wide, g);
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
+    sum = fadd(sum, s);
+  }
+  __shared__ double warp_sum[kThreads / 32];
+  double d = sum;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = d;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 32; ++w) d += warp_sum[w];
+    part[blockIdx.x] = d;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part, int n, float* norm) {
+  pdl_begin();
+  double d = 0.0;
+  for (int i = threadIdx.x; i < n; i += kThreads) d += part[i];
+  __shared__ double warp_sum[kThreads / 32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = d;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kThreads / 32; ++w) d += warp_sum[w];
+    *norm = static_cast<float>(sqrt(d));
+  }
+}
+
+bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// CTAs of a launch over `chunks` chunks: as many as are resident, so that every
+// CTA takes one contiguous range.
+template <typename K>
+int grid_of(K kernel, int chunks, int num_sms) {
+  const int64_t full = static_cast<int64_t>(num_sms) * resident_blocks(kernel, kThreads, 0);
+  return static_cast<int>(std::min<int64_t>(chunks, full));
+}
+
+// Calls fn(table) for the list in as few tables as it takes.
+template <typename Fn>
+cudaError_t for_tables(const Entry* list, int64_t count, Fn fn) {
+  int64_t i = 0;
+  while (i < count) {
+    Table<kLargeTable> big;
+    big.count = 0;
+    int64_t chunks = 0;
+    for (; i < count && big.count < kLargeTable; ++i) {
+      if (list[i].n == 0) continue;
+      const int64_t c = (list[i].n + kChunk - 1) / kChunk;
+      if (chunks + c > 0x7fffffff) {
+        if (big.count > 0) break;
+        return cudaErrorInvalidValue;  // a tensor of 2^42 entries
+      }
+      big.e[big.count] = list[i];
+      big.e[big.count++].first = static_cast<int>(chunks);
+      chunks += c;
+    }
+    if (big.count == 0) break;
+    big.chunks = static_cast<int>(chunks);
+    cudaError_t e;
+    if (big.count <= kSmallTable) {
+      Table<kSmallTable> small;
+      std::copy(big.e, big.e + big.count, small.e);
+      small.count = big.count;
+      small.chunks = big.chunks;
+      e = fn(small);
+    } else {
+      e = fn(big);
+    }
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+template <typename P, typename G, int BITS>
+cudaError_t step_tables(const Entry* list, int64_t count, const Scalars& k, int num_sms, cudaStream_t s) {
+  return for_tables(list, count, [&](const auto& t) {
+    constexpr int N = sizeof(t.e) / sizeof(Entry);
+    auto kernel = adamw_kernel<P, G, BITS, N>;
+    return launch_kernel(kernel, dim3(grid_of(kernel, t.chunks, num_sms)), dim3(kThreads), 0, s, 0, t, k);
+  });
+}
+
+}  // namespace
+
+cudaError_t launch_adamw(const AdamwArgs& a, int num_sms, cudaStream_t s) {
+  Scalars k;
+  k.b1 = static_cast<float>(a.beta1);
+  k.c1 = static_cast<float>(1.0 - a.beta1);
+  k.b2 = static_cast<float>(a.beta2);
+  k.c2 = static_cast<float>(1.0 - a.beta2);
+  k.rs = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(a.beta2, static_cast<double>(a.step))));
+  k.eps = static_cast<float>(a.eps);
+  k.norm = a.grad_norm;
+  k.max_norm = static_cast<float>(a.max_norm);
+  const double rate = a.lr / (1.0 - std::pow(a.beta1, static_cast<double>(a.step)));
+  constexpr int kBatch = 4 * kLargeTable;
+  Entry list[kBatch];
+  for (int64_t i0 = 0; i0 < a.count; i0 += kBatch) {
+    const int64_t n = std::min<int64_t>(kBatch, a.count - i0);
+    for (int64_t i = 0; i < n; ++i) {
+      const mpc_adamw_tensor& t = a.tensors[i0 + i];
+      list[i] = Entry{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.scale_m, t.scale_v, t.copy, t.n,
+                      static_cast<float>(1.0 - a.lr * t.lr_scale * t.weight_decay),
+                      static_cast<float>(rate * t.lr_scale), 0,
+                      on16(t.param) && on16(t.grad) && on16(t.exp_avg) && on16(t.exp_avg_sq) && on16(t.copy)};
+    }
+    cudaError_t e;
+    using b16 = __nv_bfloat16;
+    if (a.state_bits == 32) {
+      if (a.param_bf16) e = a.grad_bf16 ? step_tables<b16, b16, 32>(list, n, k, num_sms, s) : step_tables<b16, float, 32>(list, n, k, num_sms, s);
+      else e = a.grad_bf16 ? step_tables<float, b16, 32>(list, n, k, num_sms, s) : step_tables<float, float, 32>(list, n, k, num_sms, s);
+    } else {
+      if (a.param_bf16) e = a.grad_bf16 ? step_tables<b16, b16, 8>(list, n, k, num_sms, s) : step_tables<b16, float, 8>(list, n, k, num_sms, s);
+      else e = a.grad_bf16 ? step_tables<float, b16, 8>(list, n, k, num_sms, s) : step_tables<float, float, 8>(list, n, k, num_sms, s);
+    }
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_adamw_decode(const mpc_adamw_tensor* tensors, int64_t count, float* const* m_out,
+                                float* const* v_out, int num_sms, cudaStream_t s) {
+  constexpr int kBatch = 4 * kLargeTable;
+  Entry list[kBatch];
+  for (int64_t i0 = 0; i0 < count; i0 += kBatch) {
+    const int64_t n = std::min<int64_t>(kBatch, count - i0);
+    for (int64_t i = 0; i < n; ++i) {
+      const mpc_adamw_tensor& t = tensors[i0 + i];
+      float* mo = m_out[i0 + i];
+      float* vo = v_out[i0 + i];
+      list[i] = Entry{mo, nullptr, t.exp_avg, t.exp_avg_sq, t.scale_m, t.scale_v, vo, t.n, 0.0f, 0.0f, 0,
+                      on16(mo) && on16(vo) && on16(t.exp_avg) && on16(t.exp_avg_sq)};
+    }
+    const cudaError_t e = for_tables(list, n, [&](const auto& t) {
+      constexpr int N = sizeof(t.e) / sizeof(Entry);
+      auto kernel = adamw_decode_kernel<N>;
+      return launch_kernel(kernel, dim3(grid_of(kernel, t.chunks, num_sms)), dim3(kThreads), 0, s, 0, t);
+    });
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+// The partial sums take one fp64 value a CTA; every table of a long list (see
+// for_tables) has its own kNormGrid of them.
+constexpr int kNormGrid = 2048;
+
+size_t grad_norm_workspace_bytes(int64_t count) {
+  const int64_t tables = std::max<int64_t>(1, 2 * (count / kLargeTable + 1));
+  return static_cast<size_t>(tables) * kNormGrid * sizeof(double);
+}
+
+cudaError_t launch_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, int grad_bf16, float* norm,
+                             double* part, int num_sms, cudaStream_t s) {
+  constexpr int kBatch = 4 * kLargeTable;
+  Entry list[kBatch];
+  int used = 0;
+  for (int64_t i0 = 0; i0 < count; i0 += kBatch) {
+    const int64_t n = std::min<int64_t>(kBatch, count - i0);
+    for (int64_t i = 0; i < n; ++i) {
+      const mpc_adamw_tensor& t = tensors[i0 + i];
+      list[i] = Entry{};
+      list[i].grad = t.grad;
+      list[i].n = t.n;
+      list[i].wide = on16(t.grad);
+    }
+    auto launch = [&](auto type) {
+      using G = decltype(type);
+      return for_tables(list, n, [&](const auto& t) {
+        constexpr int N = sizeof(t.e) / sizeof(Entry);
+        auto kernel = grad_square_kernel<G, N>;
+        const int grid = std::min(kNormGrid, grid_of(kernel, t.chunks, num_sms));
+        const cudaError_t e = launch_kernel(kernel, dim3(grid), dim3(kThreads), 0, s, 0, t, part + used);
+        used += grid;
+        return e;
+      });
+    };
+    const cudaError_t e = grad_bf16 ? launch(__nv_bfloat16{}) : launch(float{});
+    if (e != cudaSuccess) return e;
+  }
+  return launch_kernel(grad_norm_kernel, dim3(1), dim3(kThreads), 0, s, 0, part, used, norm);
+}
+
+}  // namespace mpc

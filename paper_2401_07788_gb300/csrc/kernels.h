@@ -6,6 +6,8 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "mpcomp.h"
+
 namespace mpc {
 
 // Which fused variant of the TopK selection a launch runs.
@@ -119,5 +121,48 @@ cudaError_t launch_quant_decompress(const uint32_t* codes, const float* scale,
                                     const float* minv, int64_t rows, int64_t L, int bits,
                                     int64_t W, float* y, int aligned, int num_sms,
                                     cudaStream_t s);
+
+// AdamW over a list of tensors and the norm of their gradients (adamw.cu); the
+// lists are host memory.
+struct AdamwArgs {
+  const mpc_adamw_tensor* tensors;
+  int64_t count;
+  int param_bf16, grad_bf16, state_bits;
+  double lr, beta1, beta2, eps;
+  int64_t step;
+  const float* grad_norm;  // device, or nullptr
+  double max_norm;
+};
+cudaError_t launch_adamw(const AdamwArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_adamw_decode(const mpc_adamw_tensor* tensors, int64_t count, float* const* m_out,
+                                float* const* v_out, int num_sms, cudaStream_t s);
+size_t grad_norm_workspace_bytes(int64_t count);
+cudaError_t launch_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, int grad_bf16, float* norm,
+                             double* part, int num_sms, cudaStream_t s);
+
+// Linear cross entropy (linear_ce.cu): the loss when `loss` is given, the
+// gradients when `dh` and `dw` are (from `lse_in` when the loss is not formed).
+struct LinearCeArgs {
+  const void* h;
+  const void* w;
+  int64_t ldh, ldw;
+  const int64_t* targets;
+  int64_t T, D, V;
+  int bf16;
+  int64_t ignore;
+  float* loss;
+  float* lse;
+  const float* lse_in;
+  const float* gloss;
+  void* dh;
+  void* dw;
+  int64_t lddh, lddw;
+  int64_t piece;
+  void* ws;
+  uint32_t spin_limit;
+  unsigned* status;
+};
+size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int grad, int64_t piece);
+cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s);
 
 }  // namespace mpc

@@ -1,0 +1,285 @@
+"""The two ends of a stage's training step that lie outside its layers: the last stage's loss over
+the vocabulary, and the optimiser step that every stage makes after its backward pass.
+
+* ``linear_cross_entropy`` / ``LinearCrossEntropy``: softmax cross entropy of a linear head
+  without its logits; the gradient of the hidden states is what the boundary before the last
+  stage compresses.
+* ``AdamWPlan``: the list of tensors that ``mpc_adamw_step``, ``mpc_grad_norm`` and
+  ``mpc_adamw_decode`` take, laid out once.
+* ``AdamW``: a ``torch.optim.Optimizer`` on these calls, with fp32 or 8-bit states, bf16 copies of
+  fp32 weights and clipping by the global norm.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import (MpcError, _DTYPES, _cuda, _dtype, mpc_adamw_step, mpc_grad_norm,
+               mpc_linear_ce_backward, mpc_linear_ce_forward, mpc_linear_ce_train)
+
+__all__ = ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
+
+BLOCK = 256  # entries of a tensor that share a scale in the 8-bit states
+
+
+# ---------------------------------------------------------------------------------------
+# Linear cross entropy
+# ---------------------------------------------------------------------------------------
+
+class _LinearCeFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, w, targets, ignore_index):
+        loss, lse = mpc_linear_ce_forward(h, w, targets, ignore_index)
+        ctx.save_for_backward(h, w, targets, lse)
+        ctx.ignore_index = ignore_index
+        return loss
+
+    @staticmethod
+    def backward(ctx, gloss):
+        h, w, targets, lse = ctx.saved_tensors
+        dh, dw = mpc_linear_ce_backward(h, w, targets, lse, gloss.contiguous().float(),
+                                        ctx.ignore_index)
+        return dh, dw, None, None
+
+
+class _LinearCeMeanFn(torch.autograd.Function):
+    """The mean: its gradient is known up to one factor when the loss is formed, so both come from
+    one call and the backward pass only applies the factor."""
+
+    @staticmethod
+    def forward(ctx, h, w, targets, ignore_index):
+        loss, dh, dw = mpc_linear_ce_train(h, w, targets, None, ignore_index)
+        ctx.save_for_backward(dh, dw)
+        count = (targets != ignore_index).sum().clamp_min(1)
+        return loss.sum() / count
+
+    @staticmethod
+    def backward(ctx, g):
+        dh, dw = ctx.saved_tensors
+        return dh * g.to(dh.dtype), dw * g.to(dw.dtype), None, None
+
+
+def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean"):
+    """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
+    ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
+    where the target is ``ignore_index``)."""
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError("reduction must be mean, sum or none")
+    rows, y = h.reshape(-1, h.shape[-1]), targets.reshape(-1)
+    grad = torch.is_grad_enabled() and (h.requires_grad or w.requires_grad)
+    if reduction == "mean":
+        if grad:
+            return _LinearCeMeanFn.apply(rows, w, y, ignore_index)
+        loss = mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
+        return loss.sum() / (y != ignore_index).sum().clamp_min(1)
+    loss = _LinearCeFn.apply(rows, w, y, ignore_index) if grad else \
+        mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
+    return loss.sum() if reduction == "sum" else loss.reshape(targets.shape)
+
+
+class LinearCrossEntropy(torch.nn.Module):
+    """The head of a last stage: a weight [vocab, hidden] and the loss of its logits."""
+
+    def __init__(self, hidden: int, vocab: int, ignore_index: int = -100, reduction: str = "mean",
+                 device=None, dtype=None):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(vocab, hidden, device=device, dtype=dtype))
+        torch.nn.init.normal_(self.weight, std=0.02)
+        self.ignore_index = int(ignore_index)
+        self.reduction = reduction
+
+    def forward(self, h: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
+        return linear_cross_entropy(h, self.weight, targets, self.ignore_index, self.reduction)
+
+
+# ---------------------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------------------
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("scale_m", ctypes.c_void_p),
+                ("scale_v", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("lr_scale", ctypes.c_double), ("weight_decay", ctypes.c_double)]
+
+
+class AdamWPlan:
+    """The tensors of an optimiser step: params (float32, or bfloat16 without a master copy),
+    grads, and the states m and v, each a list with one contiguous CUDA tensor for each param.
+
+    States are fp32, or 8-bit codes (m int8, v uint8) with ``m_scale`` and ``v_scale`` (fp32, one
+    for each block of 256 entries).  ``m`` None allocates zero states of ``state_bits``.  ``copies``
+    (bfloat16, entries may be None) receive the new params as well.  ``weight_decay`` and
+    ``lr_scale`` are one number or one for each tensor.
+    """
+
+    def __init__(self, params, grads, m=None, v=None, m_scale=None, v_scale=None, copies=None,
+                 weight_decay=0.0, lr_scale=1.0, state_bits: int = 32):
+        params, grads = list(params), list(grads)
+        n = len(params)
+        if n == 0:
+            raise MpcError(1, "a plan needs at least one tensor")
+        if (m is None) != (v is None):
+            raise MpcError(1, "m and v are given together")
+        self.device = params[0].device
+        self.sizes = [p.numel() for p in params]
+        blocks = [-(-k // BLOCK) for k in self.sizes]
+        if m is None:
+            if state_bits not in (32, 8):
+                raise MpcError(1, "state_bits must be 32 or 8")
+            kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8)
+            m, v = ([torch.zeros(k, dtype=t, device=self.device) for k in self.sizes] for t in kinds)
+            if state_bits == 8:
+                m_scale, v_scale = ([torch.zeros(b, device=self.device) for b in blocks]
+                                    for _ in range(2))
+        m, v = list(m), list(v)
+        self.state_bits = 8 if m and m[0].dtype == torch.int8 else 32
+        self.param_type, self.grad_type = _dtype(params[0], "param"), _dtype(grads[0], "grad") if grads else 0
+        kinds = {"param": params[0].dtype, "grad": grads[0].dtype if grads else None}
+        lists = {"param": params, "grad": grads, "m": m, "v": v}
+        if self.state_bits == 8:
+            if m_scale is None or v_scale is None:
+                raise MpcError(1, "8-bit states need m_scale and v_scale")
+            lists.update(m_scale=list(m_scale), v_scale=list(v_scale))
+            kinds.update(m=torch.int8, v=torch.uint8, m_scale=torch.float32, v_scale=torch.float32)
+        else:
+            kinds.update(m=torch.float32, v=torch.float32)
+        for name, tensors in lists.items():
+            if len(tensors) != n:
+                raise MpcError(1, "%d params but %d entries of %s" % (n, len(tensors), name))
+            for t, k in zip(tensors, blocks if name.endswith("scale") else self.sizes):
+                self._check(t, kinds[name], name, k)
+        copies = [None] * n if copies is None else list(copies)
+        if len(copies) != n:
+            raise MpcError(1, "%d params but %d copies" % (n, len(copies)))
+        for t, k in zip(copies, self.sizes):
+            if t is not None:
+                self._check(t, torch.bfloat16, "copy", k)
+        self.params, self.m, self.v, self.copies = params, m, v, copies
+        self.m_scale, self.v_scale = lists.get("m_scale"), lists.get("v_scale")
+        self.count = n
+        self.table = (_Tensor * n)()
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        scale = [float(lr_scale)] * n if isinstance(lr_scale, (int, float)) else list(lr_scale)
+        if len(decay) != n or len(scale) != n:
+            raise MpcError(1, "weight_decay and lr_scale are one number or one for each tensor")
+        for i, e in enumerate(self.table):
+            e.param, e.exp_avg, e.exp_avg_sq = params[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr()
+            if self.state_bits == 8:
+                e.scale_m, e.scale_v = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
+            e.copy = None if copies[i] is None else copies[i].data_ptr()
+            e.n, e.lr_scale, e.weight_decay = self.sizes[i], scale[i], decay[i]
+        self.grads = [None] * n
+        self.set_grads(grads)
+
+    def _check(self, t, dtype, name, n):
+        _cuda(t, dtype, name)
+        if t.numel() != n or t.device != self.device:
+            raise MpcError(1, "%s must hold %d entries on %s" % (name, n, self.device))
+
+    def set_grads(self, grads) -> None:
+        """Other gradient tensors for the next calls, e.g. those of a new backward pass."""
+        if len(grads) != self.count:
+            raise MpcError(1, "%d params but %d grads" % (self.count, len(grads)))
+        dtype = torch.bfloat16 if self.grad_type else torch.float32
+        for i, g in enumerate(grads):
+            self._check(g, dtype, "grad", self.sizes[i])
+        for i, g in enumerate(grads):
+            self.table[i].grad = g.data_ptr()
+        self.grads = list(grads)
+
+    def set_group(self, i: int, lr_scale: float, weight_decay: float) -> None:
+        """The factor on lr and the weight decay of tensor i from the next step on."""
+        self.table[i].lr_scale, self.table[i].weight_decay = lr_scale, weight_decay
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW in one launch for all tensors of a type (and one more pass over the gradients when
+    ``max_norm`` is set, which clips by the norm of all of them and leaves out a step whose norm is
+    not finite).
+
+    ``state_bits``: 32, or 8 for states in blocks of 256 codes.  ``copies``: {param: bfloat16 tensor}
+    that receives the param's new values, for a forward pass in bf16 from fp32 weights.
+    Parameters without a gradient are left alone, as are their states.
+    """
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 1e-2, state_bits: int = 32, max_norm: float = 0.0, copies=None):
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        if not 0.0 <= betas[0] < 1.0 or not 0.0 <= betas[1] < 1.0 or eps < 0.0 or lr < 0.0:
+            raise ValueError("lr, betas or eps out of range")
+        super().__init__(params, {"lr": lr, "betas": betas, "eps": eps, "weight_decay": weight_decay})
+        self.state_bits, self.max_norm = state_bits, max_norm
+        self.copies = {} if copies is None else dict(copies)
+        self._plans = {}
+        self.last_norm = None  # device fp32 of one entry, when max_norm is set
+
+    def _state(self, p):
+        s = self.state[p]
+        if "exp_avg" not in s:
+            n = p.numel()
+            low = self.state_bits == 8
+            s["step"] = 0
+            s["exp_avg"] = torch.zeros(n, dtype=torch.int8 if low else torch.float32, device=p.device)
+            s["exp_avg_sq"] = torch.zeros(n, dtype=torch.uint8 if low else torch.float32, device=p.device)
+            if low:
+                s["scale_m"] = torch.zeros(-(-n // BLOCK), device=p.device)
+                s["scale_v"] = torch.zeros(-(-n // BLOCK), device=p.device)
+        return s
+
+    def load_state_dict(self, state_dict):
+        """Restores the states in the types they were saved in (the codes of 8-bit states are not
+        numbers to be cast to the parameter's type)."""
+        super().load_state_dict(state_dict)
+        flat = [p for g in self.param_groups for p in g["params"]]
+        saved = [i for g in state_dict["param_groups"] for i in g["params"]]
+        for p, i in zip(flat, saved):
+            for k, x in state_dict["state"].get(i, {}).items():
+                self.state[p][k] = x.to(p.device).clone() if isinstance(x, torch.Tensor) else x
+        self._plans = {}
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        lists = {}
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                s = self._state(p)
+                s["step"] += 1
+                key = (p.dtype, p.grad.dtype, p.device, s["step"], tuple(group["betas"]), group["eps"])
+                lists.setdefault(key, []).append((p, s, group))
+        plans = []
+        for key, entries in lists.items():
+            ident = (key[0], key[1], key[2], tuple(id(p) for p, _, _ in entries))
+            plan = self._plans.get(ident)
+            grads = [p.grad for p, _, _ in entries]
+            if plan is None or any(a.data_ptr() != p.data_ptr() for a, (p, _, _) in zip(plan.params, entries)):
+                low = self.state_bits == 8
+                plan = AdamWPlan([p.detach() for p, _, _ in entries], grads,
+                                 [s["exp_avg"] for _, s, _ in entries],
+                                 [s["exp_avg_sq"] for _, s, _ in entries],
+                                 [s["scale_m"] for _, s, _ in entries] if low else None,
+                                 [s["scale_v"] for _, s, _ in entries] if low else None,
+                                 [self.copies.get(p) for p, _, _ in entries])
+                self._plans[ident] = plan
+            else:
+                plan.set_grads(grads)
+            for i, (_, _, group) in enumerate(entries):
+                plan.set_group(i, group["lr"], group["weight_decay"])
+            plans.append((key, plan))
+        norm = None
+        if self.max_norm > 0.0 and plans:
+            norms = [mpc_grad_norm(plan) for _, plan in plans]
+            norm = norms[0] if len(norms) == 1 else torch.linalg.vector_norm(torch.cat(norms)).view(1)
+            self.last_norm = norm
+        for (_, _, _, step, betas, eps), plan in plans:
+            mpc_adamw_step(plan, 1.0, betas[0], betas[1], eps, step, grad_norm=norm, max_norm=self.max_norm)
+        return loss
