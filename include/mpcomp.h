@@ -307,12 +307,16 @@ typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
  *           token does not count either.
  *   loss, lse  [tokens] fp32, out.
  *   ws      workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
- *           hidden, vocab, type, 0, 0), 256-byte aligned.
+ *           hidden, vocab, type, 0, 0, ldw), 256-byte aligned.  The query takes
+ *           ldw because the matrix units read a bf16 w in place when its rows
+ *           start on 16 bytes; it is copied into the workspace otherwise (pass
+ *           ldw = 0 when w itself is not 16-byte aligned), as an fp32 w always
+ *           is, split into three bf16 terms.
  * Products are summed in fp32 and fp32 inputs are not rounded to a narrower
  * type.  tokens = 0 is a no-op.  Requires hidden >= 1, 1 <= vocab <= 2^31-1,
  * tokens <= 2^31-1. */
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
-                                     int grad, int64_t piece);
+                                     int grad, int64_t piece, int64_t ldw);
 mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
                                  const int64_t* targets, int64_t tokens, int64_t hidden,
                                  int64_t vocab, mpc_dtype type, int64_t ignore_index, float* loss,
@@ -328,7 +332,7 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
  *   piece  vocabulary entries whose c is in the workspace at a time; 0 lets the
  *          library choose (1 GiB of c at most).
  *   ws     workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
- *          hidden, vocab, type, 1, piece), 256-byte aligned.
+ *          hidden, vocab, type, 1, piece, ldw), 256-byte aligned.
  * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
  * tokens = 0 writes dw = 0. */
 mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,

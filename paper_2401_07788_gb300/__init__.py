@@ -71,7 +71,7 @@ _SIGNATURES = {
                                    _INT),
     "mpc_quant_compress_noalloc": ([_VP, _I64, _I64, _INT, _INT, _U64, _VP, _VP, _VP, _VP],
                                    _INT),
-    "mpc_linear_ce_workspace_bytes": ([_I64, _I64, _I64, _INT, _INT, _I64], _SZ),
+    "mpc_linear_ce_workspace_bytes": ([_I64, _I64, _I64, _INT, _INT, _I64, _I64], _SZ),
     "mpc_linear_ce_forward": ([_VP, _I64, _VP, _I64, _VP, _I64, _I64, _I64, _INT, _I64, _VP, _VP,
                                _VP, _SZ, _VP], _INT),
     "mpc_linear_ce_backward": ([_VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _I64, _I64, _INT, _I64,
@@ -459,8 +459,11 @@ def _vector(t, n: int, dtype: torch.dtype, name: str, device):
 
 
 def mpc_linear_ce_workspace_bytes(tokens: int, hidden: int, vocab: int, dtype=torch.float32,
-                                  grad: bool = False, piece: int = 0) -> int:
-    return int(lib().mpc_linear_ce_workspace_bytes(tokens, hidden, vocab, _DTYPES[dtype], grad, piece))
+                                  grad: bool = False, piece: int = 0, ldw: int | None = None) -> int:
+    """Bytes of workspace; ldw: the distance of w's rows (hidden when None, 0 for a w that is not
+    16-byte aligned)."""
+    return int(lib().mpc_linear_ce_workspace_bytes(tokens, hidden, vocab, _DTYPES[dtype], grad, piece,
+                                                   hidden if ldw is None else ldw))
 
 
 def _linear_ce_args(h, w, targets, ignore_index, grad, piece, ws, stream):
@@ -471,7 +474,8 @@ def _linear_ce_args(h, w, targets, ignore_index, grad, piece, ws, stream):
     ldw = _matrix(w, "w", D, h)
     V = w.shape[0]
     _vector(targets, T, torch.int64, "targets", h.device)
-    need = mpc_linear_ce_workspace_bytes(T, D, V, h.dtype, grad, piece)
+    need = mpc_linear_ce_workspace_bytes(T, D, V, h.dtype, grad, piece,
+                                         0 if w.data_ptr() % 16 else ldw)
     given = ws
     ws, wsb = _workspace(need, ws, h.device)
     if given is None:

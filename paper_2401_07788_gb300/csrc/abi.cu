@@ -629,7 +629,8 @@ mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size
   if (grad) MPC_TRY(check_matrix(a.dh, a.T, a.D, a.lddh, type, "dh"));
   MPC_TRY(check_ptr(a.targets, 8, "targets"));
   if (a.gloss != nullptr) MPC_TRY(check_ptr(a.gloss, 4, "gloss"));
-  const size_t need = mpc_linear_ce_workspace_bytes(a.T, a.D, a.V, type, grad, a.piece);
+  const size_t need = mpc_linear_ce_workspace_bytes(a.T, a.D, a.V, type, grad, a.piece,
+                                                    aligned_to(a.w, 16) ? a.ldw : 0);
   if (a.ws == nullptr || ws_bytes < need)
     return set_error(MPC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
                      a.ws == nullptr ? (size_t)0 : ws_bytes);
@@ -646,9 +647,9 @@ mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size
 }  // namespace
 
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
-                                     int grad, int64_t piece) {
+                                     int grad, int64_t piece, int64_t ldw) {
   if (tokens == 0 || !linear_ce_sizes_ok(tokens, hidden, vocab, piece)) return 0;
-  return mpc::linear_ce_workspace_bytes(tokens, hidden, vocab, type == MPC_BF16, grad, piece);
+  return mpc::linear_ce_workspace_bytes(tokens, hidden, vocab, type == MPC_BF16, grad, piece, ldw);
 }
 
 mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
