@@ -21,12 +21,13 @@
 namespace mpc {
 namespace {
 
-constexpr int kM = 128;        // rows of an output tile (lanes of tensor memory)
+constexpr int kM = 128;        // rows of a CTA's output tile (lanes of tensor memory)
+constexpr int kPair = 2 * kM;  // rows of a CTA pair's output tile
 constexpr int kN = 256;        // columns of an output tile
 constexpr int kK = 64;         // K elements of a stage: 128 bytes, one swizzle row
-constexpr int kStages = 4;
+constexpr int kStages = 6;
 constexpr int kBytesA = kM * kK * 2;
-constexpr int kBytesB = kN * kK * 2;
+constexpr int kBytesB = kN / 2 * kK * 2;
 constexpr int kStageBytes = kBytesA + kBytesB;
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(256)
                    int64_t padded, int D, int Dp, uint16_t* __restrict__ out) {
   pdl_begin();
   const int64_t n = count != nullptr ? *count : rows;
-  const int64_t need = min64((n + kM - 1) / kM * kM, padded);  // rows that a product may touch
+  const int64_t need = min64((n + kPair - 1) / kPair * kPair, padded);  // rows that a product may touch
   const int groups = Dp / 8;
   const int64_t plane = padded * Dp;
   for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < need * groups; q += gridDim.x * int64_t{256}) {
@@ -149,11 +150,14 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------------------
-// The matrix products: C[m][n] = sum_k A[m][k] B[n][k] in 128 x 256 tiles.
+// The matrix products: C[m][n] = sum_k A[m][k] B[n][k] in 256 x 256 tiles.
 //
-// A persistent CTA per SM: warp 0 copies operand tiles to shared memory through
-// tensor maps (kStages stages of 48 KB), one thread of warp 1 issues the
-// products, eight warps take the finished tile from tensor memory.  Two
+// A persistent pair of CTAs on two SMs per tile, 128 rows each: every CTA copies
+// its rows of A and half the rows of B, so an SM reads 32 KB from L2 for 2^20
+// products (48 KB with a tile of its own).  Warp 0 copies operand tiles through
+// tensor maps (kStages stages of 32 KB a CTA), one thread of the first CTA's warp
+// 1 issues the products of both, eight warps a CTA take the finished tile from
+// tensor memory.  Two
 // accumulators of 256 columns fill the tensor memory, so a tile's epilogue runs
 // under the next tile's products.
 //
@@ -227,7 +231,7 @@ __device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
   const int m = MODE == kDw ? g.width : valid;
   const int n = MODE == kDh || MODE == kDw ? g.D : g.width;
   const int k = MODE == kDh ? g.width : MODE == kDw ? valid : g.D;
-  s.m_tiles = (m + kM - 1) / kM;
+  s.m_tiles = (m + kPair - 1) / kPair;
   s.n_tiles = (n + kN - 1) / kN;
   s.blocks = (k + kK - 1) / kK;
   s.splits = MODE == kDh ? g.splits : 1;
@@ -241,13 +245,13 @@ template <int MODE>
 __device__ __forceinline__ Tile tile_of(const Shape& s, int i) {
   Tile t;
   if (MODE == kLoss || MODE == kCoef) {
-    t.m0 = i % s.m_tiles * kM;
+    t.m0 = i % s.m_tiles * kPair;
     t.n0 = i / s.m_tiles * kN;
     t.split = 0;
   } else {
     t.n0 = i % s.n_tiles * kN;
     i /= s.n_tiles;
-    t.m0 = i % s.m_tiles * kM;
+    t.m0 = i % s.m_tiles * kPair;
     t.split = i / s.m_tiles;
   }
   t.k0 = static_cast<int>(static_cast<int64_t>(s.blocks) * t.split / s.splits);
@@ -399,16 +403,22 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
   }
 }
 
+// Columns of a tile that the product forms: a multiple of 16.  Each CTA of the
+// pair holds half of them as rows of B.
+__device__ __forceinline__ int tile_cols(int cols, int n0) { return min((cols - n0 + 15) / 16 * 16, kN); }
+
 template <int MODE>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ Gemm g) {
   constexpr bool A_MN = MODE == kDw, B_MN = MODE == kDh || MODE == kDw;
   extern __shared__ uint8_t raw[];
+  // full and taken are used in the first CTA, for both; empty and done in each
   __shared__ uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
   __shared__ uint32_t tmem;
   uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_rank());
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&full[i], 1);
@@ -416,7 +426,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&done[i], 1);
-      mbar_init(&taken[i], kEpiWarps);
+      mbar_init(&taken[i], 2 * kEpiWarps);
     }
     mbar_init(&drain, 1);
     fence_mbar_init();
@@ -426,20 +436,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (warp == 1) tmem_alloc(&tmem, 512);
   tc_fence_before();
   __syncthreads();
+  cluster_sync();
   tc_fence_after();
   const uint32_t acc = tmem;
   pdl_begin();
   const int valid = g.head->valid;
   const Shape s = shape_of<MODE>(g, valid);
   const int total = s.total();
+  const int cols = MODE == kDh || MODE == kDw ? g.D : g.width;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (warp == 0) {
     if (lane == 0) {
       fence_proxy_async_all();  // operands that earlier kernels wrote
       uint32_t it = 0;
       bool ok = true;
-      for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
+      for (int i = pair; i < total && ok; i += pairs) {
         const Tile t = tile_of<MODE>(s, i);
+        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(cols, t.n0) / 2);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk) {
           const int blocks = min(g.chunk, t.k1 - c);
           for (int j = 0; j < blocks * g.terms; ++j, ++it) {
@@ -451,35 +465,43 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             term_planes(g.terms, j / blocks, &pa, &pb);
             uint8_t* a = stage0 + st * kStageBytes;
             uint8_t* b = a + kBytesA;
-            mbar_arrive_expect_tx(&full[st], kStageBytes);
+            const uint32_t bar = dsmem_addr(&full[st], 0);
+            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kStageBytes);
             if (A_MN) {
 #pragma unroll
-              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, t.m0 + q * 64, kb * kK, pa, &full[st]);
+              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, pa, bar);
             } else {
-              tensor_g2s(a, &map_a, kb * kK, t.m0, pa, &full[st]);
+              tensor_g2s(a, &map_a, kb * kK, m0, pa, bar);
             }
             if (B_MN) {
               const int k_at = kb * kK + (MODE == kDh ? static_cast<int>(g.v0) : 0);
 #pragma unroll
-              for (int q = 0; q < kN / 64; ++q) tensor_g2s(b + q * kK * 128, &map_b, t.n0 + q * 64, k_at, pb, &full[st]);
+              for (int q = 0; q < kN / 128; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
             } else {
-              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + t.n0, pb, &full[st]);
+              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, pb, bar);
             }
           }
         }
       }
-      // copies in flight must land before the CTA may leave (at once unless a wait gave up)
-      for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-        mbar_wait_bounded(&full[i % kStages], i / kStages & 1, kDrainPolls, g.status);
+      // Copies in flight must land before either CTA leaves (the cluster barrier
+      // below).  The first CTA sees both CTAs' copies arrive; where a wait gave up,
+      // the second one may have sent some that the first no longer counts, and
+      // gives them a millisecond.
+      if (rank == 0) {
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+          mbar_wait_bounded(&full[i % kStages], i / kStages & 1, kDrainPolls, g.status);
+      } else if (!ok) {
+        const uint64_t until = global_ns() + 1000000;
+        while (global_ns() < until) __nanosleep(1000);
+      }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       uint32_t it = 0, n = 0;
       bool ok = true;
-      for (int i = blockIdx.x; i < total && ok; i += gridDim.x) {
+      for (int i = pair; i < total && ok; i += pairs) {
         const Tile t = tile_of<MODE>(s, i);
-        const int cols = MODE == kDh || MODE == kDw ? g.D : g.width;
-        const uint32_t idesc = mma_desc(kM, min((cols - t.n0 + 15) / 16 * 16, kN), A_MN, B_MN);
+        const uint32_t idesc = mma_desc(kPair, tile_cols(cols, t.n0), A_MN, B_MN);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
           ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
           tc_fence_after();
@@ -500,9 +522,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
               mma_bf16(d, da, db, idesc, fresh);
               fresh = false;
             }
-            mma_commit(&empty[st]);
+            mma_commit_pair(&empty[st]);
           }
-          if (ok) mma_commit(&done[n & 1]);
+          if (ok) mma_commit_pair(&done[n & 1]);
         }
       }
       if (!ok) {  // products in flight must end before the tensor memory is given back
@@ -514,7 +536,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const int quad = warp & 3, half = (warp - 2) >> 2;
     uint32_t n = 0;
     bool ok = true;
-    for (int i = blockIdx.x; i < total; i += gridDim.x) {
+    for (int i = pair; i < total; i += pairs) {
       const Tile t = tile_of<MODE>(s, i);
       float x[kHalf];
 #pragma unroll
@@ -539,15 +561,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&taken[n & 1]);
+        if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
       }
       if (!ok) break;
-      epilogue<MODE>(g, valid, t, t.m0 + quad * 32 + lane, t.n0 + half * kHalf, x);
+      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x);
     }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  cluster_sync();  // nothing signals or reads the other CTA's shared memory any more
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(acc, 512);
@@ -619,13 +642,14 @@ struct Layout {
 };
 
 // Parts of K for dh: full waves of the SMs for the least part sums.
-int splits_for(int64_t T, int64_t D, int64_t piece, int num_sms) {
-  const int64_t tiles = (T + kM - 1) / kM * ((D + kN - 1) / kN);
+int splits_for(int64_t T, int64_t D, int64_t piece) {
+  constexpr int pairs = 76;  // of the 152 SMs
+  const int64_t tiles = (T + kPair - 1) / kPair * ((D + kN - 1) / kN);
   const int64_t blocks = (piece + kK - 1) / kK;
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= kMaxSplits && s * 8 <= std::max<int64_t>(blocks, 8); ++s) {
-    const double waves = static_cast<double>((tiles * s + num_sms - 1) / num_sms) / s * (1.0 + 0.02 * s);
+    const double waves = static_cast<double>((tiles * s + pairs - 1) / pairs) / s * (1.0 + 0.02 * s);
     if (waves < least) {
       least = waves;
       best = s;
@@ -644,7 +668,7 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, bool grad, int64_t pie
   };
   l.planes = bf16 ? 1 : 3;
   l.pack_w = !bf16 || ldw < D || ldw % 8 != 0;
-  l.padded = round_up(T, kM);
+  l.padded = round_up(T, kPair);
   l.Dp = round_up(D, 8);
   l.parts = static_cast<int>((V + kHalf - 1) / kHalf);
   l.head = take(sizeof(Header));
@@ -663,7 +687,7 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, bool grad, int64_t pie
     l.lds = round_up(D, 8);
     l.splits = kMaxSplits;
     l.coef = take(static_cast<size_t>(l.planes) * l.padded * l.ldc * 2);
-    l.sum = take(static_cast<size_t>(splits_for(T, D, l.piece, 152)) * l.padded * l.lds * 4);
+    l.sum = take(static_cast<size_t>(splits_for(T, D, l.piece)) * l.padded * l.lds * 4);
   }
   l.total = at;
   return l;
@@ -708,8 +732,8 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const Gemm& 
   constexpr int smem = kStages * kStageBytes + 1024;
   const cudaError_t e = ensure_dynamic_smem(ce_gemm_kernel<MODE>, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(ce_gemm_kernel<MODE>, dim3(static_cast<unsigned>(std::min<int64_t>(tiles, num_sms))),
-                       dim3(kGemmThreads), smem, s, 0, a, b, g);
+  const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(tiles, num_sms / 2));
+  return launch_kernel(ce_gemm_kernel<MODE>, dim3(grid), dim3(kGemmThreads), smem, s, 2, a, b, g);
 }
 
 #define CE_TRY(expr)                      \
@@ -751,7 +775,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   const int64_t hplane = l.padded * l.Dp, wplane = l.pack_w ? a.V * l.Dp : a.V * wld;
   CUtensorMap h_rows, w_rows;  // K = D contiguous
   CE_TRY(make_map(&h_rows, hp, D, l.padded, P, l.Dp, hplane, kM));
-  CE_TRY(make_map(&w_rows, w, D, a.V, P, wld, wplane, kN));
+  CE_TRY(make_map(&w_rows, w, D, a.V, P, wld, wplane, kM));
   Gemm g = {};
   g.head = head;
   g.row = row;
@@ -764,7 +788,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   // K blocks of an accumulator: 16 steps for the logits that the loss shows in
   // fp32, 32 for fp32 gradients, any number where results are rounded to bf16
   const int any = 1 << 30, few = 4, some = 8;
-  const int64_t mt = l.padded / kM, dt = (a.D + kN - 1) / kN;
+  const int64_t mt = l.padded / kPair, dt = (a.D + kN - 1) / kN;
   const float* lse = a.lse_in;
   if (a.loss != nullptr) {
     g.width = static_cast<int>(a.V);
@@ -786,7 +810,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.sum = reinterpret_cast<float*>(ws + l.sum);
   g.lds = l.lds;
   g.sum_split = l.padded * l.lds;
-  g.splits = splits_for(a.T, a.D, l.piece, 152);
+  g.splits = splits_for(a.T, a.D, l.piece);
   g.dw = a.dw;
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
@@ -807,7 +831,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, mt * vt, num_sms, s));
     g.chunk = bf16 ? any : some;
     CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, mt * dt * g.splits, num_sms, s));
-    CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, (width + kM - 1) / kM * dt, num_sms, s));
+    CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, (width + kPair - 1) / kPair * dt, num_sms, s));
   }
   return launch_kernel(ce_dh_out_kernel<E>, dim3(static_cast<unsigned>(std::min<int64_t>(a.T, 4096))), dim3(256), 0, s, 0,
                        T, a.D, place, g.sum, l.lds, g.splits, g.sum_split, static_cast<E*>(a.dh), a.lddh);

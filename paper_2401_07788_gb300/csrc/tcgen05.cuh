@@ -1,6 +1,8 @@
 // tcgen05.cuh -- inline PTX wrappers for the 5th-generation tensor cores and
 // tensor-map copies (sm_103a): bf16 operands in 128-byte-swizzled shared memory,
-// fp32 accumulators in tensor memory.
+// fp32 accumulators in tensor memory, products of CTA pairs (cta_group::2): the
+// two CTAs of a cluster each hold half of A's rows, half of B's and the
+// accumulator of their own rows of A; the CTA of rank 0 issues the products.
 #pragma once
 
 #include <cuda.h>
@@ -13,12 +15,13 @@ namespace mpc {
 // Tensor-map copies.  The innermost coordinate x is a multiple of 8 bf16
 // elements (16 bytes) in every call.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ void tensor_g2s(void* dst, const CUtensorMap* map, int x, int y, int z,
-                                           uint64_t* bar) {
+// To this CTA's shared memory; `bar` is a cluster address, of a barrier in either
+// CTA of the pair.
+__device__ __forceinline__ void tensor_g2s(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
-          smem_addr(dst)),
-      "l"(map), "r"(smem_addr(bar)), "r"(x), "r"(y), "r"(z)
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_addr(dst)),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
@@ -32,12 +35,12 @@ __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.pr
 // Tensor memory.  alloc/dealloc/ld are warp-wide.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t* dst_smem, uint32_t cols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst_smem)), "r"(cols)
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst_smem)), "r"(cols)
                : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -70,7 +73,7 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
          static_cast<uint64_t>((stride >> 4) & 0x3fff) << 32 | uint64_t{1} << 46 | uint64_t{2} << 61;
 }
 
-// Instruction descriptor: bf16 x bf16 -> fp32, M x N; a_mn / b_mn: the operand is
+// Instruction descriptor: bf16 x bf16 -> fp32, M x N over the pair; a_mn / b_mn: the operand is
 // contiguous along M / N instead of K.
 __host__ __device__ constexpr uint32_t mma_desc(int M, int N, bool a_mn, bool b_mn) {
   return 1u << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(a_mn) << 15 | static_cast<uint32_t>(b_mn) << 16 |
@@ -82,17 +85,26 @@ __host__ __device__ constexpr uint32_t mma_desc(int M, int N, bool a_mn, bool b_
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool fresh) {
   asm volatile(
       "{\n .reg .pred p;\n setp.eq.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(fresh))
       : "memory");
 }
-// `bar` gets one arrival once every product this thread issued is done.
+// `bar` (of this CTA; of both CTAs of the pair, at the same offset) gets one
+// arrival once every product this thread issued is done.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
                : "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_addr(bar)),
+      "h"(static_cast<uint16_t>(3))
+      : "memory");
+}
+// One arrival on a barrier of either CTA, given by its cluster address.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // 32-byte store (address 32-byte aligned).
