@@ -294,6 +294,9 @@ mpc_status mpc_quant_compress_noalloc(const float* x, int64_t rows, int64_t row_
 /* Element types of the calls below that take more than fp32. */
 typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
 
+/* The call that a linear cross-entropy workspace is for. */
+typedef enum { MPC_CE_FORWARD = 0, MPC_CE_BACKWARD = 1, MPC_CE_TRAIN = 2 } mpc_ce_pass;
+
 /* Softmax cross entropy of a linear head, in pieces of the vocabulary, without
  * keeping the logits:
  *   l[t][v] = sum_d h[t][d] w[v][d];   lse[t] = log sum_v exp l[t][v];
@@ -307,7 +310,7 @@ typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
  *           token does not count either.
  *   loss, lse  [tokens] fp32, out.
  *   ws      workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
- *           hidden, vocab, type, 0, 0, ldw), 256-byte aligned.  The query takes
+ *           hidden, vocab, type, MPC_CE_FORWARD, 0, ldw), 256-byte aligned.  The query takes
  *           ldw because the matrix units read a bf16 w in place when its rows
  *           start on 16 bytes; it is copied into the workspace otherwise (pass
  *           ldw = 0 when w itself is not 16-byte aligned), as an fp32 w always
@@ -316,7 +319,7 @@ typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
  * type.  tokens = 0 is a no-op.  Requires hidden >= 1, 1 <= vocab <= 2^31-1,
  * tokens <= 2^31-1. */
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
-                                     int grad, int64_t piece, int64_t ldw);
+                                     mpc_ce_pass pass, int64_t piece, int64_t ldw);
 mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
                                  const int64_t* targets, int64_t tokens, int64_t hidden,
                                  int64_t vocab, mpc_dtype type, int64_t ignore_index, float* loss,
@@ -332,7 +335,8 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
  *   piece  vocabulary entries whose c is in the workspace at a time; 0 lets the
  *          library choose (1 GiB of c at most).
  *   ws     workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
- *          hidden, vocab, type, 1, piece, ldw), 256-byte aligned.
+ *          hidden, vocab, type, MPC_CE_BACKWARD, piece, ldw), 256-byte
+ *          aligned.
  * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
  * tokens = 0 writes dw = 0. */
 mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
@@ -343,7 +347,12 @@ mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int
                                   mpc_stream_t stream);
 
 /* Loss and gradients in one call, for a training step that knows g beforehand:
- * the arguments and results of the two calls above. */
+ * the arguments and results of the two calls above.  With piece = 0 (or >= vocab)
+ * and 257 to 16384 tokens whose exponentials take 4 GiB of workspace at most (2
+ * bytes each, 6 for fp32), the logits are formed once; otherwise as in the two
+ * calls.
+ *   ws  workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens, hidden,
+ *       vocab, type, MPC_CE_TRAIN, piece, ldw), 256-byte aligned. */
 mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_t ldw,
                                const int64_t* targets, const float* gloss, int64_t tokens,
                                int64_t hidden, int64_t vocab, mpc_dtype type, int64_t ignore_index,

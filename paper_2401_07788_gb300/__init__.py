@@ -459,14 +459,14 @@ def _vector(t, n: int, dtype: torch.dtype, name: str, device):
 
 
 def mpc_linear_ce_workspace_bytes(tokens: int, hidden: int, vocab: int, dtype=torch.float32,
-                                  grad: bool = False, piece: int = 0, ldw: int | None = None) -> int:
-    """Bytes of workspace; ldw: the distance of w's rows (hidden when None, 0 for a w that is not
+                                  grad: int = 0, piece: int = 0, ldw: int | None = None) -> int:
+    """Bytes of workspace; grad: 0 forward, 1 backward, 2 training in one call; ldw: the distance of w's rows (hidden when None, 0 for a w that is not
     16-byte aligned)."""
     return int(lib().mpc_linear_ce_workspace_bytes(tokens, hidden, vocab, _DTYPES[dtype], grad, piece,
                                                    hidden if ldw is None else ldw))
 
 
-def _linear_ce_args(h, w, targets, ignore_index, grad, piece, ws, stream):
+def _linear_ce_args(h, w, targets, grad, piece, ws, stream):
     ldh = _matrix(h, "h")
     T, D = h.shape
     if D == 0 or w.dim() != 2 or w.shape[0] == 0:
@@ -487,7 +487,7 @@ def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, ls
                           stream=None):
     """Softmax cross entropy of the logits h [T, D] @ w [V, D].T against targets [T] (int64).
     Returns (loss [T], lse [T]) in fp32; both are 0 for tokens whose target is ignore_index."""
-    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, False, 0, ws, stream)
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 0, 0, ws, stream)
     new = []
     if loss is None:
         loss = torch.empty(T, dtype=torch.float32, device=h.device)
@@ -523,7 +523,7 @@ def mpc_linear_ce_backward(h, w, targets, lse, gloss=None, ignore_index: int = -
     """The gradient of mpc_linear_ce_forward from its lse: (dh [T, D], dw [V, D]) in the type of h.
     gloss [T] fp32 is the gradient of each token's loss; None means that of the mean over the
     tokens that count.  piece: vocabulary entries held in the workspace at a time (0: automatic)."""
-    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, True, piece, ws, stream)
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 1, piece, ws, stream)
     _vector(lse, T, torch.float32, "lse", h.device)
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
@@ -539,7 +539,7 @@ def mpc_linear_ce_train(h, w, targets, gloss=None, ignore_index: int = -100, pie
                         loss=None, dh=None, dw=None, ws=None, stream=None):
     """Loss and gradient in one call: (loss [T], dh [T, D], dw [V, D]); arguments as for
     mpc_linear_ce_forward and mpc_linear_ce_backward."""
-    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, ignore_index, True, piece, ws, stream)
+    T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 2, piece, ws, stream)
     if loss is None:
         loss = torch.empty(T, dtype=torch.float32, device=h.device)
         _on(stream, loss)

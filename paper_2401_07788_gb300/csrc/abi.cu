@@ -608,8 +608,9 @@ bool linear_ce_sizes_ok(int64_t tokens, int64_t hidden, int64_t vocab, int64_t p
 }
 
 // Shared body of the three linear cross-entropy calls.
-mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size_t ws_bytes,
+mpc_status linear_ce_common(mpc::LinearCeArgs a, mpc_ce_pass pass, mpc_dtype type, size_t ws_bytes,
                             mpc_stream_t stream) {
+  const bool grad = pass != MPC_CE_FORWARD;
   MPC_TRY(check_type(type, "type"));
   if (!linear_ce_sizes_ok(a.T, a.D, a.V, a.piece))
     return set_error(MPC_ERR_INVALID_ARG, "tokens=%lld hidden=%lld vocab=%lld piece=%lld", (long long)a.T,
@@ -629,7 +630,7 @@ mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size
   if (grad) MPC_TRY(check_matrix(a.dh, a.T, a.D, a.lddh, type, "dh"));
   MPC_TRY(check_ptr(a.targets, 8, "targets"));
   if (a.gloss != nullptr) MPC_TRY(check_ptr(a.gloss, 4, "gloss"));
-  const size_t need = mpc_linear_ce_workspace_bytes(a.T, a.D, a.V, type, grad, a.piece,
+  const size_t need = mpc_linear_ce_workspace_bytes(a.T, a.D, a.V, type, pass, a.piece,
                                                     aligned_to(a.w, 16) ? a.ldw : 0);
   if (a.ws == nullptr || ws_bytes < need)
     return set_error(MPC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need,
@@ -647,9 +648,9 @@ mpc_status linear_ce_common(mpc::LinearCeArgs a, bool grad, mpc_dtype type, size
 }  // namespace
 
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
-                                     int grad, int64_t piece, int64_t ldw) {
-  if (tokens == 0 || !linear_ce_sizes_ok(tokens, hidden, vocab, piece)) return 0;
-  return mpc::linear_ce_workspace_bytes(tokens, hidden, vocab, type == MPC_BF16, grad, piece, ldw);
+                                     mpc_ce_pass pass, int64_t piece, int64_t ldw) {
+  if (tokens == 0 || pass < MPC_CE_FORWARD || pass > MPC_CE_TRAIN || !linear_ce_sizes_ok(tokens, hidden, vocab, piece)) return 0;
+  return mpc::linear_ce_workspace_bytes(tokens, hidden, vocab, type == MPC_BF16, pass, piece, ldw);
 }
 
 mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,
@@ -673,7 +674,7 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
   a.loss = loss;
   a.lse = lse;
   a.ws = ws;
-  return linear_ce_common(a, false, type, ws_bytes, stream);
+  return linear_ce_common(a, MPC_CE_FORWARD, type, ws_bytes, stream);
 }
 
 mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
@@ -701,7 +702,7 @@ mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int
   a.lddw = lddw;
   a.piece = piece;
   a.ws = ws;
-  return linear_ce_common(a, true, type, ws_bytes, stream);
+  return linear_ce_common(a, MPC_CE_BACKWARD, type, ws_bytes, stream);
 }
 
 mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_t ldw,
@@ -728,7 +729,7 @@ mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_
   a.lddw = lddw;
   a.piece = piece;
   a.ws = ws;
-  return linear_ce_common(a, true, type, ws_bytes, stream);
+  return linear_ce_common(a, MPC_CE_TRAIN, type, ws_bytes, stream);
 }
 
 namespace {

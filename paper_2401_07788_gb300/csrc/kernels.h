@@ -162,7 +162,7 @@ struct LinearCeArgs {
   uint32_t spin_limit;
   unsigned* status;
 };
-size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int grad, int64_t piece,
+size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int pass, int64_t piece,
                                  int64_t ldw);
 cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s);
 

@@ -1,6 +1,5 @@
 // linear_ce.cu -- softmax cross entropy of a linear head over a large
-// vocabulary, with its gradient, in pieces of the vocabulary: the logits are
-// never kept.
+// vocabulary, with its gradient: the logits are never kept.
 //
 //   l[t][v] = <h[t], w[v]>            t over the tokens whose target counts
 //   lse[t]  = log sum_v exp l[t][v];  loss[t] = lse[t] - l[t][target[t]]
@@ -11,100 +10,77 @@
 // a scan of the targets lists the others, and every kernel below works on that
 // list, whose length stays on the device.  Whatever their hidden states hold
 // (padding is often NaN) reaches nothing.
+//
+// Forward: one pass of products (kLoss).  Backward from lse: per piece of the
+// vocabulary the products again (kCoef), then dh and dw: 8 T D V operations with
+// the forward's.  Training in one call, where g is known beforehand: the
+// exponentials of the one pass are kept in bf16 (kExp) and made coefficients
+// without forming the logits again, 6 T D V operations:
+//   e[t][v] = 2^(l log2e - ref[t]),  s[t] = sum_v e,  e[t][target[t]] := 0
+//   dh[t] = g/s sum_v e w + g (p - 1) w[target],   p = softmax at the target
+//   dw[v] = sum_t e (g/s h[t]) + sum over tokens with target v of g (p - 1) h[t]
+// The last sum needs the tokens grouped by target; a stable order is found by
+// counting, for each token, those before it (ce_rank_kernel).
 #include <algorithm>
-#include <cuda_bf16.h>
 
 #include "kernels.h"
 #include "launch_util.h"
-#include "tcgen05.cuh"
+#include "linear_ce_gemm.cuh"
 
 namespace mpc {
 namespace {
-
-constexpr int kM = 128;        // rows of a CTA's output tile (lanes of tensor memory)
-constexpr int kPair = 2 * kM;  // rows of a CTA pair's output tile
-constexpr int kN = 256;        // columns of an output tile
-constexpr int kK = 64;         // K elements of a stage: 128 bytes, one swizzle row
-constexpr int kStages = 6;
-constexpr int kBytesA = kM * kK * 2;
-constexpr int kBytesB = kN / 2 * kK * 2;
-constexpr int kStageBytes = kBytesA + kBytesB;
-constexpr int kEpiWarps = 8;
-constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
-constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct Header {
-  int valid;  // tokens that count
-  float mean; // 1 / valid (0 when none counts)
-};
 
 __device__ __forceinline__ void from_float(float x, float* p) { *p = x; }
 __device__ __forceinline__ void from_float(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
 
 // ---------------------------------------------------------------------------
 // The list of tokens that count: row[i] = token, target[i], and place[t] = i
-// (-1 for the others), in token order; one CTA.  A target outside [0, V) that is
-// not ignore_index is reported and left out too.
+// (-1 for the others), in token order.  A CTA takes 1024 tokens and counts those
+// before them itself (8 bytes each from L2: cheaper than another launch up to
+// millions of tokens).  A target outside [0, V) that is not ignore_index is
+// reported and left out too.
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(1024)
-    ce_scan_kernel(const int64_t* __restrict__ targets, int T, int64_t V, int64_t ignore,
-                   Header* head, int* row, int* target, int* place, unsigned* status) {
-  pdl_begin();
-  __shared__ int warp_count[32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int base = 0;
-  for (int t0 = 0; t0 < T; t0 += 1024) {
-    const int t = t0 + threadIdx.x;
-    bool keep = false;
-    int64_t y = 0;
-    if (t < T) {
-      y = targets[t];
-      keep = y != ignore;
-      if (keep && (y < 0 || y >= V)) {
-        set_status(status, STATUS_BAD_INDEX);
-        keep = false;
-      }
-    }
-    const unsigned b = __ballot_sync(kFull, keep);
-    if (lane == 0) warp_count[warp] = __popc(b);
-    __syncthreads();
-    int before = base, total = 0;
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) before += warp_count[w];
-      total += warp_count[w];
-    }
-    const int i = before + __popc(b & lanemask_lt());
-    if (t < T) place[t] = keep ? i : -1;
-    if (keep) {
-      row[i] = t;
-      target[i] = static_cast<int>(y);
-    }
-    base += total;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    head->valid = base;
-    head->mean = base > 0 ? fdiv(1.0f, static_cast<float>(base)) : 0.0f;
-  }
-}
+constexpr int kScan = 1024;
 
-// ---------------------------------------------------------------------------
-// Operands in bf16 planes.  A bf16 tensor is one plane.  An fp32 x is the sum of
-// three, x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1) (24 bits), and a
-// product of two fp32 tensors the sum of the plane products i + j <= 2, six of
-// them: what is left out is below 2^-24 of a term.  One kernel so serves both
-// types, an fp32 product being a bf16 one with six times the K steps.
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
-  const __nv_bfloat16 a = __float2bfloat16_rn(x);
-  const float r = fsub(x, __bfloat162float(a));
-  const __nv_bfloat16 b = __float2bfloat16_rn(r);
-  const __nv_bfloat16 c = __float2bfloat16_rn(fsub(r, __bfloat162float(b)));
-  p[0] = __bfloat16_as_ushort(a);
-  p[1] = __bfloat16_as_ushort(b);
-  p[2] = __bfloat16_as_ushort(c);
+__global__ void __launch_bounds__(kScan)
+    ce_scan_kernel(const int64_t* __restrict__ targets, int T, int64_t V, int64_t ignore, Header* head, int* row,
+                   int* target, int* place, int* pos, int* flags, unsigned* status) {
+  pdl_begin();
+  __shared__ int before_of[32], count_of[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto counts = [&](int64_t v) { return v != ignore && v >= 0 && v < V; };
+  const int t0 = blockIdx.x * kScan, t = t0 + threadIdx.x;
+  int64_t y = ignore;
+  if (t < T) y = targets[t];
+  int before = 0;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < t0; i += kScan) before += counts(targets[i]);
+  const bool keep = t < T && counts(y);
+  if (y != ignore && !keep) set_status(status, STATUS_BAD_INDEX);
+  before = __reduce_add_sync(kFull, before);
+  const unsigned kept = __ballot_sync(kFull, keep);
+  if (lane == 0) {
+    before_of[warp] = before;
+    count_of[warp] = __popc(kept);
+  }
+  __syncthreads();
+  const int mine = count_of[lane];
+  const int through = static_cast<int>(warp_inclusive_scan(static_cast<unsigned>(mine), lane));
+  const int base = __reduce_add_sync(kFull, before_of[lane]);
+  const int i = base + __shfl_sync(kFull, through - mine, warp) + __popc(kept & lanemask_lt());
+  if (t < T) place[t] = keep ? i : -1;
+  if (keep) {
+    row[i] = t;
+    target[i] = static_cast<int>(y);
+  }
+  if (t < T && pos != nullptr) pos[t] = 0;
+  if (flags != nullptr && threadIdx.x < kScan / kPair) flags[blockIdx.x * (kScan / kPair) + threadIdx.x] = 0;
+  const int total = base + __shfl_sync(kFull, through, 31);
+  if (t0 + kScan >= T && threadIdx.x == 0) {
+    head->valid = total;
+    head->mean = total > 0 ? fdiv(1.0f, static_cast<float>(total)) : 0.0f;
+    head->redo = 0;
+  }
 }
 
 template <typename E>
@@ -116,509 +92,388 @@ __device__ __forceinline__ void planes_of<__nv_bfloat16>(__nv_bfloat16 x, uint16
   p[0] = __bfloat16_as_ushort(x);
 }
 
-// out[plane][r][0..Dp) of `rows` rows: row r is x's row list[r] (r itself without
-// a list); zeros for r >= *count and for columns >= D.
-template <typename E, int P>
-__global__ void __launch_bounds__(256)
-    ce_pack_kernel(const E* __restrict__ x, int64_t ld, const int* __restrict__ list, const int* count, int64_t rows,
-                   int64_t padded, int D, int Dp, uint16_t* __restrict__ out) {
-  pdl_begin();
-  const int64_t n = count != nullptr ? *count : rows;
-  const int64_t need = min64((n + kPair - 1) / kPair * kPair, padded);  // rows that a product may touch
-  const int groups = Dp / 8;
-  const int64_t plane = padded * Dp;
-  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < need * groups; q += gridDim.x * int64_t{256}) {
-    const int64_t r = q / groups;
-    const int d0 = static_cast<int>(q % groups) * 8;
-    uint16_t p[8][3];
-    const E* src = r < n ? x + (list != nullptr ? list[r] : r) * ld + d0 : nullptr;
+// Eight elements from p on; those from `left` on are zero.
+template <typename E>
+__device__ __forceinline__ void load8(const E* p, int left, bool wide, E (&x)[8]) {
+  if (wide && left >= 8) {
+    uint4 u[sizeof(E) / 2];
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) u[k] = reinterpret_cast<const uint4*>(p)[k];
+    memcpy(x, u, sizeof(x));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = j < left ? p[j] : E(0.0f);
+  }
+}
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+template <int P>
+__device__ __forceinline__ void store_planes8(uint16_t* out, int64_t plane, const uint16_t (&p)[8][3]) {
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    uint4 u;
+    u.x = p[0][k] | static_cast<uint32_t>(p[1][k]) << 16;
+    u.y = p[2][k] | static_cast<uint32_t>(p[3][k]) << 16;
+    u.z = p[4][k] | static_cast<uint32_t>(p[5][k]) << 16;
+    u.w = p[6][k] | static_cast<uint32_t>(p[7][k]) << 16;
+    *reinterpret_cast<uint4*>(out + k * plane) = u;
+  }
+}
+// Eight values of packed planes.
+template <int P>
+__device__ __forceinline__ void load_planes8(const uint16_t* in, int64_t plane, float (&x)[8]) {
+#pragma unroll
+  for (int k = P - 1; k >= 0; --k) {
+    const uint4 u = *reinterpret_cast<const uint4*>(in + k * plane);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      if (src != nullptr && d0 + j < D) planes_of<E>(src[j], p[j]);
-      else p[j][0] = p[j][1] = p[j][2] = 0;
+      const float v = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+      x[j] = k == P - 1 ? v : fadd(v, x[j]);
     }
+  }
+}
+
+// Rows that a product of row pairs may touch: zero from the last one that counts on.
+__device__ __forceinline__ int64_t rows_touched(int64_t n) { return (n + kPair - 1) / kPair * kPair; }
+
+// The listed rows of h in planes, out[plane][i][0..Dp), one warp a row; with `ref`
+// also the logit of each row's target in base 2.
+template <typename E, int P>
+__global__ void __launch_bounds__(256)
+    ce_pack_h_kernel(const E* __restrict__ h, int64_t ldh, const Header* head, const int* __restrict__ row,
+                     int64_t padded, int D, int Dp, int wide_h, uint16_t* __restrict__ out,
+                     const E* __restrict__ w, int64_t ldw, const int* __restrict__ target, int wide_w, float* ref) {
+  pdl_begin();
+  const int n = head->valid, lane = threadIdx.x & 31;
+  const int64_t m = blockIdx.x * int64_t{8} + (threadIdx.x >> 5);
+  if (m >= rows_touched(n)) return;
+  const bool live = m < n;
+  const E* src = live ? h + row[m] * ldh : nullptr;
+  const E* at = live && ref != nullptr ? w + target[m] * ldw : nullptr;
+  float dot = 0.0f;
+  for (int d = lane * 8; d < Dp; d += 256) {
+    uint16_t p[8][3] = {};
+    if (live) {
+      E x[8];
+      load8(src + d, D - d, wide_h, x);
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-      uint4 u;
-      u.x = p[0][k] | static_cast<uint32_t>(p[1][k]) << 16;
-      u.y = p[2][k] | static_cast<uint32_t>(p[3][k]) << 16;
-      u.z = p[4][k] | static_cast<uint32_t>(p[5][k]) << 16;
-      u.w = p[6][k] | static_cast<uint32_t>(p[7][k]) << 16;
-      *reinterpret_cast<uint4*>(out + k * plane + r * Dp + d0) = u;
+      for (int j = 0; j < 8; ++j) planes_of<E>(x[j], p[j]);
+      if (ref != nullptr) {
+        E y[8];
+        load8(at + d, D - d, wide_w, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot = __fmaf_rn(to_float(x[j]), to_float(y[j]), dot);
+      }
+    }
+    store_planes8<P>(out + m * Dp + d, padded * Dp, p);
+  }
+  if (live && ref != nullptr) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) dot = fadd(dot, __shfl_xor_sync(kFull, dot, o));
+    if (lane == 0) ref[m] = fmul(dot, kLog2e);
+  }
+}
+
+// w in planes, for an fp32 w or rows that a tensor map cannot read.
+template <typename E, int P>
+__global__ void __launch_bounds__(256)
+    ce_pack_w_kernel(const E* __restrict__ w, int64_t ldw, int64_t V, int D, int Dp, int wide,
+                     uint16_t* __restrict__ out) {
+  pdl_begin();
+  const int groups = Dp / 8;
+  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < V * groups; q += gridDim.x * int64_t{256}) {
+    const int64_t r = q / groups;
+    const int d = static_cast<int>(q - r * groups) * 8;
+    E x[8];
+    uint16_t p[8][3];
+    load8(w + r * ldw + d, D - d, wide, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) planes_of<E>(x[j], p[j]);
+    store_planes8<P>(out + r * Dp + d, V * Dp, p);
+  }
+}
+
+// Largest value and sum of a row's half tiles over a CTA of 32 rows (lanes) x 32
+// warps, in a fixed order; the result is valid in warp 0.  RELATIVE: the sums are
+// over exp2 from each part's own largest value, else from one reference.
+template <bool RELATIVE>
+__device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T, int m, int n) {
+  __shared__ float top_of[32][33], sum_of[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float top = -INFINITY, sum = 0.0f;
+  if (m < n) {
+    if (RELATIVE) {
+      for (int i = warp; i < parts; i += 32) top = fmaxf(top, part[static_cast<int64_t>(i) * T + m].x);
+    }
+    for (int i = warp; i < parts; i += 32) {
+      const float2 p = part[static_cast<int64_t>(i) * T + m];
+      if (RELATIVE) {
+        if (p.x != -INFINITY) sum = fadd(sum, fmul(p.y, exp2f(fsub(p.x, top))));
+      } else {
+        top = fmaxf(top, p.x);
+        sum = fadd(sum, p.y);
+      }
     }
   }
-}
-
-// ---------------------------------------------------------------------------
-// The matrix products: C[m][n] = sum_k A[m][k] B[n][k] in 256 x 256 tiles.
-//
-// A persistent pair of CTAs on two SMs per tile, 128 rows each: every CTA copies
-// its rows of A and half the rows of B, so an SM reads 32 KB from L2 for 2^20
-// products (48 KB with a tile of its own).  Warp 0 copies operand tiles through
-// tensor maps (kStages stages of 32 KB a CTA), one thread of the first CTA's warp
-// 1 issues the products of both, eight warps a CTA take the finished tile from
-// tensor memory.  Two
-// accumulators of 256 columns fill the tensor memory, so a tile's epilogue runs
-// under the next tile's products.
-//
-// kLoss   A = h [valid][D],  B = w [V][D]: a tile's logits become, for each token
-//         and half tile, their largest and the sum of exponentials over it.
-// kCoef   the same products again: the coefficients c of a piece of the vocabulary,
-//         rounded to bf16 planes.
-// kDh     A = c [valid][piece], B = w^T [D][piece]: dh, K split over several CTAs
-//         where there are few tiles, each split's sum kept in fp32.
-// kDw     A = c^T [piece][valid], B = h^T [D][valid]: dw of the piece.
-//
-// An accumulator adds each product step with truncation: about 5e-9 of its value
-// a step of 16, always towards zero (measured: dh over 50257 entries 9e-5 off).
-// Where fp32 results depend on it, an accumulator sums a chunk of K blocks only,
-// the smallest plane products first, and the epilogue adds the chunks in fp32
-// with rounding to nearest; two accumulators in turn keep the products running.
-// Operands whose K is not the contiguous axis (w^T, c^T, h^T) are read as they
-// are: rows of 64 M/N-elements, and the product's descriptors say so.
-// ---------------------------------------------------------------------------
-enum Mode { kLoss, kCoef, kDh, kDw };
-
-struct Gemm {
-  const Header* head;
-  const int* row;       // token of a listed row
-  const int* target;
-  int T;                // tokens (upper bound of the list)
-  int D;
-  int width;            // vocabulary entries of the piece
-  int64_t v0;           // its first one
-  int terms;            // 1 (bf16) or 6 (fp32 in three planes)
-  int chunk;            // K blocks that one accumulator sums (see ce_gemm_kernel)
-  int splits;           // kDh: parts of K
-  int first;            // kDh: the piece that starts the sums
-  float2* part;         // kLoss: [half tile][T] (largest logit, sum), base 2
-  float* at_target;     // kLoss: [T]
-  const float* lse;     // kCoef: [T] by token
-  const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
-  uint16_t* coef;       // kCoef: [plane][rows][ldc]
-  int64_t ldc, coef_plane;
-  float* sum;           // kDh: [split][rows][lds]
-  int64_t lds, sum_split;
-  void* dw;             // kDw
-  int64_t lddw;
-  int dw_bf16, dw_wide; // type; rows and base suit 32-byte stores
-  uint32_t spin_limit;
-  unsigned* status;
-};
-
-// Plane pair of a term, smallest products first.
-__device__ __forceinline__ void term_planes(int terms, int t, int* a, int* b) {
-  if (terms == 1) {
-    *a = *b = 0;
-  } else {  // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), two bits each
-    *a = (0x052 >> (2 * t)) & 3;
-    *b = (0x118 >> (2 * t)) & 3;
+  top_of[warp][lane] = top;
+  sum_of[warp][lane] = sum;
+  __syncthreads();
+  float2 r = make_float2(-INFINITY, 0.0f);
+  if (warp == 0) {
+    for (int w = 0; w < 32; ++w) r.x = fmaxf(r.x, top_of[w][lane]);
+    for (int w = 0; w < 32; ++w) {
+      const float t = top_of[w][lane];
+      if (!RELATIVE) r.y = fadd(r.y, sum_of[w][lane]);
+      else if (t != -INFINITY) r.y = fadd(r.y, fmul(sum_of[w][lane], exp2f(fsub(t, r.x))));
+    }
   }
-}
-
-struct Tile {
-  int m0, n0, split, k0, k1;  // K blocks [k0, k1)
-};
-
-struct Shape {
-  int m_tiles, n_tiles, blocks, splits;
-  __device__ int total() const { return m_tiles * n_tiles * splits; }
-};
-
-template <int MODE>
-__device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
-  Shape s;
-  const int m = MODE == kDw ? g.width : valid;
-  const int n = MODE == kDh || MODE == kDw ? g.D : g.width;
-  const int k = MODE == kDh ? g.width : MODE == kDw ? valid : g.D;
-  s.m_tiles = (m + kPair - 1) / kPair;
-  s.n_tiles = (n + kN - 1) / kN;
-  s.blocks = (k + kK - 1) / kK;
-  s.splits = MODE == kDh ? g.splits : 1;
-  return s;
-}
-
-// Order of the tiles: those that run at the same time share operands in L2.  For
-// the logits all tokens pass one stretch of the vocabulary; for dh and dw the
-// columns of one row tile of c run together, so that c is read from HBM once.
-template <int MODE>
-__device__ __forceinline__ Tile tile_of(const Shape& s, int i) {
-  Tile t;
-  if (MODE == kLoss || MODE == kCoef) {
-    t.m0 = i % s.m_tiles * kPair;
-    t.n0 = i / s.m_tiles * kN;
-    t.split = 0;
-  } else {
-    t.n0 = i % s.n_tiles * kN;
-    i /= s.n_tiles;
-    t.m0 = i % s.m_tiles * kPair;
-    t.split = i / s.m_tiles;
-  }
-  t.k0 = static_cast<int>(static_cast<int64_t>(s.blocks) * t.split / s.splits);
-  t.k1 = static_cast<int>(static_cast<int64_t>(s.blocks) * (t.split + 1) / s.splits);
-  return t;
-}
-
-__device__ __forceinline__ float exp2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-  uint32_t u;
-  memcpy(&u, &p, 4);
-  return u;
-}
 
-// One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
-template <int MODE>
-__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf]) {
-  if (MODE == kLoss) {
-    const int cols = min(g.width - n0, kHalf);
-    if (cols <= 0 || m >= valid) return;
-    const int y = static_cast<int>(g.target[m] - n0);
-    if (cols < kHalf) {
-#pragma unroll
-      for (int j = 0; j < kHalf; ++j)
-        if (j >= cols) x[j] = -INFINITY;
-    }
-    if (y >= 0 && y < cols) {
-      float v = x[0];
-#pragma unroll
-      for (int j = 1; j < kHalf; ++j) v = j == y ? x[j] : v;
-      g.at_target[m] = v;
-    }
-    // base 2 throughout: exp(l - top) = 2^(l log2e - top log2e), one rounding in the exponent
-    float top = x[0];
-#pragma unroll
-    for (int j = 1; j < kHalf; ++j) top = fmaxf(top, x[j]);
-    const float base = fmul(top, kLog2e);
-    const float shift = base == -INFINITY ? 0.0f : -base;
-    float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kHalf; j += 4) {
-      s0 = fadd(s0, exp2_approx(__fmaf_rn(x[j], kLog2e, shift)));
-      s1 = fadd(s1, exp2_approx(__fmaf_rn(x[j + 1], kLog2e, shift)));
-      s2 = fadd(s2, exp2_approx(__fmaf_rn(x[j + 2], kLog2e, shift)));
-      s3 = fadd(s3, exp2_approx(__fmaf_rn(x[j + 3], kLog2e, shift)));
-    }
-    g.part[static_cast<int64_t>(n0 / kHalf) * g.T + m] = make_float2(base, fadd(fadd(s0, s1), fadd(s2, s3)));
-  } else if (MODE == kCoef) {
-    if (n0 >= g.ldc) return;
-    const bool live = m < valid;
-    float shift = 0.0f, weight = 0.0f, scale = 0.0f;
-    int y = -1;
-    if (live) {
-      const int token = g.row[m];
-      const float lse = g.lse[token];
-      weight = g.gloss != nullptr ? g.gloss[token] : g.head->mean;
-      // what the rounding of lse log2e leaves out goes into the factor
-      shift = fmul(lse, -kLog2e);
-      scale = fmul(weight, exp2f(-__fmaf_rn(lse, kLog2e, shift)));
-      y = static_cast<int>(g.target[m] - g.v0 - n0);
-    }
-#pragma unroll
-    for (int j = 0; j < kHalf; ++j)
-      x[j] = live ? fmul(scale, exp2_approx(__fmaf_rn(x[j], kLog2e, shift))) : 0.0f;
-    if (y >= 0 && y < kHalf) {
-#pragma unroll
-      for (int j = 0; j < kHalf; ++j)
-        if (j == y) x[j] = fsub(x[j], weight);
-    }
-    uint16_t* out = g.coef + m * g.ldc + n0;
-    if (g.terms == 1) {
-#pragma unroll
-      for (int j = 0; j < kHalf; j += 16) {
-        uint32_t u[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
-        st_v8(out + j, u);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < kHalf; j += 16) {
-        uint32_t u[3][8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          uint16_t a[3], b[3];
-          split(x[j + 2 * q], a);
-          split(x[j + 2 * q + 1], b);
-#pragma unroll
-          for (int k = 0; k < 3; ++k) u[k][q] = a[k] | static_cast<uint32_t>(b[k]) << 16;
-        }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) st_v8(out + k * g.coef_plane + j, u[k]);
-      }
-    }
-  } else if (MODE == kDh) {
-    if (m >= valid) return;
-    float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
-#pragma unroll
-    for (int j = 0; j < kHalf; j += 8) {
-      if (n0 + j < g.lds) {
-        uint32_t u[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          if (!g.first) x[j + q] = fadd(x[j + q], out[j + q]);
-          u[q] = __float_as_uint(x[j + q]);
-        }
-        st_v8(out + j, u);
-      }
-    }
-  } else {
-    if (m >= g.width) return;
-    const int64_t at = (g.v0 + m) * g.lddw + n0;
-    if (g.dw_bf16) {
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.dw) + at;
-#pragma unroll
-      for (int j = 0; j < kHalf; j += 16) {
-        if (g.dw_wide && n0 + j + 16 <= g.D) {
-          uint32_t u[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
-          st_v8(out + j, u);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            if (n0 + j + q < g.D) out[j + q] = __float2bfloat16_rn(x[j + q]);
-        }
-      }
-    } else {
-      float* out = static_cast<float*>(g.dw) + at;
-#pragma unroll
-      for (int j = 0; j < kHalf; j += 8) {
-        if (g.dw_wide && n0 + j + 8 <= g.D) {
-          uint32_t u[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[j + q]);
-          st_v8(out + j, u);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (n0 + j + q < g.D) out[j + q] = x[j + q];
-        }
-      }
-    }
-  }
-}
-
-// Columns of a tile that the product forms: a multiple of 16.  Each CTA of the
-// pair holds half of them as rows of B.
-__device__ __forceinline__ int tile_cols(int cols, int n0) { return min((cols - n0 + 15) / 16 * 16, kN); }
-
-template <int MODE>
-__global__ void __launch_bounds__(kGemmThreads, 1)
-    ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const __grid_constant__ Gemm g) {
-  constexpr bool A_MN = MODE == kDw, B_MN = MODE == kDh || MODE == kDw;
-  extern __shared__ uint8_t raw[];
-  // full and taken are used in the first CTA, for both; empty and done in each
-  __shared__ uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
-  __shared__ uint32_t tmem;
-  uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(cluster_rank());
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&done[i], 1);
-      mbar_init(&taken[i], 2 * kEpiWarps);
-    }
-    mbar_init(&drain, 1);
-    fence_mbar_init();
-    prefetch_map(&map_a);
-    prefetch_map(&map_b);
-  }
-  if (warp == 1) tmem_alloc(&tmem, 512);
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync();
-  tc_fence_after();
-  const uint32_t acc = tmem;
+// Forward: lse and loss of the tokens that count.
+__global__ void __launch_bounds__(1024)
+    ce_finish_kernel(int T, const Header* head, const int* row, const int* place, const float2* part, int parts,
+                     const float* at_target, float* loss, float* lse) {
   pdl_begin();
-  const int valid = g.head->valid;
-  const Shape s = shape_of<MODE>(g, valid);
-  const int total = s.total();
-  const int cols = MODE == kDh || MODE == kDw ? g.D : g.width;
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-
-  if (warp == 0) {
-    if (lane == 0) {
-      fence_proxy_async_all();  // operands that earlier kernels wrote
-      uint32_t it = 0;
-      bool ok = true;
-      for (int i = pair; i < total && ok; i += pairs) {
-        const Tile t = tile_of<MODE>(s, i);
-        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(cols, t.n0) / 2);
-        for (int c = t.k0; c < t.k1 && ok; c += g.chunk) {
-          const int blocks = min(g.chunk, t.k1 - c);
-          for (int j = 0; j < blocks * g.terms; ++j, ++it) {
-            const int kb = c + j % blocks;
-            const int st = it % kStages;
-            ok = mbar_wait_bounded(&empty[st], (it / kStages & 1) ^ 1, g.spin_limit, g.status);
-            if (!ok) break;
-            int pa, pb;
-            term_planes(g.terms, j / blocks, &pa, &pb);
-            uint8_t* a = stage0 + st * kStageBytes;
-            uint8_t* b = a + kBytesA;
-            const uint32_t bar = dsmem_addr(&full[st], 0);
-            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kStageBytes);
-            if (A_MN) {
-#pragma unroll
-              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, pa, bar);
-            } else {
-              tensor_g2s(a, &map_a, kb * kK, m0, pa, bar);
-            }
-            if (B_MN) {
-              const int k_at = kb * kK + (MODE == kDh ? static_cast<int>(g.v0) : 0);
-#pragma unroll
-              for (int q = 0; q < kN / 128; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
-            } else {
-              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, pb, bar);
-            }
-          }
-        }
-      }
-      // Copies in flight must land before either CTA leaves (the cluster barrier
-      // below).  The first CTA sees both CTAs' copies arrive; where a wait gave up,
-      // the second one may have sent some that the first no longer counts, and
-      // gives them a millisecond.
-      if (rank == 0) {
-        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-          mbar_wait_bounded(&full[i % kStages], i / kStages & 1, kDrainPolls, g.status);
-      } else if (!ok) {
-        const uint64_t until = global_ns() + 1000000;
-        while (global_ns() < until) __nanosleep(1000);
-      }
-    }
-  } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      uint32_t it = 0, n = 0;
-      bool ok = true;
-      for (int i = pair; i < total && ok; i += pairs) {
-        const Tile t = tile_of<MODE>(s, i);
-        const uint32_t idesc = mma_desc(kPair, tile_cols(cols, t.n0), A_MN, B_MN);
-        for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
-          ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
-          tc_fence_after();
-          const uint32_t d = acc + (n & 1) * kN;
-          bool fresh = true;
-          const int steps = min(g.chunk, t.k1 - c) * g.terms;
-          for (int k = 0; k < steps && ok; ++k, ++it) {
-            const int st = it % kStages;
-            ok = mbar_wait_bounded(&full[st], it / kStages & 1, g.spin_limit, g.status);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t a = smem_addr(stage0 + st * kStageBytes), b = a + kBytesA;
-#pragma unroll
-            for (int q = 0; q < kK / 16; ++q) {
-              // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
-              const uint64_t da = A_MN ? smem_desc(a + q * 2048, kK * 128, 1024) : smem_desc(a + q * 32, 16, 1024);
-              const uint64_t db = B_MN ? smem_desc(b + q * 2048, kK * 128, 1024) : smem_desc(b + q * 32, 16, 1024);
-              mma_bf16(d, da, db, idesc, fresh);
-              fresh = false;
-            }
-            mma_commit_pair(&empty[st]);
-          }
-          if (ok) mma_commit_pair(&done[n & 1]);
-        }
-      }
-      if (!ok) {  // products in flight must end before the tensor memory is given back
-        mma_commit(&drain);
-        mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
-      }
-    }
-  } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;
-    uint32_t n = 0;
-    bool ok = true;
-    for (int i = pair; i < total; i += pairs) {
-      const Tile t = tile_of<MODE>(s, i);
-      float x[kHalf];
-#pragma unroll
-      for (int q = 0; q < kHalf; ++q) x[q] = 0.0f;
-      for (int c = t.k0; c < t.k1; c += g.chunk, ++n) {
-        ok = mbar_wait_bounded(&done[n & 1], n / 2 & 1, g.spin_limit, g.status);
-        ok = __all_sync(kFull, ok);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t at = acc + (n & 1) * kN + half * kHalf + (static_cast<uint32_t>(quad * 32) << 16);
-#pragma unroll
-        for (int q = 0; q < kHalf; q += 64) {
-          float y[64];
-          tmem_ld32(at + q, y);
-          tmem_ld32(at + q + 32, y + 32);
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            asm volatile("" : "+f"(y[j]));  // nothing uses y before the wait
-            x[q + j] = fadd(x[q + j], y[j]);
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
-      }
-      if (!ok) break;
-      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x);
-    }
-  }
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync();  // nothing signals or reads the other CTA's shared memory any more
-  if (warp == 1) {
-    tc_fence_after();
-    tmem_dealloc(acc, 512);
+  const int t = blockIdx.x * 32 + (threadIdx.x & 31), n = head->valid;
+  if (threadIdx.x < 32 && t < T && place[t] < 0) loss[t] = lse[t] = 0.0f;
+  if (blockIdx.x * 32 >= n) return;
+  const int m = t;  // as a place in the list from here on
+  const float2 r = sum_parts<true>(part, parts, T, m, n);
+  if (threadIdx.x < 32 && m < n) {
+    // both measured from the largest logit, so that a small loss keeps its digits
+    const float l = log2f(r.y);
+    lse[row[m]] = fmul(fadd(r.x, l), kLn2);
+    loss[row[m]] = fmul(fsub(l, __fmaf_rn(at_target[m], kLog2e, -r.x)), kLn2);
   }
 }
 
-// lse and loss of each token from its half tiles' sums; one warp a token.
+// Training: the sum of each row's exponentials.  A sum out of range (the loss is
+// over 27, or the reference far off) takes the row's largest logit as reference
+// and marks its row tile.
+__global__ void __launch_bounds__(1024)
+    ce_sum_kernel(int T, Header* head, const float2* part, int parts, float* sum, float* ref, int* flags) {
+  pdl_begin();
+  const int m = blockIdx.x * 32 + (threadIdx.x & 31), n = head->valid;
+  if (blockIdx.x * 32 >= n) return;
+  const float2 r = sum_parts<false>(part, parts, T, m, n);
+  if (threadIdx.x < 32 && m < n) {
+    sum[m] = r.y;
+    if (!(r.y > 0x1p-40f && r.y < 0x1p40f) && fabsf(r.x) < INFINITY) {
+      ref[m] = r.x;
+      flags[m / kPair] = 1;
+      head->redo = 1;
+    }
+  }
+}
+
+// pos[i] = tokens of the list that come before token i in the order by target,
+// then by place.  CTA (x, y) counts for 256 tokens over every gridDim.y-th block
+// of 256 others: two instructions a pair, 4 us for 8192 tokens.  Integer sums: the
+// order of the atomics does not show.
 __global__ void __launch_bounds__(256)
-    ce_finish_kernel(int T, const int* place, const float2* part, int parts, const float* at_target, float* loss,
-                     float* lse) {
+    ce_rank_kernel(const Header* head, const int* __restrict__ target, int* pos) {
   pdl_begin();
-  const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (t >= T) return;
-  const int m = place[t];
-  if (m < 0) {
-    if (lane == 0) loss[t] = lse[t] = 0.0f;
-    return;
+  __shared__ int4 others[64];
+  const int n = head->valid;
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (blockIdx.x * 256 >= n) return;
+  const int y = i < n ? target[i] : 0;
+  int count = 0;
+  for (int b = blockIdx.y; b * 256 < n; b += gridDim.y) {
+    const int j = b * 256 + threadIdx.x;
+    __syncthreads();
+    reinterpret_cast<int*>(others)[threadIdx.x] = j < n ? target[j] : 0x7fffffff;
+    __syncthreads();
+    if (b == blockIdx.x) {
+      for (int q = 0; q < 256; ++q) {
+        const int o = reinterpret_cast<const int*>(others)[q];
+        count += o < y || (o == y && q < static_cast<int>(threadIdx.x));
+      }
+    } else {
+      const int below = b < blockIdx.x ? y + 1 : y;  // earlier tokens with the same target come before
+#pragma unroll 8
+      for (int q = 0; q < 64; ++q) {
+        const int4 o = others[q];
+        count += (o.x < below) + (o.y < below) + (o.z < below) + (o.w < below);
+      }
+    }
   }
-  float top = -INFINITY;
-  for (int i = lane; i < parts; i += 32) top = fmaxf(top, part[static_cast<int64_t>(i) * T + m].x);
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-  float sum = 0.0f;
-  for (int i = lane; i < parts; i += 32) {
-    const float2 p = part[static_cast<int64_t>(i) * T + m];
-    sum = fadd(sum, fmul(p.y, exp2f(fsub(p.x, top))));
+  if (i < n) atomicAdd(&pos[i], count);
+}
+
+struct Finish {
+  int T, D, Dp, parts;
+  int64_t V, padded;
+  const Header* head;
+  const int* row;
+  const int* target;
+  const int* place;
+  const int* pos;
+  const int* flags;
+  const float2* part;
+  const float* at_target;
+  const float* ref;
+  const float* sum;
+  const float* gloss;
+  const uint16_t* hp;
+  const float* lse;    // given lse and no sums (logits formed twice): [T] by token
+  const float* loss_in;
+  uint16_t* hs;        // h times g/s in planes, or nullptr
+  float* scale;        // g/s
+  float* coef;         // g (p - 1)
+  int* order;          // token at each position by target
+  int* sorted;         // its target
+  int* seg_first;
+  float* loss;
+};
+
+// Training: the target's coefficients and the order by target, and where the
+// exponentials are kept the loss, the factors and the scaled hidden states; one
+// warp a row.
+template <int P>
+__global__ void __launch_bounds__(256) ce_scale_kernel(const Finish f) {
+  pdl_begin();
+  const int n = f.head->valid, lane = threadIdx.x & 31;
+  const int64_t m = blockIdx.x * int64_t{8} + (threadIdx.x >> 5);
+  for (int64_t v = blockIdx.x * int64_t{256} + threadIdx.x; v < f.V; v += gridDim.x * int64_t{256}) f.seg_first[v] = 0;
+  if (f.hs != nullptr && lane == 0 && m < f.T && f.place[m] < 0) f.loss[m] = 0.0f;  // m as a token here
+  if (m >= rows_touched(n)) return;
+  float scale = 0.0f;
+  if (m < n) {
+    const int t = f.row[m];
+    const float g = f.gloss != nullptr ? f.gloss[t] : f.head->mean;
+    float loss;
+    if (f.hs != nullptr) {
+      float s = f.sum[m];
+      if (f.flags[m / kPair] != 0) {
+        s = 0.0f;
+        for (int i = lane; i < f.parts; i += 32) s = fadd(s, f.part[static_cast<int64_t>(i) * f.T + m].y);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
+      }
+      // lse - l[target], both measured from ref
+      loss = fmul(fsub(log2f(s), __fmaf_rn(f.at_target[m], kLog2e, -f.ref[m])), kLn2);
+      scale = fdiv(g, s);
+      if (lane == 0) {
+        f.loss[t] = loss;
+        f.scale[m] = scale;
+      }
+    } else {
+      loss = f.loss_in != nullptr ? f.loss_in[t] : __fmaf_rn(f.ref[m], -kLn2, f.lse[t]);
+    }
+    if (lane == 0) {
+      f.coef[m] = fmul(g, expm1f(-loss));
+      f.order[f.pos[m]] = static_cast<int>(m);
+      f.sorted[f.pos[m]] = f.target[m];
+    }
   }
-  for (int o = 16; o > 0; o >>= 1) sum = fadd(sum, __shfl_xor_sync(kFull, sum, o));
-  if (lane == 0) {
-    const float l = __fmaf_rn(top, kLn2, logf(sum));
-    lse[t] = l;
-    loss[t] = fsub(l, at_target[m]);
+  if (f.hs == nullptr) return;
+  const int64_t plane = f.padded * f.Dp;
+  for (int d = lane * 8; d < f.Dp; d += 256) {
+    uint16_t p[8][3] = {};
+    if (m < n) {
+      float x[8];
+      load_planes8<P>(f.hp + m * f.Dp + d, plane, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) split(fmul(x[j], scale), p[j]);
+    }
+    store_planes8<P>(f.hs + m * f.Dp + d, plane, p);
+  }
+}
+
+// Target gradients: a CTA takes kRun tokens in the order by target and sums
+// coef h over each run with one target, in token order, into seg_sum at the run's
+// first position.
+template <int P>
+__global__ void __launch_bounds__(256)
+    ce_target_kernel(const Header* head, const int* __restrict__ order, const int* __restrict__ sorted,
+                     const float* __restrict__ coef, const uint16_t* __restrict__ hp, int64_t plane, int Dp,
+                     int* seg_first, int* seg_end, float* seg_sum, int64_t lds) {
+  pdl_begin();
+  __shared__ int at[kRun], y[kRun + 1];
+  __shared__ float c[kRun];
+  const int n = head->valid;
+  const int p0 = blockIdx.x * kRun;
+  if (p0 >= n) return;
+  const int count = min(kRun, n - p0);
+  if (threadIdx.x < count) {
+    const int m = order[p0 + threadIdx.x];
+    at[threadIdx.x] = m;
+    c[threadIdx.x] = coef[m];
+    const int mine = sorted[p0 + threadIdx.x];
+    y[threadIdx.x] = mine;
+    if (p0 + threadIdx.x == 0 || sorted[p0 + threadIdx.x - 1] != mine) seg_first[mine] = p0 + threadIdx.x + 1;
+    if (p0 + threadIdx.x + 1 == n || sorted[p0 + threadIdx.x + 1] != mine) seg_end[mine] = p0 + threadIdx.x + 1;
+  }
+  __syncthreads();
+  for (int d = threadIdx.x * 8; d < Dp; d += 256 * 8) {
+    float s[8] = {};
+    int first = 0;
+#pragma unroll 4
+    for (int q = 0; q < count; ++q) {
+      float x[8];
+      load_planes8<P>(hp + static_cast<int64_t>(at[q]) * Dp + d, plane, x);
+      const float f = c[q];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = __fmaf_rn(f, x[j], s[j]);
+      if (q + 1 == count || y[q + 1] != y[q]) {
+        float4* out = reinterpret_cast<float4*>(seg_sum + (p0 + first) * lds + d);
+        out[0] = make_float4(s[0], s[1], s[2], s[3]);
+        out[1] = make_float4(s[4], s[5], s[6], s[7]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = 0.0f;
+        first = q + 1;
+      }
+    }
   }
 }
 
 // dh in the caller's type and order from the splits' sums; zero for tokens that
-// do not count.
+// do not count.  Times `scale` and plus `coef` times the target's row of w where given.
 template <typename E>
 __global__ void __launch_bounds__(256)
-    ce_dh_out_kernel(int T, int64_t D, const int* place, const float* sum, int64_t lds, int splits, int64_t sum_split,
-                     E* dh, int64_t lddh) {
+    ce_dh_out_kernel(int T, int D, int groups, const int* place, const float* sum, int64_t lds, int splits,
+                     int64_t sum_split, const float* scale, const float* coef, const E* __restrict__ w, int64_t ldw,
+                     const int* target, int wide_w, E* dh, int64_t lddh, int wide) {
   pdl_begin();
-  for (int t = blockIdx.x; t < T; t += gridDim.x) {
+  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(T) * groups;
+       q += gridDim.x * int64_t{256}) {
+    const int t = static_cast<int>(q / groups);
+    const int d = static_cast<int>(q - static_cast<int64_t>(t) * groups) * 8;
     const int m = place[t];
-    for (int64_t d = threadIdx.x; d < D; d += blockDim.x) {
-      float x = 0.0f;
-      if (m >= 0)
-        for (int i = 0; i < splits; ++i) x = fadd(x, sum[i * sum_split + m * lds + d]);
-      from_float(x, dh + t * lddh + d);
+    float x[8] = {};
+    if (m >= 0) {
+      for (int i = 0; i < splits; ++i) {
+        const float4* in = reinterpret_cast<const float4*>(sum + i * sum_split + m * lds + d);
+        const float4 a = in[0], b = in[1];
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fadd(x[j], v[j]);
+      }
+      if (coef != nullptr) {
+        const float s = scale != nullptr ? scale[m] : 1.0f, c = coef[m];
+        E y[8];
+        load8(w + target[m] * ldw + d, D - d, wide_w, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __fmaf_rn(c, to_float(y[j]), fmul(x[j], s));
+      }
+    }
+    E out[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) from_float(x[j], &out[j]);
+    E* to = dh + t * lddh + d;
+    if (wide && d + 8 <= D) {
+      uint4 u[sizeof(E) / 2];
+      memcpy(u, out, sizeof(out));
+#pragma unroll
+      for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) reinterpret_cast<uint4*>(to)[k] = u[k];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (d + j < D) to[j] = out[j];
     }
   }
 }
@@ -632,13 +487,24 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // The coefficients of a piece take 1 GiB at most (0.4 % of the memory; a shorter
 // vocabulary piece makes smaller products and more launches).
 constexpr int64_t kPieceBytes = int64_t{1} << 30;
+// A training step keeps the exponentials where they take 4 GiB at most and the
+// tokens are few enough to be ordered by counting pairs (16384: 2^28 pairs, 20 us);
+// beyond either it forms the logits twice, a third more operations.  So it does
+// for the tokens of one row tile: there the products wait for w, and an entry of
+// dw, a sum of few terms then, is spared one of its roundings (of g/s h); in bf16
+// the targets' c, which dominate such sums, are added to dh and dw in fp32.
+constexpr int64_t kKeptBytes = int64_t{4} << 30;
+constexpr int64_t kKeptTokens = 16384;
 constexpr int kMaxSplits = 8;
+
+enum Pass { kForward = 0, kBackward = 1, kTrain = 2 };
 
 struct Layout {
   size_t head, row, target, place, at_target, part, lse, h, w, coef, sum, total;
-  int parts, planes, splits;
-  bool pack_w;
-  int64_t piece, padded, Dp, lds, ldc;
+  size_t flags, pos, order, sorted, ref, sums, scale, factor, hs, seg_first, seg_end, seg_sum;  // kept
+  int parts, planes, tiles;
+  bool pack_w, kept, apart;
+  int64_t piece, padded, Dp, ldc;
 };
 
 // Parts of K for dh: full waves of the SMs for the least part sums.
@@ -658,7 +524,7 @@ int splits_for(int64_t T, int64_t D, int64_t piece) {
   return best;
 }
 
-Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, bool grad, int64_t piece, int64_t ldw) {
+Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piece, int64_t ldw) {
   Layout l = {};
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -669,6 +535,7 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, bool grad, int64_t pie
   l.planes = bf16 ? 1 : 3;
   l.pack_w = !bf16 || ldw < D || ldw % 8 != 0;
   l.padded = round_up(T, kPair);
+  l.tiles = static_cast<int>(l.padded / kPair);
   l.Dp = round_up(D, 8);
   l.parts = static_cast<int>((V + kHalf - 1) / kHalf);
   l.head = take(sizeof(Header));
@@ -680,14 +547,25 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, bool grad, int64_t pie
   l.part = take(static_cast<size_t>(l.parts) * T * 8);
   l.h = take(static_cast<size_t>(l.planes) * l.padded * l.Dp * 2);
   l.w = take(l.pack_w ? static_cast<size_t>(l.planes) * V * l.Dp * 2 : 0);
-  if (grad) {
-    const int64_t most = std::max<int64_t>(kN, kPieceBytes / (l.padded * 2 * l.planes) / kN * kN);
-    l.piece = std::min(V, piece > 0 ? piece : most);
-    l.ldc = round_up(l.piece, kN);
-    l.lds = round_up(D, 8);
-    l.splits = kMaxSplits;
-    l.coef = take(static_cast<size_t>(l.planes) * l.padded * l.ldc * 2);
-    l.sum = take(static_cast<size_t>(splits_for(T, D, l.piece)) * l.padded * l.lds * 4);
+  if (pass == kForward) {
+    l.total = at;
+    return l;
+  }
+  l.kept = pass == kTrain && T > kPair && T <= kKeptTokens && (piece == 0 || piece >= V) &&
+           l.padded * round_up(V, kN) * 2 * l.planes <= kKeptBytes;
+  const int64_t most = std::max<int64_t>(kN, kPieceBytes / (l.padded * 2 * l.planes) / kN * kN);
+  l.piece = l.kept ? V : std::min(V, piece > 0 ? piece : most);
+  l.ldc = round_up(l.piece, kN);
+  l.coef = take(static_cast<size_t>(l.planes) * l.padded * l.ldc * 2);
+  l.sum = take(static_cast<size_t>(splits_for(T, D, l.piece)) * l.padded * l.Dp * 4);
+  l.apart = !l.kept && bf16 && T <= kPair;
+  if (l.kept || l.apart) {
+    l.flags = take(round_up(l.tiles, kScan / kPair) * 4);
+    for (size_t* p : {&l.pos, &l.order, &l.sorted, &l.ref, &l.sums, &l.scale, &l.factor}) *p = take(T * 4);
+    l.hs = take(l.kept ? static_cast<size_t>(l.planes) * l.padded * l.Dp * 2 : 0);
+    l.seg_first = take(V * 4);
+    l.seg_end = take(V * 4);
+    l.seg_sum = take(static_cast<size_t>(T) * l.Dp * 4);
   }
   l.total = at;
   return l;
@@ -747,35 +625,41 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   constexpr bool bf16 = sizeof(E) == 2;
   constexpr int P = bf16 ? 1 : 3;
   const int T = static_cast<int>(a.T), D = static_cast<int>(a.D);
-  const int64_t ldw = (reinterpret_cast<uintptr_t>(a.w) & 15) == 0 ? a.ldw : 0;
-  const Layout l = layout(a.T, a.D, a.V, bf16, a.dw != nullptr, a.piece, ldw);
+  auto on16 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+  const int pass = a.dw == nullptr ? kForward : a.loss == nullptr ? kBackward : kTrain;
+  const Layout l = layout(a.T, a.D, a.V, bf16, pass, a.piece, on16(a.w) ? a.ldw : 0);
   char* ws = static_cast<char*>(a.ws);
+  auto ints = [&](size_t at) { return reinterpret_cast<int*>(ws + at); };
+  auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   Header* head = reinterpret_cast<Header*>(ws + l.head);
-  int* row = reinterpret_cast<int*>(ws + l.row);
-  int* target = reinterpret_cast<int*>(ws + l.target);
-  int* place = reinterpret_cast<int*>(ws + l.place);
+  int *row = ints(l.row), *target = ints(l.target), *place = ints(l.place);
   uint16_t* hp = reinterpret_cast<uint16_t*>(ws + l.h);
   uint16_t* wp = reinterpret_cast<uint16_t*>(ws + l.w);
-  CE_TRY(launch_kernel(ce_scan_kernel, dim3(1), dim3(1024), 0, s, 0, a.targets, T, a.V, a.ignore, head, row, target,
-                       place, a.status));
-  auto pack_grid = [&](int64_t rows) {
-    return dim3(static_cast<unsigned>(std::min<int64_t>((rows * (l.Dp / 8) + 255) / 256, num_sms * 16)));
-  };
-  CE_TRY(launch_kernel(ce_pack_kernel<E, P>, pack_grid(l.padded), dim3(256), 0, s, 0, static_cast<const E*>(a.h), a.ldh,
-                       row, &head->valid, a.T, l.padded, D, static_cast<int>(l.Dp), hp));
-  const void* w = a.w;
+  const E* h = static_cast<const E*>(a.h);
+  const E* w = static_cast<const E*>(a.w);
+  const int wide_h = on16(h) && a.ldh * sizeof(E) % 16 == 0, wide_w = on16(w) && a.ldw * sizeof(E) % 16 == 0;
+  const int wide_dh = on16(a.dh) && a.lddh * sizeof(E) % 16 == 0;
+  const int Dp = static_cast<int>(l.Dp);
+  const unsigned rows8 = static_cast<unsigned>(l.padded / 8), rows32 = static_cast<unsigned>((a.T + 31) / 32);
+  const bool by_target = l.kept || l.apart;
+  CE_TRY(launch_kernel(ce_scan_kernel, dim3(static_cast<unsigned>((a.T + kScan - 1) / kScan)), dim3(kScan), 0, s, 0,
+                       a.targets, T, a.V, a.ignore, head, row, target, place, by_target ? ints(l.pos) : nullptr,
+                       l.kept ? ints(l.flags) : nullptr, a.status));
+  CE_TRY(launch_kernel(ce_pack_h_kernel<E, P>, dim3(rows8), dim3(256), 0, s, 0, h, a.ldh, head, row, l.padded, D, Dp,
+                       wide_h, hp, w, a.ldw, target, wide_w, by_target ? floats(l.ref) : nullptr));
+  const void* wt = w;
   int64_t wld = a.ldw;
   if (l.pack_w) {
-    CE_TRY(launch_kernel(ce_pack_kernel<E, P>, pack_grid(a.V), dim3(256), 0, s, 0, static_cast<const E*>(a.w), a.ldw,
-                         static_cast<const int*>(nullptr), static_cast<const int*>(nullptr), a.V, a.V, D,
-                         static_cast<int>(l.Dp), wp));
-    w = wp;
+    const int64_t blocks = std::min<int64_t>((a.V * (Dp / 8) + 255) / 256, num_sms * 16);
+    CE_TRY(launch_kernel(ce_pack_w_kernel<E, P>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0, w, a.ldw, a.V, D,
+                         Dp, wide_w, wp));
+    wt = wp;
     wld = l.Dp;
   }
-  const int64_t hplane = l.padded * l.Dp, wplane = l.pack_w ? a.V * l.Dp : a.V * wld;
+  const int64_t hplane = l.padded * l.Dp, wplane = a.V * wld;
   CUtensorMap h_rows, w_rows;  // K = D contiguous
   CE_TRY(make_map(&h_rows, hp, D, l.padded, P, l.Dp, hplane, kM));
-  CE_TRY(make_map(&w_rows, w, D, a.V, P, wld, wplane, kM));
+  CE_TRY(make_map(&w_rows, wt, D, a.V, P, wld, wplane, kM));
   Gemm g = {};
   g.head = head;
   g.row = row;
@@ -785,62 +669,120 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.terms = bf16 ? 1 : 6;
   g.spin_limit = a.spin_limit;
   g.status = a.status;
-  // K blocks of an accumulator: 16 steps for the logits that the loss shows in
-  // fp32, 32 for fp32 gradients, any number where results are rounded to bf16
-  const int any = 1 << 30, few = 4, some = 8;
-  const int64_t mt = l.padded / kPair, dt = (a.D + kN - 1) / kN;
-  const float* lse = a.lse_in;
-  if (a.loss != nullptr) {
-    g.width = static_cast<int>(a.V);
-    g.part = reinterpret_cast<float2*>(ws + l.part);
-    g.at_target = reinterpret_cast<float*>(ws + l.at_target);
-    float* out = a.lse != nullptr ? a.lse : reinterpret_cast<float*>(ws + l.lse);
-    g.chunk = few;
-    CE_TRY(launch_gemm<kLoss>(h_rows, w_rows, g, mt * ((a.V + kN - 1) / kN), num_sms, s));
-    CE_TRY(launch_kernel(ce_finish_kernel, dim3((T + 7) / 8), dim3(256), 0, s, 0, T, place, g.part, l.parts, g.at_target,
-                         a.loss, out));
-    lse = out;
-  }
-  if (a.dw == nullptr) return cudaSuccess;
-  g.lse = lse;
-  g.gloss = a.gloss;
+  g.part = reinterpret_cast<float2*>(ws + l.part);
+  g.at_target = floats(l.at_target);
   g.coef = reinterpret_cast<uint16_t*>(ws + l.coef);
   g.ldc = l.ldc;
   g.coef_plane = l.padded * l.ldc;
-  g.sum = reinterpret_cast<float*>(ws + l.sum);
-  g.lds = l.lds;
-  g.sum_split = l.padded * l.lds;
-  g.splits = splits_for(a.T, a.D, l.piece);
+  g.sum = floats(l.sum);
+  g.lds = l.Dp;
+  g.sum_split = l.padded * l.Dp;
   g.dw = a.dw;
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
   g.dw_wide = (a.lddw * sizeof(E)) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 32 == 0;
-  CUtensorMap w_cols, h_cols;  // K = vocabulary, tokens: boxes of 64 columns x 64 k
-  CE_TRY(make_map(&w_cols, w, D, a.V, P, wld, wplane, kK));
+  // K blocks of an accumulator.  fp32 results: 8 steps for logits, 16 for gradients
+  // (six plane products keep the units busy for each).  bf16 gradients: any number.
+  // bf16 logits: 64 steps keep the mean over many tokens to 3e-7 of the loss; few
+  // tokens, where the products wait for memory anyway, get 8.
+  const int any = 1 << 30, few = 2, some = 4;
+  const int logits = bf16 && a.T > kPair ? 16 : few;
+  const int64_t mt = l.tiles, dt = (a.D + kN - 1) / kN, vt = (a.V + kN - 1) / kN;
+  const unsigned out_blocks =
+      static_cast<unsigned>(std::min<int64_t>((a.T * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
+  auto dh_out = [&](const float* scale, const float* coef) {
+    return launch_kernel(ce_dh_out_kernel<E>, dim3(out_blocks), dim3(256), 0, s, 0, T, D, Dp / 8, place, g.sum, g.lds,
+                         g.splits, g.sum_split, scale, coef, w, a.ldw, target, wide_w, static_cast<E*>(a.dh), a.lddh,
+                         wide_dh);
+  };
+  CUtensorMap w_cols, h_cols, c_rows, c_cols;  // K = vocabulary, tokens: boxes of 64 columns x 64 k
+  if (pass != kForward) CE_TRY(make_map(&w_cols, wt, D, a.V, P, wld, wplane, kK));
+
+  int* pos = ints(l.pos);
+  float *ref = floats(l.ref), *scale = floats(l.scale), *factor = floats(l.factor);
+  Finish f = {T, D, Dp, l.parts, a.V, l.padded, head, row, target, place, pos, ints(l.flags), g.part, g.at_target, ref,
+              floats(l.sums), a.gloss, hp, a.lse_in, nullptr, nullptr, scale, factor, ints(l.order), ints(l.sorted),
+              ints(l.seg_first), a.loss};
+  auto rank = [&] {
+    return launch_kernel(ce_rank_kernel, dim3(static_cast<unsigned>((a.T + 255) / 256), 8), dim3(256), 0, s, 0, head,
+                         target, pos);
+  };
+  auto by_targets = [&] {  // the factors, then the targets' part of dw
+    CE_TRY(launch_kernel(ce_scale_kernel<P>, dim3(rows8), dim3(256), 0, s, 0, f));
+    g.seg_first = f.seg_first;
+    g.seg_end = ints(l.seg_end);
+    g.seg_sum = floats(l.seg_sum);
+    return launch_kernel(ce_target_kernel<P>, dim3(static_cast<unsigned>((a.T + kRun - 1) / kRun)), dim3(256), 0, s, 0, head,
+                         f.order, f.sorted, factor, hp, hplane, Dp, f.seg_first, ints(l.seg_end), floats(l.seg_sum), l.Dp);
+  };
+
+  if (l.kept) {
+    uint16_t* hs = reinterpret_cast<uint16_t*>(ws + l.hs);
+    f.hs = hs;
+    CE_TRY(rank());
+    g.width = static_cast<int>(a.V);
+    g.ref = ref;
+    g.chunk = logits;
+    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    CE_TRY(launch_kernel(ce_sum_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, g.part, l.parts, floats(l.sums), ref,
+                         ints(l.flags)));
+    g.redo = ints(l.flags);
+    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    CE_TRY(by_targets());
+    CE_TRY(make_map(&h_cols, hs, D, l.padded, P, l.Dp, hplane, kK));
+    CE_TRY(make_map(&c_rows, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kM));
+    CE_TRY(make_map(&c_cols, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kK));
+    g.first = 1;
+    g.splits = splits_for(a.T, a.D, a.V);
+    g.chunk = bf16 ? any : some;
+    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, mt * dt * g.splits, num_sms, s));
+    CE_TRY(dh_out(scale, factor));
+    return launch_gemm<kDw>(c_cols, h_cols, g, (a.V + kPair - 1) / kPair * dt, num_sms, s);
+  }
+
+  const float* lse = a.lse_in;
+  if (a.loss != nullptr) {
+    float* out = a.lse != nullptr ? a.lse : floats(l.lse);
+    g.width = static_cast<int>(a.V);
+    g.chunk = logits;
+    CE_TRY(launch_gemm<kLoss>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    CE_TRY(launch_kernel(ce_finish_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, row, place, g.part, l.parts,
+                         g.at_target, a.loss, out));
+    lse = out;
+  }
+  if (pass == kForward) return cudaSuccess;
+  g.lse = lse;
+  g.gloss = a.gloss;
+  g.loss = a.loss;
+  if (l.apart) {
+    g.apart = 1;
+    f.lse = lse;
+    f.loss_in = a.loss;
+    CE_TRY(rank());
+    CE_TRY(by_targets());
+  }
+  g.splits = splits_for(a.T, a.D, l.piece);
   CE_TRY(make_map(&h_cols, hp, D, l.padded, P, l.Dp, hplane, kK));
   for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
     const int width = static_cast<int>(std::min(l.piece, a.V - v0));
-    const int64_t vt = (width + kN - 1) / kN;
     g.v0 = v0;
     g.width = width;
     g.first = v0 == 0;
-    CUtensorMap c_rows, c_cols;
     CE_TRY(make_map(&c_rows, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kM));
     CE_TRY(make_map(&c_cols, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kK));
     g.chunk = bf16 ? any : few;
-    CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, mt * ((width + kN - 1) / kN), num_sms, s));
     g.chunk = bf16 ? any : some;
     CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, mt * dt * g.splits, num_sms, s));
     CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, (width + kPair - 1) / kPair * dt, num_sms, s));
   }
-  return launch_kernel(ce_dh_out_kernel<E>, dim3(static_cast<unsigned>(std::min<int64_t>(a.T, 4096))), dim3(256), 0, s, 0,
-                       T, a.D, place, g.sum, l.lds, g.splits, g.sum_split, static_cast<E*>(a.dh), a.lddh);
+  return dh_out(nullptr, l.apart ? factor : nullptr);
 }
 
 }  // namespace
 
-size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int grad, int64_t piece, int64_t ldw) {
-  return layout(T, D, V, bf16 != 0, grad != 0, piece, ldw).total;
+size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int pass, int64_t piece, int64_t ldw) {
+  return layout(T, D, V, bf16 != 0, pass, piece, ldw).total;
 }
 
 cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s) {

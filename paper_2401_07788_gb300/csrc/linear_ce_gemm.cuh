@@ -1,0 +1,564 @@
+// linear_ce_gemm.cuh -- the matrix products of the linear cross entropy on the
+// tensor cores, with the softmax in their epilogues.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "tcgen05.cuh"
+
+namespace mpc {
+namespace {
+
+constexpr int kM = 128;        // rows of a CTA's output tile (lanes of tensor memory)
+constexpr int kPair = 2 * kM;  // rows of a CTA pair's output tile
+constexpr int kN = 256;        // columns of an output tile
+constexpr int kK = 64;         // K elements of a stage: 128 bytes, one swizzle row
+constexpr int kStages = 6;
+constexpr int kBytesA = kM * kK * 2;
+constexpr int kBytesB = kN / 2 * kK * 2;
+constexpr int kStageBytes = kBytesA + kBytesB;
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
+constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
+constexpr int kRun = 32;       // sorted tokens whose target gradients one CTA sums
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Header {
+  int valid;   // tokens that count
+  float mean;  // 1 / valid (0 when none counts)
+  int redo;    // some token's exponentials are formed again (see kExp)
+};
+
+// ---------------------------------------------------------------------------
+// Operands in bf16 planes.  A bf16 tensor is one plane.  An fp32 x is the sum of
+// three, x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1) (24 bits), and a
+// product of two fp32 tensors the sum of the plane products i + j <= 2, six of
+// them: what is left out is below 2^-24 of a term.  One kernel so serves both
+// types, an fp32 product being a bf16 one with six times the K steps.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
+  const __nv_bfloat16 a = __float2bfloat16_rn(x);
+  const float r = fsub(x, __bfloat162float(a));
+  const __nv_bfloat16 b = __float2bfloat16_rn(r);
+  const __nv_bfloat16 c = __float2bfloat16_rn(fsub(r, __bfloat162float(b)));
+  p[0] = __bfloat16_as_ushort(a);
+  p[1] = __bfloat16_as_ushort(b);
+  p[2] = __bfloat16_as_ushort(c);
+}
+
+// ---------------------------------------------------------------------------
+// The matrix products: C[m][n] = sum_k A[m][k] B[n][k] in 256 x 256 tiles.
+//
+// A persistent pair of CTAs on two SMs per tile, 128 rows each: every CTA copies
+// its rows of A and half the rows of B, so an SM reads 32 KB from L2 for 2^20
+// products (48 KB with a tile of its own).  Warp 0 copies operand tiles through
+// tensor maps (kStages stages of 32 KB a CTA), one thread of the first CTA's warp
+// 1 issues the products of both, eight warps a CTA take the finished tile from
+// tensor memory.  Two
+// accumulators of 256 columns fill the tensor memory, so a tile's epilogue runs
+// under the next tile's products.
+//
+// kLoss   A = h [valid][D],  B = w [V][D]: a tile's logits become, for each token
+//         and half tile, their largest and the sum of exponentials over it.
+// kExp    the same for a training step that keeps the exponentials: with a reference
+//         ref[t] near the logits, e = 2^(l log2e - ref) rounded to bf16 planes (its
+//         relative error is that of a rounded probability) and their sums.  The
+//         factor that makes them coefficients is applied where it is exact: to dh's
+//         sums, and to h for dw.  e of the target is 0: its coefficient p - 1 is a
+//         difference, and goes its own way in fp32.  ref is the target's logit, so a
+//         sum is out of range only for a token with a loss over 27; such tokens set
+//         a flag, take their largest logit as ref, and a second launch of the kernel
+//         (which returns at once without a flag) forms their row tiles again.
+// kCoef   the logits' products again, when lse is known: the coefficients c of a
+//         piece of the vocabulary, rounded to bf16 planes.
+// kDh     A = c [valid][piece], B = w^T [D][piece]: dh, K split over several CTAs
+//         where there are few tiles, each split's sum kept in fp32.
+// kDw     A = c^T [piece][valid], B = h^T [D][valid]: dw of the piece.
+//
+// An accumulator adds each product step with truncation: about 5e-9 of its value
+// a step of 16, always towards zero (measured: dh over 50257 entries 9e-5 off).
+// Where fp32 results depend on it, an accumulator sums a chunk of K blocks only,
+// the smallest plane products first, and the epilogue adds the chunks in fp32
+// with rounding to nearest; two accumulators in turn keep the products running.
+// Operands whose K is not the contiguous axis (w^T, c^T, h^T) are read as they
+// are: rows of 64 M/N-elements, and the product's descriptors say so.
+// ---------------------------------------------------------------------------
+enum Mode { kLoss, kExp, kCoef, kDh, kDw };
+
+struct Gemm {
+  const Header* head;
+  const int* row;       // token of a listed row
+  const int* target;
+  int T;                // tokens (upper bound of the list)
+  int D;
+  int width;            // vocabulary entries of the piece
+  int64_t v0;           // its first one
+  int terms;            // 1 (bf16) or 6 (fp32 in three planes)
+  int chunk;            // K blocks that one accumulator sums (see ce_gemm_kernel)
+  int splits;           // kDh: parts of K
+  int first;            // kDh: the piece that starts the sums
+  float2* part;         // kLoss, kExp: [half tile][T] (largest logit, sum), base 2
+  float* at_target;     // kLoss, kExp: [T]
+  const float* ref;     // kExp: [T]
+  const int* redo;      // kExp: nullptr, or the row tiles to form again
+  const int* seg_first; // kDw: nullptr, or per entry 1 + the first sorted token with that target (0: none)
+  const int* seg_end;   // kDw: the position after its last one
+  const float* seg_sum; // kDw: [T][lds], the tokens' sums at the first position of each run of kRun
+  const float* lse;     // kCoef: [T] by token
+  const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
+  const float* loss;    // kCoef: [T] by token where the forward pass gave it, or nullptr
+  int apart;            // kCoef: the target's c goes its own way in fp32
+  uint16_t* coef;       // kExp, kCoef: [plane][rows][ldc]
+  int64_t ldc, coef_plane;
+  float* sum;           // kDh: [split][rows][lds]
+  int64_t lds, sum_split;
+  void* dw;             // kDw
+  int64_t lddw;
+  int dw_bf16, dw_wide; // type; rows and base suit 32-byte stores
+  uint32_t spin_limit;
+  unsigned* status;
+};
+
+// Plane pair of a term, smallest products first.
+__device__ __forceinline__ void term_planes(int terms, int t, int* a, int* b) {
+  if (terms == 1) {
+    *a = *b = 0;
+  } else {  // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), two bits each
+    *a = (0x052 >> (2 * t)) & 3;
+    *b = (0x118 >> (2 * t)) & 3;
+  }
+}
+
+struct Tile {
+  int m0, n0, split, k0, k1;  // K blocks [k0, k1)
+};
+
+struct Shape {
+  int m_tiles, n_tiles, blocks, splits;
+  __device__ int total() const { return m_tiles * n_tiles * splits; }
+};
+
+template <int MODE>
+__device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
+  Shape s;
+  const int m = MODE == kDw ? g.width : valid;
+  const int n = MODE == kDh || MODE == kDw ? g.D : g.width;
+  const int k = MODE == kDh ? g.width : MODE == kDw ? valid : g.D;
+  s.m_tiles = (m + kPair - 1) / kPair;
+  s.n_tiles = (n + kN - 1) / kN;
+  s.blocks = (k + kK - 1) / kK;
+  s.splits = MODE == kDh ? g.splits : 1;
+  return s;
+}
+
+// Order of the tiles: those that run at the same time share operands in L2.  For
+// the logits all tokens pass one stretch of the vocabulary; for dh and dw the
+// columns of one row tile of c run together, so that c is read from HBM once.
+template <int MODE>
+__device__ __forceinline__ Tile tile_of(const Shape& s, int i) {
+  Tile t;
+  if (MODE == kLoss || MODE == kExp || MODE == kCoef) {
+    t.m0 = i % s.m_tiles * kPair;
+    t.n0 = i / s.m_tiles * kN;
+    t.split = 0;
+  } else {
+    t.n0 = i % s.n_tiles * kN;
+    i /= s.n_tiles;
+    t.m0 = i % s.m_tiles * kPair;
+    t.split = i / s.m_tiles;
+  }
+  t.k0 = static_cast<int>(static_cast<int64_t>(s.blocks) * t.split / s.splits);
+  t.k1 = static_cast<int>(static_cast<int64_t>(s.blocks) * (t.split + 1) / s.splits);
+  return t;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  uint32_t u;
+  memcpy(&u, &p, 4);
+  return u;
+}
+
+// A lane's row of a half tile as bf16 planes of the coefficients.
+__device__ __forceinline__ void store_planes(const Gemm& g, int64_t m, int n0, const float (&x)[kHalf]) {
+  uint16_t* out = g.coef + m * g.ldc + n0;
+  if (g.terms == 1) {
+#pragma unroll
+    for (int j = 0; j < kHalf; j += 16) {
+      uint32_t u[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
+      st_v8(out + j, u);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kHalf; j += 16) {
+      uint32_t u[3][8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        uint16_t a[3], b[3];
+        split(x[j + 2 * q], a);
+        split(x[j + 2 * q + 1], b);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) u[k][q] = a[k] | static_cast<uint32_t>(b[k]) << 16;
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) st_v8(out + k * g.coef_plane + j, u[k]);
+    }
+  }
+}
+
+// One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
+template <int MODE>
+__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf]) {
+  if (MODE == kLoss || MODE == kExp) {
+    const int cols = min(g.width - n0, kHalf);
+    if (MODE == kLoss && (cols <= 0 || m >= valid)) return;
+    if (MODE == kExp && (n0 >= g.ldc)) return;
+    const bool live = m < valid;
+    if (live && cols > 0) {
+      const int y = static_cast<int>(g.target[m] - n0);
+      if (cols < kHalf) {
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j)
+          if (j >= cols) x[j] = -INFINITY;
+      }
+      const bool here = y >= 0 && y < cols;
+      if (here) {
+        float v = x[0];
+#pragma unroll
+        for (int j = 1; j < kHalf; ++j) v = j == y ? x[j] : v;
+        g.at_target[m] = v;
+      }
+      // base 2 throughout: exp(l - top) = 2^(l log2e - top log2e), one rounding in the exponent
+      float top = x[0];
+#pragma unroll
+      for (int j = 1; j < kHalf; ++j) top = fmaxf(top, x[j]);
+      const float base = fmul(top, kLog2e);
+      const float shift = MODE == kExp ? -g.ref[m] : base == -INFINITY ? 0.0f : -base;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < kHalf; ++j) {
+        const float e = exp2_approx(__fmaf_rn(x[j], kLog2e, shift));
+        sum[j & 3] = fadd(sum[j & 3], e);
+        if (MODE == kExp) x[j] = e;
+      }
+      g.part[static_cast<int64_t>(n0 / kHalf) * g.T + m] =
+          make_float2(base, fadd(fadd(sum[0], sum[1]), fadd(sum[2], sum[3])));
+      if (MODE == kExp && here) {
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j)
+          if (j == y) x[j] = 0.0f;
+      }
+    }
+    if (MODE == kExp) {
+      if (!live) {
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) x[j] = 0.0f;
+      }
+      store_planes(g, m, n0, x);
+    }
+  } else if (MODE == kCoef) {
+    if (n0 >= g.ldc) return;
+    const bool live = m < valid;
+    float shift = 0.0f, scale = 0.0f, at_y = 0.0f;
+    int y = -1;
+    if (live) {
+      const int token = g.row[m];
+      const float lse = g.lse[token];
+      const float weight = g.gloss != nullptr ? g.gloss[token] : g.head->mean;
+      // what the rounding of lse log2e leaves out goes into the factor
+      shift = fmul(lse, -kLog2e);
+      scale = fmul(weight, exp2f(-__fmaf_rn(lse, kLog2e, shift)));
+      y = static_cast<int>(g.target[m] - g.v0 - n0);
+      if (y >= 0 && y < kHalf && !g.apart) {  // p - 1 from the loss, not as a difference
+        float v = x[0];
+#pragma unroll
+        for (int j = 1; j < kHalf; ++j) v = j == y ? x[j] : v;
+        at_y = fmul(weight, expm1f(g.loss != nullptr ? -g.loss[token] : fsub(v, lse)));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j)
+      x[j] = live ? fmul(scale, exp2_approx(__fmaf_rn(x[j], kLog2e, shift))) : 0.0f;
+    if (y >= 0 && y < kHalf) {
+#pragma unroll
+      for (int j = 0; j < kHalf; ++j)
+        if (j == y) x[j] = at_y;
+    }
+    store_planes(g, m, n0, x);
+  } else if (MODE == kDh) {
+    if (m >= valid) return;
+    float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
+#pragma unroll
+    for (int j = 0; j < kHalf; j += 8) {
+      if (n0 + j < g.lds) {
+        uint32_t u[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          if (!g.first) x[j + q] = fadd(x[j + q], out[j + q]);
+          u[q] = __float_as_uint(x[j + q]);
+        }
+        st_v8(out + j, u);
+      }
+    }
+  } else {
+    if (m >= g.width) return;
+    if (g.seg_first != nullptr) {  // the tokens whose target this entry is
+      const int first = g.seg_first[g.v0 + m];
+      if (first > 0) {
+        const int end = g.seg_end[g.v0 + m];
+        for (int p = first - 1; p < end; p = (p / kRun + 1) * kRun) {
+          const float* add = g.seg_sum + p * g.lds + n0;
+#pragma unroll
+          for (int j = 0; j < kHalf; j += 4) {
+            if (n0 + j < g.D) {
+              const float4 v = *reinterpret_cast<const float4*>(add + j);
+              x[j] = fadd(x[j], v.x);
+              x[j + 1] = fadd(x[j + 1], v.y);
+              x[j + 2] = fadd(x[j + 2], v.z);
+              x[j + 3] = fadd(x[j + 3], v.w);
+            }
+          }
+        }
+      }
+    }
+    const int64_t at = (g.v0 + m) * g.lddw + n0;
+    if (g.dw_bf16) {
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.dw) + at;
+#pragma unroll
+      for (int j = 0; j < kHalf; j += 16) {
+        if (g.dw_wide && n0 + j + 16 <= g.D) {
+          uint32_t u[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
+          st_v8(out + j, u);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (n0 + j + q < g.D) out[j + q] = __float2bfloat16_rn(x[j + q]);
+        }
+      }
+    } else {
+      float* out = static_cast<float*>(g.dw) + at;
+#pragma unroll
+      for (int j = 0; j < kHalf; j += 8) {
+        if (g.dw_wide && n0 + j + 8 <= g.D) {
+          uint32_t u[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[j + q]);
+          st_v8(out + j, u);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (n0 + j + q < g.D) out[j + q] = x[j + q];
+        }
+      }
+    }
+  }
+}
+
+template <int MODE>
+__device__ __forceinline__ bool skipped(const Gemm& g, const Tile& t) {
+  return MODE == kExp && g.redo != nullptr && g.redo[t.m0 / kPair] == 0;
+}
+
+// Columns of a tile that the product forms: a multiple of 16.  Each CTA of the
+// pair holds half of them as rows of B.
+__device__ __forceinline__ int tile_cols(int cols, int n0) { return min((cols - n0 + 15) / 16 * 16, kN); }
+
+template <int MODE>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const __grid_constant__ Gemm g) {
+  constexpr bool A_MN = MODE == kDw, B_MN = MODE == kDh || MODE == kDw;
+  extern __shared__ uint8_t raw[];
+  // full and taken are used in the first CTA, for both; empty and done in each
+  __shared__ uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
+  __shared__ uint32_t tmem;
+  uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_rank());
+  if (MODE == kExp && g.redo != nullptr) {
+    pdl_begin();
+    if (g.head->redo == 0) return;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&done[i], 1);
+      mbar_init(&taken[i], 2 * kEpiWarps);
+    }
+    mbar_init(&drain, 1);
+    fence_mbar_init();
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+  }
+  if (warp == 1) tmem_alloc(&tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t acc = tmem;
+  pdl_begin();
+  const int valid = g.head->valid;
+  const Shape s = shape_of<MODE>(g, valid);
+  const int total = s.total();
+  const int cols = MODE == kDh || MODE == kDw ? g.D : g.width;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      fence_proxy_async_all();  // operands that earlier kernels wrote
+      uint32_t it = 0;
+      bool ok = true;
+      for (int i = pair; i < total && ok; i += pairs) {
+        const Tile t = tile_of<MODE>(s, i);
+        if (skipped<MODE>(g, t)) continue;
+        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(cols, t.n0) / 2);
+        for (int c = t.k0; c < t.k1 && ok; c += g.chunk) {
+          const int blocks = min(g.chunk, t.k1 - c);
+          for (int j = 0; j < blocks * g.terms; ++j, ++it) {
+            const int kb = c + j % blocks;
+            const int st = it % kStages;
+            ok = mbar_wait_bounded(&empty[st], (it / kStages & 1) ^ 1, g.spin_limit, g.status);
+            if (!ok) break;
+            int pa, pb;
+            term_planes(g.terms, j / blocks, &pa, &pb);
+            uint8_t* a = stage0 + st * kStageBytes;
+            uint8_t* b = a + kBytesA;
+            const uint32_t bar = dsmem_addr(&full[st], 0);
+            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kStageBytes);
+            if (A_MN) {
+#pragma unroll
+              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, pa, bar);
+            } else {
+              tensor_g2s(a, &map_a, kb * kK, m0, pa, bar);
+            }
+            if (B_MN) {
+              const int k_at = kb * kK + (MODE == kDh ? static_cast<int>(g.v0) : 0);
+#pragma unroll
+              for (int q = 0; q < kN / 128; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
+            } else {
+              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, pb, bar);
+            }
+          }
+        }
+      }
+      // Copies in flight must land before either CTA leaves (the cluster barrier
+      // below).  The first CTA sees both CTAs' copies arrive; where a wait gave up,
+      // the second one may have sent some that the first no longer counts, and
+      // gives them a millisecond.
+      if (rank == 0) {
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+          mbar_wait_bounded(&full[i % kStages], i / kStages & 1, kDrainPolls, g.status);
+      } else if (!ok) {
+        const uint64_t until = global_ns() + 1000000;
+        while (global_ns() < until) __nanosleep(1000);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t it = 0, n = 0;
+      bool ok = true;
+      for (int i = pair; i < total && ok; i += pairs) {
+        const Tile t = tile_of<MODE>(s, i);
+        if (skipped<MODE>(g, t)) continue;
+        const uint32_t idesc = mma_desc(kPair, tile_cols(cols, t.n0), A_MN, B_MN);
+        for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
+          ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
+          tc_fence_after();
+          const uint32_t d = acc + (n & 1) * kN;
+          bool fresh = true;
+          const int steps = min(g.chunk, t.k1 - c) * g.terms;
+          for (int k = 0; k < steps && ok; ++k, ++it) {
+            const int st = it % kStages;
+            ok = mbar_wait_bounded(&full[st], it / kStages & 1, g.spin_limit, g.status);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = smem_addr(stage0 + st * kStageBytes), b = a + kBytesA;
+#pragma unroll
+            for (int q = 0; q < kK / 16; ++q) {
+              // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
+              const uint64_t da = A_MN ? smem_desc(a + q * 2048, kK * 128, 1024) : smem_desc(a + q * 32, 16, 1024);
+              const uint64_t db = B_MN ? smem_desc(b + q * 2048, kK * 128, 1024) : smem_desc(b + q * 32, 16, 1024);
+              mma_bf16(d, da, db, idesc, fresh);
+              fresh = false;
+            }
+            mma_commit_pair(&empty[st]);
+          }
+          if (ok) mma_commit_pair(&done[n & 1]);
+        }
+      }
+      if (!ok) {  // products in flight must end before the tensor memory is given back
+        mma_commit(&drain);
+        mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    uint32_t n = 0;
+    bool ok = true;
+    for (int i = pair; i < total; i += pairs) {
+      const Tile t = tile_of<MODE>(s, i);
+      if (skipped<MODE>(g, t)) continue;
+      float x[kHalf];
+      if (t.k0 == t.k1) {
+#pragma unroll
+        for (int q = 0; q < kHalf; ++q) x[q] = 0.0f;
+      }
+      for (int c = t.k0; c < t.k1; c += g.chunk, ++n) {
+        ok = mbar_wait_bounded(&done[n & 1], n / 2 & 1, g.spin_limit, g.status);
+        ok = __all_sync(kFull, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t at = acc + (n & 1) * kN + half * kHalf + (static_cast<uint32_t>(quad * 32) << 16);
+        if (c == t.k0) {
+#pragma unroll
+          for (int q = 0; q < kHalf; q += 32) tmem_ld32(at + q, x + q);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j) asm volatile("" : "+f"(x[j]));  // nothing uses x before the wait
+        } else {
+#pragma unroll
+          for (int q = 0; q < kHalf; q += 64) {
+            float y[64];
+            tmem_ld32(at + q, y);
+            tmem_ld32(at + q + 32, y + 32);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 64; ++j) {
+              asm volatile("" : "+f"(y[j]));
+              x[q + j] = fadd(x[q + j], y[j]);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+      }
+      if (!ok) break;
+      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // nothing signals or reads the other CTA's shared memory any more
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(acc, 512);
+  }
+}
+
+}  // namespace
+}  // namespace mpc

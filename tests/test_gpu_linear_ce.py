@@ -309,3 +309,42 @@ def test_autograd(mpc):
             assert err < 2e-5, (reduction, err)
         with torch.no_grad():
             assert float((head(h, y).double() - ref).norm() / ref.norm()) < 2e-5
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["plain", "hopeless", "one row", "same target", "weights"])
+def test_exponentials_kept(mpc, dtype, kind):
+    """Training that forms the logits once (more tokens than a row tile): ordinary tokens, losses far
+    beyond exp's range in some row tiles, one such token alone, runs of one target that span several
+    sums, given weights.  In bf16 a term of dw takes two roundings of up to 2^-8 (the exponential's,
+    the scaled hidden state's): the tolerance for c gets one more of them."""
+    T, D, V = 700, 72, 900
+    h, w, y = inputs(T, D, V, dtype, seed=20, ignored=0.1)
+    gloss = None
+    if kind in ("hopeless", "one row"):
+        w = (w.float() / w.float().norm(dim=1, keepdim=True)).to(dtype)
+        lot = torch.arange(T, device="cuda") == 650 if kind == "one row" else \
+            (torch.arange(T, device="cuda") % 3 == 0) & (torch.arange(T, device="cuda") < 500)
+        y[650] = 17
+        sign = torch.where(torch.arange(T, device="cuda") % 2 == 0, -400.0, 400.0)[:, None]
+        h = torch.where((lot & (y >= 0))[:, None], (w.float()[y.clamp_min(0)] * sign).to(dtype), h)
+    elif kind == "same target":
+        y[y >= 0] = torch.where(y[y >= 0] % 4 == 0, y[y >= 0], 5)
+    elif kind == "weights":
+        gloss = torch.randn(T, device="cuda")
+    want = oracle(h, w, y, gloss)
+    if dtype == torch.bfloat16:
+        rows = (y != -100).nonzero()[:, 0]
+        hd, wd = h[rows].double(), w.double()
+        c = torch.softmax(hd @ wd.t(), 1)
+        c[torch.arange(len(rows), device="cuda"), y[rows]] -= 1.0
+        c *= (torch.full((len(rows),), 1.0 / len(rows), device="cuda") if gloss is None else gloss[rows]).double()[:, None]
+        want["dw"] = (want["dw"][0], want["dw"][1] + 2.0 ** -8 * (c.abs().t() @ hd.abs()))
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, w, y, gloss)
+    near(loss, want["loss"], "loss")
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
+    again = mpc.mpc_linear_ce_train(h, w, y, gloss)
+    for a, b in zip((loss, dh, dw), again):
+        assert torch.equal(a, b)
+    assert mpc.mpc_get_status() == 0
