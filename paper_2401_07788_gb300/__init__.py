@@ -12,6 +12,7 @@ the library.  Every operator runs in the library's kernels; there is no fallback
 
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -130,6 +131,13 @@ def _ptr(t: torch.Tensor | None):
 def _stream(stream) -> ctypes.c_void_p:
     s = torch.cuda.current_stream() if stream is None else stream
     return _VP(s.cuda_stream)
+
+
+def _raw_stream(stream) -> int:
+    """The same as an integer, without making a stream object for the current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _cuda(t: torch.Tensor, dtype: torch.dtype, name: str) -> torch.Tensor:
@@ -443,6 +451,10 @@ def _matrix(t: torch.Tensor, name: str, cols: int | None = None, like=None) -> i
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _address(t) -> int | None:
+    return None if t is None else t.data_ptr()
+
+
 def _on(stream, *tensors):
     """Tells the allocator that a call on `stream` uses what was allocated for it here."""
     if stream is not None:
@@ -498,9 +510,9 @@ def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, ls
     _on(stream, *new)
     _vector(loss, T, torch.float32, "loss", h.device)
     _vector(lse, T, torch.float32, "lse", h.device)
-    _check(lib().mpc_linear_ce_forward(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), T, D, V,
-                                       _DTYPES[h.dtype], ignore_index, _ptr(loss), _ptr(lse),
-                                       _ptr(ws), wsb, _stream(stream)))
+    _check(lib().mpc_linear_ce_forward(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), T, D, V,
+                                       _DTYPES[h.dtype], ignore_index, loss.data_ptr(), lse.data_ptr(),
+                                       _address(ws), wsb, _raw_stream(stream)))
     return loss, lse
 
 
@@ -528,10 +540,10 @@ def mpc_linear_ce_backward(h, w, targets, lse, gloss=None, ignore_index: int = -
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
     dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
-    _check(lib().mpc_linear_ce_backward(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), _ptr(lse),
-                                        _ptr(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece,
-                                        _ptr(dh), lddh, _ptr(dw), lddw, _ptr(ws), wsb,
-                                        _stream(stream)))
+    _check(lib().mpc_linear_ce_backward(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), lse.data_ptr(),
+                                        _address(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece,
+                                        dh.data_ptr(), lddh, dw.data_ptr(), lddw, _address(ws), wsb,
+                                        _raw_stream(stream)))
     return dh, dw
 
 
@@ -547,9 +559,9 @@ def mpc_linear_ce_train(h, w, targets, gloss=None, ignore_index: int = -100, pie
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
     dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
-    _check(lib().mpc_linear_ce_train(_ptr(h), ldh, _ptr(w), ldw, _ptr(targets), _ptr(gloss), T, D,
-                                     V, _DTYPES[h.dtype], ignore_index, piece, _ptr(loss), _ptr(dh),
-                                     lddh, _ptr(dw), lddw, _ptr(ws), wsb, _stream(stream)))
+    _check(lib().mpc_linear_ce_train(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), _address(gloss), T, D,
+                                     V, _DTYPES[h.dtype], ignore_index, piece, loss.data_ptr(), dh.data_ptr(),
+                                     lddh, dw.data_ptr(), lddw, _address(ws), wsb, _raw_stream(stream)))
     return loss, dh, dw
 
 
@@ -566,8 +578,8 @@ def mpc_adamw_step(plan, lr: float, beta1: float, beta2: float, eps: float, step
     if grad_norm is not None:
         _vector(grad_norm, 1, torch.float32, "grad_norm", plan.device)
     _check(lib().mpc_adamw_step(plan.table, plan.count, plan.param_type, plan.grad_type,
-                                plan.state_bits, lr, beta1, beta2, eps, step, _ptr(grad_norm),
-                                max_norm, _stream(stream)))
+                                plan.state_bits, lr, beta1, beta2, eps, step, _address(grad_norm),
+                                max_norm, _raw_stream(stream)))
 
 
 def mpc_adamw_decode(plan, m_out, v_out, stream=None):
@@ -575,14 +587,17 @@ def mpc_adamw_decode(plan, m_out, v_out, stream=None):
     m_out and v_out (one for each tensor of the plan)."""
     if plan.state_bits != 8:
         raise MpcError(1, "the plan's states are not 8-bit codes")
-    if len(m_out) != plan.count or len(v_out) != plan.count:
-        raise MpcError(1, "m_out and v_out must hold one tensor for each of the plan's %d" % plan.count)
+    lists = []
     for name, outs in (("m_out", m_out), ("v_out", v_out)):
+        if len(outs) != plan.count:
+            raise MpcError(1, "%s must hold one tensor for each of the plan's %d" % (name, plan.count))
         for t, n in zip(outs, plan.sizes):
-            _vector(t, n, torch.float32, name, plan.device)
-    array = _VP * max(1, plan.count)
-    _check(lib().mpc_adamw_decode(plan.table, plan.count, array(*[t.data_ptr() for t in m_out]),
-                                  array(*[t.data_ptr() for t in v_out]), _stream(stream)))
+            if (t.dtype is not torch.float32 or t.get_device() != plan.index or t.numel() != n
+                    or not t.is_contiguous()):
+                _vector(t, n, torch.float32, name, plan.device)
+        lists.append(array.array("Q", [t.data_ptr() for t in outs]))
+    _check(lib().mpc_adamw_decode(plan.table, plan.count, lists[0].buffer_info()[0],
+                                  lists[1].buffer_info()[0], _raw_stream(stream)))
     return m_out, v_out
 
 
@@ -591,17 +606,21 @@ def mpc_grad_norm_workspace_bytes(count: int) -> int:
 
 
 def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
-    """The 2-norm of all gradients of an ``AdamWPlan`` together, as a device fp32 of one entry."""
+    """The 2-norm of all gradients of an ``AdamWPlan`` together, as a device fp32 of one entry.
+    Without ``ws`` the plan's own workspace is used: calls on one plan are to be ordered."""
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=plan.device)
         _on(stream, norm)
     _vector(norm, 1, torch.float32, "norm", plan.device)
-    given = ws
-    ws, wsb = _workspace(mpc_grad_norm_workspace_bytes(plan.count), ws, plan.device)
-    if given is None:
+    if ws is None:
+        if plan.norm_ws is None:
+            plan.norm_ws = torch.empty(mpc_grad_norm_workspace_bytes(plan.count), dtype=torch.uint8,
+                                       device=plan.device)
+        ws = plan.norm_ws
         _on(stream, ws)
-    _check(lib().mpc_grad_norm(plan.table, plan.count, plan.grad_type, _ptr(norm), _ptr(ws), wsb,
-                               _stream(stream)))
+    wsb = ws.numel() * ws.element_size()
+    _check(lib().mpc_grad_norm(plan.table, plan.count, plan.grad_type, norm.data_ptr(), _address(ws), wsb,
+                               _raw_stream(stream)))
     return norm
 
 

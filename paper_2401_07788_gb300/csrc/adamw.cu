@@ -87,6 +87,20 @@ __device__ __forceinline__ void my_range(const Table<N>& t, int* c0, int* c1, in
   *at = lo;
 }
 
+// Calls f(entry, k0, k1) for each tensor's chunks k0..k1-1 in this CTA's range.
+template <int N, class F>
+__device__ __forceinline__ void for_range(const Table<N>& t, F f) {
+  int c, c1, at;
+  my_range(t, &c, &c1, &at);
+  while (c < c1) {
+    const Entry& e = t.e[at];
+    const int end = at + 1 < t.count ? min(c1, t.e[at + 1].first) : c1;
+    f(e, c - e.first, end - e.first);
+    c = end;
+    ++at;
+  }
+}
+
 __device__ __forceinline__ float bf_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
@@ -160,17 +174,25 @@ __device__ __forceinline__ void store_codes(void* p, int64_t i, int left, bool w
   }
 }
 
+// Byte j of a word as a float: the bits of 2^23 + byte, less 2^23 (exact, and two
+// full-rate instructions where an integer conversion runs at a quarter rate).
+__device__ __forceinline__ float byte_float(uint32_t u, int j, float less) {
+  return fsub(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 | j)), less);
+}
+constexpr float kTwo23 = 8388608.0f;
+
 // The squares of a code are exact in fp32, so a value carries three (m) or four
-// (v) roundings.
-__device__ __forceinline__ float decode_m(uint32_t u, int j, float s) {
-  const float c = static_cast<float>(static_cast<int8_t>(u >> (8 * j)));
+// (v) roundings.  Signed codes are read with their sign bit flipped (c + 128).
+__device__ __forceinline__ float decode_m(uint32_t flipped, int j, float s) {
+  const float c = byte_float(flipped, j, kTwo23 + 128.0f);
   return fmul(fmul(fmul(c, fabsf(c)), static_cast<float>(1.0 / (127.0 * 127.0))), s);
 }
 __device__ __forceinline__ float decode_v(uint32_t u, int j, float s) {
-  const float c = static_cast<float>((u >> (8 * j)) & 0xffu);
+  const float c = byte_float(u, j, kTwo23);
   const float c2 = fmul(c, c);
   return fmul(fmul(fmul(c2, c2), static_cast<float>(1.0 / (255.0 * 255.0 * 255.0 * 255.0))), s);
 }
+constexpr uint32_t kFlip = 0x80808080u;
 
 // 1/top, or 0 for a block without a value in the normal range (its codes are 0).
 __device__ __forceinline__ float inverse(float top) {
@@ -179,25 +201,40 @@ __device__ __forceinline__ float inverse(float top) {
 
 __device__ __forceinline__ float root_approx(float x) {
   float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float root_any(float x) {  // subnormals too
+  float r;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
-// The code of y in [0, 1]: how many midpoints lie at or below it.  The midpoint
-// under code c of LEVELS is K (2c(c-1) + 1), K = 1/(2 LEVELS^2), halfway between
-// the neighbouring squares, and its square for FOURTH (v).  c - 1/2 is the
+// The code of y in [0, 1] as a float: how many midpoints lie at or below it.  The
+// midpoint under code c of LEVELS is K (2c(c-1) + 1), K = 1/(2 LEVELS^2), halfway
+// between the neighbouring squares, and its square for FOURTH (v).  c - 1/2 is the
 // root of LEVELS^2 y - 1/4 there, so an approximate root, lowered by 1e-3 (its
-// error in c is below 2e-4), gives the code or the one before it, and the exact
-// midpoint decides: the result does not depend on the approximation.
+// error in c is below 2e-4) and rounded, gives the code or the one before it, and
+// the exact midpoint decides: the result does not depend on the approximation.
+// (2c(c+1) + 1 is exact in fp32.)  NaN gives 0.
 template <int LEVELS, bool FOURTH>
-__device__ __forceinline__ int encode(float y) {
+__device__ __forceinline__ float encode(float y) {
   constexpr float K = static_cast<float>(1.0 / (2.0 * LEVELS * LEVELS));
   const float s = FOURTH ? root_approx(y) : y;
   const float z = fmaxf(__fmaf_rn(s, static_cast<float>(LEVELS * LEVELS), -0.25f), 0.0f);
-  int c = min(static_cast<int>(fadd(root_approx(z), 0.499f)), LEVELS - 1);
-  float mid = fmul(static_cast<float>(2 * c * (c + 1) + 1), K);
+  const float c = fsub(fadd(fsub(root_approx(z), 1e-3f), kTwo23), kTwo23);
+  const float up = fadd(c, 1.0f);
+  float mid = fmul(__fmaf_rn(fadd(c, c), up, 1.0f), K);
   if (FOURTH) mid = fmul(mid, mid);
-  return y >= mid ? c + 1 : c;
+  return y >= mid ? up : c;
+}
+
+// The low bytes of four floats in [2^23, 2^23 + 256) as one word.
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  const uint32_t lo = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+  const uint32_t hi = __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
 }
 
 __device__ __forceinline__ float warp_max(float x) {  // x >= 0 or NaN
@@ -214,76 +251,77 @@ __global__ void __launch_bounds__(kThreads)
     if (!(norm <= 3.402823466e38f)) return;  // not finite: the step is skipped
     if (k.max_norm > 0.0f) clip = fminf(fdiv(k.max_norm, fadd(norm, 1e-6f)), 1.0f);
   }
-  int c0, c1, at;
-  my_range(t, &c0, &c1, &at);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int c = c0; c < c1; ++c) {
-    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
-    const Entry& e = t.e[at];
-    const int64_t base = static_cast<int64_t>(c - e.first) * kChunk + warp * (32 * kLane);
-    if (base >= e.n) continue;
-    const int64_t i = base + lane * kLane;
-    const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+  for_range(t, [&](const Entry& e, int k0, int k1) {
     const bool wide = e.wide;
-    float p[8], g[8], m[8], v[8];
-    load8(static_cast<const G*>(e.grad), i, left, wide, g);
-    load8(static_cast<const P*>(e.param), i, left, wide, p);
-    const int64_t block = base >> 8;
-    if (BITS == 32) {
-      load8(static_cast<const float*>(e.m), i, left, wide, m);
-      load8(static_cast<const float*>(e.v), i, left, wide, v);
-    } else {
-      const uint2 um = load_codes(e.m, i, left, wide), uv = load_codes(e.v, i, left, wide);
-      const float sm = e.sm[block], sv = e.sv[block];
+    const float keep = e.keep, rate = e.step;
+    for (int chunk = k0; chunk < k1; ++chunk) {
+      const int64_t base = static_cast<int64_t>(chunk) * kChunk + warp * (32 * kLane);
+      if (base >= e.n) break;  // the tensor's last chunk
+      const int64_t i = base + lane * kLane;
+      const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+      float p[8], g[8], m[8], v[8];
+      load8(static_cast<const G*>(e.grad), i, left, wide, g);
+      load8(static_cast<const P*>(e.param), i, left, wide, p);
+      const int64_t block = base >> 8;
+      if (BITS == 32) {
+        load8(static_cast<const float*>(e.m), i, left, wide, m);
+        load8(static_cast<const float*>(e.v), i, left, wide, v);
+      } else {
+        const uint2 um = load_codes(e.m, i, left, wide), uv = load_codes(e.v, i, left, wide);
+        const float sm = e.sm[block], sv = e.sv[block];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          m[j] = decode_m((j < 4 ? um.x : um.y) ^ kFlip, j & 3, sm);
+          v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+        }
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        m[j] = decode_m(j < 4 ? um.x : um.y, j & 3, sm);
-        v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+        const float gj = fmul(g[j], clip);
+        m[j] = fadd(fmul(m[j], k.b1), fmul(gj, k.c1));
+        v[j] = fadd(fmul(v[j], k.b2), fmul(fmul(gj, k.c2), gj));
+        // 8-bit states are bound by instructions: the root and the quotient, which
+        // reach param alone, are the 1 and 2 ulp ones there
+        const float root = BITS == 32 ? __fsqrt_rn(v[j]) : root_any(v[j]);
+        const float under = fadd(fmul(root, k.rs), k.eps);
+        const float quotient = BITS == 32 ? fdiv(m[j], under) : __fdividef(m[j], under);
+        p[j] = fsub(fmul(p[j], keep), fmul(quotient, rate));
+      }
+      store8(static_cast<P*>(e.param), i, left, wide, p);
+      if (e.copy != nullptr) store8(static_cast<__nv_bfloat16*>(e.copy), i, left, wide, p);
+      if (BITS == 32) {
+        store8(static_cast<float*>(e.m), i, left, wide, m);
+        store8(static_cast<float*>(e.v), i, left, wide, v);
+      } else {
+        float tm = 0.0f, tv = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (j >= left) m[j] = v[j] = 0.0f;
+          tm = fmaxf(tm, fabsf(m[j]));
+          tv = fmaxf(tv, v[j]);
+        }
+        tm = warp_max(tm);
+        tv = warp_max(tv);
+        const float im = inverse(tm), iv = inverse(tv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          m[j] = fadd(copysignf(encode<127, false>(fmul(fabsf(m[j]), im)), m[j]), kTwo23 + 128.0f);
+          const float y = fmul(v[j], iv);
+          const float c = encode<255, true>(y);
+          v[j] = fadd(y > 0.0f ? fmaxf(c, 1.0f) : c, kTwo23);
+        }
+        store_codes(e.m, i, left, wide,
+                    make_uint2(low_bytes(m[0], m[1], m[2], m[3]) ^ kFlip, low_bytes(m[4], m[5], m[6], m[7]) ^ kFlip));
+        store_codes(e.v, i, left, wide,
+                    make_uint2(low_bytes(v[0], v[1], v[2], v[3]), low_bytes(v[4], v[5], v[6], v[7])));
+        if (lane == 0) {
+          e.sm[block] = tm;
+          e.sv[block] = tv;
+        }
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gj = fmul(g[j], clip);
-      m[j] = fadd(fmul(m[j], k.b1), fmul(gj, k.c1));
-      v[j] = fadd(fmul(v[j], k.b2), fmul(fmul(gj, k.c2), gj));
-      const float under = fadd(fmul(__fsqrt_rn(v[j]), k.rs), k.eps);
-      p[j] = fsub(fmul(p[j], e.keep), fmul(fdiv(m[j], under), e.step));
-    }
-    store8(static_cast<P*>(e.param), i, left, wide, p);
-    if (e.copy != nullptr) store8(static_cast<__nv_bfloat16*>(e.copy), i, left, wide, p);
-    if (BITS == 32) {
-      store8(static_cast<float*>(e.m), i, left, wide, m);
-      store8(static_cast<float*>(e.v), i, left, wide, v);
-    } else {
-      float tm = 0.0f, tv = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j >= left) m[j] = v[j] = 0.0f;
-        tm = fmaxf(tm, fabsf(m[j]));
-        tv = fmaxf(tv, v[j]);
-      }
-      tm = warp_max(tm);
-      tv = warp_max(tv);
-      const float im = inverse(tm), iv = inverse(tv);
-      uint2 um = make_uint2(0, 0), uv = make_uint2(0, 0);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        int cm = encode<127, false>(fmul(fabsf(m[j]), im));
-        if (m[j] < 0.0f) cm = -cm;
-        const float y = fmul(v[j], iv);
-        int cv = encode<255, true>(y);
-        if (y > 0.0f) cv = max(cv, 1);
-        (j < 4 ? um.x : um.y) |= static_cast<uint32_t>(cm & 0xff) << (8 * (j & 3));
-        (j < 4 ? uv.x : uv.y) |= static_cast<uint32_t>(cv) << (8 * (j & 3));
-      }
-      store_codes(e.m, i, left, wide, um);
-      store_codes(e.v, i, left, wide, uv);
-      if (lane == 0) {
-        e.sm[block] = tm;
-        e.sv[block] = tv;
-      }
-    }
-  }
+  });
 }
 
 // The values that 8-bit states stand for: param and copy of an entry are the
@@ -291,27 +329,26 @@ __global__ void __launch_bounds__(kThreads)
 template <int N>
 __global__ void __launch_bounds__(kThreads) adamw_decode_kernel(const __grid_constant__ Table<N> t) {
   pdl_begin();
-  int c0, c1, at;
-  my_range(t, &c0, &c1, &at);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int c = c0; c < c1; ++c) {
-    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
-    const Entry& e = t.e[at];
-    const int64_t base = static_cast<int64_t>(c - e.first) * kChunk + warp * (32 * kLane);
-    if (base >= e.n) continue;
-    const int64_t i = base + lane * kLane;
-    const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
-    const uint2 um = load_codes(e.m, i, left, e.wide), uv = load_codes(e.v, i, left, e.wide);
-    const float sm = e.sm[base >> 8], sv = e.sv[base >> 8];
-    float m[8], v[8];
+  for_range(t, [&](const Entry& e, int k0, int k1) {
+#pragma unroll 2
+    for (int chunk = k0; chunk < k1; ++chunk) {
+      const int64_t base = static_cast<int64_t>(chunk) * kChunk + warp * (32 * kLane);
+      if (base >= e.n) break;
+      const int64_t i = base + lane * kLane;
+      const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+      const uint2 um = load_codes(e.m, i, left, e.wide), uv = load_codes(e.v, i, left, e.wide);
+      const float sm = e.sm[base >> 8], sv = e.sv[base >> 8];
+      float m[8], v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      m[j] = decode_m(j < 4 ? um.x : um.y, j & 3, sm);
-      v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+      for (int j = 0; j < 8; ++j) {
+        m[j] = decode_m((j < 4 ? um.x : um.y) ^ kFlip, j & 3, sm);
+        v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
+      }
+      store8(static_cast<float*>(e.param), i, left, e.wide, m);
+      store8(static_cast<float*>(e.copy), i, left, e.wide, v);
     }
-    store8(static_cast<float*>(e.param), i, left, e.wide, m);
-    store8(static_cast<float*>(e.copy), i, left, e.wide, v);
-  }
+  });
 }
 
 // Sum of squares of this CTA's chunks: fp32 over the entries of a thread, then
@@ -320,21 +357,19 @@ template <typename G, int N>
 __global__ void __launch_bounds__(kThreads)
     grad_square_kernel(const __grid_constant__ Table<N> t, double* part) {
   pdl_begin();
-  int c0, c1, at;
-  my_range(t, &c0, &c1, &at);
   float sum = 0.0f;
-  for (int c = c0; c < c1; ++c) {
-    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
-    const Entry& e = t.e[at];
-    const int64_t i = static_cast<int64_t>(c - e.first) * kChunk + threadIdx.x * kLane;
-    if (i >= e.n) continue;
-    float g[8];
-    load8(static_cast<const G*>(e.grad), i, static_cast<int>(min64(e.n - i, kLane)), e.wide, g);
-    float s = 0.0f;
+  for_range(t, [&](const Entry& e, int k0, int k1) {
+#pragma unroll 4
+    for (int chunk = k0; chunk < k1; ++chunk) {
+      const int64_t i = static_cast<int64_t>(chunk) * kChunk + threadIdx.x * kLane;
+      float g[8];
+      load8(static_cast<const G*>(e.grad), i, static_cast<int>(min64(max64(e.n - i, 0), kLane)), e.wide, g);
+      float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
-    sum = fadd(sum, s);
-  }
+      for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
+      sum = fadd(sum, s);
+    }
+  });
   __shared__ double warp_sum[kThreads / 32];
   double d = sum;
 #pragma unroll

@@ -495,7 +495,6 @@ constexpr int64_t kPieceBytes = int64_t{1} << 30;
 // the targets' c, which dominate such sums, are added to dh and dw in fp32.
 constexpr int64_t kKeptBytes = int64_t{4} << 30;
 constexpr int64_t kKeptTokens = 16384;
-constexpr int kMaxSplits = 8;
 
 enum Pass { kForward = 0, kBackward = 1, kTrain = 2 };
 
@@ -507,21 +506,40 @@ struct Layout {
   int64_t piece, padded, Dp, ldc;
 };
 
-// Parts of K for dh: full waves of the SMs for the least part sums.
-int splits_for(int64_t T, int64_t D, int64_t piece) {
-  constexpr int pairs = 76;  // of the 152 SMs
-  const int64_t tiles = (T + kPair - 1) / kPair * ((D + kN - 1) / kN);
-  const int64_t blocks = (piece + kK - 1) / kK;
-  int best = 1;
-  double least = 1e30;
-  for (int s = 1; s <= kMaxSplits && s * 8 <= std::max<int64_t>(blocks, 8); ++s) {
-    const double waves = static_cast<double>((tiles * s + pairs - 1) / pairs) / s * (1.0 + 0.02 * s);
-    if (waves < least) {
-      least = waves;
-      best = s;
+// Widths of tiles, and parts of K for dh, by an estimate of the products' time in
+// cycles: waves of tiles over the SM pairs, a K step of a tile bound by its copies
+// from L2 (about 60 bytes a cycle an SM: 546 cycles for 256 columns, 410 for 128,
+// 341 for 64, where the products take 512, 256 and 128), an epilogue a tile, and
+// for each part its sums written and read once more.
+constexpr int kPairs = 76;  // of the 152 SMs
+constexpr int kMaxSplits = 32;
+
+struct Plan {
+  int tile_n, splits;
+};
+
+Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int terms, int narrowest, int most_splits) {
+  Plan best = {kN, 1};
+  double least = 1e300;
+  const int64_t mt = (m + kPair - 1) / kPair;
+  for (int tn = kN; tn >= narrowest; tn /= 2) {
+    const int64_t nt = (n + tn - 1) / tn;
+    const double step = (kBytesA + tn / 2 * kK * 2) / 60.0, end = 1000.0 + 3000.0 * tn / kN;
+    for (int s = 1; s <= most_splits && s <= std::max<int64_t>(blocks, 1); ++s) {
+      const int64_t waves = (mt * nt * s + kPairs - 1) / kPairs;
+      const double sums = s > 1 ? static_cast<double>(s) * m * n * 8.0 / 3500.0 : 0.0;
+      const double cost = waves * (((blocks + s - 1) / s) * terms * step + end) + sums;
+      if (cost < 0.98 * least) {
+        least = cost;
+        best = Plan{tn, s};
+      }
     }
   }
   return best;
+}
+
+Plan plan_dh(int64_t T, int64_t D, int64_t piece, int planes) {
+  return plan_tiles(T, D, (piece + kK - 1) / kK, planes == 1 ? 1 : 6, 64, kMaxSplits);
 }
 
 Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piece, int64_t ldw) {
@@ -557,7 +575,7 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piec
   l.piece = l.kept ? V : std::min(V, piece > 0 ? piece : most);
   l.ldc = round_up(l.piece, kN);
   l.coef = take(static_cast<size_t>(l.planes) * l.padded * l.ldc * 2);
-  l.sum = take(static_cast<size_t>(splits_for(T, D, l.piece)) * l.padded * l.Dp * 4);
+  l.sum = take(static_cast<size_t>(plan_dh(T, D, l.piece, l.planes).splits) * l.padded * l.Dp * 4);
   l.apart = !l.kept && bf16 && T <= kPair;
   if (l.kept || l.apart) {
     l.flags = take(round_up(l.tiles, kScan / kPair) * 4);
@@ -605,8 +623,10 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t r
 }
 
 template <int MODE>
-cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const Gemm& g, int64_t tiles, int num_sms,
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const Gemm& g, int64_t m, int64_t n, int num_sms,
                         cudaStream_t s) {
+  const int64_t tiles = (m + kPair - 1) / kPair * ((n + g.tile_n - 1) / g.tile_n) * (MODE == kDh ? g.splits : 1);
+  if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
   constexpr int smem = kStages * kStageBytes + 1024;
   const cudaError_t e = ensure_dynamic_smem(ce_gemm_kernel<MODE>, smem);
   if (e != cudaSuccess) return e;
@@ -659,14 +679,17 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   const int64_t hplane = l.padded * l.Dp, wplane = a.V * wld;
   CUtensorMap h_rows, w_rows;  // K = D contiguous
   CE_TRY(make_map(&h_rows, hp, D, l.padded, P, l.Dp, hplane, kM));
-  CE_TRY(make_map(&w_rows, wt, D, a.V, P, wld, wplane, kM));
+  const int terms = bf16 ? 1 : 6;
+  const int64_t d_blocks = (a.D + kK - 1) / kK;
+  const int logits_n = plan_tiles(a.T, a.V, d_blocks, terms, 128, 1).tile_n;
+  CE_TRY(make_map(&w_rows, wt, D, a.V, P, wld, wplane, logits_n / 2));
   Gemm g = {};
   g.head = head;
   g.row = row;
   g.target = target;
   g.T = T;
   g.D = D;
-  g.terms = bf16 ? 1 : 6;
+  g.terms = terms;
   g.spin_limit = a.spin_limit;
   g.status = a.status;
   g.part = reinterpret_cast<float2*>(ws + l.part);
@@ -687,7 +710,8 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   // tokens, where the products wait for memory anyway, get 8.
   const int any = 1 << 30, few = 2, some = 4;
   const int logits = bf16 && a.T > kPair ? 16 : few;
-  const int64_t mt = l.tiles, dt = (a.D + kN - 1) / kN, vt = (a.V + kN - 1) / kN;
+  const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
+  const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, terms, 64, 1).tile_n;
   const unsigned out_blocks =
       static_cast<unsigned>(std::min<int64_t>((a.T * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
   auto dh_out = [&](const float* scale, const float* coef) {
@@ -723,21 +747,24 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.width = static_cast<int>(a.V);
     g.ref = ref;
     g.chunk = logits;
-    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    g.tile_n = logits_n;
+    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_sum_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, g.part, l.parts, floats(l.sums), ref,
                          ints(l.flags)));
     g.redo = ints(l.flags);
-    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(by_targets());
     CE_TRY(make_map(&h_cols, hs, D, l.padded, P, l.Dp, hplane, kK));
     CE_TRY(make_map(&c_rows, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kM));
     CE_TRY(make_map(&c_cols, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kK));
     g.first = 1;
-    g.splits = splits_for(a.T, a.D, a.V);
+    g.splits = dh_plan.splits;
+    g.tile_n = dh_plan.tile_n;
     g.chunk = bf16 ? any : some;
-    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, mt * dt * g.splits, num_sms, s));
+    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
     CE_TRY(dh_out(scale, factor));
-    return launch_gemm<kDw>(c_cols, h_cols, g, (a.V + kPair - 1) / kPair * dt, num_sms, s);
+    g.tile_n = dw_n;
+    return launch_gemm<kDw>(c_cols, h_cols, g, a.V, a.D, num_sms, s);
   }
 
   const float* lse = a.lse_in;
@@ -745,7 +772,8 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     float* out = a.lse != nullptr ? a.lse : floats(l.lse);
     g.width = static_cast<int>(a.V);
     g.chunk = logits;
-    CE_TRY(launch_gemm<kLoss>(h_rows, w_rows, g, mt * vt, num_sms, s));
+    g.tile_n = logits_n;
+    CE_TRY(launch_gemm<kLoss>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_finish_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, row, place, g.part, l.parts,
                          g.at_target, a.loss, out));
     lse = out;
@@ -761,7 +789,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     CE_TRY(rank());
     CE_TRY(by_targets());
   }
-  g.splits = splits_for(a.T, a.D, l.piece);
+  g.splits = dh_plan.splits;
   CE_TRY(make_map(&h_cols, hp, D, l.padded, P, l.Dp, hplane, kK));
   for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
     const int width = static_cast<int>(std::min(l.piece, a.V - v0));
@@ -771,10 +799,13 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     CE_TRY(make_map(&c_rows, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kM));
     CE_TRY(make_map(&c_cols, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kK));
     g.chunk = bf16 ? any : few;
-    CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, mt * ((width + kN - 1) / kN), num_sms, s));
+    g.tile_n = logits_n;
+    CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, a.T, width, num_sms, s));
     g.chunk = bf16 ? any : some;
-    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, mt * dt * g.splits, num_sms, s));
-    CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, (width + kPair - 1) / kPair * dt, num_sms, s));
+    g.tile_n = dh_plan.tile_n;
+    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
+    g.tile_n = dw_n;
+    CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, width, a.D, num_sms, s));
   }
   return dh_out(nullptr, l.apart ? factor : nullptr);
 }

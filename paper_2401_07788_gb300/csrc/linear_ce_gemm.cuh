@@ -95,6 +95,7 @@ struct Gemm {
   int width;            // vocabulary entries of the piece
   int64_t v0;           // its first one
   int terms;            // 1 (bf16) or 6 (fp32 in three planes)
+  int tile_n;           // columns of a tile: 64 (dh, dw), 128 or 256
   int chunk;            // K blocks that one accumulator sums (see ce_gemm_kernel)
   int splits;           // kDh: parts of K
   int first;            // kDh: the piece that starts the sums
@@ -146,7 +147,7 @@ __device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
   const int n = MODE == kDh || MODE == kDw ? g.D : g.width;
   const int k = MODE == kDh ? g.width : MODE == kDw ? valid : g.D;
   s.m_tiles = (m + kPair - 1) / kPair;
-  s.n_tiles = (n + kN - 1) / kN;
+  s.n_tiles = (n + g.tile_n - 1) / g.tile_n;
   s.blocks = (k + kK - 1) / kK;
   s.splits = MODE == kDh ? g.splits : 1;
   return s;
@@ -156,14 +157,14 @@ __device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
 // the logits all tokens pass one stretch of the vocabulary; for dh and dw the
 // columns of one row tile of c run together, so that c is read from HBM once.
 template <int MODE>
-__device__ __forceinline__ Tile tile_of(const Shape& s, int i) {
+__device__ __forceinline__ Tile tile_of(const Gemm& g, const Shape& s, int i) {
   Tile t;
   if (MODE == kLoss || MODE == kExp || MODE == kCoef) {
     t.m0 = i % s.m_tiles * kPair;
-    t.n0 = i / s.m_tiles * kN;
+    t.n0 = i / s.m_tiles * g.tile_n;
     t.split = 0;
   } else {
-    t.n0 = i % s.n_tiles * kN;
+    t.n0 = i % s.n_tiles * g.tile_n;
     i /= s.n_tiles;
     t.m0 = i % s.m_tiles * kPair;
     t.split = i / s.m_tiles;
@@ -216,7 +217,8 @@ __device__ __forceinline__ void store_planes(const Gemm& g, int64_t m, int n0, c
 
 // One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
 template <int MODE>
-__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf]) {
+__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf],
+                                         float* scratch) {
   if (MODE == kLoss || MODE == kExp) {
     const int cols = min(g.width - n0, kHalf);
     if (MODE == kLoss && (cols <= 0 || m >= valid)) return;
@@ -296,9 +298,10 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
   } else if (MODE == kDh) {
     if (m >= valid) return;
     float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
+    const int cols = min(static_cast<int>(g.lds) - n0, g.tile_n);
 #pragma unroll
     for (int j = 0; j < kHalf; j += 8) {
-      if (n0 + j < g.lds) {
+      if (j < cols) {
         uint32_t u[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
@@ -309,8 +312,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
       }
     }
   } else {
-    if (m >= g.width) return;
-    if (g.seg_first != nullptr) {  // the tokens whose target this entry is
+    if (g.seg_first != nullptr && m < g.width) {  // the tokens whose target this entry is
       const int first = g.seg_first[g.v0 + m];
       if (first > 0) {
         const int end = g.seg_end[g.v0 + m];
@@ -329,35 +331,62 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         }
       }
     }
-    const int64_t at = (g.v0 + m) * g.lddw + n0;
-    if (g.dw_bf16) {
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.dw) + at;
+    const int cols = min(g.D - n0, g.tile_n);
+    if (g.dw_wide) {
+      if (m >= g.width) return;
+      const int64_t at = (g.v0 + m) * g.lddw + n0;
+      if (g.dw_bf16) {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(g.dw) + at;
 #pragma unroll
-      for (int j = 0; j < kHalf; j += 16) {
-        if (g.dw_wide && n0 + j + 16 <= g.D) {
-          uint32_t u[8];
+        for (int j = 0; j < kHalf; j += 16) {
+          if (j + 16 <= cols) {
+            uint32_t u[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
-          st_v8(out + j, u);
-        } else {
+            for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
+            st_v8(out + j, u);
+          } else {
 #pragma unroll
-          for (int q = 0; q < 16; ++q)
-            if (n0 + j + q < g.D) out[j + q] = __float2bfloat16_rn(x[j + q]);
+            for (int q = 0; q < 16; ++q)
+              if (j + q < cols) out[j + q] = __float2bfloat16_rn(x[j + q]);
+          }
+        }
+      } else {
+        float* out = static_cast<float*>(g.dw) + at;
+#pragma unroll
+        for (int j = 0; j < kHalf; j += 8) {
+          if (j + 8 <= cols) {
+            uint32_t u[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[j + q]);
+            st_v8(out + j, u);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if (j + q < cols) out[j + q] = x[j + q];
+          }
         }
       }
     } else {
-      float* out = static_cast<float*>(g.dw) + at;
+      // Rows that start anywhere: 16 columns at a time through shared memory, so that
+      // a store covers two rows' neighbours (5 sectors) and not 32 rows' (32).
+      const int lane = threadIdx.x & 31, m0 = m - lane, row = lane >> 4, col = lane & 15;
 #pragma unroll
-      for (int j = 0; j < kHalf; j += 8) {
-        if (g.dw_wide && n0 + j + 8 <= g.D) {
-          uint32_t u[8];
+      for (int j = 0; j < kHalf; j += 16) {
+        if (j < cols) {
+          __syncwarp();
 #pragma unroll
-          for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[j + q]);
-          st_v8(out + j, u);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (n0 + j + q < g.D) out[j + q] = x[j + q];
+          for (int q = 0; q < 16; ++q) scratch[lane * 17 + q] = x[j + q];
+          __syncwarp();
+          const int rows = g.width - m0;
+#pragma unroll 4
+          for (int r = row; r < 32; r += 2) {
+            if (r < rows && j + col < cols) {
+              const int64_t at = (g.v0 + m0 + r) * g.lddw + n0 + j + col;
+              const float v = scratch[r * 17 + col];
+              if (g.dw_bf16) static_cast<__nv_bfloat16*>(g.dw)[at] = __float2bfloat16_rn(v);
+              else static_cast<float*>(g.dw)[at] = v;
+            }
+          }
         }
       }
     }
@@ -371,7 +400,9 @@ __device__ __forceinline__ bool skipped(const Gemm& g, const Tile& t) {
 
 // Columns of a tile that the product forms: a multiple of 16.  Each CTA of the
 // pair holds half of them as rows of B.
-__device__ __forceinline__ int tile_cols(int cols, int n0) { return min((cols - n0 + 15) / 16 * 16, kN); }
+__device__ __forceinline__ int tile_cols(const Gemm& g, int cols, int n0) {
+  return min((cols - n0 + 15) / 16 * 16, g.tile_n);
+}
 
 template <int MODE>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -382,6 +413,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   // full and taken are used in the first CTA, for both; empty and done in each
   __shared__ uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
   __shared__ uint32_t tmem;
+  __shared__ float scratch[MODE == kDw ? kEpiWarps * 32 * 17 : 1];
   uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = static_cast<int>(cluster_rank());
@@ -421,10 +453,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       fence_proxy_async_all();  // operands that earlier kernels wrote
       uint32_t it = 0;
       bool ok = true;
+      // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
+      const int b_blocks = (g.tile_n / 2 + 63) / 64;
+      const uint32_t bytes = 2 * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
       for (int i = pair; i < total && ok; i += pairs) {
-        const Tile t = tile_of<MODE>(s, i);
+        const Tile t = tile_of<MODE>(g, s, i);
         if (skipped<MODE>(g, t)) continue;
-        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(cols, t.n0) / 2);
+        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g, cols, t.n0) / 2);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk) {
           const int blocks = min(g.chunk, t.k1 - c);
           for (int j = 0; j < blocks * g.terms; ++j, ++it) {
@@ -437,7 +472,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             uint8_t* a = stage0 + st * kStageBytes;
             uint8_t* b = a + kBytesA;
             const uint32_t bar = dsmem_addr(&full[st], 0);
-            if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * kStageBytes);
+            if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
             if (A_MN) {
 #pragma unroll
               for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, pa, bar);
@@ -446,8 +481,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
             if (B_MN) {
               const int k_at = kb * kK + (MODE == kDh ? static_cast<int>(g.v0) : 0);
-#pragma unroll
-              for (int q = 0; q < kN / 128; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
+              for (int q = 0; q < b_blocks; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
             } else {
               tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, pb, bar);
             }
@@ -471,9 +505,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       uint32_t it = 0, n = 0;
       bool ok = true;
       for (int i = pair; i < total && ok; i += pairs) {
-        const Tile t = tile_of<MODE>(s, i);
+        const Tile t = tile_of<MODE>(g, s, i);
         if (skipped<MODE>(g, t)) continue;
-        const uint32_t idesc = mma_desc(kPair, tile_cols(cols, t.n0), A_MN, B_MN);
+        const uint32_t idesc = mma_desc(kPair, tile_cols(g, cols, t.n0), A_MN, B_MN);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
           ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
           tc_fence_after();
@@ -509,7 +543,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     uint32_t n = 0;
     bool ok = true;
     for (int i = pair; i < total; i += pairs) {
-      const Tile t = tile_of<MODE>(s, i);
+      const Tile t = tile_of<MODE>(g, s, i);
       if (skipped<MODE>(g, t)) continue;
       float x[kHalf];
       if (t.k0 == t.k1) {
@@ -521,6 +555,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         ok = __all_sync(kFull, ok);
         if (!ok) break;
         tc_fence_after();
+        if (half * kHalf >= g.tile_n) {  // a narrow tile: the first four warps take it
+          if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+          continue;
+        }
         const uint32_t at = acc + (n & 1) * kN + half * kHalf + (static_cast<uint32_t>(quad * 32) << 16);
         if (c == t.k0) {
 #pragma unroll
@@ -547,7 +585,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
       }
       if (!ok) break;
-      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x);
+      if (half * kHalf >= g.tile_n) continue;
+      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x,
+                     scratch + (MODE == kDw ? (warp - 2) * 32 * 17 : 0));
     }
   }
   __syncwarp();

@@ -124,6 +124,8 @@ class AdamWPlan:
         if (m is None) != (v is None):
             raise MpcError(1, "m and v are given together")
         self.device = params[0].device
+        self.index = params[0].get_device()
+        self.norm_ws = None  # mpc_grad_norm's workspace, made by its first call
         self.sizes = [p.numel() for p in params]
         blocks = [-(-k // BLOCK) for k in self.sizes]
         if m is None:
