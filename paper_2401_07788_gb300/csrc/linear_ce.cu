@@ -813,10 +813,12 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
 }  // namespace
 
 size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int pass, int64_t piece, int64_t ldw) {
+  if (linear_ce_few_fits(T, D)) return linear_ce_few_workspace_bytes(T, D, V, pass != kForward);
   return layout(T, D, V, bf16 != 0, pass, piece, ldw).total;
 }
 
 cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
+  if (linear_ce_few_fits(a.T, a.D)) return launch_linear_ce_few(a, num_sms, s);
   return a.bf16 ? run<__nv_bfloat16>(a, num_sms, s) : run<float>(a, num_sms, s);
 }
 

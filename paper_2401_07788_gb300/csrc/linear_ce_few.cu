@@ -1,0 +1,558 @@
+// linear_ce_few.cu -- the linear cross entropy of a few tokens (16 at most): a
+// scored token of a served model, the last tokens of a batch.
+//
+// With so few tokens the work is one pass over w (and one over dw): T products a
+// byte pair of w, under the fp32 rate of the SMs, so plain fp32 FMAs read w once at
+// the memory's rate, where tiles of the matrix units would be empty rows for the
+// most part (and an fp32 w would first be split into bf16 planes, 2.5 times its
+// size of traffic).
+//
+//   ce_few_logits   a warp takes R rows of w at a time, its lanes the columns: T R
+//                   sums a lane, added up over the lanes by halving exchanges, then
+//                   a running (largest, sum of exponentials) for each token
+//   ce_few_finish   lse and loss
+//   ce_few_grad     one pass over w and dw: c of 64 rows at a time in shared
+//                   memory, a thread owns a few columns, with h and the sums of dh
+//                   of each token for them in registers
+//   ce_few_dh       dh from the CTAs' sums
+//
+// Tokens keep their places here; one that does not count has a zero row of h, and
+// zero results.
+#include <algorithm>
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "launch_util.h"
+
+namespace mpc {
+namespace {
+
+constexpr int kFewTokens = 16;
+constexpr int kFewThreads = 512;
+constexpr int kFewWarps = kFewThreads / 32;
+constexpr int kFewBytes = 200 * 1024;  // of h in fp32 in shared memory
+constexpr float kL2e = 1.4426950408889634f;
+constexpr float kL2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float few_float(float x) { return x; }
+__device__ __forceinline__ float few_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void few_from(float x, float* p) { *p = x; }
+__device__ __forceinline__ void few_from(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
+
+struct Few {
+  const void* h;
+  const void* w;
+  int64_t ldh, ldw;
+  const int64_t* targets;
+  int T, D;
+  int64_t V, ignore;
+  float2* part;    // [CTA][kFewTokens] (largest logit, sum), base 2
+  float* at;       // [kFewTokens] the target's logit
+  float* logits;   // [T][V] for the gradient, or nullptr
+  float* lse;      // [T]
+  float* loss;     // [T], or nullptr
+  const float* gloss;
+  float* weight;   // [kFewTokens] g, 0 for tokens that do not count
+  float* sums;     // [CTA][T][D] of dh
+  void* dh;
+  void* dw;
+  int64_t lddh, lddw;
+  int parts;
+  unsigned* status;
+};
+
+__device__ __forceinline__ int few_target(const Few& f, int t) {
+  if (t >= f.T) return -1;
+  const int64_t y = f.targets[t];
+  return y != f.ignore && y >= 0 && y < f.V ? static_cast<int>(y) : -1;
+}
+
+// V elements from p on as floats.
+template <int N>
+__device__ __forceinline__ void few_load(const float* p, float (&x)[N]) {
+  if (N == 2) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    x[0] = v.x; x[1] = v.y;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j + 4 <= N; j += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p + j);
+    x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
+  }
+}
+template <int N>
+__device__ __forceinline__ void few_load(const __nv_bfloat16* p, float (&x)[N]) {
+  uint32_t u[N / 2];
+  if (N == 8) *reinterpret_cast<uint4*>(u) = *reinterpret_cast<const uint4*>(p);
+  else if (N == 4) *reinterpret_cast<uint2*>(u) = *reinterpret_cast<const uint2*>(p);
+  else u[0] = *reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) {
+    x[2 * j] = __uint_as_float(u[j] << 16);
+    x[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+  }
+}
+
+// The rows of h of TT tokens in shared memory, fp32.  Columns of a 16-byte group
+// of 8 bf16 are kept in two halves of 4, so that 128-bit reads of neighbouring
+// lanes do not meet in a bank.
+template <typename E, int TT, bool WIDE>
+__device__ __forceinline__ int few_place(int d, int Dp) {
+  if (!WIDE || sizeof(E) == 4) return d;
+  return (d >> 2 & 1) * (Dp / 2) + (d >> 3) * 4 + (d & 3);
+}
+
+// WIDE: rows of w start on 16 bytes and are read in 16-byte groups; otherwise
+// element by element, neighbouring lanes neighbouring elements.
+template <typename E, int TT, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few f) {
+  constexpr int VEC = WIDE ? 16 / sizeof(E) : 1;
+  constexpr int R = TT >= 8 ? 4 : 8;  // rows a warp takes at a time
+  constexpr int N = R * TT;
+  pdl_begin();
+  extern __shared__ float sh[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int Dp = (f.D + 7) / 8 * 8;
+  const E* h = static_cast<const E*>(f.h);
+  const E* w = static_cast<const E*>(f.w);
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const bool live = few_target(f, t) >= 0;
+    for (int d = threadIdx.x; d < Dp; d += kFewThreads)
+      sh[t * Dp + few_place<E, TT, WIDE>(d, Dp)] = live && d < f.D ? few_float(h[t * f.ldh + d]) : 0.0f;
+  }
+  if (blockIdx.x == 0 && threadIdx.x < f.T) {
+    const int64_t y = f.targets[threadIdx.x];
+    if (y != f.ignore && (y < 0 || y >= f.V)) set_status(f.status, STATUS_BAD_INDEX);
+  }
+  __syncthreads();
+
+  // this lane's sums after the exchange: indices idx .. idx + C - 1 of r * TT + t
+  constexpr int C = N > 32 ? N / 32 : 1;
+  int idx = 0;
+  bool counts = true;  // the one lane of those that hold the same sum
+  {
+    int c = N;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      if (c > 1) {
+        c /= 2;
+        if (lane & o) idx += c;
+      } else if (lane & o) {
+        counts = false;
+      }
+    }
+  }
+  float top[C], sum[C];
+  int target[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    top[i] = -INFINITY;
+    sum[i] = 0.0f;
+    target[i] = few_target(f, (idx + i) % TT);
+  }
+  const int64_t groups = (f.V + R - 1) / R;
+  for (int64_t g = blockIdx.x * kFewWarps + warp; g < groups; g += gridDim.x * kFewWarps) {
+    const int64_t v0 = g * R;
+    float acc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+    const E* rows[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) rows[r] = w + min64(v0 + r, f.V - 1) * f.ldw;
+    const int whole = WIDE ? f.D / VEC * VEC : f.D;
+    if constexpr (WIDE) {
+      for (int d = lane * VEC; d < whole; d += 32 * VEC) {
+        uint4 u[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) u[r] = *reinterpret_cast<const uint4*>(rows[r] + d);
+#pragma unroll
+        for (int q = 0; q < VEC; q += 4) {
+          float x[R][4];
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if constexpr (sizeof(E) == 4) {
+              x[r][0] = __uint_as_float(u[r].x); x[r][1] = __uint_as_float(u[r].y);
+              x[r][2] = __uint_as_float(u[r].z); x[r][3] = __uint_as_float(u[r].w);
+            } else {
+              const uint32_t lo = q == 0 ? u[r].x : u[r].z, hi = q == 0 ? u[r].y : u[r].w;
+              x[r][0] = __uint_as_float(lo << 16); x[r][1] = __uint_as_float(lo & 0xffff0000u);
+              x[r][2] = __uint_as_float(hi << 16); x[r][3] = __uint_as_float(hi & 0xffff0000u);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            const float4 y = *reinterpret_cast<const float4*>(&sh[t * Dp + few_place<E, TT, WIDE>(d + q, Dp)]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              float& to = acc[r * TT + t];
+              to = __fmaf_rn(x[r][0], y.x, to);
+              to = __fmaf_rn(x[r][1], y.y, to);
+              to = __fmaf_rn(x[r][2], y.z, to);
+              to = __fmaf_rn(x[r][3], y.w, to);
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int d = lane; d < whole; d += 32) {
+        float x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = few_float(rows[r][d]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          const float y = sh[t * Dp + d];
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[r * TT + t] = __fmaf_rn(x[r], y, acc[r * TT + t]);
+        }
+      }
+    }
+    if (WIDE && whole + lane < f.D) {  // the columns after the last whole group
+      const int d = whole + lane;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float x = few_float(rows[r][d]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          acc[r * TT + t] = __fmaf_rn(x, sh[t * Dp + few_place<E, TT, WIDE>(d, Dp)], acc[r * TT + t]);
+      }
+    }
+    // sums over the lanes: halve the list and the lanes' share of it at each step
+    {
+      int c = N;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        if (c > 1) {
+          c /= 2;
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            if (i < c) {
+              const bool up = lane & o;
+              const float give = up ? acc[i] : acc[i + c];
+              const float keep = up ? acc[i + c] : acc[i];
+              acc[i] = fadd(keep, __shfl_xor_sync(kFull, give, o));
+            }
+          }
+        } else {
+          acc[0] = fadd(acc[0], __shfl_xor_sync(kFull, acc[0], o));
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int t = (idx + i) % TT;
+      const int64_t v = v0 + (idx + i) / TT;
+      if (v < f.V && counts) {
+        if (v == target[i]) f.at[t] = acc[i];
+        if (f.logits != nullptr && t < f.T) f.logits[t * f.V + v] = acc[i];
+        const float l = fmul(acc[i], kL2e);
+        const float up = fmaxf(top[i], l);
+        if (up != -INFINITY) {
+          const float old = top[i] == -INFINITY ? 0.0f : fmul(sum[i], exp2f(fsub(top[i], up)));
+          // the rounding of l is undone in the sum: both sides of loss use the exact product
+          sum[i] = fadd(old, exp2f(__fmaf_rn(acc[i], kL2e, -up)));
+          top[i] = up;
+        } else if (acc[i] != acc[i]) {
+          sum[i] = acc[i];
+        }
+      }
+    }
+  }
+  __shared__ float2 all[kFewWarps][N];
+  if (counts) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) all[warp][idx + i] = make_float2(top[i], sum[i]);
+  }
+  __syncthreads();
+  if (threadIdx.x < TT) {
+    const int t = threadIdx.x;
+    float m = -INFINITY, s = 0.0f;
+    for (int q = 0; q < kFewWarps; ++q)
+      for (int r = 0; r < R; ++r) m = fmaxf(m, all[q][r * TT + t].x);
+    for (int q = 0; q < kFewWarps; ++q)
+      for (int r = 0; r < R; ++r) {
+        const float2 p = all[q][r * TT + t];
+        if (p.x != -INFINITY) s = fadd(s, fmul(p.y, exp2f(fsub(p.x, m))));
+        else if (p.y != p.y) s = p.y;
+      }
+    f.part[blockIdx.x * kFewTokens + t] = make_float2(m, s);
+  }
+}
+
+// lse and loss, one warp a token; the weights of a gradient.
+__global__ void __launch_bounds__(kFewTokens * 32) ce_few_finish_kernel(const Few f, int given) {
+  pdl_begin();
+  const int t = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned counted = __ballot_sync(kFull, few_target(f, lane) >= 0);
+  const int n = __popc(counted);
+  const bool live = counted >> t & 1;
+  if (lane == 0 && f.weight != nullptr) {
+    const float mean = n > 0 ? fdiv(1.0f, static_cast<float>(n)) : 0.0f;
+    f.weight[t] = !live ? 0.0f : f.gloss != nullptr ? f.gloss[t] : mean;
+  }
+  if (t >= f.T || given) return;
+  float m = -INFINITY, s = 0.0f;
+  for (int i = lane; i < f.parts; i += 32) m = fmaxf(m, f.part[i * kFewTokens + t].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+  for (int i = lane; i < f.parts; i += 32) {
+    const float2 p = f.part[i * kFewTokens + t];
+    if (p.x != -INFINITY) s = fadd(s, fmul(p.y, exp2f(fsub(p.x, m))));
+    else if (p.y != p.y) s = p.y;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
+  if (lane == 0) {
+    const float l = log2f(s);
+    f.lse[t] = live ? fmul(fadd(m, l), kL2) : 0.0f;
+    if (f.loss != nullptr) f.loss[t] = live ? fmul(fsub(l, __fmaf_rn(f.at[t], kL2e, -m)), kL2) : 0.0f;
+  }
+}
+
+// Columns that a thread of the gradient kernel owns: h and dh's sums of TT tokens
+// for each are 2 TT registers.
+__host__ __device__ constexpr int few_cols(int tt) { return tt >= 16 ? 2 : 4; }
+template <int BYTES> struct FewWord;
+template <> struct FewWord<4> { using type = uint32_t; };
+template <> struct FewWord<8> { using type = uint2; };
+template <> struct FewWord<16> { using type = uint4; };
+
+// dw rows of this CTA's range and its sums of dh.  Threads: G column groups of
+// few_cols(TT) (neighbouring columns when WIDE, G apart otherwise) by RL rows at a time; a CTA
+// takes the columns of blockIdx.y.
+template <typename E, int TT, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads, 1) ce_few_grad_kernel(const Few f, int G, int RL, int with_loss) {
+  constexpr int kRows = 64, CP = few_cols(TT);
+  pdl_begin();
+  __shared__ float c[kRows][TT];
+  __shared__ float lse_of[TT], weight_of[TT], minus_loss[TT];
+  __shared__ int target_of[TT];
+  extern __shared__ float red[];
+  const E* h = static_cast<const E*>(f.h);
+  const E* w = static_cast<const E*>(f.w);
+  E* dw = static_cast<E*>(f.dw);
+  const int group = threadIdx.x % G, rl = threadIdx.x / G;
+  const int d0 = blockIdx.y * G * CP + (WIDE ? group * CP : group);
+  auto col = [&](int j) { return WIDE ? d0 + j : d0 + j * G; };
+  if (threadIdx.x < TT) {
+    const int t = threadIdx.x;
+    target_of[t] = few_target(f, t);
+    weight_of[t] = f.weight[t];
+    lse_of[t] = t < f.T ? f.lse[t] : 0.0f;
+    minus_loss[t] = t < f.T && target_of[t] >= 0
+                        ? (with_loss ? -f.loss[t] : fsub(f.logits[t * f.V + target_of[t]], f.lse[t]))
+                        : 0.0f;
+  }
+  float x[TT][CP], sum[TT][CP];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const bool live = few_target(f, t) >= 0;
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+      x[t][j] = live && col(j) < f.D ? few_float(h[t * f.ldh + col(j)]) : 0.0f;
+      sum[t][j] = 0.0f;
+    }
+  }
+  const bool full = WIDE && d0 + CP <= f.D;
+  const int64_t first = f.V * blockIdx.x / gridDim.x, last = f.V * (blockIdx.x + 1) / gridDim.x;
+  for (int64_t v0 = first; v0 < last; v0 += kRows) {
+    const int rows = static_cast<int>(min64(last - v0, kRows));
+    __syncthreads();
+    for (int q = threadIdx.x; q < rows * TT; q += blockDim.x) {
+      const int r = q % rows, t = q / rows;  // neighbouring threads read neighbouring logits
+      float p = 0.0f;
+      if (target_of[t] >= 0)
+        p = fmul(weight_of[t], target_of[t] == v0 + r ? expm1f(minus_loss[t])
+                                                      : expf(fsub(f.logits[t * f.V + v0 + r], lse_of[t])));
+      c[r][t] = p;
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int r = rl; r < rows; r += RL) {
+      const int64_t v = v0 + r;
+      float y[CP], z[CP] = {};
+      if (full) {
+        few_load<CP>(w + v * f.ldw + d0, y);
+      } else {
+#pragma unroll
+        for (int j = 0; j < CP; ++j) y[j] = col(j) < f.D ? few_float(w[v * f.ldw + col(j)]) : 0.0f;
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const float a = c[r][t];
+#pragma unroll
+        for (int j = 0; j < CP; ++j) {
+          sum[t][j] = __fmaf_rn(a, y[j], sum[t][j]);
+          z[j] = __fmaf_rn(a, x[t][j], z[j]);
+        }
+      }
+      E out[CP];
+#pragma unroll
+      for (int j = 0; j < CP; ++j) few_from(z[j], &out[j]);
+      E* to = dw + v * f.lddw;
+      if (full && (reinterpret_cast<uintptr_t>(to + d0) & (CP * sizeof(E) - 1)) == 0) {
+        using U = typename FewWord<CP * sizeof(E)>::type;
+        U u;
+        memcpy(&u, out, sizeof(u));
+        *reinterpret_cast<U*>(to + d0) = u;
+      } else {
+#pragma unroll
+        for (int j = 0; j < CP; ++j)
+          if (col(j) < f.D) to[col(j)] = out[j];
+      }
+    }
+  }
+  // the row lanes' sums, in their order
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    if (t < f.T) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < CP; ++j) red[(rl * CP + j) * G + group] = sum[t][j];
+      __syncthreads();
+      if (rl == 0) {
+#pragma unroll
+        for (int j = 0; j < CP; ++j) {
+          float s = 0.0f;
+          for (int q = 0; q < RL; ++q) s = fadd(s, red[(q * CP + j) * G + group]);
+          if (col(j) < f.D) f.sums[(static_cast<int64_t>(blockIdx.x) * f.T + t) * f.D + col(j)] = s;
+        }
+      }
+    }
+  }
+}
+
+// dh: the sums of the CTAs, four interleaved running sums.
+template <typename E>
+__global__ void __launch_bounds__(256) ce_few_dh_kernel(const Few f, int ranges) {
+  pdl_begin();
+  __shared__ float part[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t q = blockIdx.x * int64_t{32} + lane, n = static_cast<int64_t>(f.T) * f.D;
+  float s = 0.0f;
+  if (q < n)
+    for (int i = warp; i < ranges; i += 8) s = fadd(s, f.sums[i * n + q]);
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && q < n) {
+    for (int i = 1; i < 8; ++i) s = fadd(s, part[i][lane]);
+    const int t = static_cast<int>(q / f.D), d = static_cast<int>(q - static_cast<int64_t>(t) * f.D);
+    few_from(few_target(f, t) >= 0 ? s : 0.0f, static_cast<E*>(f.dh) + t * f.lddh + d);
+  }
+}
+
+int few_tokens_up(int64_t T) {
+  int tt = 1;
+  while (tt < T) tt *= 2;
+  return tt;
+}
+int few_ranges(int64_t V, int num_sms) { return static_cast<int>(std::min<int64_t>(2 * num_sms, (V + 15) / 16)); }
+constexpr int kMostSms = 160;
+
+size_t few_up(size_t x) { return (x + 255) / 256 * 256; }
+
+template <typename E, int TT>
+cudaError_t few_run(const LinearCeArgs& a, Few f, int num_sms, cudaStream_t s) {
+  const bool grad = a.dw != nullptr, given = a.loss == nullptr;
+  const bool wide = (reinterpret_cast<uintptr_t>(a.w) & 15) == 0 && a.ldw * sizeof(E) % 16 == 0;
+  const int Dp = (f.D + 7) / 8 * 8;
+  const int smem = TT * Dp * 4;
+  auto logits = wide ? ce_few_logits_kernel<E, TT, true> : ce_few_logits_kernel<E, TT, false>;
+  cudaError_t e = ensure_dynamic_smem(logits, kFewBytes);
+  if (e != cudaSuccess) return e;
+  f.parts = num_sms;
+  e = launch_kernel(logits, dim3(num_sms), dim3(kFewThreads), smem, s, 0, f);
+  if (e != cudaSuccess) return e;
+  e = launch_kernel(ce_few_finish_kernel, dim3(1), dim3(kFewTokens * 32), 0, s, 0, f, given ? 1 : 0);
+  if (e != cudaSuccess || !grad) return e;
+  constexpr int CP = few_cols(TT);
+  const int G = std::min((f.D + CP - 1) / CP, 256), RL = kFewThreads / G;
+  const int ranges = few_ranges(a.V, num_sms);
+  auto back = wide ? ce_few_grad_kernel<E, TT, true> : ce_few_grad_kernel<E, TT, false>;
+  e = launch_kernel(back, dim3(ranges, (f.D + CP * G - 1) / (CP * G)), dim3(G * RL), G * RL * CP * 4, s, 0, f, G, RL,
+                    given ? 0 : 1);
+  if (e != cudaSuccess) return e;
+  const int64_t n = static_cast<int64_t>(f.T) * f.D;
+  return launch_kernel(ce_few_dh_kernel<E>, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(256), 0, s, 0, f, ranges);
+}
+
+template <typename E>
+cudaError_t few_typed(const LinearCeArgs& a, const Few& f, int num_sms, cudaStream_t s) {
+  switch (few_tokens_up(a.T)) {
+    case 1: return few_run<E, 1>(a, f, num_sms, s);
+    case 2: return few_run<E, 2>(a, f, num_sms, s);
+    case 4: return few_run<E, 4>(a, f, num_sms, s);
+    case 8: return few_run<E, 8>(a, f, num_sms, s);
+    default: return few_run<E, 16>(a, f, num_sms, s);
+  }
+}
+
+struct FewLayout {
+  size_t part, at, weight, lse, logits, sums, total;
+};
+FewLayout few_layout(int64_t T, int64_t D, int64_t V, bool grad) {
+  FewLayout l = {};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t p = at;
+    at += few_up(bytes);
+    return p;
+  };
+  l.part = take(kMostSms * kFewTokens * 8);
+  l.at = take(kFewTokens * 4);
+  l.weight = take(kFewTokens * 4);
+  l.lse = take(kFewTokens * 4);
+  if (grad) {
+    l.logits = take(static_cast<size_t>(T) * V * 4);
+    l.sums = take(static_cast<size_t>(few_ranges(V, kMostSms)) * T * D * 4);
+  }
+  l.total = at;
+  return l;
+}
+
+}  // namespace
+
+bool linear_ce_few_fits(int64_t T, int64_t D) {
+  return T <= kFewTokens && D <= kFewBytes && few_tokens_up(T) * ((D + 7) / 8 * 8) * 4 <= kFewBytes;
+}
+
+size_t linear_ce_few_workspace_bytes(int64_t T, int64_t D, int64_t V, int grad) {
+  return few_layout(T, D, V, grad != 0).total;
+}
+
+cudaError_t launch_linear_ce_few(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
+  const bool grad = a.dw != nullptr;
+  const FewLayout l = few_layout(a.T, a.D, a.V, grad);
+  char* ws = static_cast<char*>(a.ws);
+  auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+  Few f = {};
+  f.h = a.h;
+  f.w = a.w;
+  f.ldh = a.ldh;
+  f.ldw = a.ldw;
+  f.targets = a.targets;
+  f.T = static_cast<int>(a.T);
+  f.D = static_cast<int>(a.D);
+  f.V = a.V;
+  f.ignore = a.ignore;
+  f.part = reinterpret_cast<float2*>(ws + l.part);
+  f.at = floats(l.at);
+  f.logits = grad ? floats(l.logits) : nullptr;
+  f.lse = a.loss == nullptr ? const_cast<float*>(a.lse_in) : a.lse != nullptr ? a.lse : floats(l.lse);
+  f.loss = a.loss;
+  f.gloss = a.gloss;
+  f.weight = grad ? floats(l.weight) : nullptr;
+  f.sums = floats(l.sums);
+  f.dh = a.dh;
+  f.dw = a.dw;
+  f.lddh = a.lddh;
+  f.lddw = a.lddw;
+  f.status = a.status;
+  num_sms = std::min(num_sms, kMostSms);
+  return a.bf16 ? few_typed<__nv_bfloat16>(a, f, num_sms, s) : few_typed<float>(a, f, num_sms, s);
+}
+
+}  // namespace mpc

@@ -348,3 +348,29 @@ def test_exponentials_kept(mpc, dtype, kind):
     for a, b in zip((loss, dh, dw), again):
         assert torch.equal(a, b)
     assert mpc.mpc_get_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 2, 3, 5, 8, 9, 16, 17])
+@pytest.mark.parametrize("D,V", [(64, 1), (8, 40), (7, 9), (768, 3001), (1001, 777), (1032, 2500), (4100, 130)])
+def test_few_tokens(mpc, dtype, T, D, V):
+    """The form for a few tokens and its first neighbour: widths of whole and of broken 16-byte groups,
+    vocabularies shorter than a warp's rows, some tokens ignored, given weights, rows further apart."""
+    h, w, y = inputs(T, D, V, dtype, seed=30, ignored=0.3)
+    gloss = torch.randn(T, device="cuda")
+    want = oracle(h, w, y, gloss)
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    near(loss, want["loss"], "loss")
+    near(lse, want["lse"], "lse")
+    dh, dw = mpc.mpc_linear_ce_backward(h, w, y, lse, gloss)
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
+    big = torch.full((V, D + 8), float("nan"), dtype=dtype, device="cuda")
+    big[:, :D] = w
+    dbig = torch.full((V, D + 3), 7.0, dtype=dtype, device="cuda")
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, big[:, :D], y, gloss, dw=dbig[:, :D])
+    near(loss, want["loss"], "loss (train)")
+    near(dh, want["dh"], "dh (train)")
+    near(dw, want["dw"], "dw (train)")
+    assert bool((dbig[:, D:] == 7.0).all())
+    assert mpc.mpc_get_status() == 0
