@@ -16,7 +16,7 @@
 // the forward's.  Training in one call, where g is known beforehand: the
 // exponentials of the one pass are kept in bf16 (kExp) and made coefficients
 // without forming the logits again, 6 T D V operations:
-//   e[t][v] = 2^(l log2e - ref[t]),  s[t] = sum_v e,  e[t][target[t]] := 0
+//   e[t][v] = 2^(l log2e - ref[t]) (0 at the target),  s[t] = sum of all of them
 //   dh[t] = g/s sum_v e w + g (p - 1) w[target],   p = softmax at the target
 //   dw[v] = sum_t e (g/s h[t]) + sum over tokens with target v of g (p - 1) h[t]
 // The last sum needs the tokens grouped by target; a stable order is found by
@@ -232,6 +232,13 @@ __device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T
   return r;
 }
 
+// log(1 + s 2^-d): the loss of a token from the sum s of the others' exponentials
+// over a base (in base 2) that lies d under the target's logit.
+__device__ __forceinline__ float loss_of(float s, float d) {
+  const float ratio = fmul(s, exp2f(-d));
+  return ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kLn2);
+}
+
 // Forward: lse and loss of the tokens that count.
 __global__ void __launch_bounds__(1024)
     ce_finish_kernel(int T, const Header* head, const int* row, const int* place, const float2* part, int parts,
@@ -243,16 +250,15 @@ __global__ void __launch_bounds__(1024)
   const int m = t;  // as a place in the list from here on
   const float2 r = sum_parts<true>(part, parts, T, m, n);
   if (threadIdx.x < 32 && m < n) {
-    // both measured from the largest logit, so that a small loss keeps its digits
-    const float l = log2f(r.y);
-    lse[row[m]] = fmul(fadd(r.x, l), kLn2);
-    loss[row[m]] = fmul(fsub(l, __fmaf_rn(at_target[m], kLog2e, -r.x)), kLn2);
+    const float l = at_target[m], v = loss_of(r.y, __fmaf_rn(l, kLog2e, -r.x));
+    loss[row[m]] = v;
+    lse[row[m]] = fadd(l, v);
   }
 }
 
-// Training: the sum of each row's exponentials.  A sum out of range (the loss is
-// over 27, or the reference far off) takes the row's largest logit as reference
-// and marks its row tile.
+// Training: the sum of each row's exponentials without the target's.  A sum out
+// of range (a loss over 27) takes the row's largest logit as reference and marks
+// its row tile.
 __global__ void __launch_bounds__(1024)
     ce_sum_kernel(int T, Header* head, const float2* part, int parts, float* sum, float* ref, int* flags) {
   pdl_begin();
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(1024)
   const float2 r = sum_parts<false>(part, parts, T, m, n);
   if (threadIdx.x < 32 && m < n) {
     sum[m] = r.y;
-    if (!(r.y > 0x1p-40f && r.y < 0x1p40f) && fabsf(r.x) < INFINITY) {
+    if (!(r.y < 0x1p40f) && fabsf(r.x) < INFINITY) {
       ref[m] = r.x;
       flags[m / kPair] = 1;
       head->redo = 1;
@@ -354,9 +360,9 @@ __global__ void __launch_bounds__(256) ce_scale_kernel(const Finish f) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
       }
-      // lse - l[target], both measured from ref
-      loss = fmul(fsub(log2f(s), __fmaf_rn(f.at_target[m], kLog2e, -f.ref[m])), kLn2);
-      scale = fdiv(g, s);
+      const float d = __fmaf_rn(f.at_target[m], kLog2e, -f.ref[m]);
+      loss = loss_of(s, d);
+      scale = fdiv(g, fadd(s, exp2f(d)));
       if (lane == 0) {
         f.loss[t] = loss;
         f.scale[m] = scale;
@@ -490,9 +496,9 @@ constexpr int64_t kPieceBytes = int64_t{1} << 30;
 // A training step keeps the exponentials where they take 4 GiB at most and the
 // tokens are few enough to be ordered by counting pairs (16384: 2^28 pairs, 20 us);
 // beyond either it forms the logits twice, a third more operations.  So it does
-// for the tokens of one row tile: there the products wait for w, and an entry of
-// dw, a sum of few terms then, is spared one of its roundings (of g/s h); in bf16
-// the targets' c, which dominate such sums, are added to dh and dw in fp32.
+// for the bf16 tokens of one row tile: there the products wait for w, and an entry
+// of dw, a sum of few terms then, is spared one of its roundings (of g/s h); the
+// targets' c, which dominate such sums, are added to dh and dw in fp32.
 constexpr int64_t kKeptBytes = int64_t{4} << 30;
 constexpr int64_t kKeptTokens = 16384;
 
@@ -507,10 +513,11 @@ struct Layout {
 };
 
 // Widths of tiles, and parts of K for dh, by an estimate of the products' time in
-// cycles: waves of tiles over the SM pairs, a K step of a tile bound by its copies
-// from L2 (about 60 bytes a cycle an SM: 546 cycles for 256 columns, 410 for 128,
-// 341 for 64, where the products take 512, 256 and 128), an epilogue a tile, and
-// for each part its sums written and read once more.
+// cycles: waves of tiles over the SM pairs, a K block of a tile bound by its copies
+// from L2 (about 60 bytes a cycle an SM: in bf16 546 cycles for 256 columns, 410
+// for 128, 341 for 64) or its products (512, 256, 128; in fp32 six times as many on
+// three times the bytes), an epilogue a tile, and for each part its sums written
+// and read once more.
 constexpr int kPairs = 76;  // of the 152 SMs
 constexpr int kMaxSplits = 32;
 
@@ -518,17 +525,18 @@ struct Plan {
   int tile_n, splits;
 };
 
-Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int terms, int narrowest, int most_splits) {
+Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int planes, int narrowest, int most_splits) {
   Plan best = {kN, 1};
   double least = 1e300;
   const int64_t mt = (m + kPair - 1) / kPair;
   for (int tn = kN; tn >= narrowest; tn /= 2) {
     const int64_t nt = (n + tn - 1) / tn;
-    const double step = (kBytesA + tn / 2 * kK * 2) / 60.0, end = 1000.0 + 3000.0 * tn / kN;
+    const double copies = planes * (kBytesA + tn / 2 * kK * 2) / 60.0, products = (planes == 1 ? 2.0 : 12.0) * tn;
+    const double step = std::max(copies, products), end = 1000.0 + 3000.0 * tn / kN;
     for (int s = 1; s <= most_splits && s <= std::max<int64_t>(blocks, 1); ++s) {
       const int64_t waves = (mt * nt * s + kPairs - 1) / kPairs;
       const double sums = s > 1 ? static_cast<double>(s) * m * n * 8.0 / 3500.0 : 0.0;
-      const double cost = waves * (((blocks + s - 1) / s) * terms * step + end) + sums;
+      const double cost = waves * (((blocks + s - 1) / s) * step + end) + sums;
       if (cost < 0.98 * least) {
         least = cost;
         best = Plan{tn, s};
@@ -539,7 +547,7 @@ Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int terms, int narrowest, 
 }
 
 Plan plan_dh(int64_t T, int64_t D, int64_t piece, int planes) {
-  return plan_tiles(T, D, (piece + kK - 1) / kK, planes == 1 ? 1 : 6, 64, kMaxSplits);
+  return plan_tiles(T, D, (piece + kK - 1) / kK, planes, 64, kMaxSplits);
 }
 
 Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piece, int64_t ldw) {
@@ -569,7 +577,7 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piec
     l.total = at;
     return l;
   }
-  l.kept = pass == kTrain && T > kPair && T <= kKeptTokens && (piece == 0 || piece >= V) &&
+  l.kept = pass == kTrain && (!bf16 || T > kPair) && T <= kKeptTokens && (piece == 0 || piece >= V) &&
            l.padded * round_up(V, kN) * 2 * l.planes <= kKeptBytes;
   const int64_t most = std::max<int64_t>(kN, kPieceBytes / (l.padded * 2 * l.planes) / kN * kN);
   l.piece = l.kept ? V : std::min(V, piece > 0 ? piece : most);
@@ -622,21 +630,21 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t r
              : cudaErrorInvalidValue;
 }
 
-template <int MODE>
+template <int MODE, int PLANES>
 cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const Gemm& g, int64_t m, int64_t n, int num_sms,
                         cudaStream_t s) {
   const int64_t tiles = (m + kPair - 1) / kPair * ((n + g.tile_n - 1) / g.tile_n) * (MODE == kDh ? g.splits : 1);
   if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
   constexpr int smem = kStages * kStageBytes + 1024;
-  const cudaError_t e = ensure_dynamic_smem(ce_gemm_kernel<MODE>, smem);
+  const cudaError_t e = ensure_dynamic_smem(ce_gemm_kernel<MODE, PLANES>, smem);
   if (e != cudaSuccess) return e;
   const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(tiles, num_sms / 2));
-  return launch_kernel(ce_gemm_kernel<MODE>, dim3(grid), dim3(kGemmThreads), smem, s, 2, a, b, g);
+  return launch_kernel(ce_gemm_kernel<MODE, PLANES>, dim3(grid), dim3(kGemmThreads), smem, s, 2, a, b, g);
 }
 
-#define CE_TRY(expr)                      \
+#define CE_TRY(...)                       \
   do {                                    \
-    const cudaError_t e_ = (expr);        \
+    const cudaError_t e_ = (__VA_ARGS__); \
     if (e_ != cudaSuccess) return e_;     \
   } while (0)
 
@@ -679,9 +687,8 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   const int64_t hplane = l.padded * l.Dp, wplane = a.V * wld;
   CUtensorMap h_rows, w_rows;  // K = D contiguous
   CE_TRY(make_map(&h_rows, hp, D, l.padded, P, l.Dp, hplane, kM));
-  const int terms = bf16 ? 1 : 6;
   const int64_t d_blocks = (a.D + kK - 1) / kK;
-  const int logits_n = plan_tiles(a.T, a.V, d_blocks, terms, 128, 1).tile_n;
+  const int logits_n = plan_tiles(a.T, a.V, d_blocks, P, 128, 1).tile_n;
   CE_TRY(make_map(&w_rows, wt, D, a.V, P, wld, wplane, logits_n / 2));
   Gemm g = {};
   g.head = head;
@@ -689,7 +696,6 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.target = target;
   g.T = T;
   g.D = D;
-  g.terms = terms;
   g.spin_limit = a.spin_limit;
   g.status = a.status;
   g.part = reinterpret_cast<float2*>(ws + l.part);
@@ -704,14 +710,13 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
   g.dw_wide = (a.lddw * sizeof(E)) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 32 == 0;
-  // K blocks of an accumulator.  fp32 results: 8 steps for logits, 16 for gradients
-  // (six plane products keep the units busy for each).  bf16 gradients: any number.
-  // bf16 logits: 64 steps keep the mean over many tokens to 3e-7 of the loss; few
-  // tokens, where the products wait for memory anyway, get 8.
-  const int any = 1 << 30, few = 2, some = 4;
-  const int logits = bf16 && a.T > kPair ? 16 : few;
+  // K blocks of an accumulator.  fp32: 48 steps.  bf16
+  // gradients: any number.  bf16 logits: 64 steps keep the mean over many tokens to
+  // 3e-7 of the loss; few tokens, where the products wait for memory anyway, get 8.
+  const int any = 1 << 30;
+  const int logits = !bf16 ? 2 : a.T > kPair ? 16 : 2, gradients = bf16 ? any : 2;
   const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
-  const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, terms, 64, 1).tile_n;
+  const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, P, 64, 1).tile_n;
   const unsigned out_blocks =
       static_cast<unsigned>(std::min<int64_t>((a.T * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
   auto dh_out = [&](const float* scale, const float* coef) {
@@ -748,11 +753,11 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.ref = ref;
     g.chunk = logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_sum_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, g.part, l.parts, floats(l.sums), ref,
                          ints(l.flags)));
     g.redo = ints(l.flags);
-    CE_TRY(launch_gemm<kExp>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(by_targets());
     CE_TRY(make_map(&h_cols, hs, D, l.padded, P, l.Dp, hplane, kK));
     CE_TRY(make_map(&c_rows, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kM));
@@ -760,11 +765,11 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.first = 1;
     g.splits = dh_plan.splits;
     g.tile_n = dh_plan.tile_n;
-    g.chunk = bf16 ? any : some;
-    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
+    g.chunk = gradients;
+    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
     CE_TRY(dh_out(scale, factor));
     g.tile_n = dw_n;
-    return launch_gemm<kDw>(c_cols, h_cols, g, a.V, a.D, num_sms, s);
+    return launch_gemm<kDw, P>(c_cols, h_cols, g, a.V, a.D, num_sms, s);
   }
 
   const float* lse = a.lse_in;
@@ -773,7 +778,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.width = static_cast<int>(a.V);
     g.chunk = logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kLoss>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kLoss, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_finish_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, row, place, g.part, l.parts,
                          g.at_target, a.loss, out));
     lse = out;
@@ -798,14 +803,14 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.first = v0 == 0;
     CE_TRY(make_map(&c_rows, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kM));
     CE_TRY(make_map(&c_cols, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kK));
-    g.chunk = bf16 ? any : few;
+    g.chunk = bf16 ? any : logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kCoef>(h_rows, w_rows, g, a.T, width, num_sms, s));
-    g.chunk = bf16 ? any : some;
+    CE_TRY(launch_gemm<kCoef, P>(h_rows, w_rows, g, a.T, width, num_sms, s));
+    g.chunk = gradients;
     g.tile_n = dh_plan.tile_n;
-    CE_TRY(launch_gemm<kDh>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
+    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
     g.tile_n = dw_n;
-    CE_TRY(launch_gemm<kDw>(c_cols, h_cols, g, width, a.D, num_sms, s));
+    CE_TRY(launch_gemm<kDw, P>(c_cols, h_cols, g, width, a.D, num_sms, s));
   }
   return dh_out(nullptr, l.apart ? factor : nullptr);
 }

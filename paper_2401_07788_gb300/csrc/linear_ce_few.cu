@@ -246,13 +246,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
       const int t = (idx + i) % TT;
       const int64_t v = v0 + (idx + i) / TT;
       if (v < f.V && counts) {
-        if (v == target[i]) f.at[t] = acc[i];
         if (f.logits != nullptr && t < f.T) f.logits[t * f.V + v] = acc[i];
+        if (v == target[i]) {  // out of the sum: a small loss is the logarithm of 1 + the others
+          f.at[t] = acc[i];
+          continue;
+        }
         const float l = fmul(acc[i], kL2e);
         const float up = fmaxf(top[i], l);
         if (up != -INFINITY) {
           const float old = top[i] == -INFINITY ? 0.0f : fmul(sum[i], exp2f(fsub(top[i], up)));
-          // the rounding of l is undone in the sum: both sides of loss use the exact product
+          // one rounding in the exponent, as in the loss
           sum[i] = fadd(old, exp2f(__fmaf_rn(acc[i], kL2e, -up)));
           top[i] = up;
         } else if (acc[i] != acc[i]) {
@@ -306,9 +309,10 @@ __global__ void __launch_bounds__(kFewTokens * 32) ce_few_finish_kernel(const Fe
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
   if (lane == 0) {
-    const float l = log2f(s);
-    f.lse[t] = live ? fmul(fadd(m, l), kL2) : 0.0f;
-    if (f.loss != nullptr) f.loss[t] = live ? fmul(fsub(l, __fmaf_rn(f.at[t], kL2e, -m)), kL2) : 0.0f;
+    const float l = f.at[t], d = __fmaf_rn(l, kL2e, -m), ratio = fmul(s, exp2f(-d));
+    const float loss = ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kL2);
+    f.lse[t] = live ? fadd(l, loss) : 0.0f;
+    if (f.loss != nullptr) f.loss[t] = live ? loss : 0.0f;
   }
 }
 

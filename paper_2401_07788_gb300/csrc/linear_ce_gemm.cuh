@@ -13,7 +13,7 @@ constexpr int kM = 128;        // rows of a CTA's output tile (lanes of tensor m
 constexpr int kPair = 2 * kM;  // rows of a CTA pair's output tile
 constexpr int kN = 256;        // columns of an output tile
 constexpr int kK = 64;         // K elements of a stage: 128 bytes, one swizzle row
-constexpr int kStages = 6;
+constexpr int kStages = 6;    // of one plane; fp32 has kStages / 3 of three
 constexpr int kBytesA = kM * kK * 2;
 constexpr int kBytesB = kN / 2 * kK * 2;
 constexpr int kStageBytes = kBytesA + kBytesB;
@@ -53,21 +53,23 @@ __device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
 // A persistent pair of CTAs on two SMs per tile, 128 rows each: every CTA copies
 // its rows of A and half the rows of B, so an SM reads 32 KB from L2 for 2^20
 // products (48 KB with a tile of its own).  Warp 0 copies operand tiles through
-// tensor maps (kStages stages of 32 KB a CTA), one thread of the first CTA's warp
+// tensor maps (six stages of 32 KB a CTA; for fp32 two stages with the three planes
+// of both operands, which serve six plane products), one thread of the first CTA's warp
 // 1 issues the products of both, eight warps a CTA take the finished tile from
 // tensor memory.  Two
 // accumulators of 256 columns fill the tensor memory, so a tile's epilogue runs
 // under the next tile's products.
 //
 // kLoss   A = h [valid][D],  B = w [V][D]: a tile's logits become, for each token
-//         and half tile, their largest and the sum of exponentials over it.
+//         and half tile, their largest and the sum of exponentials over it, the
+//         target's logit left out and kept by itself.
 // kExp    the same for a training step that keeps the exponentials: with a reference
 //         ref[t] near the logits, e = 2^(l log2e - ref) rounded to bf16 planes (its
 //         relative error is that of a rounded probability) and their sums.  The
 //         factor that makes them coefficients is applied where it is exact: to dh's
-//         sums, and to h for dw.  e of the target is 0: its coefficient p - 1 is a
-//         difference, and goes its own way in fp32.  ref is the target's logit, so a
-//         sum is out of range only for a token with a loss over 27; such tokens set
+//         sums, and to h for dw.  e of the target is 0: its coefficient p - 1 goes its
+//         own way in fp32.  ref is the target's logit, so a sum is out of range only
+//         for a token with a loss over 27; such tokens set
 //         a flag, take their largest logit as ref, and a second launch of the kernel
 //         (which returns at once without a flag) forms their row tiles again.
 // kCoef   the logits' products again, when lse is known: the coefficients c of a
@@ -78,9 +80,10 @@ __device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
 //
 // An accumulator adds each product step with truncation: about 5e-9 of its value
 // a step of 16, always towards zero (measured: dh over 50257 entries 9e-5 off).
-// Where fp32 results depend on it, an accumulator sums a chunk of K blocks only,
-// the smallest plane products first, and the epilogue adds the chunks in fp32
-// with rounding to nearest; two accumulators in turn keep the products running.
+// Where fp32 results depend on it, an accumulator sums a chunk of K blocks only
+// (within a block the smallest plane products first), and the epilogue adds the
+// chunks in fp32 with rounding to nearest; two accumulators in turn keep the
+// products running.
 // Operands whose K is not the contiguous axis (w^T, c^T, h^T) are read as they
 // are: rows of 64 M/N-elements, and the product's descriptors say so.
 // ---------------------------------------------------------------------------
@@ -94,7 +97,6 @@ struct Gemm {
   int D;
   int width;            // vocabulary entries of the piece
   int64_t v0;           // its first one
-  int terms;            // 1 (bf16) or 6 (fp32 in three planes)
   int tile_n;           // columns of a tile: 64 (dh, dw), 128 or 256
   int chunk;            // K blocks that one accumulator sums (see ce_gemm_kernel)
   int splits;           // kDh: parts of K
@@ -121,9 +123,10 @@ struct Gemm {
   unsigned* status;
 };
 
-// Plane pair of a term, smallest products first.
-__device__ __forceinline__ void term_planes(int terms, int t, int* a, int* b) {
-  if (terms == 1) {
+// Plane pair of a product, smallest products first.
+template <int PLANES>
+__device__ __forceinline__ void term_planes(int t, int* a, int* b) {
+  if (PLANES == 1) {
     *a = *b = 0;
   } else {  // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), two bits each
     *a = (0x052 >> (2 * t)) & 3;
@@ -187,9 +190,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // A lane's row of a half tile as bf16 planes of the coefficients.
+template <int PLANES>
 __device__ __forceinline__ void store_planes(const Gemm& g, int64_t m, int n0, const float (&x)[kHalf]) {
   uint16_t* out = g.coef + m * g.ldc + n0;
-  if (g.terms == 1) {
+  if (PLANES == 1) {
 #pragma unroll
     for (int j = 0; j < kHalf; j += 16) {
       uint32_t u[8];
@@ -216,7 +220,7 @@ __device__ __forceinline__ void store_planes(const Gemm& g, int64_t m, int n0, c
 }
 
 // One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
-template <int MODE>
+template <int MODE, int PLANES>
 __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf],
                                          float* scratch) {
   if (MODE == kLoss || MODE == kExp) {
@@ -231,12 +235,14 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         for (int j = 0; j < kHalf; ++j)
           if (j >= cols) x[j] = -INFINITY;
       }
-      const bool here = y >= 0 && y < cols;
-      if (here) {
+      if (y >= 0 && y < cols) {  // out of the sum: a small loss is the logarithm of 1 + the others
         float v = x[0];
 #pragma unroll
         for (int j = 1; j < kHalf; ++j) v = j == y ? x[j] : v;
         g.at_target[m] = v;
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j)
+          if (j == y) x[j] = -INFINITY;
       }
       // base 2 throughout: exp(l - top) = 2^(l log2e - top log2e), one rounding in the exponent
       float top = x[0];
@@ -253,18 +259,13 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
       }
       g.part[static_cast<int64_t>(n0 / kHalf) * g.T + m] =
           make_float2(base, fadd(fadd(sum[0], sum[1]), fadd(sum[2], sum[3])));
-      if (MODE == kExp && here) {
-#pragma unroll
-        for (int j = 0; j < kHalf; ++j)
-          if (j == y) x[j] = 0.0f;
-      }
     }
     if (MODE == kExp) {
       if (!live) {
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) x[j] = 0.0f;
       }
-      store_planes(g, m, n0, x);
+      store_planes<PLANES>(g, m, n0, x);
     }
   } else if (MODE == kCoef) {
     if (n0 >= g.ldc) return;
@@ -294,7 +295,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
       for (int j = 0; j < kHalf; ++j)
         if (j == y) x[j] = at_y;
     }
-    store_planes(g, m, n0, x);
+    store_planes<PLANES>(g, m, n0, x);
   } else if (MODE == kDh) {
     if (m >= valid) return;
     float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
@@ -404,7 +405,7 @@ __device__ __forceinline__ int tile_cols(const Gemm& g, int cols, int n0) {
   return min((cols - n0 + 15) / 16 * 16, g.tile_n);
 }
 
-template <int MODE>
+template <int MODE, int PLANES>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ Gemm g) {
@@ -447,6 +448,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const int total = s.total();
   const int cols = MODE == kDh || MODE == kDw ? g.D : g.width;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  constexpr uint32_t stages = kStages / PLANES;
 
   if (warp == 0) {
     if (lane == 0) {
@@ -455,35 +457,32 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       bool ok = true;
       // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
       const int b_blocks = (g.tile_n / 2 + 63) / 64;
-      const uint32_t bytes = 2 * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
+      const uint32_t bytes = 2 * PLANES * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
       for (int i = pair; i < total && ok; i += pairs) {
         const Tile t = tile_of<MODE>(g, s, i);
         if (skipped<MODE>(g, t)) continue;
         const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g, cols, t.n0) / 2);
-        for (int c = t.k0; c < t.k1 && ok; c += g.chunk) {
-          const int blocks = min(g.chunk, t.k1 - c);
-          for (int j = 0; j < blocks * g.terms; ++j, ++it) {
-            const int kb = c + j % blocks;
-            const int st = it % kStages;
-            ok = mbar_wait_bounded(&empty[st], (it / kStages & 1) ^ 1, g.spin_limit, g.status);
-            if (!ok) break;
-            int pa, pb;
-            term_planes(g.terms, j / blocks, &pa, &pb);
-            uint8_t* a = stage0 + st * kStageBytes;
+        for (int kb = t.k0; kb < t.k1; ++kb, ++it) {
+          const int st = it % stages;
+          ok = mbar_wait_bounded(&empty[st], (it / stages & 1) ^ 1, g.spin_limit, g.status);
+          if (!ok) break;
+          const uint32_t bar = dsmem_addr(&full[st], 0);
+          if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
+#pragma unroll
+          for (int p = 0; p < PLANES; ++p) {
+            uint8_t* a = stage0 + (st * PLANES + p) * kStageBytes;
             uint8_t* b = a + kBytesA;
-            const uint32_t bar = dsmem_addr(&full[st], 0);
-            if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
             if (A_MN) {
 #pragma unroll
-              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, pa, bar);
+              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, p, bar);
             } else {
-              tensor_g2s(a, &map_a, kb * kK, m0, pa, bar);
+              tensor_g2s(a, &map_a, kb * kK, m0, p, bar);
             }
             if (B_MN) {
               const int k_at = kb * kK + (MODE == kDh ? static_cast<int>(g.v0) : 0);
-              for (int q = 0; q < b_blocks; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, pb, bar);
+              for (int q = 0; q < b_blocks; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, k_at, p, bar);
             } else {
-              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, pb, bar);
+              tensor_g2s(b, &map_b, kb * kK, static_cast<int>(g.v0) + n0, p, bar);
             }
           }
         }
@@ -493,8 +492,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       // the second one may have sent some that the first no longer counts, and
       // gives them a millisecond.
       if (rank == 0) {
-        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-          mbar_wait_bounded(&full[i % kStages], i / kStages & 1, kDrainPolls, g.status);
+        for (uint32_t i = it > stages ? it - stages : 0; i < it; ++i)
+          mbar_wait_bounded(&full[i % stages], i / stages & 1, kDrainPolls, g.status);
       } else if (!ok) {
         const uint64_t until = global_ns() + 1000000;
         while (global_ns() < until) __nanosleep(1000);
@@ -513,20 +512,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           tc_fence_after();
           const uint32_t d = acc + (n & 1) * kN;
           bool fresh = true;
-          const int steps = min(g.chunk, t.k1 - c) * g.terms;
-          for (int k = 0; k < steps && ok; ++k, ++it) {
-            const int st = it % kStages;
-            ok = mbar_wait_bounded(&full[st], it / kStages & 1, g.spin_limit, g.status);
+          const int steps = min(g.chunk, t.k1 - c);
+          for (int k = 0; k < steps; ++k, ++it) {
+            const int st = it % stages;
+            ok = mbar_wait_bounded(&full[st], it / stages & 1, g.spin_limit, g.status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t a = smem_addr(stage0 + st * kStageBytes), b = a + kBytesA;
+            const uint32_t base = smem_addr(stage0 + st * PLANES * kStageBytes);
 #pragma unroll
-            for (int q = 0; q < kK / 16; ++q) {
-              // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
-              const uint64_t da = A_MN ? smem_desc(a + q * 2048, kK * 128, 1024) : smem_desc(a + q * 32, 16, 1024);
-              const uint64_t db = B_MN ? smem_desc(b + q * 2048, kK * 128, 1024) : smem_desc(b + q * 32, 16, 1024);
-              mma_bf16(d, da, db, idesc, fresh);
-              fresh = false;
+            for (int term = 0; term < (PLANES == 1 ? 1 : 6); ++term) {
+              int pa, pb;
+              term_planes<PLANES>(term, &pa, &pb);
+              const uint32_t a = base + pa * kStageBytes, b = base + pb * kStageBytes + kBytesA;
+#pragma unroll
+              for (int q = 0; q < kK / 16; ++q) {
+                // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
+                const uint64_t da = A_MN ? smem_desc(a + q * 2048, kK * 128, 1024) : smem_desc(a + q * 32, 16, 1024);
+                const uint64_t db = B_MN ? smem_desc(b + q * 2048, kK * 128, 1024) : smem_desc(b + q * 32, 16, 1024);
+                mma_bf16(d, da, db, idesc, fresh);
+                fresh = false;
+              }
             }
             mma_commit_pair(&empty[st]);
           }
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if (!ok) break;
       if (half * kHalf >= g.tile_n) continue;
-      epilogue<MODE>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x,
+      epilogue<MODE, PLANES>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x,
                      scratch + (MODE == kDw ? (warp - 2) * 32 * 17 : 0));
     }
   }
