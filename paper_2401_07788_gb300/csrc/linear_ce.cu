@@ -631,15 +631,16 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t r
 }
 
 template <int MODE, int PLANES>
-cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const Gemm& g, int64_t m, int64_t n, int num_sms,
+cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const Gemm& g, int64_t m, int64_t n, int num_sms,
                         cudaStream_t s) {
   const int64_t tiles = (m + kPair - 1) / kPair * ((n + g.tile_n - 1) / g.tile_n) * (MODE == kDh ? g.splits : 1);
   if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
-  constexpr int smem = kStages * kStageBytes + 1024;
+  constexpr bool stores = MODE == kExp || MODE == kCoef;
+  constexpr int smem = kStages * kStageBytes + 1024 + (stores ? kEpiWarps * kStoreBytes : 0);
   const cudaError_t e = ensure_dynamic_smem(ce_gemm_kernel<MODE, PLANES>, smem);
   if (e != cudaSuccess) return e;
   const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(tiles, num_sms / 2));
-  return launch_kernel(ce_gemm_kernel<MODE, PLANES>, dim3(grid), dim3(kGemmThreads), smem, s, 2, a, b, g);
+  return launch_kernel(ce_gemm_kernel<MODE, PLANES>, dim3(grid), dim3(kGemmThreads), smem, s, 2, a, b, c, g);
 }
 
 #define CE_TRY(...)                       \
@@ -700,9 +701,8 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.status = a.status;
   g.part = reinterpret_cast<float2*>(ws + l.part);
   g.at_target = floats(l.at_target);
-  g.coef = reinterpret_cast<uint16_t*>(ws + l.coef);
-  g.ldc = l.ldc;
-  g.coef_plane = l.padded * l.ldc;
+  uint16_t* coef = reinterpret_cast<uint16_t*>(ws + l.coef);
+  const int64_t coef_plane = l.padded * l.ldc;
   g.sum = floats(l.sum);
   g.lds = l.Dp;
   g.sum_split = l.padded * l.Dp;
@@ -725,6 +725,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
                          wide_dh);
   };
   CUtensorMap w_cols, h_cols, c_rows, c_cols;  // K = vocabulary, tokens: boxes of 64 columns x 64 k
+  CUtensorMap c_out;                           // boxes of 64 columns x 32 rows
   if (pass != kForward) CE_TRY(make_map(&w_cols, wt, D, a.V, P, wld, wplane, kK));
 
   int* pos = ints(l.pos);
@@ -749,27 +750,28 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     uint16_t* hs = reinterpret_cast<uint16_t*>(ws + l.hs);
     f.hs = hs;
     CE_TRY(rank());
+    CE_TRY(make_map(&c_out, coef, a.V, l.padded, P, l.ldc, coef_plane, 32));
     g.width = static_cast<int>(a.V);
     g.ref = ref;
     g.chunk = logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, c_out, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_sum_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, g.part, l.parts, floats(l.sums), ref,
                          ints(l.flags)));
     g.redo = ints(l.flags);
-    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kExp, P>(h_rows, w_rows, c_out, g, a.T, a.V, num_sms, s));
     CE_TRY(by_targets());
     CE_TRY(make_map(&h_cols, hs, D, l.padded, P, l.Dp, hplane, kK));
-    CE_TRY(make_map(&c_rows, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kM));
-    CE_TRY(make_map(&c_cols, g.coef, a.V, l.padded, P, l.ldc, g.coef_plane, kK));
+    CE_TRY(make_map(&c_rows, coef, a.V, l.padded, P, l.ldc, coef_plane, kM));
+    CE_TRY(make_map(&c_cols, coef, a.V, l.padded, P, l.ldc, coef_plane, kK));
     g.first = 1;
     g.splits = dh_plan.splits;
     g.tile_n = dh_plan.tile_n;
     g.chunk = gradients;
-    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
+    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, w_cols, g, a.T, a.D, num_sms, s));
     CE_TRY(dh_out(scale, factor));
     g.tile_n = dw_n;
-    return launch_gemm<kDw, P>(c_cols, h_cols, g, a.V, a.D, num_sms, s);
+    return launch_gemm<kDw, P>(c_cols, h_cols, h_cols, g, a.V, a.D, num_sms, s);
   }
 
   const float* lse = a.lse_in;
@@ -778,7 +780,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.width = static_cast<int>(a.V);
     g.chunk = logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kLoss, P>(h_rows, w_rows, g, a.T, a.V, num_sms, s));
+    CE_TRY(launch_gemm<kLoss, P>(h_rows, w_rows, w_rows, g, a.T, a.V, num_sms, s));
     CE_TRY(launch_kernel(ce_finish_kernel, dim3(rows32), dim3(1024), 0, s, 0, T, head, row, place, g.part, l.parts,
                          g.at_target, a.loss, out));
     lse = out;
@@ -801,16 +803,17 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.v0 = v0;
     g.width = width;
     g.first = v0 == 0;
-    CE_TRY(make_map(&c_rows, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kM));
-    CE_TRY(make_map(&c_cols, g.coef, width, l.padded, P, l.ldc, g.coef_plane, kK));
+    CE_TRY(make_map(&c_rows, coef, width, l.padded, P, l.ldc, coef_plane, kM));
+    CE_TRY(make_map(&c_cols, coef, width, l.padded, P, l.ldc, coef_plane, kK));
+    CE_TRY(make_map(&c_out, coef, width, l.padded, P, l.ldc, coef_plane, 32));
     g.chunk = bf16 ? any : logits;
     g.tile_n = logits_n;
-    CE_TRY(launch_gemm<kCoef, P>(h_rows, w_rows, g, a.T, width, num_sms, s));
+    CE_TRY(launch_gemm<kCoef, P>(h_rows, w_rows, c_out, g, a.T, width, num_sms, s));
     g.chunk = gradients;
     g.tile_n = dh_plan.tile_n;
-    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, g, a.T, a.D, num_sms, s));
+    CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, w_cols, g, a.T, a.D, num_sms, s));
     g.tile_n = dw_n;
-    CE_TRY(launch_gemm<kDw, P>(c_cols, h_cols, g, width, a.D, num_sms, s));
+    CE_TRY(launch_gemm<kDw, P>(c_cols, h_cols, h_cols, g, width, a.D, num_sms, s));
   }
   return dh_out(nullptr, l.apart ? factor : nullptr);
 }

@@ -18,6 +18,7 @@ constexpr int kBytesA = kM * kK * 2;
 constexpr int kBytesB = kN / 2 * kK * 2;
 constexpr int kStageBytes = kBytesA + kBytesB;
 constexpr int kEpiWarps = 8;
+constexpr int kStoreBytes = 4096;  // of an epilogue warp's stores of c
 constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
 constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
 constexpr int kRun = 32;       // sorted tokens whose target gradients one CTA sums
@@ -112,8 +113,6 @@ struct Gemm {
   const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
   const float* loss;    // kCoef: [T] by token where the forward pass gave it, or nullptr
   int apart;            // kCoef: the target's c goes its own way in fp32
-  uint16_t* coef;       // kExp, kCoef: [plane][rows][ldc]
-  int64_t ldc, coef_plane;
   float* sum;           // kDh: [split][rows][lds]
   int64_t lds, sum_split;
   void* dw;             // kDw
@@ -133,6 +132,12 @@ __device__ __forceinline__ void term_planes(int t, int* a, int* b) {
     *b = (0x118 >> (2 * t)) & 3;
   }
 }
+
+// What an epilogue needs of its row, loaded before the tile is waited for.
+struct Row {
+  int target;
+  float ref;  // kExp
+};
 
 struct Tile {
   int m0, n0, split, k0, k1;  // K blocks [k0, k1)
@@ -189,47 +194,54 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return u;
 }
 
-// A lane's row of a half tile as bf16 planes of the coefficients.
+// A warp's 32 rows of a half tile as bf16 planes of the coefficients, by tensor-map
+// stores of 64 columns from its 4 KB of shared memory: a row's 16-byte groups lie
+// swizzled, so the lanes' writes meet in no bank, and HBM gets whole lines (one
+// 32-byte store a lane reached 32 lines an instruction).  What lies outside the
+// piece is not written.
 template <int PLANES>
-__device__ __forceinline__ void store_planes(const Gemm& g, int64_t m, int n0, const float (&x)[kHalf]) {
-  uint16_t* out = g.coef + m * g.ldc + n0;
-  if (PLANES == 1) {
+__device__ __forceinline__ void store_planes(const Gemm& g, const CUtensorMap* map, uint8_t* buf, int m, int n0,
+                                             float (&x)[kHalf]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int j = 0; j < kHalf; j += 16) {
-      uint32_t u[8];
+  for (int h = 0; h < kHalf; h += 64) {
+    if (n0 + h < g.width) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) u[q] = pack_bf16(x[j + 2 * q], x[j + 2 * q + 1]);
-      st_v8(out + j, u);
-    }
-  } else {
+      for (int p = 0; p < PLANES; ++p) {
+        uint32_t u[32];
 #pragma unroll
-    for (int j = 0; j < kHalf; j += 16) {
-      uint32_t u[3][8];
+        for (int q = 0; q < 32; ++q) {
+          float &lo = x[h + 2 * q], &hi = x[h + 2 * q + 1];
+          u[q] = pack_bf16(lo, hi);
+          if (p + 1 < PLANES) {
+            lo = fsub(lo, __uint_as_float(u[q] << 16));
+            hi = fsub(hi, __uint_as_float(u[q] & 0xffff0000u));
+          }
+        }
+        if (lane == 0) bulk_wait_read();
+        __syncwarp();
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        uint16_t a[3], b[3];
-        split(x[j + 2 * q], a);
-        split(x[j + 2 * q + 1], b);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) u[k][q] = a[k] | static_cast<uint32_t>(b[k]) << 16;
+        for (int c = 0; c < 8; ++c)
+          *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) * 16)) =
+              make_uint4(u[4 * c], u[4 * c + 1], u[4 * c + 2], u[4 * c + 3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) tensor_s2g(map, n0 + h, m - lane, p, buf);
       }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) st_v8(out + k * g.coef_plane + j, u[k]);
     }
   }
 }
 
 // One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
 template <int MODE, int PLANES>
-__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, float (&x)[kHalf],
-                                         float* scratch) {
+__device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, const Row& row, float (&x)[kHalf],
+                                         float* scratch, const CUtensorMap* map_c, uint8_t* buf) {
   if (MODE == kLoss || MODE == kExp) {
     const int cols = min(g.width - n0, kHalf);
     if (MODE == kLoss && (cols <= 0 || m >= valid)) return;
-    if (MODE == kExp && (n0 >= g.ldc)) return;
     const bool live = m < valid;
     if (live && cols > 0) {
-      const int y = static_cast<int>(g.target[m] - n0);
+      const int y = row.target - n0;
       if (cols < kHalf) {
 #pragma unroll
         for (int j = 0; j < kHalf; ++j)
@@ -245,11 +257,12 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
           if (j == y) x[j] = -INFINITY;
       }
       // base 2 throughout: exp(l - top) = 2^(l log2e - top log2e), one rounding in the exponent
-      float top = x[0];
+      float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-      for (int j = 1; j < kHalf; ++j) top = fmaxf(top, x[j]);
+      for (int j = 4; j < kHalf; ++j) tops[j & 3] = fmaxf(tops[j & 3], x[j]);
+      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       const float base = fmul(top, kLog2e);
-      const float shift = MODE == kExp ? -g.ref[m] : base == -INFINITY ? 0.0f : -base;
+      const float shift = MODE == kExp ? -row.ref : base == -INFINITY ? 0.0f : -base;
       float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < kHalf; ++j) {
@@ -265,10 +278,9 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) x[j] = 0.0f;
       }
-      store_planes<PLANES>(g, m, n0, x);
+      store_planes<PLANES>(g, map_c, buf, m, n0, x);
     }
   } else if (MODE == kCoef) {
-    if (n0 >= g.ldc) return;
     const bool live = m < valid;
     float shift = 0.0f, scale = 0.0f, at_y = 0.0f;
     int y = -1;
@@ -295,7 +307,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
       for (int j = 0; j < kHalf; ++j)
         if (j == y) x[j] = at_y;
     }
-    store_planes<PLANES>(g, m, n0, x);
+    store_planes<PLANES>(g, map_c, buf, m, n0, x);
   } else if (MODE == kDh) {
     if (m >= valid) return;
     float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
@@ -408,7 +420,7 @@ __device__ __forceinline__ int tile_cols(const Gemm& g, int cols, int n0) {
 template <int MODE, int PLANES>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const __grid_constant__ Gemm g) {
+                   const __grid_constant__ CUtensorMap map_c, const __grid_constant__ Gemm g) {
   constexpr bool A_MN = MODE == kDw, B_MN = MODE == kDh || MODE == kDw;
   extern __shared__ uint8_t raw[];
   // full and taken are used in the first CTA, for both; empty and done in each
@@ -550,6 +562,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     for (int i = pair; i < total; i += pairs) {
       const Tile t = tile_of<MODE>(g, s, i);
       if (skipped<MODE>(g, t)) continue;
+      const int m = t.m0 + rank * kM + quad * 32 + lane;
+      Row row = {-1, 0.0f};
+      if ((MODE == kLoss || MODE == kExp) && m < valid) {
+        row.target = g.target[m];
+        if (MODE == kExp) row.ref = g.ref[m];
+      }
       float x[kHalf];
       if (t.k0 == t.k1) {
 #pragma unroll
@@ -591,10 +609,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if (!ok) break;
       if (half * kHalf >= g.tile_n) continue;
-      epilogue<MODE, PLANES>(g, valid, t, t.m0 + rank * kM + quad * 32 + lane, t.n0 + half * kHalf, x,
-                     scratch + (MODE == kDw ? (warp - 2) * 32 * 17 : 0));
+      epilogue<MODE, PLANES>(g, valid, t, m, t.n0 + half * kHalf, row, x, scratch + (MODE == kDw ? (warp - 2) * 32 * 17 : 0),
+                             &map_c, stage0 + kStages * kStageBytes + (warp - 2) * kStoreBytes);
     }
   }
+  if ((MODE == kExp || MODE == kCoef) && lane == 0) bulk_wait();
   __syncwarp();
   tc_fence_before();
   __syncthreads();
