@@ -710,11 +710,12 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
   g.dw_wide = (a.lddw * sizeof(E)) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 32 == 0;
-  // K blocks of an accumulator.  fp32: 48 steps.  bf16
-  // gradients: any number.  bf16 logits: 64 steps keep the mean over many tokens to
-  // 3e-7 of the loss; few tokens, where the products wait for memory anyway, get 8.
-  const int any = 1 << 30;
-  const int logits = !bf16 ? 2 : a.T > kPair ? 16 : 2, gradients = bf16 ? any : 2;
+  // K blocks of an accumulator.  fp32: 96 steps over many tokens (2.5e-7; 48 steps
+  // cost 3 to 8 % there), 48 for few.  bf16 gradients: any number.  bf16 logits: 64
+  // steps keep the mean over many tokens to 3e-7 of the loss; few tokens, where the
+  // products wait for memory anyway, get 8.
+  const int any = 1 << 30, exact = a.T > kPair ? 4 : 2;
+  const int logits = !bf16 ? exact : a.T > kPair ? 16 : 2, gradients = bf16 ? any : exact;
   const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
   const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, P, 64, 1).tile_n;
   const unsigned out_blocks =
