@@ -386,8 +386,8 @@ typedef struct {
  *   m <- beta1 m + (1-beta1) g;   v <- beta2 v + ((1-beta2) g) g;
  *   p <- p (1 - lr' wd) - lr'/(1-beta1^step) * (m / (sqrt(v)/sqrt(1-beta2^step) + eps)),
  * lr' = lr lr_scale; every step one fp32 round-to-nearest operation (with 8-bit
- * states the last root and quotient carry up to 2 ulp more), rounded to param_type
- * at the end.
+ * states the root and the quotient carry up to 2 ulp more, and a v below 2^-126
+ * counts as 0 in the root), rounded to param_type at the end.
  *   state_bits 32: m and v are fp32.  8: codes in blocks of MPC_ADAMW_BLOCK
  *     consecutive entries of a tensor that share one fp32 scale s, the largest
  *     |m| (v) of the block: code c of m stands for sign(c) (c/127)^2 s, of v for

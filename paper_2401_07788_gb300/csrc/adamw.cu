@@ -19,8 +19,8 @@
 // What bounds it: memory.  fp32 states move 28 bytes an entry (p, m, v read and
 // written, g read).  The work is laid out over chunks of 2048 entries that never
 // straddle two tensors: a CTA of 256 threads takes a contiguous range of chunks
-// of the whole list, a warp 256 entries, a lane 8 consecutive ones (16-byte
-// loads; a warp's entries are one 8-bit block, so a block's largest is one warp
+// of the whole list, a warp 256 entries, a lane 8 consecutive ones (32-byte
+// accesses in fp32; a warp's entries are one 8-bit block, so a block's largest is one warp
 // reduction).  The list travels as a kernel argument: no copy to the device
 // precedes the launch, and a captured graph holds it by value.
 #include <algorithm>
@@ -50,7 +50,7 @@ struct Entry {
   float keep;  // 1 - lr wd
   float step;  // lr / (1 - b1^t)
   int first;   // the tensor's first chunk in the launch
-  int wide;    // every pointer suits 16-byte accesses
+  int wide;    // every pointer is on 32 bytes
 };
 
 template <int N>
@@ -101,6 +101,8 @@ __device__ __forceinline__ void for_range(const Table<N>& t, F f) {
   }
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 __device__ __forceinline__ float bf_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
@@ -110,13 +112,13 @@ __device__ __forceinline__ uint32_t bf_pack(float lo, float hi) {
   return u;
 }
 
-// Eight entries from i on as floats (left = how many of them exist).
+// Eight entries from i on as floats (left = how many of them exist).  fp32 goes by
+// 32-byte accesses: a lane's whole sector at once.
 __device__ __forceinline__ void load8(const float* p, int64_t i, int left, bool wide, float (&x)[8]) {
   if (wide && left >= 8) {
-    const float4 a = *reinterpret_cast<const float4*>(p + i);
-    const float4 b = *reinterpret_cast<const float4*>(p + i + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                 : "l"(p + i));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = j < left ? p[i + j] : 0.0f;
@@ -134,8 +136,9 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, int64_t i, int lef
 }
 __device__ __forceinline__ void store8(float* p, int64_t i, int left, bool wide, const float (&x)[8]) {
   if (wide && left >= 8) {
-    *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "f"(x[0]), "f"(x[1]),
+                 "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                 : "memory");
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -199,35 +202,35 @@ __device__ __forceinline__ float inverse(float top) {
   return top < 1.17549435e-38f ? 0.0f : fdiv(1.0f, top);
 }
 
-__device__ __forceinline__ float root_approx(float x) {
+__device__ __forceinline__ float root_approx(float x) {  // subnormal x counts as 0
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-
-__device__ __forceinline__ float root_any(float x) {  // subnormals too
+__device__ __forceinline__ float inverse_approx(float x) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
-// The code of y in [0, 1] as a float: how many midpoints lie at or below it.  The
-// midpoint under code c of LEVELS is K (2c(c-1) + 1), K = 1/(2 LEVELS^2), halfway
-// between the neighbouring squares, and its square for FOURTH (v).  c - 1/2 is the
-// root of LEVELS^2 y - 1/4 there, so an approximate root, lowered by 1e-3 (its
-// error in c is below 2e-4) and rounded, gives the code or the one before it, and
-// the exact midpoint decides: the result does not depend on the approximation.
-// (2c(c+1) + 1 is exact in fp32.)  NaN gives 0.
+// The code of y in [0, 1], as 2^23 + code: how many midpoints lie at or below y.
+// The midpoint under code c of LEVELS is K (2c(c-1) + 1), K = 1/(2 LEVELS^2),
+// halfway between the neighbouring squares, and its square for FOURTH (v).  There
+// the root of LEVELS^2 y - 1/4 is c - 1/2, so the floor of an approximate root
+// (off by less than 2e-4) is the code or the one before it, and the exact midpoint
+// over it decides: the result does not depend on the approximation.  (2c(c+1) + 1
+// is exact in fp32.  Below a quarter the root of the negative value's magnitude,
+// at most 1/2, gives 0 as well.)
 template <int LEVELS, bool FOURTH>
 __device__ __forceinline__ float encode(float y) {
   constexpr float K = static_cast<float>(1.0 / (2.0 * LEVELS * LEVELS));
   const float s = FOURTH ? root_approx(y) : y;
-  const float z = fmaxf(__fmaf_rn(s, static_cast<float>(LEVELS * LEVELS), -0.25f), 0.0f);
-  const float c = fsub(fadd(fsub(root_approx(z), 1e-3f), kTwo23), kTwo23);
-  const float up = fadd(c, 1.0f);
-  float mid = fmul(__fmaf_rn(fadd(c, c), up, 1.0f), K);
+  const float z = __fmaf_rn(s, static_cast<float>(LEVELS * LEVELS), -0.25f);
+  const float t = __fadd_rd(root_approx(fabsf(z)), kTwo23);
+  const float c = fsub(t, kTwo23);
+  float mid = fmul(__fmaf_rn(c, __fmaf_rn(c, 2.0f, 2.0f), 1.0f), K);
   if (FOURTH) mid = fmul(mid, mid);
-  return y >= mid ? up : c;
+  return y >= mid ? fadd(t, 1.0f) : t;
 }
 
 // The low bytes of four floats in [2^23, 2^23 + 256) as one word.
@@ -260,6 +263,15 @@ __global__ void __launch_bounds__(kThreads)
       if (base >= e.n) break;  // the tensor's last chunk
       const int64_t i = base + lane * kLane;
       const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
+      if (BITS == 8 && i + kChunk < e.n) {
+        // this warp's next entries, from HBM while these are worked on: 459 -> 401 us
+        // for 153M entries (fp32 states, which have more bytes in flight, lose 6 %)
+        const int64_t next = i + kChunk;
+        prefetch_l2(static_cast<const P*>(e.param) + next);
+        prefetch_l2(static_cast<const G*>(e.grad) + next);
+        prefetch_l2(static_cast<const uint8_t*>(e.m) + next);
+        prefetch_l2(static_cast<const uint8_t*>(e.v) + next);
+      }
       float p[8], g[8], m[8], v[8];
       load8(static_cast<const G*>(e.grad), i, left, wide, g);
       load8(static_cast<const P*>(e.param), i, left, wide, p);
@@ -283,9 +295,9 @@ __global__ void __launch_bounds__(kThreads)
         v[j] = fadd(fmul(v[j], k.b2), fmul(fmul(gj, k.c2), gj));
         // 8-bit states are bound by instructions: the root and the quotient, which
         // reach param alone, are the 1 and 2 ulp ones there
-        const float root = BITS == 32 ? __fsqrt_rn(v[j]) : root_any(v[j]);
+        const float root = BITS == 32 ? __fsqrt_rn(v[j]) : root_approx(v[j]);
         const float under = fadd(fmul(root, k.rs), k.eps);
-        const float quotient = BITS == 32 ? fdiv(m[j], under) : __fdividef(m[j], under);
+        const float quotient = BITS == 32 ? fdiv(m[j], under) : fmul(m[j], inverse_approx(under));
         p[j] = fsub(fmul(p[j], keep), fmul(quotient, rate));
       }
       store8(static_cast<P*>(e.param), i, left, wide, p);
@@ -294,10 +306,14 @@ __global__ void __launch_bounds__(kThreads)
         store8(static_cast<float*>(e.m), i, left, wide, m);
         store8(static_cast<float*>(e.v), i, left, wide, v);
       } else {
+        if (left < 8) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j >= left) m[j] = v[j] = 0.0f;
+        }
         float tm = 0.0f, tv = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (j >= left) m[j] = v[j] = 0.0f;
           tm = fmaxf(tm, fabsf(m[j]));
           tv = fmaxf(tv, v[j]);
         }
@@ -306,10 +322,12 @@ __global__ void __launch_bounds__(kThreads)
         const float im = inverse(tm), iv = inverse(tv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          m[j] = fadd(copysignf(encode<127, false>(fmul(fabsf(m[j]), im)), m[j]), kTwo23 + 128.0f);
+          // 2^23 + 128 + c for m >= 0; (2^24 + 128) - (2^23 + c) below
+          const float cm = encode<127, false>(fmul(fabsf(m[j]), im));
+          m[j] = m[j] < 0.0f ? fsub(2.0f * kTwo23 + 128.0f, cm) : fadd(cm, 128.0f);
           const float y = fmul(v[j], iv);
-          const float c = encode<255, true>(y);
-          v[j] = fadd(y > 0.0f ? fmaxf(c, 1.0f) : c, kTwo23);
+          v[j] = encode<255, true>(y);
+          if (y > 0.0f) v[j] = fmaxf(v[j], kTwo23 + 1.0f);
         }
         store_codes(e.m, i, left, wide,
                     make_uint2(low_bytes(m[0], m[1], m[2], m[3]) ^ kFlip, low_bytes(m[4], m[5], m[6], m[7]) ^ kFlip));
@@ -330,24 +348,29 @@ template <int N>
 __global__ void __launch_bounds__(kThreads) adamw_decode_kernel(const __grid_constant__ Table<N> t) {
   pdl_begin();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for_range(t, [&](const Entry& e, int k0, int k1) {
-#pragma unroll 2
-    for (int chunk = k0; chunk < k1; ++chunk) {
-      const int64_t base = static_cast<int64_t>(chunk) * kChunk + warp * (32 * kLane);
-      if (base >= e.n) break;
-      const int64_t i = base + lane * kLane;
-      const int left = static_cast<int>(min64(max64(e.n - i, 0), kLane));
-      const uint2 um = load_codes(e.m, i, left, e.wide), uv = load_codes(e.v, i, left, e.wide);
-      const float sm = e.sm[base >> 8], sv = e.sv[base >> 8];
-      float m[8], v[8];
+  auto decode = [&](const Entry& e, int chunk, bool whole) {
+    const int64_t base = static_cast<int64_t>(chunk) * kChunk + warp * (32 * kLane);
+    if (!whole && base >= e.n) return;
+    const int64_t i = base + lane * kLane;
+    const int left = whole ? kLane : static_cast<int>(min64(max64(e.n - i, 0), kLane));
+    const bool wide = whole || e.wide;
+    const uint2 um = load_codes(e.m, i, left, wide), uv = load_codes(e.v, i, left, wide);
+    const float sm = e.sm[base >> 8], sv = e.sv[base >> 8];
+    float m[8], v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        m[j] = decode_m((j < 4 ? um.x : um.y) ^ kFlip, j & 3, sm);
-        v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
-      }
-      store8(static_cast<float*>(e.param), i, left, e.wide, m);
-      store8(static_cast<float*>(e.copy), i, left, e.wide, v);
+    for (int j = 0; j < 8; ++j) {
+      m[j] = decode_m((j < 4 ? um.x : um.y) ^ kFlip, j & 3, sm);
+      v[j] = decode_v(j < 4 ? uv.x : uv.y, j & 3, sv);
     }
+    store8(static_cast<float*>(e.param), i, left, wide, m);
+    store8(static_cast<float*>(e.copy), i, left, wide, v);
+  };
+  for_range(t, [&](const Entry& e, int k0, int k1) {
+    const int whole = e.wide ? static_cast<int>(min64(k1, e.n / kChunk)) : k0;
+    int chunk = k0;
+#pragma unroll 2
+    for (; chunk < whole; ++chunk) decode(e, chunk, true);  // no condition between the loads
+    for (; chunk < k1; ++chunk) decode(e, chunk, false);
   });
 }
 
@@ -358,17 +381,22 @@ __global__ void __launch_bounds__(kThreads)
     grad_square_kernel(const __grid_constant__ Table<N> t, double* part) {
   pdl_begin();
   float sum = 0.0f;
-  for_range(t, [&](const Entry& e, int k0, int k1) {
-#pragma unroll 4
-    for (int chunk = k0; chunk < k1; ++chunk) {
-      const int64_t i = static_cast<int64_t>(chunk) * kChunk + threadIdx.x * kLane;
-      float g[8];
-      load8(static_cast<const G*>(e.grad), i, static_cast<int>(min64(max64(e.n - i, 0), kLane)), e.wide, g);
-      float s = 0.0f;
+  auto add = [&](const Entry& e, int chunk, bool whole) {
+    const int64_t i = static_cast<int64_t>(chunk) * kChunk + threadIdx.x * kLane;
+    float g[8];
+    load8(static_cast<const G*>(e.grad), i, whole ? kLane : static_cast<int>(min64(max64(e.n - i, 0), kLane)),
+          whole || e.wide, g);
+    float s = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
-      sum = fadd(sum, s);
-    }
+    for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
+    sum = fadd(sum, s);
+  };
+  for_range(t, [&](const Entry& e, int k0, int k1) {
+    const int whole = e.wide ? static_cast<int>(min64(k1, e.n / kChunk)) : k0;
+    int chunk = k0;
+#pragma unroll 4
+    for (; chunk < whole; ++chunk) add(e, chunk, true);  // no condition between the loads
+    for (; chunk < k1; ++chunk) add(e, chunk, false);
   });
   __shared__ double warp_sum[kThreads / 32];
   double d = sum;
@@ -397,7 +425,7 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part,
   }
 }
 
-bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 
 // CTAs of a launch over `chunks` chunks: as many as are resident, so that every
 // CTA takes one contiguous range.
@@ -474,7 +502,7 @@ cudaError_t launch_adamw(const AdamwArgs& a, int num_sms, cudaStream_t s) {
       list[i] = Entry{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.scale_m, t.scale_v, t.copy, t.n,
                       static_cast<float>(1.0 - a.lr * t.lr_scale * t.weight_decay),
                       static_cast<float>(rate * t.lr_scale), 0,
-                      on16(t.param) && on16(t.grad) && on16(t.exp_avg) && on16(t.exp_avg_sq) && on16(t.copy)};
+                      on32(t.param) && on32(t.grad) && on32(t.exp_avg) && on32(t.exp_avg_sq) && on32(t.copy)};
     }
     cudaError_t e;
     using b16 = __nv_bfloat16;
@@ -501,7 +529,7 @@ cudaError_t launch_adamw_decode(const mpc_adamw_tensor* tensors, int64_t count, 
       float* mo = m_out[i0 + i];
       float* vo = v_out[i0 + i];
       list[i] = Entry{mo, nullptr, t.exp_avg, t.exp_avg_sq, t.scale_m, t.scale_v, vo, t.n, 0.0f, 0.0f, 0,
-                      on16(mo) && on16(vo) && on16(t.exp_avg) && on16(t.exp_avg_sq)};
+                      on32(mo) && on32(vo) && on32(t.exp_avg) && on32(t.exp_avg_sq)};
     }
     const cudaError_t e = for_tables(list, n, [&](const auto& t) {
       constexpr int N = sizeof(t.e) / sizeof(Entry);
@@ -534,7 +562,7 @@ cudaError_t launch_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, int
       list[i] = Entry{};
       list[i].grad = t.grad;
       list[i].n = t.n;
-      list[i].wide = on16(t.grad);
+      list[i].wide = on32(t.grad);
     }
     auto launch = [&](auto type) {
       using G = decltype(type);

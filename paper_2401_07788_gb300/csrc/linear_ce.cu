@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(1024)
 
 // pos[i] = tokens of the list that come before token i in the order by target,
 // then by place.  CTA (x, y) counts for 256 tokens over every gridDim.y-th block
-// of 256 others: two instructions a pair, 4 us for 8192 tokens.  Integer sums: the
+// of 256 others: two instructions a pair.  Integer sums: the
 // order of the atomics does not show.
 __global__ void __launch_bounds__(256)
     ce_rank_kernel(const Header* head, const int* __restrict__ target, int* pos) {
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(256)
   for (int d = threadIdx.x * 8; d < Dp; d += 256 * 8) {
     float s[8] = {};
     int first = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int q = 0; q < count; ++q) {
       float x[8];
       load_planes8<P>(hp + static_cast<int64_t>(at[q]) * Dp + d, plane, x);
@@ -452,6 +452,7 @@ __global__ void __launch_bounds__(256)
     const int m = place[t];
     float x[8] = {};
     if (m >= 0) {
+#pragma unroll 8
       for (int i = 0; i < splits; ++i) {
         const float4* in = reinterpret_cast<const float4*>(sum + i * sum_split + m * lds + d);
         const float4 a = in[0], b = in[1];
@@ -710,12 +711,15 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
   g.dw_wide = (a.lddw * sizeof(E)) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 32 == 0;
-  // K blocks of an accumulator.  fp32: 96 steps over many tokens (2.5e-7; 48 steps
-  // cost 3 to 8 % there), 48 for few.  bf16 gradients: any number.  bf16 logits: 64
-  // steps keep the mean over many tokens to 3e-7 of the loss; few tokens, where the
-  // products wait for memory anyway, get 8.
-  const int any = 1 << 30, exact = a.T > kPair ? 4 : 2;
-  const int logits = !bf16 ? exact : a.T > kPair ? 16 : 2, gradients = bf16 ? any : exact;
+  // K blocks of an accumulator (4 truncating steps each in bf16, 24 in fp32; about
+  // 1.4e-8 of a result a step).  fp32: two, 48 steps (four measured 3 to 8 % faster
+  // and 1.3e-6 off, more than an fp32 sum).  bf16 logits, whose loss is fp32: equal
+  // chunks of up to 12, and 2 for few tokens, where the products wait for memory
+  // anyway.  bf16 gradients: any number.
+  const int any = 1 << 30, exact = 2;
+  const int64_t parts = (d_blocks + 11) / 12;
+  const int logits = !bf16 || a.T <= kPair ? exact : static_cast<int>((d_blocks + parts - 1) / parts);
+  const int gradients = bf16 ? any : exact;
   const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
   const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, P, 64, 1).tile_n;
   const unsigned out_blocks =
@@ -735,7 +739,8 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
               floats(l.sums), a.gloss, hp, a.lse_in, nullptr, nullptr, scale, factor, ints(l.order), ints(l.sorted),
               ints(l.seg_first), a.loss};
   auto rank = [&] {
-    return launch_kernel(ce_rank_kernel, dim3(static_cast<unsigned>((a.T + 255) / 256), 8), dim3(256), 0, s, 0, head,
+    const unsigned blocks = static_cast<unsigned>((a.T + 255) / 256);
+    return launch_kernel(ce_rank_kernel, dim3(blocks, std::min(blocks, 32u)), dim3(256), 0, s, 0, head,
                          target, pos);
   };
   auto by_targets = [&] {  // the factors, then the targets' part of dw

@@ -21,7 +21,7 @@ constexpr int kEpiWarps = 8;
 constexpr int kStoreBytes = 4096;  // of an epilogue warp's stores of c
 constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
 constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
-constexpr int kRun = 32;       // sorted tokens whose target gradients one CTA sums
+constexpr int kRun = 16;       // sorted tokens whose target gradients one CTA sums
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
