@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -444,11 +445,13 @@ def _matrix(t: torch.Tensor, name: str, cols: int | None = None, like=None) -> i
         raise MpcError(1, "%s must be 2-d%s" % (name, "" if cols is None else " with %d columns" % cols))
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         raise MpcError(1, "%s must be %s on %s" % (name, like.dtype, like.device))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, width = t.shape
+    apart, step = t.stride()
+    if width > 1 and step != 1:
         raise MpcError(1, "the rows of %s must be contiguous" % name)
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if rows > 1 and apart < width:
         raise MpcError(1, "the rows of %s overlap" % name)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return apart if rows > 1 else width
 
 
 def _address(t) -> int | None:
@@ -467,6 +470,15 @@ def _vector(t, n: int, dtype: torch.dtype, name: str, device):
     _cuda(t, dtype, name)
     if t.numel() != n or t.device != device:
         raise MpcError(1, "%s must hold %d entries on %s" % (name, n, device))
+    return t
+
+
+def _vector_or_new(t, n: int, name: str, device, stream):
+    """An fp32 output of n entries: the caller's, checked, or a new one."""
+    if t is not None:
+        return _vector(t, n, torch.float32, name, device)
+    t = torch.empty(n, dtype=torch.float32, device=device)
+    _on(stream, t)
     return t
 
 
@@ -500,16 +512,8 @@ def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, ls
     """Softmax cross entropy of the logits h [T, D] @ w [V, D].T against targets [T] (int64).
     Returns (loss [T], lse [T]) in fp32; both are 0 for tokens whose target is ignore_index."""
     T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 0, 0, ws, stream)
-    new = []
-    if loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=h.device)
-        new.append(loss)
-    if lse is None:
-        lse = torch.empty(T, dtype=torch.float32, device=h.device)
-        new.append(lse)
-    _on(stream, *new)
-    _vector(loss, T, torch.float32, "loss", h.device)
-    _vector(lse, T, torch.float32, "lse", h.device)
+    loss = _vector_or_new(loss, T, "loss", h.device, stream)
+    lse = _vector_or_new(lse, T, "lse", h.device, stream)
     _check(lib().mpc_linear_ce_forward(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), T, D, V,
                                        _DTYPES[h.dtype], ignore_index, loss.data_ptr(), lse.data_ptr(),
                                        _address(ws), wsb, _raw_stream(stream)))
@@ -517,17 +521,17 @@ def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, ls
 
 
 def _linear_ce_grads(h, w, dh, dw, stream):
-    new = []
-    if dh is None:
-        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        new.append(dh)
-    if dw is None:
-        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
-        new.append(dw)
-    _on(stream, *new)
-    if dh.shape != h.shape or dw.shape != w.shape:
-        raise MpcError(1, "dh and dw must have the shapes of h and w")
-    return dh, _matrix(dh, "dh", h.shape[1], h), dw, _matrix(dw, "dw", h.shape[1], h)
+    out = []
+    for name, t, of in (("dh", dh, h), ("dw", dw, w)):
+        if t is None:
+            t = torch.empty(of.shape, dtype=of.dtype, device=of.device)
+            _on(stream, t)
+            out += [t, of.shape[1]]
+        else:
+            if t.shape != of.shape:
+                raise MpcError(1, "%s must have the shape of %s" % (name, name[1:]))
+            out += [t, _matrix(t, name, of.shape[1], of)]
+    return out
 
 
 def mpc_linear_ce_backward(h, w, targets, lse, gloss=None, ignore_index: int = -100, piece: int = 0,
@@ -552,10 +556,7 @@ def mpc_linear_ce_train(h, w, targets, gloss=None, ignore_index: int = -100, pie
     """Loss and gradient in one call: (loss [T], dh [T, D], dw [V, D]); arguments as for
     mpc_linear_ce_forward and mpc_linear_ce_backward."""
     T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 2, piece, ws, stream)
-    if loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=h.device)
-        _on(stream, loss)
-    _vector(loss, T, torch.float32, "loss", h.device)
+    loss = _vector_or_new(loss, T, "loss", h.device, stream)
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
     dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
@@ -582,6 +583,11 @@ def mpc_adamw_step(plan, lr: float, beta1: float, beta2: float, eps: float, step
                                 max_norm, _raw_stream(stream)))
 
 
+_numel, _data_ptr, _is_contiguous, _index_of = (
+    torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device)
+_dtype_of = operator.attrgetter("dtype")
+
+
 def mpc_adamw_decode(plan, m_out, v_out, stream=None):
     """The fp32 values that the 8-bit states of an ``AdamWPlan`` stand for, into the tensors of
     m_out and v_out (one for each tensor of the plan)."""
@@ -591,11 +597,15 @@ def mpc_adamw_decode(plan, m_out, v_out, stream=None):
     for name, outs in (("m_out", m_out), ("v_out", v_out)):
         if len(outs) != plan.count:
             raise MpcError(1, "%s must hold one tensor for each of the plan's %d" % (name, plan.count))
-        for t, n in zip(outs, plan.sizes):
-            if (t.dtype is not torch.float32 or t.get_device() != plan.index or t.numel() != n
-                    or not t.is_contiguous()):
+        try:  # one pass a property, each without a Python frame a tensor
+            fine = (list(map(_numel, outs)) == plan.sizes and set(map(_dtype_of, outs)) == {torch.float32}
+                    and set(map(_index_of, outs)) == {plan.index} and all(map(_is_contiguous, outs)))
+        except TypeError:
+            fine = False
+        if not fine:
+            for t, n in zip(outs, plan.sizes):
                 _vector(t, n, torch.float32, name, plan.device)
-        lists.append(array.array("Q", [t.data_ptr() for t in outs]))
+        lists.append(array.array("Q", map(_data_ptr, outs)))
     _check(lib().mpc_adamw_decode(plan.table, plan.count, lists[0].buffer_info()[0],
                                   lists[1].buffer_info()[0], _raw_stream(stream)))
     return m_out, v_out
@@ -608,10 +618,7 @@ def mpc_grad_norm_workspace_bytes(count: int) -> int:
 def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
     """The 2-norm of all gradients of an ``AdamWPlan`` together, as a device fp32 of one entry.
     Without ``ws`` the plan's own workspace is used: calls on one plan are to be ordered."""
-    if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=plan.device)
-        _on(stream, norm)
-    _vector(norm, 1, torch.float32, "norm", plan.device)
+    norm = _vector_or_new(norm, 1, "norm", plan.device, stream)
     if ws is None:
         if plan.norm_ws is None:
             plan.norm_ws = torch.empty(mpc_grad_norm_workspace_bytes(plan.count), dtype=torch.uint8,

@@ -437,6 +437,30 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// A target whose tokens go past the end of a block of kRun: the CTA of the block in
+// which it starts adds up its blocks' sums, at the first one's place.  (Left to
+// the rows of dw, a frequent target's blocks made one thread's tail: 40 us of 390
+// at 8192 x 768 x 50257.)
+__global__ void __launch_bounds__(256)
+    ce_join_kernel(const Header* head, const int* __restrict__ sorted, const int* __restrict__ seg_first,
+                   const int* __restrict__ seg_end, float* seg_sum, int64_t lds) {
+  pdl_begin();
+  const int n = head->valid;
+  const int next = (blockIdx.x + 1) * kRun;
+  if (next >= n) return;
+  const int y = sorted[next];
+  if (sorted[next - 1] != y) return;
+  const int first = seg_first[y] - 1;
+  if (first < next - kRun) return;  // starts in an earlier block
+  const int end = seg_end[y];
+  for (int64_t d = threadIdx.x; d < lds; d += 256) {
+    float s = seg_sum[first * lds + d];
+#pragma unroll 8
+    for (int p = next; p < end; p += kRun) s = fadd(s, seg_sum[p * lds + d]);
+    seg_sum[first * lds + d] = s;
+  }
+}
+
 // dh in the caller's type and order from the splits' sums; zero for tokens that
 // do not count.  Times `scale` and plus `coef` times the target's row of w where given.
 template <typename E>
@@ -746,10 +770,12 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   auto by_targets = [&] {  // the factors, then the targets' part of dw
     CE_TRY(launch_kernel(ce_scale_kernel<P>, dim3(rows8), dim3(256), 0, s, 0, f));
     g.seg_first = f.seg_first;
-    g.seg_end = ints(l.seg_end);
     g.seg_sum = floats(l.seg_sum);
-    return launch_kernel(ce_target_kernel<P>, dim3(static_cast<unsigned>((a.T + kRun - 1) / kRun)), dim3(256), 0, s, 0, head,
-                         f.order, f.sorted, factor, hp, hplane, Dp, f.seg_first, ints(l.seg_end), floats(l.seg_sum), l.Dp);
+    const unsigned runs = static_cast<unsigned>((a.T + kRun - 1) / kRun);
+    CE_TRY(launch_kernel(ce_target_kernel<P>, dim3(runs), dim3(256), 0, s, 0, head, f.order, f.sorted, factor, hp, hplane,
+                         Dp, f.seg_first, ints(l.seg_end), floats(l.seg_sum), l.Dp));
+    return launch_kernel(ce_join_kernel, dim3(runs), dim3(256), 0, s, 0, head, f.sorted, f.seg_first, ints(l.seg_end),
+                         floats(l.seg_sum), l.Dp);
   };
 
   if (l.kept) {

@@ -107,8 +107,7 @@ struct Gemm {
   const float* ref;     // kExp: [T]
   const int* redo;      // kExp: nullptr, or the row tiles to form again
   const int* seg_first; // kDw: nullptr, or per entry 1 + the first sorted token with that target (0: none)
-  const int* seg_end;   // kDw: the position after its last one
-  const float* seg_sum; // kDw: [T][lds], the tokens' sums at the first position of each run of kRun
+  const float* seg_sum; // kDw: [T][lds], the sum of its tokens' gradients at that position
   const float* lse;     // kCoef: [T] by token
   const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
   const float* loss;    // kCoef: [T] by token where the forward pass gave it, or nullptr
@@ -137,6 +136,7 @@ __device__ __forceinline__ void term_planes(int t, int* a, int* b) {
 struct Row {
   int target;
   float ref;  // kExp
+  int first;  // kDw: seg_first
 };
 
 struct Tile {
@@ -325,22 +325,16 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
       }
     }
   } else {
-    if (g.seg_first != nullptr && m < g.width) {  // the tokens whose target this entry is
-      const int first = g.seg_first[g.v0 + m];
-      if (first > 0) {
-        const int end = g.seg_end[g.v0 + m];
-        for (int p = first - 1; p < end; p = (p / kRun + 1) * kRun) {
-          const float* add = g.seg_sum + p * g.lds + n0;
+    if (row.first > 0) {  // the tokens whose target this entry is
+      const float* add = g.seg_sum + (row.first - 1) * g.lds + n0;
 #pragma unroll
-          for (int j = 0; j < kHalf; j += 4) {
-            if (n0 + j < g.D) {
-              const float4 v = *reinterpret_cast<const float4*>(add + j);
-              x[j] = fadd(x[j], v.x);
-              x[j + 1] = fadd(x[j + 1], v.y);
-              x[j + 2] = fadd(x[j + 2], v.z);
-              x[j + 3] = fadd(x[j + 3], v.w);
-            }
-          }
+      for (int j = 0; j < kHalf; j += 4) {
+        if (n0 + j < g.D) {
+          const float4 v = *reinterpret_cast<const float4*>(add + j);
+          x[j] = fadd(x[j], v.x);
+          x[j + 1] = fadd(x[j + 1], v.y);
+          x[j + 2] = fadd(x[j + 2], v.z);
+          x[j + 3] = fadd(x[j + 3], v.w);
         }
       }
     }
@@ -563,7 +557,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const Tile t = tile_of<MODE>(g, s, i);
       if (skipped<MODE>(g, t)) continue;
       const int m = t.m0 + rank * kM + quad * 32 + lane;
-      Row row = {-1, 0.0f};
+      Row row = {-1, 0.0f, 0};
+      if (MODE == kDw && g.seg_first != nullptr && m < g.width) row.first = g.seg_first[g.v0 + m];
       if ((MODE == kLoss || MODE == kExp) && m < valid) {
         row.target = g.target[m];
         if (MODE == kExp) row.ref = g.ref[m];
