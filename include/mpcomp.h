@@ -316,8 +316,8 @@ typedef enum { MPC_CE_FORWARD = 0, MPC_CE_BACKWARD = 1, MPC_CE_TRAIN = 2 } mpc_c
  *           ldw = 0 when w itself is not 16-byte aligned), as an fp32 w always
  *           is, split into three bf16 terms.
  * Products are summed in fp32 and fp32 inputs are not rounded to a narrower
- * type.  tokens = 0 is a no-op.  Requires hidden >= 1, 1 <= vocab <= 2^31-1,
- * tokens <= 2^31-1. */
+ * type.  tokens = 0 is a no-op.  Requires 1 <= hidden <= 2^24, 1 <= vocab <=
+ * 2^30, tokens <= 2^30. */
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
                                      mpc_ce_pass pass, int64_t piece, int64_t ldw);
 mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int64_t ldw,

@@ -603,8 +603,9 @@ mpc_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, i
 }
 
 bool linear_ce_sizes_ok(int64_t tokens, int64_t hidden, int64_t vocab, int64_t piece) {
-  return tokens >= 0 && tokens <= 0x7fffffffLL && hidden >= 1 && hidden <= (1 << 24) && vocab >= 1 &&
-         vocab <= 0x7fffffffLL && piece >= 0;
+  constexpr int64_t most = int64_t{1} << 30;
+  return tokens >= 0 && tokens <= most && hidden >= 1 && hidden <= (1 << 24) && vocab >= 1 && vocab <= most &&
+         piece >= 0;
 }
 
 // Shared body of the three linear cross-entropy calls.

@@ -739,8 +739,9 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   // 1.4e-8 of a result a step).  fp32: two, 48 steps (four measured 3 to 8 % faster
   // and 1.3e-6 off, more than an fp32 sum).  bf16 logits, whose loss is fp32: equal
   // chunks of up to 12, and 2 for few tokens, where the products wait for memory
-  // anyway.  bf16 gradients: any number.
-  const int any = 1 << 30, exact = 2;
+  // anyway.  bf16 gradients: any number (8192 keep an accumulator's wait far below
+  // the default limit of a wait).
+  const int any = 8192, exact = 2;
   const int64_t parts = (d_blocks + 11) / 12;
   const int logits = !bf16 || a.T <= kPair ? exact : static_cast<int>((d_blocks + parts - 1) / parts);
   const int gradients = bf16 ? any : exact;

@@ -61,13 +61,20 @@ class _LinearCeMeanFn(torch.autograd.Function):
         return dh * g.to(dh.dtype), dw * g.to(dw.dtype), None, None
 
 
+def _rows_apart(t):
+    """t itself, or a copy where its rows are not contiguous or share memory (broadcast)."""
+    fine = (t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] == 1)
+    return t if fine else t.contiguous()
+
+
 def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean"):
     """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
     ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
     where the target is ``ignore_index``)."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none")
-    rows, y = h.reshape(-1, h.shape[-1]), targets.reshape(-1)
+    rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()
+    w = _rows_apart(w)
     grad = torch.is_grad_enabled() and (h.requires_grad or w.requires_grad)
     if reduction == "mean":
         if grad:
@@ -200,7 +207,7 @@ class AdamWPlan:
 class AdamW(torch.optim.Optimizer):
     """AdamW in one launch for all tensors of a type (and one more pass over the gradients when
     ``max_norm`` is set, which clips by the norm of all of them and leaves out a step whose norm is
-    not finite).
+    not finite; it still counts as a step for the bias corrections).
 
     ``state_bits``: 32, or 8 for states in blocks of 256 codes.  ``copies``: {param: bfloat16 tensor}
     that receives the param's new values, for a forward pass in bf16 from fp32 weights.
@@ -254,6 +261,8 @@ class AdamW(torch.optim.Optimizer):
             for p in group["params"]:
                 if p.grad is None:
                     continue
+                if p.grad.is_sparse:
+                    raise MpcError(1, "sparse gradients are not supported")
                 s = self._state(p)
                 s["step"] += 1
                 key = (p.dtype, p.grad.dtype, p.device, s["step"], tuple(group["betas"]), group["eps"])
@@ -262,7 +271,7 @@ class AdamW(torch.optim.Optimizer):
         for key, entries in lists.items():
             ident = (key[0], key[1], key[2], tuple(id(p) for p, _, _ in entries))
             plan = self._plans.get(ident)
-            grads = [p.grad for p, _, _ in entries]
+            grads = [p.grad.contiguous() for p, _, _ in entries]
             if plan is None or any(a.data_ptr() != p.data_ptr() for a, (p, _, _) in zip(plan.params, entries)):
                 low = self.state_bits == 8
                 plan = AdamWPlan([p.detach() for p, _, _ in entries], grads,
@@ -279,9 +288,17 @@ class AdamW(torch.optim.Optimizer):
             plans.append((key, plan))
         norm = None
         if self.max_norm > 0.0 and plans:
-            norms = [mpc_grad_norm(plan) for _, plan in plans]
-            norm = norms[0] if len(norms) == 1 else torch.linalg.vector_norm(torch.cat(norms)).view(1)
+            norms = []
+            for key, plan in plans:
+                with torch.cuda.device(key[2]):
+                    norms.append(mpc_grad_norm(plan))
+            if len(norms) > 1:  # lists of several types or steps: the norm of their norms
+                norm = torch.linalg.vector_norm(torch.cat([x.to(norms[0].device) for x in norms])).view(1)
+            else:
+                norm = norms[0]
             self.last_norm = norm
-        for (_, _, _, step, betas, eps), plan in plans:
-            mpc_adamw_step(plan, 1.0, betas[0], betas[1], eps, step, grad_norm=norm, max_norm=self.max_norm)
+        for (_, _, device, step, betas, eps), plan in plans:
+            with torch.cuda.device(device):
+                mpc_adamw_step(plan, 1.0, betas[0], betas[1], eps, step,
+                               grad_norm=None if norm is None else norm.to(device), max_norm=self.max_norm)
         return loss

@@ -374,3 +374,57 @@ def test_few_tokens(mpc, dtype, T, D, V):
     near(dw, want["dw"], "dw (train)")
     assert bool((dbig[:, D:] == 7.0).all())
     assert mpc.mpc_get_status() == 0
+
+
+def test_autograd_of_layouts(mpc):
+    """Hidden states that are broadcast, transposed or cut out of something wider; a transposed weight."""
+    D, V = 40, 90
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    y = torch.randint(0, V, (60,), device="cuda", generator=gen)
+    one = torch.randn(1, D, device="cuda", generator=gen)
+    flat = torch.randn(D, 60, device="cuda", generator=gen)
+    wide = torch.randn(60, D + 9, device="cuda", generator=gen)
+    wt = torch.randn(D, V, device="cuda", generator=gen)
+    for base, view in ((one, lambda t: t.expand(60, D)), (flat, lambda t: t.t()), (wide, lambda t: t[:, 5:5 + D])):
+        a, b = base.clone().requires_grad_(True), base.double().requires_grad_(True)
+        u, v = wt.clone().requires_grad_(True), wt.double().requires_grad_(True)
+        loss = mpc.linear_cross_entropy(view(a), u.t(), y)
+        ref = torch.nn.functional.cross_entropy(view(b) @ v, y)
+        loss.backward()
+        ref.backward()
+        assert abs(float(loss.detach()) - float(ref.detach())) < 2e-5 * abs(float(ref.detach()))
+        for got, want in ((a.grad, b.grad), (u.grad, v.grad)):
+            assert got.shape == want.shape
+            assert float((got.double() - want).norm()) < 2e-5 * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [100, 600])
+def test_a_wait_that_gives_up_is_reported(mpc, dtype, T):
+    """With the limit of device-side waits at 0 every first wait gives up: the products' kernels return,
+    the status says so, and the next call is as before."""
+    h, w, y = inputs(T, 96, 1000, dtype, seed=40)
+    before = mpc.mpc_linear_ce_train(h, w, y)
+    assert mpc.mpc_get_status() == 0
+    mpc.mpc_set_knob(mpc.MPC_KNOB_SPIN_LIMIT, 0)
+    try:
+        mpc.mpc_linear_ce_train(h, w, y)
+        assert mpc.mpc_get_status() == 5
+    finally:
+        mpc.mpc_set_knob(mpc.MPC_KNOB_SPIN_LIMIT, 1 << 20)
+    assert mpc.mpc_get_status() == 0
+    for a, b in zip(before, mpc.mpc_linear_ce_train(h, w, y)):
+        assert torch.equal(a, b)
+
+
+def test_plain_stream_order_gives_the_same(mpc):
+    """Launches with and without programmatic dependent launch."""
+    h, w, y = inputs(700, 136, 1300, torch.bfloat16, seed=41)
+    with_pdl = [x.clone() for x in mpc.mpc_linear_ce_train(h, w, y)]
+    mpc.mpc_set_knob(mpc.MPC_KNOB_PDL, 0)
+    try:
+        without = mpc.mpc_linear_ce_train(h, w, y)
+    finally:
+        mpc.mpc_set_knob(mpc.MPC_KNOB_PDL, 1)
+    for a, b in zip(with_pdl, without):
+        assert torch.equal(a, b)
