@@ -509,6 +509,45 @@ __global__ void __launch_bounds__(256)
   }
 }
 
+// dw of a piece from the sums of parts of the tokens.
+template <typename E>
+__global__ void __launch_bounds__(256)
+    ce_dw_out_kernel(int width, int D, int groups, const float* __restrict__ sum, int64_t lds, int splits,
+                     int64_t sum_split, const int* __restrict__ seg_first, const float* __restrict__ seg_sum, E* dw,
+                     int64_t lddw, int wide) {
+  pdl_begin();
+  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(width) * groups;
+       q += gridDim.x * int64_t{256}) {
+    const int64_t v = q / groups;
+    const int d = static_cast<int>(q - v * groups) * 8;
+    float x[8] = {};
+    auto add = [&](const float* from) {
+      const float4 a = reinterpret_cast<const float4*>(from)[0], b = reinterpret_cast<const float4*>(from)[1];
+      const float y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = fadd(x[j], y[j]);
+    };
+#pragma unroll 4
+    for (int i = 0; i < splits; ++i) add(sum + i * sum_split + v * lds + d);
+    const int first = seg_first != nullptr ? seg_first[v] : 0;
+    if (first > 0) add(seg_sum + (first - 1) * lds + d);
+    E out[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) from_float(x[j], &out[j]);
+    E* to = dw + v * lddw + d;
+    if (wide && d + 8 <= D) {
+      uint4 u[sizeof(E) / 2];
+      memcpy(u, out, sizeof(out));
+#pragma unroll
+      for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) reinterpret_cast<uint4*>(to)[k] = u[k];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (d + j < D) to[j] = out[j];
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Workspace and launches
 // ---------------------------------------------------------------------------
@@ -530,7 +569,7 @@ constexpr int64_t kKeptTokens = 16384;
 enum Pass { kForward = 0, kBackward = 1, kTrain = 2 };
 
 struct Layout {
-  size_t head, row, target, place, at_target, part, lse, h, w, coef, sum, total;
+  size_t head, row, target, place, at_target, part, lse, h, w, coef, sum, dw_sum, total;
   size_t flags, pos, order, sorted, ref, sums, scale, factor, hs, seg_first, seg_end, seg_sum;  // kept
   int parts, planes, tiles;
   bool pack_w, kept, apart;
@@ -571,6 +610,12 @@ Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int planes, int narrowest,
   return best;
 }
 
+// dw in parts needs its sums and one more pass, for a vocabulary of few tiles.
+constexpr int kMostDwSplits = 16;
+Plan plan_dw(int64_t T, int64_t D, int64_t piece, int planes) {
+  return plan_tiles(piece, D, (T + kK - 1) / kK, planes, 64, kMostDwSplits);
+}
+
 Plan plan_dh(int64_t T, int64_t D, int64_t piece, int planes) {
   return plan_tiles(T, D, (piece + kK - 1) / kK, planes, 64, kMaxSplits);
 }
@@ -608,6 +653,8 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piec
   l.piece = l.kept ? V : std::min(V, piece > 0 ? piece : most);
   l.ldc = round_up(l.piece, kN);
   l.coef = take(static_cast<size_t>(l.planes) * l.padded * l.ldc * 2);
+  const Plan dw = plan_dw(T, D, l.piece, l.planes);
+  l.dw_sum = take(dw.splits > 1 ? static_cast<size_t>(dw.splits) * l.piece * l.Dp * 4 : 0);
   l.sum = take(static_cast<size_t>(plan_dh(T, D, l.piece, l.planes).splits) * l.padded * l.Dp * 4);
   l.apart = !l.kept && bf16 && T <= kPair;
   if (l.kept || l.apart) {
@@ -658,7 +705,8 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t r
 template <int MODE, int PLANES>
 cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const Gemm& g, int64_t m, int64_t n, int num_sms,
                         cudaStream_t s) {
-  const int64_t tiles = (m + kPair - 1) / kPair * ((n + g.tile_n - 1) / g.tile_n) * (MODE == kDh ? g.splits : 1);
+  const int64_t tiles = (m + kPair - 1) / kPair * ((n + g.tile_n - 1) / g.tile_n) *
+                        (MODE == kDh || MODE == kDw ? g.splits : 1);
   if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
   constexpr bool stores = MODE == kExp || MODE == kCoef;
   constexpr int smem = kStages * kStageBytes + 1024 + (stores ? kEpiWarps * kStoreBytes : 0);
@@ -746,13 +794,28 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   const int logits = !bf16 || a.T <= kPair ? exact : static_cast<int>((d_blocks + parts - 1) / parts);
   const int gradients = bf16 ? any : exact;
   const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
-  const int dw_n = pass == kForward ? kN : plan_tiles(l.piece, a.D, (a.T + kK - 1) / kK, P, 64, 1).tile_n;
+  const Plan dw_plan = pass == kForward ? Plan{kN, 1} : plan_dw(a.T, a.D, l.piece, P);
+  const int wide_dw = on16(a.dw) && a.lddw * sizeof(E) % 16 == 0;
   const unsigned out_blocks =
       static_cast<unsigned>(std::min<int64_t>((a.T * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
   auto dh_out = [&](const float* scale, const float* coef) {
     return launch_kernel(ce_dh_out_kernel<E>, dim3(out_blocks), dim3(256), 0, s, 0, T, D, Dp / 8, place, g.sum, g.lds,
                          g.splits, g.sum_split, scale, coef, w, a.ldw, target, wide_w, static_cast<E*>(a.dh), a.lddh,
                          wide_dh);
+  };
+  // dw of the piece in g, from the maps of c^T and of h^T
+  auto dw_of_piece = [&](const CUtensorMap& c, const CUtensorMap& hm) {
+    Gemm d = g;
+    d.tile_n = dw_plan.tile_n;
+    d.splits = dw_plan.splits;
+    d.sum = dw_plan.splits > 1 ? floats(l.dw_sum) : nullptr;
+    d.sum_split = l.piece * l.Dp;
+    CE_TRY(launch_gemm<kDw, P>(c, hm, hm, d, d.width, a.D, num_sms, s));
+    if (d.sum == nullptr) return cudaSuccess;
+    const int64_t blocks = std::min<int64_t>((static_cast<int64_t>(d.width) * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16);
+    return launch_kernel(ce_dw_out_kernel<E>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0, d.width, D, Dp / 8,
+                         d.sum, d.lds, d.splits, d.sum_split, d.seg_first == nullptr ? nullptr : d.seg_first + d.v0,
+                         d.seg_sum, static_cast<E*>(a.dw) + d.v0 * a.lddw, a.lddw, wide_dw);
   };
   CUtensorMap w_cols, h_cols, c_rows, c_cols;  // K = vocabulary, tokens: boxes of 64 columns x 64 k
   CUtensorMap c_out;                           // boxes of 64 columns x 32 rows
@@ -803,8 +866,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.chunk = gradients;
     CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, w_cols, g, a.T, a.D, num_sms, s));
     CE_TRY(dh_out(scale, factor));
-    g.tile_n = dw_n;
-    return launch_gemm<kDw, P>(c_cols, h_cols, h_cols, g, a.V, a.D, num_sms, s);
+    return dw_of_piece(c_cols, h_cols);
   }
 
   const float* lse = a.lse_in;
@@ -845,8 +907,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.chunk = gradients;
     g.tile_n = dh_plan.tile_n;
     CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, w_cols, g, a.T, a.D, num_sms, s));
-    g.tile_n = dw_n;
-    CE_TRY(launch_gemm<kDw, P>(c_cols, h_cols, h_cols, g, width, a.D, num_sms, s));
+    CE_TRY(dw_of_piece(c_cols, h_cols));
   }
   return dh_out(nullptr, l.apart ? factor : nullptr);
 }

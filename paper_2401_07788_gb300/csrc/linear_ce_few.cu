@@ -19,6 +19,7 @@
 // Tokens keep their places here; one that does not count has a zero row of h, and
 // zero results.
 #include <algorithm>
+#include <type_traits>
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -71,6 +72,10 @@ __device__ __forceinline__ int few_target(const Few& f, int t) {
 // V elements from p on as floats.
 template <int N>
 __device__ __forceinline__ void few_load(const float* p, float (&x)[N]) {
+  if (N == 1) {
+    x[0] = p[0];
+    return;
+  }
   if (N == 2) {
     const float2 v = *reinterpret_cast<const float2*>(p);
     x[0] = v.x; x[1] = v.y;
@@ -84,6 +89,9 @@ __device__ __forceinline__ void few_load(const float* p, float (&x)[N]) {
 }
 template <int N>
 __device__ __forceinline__ void few_load(const __nv_bfloat16* p, float (&x)[N]) {
+  if constexpr (N == 1) {
+    x[0] = __bfloat162float(p[0]);
+  } else {
   uint32_t u[N / 2];
   if (N == 8) *reinterpret_cast<uint4*>(u) = *reinterpret_cast<const uint4*>(p);
   else if (N == 4) *reinterpret_cast<uint2*>(u) = *reinterpret_cast<const uint2*>(p);
@@ -93,22 +101,25 @@ __device__ __forceinline__ void few_load(const __nv_bfloat16* p, float (&x)[N]) 
     x[2 * j] = __uint_as_float(u[j] << 16);
     x[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
   }
+  }
 }
 
 // The rows of h of TT tokens in shared memory, fp32.  Columns of a 16-byte group
 // of 8 bf16 are kept in two halves of 4, so that 128-bit reads of neighbouring
 // lanes do not meet in a bank.
-template <typename E, int TT, bool WIDE>
+template <typename E, int W>
 __device__ __forceinline__ int few_place(int d, int Dp) {
-  if (!WIDE || sizeof(E) == 4) return d;
+  if (W * sizeof(E) < 16 || sizeof(E) == 4) return d;
   return (d >> 2 & 1) * (Dp / 2) + (d >> 3) * 4 + (d & 3);
 }
 
-// WIDE: rows of w start on 16 bytes and are read in 16-byte groups; otherwise
-// element by element, neighbouring lanes neighbouring elements.
-template <typename E, int TT, bool WIDE>
-__global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few f) {
-  constexpr int VEC = WIDE ? 16 / sizeof(E) : 1;
+// W elements of w an access: 16 bytes where its rows start on 16, else pairs of
+// bf16 where they start on 4, else one element; neighbouring lanes neighbouring
+// accesses.  Tokens t0 .. t0 + TT - 1.
+template <typename E, int TT, int W>
+__global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few f, int t0) {
+  constexpr int VEC = W;
+  constexpr bool WIDE = W * sizeof(E) == 16;
   constexpr int R = TT >= 8 ? 4 : 8;  // rows a warp takes at a time
   constexpr int N = R * TT;
   pdl_begin();
@@ -119,11 +130,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
   const E* w = static_cast<const E*>(f.w);
 #pragma unroll
   for (int t = 0; t < TT; ++t) {
-    const bool live = few_target(f, t) >= 0;
+    const bool live = few_target(f, t0 + t) >= 0;
     for (int d = threadIdx.x; d < Dp; d += kFewThreads)
-      sh[t * Dp + few_place<E, TT, WIDE>(d, Dp)] = live && d < f.D ? few_float(h[t * f.ldh + d]) : 0.0f;
+      sh[t * Dp + few_place<E, W>(d, Dp)] = live && d < f.D ? few_float(h[(t0 + t) * f.ldh + d]) : 0.0f;
   }
-  if (blockIdx.x == 0 && threadIdx.x < f.T) {
+  if (blockIdx.x == 0 && t0 == 0 && threadIdx.x < f.T) {
     const int64_t y = f.targets[threadIdx.x];
     if (y != f.ignore && (y < 0 || y >= f.V)) set_status(f.status, STATUS_BAD_INDEX);
   }
@@ -151,7 +162,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
   for (int i = 0; i < C; ++i) {
     top[i] = -INFINITY;
     sum[i] = 0.0f;
-    target[i] = few_target(f, (idx + i) % TT);
+    target[i] = few_target(f, t0 + (idx + i) % TT);
   }
   const int64_t groups = (f.V + R - 1) / R;
   for (int64_t g = blockIdx.x * kFewWarps + warp; g < groups; g += gridDim.x * kFewWarps) {
@@ -162,7 +173,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
     const E* rows[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) rows[r] = w + min64(v0 + r, f.V - 1) * f.ldw;
-    const int whole = WIDE ? f.D / VEC * VEC : f.D;
+    const int whole = f.D / VEC * VEC;
     if constexpr (WIDE) {
       for (int d = lane * VEC; d < whole; d += 32 * VEC) {
         uint4 u[R];
@@ -184,7 +195,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
           }
 #pragma unroll
           for (int t = 0; t < TT; ++t) {
-            const float4 y = *reinterpret_cast<const float4*>(&sh[t * Dp + few_place<E, TT, WIDE>(d + q, Dp)]);
+            const float4 y = *reinterpret_cast<const float4*>(&sh[t * Dp + few_place<E, W>(d + q, Dp)]);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
               float& to = acc[r * TT + t];
@@ -197,27 +208,30 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
         }
       }
     } else {
-#pragma unroll 4
-      for (int d = lane; d < whole; d += 32) {
-        float x[R];
+#pragma unroll (W == 1 ? 4 : 2)
+      for (int d = lane * W; d < whole; d += 32 * W) {
+        float x[R][W];
 #pragma unroll
-        for (int r = 0; r < R; ++r) x[r] = few_float(rows[r][d]);
+        for (int r = 0; r < R; ++r) few_load<W>(rows[r] + d, x[r]);
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-          const float y = sh[t * Dp + d];
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r * TT + t] = __fmaf_rn(x[r], y, acc[r * TT + t]);
+          for (int j = 0; j < W; ++j) {
+            const float y = sh[t * Dp + d + j];
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r * TT + t] = __fmaf_rn(x[r][j], y, acc[r * TT + t]);
+          }
         }
       }
     }
-    if (WIDE && whole + lane < f.D) {  // the columns after the last whole group
+    if (W > 1 && whole + lane < f.D) {  // the columns after the last whole group
       const int d = whole + lane;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float x = few_float(rows[r][d]);
 #pragma unroll
         for (int t = 0; t < TT; ++t)
-          acc[r * TT + t] = __fmaf_rn(x, sh[t * Dp + few_place<E, TT, WIDE>(d, Dp)], acc[r * TT + t]);
+          acc[r * TT + t] = __fmaf_rn(x, sh[t * Dp + few_place<E, W>(d, Dp)], acc[r * TT + t]);
       }
     }
     // sums over the lanes: halve the list and the lanes' share of it at each step
@@ -243,7 +257,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
     }
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int t = (idx + i) % TT;
+      const int t = t0 + (idx + i) % TT;
       const int64_t v = v0 + (idx + i) / TT;
       if (v < f.V && counts) {
         if (f.logits != nullptr && t < f.T) f.logits[t * f.V + v] = acc[i];
@@ -281,7 +295,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
         if (p.x != -INFINITY) s = fadd(s, fmul(p.y, exp2f(fsub(p.x, m))));
         else if (p.y != p.y) s = p.y;
       }
-    f.part[blockIdx.x * kFewTokens + t] = make_float2(m, s);
+    f.part[blockIdx.x * kFewTokens + t0 + t] = make_float2(m, s);
   }
 }
 
@@ -319,19 +333,24 @@ __global__ void __launch_bounds__(kFewTokens * 32) ce_few_finish_kernel(const Fe
 // Columns that a thread of the gradient kernel owns: h and dh's sums of TT tokens
 // for each are 2 TT registers.
 __host__ __device__ constexpr int few_cols(int tt) { return tt >= 16 ? 2 : 4; }
+// CTAs of the gradient kernel on an SM, as its registers allow.
+__host__ __device__ constexpr int few_resident(int tt) { return tt <= 2 ? 4 : tt == 4 ? 3 : 2; }
+constexpr int kGradThreads = 256;
 template <int BYTES> struct FewWord;
+template <> struct FewWord<2> { using type = uint16_t; };
 template <> struct FewWord<4> { using type = uint32_t; };
 template <> struct FewWord<8> { using type = uint2; };
 template <> struct FewWord<16> { using type = uint4; };
 
 // dw rows of this CTA's range and its sums of dh.  Threads: G column groups of
-// few_cols(TT) (neighbouring columns when WIDE, G apart otherwise) by RL rows at a time; a CTA
-// takes the columns of blockIdx.y.
-template <typename E, int TT, bool WIDE>
-__global__ void __launch_bounds__(kFewThreads, 1) ce_few_grad_kernel(const Few f, int G, int RL, int with_loss) {
-  constexpr int kRows = 64, CP = few_cols(TT);
+// few_cols(TT), in accesses of A neighbouring columns that lie G accesses apart, by
+// RL rows at a time; a CTA takes the columns of blockIdx.y.  D is a multiple of A;
+// dw_words: dw's rows suit accesses of A.
+template <typename E, int TT, int W>
+__global__ void __launch_bounds__(kGradThreads, few_resident(TT)) ce_few_grad_kernel(const Few f, int G, int RL, int with_loss, int dw_words) {
+  constexpr int kRows = 64, CP = few_cols(TT), A = W < CP ? W : CP, U = 4;
   pdl_begin();
-  __shared__ float c[kRows][TT];
+  __shared__ __align__(16) float c[kRows][TT];
   __shared__ float lse_of[TT], weight_of[TT], minus_loss[TT];
   __shared__ int target_of[TT];
   extern __shared__ float red[];
@@ -339,8 +358,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_grad_kernel(const Few f
   const E* w = static_cast<const E*>(f.w);
   E* dw = static_cast<E*>(f.dw);
   const int group = threadIdx.x % G, rl = threadIdx.x / G;
-  const int d0 = blockIdx.y * G * CP + (WIDE ? group * CP : group);
-  auto col = [&](int j) { return WIDE ? d0 + j : d0 + j * G; };
+  const int d0 = blockIdx.y * G * CP + group * A;
+  auto col = [&](int j) { return d0 + j / A * G * A + j % A; };
+  int at[CP / A];  // where each access reads, within the row
+#pragma unroll
+  for (int k = 0; k < CP / A; ++k) at[k] = min(col(k * A), f.D - A);
   if (threadIdx.x < TT) {
     const int t = threadIdx.x;
     target_of[t] = few_target(f, t);
@@ -360,7 +382,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_grad_kernel(const Few f
       sum[t][j] = 0.0f;
     }
   }
-  const bool full = WIDE && d0 + CP <= f.D;
   const int64_t first = f.V * blockIdx.x / gridDim.x, last = f.V * (blockIdx.x + 1) / gridDim.x;
   for (int64_t v0 = first; v0 < last; v0 += kRows) {
     const int rows = static_cast<int>(min64(last - v0, kRows));
@@ -374,38 +395,65 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_grad_kernel(const Few f
       c[r][t] = p;
     }
     __syncthreads();
-#pragma unroll 2
-    for (int r = rl; r < rows; r += RL) {
-      const int64_t v = v0 + r;
-      float y[CP], z[CP] = {};
-      if (full) {
-        few_load<CP>(w + v * f.ldw + d0, y);
-      } else {
+    // U rows at a time, all their loads first (the stores of one row could be to what
+    // the next one loads, for all the compiler knows) and without conditions: past
+    // the end the last row and group are read again, with coefficients of 0 for
+    // rows and nothing stored for columns
+    for (int r0 = rl; r0 < rows; r0 += RL * U) {
+      float y[U][CP];
 #pragma unroll
-        for (int j = 0; j < CP; ++j) y[j] = col(j) < f.D ? few_float(w[v * f.ldw + col(j)]) : 0.0f;
-      }
+      for (int u = 0; u < U; ++u) {
+        const E* from = w + (v0 + min(r0 + u * RL, rows - 1)) * f.ldw;
 #pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        const float a = c[r][t];
+        for (int k = 0; k < CP; k += A) {
+          float part[A];
+          few_load<A>(from + at[k / A], part);
 #pragma unroll
-        for (int j = 0; j < CP; ++j) {
-          sum[t][j] = __fmaf_rn(a, y[j], sum[t][j]);
-          z[j] = __fmaf_rn(a, x[t][j], z[j]);
+          for (int j = 0; j < A; ++j) y[u][k + j] = part[j];
         }
       }
-      E out[CP];
 #pragma unroll
-      for (int j = 0; j < CP; ++j) few_from(z[j], &out[j]);
-      E* to = dw + v * f.lddw;
-      if (full && (reinterpret_cast<uintptr_t>(to + d0) & (CP * sizeof(E) - 1)) == 0) {
-        using U = typename FewWord<CP * sizeof(E)>::type;
-        U u;
-        memcpy(&u, out, sizeof(u));
-        *reinterpret_cast<U*>(to + d0) = u;
-      } else {
+      for (int u = 0; u < U; ++u) {
+        const int r = r0 + u * RL;
+        if (r < rows) {
+          float z[CP] = {}, a[TT];
+          if constexpr (TT >= 4) {
 #pragma unroll
-        for (int j = 0; j < CP; ++j)
-          if (col(j) < f.D) to[col(j)] = out[j];
+            for (int t = 0; t < TT; t += 4) {
+              const float4 q = *reinterpret_cast<const float4*>(&c[r][t]);
+              a[t] = q.x; a[t + 1] = q.y; a[t + 2] = q.z; a[t + 3] = q.w;
+            }
+          } else {
+#pragma unroll
+            for (int t = 0; t < TT; ++t) a[t] = c[r][t];
+          }
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int j = 0; j < CP; ++j) {
+              sum[t][j] = __fmaf_rn(a[t], y[u][j], sum[t][j]);
+              z[j] = __fmaf_rn(a[t], x[t][j], z[j]);
+            }
+          }
+          E* to = dw + (v0 + r) * f.lddw;
+#pragma unroll
+          for (int k = 0; k < CP; k += A) {
+            E out[A];
+#pragma unroll
+            for (int j = 0; j < A; ++j) few_from(z[k + j], &out[j]);
+            if (col(k) < f.D) {
+              if (A == 1 || dw_words) {
+                using U_ = typename FewWord<A * sizeof(E)>::type;
+                U_ word;
+                memcpy(&word, out, sizeof(word));
+                *reinterpret_cast<U_*>(to + col(k)) = word;
+              } else {
+#pragma unroll
+                for (int j = 0; j < A; ++j) to[col(k) + j] = out[j];
+              }
+            }
+          }
+        }
       }
     }
   }
@@ -453,45 +501,90 @@ int few_tokens_up(int64_t T) {
   while (tt < T) tt *= 2;
   return tt;
 }
-int few_ranges(int64_t V, int num_sms) { return static_cast<int>(std::min<int64_t>(2 * num_sms, (V + 15) / 16)); }
+// The gradient kernel's shape: G column groups by RL rows a CTA, `columns` CTAs
+// across and `ranges` parts of the vocabulary, as many as are resident.
+struct FewShape {
+  int G, RL, columns, ranges;
+};
+FewShape few_shape(int64_t T, int64_t D, int64_t V, int num_sms) {
+  const int tt = few_tokens_up(T), cp = few_cols(tt);
+  FewShape p;
+  p.G = static_cast<int>(std::min<int64_t>((D + cp - 1) / cp, kGradThreads));
+  p.RL = kGradThreads / p.G;
+  p.columns = static_cast<int>((D + cp * p.G - 1) / (cp * p.G));
+  const int resident = num_sms * few_resident(tt);
+  p.ranges = static_cast<int>(std::min<int64_t>((resident + p.columns - 1) / p.columns, (V + 15) / 16));
+  return p;
+}
 constexpr int kMostSms = 160;
 
 size_t few_up(size_t x) { return (x + 255) / 256 * 256; }
 
-template <typename E, int TT>
+// Tokens that the logits kernel takes at a time: h of them in shared memory.
+int few_group(int64_t T, int64_t D) {
+  int tt = few_tokens_up(T);
+  while (tt > 1 && tt * ((D + 7) / 8 * 8) * 4 > kFewBytes) tt /= 2;
+  return tt;
+}
+
+template <typename E, int TT, int W>
+cudaError_t few_logits(const Few& f, int num_sms, cudaStream_t s) {
+  auto kernel = ce_few_logits_kernel<E, TT, W>;
+  cudaError_t e = ensure_dynamic_smem(kernel, kFewBytes);
+  for (int t0 = 0; t0 < f.T && e == cudaSuccess; t0 += TT)
+    e = launch_kernel(kernel, dim3(num_sms), dim3(kFewThreads), TT * ((f.D + 7) / 8 * 8) * 4, s, 0, f, t0);
+  return e;
+}
+
+template <typename E, int TT, int W>
+cudaError_t few_grad(const Few& f, int num_sms, bool with_loss, cudaStream_t s) {
+  constexpr int CP = few_cols(TT), A = W < CP ? W : CP;
+  const FewShape p = few_shape(f.T, f.D, f.V, num_sms);
+  const bool words = reinterpret_cast<uintptr_t>(f.dw) % (A * sizeof(E)) == 0 && f.lddw % A == 0;
+  cudaError_t e = launch_kernel(ce_few_grad_kernel<E, TT, W>, dim3(p.ranges, p.columns), dim3(p.G * p.RL),
+                                p.G * p.RL * CP * 4, s, 0, f, p.G, p.RL, with_loss ? 1 : 0, words ? 1 : 0);
+  if (e != cudaSuccess) return e;
+  const int64_t n = static_cast<int64_t>(f.T) * f.D;
+  return launch_kernel(ce_few_dh_kernel<E>, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(256), 0, s, 0, f, p.ranges);
+}
+
+// Calls fn with the token count as a compile-time constant.
+template <class F>
+cudaError_t few_tokens(int tt, F fn) {
+  switch (tt) {
+    case 1: return fn(std::integral_constant<int, 1>{});
+    case 2: return fn(std::integral_constant<int, 2>{});
+    case 4: return fn(std::integral_constant<int, 4>{});
+    case 8: return fn(std::integral_constant<int, 8>{});
+    default: return fn(std::integral_constant<int, 16>{});
+  }
+}
+
+template <typename E, int W>
 cudaError_t few_run(const LinearCeArgs& a, Few f, int num_sms, cudaStream_t s) {
   const bool grad = a.dw != nullptr, given = a.loss == nullptr;
-  const bool wide = (reinterpret_cast<uintptr_t>(a.w) & 15) == 0 && a.ldw * sizeof(E) % 16 == 0;
-  const int Dp = (f.D + 7) / 8 * 8;
-  const int smem = TT * Dp * 4;
-  auto logits = wide ? ce_few_logits_kernel<E, TT, true> : ce_few_logits_kernel<E, TT, false>;
-  cudaError_t e = ensure_dynamic_smem(logits, kFewBytes);
-  if (e != cudaSuccess) return e;
   f.parts = num_sms;
-  e = launch_kernel(logits, dim3(num_sms), dim3(kFewThreads), smem, s, 0, f);
+  cudaError_t e = few_tokens(few_group(f.T, f.D), [&](auto tt) { return few_logits<E, tt.value, W>(f, num_sms, s); });
   if (e != cudaSuccess) return e;
   e = launch_kernel(ce_few_finish_kernel, dim3(1), dim3(kFewTokens * 32), 0, s, 0, f, given ? 1 : 0);
   if (e != cudaSuccess || !grad) return e;
-  constexpr int CP = few_cols(TT);
-  const int G = std::min((f.D + CP - 1) / CP, 256), RL = kFewThreads / G;
-  const int ranges = few_ranges(a.V, num_sms);
-  auto back = wide ? ce_few_grad_kernel<E, TT, true> : ce_few_grad_kernel<E, TT, false>;
-  e = launch_kernel(back, dim3(ranges, (f.D + CP * G - 1) / (CP * G)), dim3(G * RL), G * RL * CP * 4, s, 0, f, G, RL,
-                    given ? 0 : 1);
-  if (e != cudaSuccess) return e;
-  const int64_t n = static_cast<int64_t>(f.T) * f.D;
-  return launch_kernel(ce_few_dh_kernel<E>, dim3(static_cast<unsigned>((n + 31) / 32)), dim3(256), 0, s, 0, f, ranges);
+  return few_tokens(few_tokens_up(f.T), [&](auto tt) {
+    constexpr int CP = few_cols(tt.value), A = W < CP ? W : CP;
+    if (f.D % A == 0) return few_grad<E, tt.value, W>(f, num_sms, !given, s);
+    return few_grad<E, tt.value, 1>(f, num_sms, !given, s);
+  });
 }
 
 template <typename E>
 cudaError_t few_typed(const LinearCeArgs& a, const Few& f, int num_sms, cudaStream_t s) {
-  switch (few_tokens_up(a.T)) {
-    case 1: return few_run<E, 1>(a, f, num_sms, s);
-    case 2: return few_run<E, 2>(a, f, num_sms, s);
-    case 4: return few_run<E, 4>(a, f, num_sms, s);
-    case 8: return few_run<E, 8>(a, f, num_sms, s);
-    default: return few_run<E, 16>(a, f, num_sms, s);
+  auto starts_on = [&](uintptr_t bytes) {
+    return reinterpret_cast<uintptr_t>(a.w) % bytes == 0 && a.ldw * sizeof(E) % bytes == 0;
+  };
+  if (starts_on(16)) return few_run<E, 16 / sizeof(E)>(a, f, num_sms, s);
+  if constexpr (sizeof(E) == 2) {
+    if (starts_on(4)) return few_run<E, 2>(a, f, num_sms, s);
   }
+  return few_run<E, 1>(a, f, num_sms, s);
 }
 
 struct FewLayout {
@@ -511,7 +604,7 @@ FewLayout few_layout(int64_t T, int64_t D, int64_t V, bool grad) {
   l.lse = take(kFewTokens * 4);
   if (grad) {
     l.logits = take(static_cast<size_t>(T) * V * 4);
-    l.sums = take(static_cast<size_t>(few_ranges(V, kMostSms)) * T * D * 4);
+    l.sums = take(static_cast<size_t>(few_shape(T, D, V, kMostSms).ranges) * T * D * 4);
   }
   l.total = at;
   return l;
@@ -520,7 +613,7 @@ FewLayout few_layout(int64_t T, int64_t D, int64_t V, bool grad) {
 }  // namespace
 
 bool linear_ce_few_fits(int64_t T, int64_t D) {
-  return T <= kFewTokens && D <= kFewBytes && few_tokens_up(T) * ((D + 7) / 8 * 8) * 4 <= kFewBytes;
+  return T <= kFewTokens && (D + 7) / 8 * 8 * 4 <= kFewBytes;
 }
 
 size_t linear_ce_few_workspace_bytes(int64_t T, int64_t D, int64_t V, int grad) {

@@ -77,7 +77,8 @@ __device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
 //         piece of the vocabulary, rounded to bf16 planes.
 // kDh     A = c [valid][piece], B = w^T [D][piece]: dh, K split over several CTAs
 //         where there are few tiles, each split's sum kept in fp32.
-// kDw     A = c^T [piece][valid], B = h^T [D][valid]: dw of the piece.
+// kDw     A = c^T [piece][valid], B = h^T [D][valid]: dw of the piece, or as for dh
+//         the fp32 sums of parts of K where the vocabulary has few tiles.
 //
 // An accumulator adds each product step with truncation: about 5e-9 of its value
 // a step of 16, always towards zero (measured: dh over 50257 entries 9e-5 off).
@@ -100,7 +101,7 @@ struct Gemm {
   int64_t v0;           // its first one
   int tile_n;           // columns of a tile: 64 (dh, dw), 128 or 256
   int chunk;            // K blocks that one accumulator sums (see ce_gemm_kernel)
-  int splits;           // kDh: parts of K
+  int splits;           // kDh, kDw: parts of K
   int first;            // kDh: the piece that starts the sums
   float2* part;         // kLoss, kExp: [half tile][T] (largest logit, sum), base 2
   float* at_target;     // kLoss, kExp: [T]
@@ -112,7 +113,7 @@ struct Gemm {
   const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
   const float* loss;    // kCoef: [T] by token where the forward pass gave it, or nullptr
   int apart;            // kCoef: the target's c goes its own way in fp32
-  float* sum;           // kDh: [split][rows][lds]
+  float* sum;           // kDh, kDw in parts (else nullptr): [split][rows][lds]
   int64_t lds, sum_split;
   void* dw;             // kDw
   int64_t lddw;
@@ -157,7 +158,7 @@ __device__ __forceinline__ Shape shape_of(const Gemm& g, int valid) {
   s.m_tiles = (m + kPair - 1) / kPair;
   s.n_tiles = (n + g.tile_n - 1) / g.tile_n;
   s.blocks = (k + kK - 1) / kK;
-  s.splits = MODE == kDh ? g.splits : 1;
+  s.splits = MODE == kDh || MODE == kDw ? g.splits : 1;
   return s;
 }
 
@@ -232,10 +233,79 @@ __device__ __forceinline__ void store_planes(const Gemm& g, const CUtensorMap* m
   }
 }
 
+// A warp's 32 rows of a half tile of dw whose rows start anywhere: 128 bytes of each
+// row at a time in shared memory (rows 33 words apart).  Of a row, a lane of eight
+// takes one 16-byte group of the destination, on its own alignment; the 16 bytes
+// before the first and after the last whole group go element by element in a second
+// pass.  (Element stores throughout, two rows an instruction: 68 us against 49 at 149
+// x 788 x 31773 in bf16, where rows on 32 bytes take 33.)
+template <int SIZE>
+__device__ __forceinline__ void store_anywhere(const Gemm& g, int m, int n0, int cols, const float (&x)[kHalf],
+                                               uint32_t* scratch) {
+  constexpr int kSeg = 128 / SIZE, kEach = 16 / SIZE;
+  const int lane = threadIdx.x & 31, m0 = m - lane, rows = min(g.width - m0, 32);
+  const int64_t ld = g.lddw * SIZE;
+  uint8_t* base = static_cast<uint8_t*>(g.dw) + (g.v0 + m0) * ld + static_cast<int64_t>(n0) * SIZE;
+#pragma unroll
+  for (int j = 0; j < kHalf; j += kSeg) {
+    if (j < cols) {
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < 32; ++q)
+        scratch[lane * 33 + q] = SIZE == 4 ? __float_as_uint(x[j + q % kSeg])
+                                           : pack_bf16(x[j + 2 * q % kSeg], x[j + (2 * q + 1) % kSeg]);
+      __syncwarp();
+      uint8_t* seg = base + j * SIZE;
+      if (cols - j >= kSeg) {
+        int r = lane >> 3;
+        uint8_t* to = seg + r * ld;
+#pragma unroll 2
+        for (; r < rows; r += 4, to += 4 * ld) {
+          const int lead = (16 - static_cast<int>(reinterpret_cast<uintptr_t>(to))) & 15;  // bytes before a whole group
+          const int off = lead + 16 * (lane & 7);
+          if (off + 16 <= 128) {
+            const uint32_t* w = scratch + r * 33 + off / 4;
+            uint4 v;
+            if (SIZE == 4 || (off & 2) == 0) {
+              v = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+              const uint32_t w1 = w[1], w2 = w[2], w3 = w[3];
+              v = make_uint4(__byte_perm(w[0], w1, 0x5432), __byte_perm(w1, w2, 0x5432), __byte_perm(w2, w3, 0x5432),
+                             __byte_perm(w3, w[4], 0x5432));
+            }
+            *reinterpret_cast<uint4*>(to + off) = v;
+          }
+        }
+#pragma unroll
+        for (int i = lane; i < 32 * kEach; i += 32) {
+          const int q = i / kEach;
+          uint8_t* row = seg + q * ld;
+          const int lead = (16 - static_cast<int>(reinterpret_cast<uintptr_t>(row))) & 15;
+          int at = i % kEach * SIZE;
+          if (at >= lead) at += 112;  // after the 7 whole groups
+          if (lead != 0 && q < rows) {
+            const uint32_t* from = scratch + q * 33;
+            if (SIZE == 4) *reinterpret_cast<uint32_t*>(row + at) = from[at / 4];
+            else *reinterpret_cast<uint16_t*>(row + at) = reinterpret_cast<const uint16_t*>(from)[at / 2];
+          }
+        }
+      } else {  // the last columns: neighbouring lanes neighbouring elements
+        const int left = cols - j;
+        for (int r = 0; r < rows; ++r)
+          for (int c = lane; c < left; c += 32) {
+            const uint32_t* from = scratch + r * 33;
+            if (SIZE == 4) *reinterpret_cast<uint32_t*>(seg + r * ld + c * 4) = from[c];
+            else *reinterpret_cast<uint16_t*>(seg + r * ld + c * 2) = reinterpret_cast<const uint16_t*>(from)[c];
+          }
+      }
+    }
+  }
+}
+
 // One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.
 template <int MODE, int PLANES>
 __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t, int m, int n0, const Row& row, float (&x)[kHalf],
-                                         float* scratch, const CUtensorMap* map_c, uint8_t* buf) {
+                                         uint32_t* scratch, const CUtensorMap* map_c, uint8_t* buf) {
   if (MODE == kLoss || MODE == kExp) {
     const int cols = min(g.width - n0, kHalf);
     if (MODE == kLoss && (cols <= 0 || m >= valid)) return;
@@ -308,8 +378,8 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         if (j == y) x[j] = at_y;
     }
     store_planes<PLANES>(g, map_c, buf, m, n0, x);
-  } else if (MODE == kDh) {
-    if (m >= valid) return;
+  } else if (MODE == kDh || g.sum != nullptr) {
+    if (m >= (MODE == kDh ? valid : g.width)) return;
     float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
     const int cols = min(static_cast<int>(g.lds) - n0, g.tile_n);
 #pragma unroll
@@ -318,7 +388,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         uint32_t u[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          if (!g.first) x[j + q] = fadd(x[j + q], out[j + q]);
+          if (MODE == kDh && !g.first) x[j + q] = fadd(x[j + q], out[j + q]);
           u[q] = __float_as_uint(x[j + q]);
         }
         st_v8(out + j, u);
@@ -374,28 +444,8 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         }
       }
     } else {
-      // Rows that start anywhere: 16 columns at a time through shared memory, so that
-      // a store covers two rows' neighbours (5 sectors) and not 32 rows' (32).
-      const int lane = threadIdx.x & 31, m0 = m - lane, row = lane >> 4, col = lane & 15;
-#pragma unroll
-      for (int j = 0; j < kHalf; j += 16) {
-        if (j < cols) {
-          __syncwarp();
-#pragma unroll
-          for (int q = 0; q < 16; ++q) scratch[lane * 17 + q] = x[j + q];
-          __syncwarp();
-          const int rows = g.width - m0;
-#pragma unroll 4
-          for (int r = row; r < 32; r += 2) {
-            if (r < rows && j + col < cols) {
-              const int64_t at = (g.v0 + m0 + r) * g.lddw + n0 + j + col;
-              const float v = scratch[r * 17 + col];
-              if (g.dw_bf16) static_cast<__nv_bfloat16*>(g.dw)[at] = __float2bfloat16_rn(v);
-              else static_cast<float*>(g.dw)[at] = v;
-            }
-          }
-        }
-      }
+      if (g.dw_bf16) store_anywhere<2>(g, m, n0, cols, x, scratch);
+      else store_anywhere<4>(g, m, n0, cols, x, scratch);
     }
   }
 }
@@ -420,7 +470,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   // full and taken are used in the first CTA, for both; empty and done in each
   __shared__ uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
   __shared__ uint32_t tmem;
-  __shared__ float scratch[MODE == kDw ? kEpiWarps * 32 * 17 : 1];
+  __shared__ uint32_t scratch[MODE == kDw ? kEpiWarps * 32 * 33 : 1];
   uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = static_cast<int>(cluster_rank());
@@ -604,7 +654,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if (!ok) break;
       if (half * kHalf >= g.tile_n) continue;
-      epilogue<MODE, PLANES>(g, valid, t, m, t.n0 + half * kHalf, row, x, scratch + (MODE == kDw ? (warp - 2) * 32 * 17 : 0),
+      epilogue<MODE, PLANES>(g, valid, t, m, t.n0 + half * kHalf, row, x, scratch + (MODE == kDw ? (warp - 2) * 32 * 33 : 0),
                              &map_c, stage0 + kStages * kStageBytes + (warp - 2) * kStoreBytes);
     }
   }
