@@ -425,6 +425,39 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* part,
   }
 }
 
+// Both steps in one CTA for a short list (kOneCta chunks): groups of 256 threads
+// take chunks in turn.
+constexpr int kOneCta = 32;
+template <typename G, int N>
+__global__ void __launch_bounds__(4 * kThreads)
+    grad_norm_one_kernel(const __grid_constant__ Table<N> t, float* norm) {
+  pdl_begin();
+  const int group = threadIdx.x / kThreads, lane = threadIdx.x % kThreads;
+  float sum = 0.0f;
+  int at = 0;
+  for (int c = group; c < t.chunks; c += 4) {
+    while (at + 1 < t.count && t.e[at + 1].first <= c) ++at;
+    const Entry& e = t.e[at];
+    const int64_t i = static_cast<int64_t>(c - e.first) * kChunk + lane * kLane;
+    float g[8];
+    load8(static_cast<const G*>(e.grad), i, static_cast<int>(min64(max64(e.n - i, 0), kLane)), e.wide, g);
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fadd(s, fmul(g[j], g[j]));
+    sum = fadd(sum, s);
+  }
+  __shared__ double warp_sum[4 * kThreads / 32];
+  double d = sum;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+  if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = d;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 4 * kThreads / 32; ++w) d += warp_sum[w];
+    *norm = static_cast<float>(sqrt(d));
+  }
+}
+
 bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 
 // CTAs of a launch over `chunks` chunks: as many as are resident, so that every
@@ -564,10 +597,17 @@ cudaError_t launch_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, int
       list[i].n = t.n;
       list[i].wide = on32(t.grad);
     }
+    bool whole = false;
     auto launch = [&](auto type) {
       using G = decltype(type);
       return for_tables(list, n, [&](const auto& t) {
         constexpr int N = sizeof(t.e) / sizeof(Entry);
+        if constexpr (N == kSmallTable) {
+          if (count <= kSmallTable && t.chunks <= kOneCta) {  // the whole list
+            whole = true;
+            return launch_kernel(grad_norm_one_kernel<G, N>, dim3(1), dim3(4 * kThreads), 0, s, 0, t, norm);
+          }
+        }
         auto kernel = grad_square_kernel<G, N>;
         const int grid = std::min(kNormGrid, grid_of(kernel, t.chunks, num_sms));
         const cudaError_t e = launch_kernel(kernel, dim3(grid), dim3(kThreads), 0, s, 0, t, part + used);
@@ -576,7 +616,7 @@ cudaError_t launch_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, int
       });
     };
     const cudaError_t e = grad_bf16 ? launch(__nv_bfloat16{}) : launch(float{});
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || whole) return e;
   }
   return launch_kernel(grad_norm_kernel, dim3(1), dim3(kThreads), 0, s, 0, part, used, norm);
 }

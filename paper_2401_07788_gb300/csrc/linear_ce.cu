@@ -20,7 +20,7 @@
 //   dh[t] = g/s sum_v e w + g (p - 1) w[target],   p = softmax at the target
 //   dw[v] = sum_t e (g/s h[t]) + sum over tokens with target v of g (p - 1) h[t]
 // The last sum needs the tokens grouped by target; a stable order is found by
-// counting, for each token, those before it (ce_rank_kernel).
+// counting, for each token, those before it (rank_tokens).
 #include <algorithm>
 
 #include "kernels.h"
@@ -141,13 +141,12 @@ __device__ __forceinline__ int64_t rows_touched(int64_t n) { return (n + kPair -
 // The listed rows of h in planes, out[plane][i][0..Dp), one warp a row; with `ref`
 // also the logit of each row's target in base 2.
 template <typename E, int P>
-__global__ void __launch_bounds__(256)
-    ce_pack_h_kernel(const E* __restrict__ h, int64_t ldh, const Header* head, const int* __restrict__ row,
-                     int64_t padded, int D, int Dp, int wide_h, uint16_t* __restrict__ out,
-                     const E* __restrict__ w, int64_t ldw, const int* __restrict__ target, int wide_w, float* ref) {
-  pdl_begin();
-  const int n = head->valid, lane = threadIdx.x & 31;
-  const int64_t m = blockIdx.x * int64_t{8} + (threadIdx.x >> 5);
+__device__ __forceinline__ void pack_h(unsigned block, const E* __restrict__ h, int64_t ldh, int n,
+                                       const int* __restrict__ row, int64_t padded, int D, int Dp, int wide_h,
+                                       uint16_t* __restrict__ out, const E* __restrict__ w, int64_t ldw,
+                                       const int* __restrict__ target, int wide_w, float* ref) {
+  const int lane = threadIdx.x & 31;
+  const int64_t m = block * int64_t{8} + (threadIdx.x >> 5);
   if (m >= rows_touched(n)) return;
   const bool live = m < n;
   const E* src = live ? h + row[m] * ldh : nullptr;
@@ -178,12 +177,10 @@ __global__ void __launch_bounds__(256)
 
 // w in planes, for an fp32 w or rows that a tensor map cannot read.
 template <typename E, int P>
-__global__ void __launch_bounds__(256)
-    ce_pack_w_kernel(const E* __restrict__ w, int64_t ldw, int64_t V, int D, int Dp, int wide,
-                     uint16_t* __restrict__ out) {
-  pdl_begin();
+__device__ __forceinline__ void pack_w(unsigned block, unsigned blocks, const E* __restrict__ w, int64_t ldw, int64_t V,
+                                       int D, int Dp, int wide, uint16_t* __restrict__ out) {
   const int groups = Dp / 8;
-  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < V * groups; q += gridDim.x * int64_t{256}) {
+  for (int64_t q = block * int64_t{256} + threadIdx.x; q < V * groups; q += blocks * int64_t{256}) {
     const int64_t r = q / groups;
     const int d = static_cast<int>(q - r * groups) * 8;
     E x[8];
@@ -193,6 +190,75 @@ __global__ void __launch_bounds__(256)
     for (int j = 0; j < 8; ++j) planes_of<E>(x[j], p[j]);
     store_planes8<P>(out + r * Dp + d, V * Dp, p);
   }
+}
+
+// pos[i] = tokens of the list that come before token i in the order by target,
+// then by place.  Block (x, y) counts for 256 tokens over every ny-th block of 256
+// others: two instructions a pair.  Integer sums: the
+// order of the atomics does not show.
+__device__ __forceinline__ void rank_tokens(int bx, int by, int ny, int n, const int* __restrict__ target, int* pos) {
+  __shared__ int4 others[64];
+  const int i = bx * 256 + threadIdx.x;
+  if (bx * 256 >= n) return;
+  const int y = i < n ? target[i] : 0;
+  int count = 0;
+  for (int b = by; b * 256 < n; b += ny) {
+    const int j = b * 256 + threadIdx.x;
+    __syncthreads();
+    reinterpret_cast<int*>(others)[threadIdx.x] = j < n ? target[j] : 0x7fffffff;
+    __syncthreads();
+    if (b == bx) {
+      for (int q = 0; q < 256; ++q) {
+        const int o = reinterpret_cast<const int*>(others)[q];
+        count += o < y || (o == y && q < static_cast<int>(threadIdx.x));
+      }
+    } else {
+      const int below = b < bx ? y + 1 : y;  // earlier tokens with the same target come before
+#pragma unroll 8
+      for (int q = 0; q < 64; ++q) {
+        const int4 o = others[q];
+        count += (o.x < below) + (o.y < below) + (o.z < below) + (o.w < below);
+      }
+    }
+  }
+  if (i < n) atomicAdd(&pos[i], count);
+}
+
+// One launch for what the first products need: h packed, w packed where it has to
+// be, and the tokens ranked where a gradient wants them by target.
+template <typename E>
+struct Prepare {
+  const Header* head;
+  const E* h;
+  const E* w;
+  int64_t ldh, ldw, V, padded;
+  int D, Dp, wide_h, wide_w;
+  const int* row;
+  const int* target;
+  uint16_t* hp;
+  uint16_t* wp;
+  float* ref;
+  int* pos;
+  unsigned h_blocks, w_blocks, rank_x, rank_y;
+};
+
+template <typename E, int P>
+__global__ void __launch_bounds__(256) ce_prepare_kernel(const Prepare<E> f) {
+  pdl_begin();
+  const int n = f.head->valid;
+  unsigned block = blockIdx.x;
+  if (block < f.h_blocks) {
+    pack_h<E, P>(block, f.h, f.ldh, n, f.row, f.padded, f.D, f.Dp, f.wide_h, f.hp, f.w, f.ldw, f.target, f.wide_w, f.ref);
+    return;
+  }
+  block -= f.h_blocks;
+  if (block < f.w_blocks) {
+    pack_w<E, P>(block, f.w_blocks, f.w, f.ldw, f.V, f.D, f.Dp, f.wide_w, f.wp);
+    return;
+  }
+  block -= f.w_blocks;
+  rank_tokens(static_cast<int>(block % f.rank_x), static_cast<int>(block / f.rank_x), static_cast<int>(f.rank_y), n,
+              f.target, f.pos);
 }
 
 // Largest value and sum of a row's half tiles over a CTA of 32 rows (lanes) x 32
@@ -273,41 +339,6 @@ __global__ void __launch_bounds__(1024)
       head->redo = 1;
     }
   }
-}
-
-// pos[i] = tokens of the list that come before token i in the order by target,
-// then by place.  CTA (x, y) counts for 256 tokens over every gridDim.y-th block
-// of 256 others: two instructions a pair.  Integer sums: the
-// order of the atomics does not show.
-__global__ void __launch_bounds__(256)
-    ce_rank_kernel(const Header* head, const int* __restrict__ target, int* pos) {
-  pdl_begin();
-  __shared__ int4 others[64];
-  const int n = head->valid;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (blockIdx.x * 256 >= n) return;
-  const int y = i < n ? target[i] : 0;
-  int count = 0;
-  for (int b = blockIdx.y; b * 256 < n; b += gridDim.y) {
-    const int j = b * 256 + threadIdx.x;
-    __syncthreads();
-    reinterpret_cast<int*>(others)[threadIdx.x] = j < n ? target[j] : 0x7fffffff;
-    __syncthreads();
-    if (b == blockIdx.x) {
-      for (int q = 0; q < 256; ++q) {
-        const int o = reinterpret_cast<const int*>(others)[q];
-        count += o < y || (o == y && q < static_cast<int>(threadIdx.x));
-      }
-    } else {
-      const int below = b < blockIdx.x ? y + 1 : y;  // earlier tokens with the same target come before
-#pragma unroll 8
-      for (int q = 0; q < 64; ++q) {
-        const int4 o = others[q];
-        count += (o.x < below) + (o.y < below) + (o.z < below) + (o.w < below);
-      }
-    }
-  }
-  if (i < n) atomicAdd(&pos[i], count);
 }
 
 struct Finish {
@@ -747,17 +778,18 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   CE_TRY(launch_kernel(ce_scan_kernel, dim3(static_cast<unsigned>((a.T + kScan - 1) / kScan)), dim3(kScan), 0, s, 0,
                        a.targets, T, a.V, a.ignore, head, row, target, place, by_target ? ints(l.pos) : nullptr,
                        l.kept ? ints(l.flags) : nullptr, a.status));
-  CE_TRY(launch_kernel(ce_pack_h_kernel<E, P>, dim3(rows8), dim3(256), 0, s, 0, h, a.ldh, head, row, l.padded, D, Dp,
-                       wide_h, hp, w, a.ldw, target, wide_w, by_target ? floats(l.ref) : nullptr));
-  const void* wt = w;
-  int64_t wld = a.ldw;
-  if (l.pack_w) {
-    const int64_t blocks = std::min<int64_t>((a.V * (Dp / 8) + 255) / 256, num_sms * 16);
-    CE_TRY(launch_kernel(ce_pack_w_kernel<E, P>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0, w, a.ldw, a.V, D,
-                         Dp, wide_w, wp));
-    wt = wp;
-    wld = l.Dp;
+  Prepare<E> pre = {head, h, w, a.ldh, a.ldw, a.V, l.padded, D, Dp, wide_h, wide_w, row, target, hp, wp,
+                    by_target ? floats(l.ref) : nullptr, by_target ? ints(l.pos) : nullptr, rows8, 0, 0, 0};
+  if (l.pack_w)
+    pre.w_blocks = static_cast<unsigned>(std::min<int64_t>((a.V * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
+  if (by_target) {
+    pre.rank_x = static_cast<unsigned>((a.T + 255) / 256);
+    pre.rank_y = std::min(pre.rank_x, 32u);
   }
+  CE_TRY(launch_kernel(ce_prepare_kernel<E, P>, dim3(pre.h_blocks + pre.w_blocks + pre.rank_x * pre.rank_y), dim3(256), 0,
+                       s, 0, pre));
+  const void* wt = l.pack_w ? static_cast<const void*>(wp) : w;
+  const int64_t wld = l.pack_w ? l.Dp : a.ldw;
   const int64_t hplane = l.padded * l.Dp, wplane = a.V * wld;
   CUtensorMap h_rows, w_rows;  // K = D contiguous
   CE_TRY(make_map(&h_rows, hp, D, l.padded, P, l.Dp, hplane, kM));
@@ -826,11 +858,6 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   Finish f = {T, D, Dp, l.parts, a.V, l.padded, head, row, target, place, pos, ints(l.flags), g.part, g.at_target, ref,
               floats(l.sums), a.gloss, hp, a.lse_in, nullptr, nullptr, scale, factor, ints(l.order), ints(l.sorted),
               ints(l.seg_first), a.loss};
-  auto rank = [&] {
-    const unsigned blocks = static_cast<unsigned>((a.T + 255) / 256);
-    return launch_kernel(ce_rank_kernel, dim3(blocks, std::min(blocks, 32u)), dim3(256), 0, s, 0, head,
-                         target, pos);
-  };
   auto by_targets = [&] {  // the factors, then the targets' part of dw
     CE_TRY(launch_kernel(ce_scale_kernel<P>, dim3(rows8), dim3(256), 0, s, 0, f));
     g.seg_first = f.seg_first;
@@ -845,7 +872,6 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   if (l.kept) {
     uint16_t* hs = reinterpret_cast<uint16_t*>(ws + l.hs);
     f.hs = hs;
-    CE_TRY(rank());
     CE_TRY(make_map(&c_out, coef, a.V, l.padded, P, l.ldc, coef_plane, 32));
     g.width = static_cast<int>(a.V);
     g.ref = ref;
@@ -888,7 +914,6 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     g.apart = 1;
     f.lse = lse;
     f.loss_in = a.loss;
-    CE_TRY(rank());
     CE_TRY(by_targets());
   }
   g.splits = dh_plan.splits;
