@@ -473,6 +473,27 @@ def _vector(t, n: int, dtype: torch.dtype, name: str, device):
     return t
 
 
+_numel, _data_ptr, _is_contiguous, _index_of = (
+    torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device)
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _vectors(tensors, sizes: list, dtype: torch.dtype, name: str, device) -> array.array:
+    """The addresses of a list of tensors after _vector's checks of each, made one property at a
+    time for the whole list (no Python frame a tensor)."""
+    if len(tensors) != len(sizes):
+        raise MpcError(1, "%s must hold %d tensors, got %d" % (name, len(sizes), len(tensors)))
+    try:
+        fine = (list(map(_numel, tensors)) == sizes and set(map(_dtype_of, tensors)) <= {dtype}
+                and set(map(_index_of, tensors)) <= {device.index} and all(map(_is_contiguous, tensors)))
+    except (TypeError, AttributeError):
+        fine = False
+    if not fine:
+        for t, n in zip(tensors, sizes):
+            _vector(t, n, dtype, name, device)
+    return array.array("Q", map(_data_ptr, tensors))
+
+
 def _vector_or_new(t, n: int, name: str, device, stream):
     """An fp32 output of n entries: the caller's, checked, or a new one."""
     if t is not None:
@@ -583,29 +604,13 @@ def mpc_adamw_step(plan, lr: float, beta1: float, beta2: float, eps: float, step
                                 max_norm, _raw_stream(stream)))
 
 
-_numel, _data_ptr, _is_contiguous, _index_of = (
-    torch.Tensor.numel, torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device)
-_dtype_of = operator.attrgetter("dtype")
-
-
 def mpc_adamw_decode(plan, m_out, v_out, stream=None):
     """The fp32 values that the 8-bit states of an ``AdamWPlan`` stand for, into the tensors of
     m_out and v_out (one for each tensor of the plan)."""
     if plan.state_bits != 8:
         raise MpcError(1, "the plan's states are not 8-bit codes")
-    lists = []
-    for name, outs in (("m_out", m_out), ("v_out", v_out)):
-        if len(outs) != plan.count:
-            raise MpcError(1, "%s must hold one tensor for each of the plan's %d" % (name, plan.count))
-        try:  # one pass a property, each without a Python frame a tensor
-            fine = (list(map(_numel, outs)) == plan.sizes and set(map(_dtype_of, outs)) == {torch.float32}
-                    and set(map(_index_of, outs)) == {plan.index} and all(map(_is_contiguous, outs)))
-        except TypeError:
-            fine = False
-        if not fine:
-            for t, n in zip(outs, plan.sizes):
-                _vector(t, n, torch.float32, name, plan.device)
-        lists.append(array.array("Q", map(_data_ptr, outs)))
+    lists = [_vectors(outs, plan.sizes, torch.float32, name, plan.device)
+             for name, outs in (("m_out", m_out), ("v_out", v_out))]
     _check(lib().mpc_adamw_decode(plan.table, plan.count, lists[0].buffer_info()[0],
                                   lists[1].buffer_info()[0], _raw_stream(stream)))
     return m_out, v_out

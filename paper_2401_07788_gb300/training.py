@@ -14,9 +14,10 @@ from __future__ import annotations
 
 import ctypes
 
+import numpy as np
 import torch
 
-from . import (MpcError, _DTYPES, _cuda, _dtype, mpc_adamw_step, mpc_grad_norm,
+from . import (MpcError, _dtype, _vectors, mpc_adamw_step, mpc_grad_norm,
                mpc_linear_ce_backward, mpc_linear_ce_forward, mpc_linear_ce_train)
 
 __all__ = ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
@@ -112,6 +113,10 @@ class _Tensor(ctypes.Structure):
                 ("lr_scale", ctypes.c_double), ("weight_decay", ctypes.c_double)]
 
 
+_TABLE = np.dtype([(name, np.float64 if kind is ctypes.c_double else np.int64 if kind is ctypes.c_int64 else np.uint64)
+                   for name, kind in _Tensor._fields_])
+
+
 class AdamWPlan:
     """The tensors of an optimiser step: params (float32, or bfloat16 without a master copy),
     grads, and the states m and v, each a list with one contiguous CUDA tensor for each param.
@@ -130,9 +135,10 @@ class AdamWPlan:
             raise MpcError(1, "a plan needs at least one tensor")
         if (m is None) != (v is None):
             raise MpcError(1, "m and v are given together")
+        self.param_type = _dtype(params[0], "param")
         self.device = params[0].device
-        self.index = params[0].get_device()
         self.norm_ws = None  # mpc_grad_norm's workspace, made by its first call
+        self.count = n
         self.sizes = [p.numel() for p in params]
         blocks = [-(-k // BLOCK) for k in self.sizes]
         if m is None:
@@ -145,63 +151,51 @@ class AdamWPlan:
                                     for _ in range(2))
         m, v = list(m), list(v)
         self.state_bits = 8 if m and m[0].dtype == torch.int8 else 32
-        self.param_type, self.grad_type = _dtype(params[0], "param"), _dtype(grads[0], "grad") if grads else 0
-        kinds = {"param": params[0].dtype, "grad": grads[0].dtype if grads else None}
-        lists = {"param": params, "grad": grads, "m": m, "v": v}
-        if self.state_bits == 8:
-            if m_scale is None or v_scale is None:
-                raise MpcError(1, "8-bit states need m_scale and v_scale")
-            lists.update(m_scale=list(m_scale), v_scale=list(v_scale))
-            kinds.update(m=torch.int8, v=torch.uint8, m_scale=torch.float32, v_scale=torch.float32)
-        else:
-            kinds.update(m=torch.float32, v=torch.float32)
-        for name, tensors in lists.items():
-            if len(tensors) != n:
-                raise MpcError(1, "%d params but %d entries of %s" % (n, len(tensors), name))
-            for t, k in zip(tensors, blocks if name.endswith("scale") else self.sizes):
-                self._check(t, kinds[name], name, k)
+        # the list that the calls take: ctypes owns it, numpy fills whole columns of it
+        self.table = (_Tensor * n)()
+        self._columns = np.frombuffer(self.table, dtype=_TABLE)
+        low = self.state_bits == 8
+        if low and (m_scale is None or v_scale is None):
+            raise MpcError(1, "8-bit states need m_scale and v_scale")
+        self._fill("param", params, params[0].dtype, self.sizes)
+        self._fill("exp_avg", m, torch.int8 if low else torch.float32, self.sizes, "m")
+        self._fill("exp_avg_sq", v, torch.uint8 if low else torch.float32, self.sizes, "v")
+        if low:
+            m_scale, v_scale = list(m_scale), list(v_scale)
+            self._fill("scale_m", m_scale, torch.float32, blocks, "m_scale")
+            self._fill("scale_v", v_scale, torch.float32, blocks, "v_scale")
         copies = [None] * n if copies is None else list(copies)
         if len(copies) != n:
             raise MpcError(1, "%d params but %d copies" % (n, len(copies)))
-        for t, k in zip(copies, self.sizes):
-            if t is not None:
-                self._check(t, torch.bfloat16, "copy", k)
+        there = [i for i, t in enumerate(copies) if t is not None]
+        if there:
+            self._columns["copy"][there] = _vectors([copies[i] for i in there], [self.sizes[i] for i in there],
+                                                    torch.bfloat16, "copy", self.device)
+        self._columns["n"] = self.sizes
+        self.set_groups(lr_scale, weight_decay)
         self.params, self.m, self.v, self.copies = params, m, v, copies
-        self.m_scale, self.v_scale = lists.get("m_scale"), lists.get("v_scale")
-        self.count = n
-        self.table = (_Tensor * n)()
-        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
-        scale = [float(lr_scale)] * n if isinstance(lr_scale, (int, float)) else list(lr_scale)
-        if len(decay) != n or len(scale) != n:
-            raise MpcError(1, "weight_decay and lr_scale are one number or one for each tensor")
-        for i, e in enumerate(self.table):
-            e.param, e.exp_avg, e.exp_avg_sq = params[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr()
-            if self.state_bits == 8:
-                e.scale_m, e.scale_v = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
-            e.copy = None if copies[i] is None else copies[i].data_ptr()
-            e.n, e.lr_scale, e.weight_decay = self.sizes[i], scale[i], decay[i]
-        self.grads = [None] * n
+        self.m_scale, self.v_scale = (m_scale, v_scale) if low else (None, None)
+        if not grads:
+            raise MpcError(1, "%d params but no grads" % n)
+        self.grad_type = _dtype(grads[0], "grad")
         self.set_grads(grads)
 
-    def _check(self, t, dtype, name, n):
-        _cuda(t, dtype, name)
-        if t.numel() != n or t.device != self.device:
-            raise MpcError(1, "%s must hold %d entries on %s" % (name, n, self.device))
+    def _fill(self, column, tensors, dtype, sizes, name=None):
+        self._columns[column] = _vectors(tensors, sizes, dtype, name or column, self.device)
 
     def set_grads(self, grads) -> None:
         """Other gradient tensors for the next calls, e.g. those of a new backward pass."""
-        if len(grads) != self.count:
-            raise MpcError(1, "%d params but %d grads" % (self.count, len(grads)))
-        dtype = torch.bfloat16 if self.grad_type else torch.float32
-        for i, g in enumerate(grads):
-            self._check(g, dtype, "grad", self.sizes[i])
-        for i, g in enumerate(grads):
-            self.table[i].grad = g.data_ptr()
-        self.grads = list(grads)
+        grads = list(grads)
+        self._fill("grad", grads, torch.bfloat16 if self.grad_type else torch.float32, self.sizes)
+        self.grads = grads
 
-    def set_group(self, i: int, lr_scale: float, weight_decay: float) -> None:
-        """The factor on lr and the weight decay of tensor i from the next step on."""
-        self.table[i].lr_scale, self.table[i].weight_decay = lr_scale, weight_decay
+    def set_groups(self, lr_scale, weight_decay) -> None:
+        """The factor on lr and the weight decay from the next step on: one number or one for each
+        tensor."""
+        for name, x in (("lr_scale", lr_scale), ("weight_decay", weight_decay)):
+            if not isinstance(x, (int, float)) and len(x) != self.count:
+                raise MpcError(1, "%s is one number or one for each tensor" % name)
+            self._columns[name] = x
 
 
 class AdamW(torch.optim.Optimizer):
@@ -283,8 +277,8 @@ class AdamW(torch.optim.Optimizer):
                 self._plans[ident] = plan
             else:
                 plan.set_grads(grads)
-            for i, (_, _, group) in enumerate(entries):
-                plan.set_group(i, group["lr"], group["weight_decay"])
+            plan.set_groups([group["lr"] for _, _, group in entries],
+                            [group["weight_decay"] for _, _, group in entries])
             plans.append((key, plan))
         norm = None
         if self.max_norm > 0.0 and plans:
