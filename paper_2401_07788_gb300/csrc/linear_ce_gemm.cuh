@@ -86,6 +86,13 @@ __device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
 // (within a block the smallest plane products first), and the epilogue adds the
 // chunks in fp32 with rounding to nearest; two accumulators in turn keep the
 // products running.
+//
+// Measured at 7373 tokens that count x 768 x 50257 in bf16 (0.57 TFLOP each): kExp
+// 380 us (302 without its epilogue, 350 without its stores: eight warps' latency and
+// the 0.7 GB of c), kDh 355, kDw 340 (1.6 to 1.7 PFLOP/s; cuBLAS does 1.7 for seconds,
+// 1.9 in a burst; the tensor pipe is 74 % busy at 1.78 GHz).  2048 tokens in fp32
+// (0.95 TFLOP of plane products each): 530, 467 and 500 us.
+//
 // Operands whose K is not the contiguous axis (w^T, c^T, h^T) are read as they
 // are: rows of 64 M/N-elements, and the product's descriptors say so.
 // ---------------------------------------------------------------------------
