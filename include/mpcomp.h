@@ -338,6 +338,8 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
  *          hidden, vocab, type, MPC_CE_BACKWARD, piece, ldw), 256-byte
  *          aligned.
  * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
+ * Up to 16 tokens go by another form, whose logits (4 bytes each) are in the
+ * workspace whatever `piece` is.
  * tokens = 0 writes dw = 0. */
 mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
                                   const int64_t* targets, const float* lse, const float* gloss,
@@ -348,7 +350,7 @@ mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int
 
 /* Loss and gradients in one call, for a training step that knows g beforehand:
  * the arguments and results of the two calls above.  With piece = 0 (or >= vocab)
- * and 257 to 16384 tokens whose exponentials take 4 GiB of workspace at most (2
+ * and 257 to 16384 tokens (17 in fp32) whose exponentials take 4 GiB of workspace at most (2
  * bytes each, 6 for fp32), the logits are formed once; otherwise as in the two
  * calls.
  *   ws  workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens, hidden,

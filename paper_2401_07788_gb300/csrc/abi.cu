@@ -170,7 +170,7 @@ bool pdl_enabled() { return g_pdl.load(std::memory_order_relaxed) != 0; }
 
 extern "C" {
 
-int mpc_version(void) { return 100; }
+int mpc_version(void) { return 200; }
 
 size_t mpc_topk_workspace_bytes(int64_t rows, int64_t row_len, int64_t k) {
   if (rows <= 0 || row_len < 1 || k < 1 || k > row_len) return 0;

@@ -428,3 +428,36 @@ def test_plain_stream_order_gives_the_same(mpc):
         mpc.mpc_set_knob(mpc.MPC_KNOB_PDL, 1)
     for a, b in zip(with_pdl, without):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_no_token_of_many_counts(mpc, dtype):
+    h, w, y = inputs(600, 40, 300, dtype, ignored=1.0)
+    for dh, dw in (mpc.mpc_linear_ce_backward(h, w, y, torch.zeros(600, device="cuda")),
+                   mpc.mpc_linear_ce_train(h, w, y)[1:]):
+        assert not dh.any() and not dw.any()
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    assert not loss.any() and not lse.any()
+    assert mpc.mpc_get_status() == 0
+
+
+def test_one_token_of_many_counts(mpc):
+    h, w, y = inputs(600, 40, 300, torch.float32, seed=50, ignored=1.0)
+    y[431] = 7
+    h[431] = w[7] * 2
+    want = oracle(h, w, y)
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    near(loss, want["loss"], "loss")
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_more_tokens_than_are_ordered(mpc, dtype):
+    """Beyond 16384 tokens a training call forms the logits twice."""
+    h, w, y = inputs(16500, 24, 200, dtype, seed=51)
+    want = oracle(h, w, y)
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    near(loss, want["loss"], "loss")
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
