@@ -126,7 +126,7 @@ template <typename E, int TT, int W>
 __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few f, int t0) {
   constexpr int VEC = W;
   constexpr bool WIDE = W * sizeof(E) == 16;
-  constexpr int R = TT >= 2 ? 4 : 8;  // rows a warp takes at a time
+  constexpr int R = TT == 1 ? 8 : 4;  // rows a warp takes at a time
   constexpr int N = R * TT;
   pdl_begin();
   extern __shared__ float sh[];
@@ -232,7 +232,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
         }
       }
     } else {
-#pragma unroll (W == 1 ? 4 : 2)
+      // enough narrow loads in flight (pairs at 4 x 1854 x 92484: 118 -> 88 us from two)
+#pragma unroll (W == 1 ? (TT <= 4 ? 8 : 4) : (TT <= 8 ? 4 : 2))
       for (int d = lane * W; d < whole; d += 32 * W) {
         float x[R][W];
 #pragma unroll
