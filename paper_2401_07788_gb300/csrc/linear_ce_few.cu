@@ -538,7 +538,7 @@ FewShape few_shape(int64_t T, int64_t D, int64_t V, int num_sms) {
   p.RL = kGradThreads / p.G;
   p.columns = static_cast<int>((D + cp * p.G - 1) / (cp * p.G));
   const int resident = num_sms * few_resident(tt);
-  p.ranges = static_cast<int>(std::min<int64_t>((resident + p.columns - 1) / p.columns, (V + 15) / 16));
+  p.ranges = static_cast<int>(std::min<int64_t>(std::max(resident / p.columns, 1), (V + 15) / 16));
   return p;
 }
 constexpr int kMostSms = 160;
