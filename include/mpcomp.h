@@ -338,8 +338,8 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
  *          hidden, vocab, type, MPC_CE_BACKWARD, piece, ldw), 256-byte
  *          aligned.
  * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
- * Up to 16 tokens go by another form, whose logits (4 bytes each) are in the
- * workspace whatever `piece` is.
+ * A few tokens (16 at most) may go by another form, whose logits (4 bytes each)
+ * are in the workspace whatever `piece` is.
  * tokens = 0 writes dw = 0. */
 mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int64_t ldw,
                                   const int64_t* targets, const float* lse, const float* gloss,

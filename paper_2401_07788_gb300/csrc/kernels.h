@@ -165,8 +165,8 @@ struct LinearCeArgs {
 size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int pass, int64_t piece,
                                  int64_t ldw);
 cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s);
-// The same for a few tokens (linear_ce_few.cu).
-bool linear_ce_few_fits(int64_t T, int64_t D);
+// The same for a few tokens (linear_ce_few.cu), where that is the faster way.
+bool linear_ce_few_fits(int64_t T, int64_t D, int64_t V, int64_t ldw, bool bf16, bool grad);
 size_t linear_ce_few_workspace_bytes(int64_t T, int64_t D, int64_t V, int grad);
 cudaError_t launch_linear_ce_few(const LinearCeArgs& a, int num_sms, cudaStream_t s);
 

@@ -22,7 +22,7 @@
 // The last sum needs the tokens grouped by target; a stable order is found by
 // counting, for each token, those before it (rank_tokens).
 //
-// Up to 16 tokens go another way (linear_ce_few.cu).  The small kernels here let
+// A few tokens go another way (linear_ce_few.cu).  The small kernels here let
 // their successor be scheduled as they start.
 //
 // What bounds it: the matrix units (linear_ce_gemm.cuh).  Measured: 8192 tokens (a
@@ -959,12 +959,15 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
 }  // namespace
 
 size_t linear_ce_workspace_bytes(int64_t T, int64_t D, int64_t V, int bf16, int pass, int64_t piece, int64_t ldw) {
-  if (linear_ce_few_fits(T, D)) return linear_ce_few_workspace_bytes(T, D, V, pass != kForward);
+  if (linear_ce_few_fits(T, D, V, ldw, bf16 != 0, pass != kForward))
+    return linear_ce_few_workspace_bytes(T, D, V, pass != kForward);
   return layout(T, D, V, bf16 != 0, pass, piece, ldw).total;
 }
 
 cudaError_t launch_linear_ce(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
-  if (linear_ce_few_fits(a.T, a.D)) return launch_linear_ce_few(a, num_sms, s);
+  const int64_t ldw = reinterpret_cast<uintptr_t>(a.w) % 16 == 0 ? a.ldw : 0;
+  if (linear_ce_few_fits(a.T, a.D, a.V, ldw, a.bf16 != 0, a.dw != nullptr))
+    return launch_linear_ce_few(a, num_sms, s);
   return a.bf16 ? run<__nv_bfloat16>(a, num_sms, s) : run<float>(a, num_sms, s);
 }
 

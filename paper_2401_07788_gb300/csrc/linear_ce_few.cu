@@ -1,4 +1,4 @@
-// linear_ce_few.cu -- the linear cross entropy of a few tokens (16 at most): a
+// linear_ce_few.cu -- the linear cross entropy of a few tokens (32 at most): a
 // scored token of a served model, the last tokens of a batch.
 //
 // With so few tokens the work is one pass over w (and one over dw): T products a
@@ -35,7 +35,8 @@
 namespace mpc {
 namespace {
 
-constexpr int kFewTokens = 16;
+constexpr int kFewTokens = 32;  // of a call; of a gradient, and of a pass over w, 16
+constexpr int kFewGroup = 16;
 constexpr int kFewThreads = 512;
 constexpr int kFewWarps = kFewThreads / 32;
 constexpr int kFewBytes = 200 * 1024;  // of h in fp32 in shared memory
@@ -547,18 +548,17 @@ size_t few_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Tokens that the logits kernel takes at a time: h of them in shared memory.
 int few_group(int64_t T, int64_t D) {
-  int tt = few_tokens_up(T);
+  int tt = std::min(few_tokens_up(T), kFewGroup);
   while (tt > 1 && tt * ((D + 7) / 8 * 8) * 4 > kFewBytes) tt /= 2;
   return tt;
 }
 
 template <typename E, int TT, int W>
-cudaError_t few_logits(const Few& f, int num_sms, cudaStream_t s) {
+cudaError_t few_logits(const Few& f, int t0, int num_sms, cudaStream_t s) {
   auto kernel = ce_few_logits_kernel<E, TT, W>;
   cudaError_t e = ensure_dynamic_smem(kernel, kFewBytes);
-  for (int t0 = 0; t0 < f.T && e == cudaSuccess; t0 += TT)
-    e = launch_kernel(kernel, dim3(num_sms), dim3(kFewThreads), TT * ((f.D + 7) / 8 * 8) * 4, s, 0, f, t0);
-  return e;
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kernel, dim3(num_sms), dim3(kFewThreads), TT * ((f.D + 7) / 8 * 8) * 4, s, 0, f, t0);
 }
 
 template <typename E, int TT, int W>
@@ -589,8 +589,13 @@ template <typename E, int W>
 cudaError_t few_run(const LinearCeArgs& a, Few f, int num_sms, cudaStream_t s) {
   const bool grad = a.dw != nullptr, given = a.loss == nullptr;
   f.parts = num_sms;
-  cudaError_t e = few_tokens(few_group(f.T, f.D), [&](auto tt) { return few_logits<E, tt.value, W>(f, num_sms, s); });
-  if (e != cudaSuccess) return e;
+  const int most = few_group(f.T, f.D);
+  cudaError_t e = cudaSuccess;
+  for (int t0 = 0; t0 < f.T; t0 += most) {
+    e = few_tokens(std::min(most, few_tokens_up(f.T - t0)),
+                   [&](auto tt) { return few_logits<E, tt.value, W>(f, t0, num_sms, s); });
+    if (e != cudaSuccess) return e;
+  }
   e = launch_kernel(ce_few_finish_kernel, dim3(1), dim3(kFewTokens * 32), 0, s, 0, f, given ? 1 : 0);
   if (e != cudaSuccess || !grad) return e;
   return few_tokens(few_tokens_up(f.T), [&](auto tt) {
@@ -637,8 +642,27 @@ FewLayout few_layout(int64_t T, int64_t D, int64_t V, bool grad) {
 
 }  // namespace
 
-bool linear_ce_few_fits(int64_t T, int64_t D) {
-  return T <= kFewTokens && (D + 7) / 8 * 8 * 4 <= kFewBytes;
+// Whether a call goes this way, or by the matrix units, whose time hardly depends on
+// so few tokens while a pass over w here takes 16 FMAs or less an element at no more
+// than the memory's rate.  Measured, this way against the other:
+//   fp32, loss       32 x 768 x 50257 145 us against 141, 17 tokens 110; 32 x 2075 x
+//                    98787 460 against 780; 32 x 4096 x 131072 1517 against 1640
+//   fp32, gradient   16 x 768 x 50257 234 us against 316, 16 x 4096 x 131072 2290
+//                    against 3150; with sums for 32 tokens in registers 383 and 4548
+//   bf16, loss       8 x 768 x 50257 40 us against 46, 8 x 4096 x 131072 258 against
+//                    360, 16 of them 70 and 504; rows off 16 bytes, which the other
+//                    way copies first: 16 x 2075 x 98787 225 against 332
+//   bf16, gradient   8 x 2075 x 98787 800 us against 804, 8 x 4096 x 131072 1027
+//                    against 1144, 16 of them 1146 and 2028
+// Small heads are bound by launches, of which this way has fewer: 16 x 300 x 5000 in
+// bf16 42 us against 67, 16 x 1001 x 30000 195 against 187.  Wide rows take several
+// passes: four over an fp32 w cost what the other way does, two over a bf16 one.
+// ldw: 0 for a w that does not start on 16 bytes, as for the workspace.
+bool linear_ce_few_fits(int64_t T, int64_t D, int64_t V, int64_t ldw, bool bf16, bool grad) {
+  if (T > (bf16 || grad ? kFewGroup : kFewTokens) || (D + 7) / 8 * 8 * 4 > kFewBytes) return false;
+  if (T > few_group(T, D) * (bf16 ? 1 : 4)) return false;
+  const bool copied = ldw == 0 || ldw % 8 != 0;  // a bf16 w by the other way
+  return !bf16 || T <= 8 || D * V < int64_t{1} << 24 || (!grad && copied);
 }
 
 size_t linear_ce_few_workspace_bytes(int64_t T, int64_t D, int64_t V, int grad) {

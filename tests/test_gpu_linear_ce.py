@@ -376,6 +376,31 @@ def test_few_tokens(mpc, dtype, T, D, V):
     assert mpc.mpc_get_status() == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [8, 9, 16, 20, 31, 32, 33])
+@pytest.mark.parametrize("D,V,off", [(768, 22000, 0), (771, 22000, 0), (768, 22000, 1), (7000, 2500, 0)])
+def test_few_tokens_of_a_large_head(mpc, dtype, T, D, V, off):
+    """Where the two forms meet over a head of more than 2^24 entries: rows on and off 16 bytes, a base
+    off 16 bytes, rows whose h takes several passes; each direction by itself and together."""
+    h, w, y = inputs(T, D, V, dtype, seed=31, ignored=0.2)
+    flat = torch.zeros(V * D + 8, dtype=dtype, device="cuda")
+    flat[off:off + V * D] = w.reshape(-1)
+    placed = flat[off:off + V * D].view(V, D)
+    gloss = torch.randn(T, device="cuda")
+    want = oracle(h, w, y, gloss)
+    loss, lse = mpc.mpc_linear_ce_forward(h, placed, y)
+    near(loss, want["loss"], "loss")
+    near(lse, want["lse"], "lse")
+    dh, dw = mpc.mpc_linear_ce_backward(h, placed, y, lse, gloss)
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, placed, y, gloss)
+    near(loss, want["loss"], "loss (train)")
+    near(dh, want["dh"], "dh (train)")
+    near(dw, want["dw"], "dw (train)")
+    assert mpc.mpc_get_status() == 0
+
+
 def test_autograd_of_layouts(mpc):
     """Hidden states that are broadcast, transposed or cut out of something wider; a transposed weight."""
     D, V = 40, 90
