@@ -374,7 +374,8 @@ template <> struct FewWord<16> { using type = uint4; };
 // dw_words: dw's rows suit accesses of A.
 template <typename E, int TT, int W>
 __global__ void __launch_bounds__(kGradThreads, few_resident(TT)) ce_few_grad_kernel(const Few f, int G, int RL, int with_loss, int dw_words) {
-  constexpr int kRows = 64, CP = few_cols(TT), A = W < CP ? W : CP, U = 4;
+  constexpr int kRows = 64, CP = few_cols(TT), A = W < CP ? W : CP, U = A == 1 && sizeof(E) == 4 && (TT == 4 || TT == 8) ? 2 : 4;
+  constexpr bool kAhead = TT >= 8 || A == 4 || U == 2;
   pdl_begin();
   __shared__ __align__(16) float c[kRows][TT];
   __shared__ float lse_of[TT], weight_of[TT], minus_loss[TT];
@@ -409,6 +410,29 @@ __global__ void __launch_bounds__(kGradThreads, few_resident(TT)) ce_few_grad_ke
     }
   }
   const int64_t first = f.V * blockIdx.x / gridDim.x, last = f.V * (blockIdx.x + 1) / gridDim.x;
+  // U rows at a time, all their loads before the first store (which could be to what
+  // the next row loads, for all the compiler knows) and without conditions: past the
+  // end the last row and group are read again, with nothing done for them.  Where
+  // registers allow, the loads run one step ahead, over the fill of c too (4096 x
+  // 131072 fp32, 16 tokens 2310 -> 1976 us, 8 1224 -> 1092, 4 1027 -> 1018); loads of
+  // single elements spill then.  2075 x 98787, four rows, four ahead, two ahead: fp32,
+  // 8 tokens 764, 793, 695 us, 4 tokens 566, 869, 557, 2 tokens 492, 856, 532; bf16, 8
+  // tokens 810, 756, 841, 4 tokens 564, 572, 591.
+  float next[U][CP];
+  auto read = [&](int64_t v) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const E* from = w + min64(v + rl + u * RL, last - 1) * f.ldw;
+#pragma unroll
+      for (int k = 0; k < CP; k += A) {
+        float part[A];
+        few_load<A>(from + at[k / A], part);
+#pragma unroll
+        for (int j = 0; j < A; ++j) next[u][k + j] = part[j];
+      }
+    }
+  };
+  if (kAhead) read(first);
   for (int64_t v0 = first; v0 < last; v0 += kRows) {
     const int rows = static_cast<int>(min64(last - v0, kRows));
     __syncthreads();
@@ -421,26 +445,17 @@ __global__ void __launch_bounds__(kGradThreads, few_resident(TT)) ce_few_grad_ke
       c[r][t] = p;
     }
     __syncthreads();
-    // U rows at a time, all their loads first (the stores of one row could be to what
-    // the next one loads, for all the compiler knows) and without conditions: past
-    // the end the last row and group are read again, with coefficients of 0 for
-    // rows and nothing stored for columns
-    for (int r0 = rl; r0 < rows; r0 += RL * U) {
+    for (int b = 0; b < rows; b += RL * U) {
       float y[U][CP];
+      if (!kAhead) read(v0 + b);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < CP; ++k) y[u][k] = next[u][k];
+      if (kAhead) read(b + RL * U < rows ? v0 + b + RL * U : v0 + kRows);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const E* from = w + (v0 + min(r0 + u * RL, rows - 1)) * f.ldw;
-#pragma unroll
-        for (int k = 0; k < CP; k += A) {
-          float part[A];
-          few_load<A>(from + at[k / A], part);
-#pragma unroll
-          for (int j = 0; j < A; ++j) y[u][k + j] = part[j];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = r0 + u * RL;
+        const int r = b + rl + u * RL;
         if (r < rows) {
           float z[CP] = {}, a[TT];
           if constexpr (TT >= 4) {
@@ -647,13 +662,14 @@ FewLayout few_layout(int64_t T, int64_t D, int64_t V, bool grad) {
 // than the memory's rate.  Measured, this way against the other:
 //   fp32, loss       32 x 768 x 50257 145 us against 141, 17 tokens 110; 32 x 2075 x
 //                    98787 460 against 780; 32 x 4096 x 131072 1517 against 1640
-//   fp32, gradient   16 x 768 x 50257 234 us against 316, 16 x 4096 x 131072 2290
+//   fp32, gradient   16 x 768 x 50257 207 us against 316, 16 x 4096 x 131072 1976
 //                    against 3150; with sums for 32 tokens in registers 383 and 4548
+//                    (one step behind in its loads)
 //   bf16, loss       8 x 768 x 50257 40 us against 46, 8 x 4096 x 131072 258 against
 //                    360, 16 of them 70 and 504; rows off 16 bytes, which the other
 //                    way copies first: 16 x 2075 x 98787 225 against 332
-//   bf16, gradient   8 x 2075 x 98787 800 us against 804, 8 x 4096 x 131072 1027
-//                    against 1144, 16 of them 1146 and 2028
+//   bf16, gradient   8 x 2075 x 98787 756 us against 804, 8 x 4096 x 131072 1025
+//                    against 1144, 16 of them 2028 and 1146 (as above)
 // Small heads are bound by launches, of which this way has fewer: 16 x 300 x 5000 in
 // bf16 42 us against 67, 16 x 1001 x 30000 195 against 187.  Wide rows take several
 // passes: four over an fp32 w cost what the other way does, two over a bf16 one.
