@@ -275,7 +275,9 @@ __global__ void __launch_bounds__(256) ce_prepare_kernel(const Prepare<E> f) {
 
 // Largest value and sum of a row's half tiles over a CTA of 32 rows (lanes) x 32
 // warps, in a fixed order; the result is valid in warp 0.  RELATIVE: the sums are
-// over exp2 from each part's own largest value, else from one reference.
+// over exp2 from each part's own largest value, else from one reference.  A part
+// whose largest is -inf sums to 0, or to NaN: a largest value does not show NaN
+// logits (fmaxf takes the other operand), so every sum is added.
 template <bool RELATIVE>
 __device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T, int m, int n) {
   __shared__ float top_of[32][33], sum_of[32][33];
@@ -288,7 +290,7 @@ __device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T
     for (int i = warp; i < parts; i += 32) {
       const float2 p = part[static_cast<int64_t>(i) * T + m];
       if (RELATIVE) {
-        if (p.x != -INFINITY) sum = fadd(sum, fmul(p.y, exp2f(fsub(p.x, top))));
+        sum = fadd(sum, p.x == -INFINITY ? p.y : fmul(p.y, exp2f(fsub(p.x, top))));
       } else {
         top = fmaxf(top, p.x);
         sum = fadd(sum, p.y);
@@ -303,8 +305,8 @@ __device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T
     for (int w = 0; w < 32; ++w) r.x = fmaxf(r.x, top_of[w][lane]);
     for (int w = 0; w < 32; ++w) {
       const float t = top_of[w][lane];
-      if (!RELATIVE) r.y = fadd(r.y, sum_of[w][lane]);
-      else if (t != -INFINITY) r.y = fadd(r.y, fmul(sum_of[w][lane], exp2f(fsub(t, r.x))));
+      const float s = sum_of[w][lane];
+      r.y = fadd(r.y, !RELATIVE || t == -INFINITY ? s : fmul(s, exp2f(fsub(t, r.x))));
     }
   }
   return r;

@@ -1,0 +1,66 @@
+"""NaN and infinity in w, in tokens that count and in gradients: they show in the results that the
+formulas give them to, whichever form a call takes, and nowhere else."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def mpc():
+    import __graft_entry__ as g
+
+    g.build()
+    import paper_2401_07788_gb300 as m
+
+    torch.cuda.set_device(0)
+    return m
+
+
+def inputs(T, D, V, dtype, ignored=0.2):
+    gen = torch.Generator(device="cuda").manual_seed(T + 7 * D + 13 * V)
+    dev = {"device": "cuda", "generator": gen}
+    w, h = torch.randn(V, D, **dev) / D ** 0.5, torch.randn(T, D, **dev)
+    y = torch.randint(0, V, (T,), **dev)
+    y[torch.randperm(T, **dev)[: int(ignored * T)]] = -100
+    return h.to(dtype), w.to(dtype), y
+
+
+TYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+
+
+@TYPES
+@pytest.mark.parametrize("T", [40, 100, 600])
+@pytest.mark.parametrize("V,first,last", [(129, 128, 129), (4225, 4224, 4225), (600, 128, 256), (600, 512, 600),
+                                          (5000, 0, 1), (5000, 4096, 5000)])
+def test_nan_in_w_reaches_every_loss(mpc, dtype, T, V, first, last):
+    """Rows of w that are NaN, alone in the last columns of a tile, all of a half tile's, and among others:
+    every token that counts has a NaN logit, so its loss and lse are NaN.  Tokens that do not count stay 0."""
+    h, w, y = inputs(T, 72, V, dtype)
+    w[first:last] = NAN
+    counts = y != -100
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    train = mpc.mpc_linear_ce_train(h, w, y)[0]
+    for x in (loss, lse, train):
+        assert bool(x[counts].isnan().all()) and not x[~counts].any()
+
+
+@TYPES
+@pytest.mark.parametrize("T", [40, 600])
+def test_nan_in_one_token(mpc, dtype, T):
+    """A token that counts and holds NaN: its own loss and row of dh, and (by its coefficients) dw; the
+    other tokens' losses and rows are as without it."""
+    h, w, y = inputs(T, 72, 900, dtype, ignored=0.0)
+    clean_loss, clean_lse = mpc.mpc_linear_ce_forward(h, w, y)
+    clean = mpc.mpc_linear_ce_train(h, w, y)
+    h[17, 5] = NAN
+    others = torch.arange(T, device="cuda") != 17
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    tloss, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    assert bool(loss[17].isnan()) and bool(lse[17].isnan()) and bool(tloss[17].isnan()) and bool(dh[17].isnan().all())
+    assert bool(dw.isnan().all())
+    assert torch.equal(loss[others], clean_loss[others]) and torch.equal(lse[others], clean_lse[others])
+    assert torch.equal(tloss[others], clean[0][others]) and torch.equal(dh[others], clean[1][others])
