@@ -294,7 +294,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) ce_few_logits_kernel(const Few
         const float l = fmul(acc[i], kL2e);
         const float up = fmaxf(top[i], l);
         if (up != -INFINITY) {
-          const float old = top[i] == -INFINITY ? 0.0f : fmul(sum[i], exp2f(fsub(top[i], up)));
+          // (a sum without a largest value is 0, or NaN where a NaN logit came first)
+          const float old = top[i] == -INFINITY ? sum[i] : fmul(sum[i], exp2f(fsub(top[i], up)));
           // one rounding in the exponent, as in the loss
           sum[i] = fadd(old, exp2f(__fmaf_rn(acc[i], kL2e, -up)));
           top[i] = up;

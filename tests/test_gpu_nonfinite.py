@@ -64,3 +64,16 @@ def test_nan_in_one_token(mpc, dtype, T):
     assert bool(dw.isnan().all())
     assert torch.equal(loss[others], clean_loss[others]) and torch.equal(lse[others], clean_lse[others])
     assert torch.equal(tloss[others], clean[0][others]) and torch.equal(dh[others], clean[1][others])
+
+
+@TYPES
+@pytest.mark.parametrize("T", [1, 2, 4, 8, 16, 32])
+@pytest.mark.parametrize("V,row", [(50257, 0), (50257, 25000), (50257, 50256), (40, 3), (129, 128)])
+def test_nan_in_w_reaches_every_loss_of_a_few_tokens(mpc, dtype, T, V, row):
+    """The same for a few tokens, where a thread goes on to other rows of w after the NaN."""
+    h, w, y = inputs(T, 40, V, dtype, ignored=0.0)
+    w[row] = NAN
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    train = mpc.mpc_linear_ce_train(h, w, y)[0]
+    for x in (loss, lse, train):
+        assert bool(x.isnan().all())
