@@ -313,10 +313,12 @@ __device__ __forceinline__ float2 sum_parts(const float2* part, int parts, int T
 }
 
 // log(1 + s 2^-d): the loss of a token from the sum s of the others' exponentials
-// over a base (in base 2) that lies d under the target's logit.
-__device__ __forceinline__ float loss_of(float s, float d) {
+// over a base (in base 2) that lies d under the target's logit l.  Where l is +inf it is
+// inf - inf (an infinite d alone would make it 0).
+__device__ __forceinline__ float loss_of(float s, float d, float l) {
   const float ratio = fmul(s, exp2f(-d));
-  return ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kLn2);
+  const float loss = ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kLn2);
+  return l == INFINITY ? __int_as_float(0x7fffffff) : loss;
 }
 
 // Forward: lse and loss of the tokens that count.
@@ -331,9 +333,10 @@ __global__ void __launch_bounds__(1024)
   const int m = t;  // as a place in the list from here on
   const float2 r = sum_parts<true>(part, parts, T, m, n);
   if (threadIdx.x < 32 && m < n) {
-    const float l = at_target[m], v = loss_of(r.y, __fmaf_rn(l, kLog2e, -r.x));
+    const float l = at_target[m], v = loss_of(r.y, __fmaf_rn(l, kLog2e, -r.x), l);
     loss[row[m]] = v;
-    lse[row[m]] = fadd(l, v);
+    // of l + loss a target at -inf leaves nothing: that of the others; one at +inf is all of it
+    lse[row[m]] = l == -INFINITY ? fmul(fadd(log2f(r.y), r.x), kLn2) : l == INFINITY ? fadd(l, r.y) : fadd(l, v);
   }
 }
 
@@ -409,7 +412,7 @@ __global__ void __launch_bounds__(256) ce_scale_kernel(const Finish f) {
         for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
       }
       const float d = __fmaf_rn(f.at_target[m], kLog2e, -f.ref[m]);
-      loss = loss_of(s, d);
+      loss = loss_of(s, d, f.at_target[m]);
       scale = fdiv(g, fadd(s, exp2f(d)));
       if (lane == 0) {
         f.loss[t] = loss;

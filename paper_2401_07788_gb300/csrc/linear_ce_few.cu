@@ -351,8 +351,15 @@ __global__ void __launch_bounds__(kFewTokens * 32) ce_few_finish_kernel(const Fe
   for (int o = 16; o > 0; o >>= 1) s = fadd(s, __shfl_xor_sync(kFull, s, o));
   if (lane == 0) {
     const float l = f.at[t], d = __fmaf_rn(l, kL2e, -m), ratio = fmul(s, exp2f(-d));
-    const float loss = ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kL2);
-    f.lse[t] = live ? fadd(l, loss) : 0.0f;
+    float loss = ratio < 1e6f ? log1pf(ratio) : fmul(fsub(log2f(s), d), kL2);
+    float lse = fadd(l, loss);
+    if (l == INFINITY) {  // inf - inf (an infinite d alone would make it 0)
+      loss = __int_as_float(0x7fffffff);
+      lse = fadd(l, s);
+    } else if (l == -INFINITY) {  // of l + loss nothing is left: that of the others
+      lse = fmul(fadd(log2f(s), m), kL2);
+    }
+    f.lse[t] = live ? lse : 0.0f;
     if (f.loss != nullptr) f.loss[t] = live ? loss : 0.0f;
   }
 }

@@ -77,3 +77,35 @@ def test_nan_in_w_reaches_every_loss_of_a_few_tokens(mpc, dtype, T, V, row):
     train = mpc.mpc_linear_ce_train(h, w, y)[0]
     for x in (loss, lse, train):
         assert bool(x.isnan().all())
+
+
+@TYPES
+@pytest.mark.parametrize("T", [1, 16, 100, 600])
+def test_target_at_an_infinite_logit(mpc, dtype, T):
+    """A target's logit of +inf: lse is +inf and the loss, inf - inf, NaN, in the forward call as in training.
+    Of -inf: lse is that of the others and the loss +inf.  (An fp32 infinity of many tokens is NaN in the
+    planes of the matrix products: not finite either.)"""
+    h, w, y = inputs(T, 40, 700, dtype, ignored=0.0)
+    h[:, 0] = 1.0
+    y[:] = torch.arange(T, device="cuda") % 600
+    w[:, 0] = 0.0
+    others = w.clone()
+    at = int(y[T // 2])
+    mine = y == at
+    for value in (INF, -INF):
+        w[at, 0] = value
+        loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+        train = mpc.mpc_linear_ce_train(h, w, y)[0]
+        logits = h.double() @ others.double().t()
+        logits[:, at] = value
+        want = torch.logsumexp(logits, 1)
+        if dtype == torch.float32 and T > 32:
+            assert not bool(loss[mine].isfinite().any() | train[mine].isfinite().any() | lse[mine].isfinite().any())
+        elif value == INF:
+            assert bool(loss[mine].isnan().all()) and bool(train[mine].isnan().all())
+            assert bool((lse[mine] == INF).all())
+            assert not bool(loss.isfinite().any() | train.isfinite().any() | lse.isfinite().any())
+        else:
+            assert bool((loss[mine] == INF).all()) and bool((train[mine] == INF).all())
+            # products of 40 terms in fp32 and an exponentials' sum: as for finite logits, 2^-18 of 1 + |lse|
+            assert bool(((lse.double() - want).abs() <= 2.0 ** -18 * (1 + want.abs())).all())
