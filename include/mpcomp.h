@@ -394,7 +394,9 @@ typedef struct {
  *     consecutive entries of a tensor that share one fp32 scale s, the largest
  *     |m| (v) of the block: code c of m stands for sign(c) (c/127)^2 s, of v for
  *     (c/255)^4 s; the nearest one is taken (of v in the square root; a v > 0
- *     never gets code 0).  All-zero codes and scales are m = v = 0.
+ *     never gets code 0, unless the block's largest is below 2^-126: then all
+ *     codes are 0).  All-zero codes and scales are m = v = 0.  A block with a NaN
+ *     in m (or v) gets the scale NaN: every entry of it stands for NaN then.
  *   grad_norm  NULL, or a device fp32 (mpc_grad_norm): g is multiplied by
  *     min(1, max_norm / (*grad_norm + 1e-6)) first when max_norm > 0, and the
  *     step changes nothing when *grad_norm is not finite.

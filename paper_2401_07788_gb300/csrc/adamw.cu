@@ -14,7 +14,8 @@
 // the least non-zero sqrt(v) is sqrt(s)/65025.  The code is the nearest one, for
 // m in m/s and for v in sqrt(v/s) (what the step divides by); a v > 0 never gets
 // code 0, so that a small v cannot turn into a division by eps alone.  The step
-// itself uses the m and v of before the coding.
+// itself uses the m and v of before the coding.  No code stands for NaN: a block
+// that has one gets the scale NaN, and all of it stands for NaN from then on.
 //
 // What bounds it: memory.  fp32 states move 28 bytes an entry (p, m, v read and
 // written, g read).  The work is laid out over chunks of 2048 entries that never
@@ -243,6 +244,13 @@ __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d
   return __byte_perm(lo, hi, 0x5410);
 }
 
+// The larger one, NaN where either is (as its bits 0x7fffffff, which warp_max takes
+// for the largest).
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
 __device__ __forceinline__ float warp_max(float x) {  // x >= 0 or NaN
   return __uint_as_float(__reduce_max_sync(kFull, __float_as_uint(x)));
 }
@@ -317,8 +325,8 @@ __global__ void __launch_bounds__(kThreads)
         float tm = 0.0f, tv = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          tm = fmaxf(tm, fabsf(m[j]));
-          tv = fmaxf(tv, v[j]);
+          tm = max_nan(tm, fabsf(m[j]));
+          tv = max_nan(tv, v[j]);
         }
         tm = warp_max(tm);
         tv = warp_max(tv);

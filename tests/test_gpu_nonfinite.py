@@ -109,3 +109,34 @@ def test_target_at_an_infinite_logit(mpc, dtype, T):
             assert bool((loss[mine] == INF).all()) and bool((train[mine] == INF).all())
             # products of 40 terms in fp32 and an exponentials' sum: as for finite logits, 2^-18 of 1 + |lse|
             assert bool(((lse.double() - want).abs() <= 2.0 ** -18 * (1 + want.abs())).all())
+
+
+@pytest.mark.parametrize("gtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,first,last", [(300, 5, 6), (2048, 256, 512), (5000, 4999, 5000), (255, 0, 255)])
+@pytest.mark.parametrize("bad", [NAN, INF], ids=["nan", "inf"])
+def test_a_bad_gradient_shows_in_8_bit_states(mpc, gtype, n, first, last, bad):
+    """A gradient that is not finite, without a norm that would leave the step out: as with fp32 states, m and
+    v of its entries are not finite afterwards, nor after a further step with good gradients; a code has no
+    value for that, so it is its block of 256 that shows it.  Other blocks are as without it."""
+    def steps(value):
+        g = torch.full((n,), 1e-3, device="cuda", dtype=gtype)
+        g[first:last] = value
+        p = torch.zeros(n, device="cuda")
+        plan = mpc.AdamWPlan([p], [g], state_bits=8)
+        seen = []
+        for k in (1, 2):
+            mpc.mpc_adamw_step(plan, 1e-3, 0.9, 0.95, 1e-8, k)
+            m, v = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+            mpc.mpc_adamw_decode(plan, [m], [v])
+            seen.append((m, v))
+            g.fill_(1e-3)
+        return p, seen
+
+    (p, seen), (clean_p, clean) = steps(bad), steps(1e-3)
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    hit[first // 256 * 256:-(-last // 256) * 256] = True
+    for (m, v), (clean_m, clean_v) in zip(seen, clean):
+        for x, c in ((m, clean_m), (v, clean_v)):
+            assert not bool(x[first:last].isfinite().any())
+            assert torch.equal(x[~hit], c[~hit])
+    assert not bool(p[first:last].isfinite().any()) and torch.equal(p[~hit], clean_p[~hit])
