@@ -29,6 +29,28 @@ BLOCK = 256  # entries of a tensor that share a scale in the 8-bit states
 # Linear cross entropy
 # ---------------------------------------------------------------------------------------
 
+class _Final(torch.autograd.Function):
+    """A gradient as it is, which raises where it is to be differentiated itself."""
+
+    @staticmethod
+    def forward(ctx, grad, *sources):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of linear_cross_entropy are not differentiable")
+
+
+def _final(grads, *sources):
+    """What a backward pass hands out.  Where autograd records it (create_graph), the gradients hang on
+    the tensors they come from by a node that refuses: as constants they would add nothing to a
+    second derivative.  (torch's once_differentiable does so only where the incoming gradient
+    requires one.)"""
+    if not torch.is_grad_enabled():
+        return grads
+    return tuple(_Final.apply(g, *sources) for g in grads)
+
+
 class _LinearCeFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, h, w, targets, ignore_index):
@@ -40,9 +62,9 @@ class _LinearCeFn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, gloss):
         h, w, targets, lse = ctx.saved_tensors
-        dh, dw = mpc_linear_ce_backward(h, w, targets, lse, gloss.contiguous().float(),
-                                        ctx.ignore_index)
-        return dh, dw, None, None
+        grads = mpc_linear_ce_backward(h, w, targets, lse, gloss.detach().contiguous().float(),
+                                       ctx.ignore_index)
+        return (*_final(grads, h, w, gloss), None, None)
 
 
 class _LinearCeMeanFn(torch.autograd.Function):
@@ -52,14 +74,16 @@ class _LinearCeMeanFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, h, w, targets, ignore_index):
         loss, dh, dw = mpc_linear_ce_train(h, w, targets, None, ignore_index)
-        ctx.save_for_backward(dh, dw)
+        ctx.save_for_backward(h, w, dh, dw)
         count = (targets != ignore_index).sum().clamp_min(1)
         return loss.sum() / count
 
     @staticmethod
     def backward(ctx, g):
-        dh, dw = ctx.saved_tensors
-        return dh * g.to(dh.dtype), dw * g.to(dw.dtype), None, None
+        h, w, dh, dw = ctx.saved_tensors
+        with torch.no_grad():
+            grads = dh * g.to(dh.dtype), dw * g.to(dw.dtype)
+        return (*_final(grads, h, w, g), None, None)
 
 
 def _rows_apart(t):
@@ -71,7 +95,7 @@ def _rows_apart(t):
 def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean"):
     """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
     ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
-    where the target is ``ignore_index``)."""
+    where the target is ``ignore_index``).  There is no second derivative: asking for one raises."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none")
     rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()

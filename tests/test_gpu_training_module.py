@@ -1,0 +1,44 @@
+"""The module and the optimizer as a training loop uses them: upstream factors, frozen operands, a second
+backward pass, memory, targets that are out of range, states that are replaced between steps."""
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mpc():
+    import __graft_entry__ as g
+
+    g.build()
+    import paper_2401_07788_gb300 as m
+
+    torch.cuda.set_device(0)
+    return m
+
+
+def inputs(T, D, V, dtype=torch.float32, ignored=0.2):
+    gen = torch.Generator(device="cuda").manual_seed(T + 7 * D + 13 * V)
+    dev = {"device": "cuda", "generator": gen}
+    w, h = torch.randn(V, D, **dev) / D ** 0.5, torch.randn(T, D, **dev)
+    y = torch.randint(0, V, (T,), **dev)
+    y[torch.randperm(T, **dev)[: int(ignored * T)]] = -100
+    return h.to(dtype), w.to(dtype), y
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+@pytest.mark.parametrize("of", ["h", "w", "factor"])
+def test_a_second_derivative_is_refused(mpc, reduction, of):
+    """Asking for it raises instead of adding nothing; gradients that are recorded but not differentiated are
+    the same as ever."""
+    h, w, y = inputs(50, 24, 90)
+    factor = torch.full((), 0.7, device="cuda")
+    {"h": h, "w": w, "factor": factor}[of].requires_grad_(True)
+    x = w if of == "w" else h.requires_grad_(True)
+    loss = mpc.linear_cross_entropy(h, w, y, reduction=reduction).sum() * factor
+    grad, = torch.autograd.grad(loss, x, create_graph=True)
+    plain, = torch.autograd.grad(mpc.linear_cross_entropy(h, w, y, reduction=reduction).sum() * factor.detach(), x)
+    assert torch.equal(grad, plain)
+    with pytest.raises(RuntimeError, match="not differentiable"):
+        grad.square().sum().backward()
