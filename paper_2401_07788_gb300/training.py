@@ -79,11 +79,12 @@ class _LinearCeMeanFn(torch.autograd.Function):
         return loss.sum() / count
 
     @staticmethod
-    def backward(ctx, g):
+    def backward(ctx, upstream):
         h, w, dh, dw = ctx.saved_tensors
-        with torch.no_grad():
-            grads = dh * g.to(dh.dtype), dw * g.to(dw.dtype)
-        return (*_final(grads, h, w, g), None, None)
+        # as a matrix and not a scalar, which would be rounded to the gradients' type first
+        g = upstream.detach().float().view(1, 1)
+        grads = tuple(torch.mul(x, g, out=torch.empty_like(x)) for x in (dh, dw))
+        return (*_final(grads, h, w, upstream), None, None)
 
 
 def _rows_apart(t):

@@ -42,3 +42,17 @@ def test_a_second_derivative_is_refused(mpc, reduction, of):
     assert torch.equal(grad, plain)
     with pytest.raises(RuntimeError, match="not differentiable"):
         grad.square().sum().backward()
+
+
+@pytest.mark.parametrize("T", [12, 500])
+@pytest.mark.parametrize("factor", [1.0, 1.0 / 3.0, 0.1, -7.0])
+def test_an_upstream_factor_is_not_rounded(mpc, T, factor):
+    """The gradient of a bf16 mean is that of the call times the fp32 factor, rounded once."""
+    h, w, y = inputs(T, 64, 300, torch.bfloat16)
+    _, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    h.requires_grad_(True)
+    w.requires_grad_(True)
+    (mpc.linear_cross_entropy(h, w, y) * factor).backward()
+    for got, plain in ((h.grad, dh), (w.grad, dw)):
+        assert got.dtype == torch.bfloat16
+        assert torch.equal(got, (plain.float() * factor).bfloat16())
