@@ -386,6 +386,22 @@ struct Finish {
   float* loss;
 };
 
+// A row of hidden states times `scale`, in planes (zero for one that is not listed).
+template <int P>
+__device__ __forceinline__ void scale_row(const Finish& f, int64_t m, int n, float scale) {
+  const int64_t plane = f.padded * f.Dp;
+  for (int d = static_cast<int>(threadIdx.x & 31) * 8; d < f.Dp; d += 256) {
+    uint16_t p[8][3] = {};
+    if (m < n) {
+      float x[8];
+      load_planes8<P>(f.hp + m * f.Dp + d, plane, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) split(fmul(x[j], scale), p[j]);
+    }
+    store_planes8<P>(f.hs + m * f.Dp + d, plane, p);
+  }
+}
+
 // Training: the target's coefficients and the order by target, and where the
 // exponentials are kept the loss, the factors and the scaled hidden states; one
 // warp a row.
@@ -427,18 +443,33 @@ __global__ void __launch_bounds__(256) ce_scale_kernel(const Finish f) {
       f.sorted[f.pos[m]] = f.target[m];
     }
   }
-  if (f.hs == nullptr) return;
-  const int64_t plane = f.padded * f.Dp;
-  for (int d = lane * 8; d < f.Dp; d += 256) {
-    uint16_t p[8][3] = {};
-    if (m < n) {
-      float x[8];
-      load_planes8<P>(f.hp + m * f.Dp + d, plane, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) split(fmul(x[j], scale), p[j]);
+  if (f.hs != nullptr) scale_row<P>(f, m, n, scale);
+}
+
+// A gradient from lse whose coefficients are taken over g (1 - p): 1 / (1 - p), the
+// factor, and the scaled hidden states; one warp a row.  1 - p comes from the loss (of
+// the forward pass, or lse less the target's logit).  Where p is 1 to the last digit
+// any small 1 - p serves: the factor takes it back from the other coefficients.
+template <int P>
+__global__ void __launch_bounds__(256) ce_over_kernel(const Finish f) {
+  pdl_begin();
+  pdl_end();
+  const int n = f.head->valid, lane = threadIdx.x & 31;
+  const int64_t m = blockIdx.x * int64_t{8} + (threadIdx.x >> 5);
+  if (m >= rows_touched(n)) return;
+  float scale = 0.0f;
+  if (m < n) {
+    const int t = f.row[m];
+    const float loss = f.loss_in != nullptr ? f.loss_in[t] : __fmaf_rn(f.ref[m], -kLn2, f.lse[t]);
+    float q = -expm1f(-loss);
+    if (q < 0x1p-60f) q = 0x1p-60f;
+    scale = fmul(f.gloss != nullptr ? f.gloss[t] : f.head->mean, q);
+    if (lane == 0) {
+      f.scale[m] = scale;
+      f.coef[m] = fdiv(1.0f, q);
     }
-    store_planes8<P>(f.hs + m * f.Dp + d, plane, p);
   }
+  scale_row<P>(f, m, n, scale);
 }
 
 // Target gradients: a CTA takes kRun tokens in the order by target and sums
@@ -538,12 +569,17 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = fadd(x[j], v[j]);
       }
+      if (scale != nullptr) {
+        const float s = scale[m];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fmul(x[j], s);
+      }
       if (coef != nullptr) {
-        const float s = scale != nullptr ? scale[m] : 1.0f, c = coef[m];
+        const float c = coef[m];
         E y[8];
         load8(w + target[m] * ldw + d, D - d, wide_w, y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __fmaf_rn(c, to_float(y[j]), fmul(x[j], s));
+        for (int j = 0; j < 8; ++j) x[j] = __fmaf_rn(c, to_float(y[j]), x[j]);
       }
     }
     E out[8];
@@ -627,7 +663,7 @@ struct Layout {
   size_t head, row, target, place, at_target, part, lse, h, w, coef, sum, dw_sum, total;
   size_t flags, pos, order, sorted, ref, sums, scale, factor, hs, seg_first, seg_end, seg_sum;  // kept
   int parts, planes, tiles;
-  bool pack_w, kept, apart;
+  bool pack_w, kept, apart, over;
   int64_t piece, padded, Dp, ldc;
 };
 
@@ -712,10 +748,13 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piec
   l.dw_sum = take(dw.splits > 1 ? static_cast<size_t>(dw.splits) * l.piece * l.Dp * 4 : 0);
   l.sum = take(static_cast<size_t>(plan_dh(T, D, l.piece, l.planes).splits) * l.padded * l.Dp * 4);
   l.apart = !l.kept && bf16 && T <= kPair;
+  l.over = !l.kept && bf16 && T > kPair;
+  if (l.kept || l.over) l.hs = take(static_cast<size_t>(l.planes) * l.padded * l.Dp * 2);
+  if (l.over)
+    for (size_t* p : {&l.ref, &l.scale, &l.factor}) *p = take(T * 4);
   if (l.kept || l.apart) {
     l.flags = take(round_up(l.tiles, kScan / kPair) * 4);
     for (size_t* p : {&l.pos, &l.order, &l.sorted, &l.ref, &l.sums, &l.scale, &l.factor}) *p = take(T * 4);
-    l.hs = take(l.kept ? static_cast<size_t>(l.planes) * l.padded * l.Dp * 2 : 0);
     l.seg_first = take(V * 4);
     l.seg_end = take(V * 4);
     l.seg_sum = take(static_cast<size_t>(T) * l.Dp * 4);
@@ -803,7 +842,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
                        a.targets, T, a.V, a.ignore, head, row, target, place, by_target ? ints(l.pos) : nullptr,
                        l.kept ? ints(l.flags) : nullptr, a.status));
   Prepare<E> pre = {head, h, w, a.ldh, a.ldw, a.V, l.padded, D, Dp, wide_h, wide_w, row, target, hp, wp,
-                    by_target ? floats(l.ref) : nullptr, by_target ? ints(l.pos) : nullptr, rows8, 0, 0, 0};
+                    by_target || (l.over && a.loss == nullptr) ? floats(l.ref) : nullptr, by_target ? ints(l.pos) : nullptr, rows8, 0, 0, 0};
   if (l.pack_w)
     pre.w_blocks = static_cast<unsigned>(std::min<int64_t>((a.V * (Dp / 8) + 255) / 256, int64_t{num_sms} * 16));
   if (by_target) {
@@ -940,8 +979,18 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     f.loss_in = a.loss;
     CE_TRY(by_targets());
   }
+  const uint16_t* h_dw = hp;
+  if (l.over) {
+    uint16_t* hs = reinterpret_cast<uint16_t*>(ws + l.hs);
+    f.hs = hs;
+    f.lse = lse;
+    f.loss_in = a.loss;
+    CE_TRY(launch_kernel(ce_over_kernel<P>, dim3(rows8), dim3(256), 0, s, 0, f));
+    g.over = factor;
+    h_dw = hs;
+  }
   g.splits = dh_plan.splits;
-  CE_TRY(make_map(&h_cols, hp, D, l.padded, P, l.Dp, hplane, kK));
+  CE_TRY(make_map(&h_cols, h_dw, D, l.padded, P, l.Dp, hplane, kK));
   for (int64_t v0 = 0; v0 < a.V; v0 += l.piece) {
     const int width = static_cast<int>(std::min(l.piece, a.V - v0));
     g.v0 = v0;
@@ -958,7 +1007,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     CE_TRY(launch_gemm<kDh, P>(c_rows, w_cols, w_cols, g, a.T, a.D, num_sms, s));
     CE_TRY(dw_of_piece(c_cols, h_cols));
   }
-  return dh_out(nullptr, l.apart ? factor : nullptr);
+  return dh_out(l.over ? scale : nullptr, l.apart ? factor : nullptr);
 }
 
 }  // namespace

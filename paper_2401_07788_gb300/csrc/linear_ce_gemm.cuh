@@ -74,7 +74,14 @@ __device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
 //         a flag, take their largest logit as ref, and a second launch of the kernel
 //         (which returns at once without a flag) forms their row tiles again.
 // kCoef   the logits' products again, when lse is known: the coefficients c of a
-//         piece of the vocabulary, rounded to bf16 planes.
+//         piece of the vocabulary, rounded to bf16 planes.  In bf16 the target's c,
+//         g (p - 1), is no entry to be rounded: it is a sum's largest term for most
+//         tokens, and where p is small the c of all tokens lie side by side, off in
+//         the same direction by up to 2^-8 (0.05 % of dh and dw at 600 x 64 x 300).
+//         Up to 256 tokens it goes its own way in fp32 (`apart`); beyond, a token's
+//         coefficients are taken over g (1 - p) (`over`): -1 for the target, and the
+//         factor is applied in fp32 to dh's sums and, with one rounding an element,
+//         to h for dw.
 // kDh     A = c [valid][piece], B = w^T [D][piece]: dh, K split over several CTAs
 //         where there are few tiles, each split's sum kept in fp32.
 // kDw     A = c^T [piece][valid], B = h^T [D][valid]: dw of the piece, or as for dh
@@ -120,6 +127,7 @@ struct Gemm {
   const float* gloss;   // kCoef: [T] by token, or nullptr for the mean
   const float* loss;    // kCoef: [T] by token where the forward pass gave it, or nullptr
   int apart;            // kCoef: the target's c goes its own way in fp32
+  const float* over;    // kCoef: nullptr, or [T] 1 / (1 - p): c over g (1 - p)
   float* sum;           // kDh, kDw in parts (else nullptr): [split][rows][lds]
   int64_t lds, sum_split;
   void* dw;             // kDw
@@ -364,7 +372,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
     if (live) {
       const int token = g.row[m];
       const float lse = g.lse[token];
-      const float weight = g.gloss != nullptr ? g.gloss[token] : g.head->mean;
+      const float weight = g.over != nullptr ? g.over[m] : g.gloss != nullptr ? g.gloss[token] : g.head->mean;
       // what the rounding of lse log2e leaves out goes into the factor
       shift = fmul(lse, -kLog2e);
       scale = fmul(weight, exp2f(-__fmaf_rn(lse, kLog2e, shift)));
@@ -373,7 +381,7 @@ __device__ __forceinline__ void epilogue(const Gemm& g, int valid, const Tile& t
         float v = x[0];
 #pragma unroll
         for (int j = 1; j < kHalf; ++j) v = j == y ? x[j] : v;
-        at_y = fmul(weight, expm1f(g.loss != nullptr ? -g.loss[token] : fsub(v, lse)));
+        at_y = g.over != nullptr ? -1.0f : fmul(weight, expm1f(g.loss != nullptr ? -g.loss[token] : fsub(v, lse)));
       }
     }
 #pragma unroll

@@ -56,3 +56,18 @@ def test_an_upstream_factor_is_not_rounded(mpc, T, factor):
     for got, plain in ((h.grad, dh), (w.grad, dw)):
         assert got.dtype == torch.bfloat16
         assert torch.equal(got, (plain.float() * factor).bfloat16())
+
+
+def test_mean_and_sum_agree_in_bf16(mpc):
+    """The mean's gradient with a factor against the sum's with the factor over the count, in 64 bits: a factor
+    that were rounded to bf16 would be off by up to 2^-9 in all entries alike, a mean of rounding errors of
+    2^-8 each over n entries stays below 2^-8 * 6 / sqrt(n)."""
+    h, w, y = inputs(600, 64, 300, torch.bfloat16)
+    grads = []
+    for reduction, factor in (("mean", 1.0 / 3.0), ("sum", 1.0 / 3.0 / int((y != -100).sum()))):
+        a, b = h.clone().requires_grad_(True), w.clone().requires_grad_(True)
+        (mpc.linear_cross_entropy(a, b, y, reduction=reduction) * factor).backward()
+        grads.append((a.grad.double(), b.grad.double()))
+    for x, z in zip(*grads):
+        ratio = float((x * z).sum() / (z * z).sum())
+        assert abs(ratio - 1.0) < 2.0 ** -8 * 6 / x.numel() ** 0.5
