@@ -878,16 +878,16 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
   g.lddw = a.lddw;
   g.dw_bf16 = bf16;
   g.dw_wide = (a.lddw * sizeof(E)) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 32 == 0;
-  // K blocks of an accumulator (4 truncating steps each in bf16, 24 in fp32; about
-  // 1.4e-8 of a result a step).  fp32: two, 48 steps (four measured 3 to 8 % faster
-  // and 1.3e-6 off, more than an fp32 sum).  bf16 logits, whose loss is fp32: equal
-  // chunks of up to 12, and 2 for few tokens, where the products wait for memory
-  // anyway.  bf16 gradients: any number (8192 keep an accumulator's wait far below
-  // the default limit of a wait).
-  const int any = 8192, exact = 2;
+  // K blocks of an accumulator (4 truncating steps each in bf16, 24 in fp32; see
+  // linear_ce_gemm.cuh).  fp32: two, 48 steps (four measured 3 to 8 % faster and
+  // 1.3e-6 off, more than an fp32 sum).  bf16 logits, whose loss is fp32: equal chunks
+  // of up to 12, and 2 for few tokens, where the products wait for memory anyway.
+  // bf16 gradients: 128, which costs nothing that shows.  (Without a limit dh over 262144
+  // entries whose first were the largest was 3.3e-4 too small, over 131072 1.2e-4.)
+  const int many = 128, exact = 2;
   const int64_t parts = (d_blocks + 11) / 12;
   const int logits = !bf16 || a.T <= kPair ? exact : static_cast<int>((d_blocks + parts - 1) / parts);
-  const int gradients = bf16 ? any : exact;
+  const int gradients = bf16 ? many : exact;
   const Plan dh_plan = pass == kForward ? Plan{kN, 1} : plan_dh(a.T, a.D, l.piece, P);
   const Plan dw_plan = pass == kForward ? Plan{kN, 1} : plan_dw(a.T, a.D, l.piece, P);
   const int wide_dw = on16(a.dw) && a.lddw * sizeof(E) % 16 == 0;
@@ -999,7 +999,7 @@ cudaError_t run(const LinearCeArgs& a, int num_sms, cudaStream_t s) {
     CE_TRY(make_map(&c_rows, coef, width, l.padded, P, l.ldc, coef_plane, kM));
     CE_TRY(make_map(&c_cols, coef, width, l.padded, P, l.ldc, coef_plane, kK));
     CE_TRY(make_map(&c_out, coef, width, l.padded, P, l.ldc, coef_plane, 32));
-    g.chunk = bf16 ? any : logits;
+    g.chunk = bf16 ? many : logits;
     g.tile_n = logits_n;
     CE_TRY(launch_gemm<kCoef, P>(h_rows, w_rows, c_out, g, a.T, width, num_sms, s));
     g.chunk = gradients;
