@@ -46,9 +46,7 @@ def _final(grads, *sources):
     the tensors they come from by a node that refuses: as constants they would add nothing to a
     second derivative.  (torch's once_differentiable does so only where the incoming gradient
     requires one.)"""
-    if not torch.is_grad_enabled():
-        return grads
-    return tuple(_Final.apply(g, *sources) for g in grads)
+    return tuple(None if g is None else _Final.apply(g, *sources) for g in grads)
 
 
 class _LinearCeFn(torch.autograd.Function):
@@ -64,27 +62,43 @@ class _LinearCeFn(torch.autograd.Function):
         h, w, targets, lse = ctx.saved_tensors
         grads = mpc_linear_ce_backward(h, w, targets, lse, gloss.detach().contiguous().float(),
                                        ctx.ignore_index)
-        return (*_final(grads, h, w, gloss), None, None)
+        grads = [g if need else None for g, need in zip(grads, ctx.needs_input_grad)]
+        if torch.is_grad_enabled():
+            grads = _final(grads, h, w, gloss)
+        return (*grads, None, None)
 
 
 class _LinearCeMeanFn(torch.autograd.Function):
     """The mean: its gradient is known up to one factor when the loss is formed, so both come from
-    one call and the backward pass only applies the factor."""
+    one call, and the backward pass applies the factor to what that call made and hands it out.
+    A further pass through a graph that is kept makes it again."""
+
+    @staticmethod
+    def _made(ctx, h, w, targets):
+        loss, *grads = mpc_linear_ce_train(h, w, targets, None, ctx.ignore_index)
+        return loss, [g if need else None for g, need in zip(grads, ctx.needs_input_grad)]
 
     @staticmethod
     def forward(ctx, h, w, targets, ignore_index):
-        loss, dh, dw = mpc_linear_ce_train(h, w, targets, None, ignore_index)
-        ctx.save_for_backward(h, w, dh, dw)
+        ctx.ignore_index = ignore_index
+        loss, ctx.grads = _LinearCeMeanFn._made(ctx, h, w, targets)
+        ctx.save_for_backward(h, w, targets)
         count = (targets != ignore_index).sum().clamp_min(1)
         return loss.sum() / count
 
     @staticmethod
     def backward(ctx, upstream):
-        h, w, dh, dw = ctx.saved_tensors
+        grads, ctx.grads = ctx.grads, None
+        if grads is None:
+            _, grads = _LinearCeMeanFn._made(ctx, *ctx.saved_tensors)
         # as a matrix and not a scalar, which would be rounded to the gradients' type first
         g = upstream.detach().float().view(1, 1)
-        grads = tuple(torch.mul(x, g, out=torch.empty_like(x)) for x in (dh, dw))
-        return (*_final(grads, h, w, upstream), None, None)
+        grads = [None if x is None or not need else torch.mul(x, g, out=x)
+                 for x, need in zip(grads, ctx.needs_input_grad)]
+        if torch.is_grad_enabled():
+            h, w, _ = ctx.saved_tensors
+            grads = _final(grads, h, w, upstream)
+        return (*grads, None, None)
 
 
 def _rows_apart(t):

@@ -71,3 +71,50 @@ def test_mean_and_sum_agree_in_bf16(mpc):
     for x, z in zip(*grads):
         ratio = float((x * z).sum() / (z * z).sum())
         assert abs(ratio - 1.0) < 2.0 ** -8 * 6 / x.numel() ** 0.5
+
+
+def test_one_gradient_of_the_weight(mpc):
+    """The backward pass hands out the gradients that the forward call made: no second dw."""
+    h, w, y = inputs(300, 256, 50000)
+    h.requires_grad_(True)
+    w.requires_grad_(True)
+    loss = mpc.linear_cross_entropy(h, w, y)
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    loss.backward()
+    assert torch.cuda.max_memory_allocated() - before < w.numel() * 4 // 2
+    assert torch.cuda.memory_allocated() - before < w.numel() * 4 // 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_a_graph_that_is_kept(mpc, dtype):
+    """Two backward passes through one graph, with factors of their own, whatever became of the first one's
+    gradients."""
+    h, w, y = inputs(300, 40, 500, dtype)
+    _, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    h.requires_grad_(True)
+    w.requires_grad_(True)
+    loss = mpc.linear_cross_entropy(h, w, y)
+    for factor in (0.3, 1.0 / 7.0, 1.0):
+        got = torch.autograd.grad(loss, (h, w), torch.full((), factor, device="cuda"), retain_graph=True)
+        for x, plain in zip(got, (dh, dw)):
+            assert torch.equal(x, (plain.float() * torch.full((), factor, device="cuda")).to(dtype))
+            x.fill_(float("nan"))
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+def test_frozen_operands(mpc, reduction):
+    """Only what requires a gradient gets one, the same as if both did; a frozen weight's is not kept."""
+    h, w, y = inputs(300, 64, 20000)
+    a, b = h.clone().requires_grad_(True), w.clone().requires_grad_(True)
+    mpc.linear_cross_entropy(a, b, y, reduction=reduction).sum().backward()
+    x = h.clone().requires_grad_(True)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    loss = mpc.linear_cross_entropy(x, w, y, reduction=reduction).sum()
+    assert torch.cuda.memory_allocated() - before < w.numel() * 4 // 2
+    loss.backward()
+    assert torch.equal(x.grad, a.grad) and w.grad is None
+    v = w.clone().requires_grad_(True)
+    mpc.linear_cross_entropy(h, v, y, reduction=reduction).sum().backward()
+    assert torch.equal(v.grad, b.grad) and h.grad is None
