@@ -41,6 +41,13 @@ class _Final(torch.autograd.Function):
         raise RuntimeError("the gradients of linear_cross_entropy are not differentiable")
 
 
+def _mean(loss, targets, ignore_index, vocab):
+    """The mean over the tokens that count, as the kernels take it for the gradient: those whose target is
+    in the vocabulary and is not ignore_index."""
+    counts = (targets == targets.clamp(0, vocab - 1)) & (targets != ignore_index)
+    return loss.sum() / counts.sum().clamp_min(1)
+
+
 def _final(grads, *sources):
     """What a backward pass hands out.  Where autograd records it (create_graph), the gradients hang on
     the tensors they come from by a node that refuses: as constants they would add nothing to a
@@ -83,8 +90,7 @@ class _LinearCeMeanFn(torch.autograd.Function):
         ctx.ignore_index = ignore_index
         loss, ctx.grads = _LinearCeMeanFn._made(ctx, h, w, targets)
         ctx.save_for_backward(h, w, targets)
-        count = (targets != ignore_index).sum().clamp_min(1)
-        return loss.sum() / count
+        return _mean(loss, targets, ignore_index, w.shape[0])
 
     @staticmethod
     def backward(ctx, upstream):
@@ -110,7 +116,8 @@ def _rows_apart(t):
 def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean"):
     """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
     ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
-    where the target is ``ignore_index``).  There is no second derivative: asking for one raises."""
+    where the target is ``ignore_index``).  A target outside [0, V) does not count either, and is reported
+    by ``mpc_get_status``.  There is no second derivative: asking for one raises."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none")
     rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()
@@ -120,7 +127,7 @@ def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str
         if grad:
             return _LinearCeMeanFn.apply(rows, w, y, ignore_index)
         loss = mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
-        return loss.sum() / (y != ignore_index).sum().clamp_min(1)
+        return _mean(loss, y, ignore_index, w.shape[0])
     loss = _LinearCeFn.apply(rows, w, y, ignore_index) if grad else \
         mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
     return loss.sum() if reduction == "sum" else loss.reshape(targets.shape)

@@ -118,3 +118,33 @@ def test_frozen_operands(mpc, reduction):
     v = w.clone().requires_grad_(True)
     mpc.linear_cross_entropy(h, v, y, reduction=reduction).sum().backward()
     assert torch.equal(v.grad, b.grad) and h.grad is None
+
+
+def test_mean_of_targets_out_of_range(mpc):
+    """A target outside the vocabulary does not count: not in the loss, nor in the number that it is divided
+    by, with and without gradients."""
+    V = 90
+    h, w, y = inputs(50, 24, V)
+    y[:4] = torch.tensor([V, -1, 1 << 40, -(1 << 40)], device="cuda")
+    counts = (y >= 0) & (y < V)
+    loss = mpc.mpc_linear_ce_forward(h, w, y)[0]
+    want = float(loss.double().sum() / counts.sum())
+    masked = torch.where(counts, y, torch.full_like(y, -100))
+    _, dh, dw = mpc.mpc_linear_ce_train(h, w, masked)
+    with torch.no_grad():
+        plain = mpc.linear_cross_entropy(h, w, y)
+    h.requires_grad_(True)
+    w.requires_grad_(True)
+    loss = mpc.linear_cross_entropy(h, w, y)
+    loss.backward()
+    assert mpc.mpc_get_status() == 6
+    assert torch.equal(h.grad, dh) and torch.equal(w.grad, dw)
+    # a sum of 36 losses in fp32 and a quotient
+    assert abs(float(plain) - want) <= 2.0 ** -20 * want and abs(float(loss.detach()) - want) <= 2.0 ** -20 * want
+
+
+def test_mean_where_the_ignored_index_is_in_the_vocabulary(mpc):
+    h, w, y = inputs(50, 24, 90, ignored=0.0)
+    y[::3] = 5
+    want = torch.nn.functional.cross_entropy(h.double() @ w.double().t(), y, ignore_index=5)
+    assert abs(float(mpc.linear_cross_entropy(h, w, y, ignore_index=5)) - float(want)) < 1e-5 * float(want)
