@@ -13,11 +13,13 @@ the vocabulary, and the optimiser step that every stage makes after its backward
 from __future__ import annotations
 
 import ctypes
+import itertools
+import operator
 
 import numpy as np
 import torch
 
-from . import (MpcError, _dtype, _vectors, mpc_adamw_step, mpc_grad_norm,
+from . import (MpcError, _data_ptr, _dtype, _numel, _vectors, mpc_adamw_step, mpc_grad_norm,
                mpc_linear_ce_backward, mpc_linear_ce_forward, mpc_linear_ce_train)
 
 __all__ = ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
@@ -298,33 +300,43 @@ class AdamW(torch.optim.Optimizer):
                 loss = closure()
         lists = {}
         for group in self.param_groups:
+            betas, eps = tuple(group["betas"]), group["eps"]
+            rate = float(group["lr"]), float(group["weight_decay"])
             for p in group["params"]:
-                if p.grad is None:
+                g = p.grad
+                if g is None:
                     continue
-                if p.grad.is_sparse:
+                if g.is_sparse:
                     raise MpcError(1, "sparse gradients are not supported")
                 s = self._state(p)
                 s["step"] += 1
-                key = (p.dtype, p.grad.dtype, p.device, s["step"], tuple(group["betas"]), group["eps"])
-                lists.setdefault(key, []).append((p, s, group))
+                key = (p.dtype, g.dtype, p.device, s["step"], betas, eps)
+                lists.setdefault(key, []).append((p, g, s, rate))
         plans = []
         for key, entries in lists.items():
-            ident = (key[0], key[1], key[2], tuple(id(p) for p, _, _ in entries))
+            params, grads, states, rates = map(list, zip(*entries))
+            ident = (*key[:3], *map(id, params))
             plan = self._plans.get(ident)
-            grads = [p.grad.contiguous() for p, _, _ in entries]
-            if plan is None or any(a.data_ptr() != p.data_ptr() for a, (p, _, _) in zip(plan.params, entries)):
-                low = self.state_bits == 8
-                plan = AdamWPlan([p.detach() for p, _, _ in entries], grads,
-                                 [s["exp_avg"] for _, s, _ in entries],
-                                 [s["exp_avg_sq"] for _, s, _ in entries],
-                                 [s["scale_m"] for _, s, _ in entries] if low else None,
-                                 [s["scale_v"] for _, s, _ in entries] if low else None,
-                                 [self.copies.get(p) for p, _, _ in entries])
+            grads = [g.contiguous() for g in grads]
+            # a plan serves again while it is about the very tensors that the optimizer holds now
+            names = ("exp_avg", "exp_avg_sq", "scale_m", "scale_v")[: 4 if self.state_bits == 8 else 2]
+            m, v, *scales = ([s[name] for s in states] for name in names)
+            copies = [self.copies.get(p) for p in params] if self.copies else None
+            held = [*params, *m, *v, *itertools.chain(*scales)]
+            places = [*map(_numel, params), *map(_data_ptr, held)]
+            if copies is not None:
+                held += copies
+                places += [None if t is None else _data_ptr(t) for t in copies]
+            if (plan is None or plan.places != places or len(plan.held) != len(held)
+                    or not all(map(operator.is_, plan.held, held))):
+                plan = AdamWPlan([p.detach() for p in params], grads, m, v, *(scales or (None, None)), copies)
+                plan.held, plan.places, plan.rates = held, places, None
                 self._plans[ident] = plan
             else:
                 plan.set_grads(grads)
-            plan.set_groups([group["lr"] for _, _, group in entries],
-                            [group["weight_decay"] for _, _, group in entries])
+            if plan.rates != rates:
+                plan.set_groups(*zip(*rates))
+                plan.rates = rates
             plans.append((key, plan))
         norm = None
         if self.max_norm > 0.0 and plans:

@@ -148,3 +148,93 @@ def test_mean_where_the_ignored_index_is_in_the_vocabulary(mpc):
     y[::3] = 5
     want = torch.nn.functional.cross_entropy(h.double() @ w.double().t(), y, ignore_index=5)
     assert abs(float(mpc.linear_cross_entropy(h, w, y, ignore_index=5)) - float(want)) < 1e-5 * float(want)
+
+
+def optimizer(mpc, made, bits, **options):
+    ps = [torch.nn.Parameter(x.clone()) for x in made]
+    return ps, mpc.AdamW(ps, lr=1e-2, betas=(0.9, 0.95), state_bits=bits, **options)
+
+
+def advance(ps, opt, grads):
+    for p, g in zip(ps, grads):
+        p.grad = g.clone()
+    opt.step()
+
+
+def same_states(a, pa, b, pb):
+    for p, q in zip(pa, pb):
+        assert torch.equal(p, q)
+        assert a.state[p].keys() == b.state[q].keys()
+        for k, x in a.state[p].items():
+            assert torch.equal(x, b.state[q][k]) if isinstance(x, torch.Tensor) else x == b.state[q][k], k
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("change", ["cleared", "replaced", "exchanged"])
+def test_states_that_are_replaced_between_steps(mpc, bits, change):
+    """A step uses the states that the optimizer holds then, wherever they came from since the last one."""
+    torch.manual_seed(1)
+    made = [torch.randn(300, device="cuda"), torch.randn(40, 30, device="cuda")]
+    grads = [torch.randn_like(x) for x in made]
+    ps, opt = optimizer(mpc, made, bits)
+    advance(ps, opt, grads)
+    advance(ps, opt, grads)
+    qs, other = optimizer(mpc, [p.detach() for p in ps], bits)
+    if change == "cleared":
+        opt.state.clear()
+    else:
+        names = [k for k, x in opt.state[ps[0]].items() if isinstance(x, torch.Tensor)]
+        for p, q in zip(ps, qs):
+            other.state[q] = {k: x.clone() if k in names else x for k, x in opt.state[p].items()}
+        if change == "replaced":  # one tensor of each, by zeros
+            for name in names:
+                opt.state[ps[1]][name] = torch.zeros_like(opt.state[ps[1]][name])
+                other.state[qs[1]][name].zero_()
+        else:  # the same tensors' memory, by new ones
+            for p in ps:
+                for name in names:
+                    opt.state[p][name].data = opt.state[p][name].clone()
+    for _ in range(2):
+        advance(ps, opt, grads)
+        advance(qs, other, grads)
+    same_states(opt, ps, other, qs)
+
+
+def test_copies_that_are_replaced_between_steps(mpc):
+    torch.manual_seed(2)
+    made = [torch.randn(300, device="cuda")]
+    grads = [torch.randn_like(x) for x in made]
+    ps, opt = optimizer(mpc, made, 32)
+    advance(ps, opt, grads)
+    for _ in range(2):  # a copy where there was none, then another one
+        opt.copies[ps[0]] = torch.zeros(300, dtype=torch.bfloat16, device="cuda")
+        old = opt.copies[ps[0]]
+        advance(ps, opt, grads)
+        assert torch.equal(old, ps[0].detach().bfloat16())
+    del opt.copies[ps[0]]
+    advance(ps, opt, grads)
+    assert not torch.equal(old, ps[0].detach().bfloat16())
+    ps[0].data = ps[0].detach()[:200].clone()
+    for k in ("exp_avg", "exp_avg_sq"):
+        opt.state[ps[0]][k] = opt.state[ps[0]][k][:200].clone()
+    before = ps[0].detach().clone()
+    advance(ps, opt, [grads[0][:200]])
+    assert not bool((ps[0].detach() == before).any())
+
+
+def test_rates_that_change_between_steps(mpc):
+    """lr and weight decay of the groups as they are at each step, numbers or a tensor changed in place."""
+    torch.manual_seed(4)
+    made, grads = [torch.randn(300, device="cuda")], [torch.randn(300, device="cuda")]
+    ps, opt = optimizer(mpc, made, 32)
+    qs, other = optimizer(mpc, made, 32)
+    rate = torch.full((), 1e-2)
+    opt.param_groups[0]["lr"] = rate
+    for lr, decay in ((1e-2, 0.0), (3e-3, 0.1), (0.0, 0.1), (1e-2, 0.5)):
+        rate.fill_(lr)
+        other.param_groups[0]["lr"] = float(rate)
+        opt.param_groups[0]["weight_decay"] = other.param_groups[0]["weight_decay"] = decay
+        before = ps[0].detach().clone()
+        advance(ps, opt, grads)
+        advance(qs, other, grads)
+        assert torch.equal(ps[0], qs[0]) and torch.equal(ps[0].detach(), before) == (lr == 0.0)
