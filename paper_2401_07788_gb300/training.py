@@ -237,6 +237,11 @@ class AdamWPlan:
         self._fill("grad", grads, torch.bfloat16 if self.grad_type else torch.float32, self.sizes)
         self.grads = grads
 
+    def drop_grads(self) -> None:
+        """Lets the gradient tensors go; calls are refused until set_grads gives others."""
+        self._columns["grad"] = 0
+        self.grads = None
+
     def set_groups(self, lr_scale, weight_decay) -> None:
         """The factor on lr and the weight decay from the next step on: one number or one for each
         tensor."""
@@ -253,7 +258,8 @@ class AdamW(torch.optim.Optimizer):
 
     ``state_bits``: 32, or 8 for states in blocks of 256 codes.  ``copies``: {param: bfloat16 tensor}
     that receives the param's new values, for a forward pass in bf16 from fp32 weights.
-    Parameters without a gradient are left alone, as are their states.
+    Parameters without a gradient are left alone, as are their states.  Nothing holds a gradient
+    after the step.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -312,7 +318,7 @@ class AdamW(torch.optim.Optimizer):
                 s["step"] += 1
                 key = (p.dtype, g.dtype, p.device, s["step"], betas, eps)
                 lists.setdefault(key, []).append((p, g, s, rate))
-        plans = []
+        plans, used = [], {}
         for key, entries in lists.items():
             params, grads, states, rates = map(list, zip(*entries))
             ident = (*key[:3], *map(id, params))
@@ -331,13 +337,14 @@ class AdamW(torch.optim.Optimizer):
                     or not all(map(operator.is_, plan.held, held))):
                 plan = AdamWPlan([p.detach() for p in params], grads, m, v, *(scales or (None, None)), copies)
                 plan.held, plan.places, plan.rates = held, places, None
-                self._plans[ident] = plan
             else:
                 plan.set_grads(grads)
             if plan.rates != rates:
                 plan.set_groups(*zip(*rates))
                 plan.rates = rates
             plans.append((key, plan))
+            used[ident] = plan
+        self._plans = used  # lists of other parameters' sets are let go
         norm = None
         if self.max_norm > 0.0 and plans:
             norms = []
@@ -353,4 +360,5 @@ class AdamW(torch.optim.Optimizer):
             with torch.cuda.device(device):
                 mpc_adamw_step(plan, 1.0, betas[0], betas[1], eps, step,
                                grad_norm=None if norm is None else norm.to(device), max_norm=self.max_norm)
+            plan.drop_grads()  # zero_grad() is to free them
         return loss

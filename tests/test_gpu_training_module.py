@@ -238,3 +238,60 @@ def test_rates_that_change_between_steps(mpc):
         advance(ps, opt, grads)
         advance(qs, other, grads)
         assert torch.equal(ps[0], qs[0]) and torch.equal(ps[0].detach(), before) == (lr == 0.0)
+
+
+@pytest.mark.parametrize("max_norm", [0.0, 1.0])
+def test_gradients_are_let_go(mpc, max_norm):
+    """After step() and zero_grad() nothing holds the gradients."""
+    ps, opt = optimizer(mpc, [torch.randn(4 << 20, device="cuda"), torch.randn(1000, 500, device="cuda").t().contiguous()],
+                        8, max_norm=max_norm)
+    bytes_of = sum(p.numel() * 4 for p in ps)
+    for layout in range(2):
+        for p in ps:
+            p.grad = torch.randn(p.shape, device="cuda")
+        if layout == 1:  # one that the step copies
+            ps[1].grad = torch.randn(1000, 500, device="cuda").t()
+        held = torch.cuda.memory_allocated()
+        opt.step()
+        opt.zero_grad()
+        assert torch.cuda.memory_allocated() <= held - bytes_of + (1 << 16) + sum(
+            x.numel() * x.element_size() for p in ps for x in opt.state[p].values() if isinstance(x, torch.Tensor)) * (layout == 0)
+
+
+def test_lists_of_changing_parameters(mpc):
+    """Any subset of the parameters may have gradients: results as with a step for each alone, and memory
+    that does not grow with the number of subsets seen."""
+    torch.manual_seed(3)
+    made = [torch.randn(50 + i, device="cuda") for i in range(6)]
+    ps, opt = optimizer(mpc, made, 32, max_norm=1e9)
+    singles = [optimizer(mpc, [x], 32, max_norm=1e9) for x in made]
+    sizes = []
+    for turn in range(2):
+        for subset in range(1, 64):
+            grads = [torch.randn_like(x) if subset >> i & 1 else None for i, x in enumerate(made)]
+            for p, g in zip(ps, grads):
+                p.grad = None if g is None else g.clone()
+            opt.step()
+            for (one, each), g in zip(singles, grads):
+                if g is not None:
+                    one[0].grad = g.clone()
+                    each.step()
+                    each.zero_grad()
+            opt.zero_grad()
+            del grads
+            sizes.append(torch.cuda.memory_allocated())
+    for p, (one, _) in zip(ps, singles):
+        assert torch.equal(p, one[0])
+    assert sizes[-1] - sizes[5] < 20 * 32768  # a plan's workspace is 32 KB
+
+
+def test_a_plan_without_gradients_is_refused(mpc):
+    p, g = torch.zeros(30, device="cuda"), torch.ones(30, device="cuda")
+    plan = mpc.AdamWPlan([p], [g])
+    plan.drop_grads()
+    for call in (lambda: mpc.mpc_adamw_step(plan, 1e-3, 0.9, 0.99, 1e-8, 1), lambda: mpc.mpc_grad_norm(plan)):
+        with pytest.raises(mpc.MpcError):
+            call()
+    plan.set_grads([g])
+    mpc.mpc_adamw_step(plan, 1e-3, 0.9, 0.99, 1e-8, 1)
+    assert bool((p < 0).all())
