@@ -134,11 +134,20 @@ def _stream(stream) -> ctypes.c_void_p:
     return _VP(s.cuda_stream)
 
 
-def _raw_stream(stream) -> int:
-    """The same as an integer, without making a stream object for the current one."""
+def _launch(call, device, stream, *args) -> None:
+    """call(*args, stream) on the device where the call's tensors are: the library launches on the current
+    device and takes its SM count and status word.  Without a stream on that device's current one."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    return stream.cuda_stream
+        raw = torch._C._cuda_getCurrentRawStream(device.index)
+    elif stream.device != device:
+        raise MpcError(1, "the stream is on %s, the tensors are on %s" % (stream.device, device))
+    else:
+        raw = stream.cuda_stream
+    if device.index == torch.cuda.current_device():
+        _check(call(*args, raw))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, raw))
 
 
 def _cuda(t: torch.Tensor, dtype: torch.dtype, name: str) -> torch.Tensor:
@@ -535,9 +544,8 @@ def mpc_linear_ce_forward(h, w, targets, ignore_index: int = -100, loss=None, ls
     T, D, V, ldh, ldw, ws, wsb = _linear_ce_args(h, w, targets, 0, 0, ws, stream)
     loss = _vector_or_new(loss, T, "loss", h.device, stream)
     lse = _vector_or_new(lse, T, "lse", h.device, stream)
-    _check(lib().mpc_linear_ce_forward(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), T, D, V,
-                                       _DTYPES[h.dtype], ignore_index, loss.data_ptr(), lse.data_ptr(),
-                                       _address(ws), wsb, _raw_stream(stream)))
+    _launch(lib().mpc_linear_ce_forward, h.device, stream, h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(),
+            T, D, V, _DTYPES[h.dtype], ignore_index, loss.data_ptr(), lse.data_ptr(), _address(ws), wsb)
     return loss, lse
 
 
@@ -565,10 +573,9 @@ def mpc_linear_ce_backward(h, w, targets, lse, gloss=None, ignore_index: int = -
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
     dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
-    _check(lib().mpc_linear_ce_backward(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), lse.data_ptr(),
-                                        _address(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece,
-                                        dh.data_ptr(), lddh, dw.data_ptr(), lddw, _address(ws), wsb,
-                                        _raw_stream(stream)))
+    _launch(lib().mpc_linear_ce_backward, h.device, stream, h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(),
+            lse.data_ptr(), _address(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece, dh.data_ptr(), lddh,
+            dw.data_ptr(), lddw, _address(ws), wsb)
     return dh, dw
 
 
@@ -581,9 +588,9 @@ def mpc_linear_ce_train(h, w, targets, gloss=None, ignore_index: int = -100, pie
     if gloss is not None:
         _vector(gloss, T, torch.float32, "gloss", h.device)
     dh, lddh, dw, lddw = _linear_ce_grads(h, w, dh, dw, stream)
-    _check(lib().mpc_linear_ce_train(h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(), _address(gloss), T, D,
-                                     V, _DTYPES[h.dtype], ignore_index, piece, loss.data_ptr(), dh.data_ptr(),
-                                     lddh, dw.data_ptr(), lddw, _address(ws), wsb, _raw_stream(stream)))
+    _launch(lib().mpc_linear_ce_train, h.device, stream, h.data_ptr(), ldh, w.data_ptr(), ldw, targets.data_ptr(),
+            _address(gloss), T, D, V, _DTYPES[h.dtype], ignore_index, piece, loss.data_ptr(), dh.data_ptr(), lddh,
+            dw.data_ptr(), lddw, _address(ws), wsb)
     return loss, dh, dw
 
 
@@ -599,9 +606,8 @@ def mpc_adamw_step(plan, lr: float, beta1: float, beta2: float, eps: float, step
     norm is not finite."""
     if grad_norm is not None:
         _vector(grad_norm, 1, torch.float32, "grad_norm", plan.device)
-    _check(lib().mpc_adamw_step(plan.table, plan.count, plan.param_type, plan.grad_type,
-                                plan.state_bits, lr, beta1, beta2, eps, step, _address(grad_norm),
-                                max_norm, _raw_stream(stream)))
+    _launch(lib().mpc_adamw_step, plan.device, stream, plan.table, plan.count, plan.param_type, plan.grad_type,
+            plan.state_bits, lr, beta1, beta2, eps, step, _address(grad_norm), max_norm)
 
 
 def mpc_adamw_decode(plan, m_out, v_out, stream=None):
@@ -611,8 +617,8 @@ def mpc_adamw_decode(plan, m_out, v_out, stream=None):
         raise MpcError(1, "the plan's states are not 8-bit codes")
     lists = [_vectors(outs, plan.sizes, torch.float32, name, plan.device)
              for name, outs in (("m_out", m_out), ("v_out", v_out))]
-    _check(lib().mpc_adamw_decode(plan.table, plan.count, lists[0].buffer_info()[0],
-                                  lists[1].buffer_info()[0], _raw_stream(stream)))
+    _launch(lib().mpc_adamw_decode, plan.device, stream, plan.table, plan.count, lists[0].buffer_info()[0],
+            lists[1].buffer_info()[0])
     return m_out, v_out
 
 
@@ -631,8 +637,8 @@ def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
         ws = plan.norm_ws
         _on(stream, ws)
     wsb = ws.numel() * ws.element_size()
-    _check(lib().mpc_grad_norm(plan.table, plan.count, plan.grad_type, norm.data_ptr(), _address(ws), wsb,
-                               _raw_stream(stream)))
+    _launch(lib().mpc_grad_norm, plan.device, stream, plan.table, plan.count, plan.grad_type, norm.data_ptr(),
+            _address(ws), wsb)
     return norm
 
 
@@ -641,7 +647,7 @@ def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
 # ---------------------------------------------------------------------------------------
 
 def mpc_get_status(stream=None) -> int:
-    """Synchronise the stream and return (and clear) the device status as a code."""
+    """Synchronise the stream and return (and clear) the current device's status as a code."""
     return int(lib().mpc_get_status(_stream(stream)))
 
 
