@@ -561,15 +561,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
       }
       // Copies in flight must land before either CTA leaves (the cluster barrier
-      // below).  The first CTA sees both CTAs' copies arrive; where a wait gave up,
-      // the second one may have sent some that the first no longer counts, and
-      // gives them a millisecond.
+      // below).  The first CTA's barriers count both CTAs' copies.  The second CTA knows
+      // its own by the products that read them, which have not been formed where the
+      // first one gave up: then it gives them a millisecond.
       if (rank == 0) {
         for (uint32_t i = it > stages ? it - stages : 0; i < it; ++i)
           mbar_wait_bounded(&full[i % stages], i / stages & 1, kDrainPolls, g.status);
-      } else if (!ok) {
-        const uint64_t until = global_ns() + 1000000;
-        while (global_ns() < until) __nanosleep(1000);
+      } else {
+        for (uint32_t i = it > stages ? it - stages : 0; i < it && ok; ++i)
+          ok = mbar_wait_bounded(&empty[i % stages], i / stages & 1, g.spin_limit, g.status);
+        if (!ok) {
+          const uint64_t until = global_ns() + 1000000;
+          while (global_ns() < until) __nanosleep(1000);
+        }
       }
     }
   } else if (warp == 1) {
@@ -611,10 +615,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (ok) mma_commit_pair(&done[n & 1]);
         }
       }
-      if (!ok) {  // products in flight must end before the tensor memory is given back
-        mma_commit(&drain);
-        mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
-      }
+      // products in flight must end before the tensor memory and the stages are given
+      // back, also where an epilogue that gave up no longer waits for them
+      mma_commit(&drain);
+      mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
     }
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
