@@ -2,7 +2,7 @@
 the vocabulary, and the optimiser step that every stage makes after its backward pass.
 
 * ``linear_cross_entropy`` / ``LinearCrossEntropy``: softmax cross entropy of a linear head
-  without its logits; the gradient of the hidden states is what the boundary before the last
+  that never holds its fp32 logits; the gradient of the hidden states is what the boundary before the last
   stage compresses.
 * ``AdamWPlan``: the list of tensors that ``mpc_adamw_step``, ``mpc_grad_norm`` and
   ``mpc_adamw_decode`` take, laid out once.
@@ -60,21 +60,21 @@ def _final(grads, *sources):
 
 class _LinearCeFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, h, w, targets, ignore_index):
+    def forward(ctx, h, w, targets, ignore_index, piece):
         loss, lse = mpc_linear_ce_forward(h, w, targets, ignore_index)
         ctx.save_for_backward(h, w, targets, lse)
-        ctx.ignore_index = ignore_index
+        ctx.ignore_index, ctx.piece = ignore_index, piece
         return loss
 
     @staticmethod
     def backward(ctx, gloss):
         h, w, targets, lse = ctx.saved_tensors
         grads = mpc_linear_ce_backward(h, w, targets, lse, gloss.detach().contiguous().float(),
-                                       ctx.ignore_index)
+                                       ctx.ignore_index, ctx.piece)
         grads = [g if need else None for g, need in zip(grads, ctx.needs_input_grad)]
         if torch.is_grad_enabled():
             grads = _final(grads, h, w, gloss)
-        return (*grads, None, None)
+        return (*grads, None, None, None)
 
 
 class _LinearCeMeanFn(torch.autograd.Function):
@@ -84,12 +84,12 @@ class _LinearCeMeanFn(torch.autograd.Function):
 
     @staticmethod
     def _made(ctx, h, w, targets):
-        loss, *grads = mpc_linear_ce_train(h, w, targets, None, ctx.ignore_index)
+        loss, *grads = mpc_linear_ce_train(h, w, targets, None, ctx.ignore_index, ctx.piece)
         return loss, [g if need else None for g, need in zip(grads, ctx.needs_input_grad)]
 
     @staticmethod
-    def forward(ctx, h, w, targets, ignore_index):
-        ctx.ignore_index = ignore_index
+    def forward(ctx, h, w, targets, ignore_index, piece):
+        ctx.ignore_index, ctx.piece = ignore_index, piece
         loss, ctx.grads = _LinearCeMeanFn._made(ctx, h, w, targets)
         ctx.save_for_backward(h, w, targets)
         return _mean(loss, targets, ignore_index, w.shape[0])
@@ -106,7 +106,7 @@ class _LinearCeMeanFn(torch.autograd.Function):
         if torch.is_grad_enabled():
             h, w, _ = ctx.saved_tensors
             grads = _final(grads, h, w, upstream)
-        return (*grads, None, None)
+        return (*grads, None, None, None)
 
 
 def _rows_apart(t):
@@ -115,11 +115,16 @@ def _rows_apart(t):
     return t if fine else t.contiguous()
 
 
-def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean"):
+def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str = "mean", piece: int = 0):
     """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
     ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
     where the target is ``ignore_index``).  A target outside [0, V) does not count either, and is reported
-    by ``mpc_get_status``.  There is no second derivative: asking for one raises."""
+    by ``mpc_get_status``.  There is no second derivative: asking for one raises.
+
+    The loss by itself keeps no logits.  The gradient of a mean does for the length of its call, as
+    exponentials (2 bytes each in bf16, 6 in fp32, 4 GiB at most), and then forms them once.
+    ``piece``: the vocabulary entries whose coefficients are held at a time instead, with the logits
+    formed twice, a third more work; as the other reductions do, in pieces of 1 GiB at most."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none")
     rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()
@@ -127,27 +132,29 @@ def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str
     grad = torch.is_grad_enabled() and (h.requires_grad or w.requires_grad)
     if reduction == "mean":
         if grad:
-            return _LinearCeMeanFn.apply(rows, w, y, ignore_index)
+            return _LinearCeMeanFn.apply(rows, w, y, ignore_index, piece)
         loss = mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
         return _mean(loss, y, ignore_index, w.shape[0])
-    loss = _LinearCeFn.apply(rows, w, y, ignore_index) if grad else \
+    loss = _LinearCeFn.apply(rows, w, y, ignore_index, piece) if grad else \
         mpc_linear_ce_forward(rows.detach(), w.detach(), y, ignore_index)[0]
     return loss.sum() if reduction == "sum" else loss.reshape(targets.shape)
 
 
 class LinearCrossEntropy(torch.nn.Module):
-    """The head of a last stage: a weight [vocab, hidden] and the loss of its logits."""
+    """The head of a last stage: a weight [vocab, hidden] and the loss of its logits; arguments as for
+    ``linear_cross_entropy``."""
 
     def __init__(self, hidden: int, vocab: int, ignore_index: int = -100, reduction: str = "mean",
-                 device=None, dtype=None):
+                 device=None, dtype=None, piece: int = 0):
         super().__init__()
         self.weight = torch.nn.Parameter(torch.empty(vocab, hidden, device=device, dtype=dtype))
         torch.nn.init.normal_(self.weight, std=0.02)
         self.ignore_index = int(ignore_index)
         self.reduction = reduction
+        self.piece = int(piece)
 
     def forward(self, h: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
-        return linear_cross_entropy(h, self.weight, targets, self.ignore_index, self.reduction)
+        return linear_cross_entropy(h, self.weight, targets, self.ignore_index, self.reduction, self.piece)
 
 
 # ---------------------------------------------------------------------------------------

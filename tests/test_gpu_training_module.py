@@ -295,3 +295,32 @@ def test_a_plan_without_gradients_is_refused(mpc):
     plan.set_grads([g])
     mpc.mpc_adamw_step(plan, 1e-3, 0.9, 0.99, 1e-8, 1)
     assert bool((p < 0).all())
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum"])
+def test_pieces_of_the_vocabulary(mpc, reduction):
+    """`piece` bounds what a training step holds: without it the exponentials of all logits, three bf16 planes
+    in fp32; with it those of a piece."""
+    T, D, V = 2048, 64, 50257
+    results = []
+    for piece in (0, 2048):
+        h, w, y = inputs(T, D, V)
+        head = mpc.LinearCrossEntropy(D, V, reduction=reduction, device="cuda", piece=piece)
+        with torch.no_grad():
+            head.weight.copy_(w)
+        h.requires_grad_(True)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        head(h, y).backward()
+        peak = torch.cuda.max_memory_allocated() - before
+        results.append((h.grad.double(), head.weight.grad.double(), peak))
+        del head
+    (dh, dw, large), (eh, ew, small) = results
+    if reduction == "mean":
+        assert large > T * V * 6
+    # the planes of h and w, dw, the tiles' sums, the coefficients of a piece, and the sums of up to 32
+    # parts of dh and 16 of a piece's dw
+    assert small < 6 * (T + V) * D + 4 * V * D + 8 * T * (V // 128 + 1) + 6 * T * 2048 + 4 * 32 * T * D + 4 * 16 * 2048 * D + (4 << 20)
+    for a, b in ((dh, eh), (dw, ew)):
+        assert float((a - b).norm()) < 2e-5 * float(a.norm())
