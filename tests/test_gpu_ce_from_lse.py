@@ -66,3 +66,23 @@ def test_a_long_sum_of_one_sign_is_not_one_sided(mpc):  # noqa: F811
     dh = mpc.mpc_linear_ce_train(h, w, torch.full((T,), 5, device="cuda"))[1][T - 1].double()
     along = float((dh * want).sum() / (want * want).sum()) - 1.0
     assert abs(along) <= 512 * 1.7e-7 + 6 * 2.5e-5, along
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [65536, 65537, 140001])
+def test_many_tokens(mpc, dtype, T):  # noqa: F811
+    """More tokens than a CTA of the list counts by itself, a fifth of them ignored, some targets out of range."""
+    h, w, y = inputs(T, 24, 40, dtype, seed=80)
+    masked = y.clone()
+    for i, bad in ((0, 40), (T // 2, -7), (T - 1, 1 << 40)):
+        y[i], masked[i] = bad, -100
+    want = bounds(h, w, masked, None)
+    loss, lse = mpc.mpc_linear_ce_forward(h, w, y)
+    near(loss, want["loss"], "loss")
+    near(lse, want["lse"], "lse")
+    assert mpc.mpc_get_status() == 6
+    loss, dh, dw = mpc.mpc_linear_ce_train(h, w, y)
+    near(loss, want["loss"], "loss (train)")
+    near(dh, want["dh"], "dh")
+    near(dw, want["dw"], "dw")
+    assert mpc.mpc_get_status() == 6
