@@ -281,6 +281,14 @@ class AdamW(torch.optim.Optimizer):
         self._plans = {}
         self.last_norm = None  # device fp32 of one entry, when max_norm is set
 
+    def __getstate__(self):
+        return {**super().__getstate__(), "state_bits": self.state_bits, "max_norm": self.max_norm,
+                "copies": self.copies}
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self._plans, self.last_norm = {}, None
+
     def _state(self, p):
         s = self.state[p]
         if "exp_avg" not in s:
