@@ -304,7 +304,10 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         """Restores the states in the types they were saved in (the codes of 8-bit states are not
-        numbers to be cast to the parameter's type)."""
+        numbers to be cast to the parameter's type); those of the other ``state_bits`` are refused."""
+        for s in state_dict["state"].values():
+            if "exp_avg" in s and (s["exp_avg"].dtype == torch.int8) != (self.state_bits == 8):
+                raise ValueError("the saved states are not of state_bits=%d" % self.state_bits)
         super().load_state_dict(state_dict)
         flat = [p for g in self.param_groups for p in g["params"]]
         saved = [i for g in state_dict["param_groups"] for i in g["params"]]

@@ -40,3 +40,32 @@ def test_a_copied_optimizer_is_whole(mpc, bits, how):
         assert a.keys() == b.keys() and a["step"] == b["step"]
         assert torch.equal(a["exp_avg"], b["exp_avg"]) and a["exp_avg"] is not b["exp_avg"]
         assert a["exp_avg"].dtype == b["exp_avg"].dtype
+
+
+@pytest.mark.parametrize("saved,here", [(32, 8), (8, 32)])
+def test_states_of_other_bits_are_refused(mpc, saved, here):
+    """States saved with one state_bits are not loaded into an optimizer of the other, which stays as it was."""
+    _, old = made(mpc, saved)
+    ps, opt = made(mpc, here)
+    before = copy.deepcopy(opt.state_dict())
+    with pytest.raises(ValueError, match="state_bits"):
+        opt.load_state_dict(old.state_dict())
+    after = opt.state_dict()
+    assert after["param_groups"] == before["param_groups"]
+    for i, s in before["state"].items():
+        for k, x in s.items():
+            assert torch.equal(x, after["state"][i][k]) if isinstance(x, torch.Tensor) else x == after["state"][i][k]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_are_loaded_as_they_were_saved(mpc, bits):
+    ps, old = made(mpc, bits)
+    qs, opt = made(mpc, bits)
+    for q in qs:
+        opt.state[q]["exp_avg"].zero_()
+        opt.state[q]["step"] = 0
+    opt.load_state_dict(old.state_dict())
+    for p, q in zip(ps, qs):
+        a, b = old.state[p], opt.state[q]
+        assert b["step"] == 3 and a["exp_avg"].dtype == b["exp_avg"].dtype and torch.equal(a["exp_avg"], b["exp_avg"])
+        assert a["exp_avg"].data_ptr() != b["exp_avg"].data_ptr()
