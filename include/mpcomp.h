@@ -297,8 +297,8 @@ typedef enum { MPC_F32 = 0, MPC_BF16 = 1 } mpc_dtype;
 /* The call that a linear cross-entropy workspace is for. */
 typedef enum { MPC_CE_FORWARD = 0, MPC_CE_BACKWARD = 1, MPC_CE_TRAIN = 2 } mpc_ce_pass;
 
-/* Softmax cross entropy of a linear head, in pieces of the vocabulary, without
- * keeping the logits:
+/* Softmax cross entropy of a linear head, tile by tile, without keeping the
+ * logits:
  *   l[t][v] = sum_d h[t][d] w[v][d];   lse[t] = log sum_v exp l[t][v];
  *   loss[t] = lse[t] - l[t][targets[t]].
  *   h       [tokens][hidden] of `type`, rows ldh elements apart (ldh >= hidden).
@@ -316,7 +316,9 @@ typedef enum { MPC_CE_FORWARD = 0, MPC_CE_BACKWARD = 1, MPC_CE_TRAIN = 2 } mpc_c
  *           ldw = 0 when w itself is not 16-byte aligned), as an fp32 w always
  *           is, split into three bf16 terms.
  * Products are summed in fp32 and fp32 inputs are not rounded to a narrower
- * type.  tokens = 0 is a no-op.  Requires 1 <= hidden <= 2^24, 1 <= vocab <=
+ * type.  A NaN logit makes its token's loss and lse NaN.  (An fp32 infinity, or a
+ * magnitude from 2^128 - 2^119 on, makes the logits that it meets NaN where the
+ * matrix units form them.)  tokens = 0 is a no-op.  Requires 1 <= hidden <= 2^24, 1 <= vocab <=
  * 2^30, tokens <= 2^30. */
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
                                      mpc_ce_pass pass, int64_t piece, int64_t ldw);
@@ -332,8 +334,8 @@ mpc_status mpc_linear_ce_forward(const void* h, int64_t ldh, const void* w, int6
  *          over the tokens that count (g = 1 / their number; 0 when none does).
  *   dh     [tokens][hidden] of `type`, rows lddh elements apart, out (zero for
  *          tokens that do not count); dw [vocab][hidden], rows lddw apart, out.
- *   piece  vocabulary entries whose c is in the workspace at a time; 0 lets the
- *          library choose (1 GiB of c at most).
+ *   piece  vocabulary entries whose c is in the workspace at a time (2 bytes each
+ *          for bf16, 6 for fp32); 0 lets the library choose (1 GiB of c at most).
  *   ws     workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens,
  *          hidden, vocab, type, MPC_CE_BACKWARD, piece, ldw), 256-byte
  *          aligned.
@@ -351,8 +353,8 @@ mpc_status mpc_linear_ce_backward(const void* h, int64_t ldh, const void* w, int
 /* Loss and gradients in one call, for a training step that knows g beforehand:
  * the arguments and results of the two calls above.  With piece = 0 (or >= vocab)
  * and 257 to 16384 tokens (17 in fp32) whose exponentials take 4 GiB of workspace at most (2
- * bytes each, 6 for fp32), the logits are formed once; otherwise as in the two
- * calls.
+ * bytes each, 6 for fp32), these are kept and the logits formed once; otherwise as
+ * in the two calls.
  *   ws  workspace of ws_bytes >= mpc_linear_ce_workspace_bytes(tokens, hidden,
  *       vocab, type, MPC_CE_TRAIN, piece, ldw), 256-byte aligned. */
 mpc_status mpc_linear_ce_train(const void* h, int64_t ldh, const void* w, int64_t ldw,

@@ -1,5 +1,7 @@
 // linear_ce.cu -- softmax cross entropy of a linear head over a large
-// vocabulary, with its gradient: the logits are never kept.
+// vocabulary, with its gradient.  The loss keeps no logits; a gradient keeps bf16
+// planes of the coefficients, of a piece of the vocabulary or of all of it (one plane
+// in bf16, three in fp32).
 //
 //   l[t][v] = <h[t], w[v]>            t over the tokens whose target counts
 //   lse[t]  = log sum_v exp l[t][v];  loss[t] = lse[t] - l[t][target[t]]
@@ -14,7 +16,7 @@
 // Forward: one pass of products (kLoss).  Backward from lse: per piece of the
 // vocabulary the products again (kCoef), then dh and dw: 8 T D V operations with
 // the forward's.  Training in one call, where g is known beforehand: the
-// exponentials of the one pass are kept in bf16 (kExp) and made coefficients
+// exponentials of the one pass are kept in bf16 planes (kExp) and made coefficients
 // without forming the logits again, 6 T D V operations:
 //   e[t][v] = 2^(l log2e - ref[t]) (0 at the target),  s[t] = sum of all of them
 //   dh[t] = g/s sum_v e w + g (p - 1) w[target],   p = softmax at the target
@@ -25,11 +27,15 @@
 // A few tokens go another way (linear_ce_few.cu).  The small kernels here let
 // their successor be scheduled as they start.
 //
-// What bounds it: the matrix units (linear_ce_gemm.cuh).  Measured: 8192 tokens (a
-// tenth ignored) x 768 x 50257 in bf16 1.20 ms, of which the three products 1.08 ms;
-// 8192 x 4096 x 131072 17.1 ms, 1.54 PFLOP/s of the 6 T D V operations; 2048 x 768 x
-// 50257 in fp32 1.71 ms; 129 x 203 x 5003 in fp32 64 us, where thirteen launches
-// wait on one another.
+// NaN: a logit that is NaN makes its token's loss, lse and gradients NaN.  An fp32
+// infinity in h or w becomes NaN in its planes.
+//
+// What bounds it: the matrix units (linear_ce_gemm.cuh).  Measured over several boxes:
+// 8192 tokens (a tenth ignored) x 768 x 50257 in bf16 1.20 to 1.26 ms, of which the
+// three products 1.08 ms (the gradient from lse where all count 1.14, the loss 0.38);
+// 8192 x 4096 x 131072 16.2 to 17.9 ms, 1.47 to 1.63 PFLOP/s of the 6 T D V operations;
+// 2048 x 768 x 50257 in fp32 1.69 to 1.74 ms; 129 x 203 x 5003 in fp32 66 to 69 us,
+// where eleven launches wait on one another.
 #include <algorithm>
 
 #include "kernels.h"

@@ -2,7 +2,7 @@
 the vocabulary, and the optimiser step that every stage makes after its backward pass.
 
 * ``linear_cross_entropy`` / ``LinearCrossEntropy``: softmax cross entropy of a linear head
-  that never holds its fp32 logits; the gradient of the hidden states is what the boundary before the last
+  whose loss keeps no logits; the gradient of the hidden states is what the boundary before the last
   stage compresses.
 * ``AdamWPlan``: the list of tensors that ``mpc_adamw_step``, ``mpc_grad_norm`` and
   ``mpc_adamw_decode`` take, laid out once.
@@ -124,7 +124,8 @@ def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str
     The loss by itself keeps no logits.  The gradient of a mean does for the length of its call, as
     exponentials (2 bytes each in bf16, 6 in fp32, 4 GiB at most), and then forms them once.
     ``piece``: the vocabulary entries whose coefficients are held at a time instead, with the logits
-    formed twice, a third more work; as the other reductions do, in pieces of 1 GiB at most."""
+    formed twice, a third more work; as the other reductions do, in pieces of 1 GiB at most.  (Up to
+    16 tokens may keep 4 bytes a logit whatever ``piece`` is.)"""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be mean, sum or none")
     rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()
