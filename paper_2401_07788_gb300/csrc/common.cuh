@@ -210,6 +210,13 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::
                    : "memory");
 }
+// The two halves of the barrier by themselves.  A CTA's shared memory exists while
+// it runs, and that a cluster is launched together does not say that all of it has
+// started: before its first access to another CTA's shared memory a kernel waits until
+// every CTA has arrived (an access to one that has not started is a fault of the
+// GPU), and after the last one it lets none leave before all have.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // Address of the same shared variable in CTA `rank` of this cluster.
 __device__ __forceinline__ uint32_t dsmem_addr(const void* local, uint32_t rank) {
   uint32_t out;

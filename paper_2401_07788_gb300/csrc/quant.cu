@@ -574,6 +574,7 @@ __global__ void __launch_bounds__(NT) quant_cta_kernel(const QuantArgs a, int sp
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool from_ws = a.ws != nullptr;
   const uint32_t C = from_ws ? 1u : cluster_size();
+  if (C > 1) cluster_arrive();
   const int64_t row = blockIdx.x / spr;
   const int64_t sidx = blockIdx.x % spr;  // slice index within the row (= cluster rank)
   const int64_t L = a.L;
@@ -639,6 +640,7 @@ __global__ void __launch_bounds__(NT) quant_cta_kernel(const QuantArgs a, int sp
       sh.redmax[warp] = kmax;
     }
     __syncthreads();
+    if (C > 1) cluster_wait();  // every CTA of the row has started
     if (warp == 0) {
       uint32_t a0 = lane < NT / 32 ? sh.redmin[lane] : 0xffffffffu;
       uint32_t a1 = lane < NT / 32 ? sh.redmax[lane] : 0u;

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(NT, (NT == 128 ? 6 : NT == 256 ? 4 : NT == 512
     arow = a.aux + srow * L;
   }
   const float* xrow = a.x + row * L;
+  if (C > 1) cluster_arrive();
 
   // ---- issue the loads: a sample of the row, x by bulk copies, err / state ----
   // The bin placement comes from a sample of the row, entries [p, p+4) spread
@@ -416,6 +417,7 @@ __global__ void __launch_bounds__(NT, (NT == 128 ? 6 : NT == 256 ? 4 : NT == 512
     }
   }
   failed = __syncthreads_or(failed);
+  if (C > 1) cluster_wait();  // every CTA of the row has started
   // A slice whose copy timed out takes part in the rest as an empty one (the
   // status word reports the timeout; the row's outputs are then unspecified).
   const int nv = failed ? 0 : n;
