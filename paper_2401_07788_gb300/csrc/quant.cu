@@ -1057,7 +1057,7 @@ cudaError_t run_quant_bits(const QuantArgs& a0, int num_sms, cudaStream_t s) {
   int64_t spr;
   if (a.ws == nullptr) {
     spr = (L + kQSCAP - 1) / kQSCAP;
-    while (a.rows * spr < 2 * num_sms && spr < 8 && L / (2 * spr) >= 1024) spr *= 2;
+    while (a.rows * spr < 2 * num_sms && 2 * spr <= 8 && L / (2 * spr) >= 1024) spr *= 2;
     if (spr > 8) return cudaErrorInvalidValue;
     a.slice = ((L + spr - 1) / spr + 127) / 128 * 128;
   } else {
