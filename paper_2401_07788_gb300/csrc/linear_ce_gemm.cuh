@@ -509,9 +509,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     prefetch_map(&map_a);
     prefetch_map(&map_b);
   }
+  cluster_sync();  // both CTAs have started: the allocation is the pair's
   if (warp == 1) tmem_alloc(&tmem, 512);
   tc_fence_before();
-  __syncthreads();
   cluster_sync();
   tc_fence_after();
   const uint32_t acc = tmem;
