@@ -424,6 +424,130 @@ mpc_status mpc_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, mpc_dty
                          float* norm, void* ws, size_t ws_bytes, mpc_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* The layers of a stage                                                    */
+/* ------------------------------------------------------------------------ */
+
+/* Dropout is decided by the library's generator and no mask is stored: entry i of
+ * a tensor (its number in row-major order, whatever its strides) takes the 16 bits
+ * from 16 (i & 3) on of splitmix64 at counter i >> 2 for the seed
+ *   seed + (*step, where step is not NULL)
+ * and is dropped when they are below round(65536 p); a kept one is multiplied by
+ * 65536 / (65536 - round(65536 p)).  A dropped entry is +0 whatever it held.  The
+ * same seed gives the same mask: the backward pass repeats the forward call's.
+ *   p     in [0, 1]; 0 keeps everything, from 1 - 2^-17 on everything is dropped.
+ *   step  device int64 or NULL: a program whose steps are replays of a captured
+ *         graph advances it there, and every replay takes another mask. */
+
+/* y = residual + drop(x), n entries of `type` (residual may be NULL), in fp32 with
+ * one rounding of the product, one of the sum and one to `type`.  The gradient of x
+ * is the same call on the gradient of y without a residual.  y may be x or residual
+ * (no partial overlap).  n = 0 is a no-op; n <= 2^40. */
+mpc_status mpc_dropout(const void* x, const void* residual, int64_t n, mpc_dtype type, double p,
+                       uint64_t seed, const int64_t* step, void* y, mpc_stream_t stream);
+
+/* Root-mean-square norm of every row, with the residual's addition before it:
+ *   h = x + residual (h = x where residual is NULL);
+ *   rstd = 1 / sqrt(mean of h^2 over the row + eps);   y = h rstd weight.
+ *   x, residual, y, h  [rows][row_len] of `type`, rows ldx, ldr, ldy, ldh elements
+ *           apart (each >= row_len).  `residual` may be NULL; `h` receives the sum
+ *           rounded to `type` and may be NULL.  y and rstd come from the sum before
+ *           it is rounded.
+ *   weight  [row_len] of `type`;  rstd  [rows] fp32, out, or NULL.
+ * Squares are summed in fp32 (a row with a magnitude beyond 2^63 has rstd = 0).
+ * y may be x or residual, and so may h, with the same row distance; y and h must
+ * not overlap.  rows = 0 is a no-op.  Requires 1 <= row_len <= 2^24, rows <= 2^31-1,
+ * eps >= 0. */
+mpc_status mpc_rms_norm_forward(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                                const void* weight, int64_t rows, int64_t row_len, mpc_dtype type,
+                                double eps, void* y, int64_t ldy, void* h, int64_t ldh, float* rstd,
+                                mpc_stream_t stream);
+
+/* Its gradient, from h and rstd of the forward call (h = x without a residual):
+ *   n = h rstd;   dx = dh + rstd (weight dy - n mean(weight dy n));
+ *   dweight = sum over rows of dy n.
+ *   dy, dh, dx  [rows][row_len] of `type`, rows lddy, lddh, lddx apart; `dh`, the
+ *           gradient that reaches h by other ways (along the residual stream), may
+ *           be NULL.  dx is the gradient of x and of residual alike; it may be dy or
+ *           dh, with the same row distance.
+ *   dweight [row_len] of `type`, out, or NULL.
+ *   ws      workspace of ws_bytes >= mpc_rms_norm_workspace_bytes(rows, row_len),
+ *           16-byte aligned.
+ * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
+ * rows = 0 writes dweight = 0. */
+size_t mpc_rms_norm_workspace_bytes(int64_t rows, int64_t row_len);
+mpc_status mpc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                                 const void* weight, const float* rstd, const void* dh,
+                                 int64_t lddh, int64_t rows, int64_t row_len, mpc_dtype type,
+                                 void* dx, int64_t lddx, void* dweight, void* ws, size_t ws_bytes,
+                                 mpc_stream_t stream);
+
+/* The norm's output as an 8-bit quantisation payload (see the head of this file),
+ * which mpc_quant_decompress reads back: with u = h weight in fp32 (one rounding of
+ * the sum, one of the product) the codes are those of mpc_quant_compress(u, 8 bits,
+ * round to nearest), bit for bit, and
+ *   scale = scale(u) rstd,   minv = min(u) rstd
+ * (a row's rstd scales its range and its values alike, so the codes do not depend on
+ * it).  codes [rows][W], W = mpc_quant_codes_words(1, row_len, 8), 16-byte aligned.
+ * The other arguments are those of mpc_rms_norm_forward. */
+mpc_status mpc_rms_norm_quant(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                              const void* weight, int64_t rows, int64_t row_len, mpc_dtype type,
+                              double eps, uint32_t* codes, float* scale, float* minv, void* h,
+                              int64_t ldh, float* rstd, mpc_stream_t stream);
+
+/* Activations of the linear layer: none, max(z, 0), z Phi(z) with the normal
+ * distribution's Phi, its form z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2, and
+ * z / (1 + exp(-z)). */
+typedef enum {
+    MPC_ACT_NONE = 0, MPC_ACT_RELU = 1, MPC_ACT_GELU = 2, MPC_ACT_GELU_TANH = 3, MPC_ACT_SILU = 4
+} mpc_act;
+
+/* The call that a linear layer's workspace is for. */
+typedef enum { MPC_LINEAR_FORWARD = 0, MPC_LINEAR_BACKWARD = 1 } mpc_linear_pass;
+
+/* Linear layer with bias, activation, dropout and residual in one call:
+ *   z = x w^T + bias;   y = residual + drop(act(z)).
+ *   x [rows][in], w [out][in], residual, y and z [rows][out] of `type`, rows ldx, ldw,
+ *   ldr, ldy, ldz elements apart; bias [out] of `type`.  bias and residual may be NULL.
+ *   z receives the values that the backward call takes where there is an activation;
+ *   NULL when none is to be kept.  Dropout counts entries of y as [rows][out].
+ *   ws  workspace of ws_bytes >= mpc_linear_workspace_bytes(rows, in, out, type,
+ *       MPC_LINEAR_FORWARD, ldx, ldw, 0), 256-byte aligned.  The query takes the row
+ *       distances because the matrix units read bf16 operands in place when their rows
+ *       start on 16 bytes; they are copied into the workspace otherwise (pass 0 for an
+ *       operand that itself is not 16-byte aligned), as fp32 ones are, split into three
+ *       bf16 terms.
+ * Products are summed in fp32 and fp32 inputs are not rounded to a narrower type;
+ * what is added to them is added in fp32 and rounded once.  (An fp32 infinity, or a
+ * magnitude from 2^128 - 2^119 on, may make the products that it meets NaN.)  y may be
+ * residual, with the same row distance.  rows = 0 is a no-op.  Requires
+ * 1 <= in, out <= 2^24, rows <= 2^30. */
+size_t mpc_linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, mpc_dtype type,
+                                  mpc_linear_pass pass, int64_t ldx, int64_t ldw, int64_t lddy);
+mpc_status mpc_linear_forward(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                              const void* bias, const void* residual, int64_t ldr, int64_t rows,
+                              int64_t in, int64_t out, mpc_dtype type, mpc_act act, double p,
+                              uint64_t seed, const int64_t* step, void* y, int64_t ldy, void* z,
+                              int64_t ldz, void* ws, size_t ws_bytes, mpc_stream_t stream);
+
+/* Its gradient (that of residual is dy itself):
+ *   dz = drop(dy) act'(z);   dx = dz w;   dw = dz^T x;   dbias = sum over rows of dz,
+ * with the mask of the forward call (the same p, seed and step).  A bf16 dz is rounded
+ * to bf16 before the products, without dropout's factor, which is applied to their sums.
+ *   dy [rows][out], z [rows][out] (NULL without an activation), x, w as above; dx
+ *   [rows][in], dw [out][in] and dbias [out] of `type`, out: each may be NULL, and is
+ *   not formed then.  x is not read without dw, w not without dx.
+ *   ws  workspace of ws_bytes >= mpc_linear_workspace_bytes(rows, in, out, type,
+ *       MPC_LINEAR_BACKWARD, ldx, ldw, lddy), 256-byte aligned.
+ * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
+ * rows = 0 writes dw = 0 and dbias = 0. */
+mpc_status mpc_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                               const void* w, int64_t ldw, const void* z, int64_t ldz,
+                               int64_t rows, int64_t in, int64_t out, mpc_dtype type, mpc_act act,
+                               double p, uint64_t seed, const int64_t* step, void* dx, int64_t lddx,
+                               void* dw, int64_t lddw, void* dbias, void* ws, size_t ws_bytes,
+                               mpc_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Status and diagnostics                                                   */
 /* ------------------------------------------------------------------------ */
 

@@ -30,7 +30,9 @@ __all__ = [
     "mpc_aqsgd_quant_compress", "mpc_aqsgd_quant_decompress", "mpc_get_status", "mpc_last_error",
     "mpc_linear_ce_workspace_bytes", "mpc_linear_ce_forward", "mpc_linear_ce_backward",
     "mpc_linear_ce_train", "mpc_adamw_step", "mpc_adamw_decode", "mpc_grad_norm_workspace_bytes",
-    "mpc_grad_norm",
+    "mpc_grad_norm", "mpc_dropout", "mpc_rms_norm_forward", "mpc_rms_norm_workspace_bytes",
+    "mpc_rms_norm_backward", "mpc_rms_norm_quant", "mpc_linear_workspace_bytes", "mpc_linear_forward",
+    "mpc_linear_backward",
     "mpc_set_knob", "MPC_KNOB_SPIN_LIMIT", "MPC_KNOB_TOPK_PATH", "MPC_KNOB_PDL", "STATUS_NAMES",
 ]
 
@@ -85,6 +87,19 @@ _SIGNATURES = {
     "mpc_adamw_decode": ([_VP, _I64, _VP, _VP, _VP], _INT),
     "mpc_grad_norm_workspace_bytes": ([_I64], _SZ),
     "mpc_grad_norm": ([_VP, _I64, _INT, _VP, _VP, _SZ, _VP], _INT),
+    "mpc_dropout": ([_VP, _VP, _I64, _INT, _F64, _U64, _VP, _VP, _VP], _INT),
+    "mpc_rms_norm_forward": ([_VP, _I64, _VP, _I64, _VP, _I64, _I64, _INT, _F64, _VP, _I64, _VP, _I64,
+                              _VP, _VP], _INT),
+    "mpc_rms_norm_workspace_bytes": ([_I64, _I64], _SZ),
+    "mpc_rms_norm_backward": ([_VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _I64, _I64, _INT, _VP, _I64,
+                               _VP, _VP, _SZ, _VP], _INT),
+    "mpc_rms_norm_quant": ([_VP, _I64, _VP, _I64, _VP, _I64, _I64, _INT, _F64, _VP, _VP, _VP, _VP, _I64,
+                            _VP, _VP], _INT),
+    "mpc_linear_workspace_bytes": ([_I64, _I64, _I64, _INT, _INT, _I64, _I64, _I64], _SZ),
+    "mpc_linear_forward": ([_VP, _I64, _VP, _I64, _VP, _VP, _I64, _I64, _I64, _I64, _INT, _INT, _F64,
+                            _U64, _VP, _VP, _I64, _VP, _I64, _VP, _SZ, _VP], _INT),
+    "mpc_linear_backward": ([_VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _I64, _I64, _I64, _INT, _INT,
+                             _F64, _U64, _VP, _VP, _I64, _VP, _I64, _VP, _VP, _SZ, _VP], _INT),
     "mpc_get_status": ([_VP], _INT),
     "mpc_last_error": ([], ctypes.c_char_p),
     "mpc_set_knob": ([_INT, _I64], _INT),
@@ -643,6 +658,226 @@ def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
 
 
 # ---------------------------------------------------------------------------------------
+# The layers of a stage
+# ---------------------------------------------------------------------------------------
+
+_ACTS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_SEEDS = 0xFFFFFFFFFFFFFFFF
+
+
+def _act(act) -> int:
+    try:
+        return _ACTS[act]
+    except (KeyError, TypeError):
+        raise MpcError(1, "act must be None, 'relu', 'gelu', 'gelu_tanh' or 'silu', got %r" % (act,)) from None
+
+
+def _step(step, device):
+    """The address of a device counter that is added to a dropout seed."""
+    return None if step is None else _vector(step, 1, torch.int64, "step", device).data_ptr()
+
+
+def _like(t, rows: int, cols: int, of, name: str, stream):
+    """An output matrix of the type and device of `of`: the caller's, checked, or a new one."""
+    if t is None:
+        t = torch.empty((rows, cols), dtype=of.dtype, device=of.device)
+        if stream is not None:
+            t.record_stream(stream)
+        return t, cols
+    ld = _matrix(t, name, cols, of)
+    if t.shape[0] != rows:
+        raise MpcError(1, "%s must have %d rows" % (name, rows))
+    return t, ld
+
+
+def _rows_like(t, name: str, of):
+    """The row distance of an input matrix with the shape, type and device of `of` (0 for None)."""
+    if t is None:
+        return 0
+    if t.shape != of.shape:
+        raise MpcError(1, "%s must have the shape %s" % (name, tuple(of.shape)))
+    return _matrix(t, name, of.shape[1], of)
+
+
+def _vector_like(t, n: int, of, name: str):
+    return None if t is None else _vector(t, n, of.dtype, name, of.device).data_ptr()
+
+
+def mpc_dropout(x, p: float, seed: int = 0, residual=None, step=None, y=None, stream=None):
+    """residual + drop(x), entries dropped with probability p and the others scaled by 1 / (1 - p); x and
+    residual contiguous, of one shape.  No mask is stored: the same ``seed`` (plus ``step``, an int64 device
+    tensor of one entry) makes the same one, so the gradient of x is this call on the gradient of y."""
+    kind = _dtype(x, "x")
+    _cuda(x, x.dtype, "x")
+    for name, t in (("residual", residual), ("y", y)):
+        if t is not None:
+            _cuda(t, x.dtype, name)
+            if t.shape != x.shape or t.device != x.device:
+                raise MpcError(1, "%s must have the shape and device of x" % name)
+    if y is None:
+        y = torch.empty_like(x)
+        _on(stream, y)
+    _launch(lib().mpc_dropout, x.device, stream, x.data_ptr(), _address(residual), x.numel(), kind, p, seed & _SEEDS,
+            _step(step, x.device), y.data_ptr())
+    return y
+
+
+def _norm_args(x, weight, residual, h, rstd, stream):
+    ldx = _matrix(x, "x")
+    rows, D = x.shape
+    if D == 0:
+        raise MpcError(1, "the rows of x must hold at least one entry")
+    w = _vector_like(weight, D, x, "weight")
+    ldr = _rows_like(residual, "residual", x)
+    ldh = ldx
+    if residual is not None:
+        h, ldh = _like(h, rows, D, x, "h", stream)
+    elif h is not None:
+        raise MpcError(1, "h is the sum with a residual; without one it is x")
+    rstd = _vector_or_new(rstd, rows, "rstd", x.device, stream)
+    return rows, D, ldx, w, ldr, h, ldh, rstd
+
+
+def mpc_rms_norm_forward(x, weight, eps: float = 1e-6, residual=None, y=None, h=None, rstd=None, stream=None):
+    """Root-mean-square norm of the rows of x [R, D], after the residual's addition where there is one.
+    Returns (y, h, rstd): h = x + residual in the type of x (x itself without a residual), rstd [R] fp32."""
+    rows, D, ldx, w, ldr, h, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    y, ldy = _like(y, rows, D, x, "y", stream)
+    _launch(lib().mpc_rms_norm_forward, x.device, stream, x.data_ptr(), ldx, _address(residual), ldr, w, rows, D,
+            _DTYPES[x.dtype], eps, y.data_ptr(), ldy, _address(h), ldh, rstd.data_ptr())
+    return y, x if h is None else h, rstd
+
+
+def mpc_rms_norm_quant(x, weight, eps: float = 1e-6, residual=None, codes=None, scale=None, minv=None, h=None,
+                       rstd=None, stream=None):
+    """The same norm with its output as an 8-bit quantisation payload for mpc_quant_decompress.  Returns
+    (codes [R, W] int32 of uint32 words, scale [R], minv [R], h, rstd)."""
+    rows, D, ldx, w, ldr, h, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    W = (D + 15) // 16 * 4
+    if codes is None:
+        codes = torch.empty((rows, W), dtype=torch.int32, device=x.device)
+        _on(stream, codes)
+    _vector(codes, rows * W, torch.int32, "codes", x.device)
+    scale = _vector_or_new(scale, rows, "scale", x.device, stream)
+    minv = _vector_or_new(minv, rows, "minv", x.device, stream)
+    _launch(lib().mpc_rms_norm_quant, x.device, stream, x.data_ptr(), ldx, _address(residual), ldr, w, rows, D,
+            _DTYPES[x.dtype], eps, codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), _address(h), ldh,
+            rstd.data_ptr())
+    return codes, scale, minv, x if h is None else h, rstd
+
+
+def mpc_rms_norm_workspace_bytes(rows: int, row_len: int) -> int:
+    return int(lib().mpc_rms_norm_workspace_bytes(rows, row_len))
+
+
+def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, need_weight: bool = True, ws=None,
+                          stream=None):
+    """The gradient of mpc_rms_norm_forward from its h and rstd: (dx, dweight).  ``dh`` is the gradient that
+    reaches h by other ways; dx is that of x and of residual alike.  ``need_weight`` False leaves dweight out."""
+    ldh = _matrix(h, "h")
+    rows, D = h.shape
+    if D == 0:
+        raise MpcError(1, "the rows of h must hold at least one entry")
+    lddy, lddh = _rows_like(dy, "dy", h), _rows_like(dh, "dh", h)
+    w = _vector_like(weight, D, h, "weight")
+    _vector(rstd, rows, torch.float32, "rstd", h.device)
+    dx, lddx = _like(dx, rows, D, h, "dx", stream)
+    if dweight is not None:
+        _vector(dweight, D, h.dtype, "dweight", h.device)
+    elif need_weight:
+        dweight = torch.empty(D, dtype=h.dtype, device=h.device)
+        _on(stream, dweight)
+    given = ws
+    ws, wsb = _workspace(mpc_rms_norm_workspace_bytes(rows, D), ws, h.device)
+    if given is None:
+        _on(stream, ws)
+    _launch(lib().mpc_rms_norm_backward, h.device, stream, dy.data_ptr(), lddy, h.data_ptr(), ldh, w, rstd.data_ptr(),
+            _address(dh), lddh, rows, D, _DTYPES[h.dtype], dx.data_ptr(), lddx, _address(dweight), _address(ws), wsb)
+    return dx, dweight
+
+
+def mpc_linear_workspace_bytes(rows: int, inputs: int, outputs: int, dtype=torch.float32, backward: bool = False,
+                               ldx: int | None = None, ldw: int | None = None, lddy: int | None = None) -> int:
+    """Bytes of workspace; ldx, ldw, lddy: the distances of the rows of x, w and dy (dense when None, 0 for an
+    operand that is not 16-byte aligned)."""
+    return int(lib().mpc_linear_workspace_bytes(rows, inputs, outputs, _DTYPES[dtype], int(backward),
+                                                inputs if ldx is None else ldx, inputs if ldw is None else ldw,
+                                                outputs if lddy is None else lddy))
+
+
+def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, device, stream):
+    need = lib().mpc_linear_workspace_bytes(
+        rows, K, N, kind, backward, 0 if x is None or x.data_ptr() % 16 else ldx,
+        0 if w is None or w.data_ptr() % 16 else ldw, 0 if dy is None or dy.data_ptr() % 16 else lddy)
+    if ws is None:
+        if need == 0:
+            return None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        _on(stream, ws)
+    return ws, ws.numel() * ws.element_size()
+
+
+def mpc_linear_forward(x, w, bias=None, residual=None, act: str | None = None, p: float = 0.0, seed: int = 0,
+                       step=None, keep: bool = False, y=None, z=None, ws=None, stream=None):
+    """residual + drop(act(x @ w.T + bias)) for x [R, K], w [N, K].  Returns (y [R, N], z): z holds the values
+    before the activation, for the backward call, with ``keep`` (else None).  act: None, "relu", "gelu",
+    "gelu_tanh" or "silu"; p, seed and step as for mpc_dropout."""
+    ldx = _matrix(x, "x")
+    rows, K = x.shape
+    ldw = _matrix(w, "w", K, x)
+    N = w.shape[0]
+    if K == 0 or N == 0:
+        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
+    kind, code = _DTYPES[x.dtype], _act(act)
+    b = _vector_like(bias, N, x, "bias")
+    y, ldy = _like(y, rows, N, x, "y", stream)
+    ldr = _rows_like(residual, "residual", y)
+    ldz = 0
+    if keep or z is not None:
+        z, ldz = _like(z, rows, N, x, "z", stream)
+    ws, wsb = _linear_ws(rows, K, N, kind, 0, x, ldx, w, ldw, None, 0, ws, x.device, stream)
+    _launch(lib().mpc_linear_forward, x.device, stream, x.data_ptr(), ldx, w.data_ptr(), ldw, b, _address(residual),
+            ldr, rows, K, N, kind, code, p, seed & _SEEDS, _step(step, x.device), y.data_ptr(), ldy, _address(z), ldz,
+            _address(ws), wsb)
+    return y, z
+
+
+def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0, seed: int = 0, step=None,
+                        need=(True, True, True), dx=None, dw=None, db=None, ws=None, stream=None):
+    """The gradient of mpc_linear_forward, with its z where it has an activation and its p, seed and step:
+    (dx [R, K], dw [N, K], db [N]); ``need`` says which are formed (the others are None).  The gradient of the
+    residual is dy.  dy, x, w: all three are given, whatever is formed."""
+    ldx = _matrix(x, "x")
+    rows, K = x.shape
+    ldw = _matrix(w, "w", K, x)
+    N = w.shape[0]
+    if K == 0 or N == 0:
+        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
+    kind, code = _DTYPES[x.dtype], _act(act)
+    lddy = _matrix(dy, "dy", N, x)
+    if dy.shape[0] != rows:
+        raise MpcError(1, "dy must have %d rows" % rows)
+    if code and z is None:
+        raise MpcError(1, "the gradient of an activation needs z (keep=True in the forward call)")
+    ldz = _rows_like(z, "z", dy)
+    lddx = lddw = 0
+    if dx is not None or need[0]:
+        dx, lddx = _like(dx, rows, K, x, "dx", stream)
+    if dw is not None or need[1]:
+        dw, lddw = _like(dw, N, K, x, "dw", stream)
+    if db is not None:
+        _vector(db, N, x.dtype, "db", x.device)
+    elif need[2]:
+        db = torch.empty(N, dtype=x.dtype, device=x.device)
+        _on(stream, db)
+    ws, wsb = _linear_ws(rows, K, N, kind, 1, x, ldx, w, ldw, dy, lddy, ws, x.device, stream)
+    _launch(lib().mpc_linear_backward, x.device, stream, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw,
+            _address(z), ldz, rows, K, N, kind, code, p, seed & _SEEDS, _step(step, x.device), _address(dx), lddx,
+            _address(dw), lddw, _address(db), _address(ws), wsb)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------------------------------
 # Status and knobs
 # ---------------------------------------------------------------------------------------
 
@@ -664,5 +899,9 @@ from .boundary import CompressionBoundary, Quant, Reuse, TopK, with_boundaries  
 # The last stage's loss and every stage's optimiser, built on the calls above.
 from .training import AdamW, AdamWPlan, LinearCrossEntropy, linear_cross_entropy  # noqa: E402
 
+# The layers between the boundaries, built on the calls above.
+from .layers import Dropout, Linear, RMSNorm, dropout, linear, rms_norm  # noqa: E402
+
+__all__ += ["Dropout", "Linear", "RMSNorm", "dropout", "linear", "rms_norm"]
 __all__ += ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
 __all__ += ["CompressionBoundary", "Quant", "TopK", "Reuse", "with_boundaries"]

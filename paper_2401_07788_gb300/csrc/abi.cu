@@ -837,6 +837,299 @@ mpc_status mpc_grad_norm(const mpc_adamw_tensor* tensors, int64_t count, mpc_dty
   return ok();
 }
 
+namespace {
+
+// rows x cols elements of `type`, rows ld apart.
+mpc_status check_rows(const void* p, int64_t rows, int64_t cols, int64_t ld, int type, const char* name) {
+  MPC_TRY(check_ptr(p, type == MPC_BF16 ? 2 : 4, name));
+  if (ld < cols)
+    return set_error(MPC_ERR_INVALID_ARG, "rows of %s are %lld elements apart, shorter than %lld", name,
+                     (long long)ld, (long long)cols);
+  if (rows > 0 && ld > INT64_MAX / 4 / rows) return set_error(MPC_ERR_INVALID_ARG, "the size of %s overflows", name);
+  return MPC_OK;
+}
+
+mpc_status check_drop(double p, const int64_t* step) {
+  if (!(p >= 0.0 && p <= 1.0)) return set_error(MPC_ERR_INVALID_ARG, "p=%g outside [0, 1]", p);
+  if (step != nullptr) MPC_TRY(check_ptr(step, 8, "step"));
+  return MPC_OK;
+}
+
+mpc_status check_ws(const void* ws, size_t given, size_t need, uintptr_t align) {
+  if (need == 0) return MPC_OK;
+  if (ws == nullptr || given < need)
+    return set_error(MPC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws == nullptr ? (size_t)0 : given);
+  return check_ptr(ws, align, "ws");
+}
+
+bool norm_sizes_ok(int64_t rows, int64_t row_len) {
+  return rows >= 0 && rows <= 0x7fffffffLL && row_len >= 1 && row_len <= (1 << 24);
+}
+
+mpc_status check_norm(int64_t rows, int64_t row_len, int type, const void* x, int64_t ldx, const void* weight) {
+  MPC_TRY(check_type(type, "type"));
+  if (!norm_sizes_ok(rows, row_len))
+    return set_error(MPC_ERR_INVALID_ARG, "rows=%lld row_len=%lld", (long long)rows, (long long)row_len);
+  if (rows == 0) return MPC_OK;
+  MPC_TRY(check_rows(x, rows, row_len, ldx, type, "the input"));
+  return check_ptr(weight, type == MPC_BF16 ? 2 : 4, "weight");
+}
+
+mpc_status rms_norm_common(const mpc::RmsNormArgs& a, mpc_dtype type, double eps, mpc_stream_t stream) {
+  MPC_TRY(check_norm(a.rows, a.D, type, a.x, a.ldx, a.weight));
+  if (!(eps >= 0.0)) return set_error(MPC_ERR_INVALID_ARG, "eps=%g < 0", eps);
+  if (a.rows == 0) return ok();
+  if (a.residual != nullptr) MPC_TRY(check_rows(a.residual, a.rows, a.D, a.ldr, type, "residual"));
+  if (a.h != nullptr) MPC_TRY(check_rows(a.h, a.rows, a.D, a.ldh, type, "h"));
+  if (a.rstd != nullptr) MPC_TRY(check_ptr(a.rstd, 4, "rstd"));
+  Device d;
+  MPC_TRY(current_device(&d));
+  const cudaError_t e = mpc::launch_rms_norm(a, d.num_sms, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "rms_norm launch");
+  return ok();
+}
+
+bool linear_sizes_ok(int64_t rows, int64_t in, int64_t out) {
+  return rows >= 0 && rows <= (int64_t{1} << 30) && in >= 1 && in <= (1 << 24) && out >= 1 && out <= (1 << 24);
+}
+
+mpc_status check_linear(const mpc::LinearArgs& a, mpc_dtype type, mpc_act act) {
+  MPC_TRY(check_type(type, "type"));
+  if (!linear_sizes_ok(a.rows, a.in, a.out))
+    return set_error(MPC_ERR_INVALID_ARG, "rows=%lld in=%lld out=%lld", (long long)a.rows, (long long)a.in, (long long)a.out);
+  if (act < MPC_ACT_NONE || act > MPC_ACT_SILU) return set_error(MPC_ERR_INVALID_ARG, "act=%d", static_cast<int>(act));
+  return check_drop(a.p, a.step);
+}
+
+// Row distances as the workspace query takes them.
+int64_t ld_in_place(const void* p, int64_t ld) { return aligned_to(p, 16) ? ld : 0; }
+
+}  // namespace
+
+mpc_status mpc_dropout(const void* x, const void* residual, int64_t n, mpc_dtype type, double p, uint64_t seed,
+                       const int64_t* step, void* y, mpc_stream_t stream) {
+  MPC_TRY(check_type(type, "type"));
+  if (n < 0 || n > (int64_t{1} << 40)) return set_error(MPC_ERR_INVALID_ARG, "n=%lld", (long long)n);
+  MPC_TRY(check_drop(p, step));
+  if (n == 0) return ok();
+  const uintptr_t align = type == MPC_BF16 ? 2 : 4;
+  MPC_TRY(check_ptr(x, align, "x"));
+  MPC_TRY(check_ptr(y, align, "y"));
+  if (residual != nullptr) MPC_TRY(check_ptr(residual, align, "residual"));
+  const mpc::DropoutArgs a = {x, residual, n, type == MPC_BF16, p, seed, step, y};
+  const cudaError_t e = mpc::launch_dropout(a, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "dropout launch");
+  return ok();
+}
+
+mpc_status mpc_rms_norm_forward(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                                int64_t rows, int64_t row_len, mpc_dtype type, double eps, void* y, int64_t ldy,
+                                void* h, int64_t ldh, float* rstd, mpc_stream_t stream) {
+  MPC_TRY(check_type(type, "type"));
+  if (rows > 0 && norm_sizes_ok(rows, row_len)) MPC_TRY(check_rows(y, rows, row_len, ldy, type, "y"));
+  mpc::RmsNormArgs a = {};
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.rows = rows;
+  a.D = row_len;
+  a.bf16 = type == MPC_BF16;
+  a.eps = static_cast<float>(eps);
+  a.y = y;
+  a.ldy = ldy;
+  a.h = h;
+  a.ldh = ldh;
+  a.rstd = rstd;
+  return rms_norm_common(a, type, eps, stream);
+}
+
+mpc_status mpc_rms_norm_quant(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                              int64_t rows, int64_t row_len, mpc_dtype type, double eps, uint32_t* codes,
+                              float* scale, float* minv, void* h, int64_t ldh, float* rstd, mpc_stream_t stream) {
+  if (rows > 0) {
+    MPC_TRY(check_ptr(codes, 16, "codes"));
+    MPC_TRY(check_ptr(scale, 4, "scale"));
+    MPC_TRY(check_ptr(minv, 4, "minv"));
+  }
+  mpc::RmsNormArgs a = {};
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.rows = rows;
+  a.D = row_len;
+  a.bf16 = type == MPC_BF16;
+  a.eps = static_cast<float>(eps);
+  a.h = h;
+  a.ldh = ldh;
+  a.rstd = rstd;
+  a.codes = codes;
+  a.scale = scale;
+  a.minv = minv;
+  a.W = static_cast<int64_t>(mpc_quant_codes_words(1, row_len, 8));
+  return rms_norm_common(a, type, eps, stream);
+}
+
+size_t mpc_rms_norm_workspace_bytes(int64_t rows, int64_t row_len) {
+  return rows == 0 || !norm_sizes_ok(rows, row_len) ? 0 : mpc::rms_norm_workspace_bytes(rows, row_len);
+}
+
+mpc_status mpc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight,
+                                 const float* rstd, const void* dh, int64_t lddh, int64_t rows, int64_t row_len,
+                                 mpc_dtype type, void* dx, int64_t lddx, void* dweight, void* ws, size_t ws_bytes,
+                                 mpc_stream_t stream) {
+  MPC_TRY(check_norm(rows, row_len, type, h, ldh, weight));
+  const uintptr_t align = type == MPC_BF16 ? 2 : 4;
+  if (dweight != nullptr) MPC_TRY(check_ptr(dweight, align, "dweight"));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    if (dweight == nullptr) return ok();
+    const cudaError_t e = cudaMemsetAsync(dweight, 0, row_len * align, s);
+    if (e != cudaSuccess) return cuda_error(e, "rms_norm clear");
+    return ok();
+  }
+  MPC_TRY(check_rows(dy, rows, row_len, lddy, type, "dy"));
+  MPC_TRY(check_ptr(rstd, 4, "rstd"));
+  if (dh != nullptr) MPC_TRY(check_rows(dh, rows, row_len, lddh, type, "dh"));
+  MPC_TRY(check_rows(dx, rows, row_len, lddx, type, "dx"));
+  MPC_TRY(check_ws(ws, ws_bytes, mpc::rms_norm_workspace_bytes(rows, row_len), 16));
+  Device d;
+  MPC_TRY(current_device(&d));
+  mpc::RmsNormArgs a = {};
+  a.x = h;
+  a.ldx = ldh;
+  a.weight = weight;
+  a.rows = rows;
+  a.D = row_len;
+  a.bf16 = type == MPC_BF16;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.dh = dh;
+  a.lddh = lddh;
+  a.rstd_in = rstd;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dweight = dweight;
+  a.ws = ws;
+  const cudaError_t e = mpc::launch_rms_norm_backward(a, d.num_sms, s);
+  if (e != cudaSuccess) return cuda_error(e, "rms_norm backward launch");
+  return ok();
+}
+
+size_t mpc_linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, mpc_dtype type, mpc_linear_pass pass,
+                                  int64_t ldx, int64_t ldw, int64_t lddy) {
+  if (rows == 0 || !linear_sizes_ok(rows, in, out) || pass < MPC_LINEAR_FORWARD || pass > MPC_LINEAR_BACKWARD) return 0;
+  return mpc::linear_workspace_bytes(rows, in, out, type == MPC_BF16, pass, ldx, ldw, lddy);
+}
+
+mpc_status mpc_linear_forward(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias,
+                              const void* residual, int64_t ldr, int64_t rows, int64_t in, int64_t out,
+                              mpc_dtype type, mpc_act act, double p, uint64_t seed, const int64_t* step, void* y,
+                              int64_t ldy, void* z, int64_t ldz, void* ws, size_t ws_bytes, mpc_stream_t stream) {
+  mpc::LinearArgs a = {};
+  a.x = x;
+  a.ldx = ldx;
+  a.w = w;
+  a.ldw = ldw;
+  a.bias = bias;
+  a.residual = residual;
+  a.ldr = ldr;
+  a.rows = rows;
+  a.in = in;
+  a.out = out;
+  a.bf16 = type == MPC_BF16;
+  a.act = act;
+  a.p = p;
+  a.seed = seed;
+  a.step = step;
+  a.y = y;
+  a.ldy = ldy;
+  a.z = z;
+  a.ldz = ldz;
+  MPC_TRY(check_linear(a, type, act));
+  if (rows == 0) return ok();
+  MPC_TRY(check_rows(x, rows, in, ldx, type, "x"));
+  MPC_TRY(check_rows(w, out, in, ldw, type, "w"));
+  MPC_TRY(check_rows(y, rows, out, ldy, type, "y"));
+  if (bias != nullptr) MPC_TRY(check_ptr(bias, type == MPC_BF16 ? 2 : 4, "bias"));
+  if (residual != nullptr) MPC_TRY(check_rows(residual, rows, out, ldr, type, "residual"));
+  if (z != nullptr) MPC_TRY(check_rows(z, rows, out, ldz, type, "z"));
+  MPC_TRY(check_ws(ws, ws_bytes,
+                   mpc::linear_workspace_bytes(rows, in, out, a.bf16, MPC_LINEAR_FORWARD, ld_in_place(x, ldx),
+                                               ld_in_place(w, ldw), 0), 256));
+  Device d;
+  MPC_TRY(current_device(&d));
+  a.ws = ws;
+  a.spin_limit = g_spin_limit.load();
+  a.status = d.status;
+  const cudaError_t e = mpc::launch_linear_forward(a, d.num_sms, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_error(e, "linear launch");
+  return ok();
+}
+
+mpc_status mpc_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                               const void* z, int64_t ldz, int64_t rows, int64_t in, int64_t out, mpc_dtype type,
+                               mpc_act act, double p, uint64_t seed, const int64_t* step, void* dx, int64_t lddx,
+                               void* dw, int64_t lddw, void* dbias, void* ws, size_t ws_bytes,
+                               mpc_stream_t stream) {
+  mpc::LinearArgs a = {};
+  a.x = x;
+  a.ldx = ldx;
+  a.w = w;
+  a.ldw = ldw;
+  a.rows = rows;
+  a.in = in;
+  a.out = out;
+  a.bf16 = type == MPC_BF16;
+  a.act = act;
+  a.p = p;
+  a.seed = seed;
+  a.step = step;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.z_in = z;
+  a.ldz = ldz;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dw = dw;
+  a.lddw = lddw;
+  a.dbias = dbias;
+  MPC_TRY(check_linear(a, type, act));
+  const uintptr_t size = a.bf16 ? 2 : 4;
+  if (dw != nullptr) MPC_TRY(check_rows(dw, out, in, lddw, type, "dw"));
+  if (dbias != nullptr) MPC_TRY(check_ptr(dbias, size, "dbias"));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    cudaError_t e = cudaSuccess;
+    if (dw != nullptr) e = cudaMemset2DAsync(dw, lddw * size, 0, in * size, out, s);
+    if (e == cudaSuccess && dbias != nullptr) e = cudaMemsetAsync(dbias, 0, out * size, s);
+    if (e != cudaSuccess) return cuda_error(e, "linear clear");
+    return ok();
+  }
+  if (dx == nullptr && dw == nullptr && dbias == nullptr) return ok();
+  MPC_TRY(check_rows(dy, rows, out, lddy, type, "dy"));
+  if (dw != nullptr) MPC_TRY(check_rows(x, rows, in, ldx, type, "x"));
+  if (dx != nullptr) {
+    MPC_TRY(check_rows(w, out, in, ldw, type, "w"));
+    MPC_TRY(check_rows(dx, rows, in, lddx, type, "dx"));
+  }
+  if (act != MPC_ACT_NONE) MPC_TRY(check_rows(z, rows, out, ldz, type, "z"));
+  MPC_TRY(check_ws(ws, ws_bytes,
+                   mpc::linear_workspace_bytes(rows, in, out, a.bf16, MPC_LINEAR_BACKWARD, ld_in_place(x, ldx),
+                                               ld_in_place(w, ldw), ld_in_place(dy, lddy)), 256));
+  Device d;
+  MPC_TRY(current_device(&d));
+  a.ws = ws;
+  a.spin_limit = g_spin_limit.load();
+  a.status = d.status;
+  const cudaError_t e = mpc::launch_linear_backward(a, d.num_sms, s);
+  if (e != cudaSuccess) return cuda_error(e, "linear backward launch");
+  return ok();
+}
+
 mpc_status mpc_get_status(mpc_stream_t stream) {
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaStreamSynchronize(s);

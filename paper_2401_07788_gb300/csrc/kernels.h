@@ -170,4 +170,76 @@ bool linear_ce_few_fits(int64_t T, int64_t D, int64_t V, int64_t ldw, bool bf16,
 size_t linear_ce_few_workspace_bytes(int64_t T, int64_t D, int64_t V, int grad);
 cudaError_t launch_linear_ce_few(const LinearCeArgs& a, int num_sms, cudaStream_t s);
 
+// The layers of a stage: dropout (dropout.cu), the root-mean-square norm
+// (rms_norm.cu) and the linear layer (linear.cu).
+struct DropoutArgs {
+  const void* x;
+  const void* residual;
+  int64_t n;
+  int bf16;
+  double p;
+  uint64_t seed;
+  const int64_t* step;
+  void* y;
+};
+cudaError_t launch_dropout(const DropoutArgs& a, cudaStream_t s);
+
+struct RmsNormArgs {
+  const void* x;
+  const void* residual;
+  const void* weight;
+  int64_t ldx, ldr, rows, D;
+  int bf16;
+  float eps;
+  void* y;          // the norm's output, or nullptr: codes, scale and minv
+  void* h;
+  int64_t ldy, ldh;
+  float* rstd;
+  uint32_t* codes;
+  float* scale;
+  float* minv;
+  int64_t W;        // words of a code row
+  // backward: dy, h (as `x`), dh; dx, dweight
+  const void* dy;
+  const void* dh;
+  void* dx;
+  void* dweight;
+  const float* rstd_in;
+  int64_t lddy, lddh, lddx;
+  void* ws;
+};
+size_t rms_norm_workspace_bytes(int64_t rows, int64_t D);
+cudaError_t launch_rms_norm(const RmsNormArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_rms_norm_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s);
+
+struct LinearArgs {
+  const void* x;
+  const void* w;
+  const void* bias;
+  const void* residual;
+  int64_t ldx, ldw, ldr, rows, in, out;
+  int bf16, act;
+  double p;
+  uint64_t seed;
+  const int64_t* step;
+  void* y;
+  void* z;
+  int64_t ldy, ldz;
+  // backward
+  const void* dy;
+  const void* z_in;
+  int64_t lddy;
+  void* dx;
+  void* dw;
+  void* dbias;
+  int64_t lddx, lddw;
+  void* ws;
+  uint32_t spin_limit;
+  unsigned* status;
+};
+size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, int pass, int64_t ldx,
+                              int64_t ldw, int64_t lddy);
+cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_linear_backward(const LinearArgs& a, int num_sms, cudaStream_t s);
+
 }  // namespace mpc

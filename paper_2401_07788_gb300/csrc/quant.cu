@@ -49,15 +49,6 @@ __device__ __forceinline__ float ord_value(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
 }
 
-// splitmix64 (Steele, Lea & Flood, OOPSLA 2014) at counter c: the finaliser
-// applied to seed + (c + 1) * golden-ratio increment.
-__device__ __forceinline__ uint64_t splitmix64_at(uint64_t seed, uint64_t c) {
-  uint64_t z = seed + (c + 1u) * 0x9E3779B97F4A7C15ull;
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-
 // u for 4 consecutive flat indices i0..i0+3: 24 bits of the low (even i) or
 // high (odd i) half of splitmix64 at counter i >> 1, times 2^-24.
 __device__ __forceinline__ void uniform4(uint64_t seed, uint64_t i0, float u[4]) {
