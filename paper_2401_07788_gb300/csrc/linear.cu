@@ -2,136 +2,416 @@
 //
 //   z = x w^T + b;   y = r + drop(act(z))
 //   dz = drop(dy) act'(z);   dx = dz w;   dw = dz^T x;   db = sum_rows dz
+//
+// Operands go to the matrix units as bf16 planes (gemm_tiles.cuh): a bf16 operand whose rows
+// start on 16 bytes as it is, another one through a copy, an fp32 one split in three.  The
+// epilogue of the products (linear_gemm.cuh) does what is done to z; where the
+// product is cut along K, because it has few tiles, linear_finish_kernel adds the parts and
+// does it there.
+//
+// Rounded to fewer bits in bf16: z as it is kept for the backward pass (2^-9 of it, which
+// moves act' by less than half as much), and dz for the two products (an error of the size of
+// the result's own rounding).  Dropout's factor stays out of dz: it scales the fp32 sums of dx,
+// dw and db, so a dz without an activation is dy's own bits.
 #include <algorithm>
 
 #include "launch_util.h"
-#include "layers.cuh"
+#include "linear_gemm.cuh"
 
 namespace mpc {
 namespace {
 
-// C[m][n] = sum_k A[m][k] B[n][k] in 64 x 64 tiles, any strides.
-struct Product {
-  int64_t m, n, k;
-  int64_t am, ak, bn, bk;  // strides
+// ---------------------------------------------------------------------------
+// Operands.  One launch: dz with its column sums, and what of x and w is not read in place.
+// ---------------------------------------------------------------------------
+template <typename E>
+struct Operand {
+  const E* p;
+  int64_t ld, rows, cols, padded;  // padded: columns of a plane's row, a multiple of 8
+  int wide;                        // rows on 16 bytes
+  uint16_t* out;                   // nullptr: read in place
+  unsigned blocks;
 };
-enum Out { kLayer, kGrad };
 
-template <typename T, int OUT>
-__global__ void __launch_bounds__(256)
-    linear_tile_kernel(const T* a, const T* b, const Product g, const LinearArgs l, const Drop d, T* c, int64_t ldc) {
-  __shared__ float as[16][65], bs[16][65];
-  pdl_begin();
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 64, n0 = static_cast<int64_t>(blockIdx.y) * 64;
-  const int tm = threadIdx.x / 16 * 4, tn = threadIdx.x % 16 * 4;
-  float acc[4][4] = {};
-  for (int64_t k0 = 0; k0 < g.k; k0 += 16) {
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-      const int r = i / 16, k = i % 16;
-      as[k][r] = m0 + r < g.m && k0 + k < g.k ? as_float(a[(m0 + r) * g.am + (k0 + k) * g.ak]) : 0.0f;
-      bs[k][r] = n0 + r < g.n && k0 + k < g.k ? as_float(b[(n0 + r) * g.bn + (k0 + k) * g.bk]) : 0.0f;
-    }
-    __syncthreads();
+constexpr int kDzRows = 128;  // rows of a CTA's part of dz: 8 threads a column group, 16 rows each
+
+template <typename E>
+struct Prepare {
+  Operand<E> x, w, dy;     // dy.out: the planes of dz, or nullptr where dz is dy itself
+  const E* z;
+  int64_t ldz;
+  int wide_z, act;
+  Drop drop;
+  float* part;             // column sums of every kDzRows rows, or nullptr
+  unsigned dz_cols;        // CTAs along the columns
+};
+
+template <typename E, int P>
+__device__ __forceinline__ void copy_planes(unsigned block, const Operand<E>& o) {
+  const int groups = static_cast<int>(o.padded / 8);
+  for (int64_t q = block * int64_t{256} + threadIdx.x; q < o.rows * groups; q += o.blocks * int64_t{256}) {
+    const int64_t r = q / groups;
+    const int c = static_cast<int>(q - r * groups) * 8;
+    E x[8];
+    uint16_t p[8][3];
+    load8(o.p + r * o.ld + c, static_cast<int>(min64(o.cols - c, 8)), o.wide, x);
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(as[k][tm + i], bs[k][tn + j], acc[i][j]);
-    __syncthreads();
+    for (int j = 0; j < 8; ++j) planes_of<E>(x[j], p[j]);
+    store_planes8<P>(o.out + r * o.padded + c, o.rows * o.padded, p);
   }
-  const uint64_t seed = OUT == kLayer && d.level > 0 ? drop_seed(d) : 0;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + tm + i, n = n0 + tn + j;
-      if (m >= g.m || n >= g.n) continue;
-      float v = acc[i][j];
-      if (OUT == kLayer) {
-        if (l.bias != nullptr) v = fadd(v, as_float(static_cast<const T*>(l.bias)[n]));
-        if (l.z != nullptr) put(static_cast<T*>(l.z) + m * l.ldz + n, v);
-        v = act_value<sizeof(T) == 2>(l.act, v);
-        if (d.level > 0) v = kept_at(seed, m * l.out + n, d.level) ? fmul(v, d.scale) : 0.0f;
-        if (l.residual != nullptr) v = fadd(v, as_float(static_cast<const T*>(l.residual)[m * l.ldr + n]));
-      } else {
-        v = fmul(v, d.scale);
+}
+
+// Eight columns a thread, 32 threads along the columns, 8 along the rows.
+template <typename E, int P>
+__device__ __forceinline__ void make_dz(unsigned block, const Prepare<E>& f) {
+  __shared__ float sums[8][256 + 8];
+  const Operand<E>& o = f.dy;
+  const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
+  const int c = static_cast<int>(block % f.dz_cols) * 256 + tc * 8;
+  const int64_t chunk = block / f.dz_cols, first = chunk * kDzRows;
+  const int64_t end = min64(o.rows, first + kDzRows);
+  const int left = static_cast<int>(o.cols - c);
+  const uint64_t seed = f.drop.level > 0 ? drop_seed(f.drop) : 0;
+  float sum[8] = {};
+  if (left > 0) {
+#pragma unroll 2
+    for (int64_t r = first + tr; r < end; r += 8) {
+      E x[8], zs[8];
+      load8(o.p + r * o.ld + c, left, o.wide, x);
+      if (f.act != MPC_ACT_NONE) load8(f.z + r * f.ldz + c, left, f.wide_z, zs);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = to_float(x[j]);
+      if (f.drop.level > 0) {
+        const uint64_t at = static_cast<uint64_t>(r) * o.cols + c;
+        const int off = static_cast<int>(at & 3) * 16;
+        uint64_t d = splitmix64_at(seed, at >> 2);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint64_t use = d;
+          if (off != 0 || q == 0) d = splitmix64_at(seed, (at >> 2) + q + 1);
+          if (off != 0) use = (use >> off) | (d << (64 - off));
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (!kept(use, k, f.drop.level)) v[4 * q + k] = 0.0f;
+        }
       }
-      put(c + m * ldc + n, v);
+      if (f.act != MPC_ACT_NONE) {
+#define MPC_EACH(A) \
+  case A:           \
+    _Pragma("unroll") for (int j = 0; j < 8; ++j) v[j] = fmul(v[j], act_slope<P == 1>(A, to_float(zs[j]))); \
+    break
+        switch (f.act) {
+          MPC_EACH(MPC_ACT_RELU);
+          MPC_EACH(MPC_ACT_GELU);
+          MPC_EACH(MPC_ACT_GELU_TANH);
+          MPC_EACH(MPC_ACT_SILU);
+          default: break;
+        }
+#undef MPC_EACH
+        if (left < 8) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j >= left) v[j] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = fadd(sum[j], v[j]);
+      if (o.out != nullptr) {
+        uint16_t p[8][3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (P == 1) p[j][0] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+          else split(v[j], p[j]);
+        }
+        store_planes8<P>(o.out + r * o.padded + c, o.rows * o.padded, p);
+      }
     }
-}
-
-// dz without dropout's factor, and its sums over 256 rows.
-template <typename T>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const LinearArgs l, const Drop d, T* dz, float* part) {
-  pdl_begin();
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (n >= l.out) return;
-  const uint64_t seed = d.level > 0 ? drop_seed(d) : 0;
-  float sum = 0.0f;
-  const int64_t end = min64(l.rows, (blockIdx.y + int64_t{1}) * 256);
-  for (int64_t m = blockIdx.y * int64_t{256}; m < end; ++m) {
-    float v = as_float(static_cast<const T*>(l.dy)[m * l.lddy + n]);
-    if (d.level > 0 && !kept_at(seed, m * l.out + n, d.level)) v = 0.0f;
-    if (l.act != MPC_ACT_NONE) v = fmul(v, act_slope<sizeof(T) == 2>(l.act, as_float(static_cast<const T*>(l.z_in)[m * l.ldz + n])));
-    sum = fadd(sum, v);
-    put(dz + m * l.out + n, v);
   }
-  part[blockIdx.y * l.out + n] = sum;
+  if (f.part == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[tr][tc * 8 + j] = sum[j];
+  __syncthreads();
+  const int64_t col = static_cast<int64_t>(block % f.dz_cols) * 256 + threadIdx.x;
+  if (col < o.cols) {
+    float v = sums[0][threadIdx.x];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) v = fadd(v, sums[r][threadIdx.x]);
+    f.part[chunk * o.cols + col] = v;
+  }
 }
-template <typename T>
-__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* part, int64_t parts, int64_t out, float scale, T* db) {
+
+template <typename E, int P>
+__global__ void __launch_bounds__(256) linear_prepare_kernel(const Prepare<E> f) {
   pdl_begin();
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (n >= out) return;
+  pdl_end();
+  unsigned block = blockIdx.x;
+  if (block < f.dy.blocks) {
+    make_dz<E, P>(block, f);
+    return;
+  }
+  block -= f.dy.blocks;
+  if (block < f.x.blocks) {
+    copy_planes<E, P>(block, f.x);
+    return;
+  }
+  copy_planes<E, P>(block - f.x.blocks, f.w);
+}
+
+// db from the column sums: 32 columns a CTA, 8 rows of threads.
+template <typename E>
+__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* part, int64_t parts, int64_t out, float scale, E* db) {
+  __shared__ float sums[8][33];
+  pdl_begin();
+  pdl_end();
+  const int64_t col = blockIdx.x * int64_t{32} + (threadIdx.x & 31);
+  const int r = threadIdx.x >> 5;
   float v = 0.0f;
-  for (int64_t p = 0; p < parts; ++p) v = fadd(v, part[p * out + n]);
-  put(db + n, fmul(v, scale));
+  if (col < out) {
+#pragma unroll 4
+    for (int64_t p = r; p < parts; p += 8) v = fadd(v, part[p * out + col]);
+  }
+  sums[r][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (r == 0 && col < out) {
+#pragma unroll
+    for (int p = 1; p < 8; ++p) v = fadd(v, sums[p][threadIdx.x]);
+    put(db + col, fmul(v, scale));
+  }
 }
 
-template <typename T, int OUT>
-cudaError_t product(const T* a, const T* b, const Product& g, const LinearArgs& l, const Drop& d, void* c, int64_t ldc,
-                    cudaStream_t s) {
-  return launch_kernel(linear_tile_kernel<T, OUT>, dim3(static_cast<unsigned>((g.m + 63) / 64), static_cast<unsigned>((g.n + 63) / 64)),
-                       dim3(256), 0, s, 0u, a, b, g, l, d, static_cast<T*>(c), ldc);
+// The parts of a product cut along K, four columns a thread, and what its epilogue would have done.
+template <typename E, bool FORWARD>
+__global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) {
+  pdl_begin();
+  pdl_end();
+  const int groups = (g.n + 3) / 4;
+  const uint64_t seed = FORWARD && g.drop.level > 0 ? drop_seed(g.drop) : 0;
+  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(g.m) * groups;
+       q += gridDim.x * int64_t{256}) {
+    const int64_t m = q / groups;
+    const int n = static_cast<int>(q - m * groups) * 4, left = min(g.n - n, 4);
+    const float* from = g.sum + m * g.lds + n;
+    float4 s = *reinterpret_cast<const float4*>(from);
+#pragma unroll 4
+    for (int p = 1; p < g.splits; ++p) {
+      const float4 a = *reinterpret_cast<const float4*>(from + p * g.sum_split);
+      s = make_float4(fadd(s.x, a.x), fadd(s.y, a.y), fadd(s.z, a.z), fadd(s.w, a.w));
+    }
+    float v[4] = {s.x, s.y, s.z, s.w};
+    if (FORWARD) {
+      if (g.bias != nullptr) add_bias<E, 4>(static_cast<const E*>(g.bias) + n, false, left, v);
+      if (g.z != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < left) put(static_cast<E*>(g.z) + m * g.ldz + n + j, v[j]);
+      }
+      apply_act<4, sizeof(E) == 2>(g.act, v);
+      if (g.drop.level > 0) apply_drop<4>(g.drop, seed, static_cast<uint64_t>(m) * g.n + n, v);
+      if (g.residual != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j < left) v[j] = fadd(as_float(static_cast<const E*>(g.residual)[m * g.ldr + n + j]), v[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = fmul(v[j], g.drop.scale);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) put(static_cast<E*>(g.y) + m * g.ldy + n + j, v[j]);
+  }
 }
 
-size_t up(size_t x) { return (x + 255) / 256 * 256; }
+// ---------------------------------------------------------------------------
+// Workspace and launches
+// ---------------------------------------------------------------------------
+constexpr int kMostSplits = 32;
 
-template <typename T>
-cudaError_t forward(const LinearArgs& a, cudaStream_t s) {
-  const Drop d = make_drop(a.p, a.seed, a.step);
-  const Product g = {a.rows, a.out, a.in, a.ldx, 1, a.ldw, 1};
-  return product<T, kLayer>(static_cast<const T*>(a.x), static_cast<const T*>(a.w), g, a, d, a.y, a.ldy, s);
+struct Layout {
+  size_t x, w, dz, part, sum, total;
+  bool pack_x, pack_w, pack_dy;  // dy: where nothing else makes a dz of it
+  int64_t Kp, Np;
+  Plan forward, dx, dw;
+};
+
+Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_t ldx, int64_t ldw, int64_t lddy) {
+  Layout l = {};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t p = at;
+    at += up(bytes);
+    return p;
+  };
+  const int planes = bf16 ? 1 : 3;
+  l.Kp = round_up(in, 8);
+  l.Np = round_up(out, 8);
+  l.pack_x = !bf16 || ldx < in || ldx % 8 != 0;
+  l.pack_w = !bf16 || ldw < in || ldw % 8 != 0;
+  l.pack_dy = !bf16 || lddy < out || lddy % 8 != 0;
+  l.x = take(l.pack_x ? static_cast<size_t>(planes) * rows * l.Kp * 2 : 0);
+  l.w = take(l.pack_w ? static_cast<size_t>(planes) * out * l.Kp * 2 : 0);
+  auto sums = [](const Plan& p, int64_t m, int64_t ld) { return p.splits > 1 ? static_cast<size_t>(p.splits) * m * ld * 4 : 0; };
+  if (pass == MPC_LINEAR_FORWARD) {
+    l.forward = plan_tiles(rows, out, (in + kK - 1) / kK, planes, 64, kMostSplits);
+    l.sum = take(sums(l.forward, rows, l.Np));
+  } else {
+    l.dz = take(static_cast<size_t>(planes) * rows * l.Np * 2);
+    l.part = take((rows + kDzRows - 1) / kDzRows * out * 4);
+    l.dx = plan_tiles(rows, in, (out + kK - 1) / kK, planes, 64, kMostSplits);
+    l.dw = plan_tiles(out, in, (rows + kK - 1) / kK, planes, 64, kMostSplits);
+    l.sum = take(std::max(sums(l.dx, rows, l.Kp), sums(l.dw, out, l.Kp)));  // dx's are read before dw's are written
+  }
+  l.total = at;
+  return l;
 }
 
-template <typename T>
-cudaError_t backward(const LinearArgs& a, cudaStream_t s) {
-  const Drop d = make_drop(a.p, a.seed, a.step);
-  T* dz = static_cast<T*>(a.ws);
-  float* part = reinterpret_cast<float*>(static_cast<char*>(a.ws) + up(a.rows * a.out * sizeof(T)));
-  const int64_t parts = (a.rows + 255) / 256;
-  cudaError_t e = launch_kernel(linear_dz_kernel<T>, dim3(static_cast<unsigned>((a.out + 255) / 256), static_cast<unsigned>(parts)),
-                                dim3(256), 0, s, 0u, a, d, dz, part);
-  if (e == cudaSuccess && a.dbias != nullptr)
-    e = launch_kernel(linear_dbias_kernel<T>, dim3(static_cast<unsigned>((a.out + 255) / 256)), dim3(256), 0, s, 0u,
-                      static_cast<const float*>(part), parts, a.out, d.scale, static_cast<T*>(a.dbias));
-  if (e == cudaSuccess && a.dx != nullptr)
-    e = product<T, kGrad>(dz, static_cast<const T*>(a.w), Product{a.rows, a.in, a.out, a.out, 1, 1, a.ldw}, a, d, a.dx, a.lddx, s);
-  if (e == cudaSuccess && a.dw != nullptr)
-    e = product<T, kGrad>(dz, static_cast<const T*>(a.x), Product{a.out, a.in, a.rows, 1, a.out, 1, a.ldx}, a, d, a.dw, a.lddw, s);
-  return e;
+bool on16(const void* p, int64_t ld, int size) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0; }
+
+#define LIN_TRY(...)                      \
+  do {                                    \
+    const cudaError_t e_ = (__VA_ARGS__); \
+    if (e_ != cudaSuccess) return e_;     \
+  } while (0)
+
+// One matrix of a product: its planes and how they lie.
+struct Matrix {
+  const void* p;
+  int64_t rows, cols, ld;
+};
+
+template <int MODE, typename E>
+cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, int64_t n, int64_t k, const Plan& plan,
+                    float* sum, int64_t lds, int num_sms, cudaStream_t s) {
+  constexpr int P = sizeof(E) == 2 ? 1 : 3;
+  g.m = static_cast<int>(m);
+  g.n = static_cast<int>(n);
+  g.blocks = static_cast<int>((k + kK - 1) / kK);
+  g.tile_n = plan.tile_n;
+  g.splits = plan.splits;
+  const int64_t mt = (m + kPair - 1) / kPair, nt = (n + plan.tile_n - 1) / plan.tile_n, tiles = mt * nt * plan.splits;
+  if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
+  g.m_tiles = static_cast<int>(mt);
+  g.n_tiles = static_cast<int>(nt);
+  g.group = 8;
+  g.chunk = P == 1 ? 128 : 2;
+  g.sum = plan.splits > 1 ? sum : nullptr;
+  g.lds = lds;
+  g.sum_split = m * lds;
+  const int size = static_cast<int>(sizeof(E));
+  g.mapped = on16(g.y, g.ldy, size) && (g.z == nullptr || on16(g.z, g.ldz, size)) &&
+             (g.residual == nullptr || on16(g.residual, g.ldr, size));
+  CUtensorMap ma, mb, my = {}, mz = {}, mr = {};
+  LIN_TRY(make_map(&ma, a.p, a.cols, a.rows, P, a.ld, a.rows * a.ld, MODE == kDw ? kK : kM));
+  LIN_TRY(make_map(&mb, b.p, b.cols, b.rows, P, b.ld, b.rows * b.ld, MODE == kForward ? plan.tile_n / 2 : kK));
+  if (g.mapped && g.sum == nullptr) {
+    LIN_TRY(make_map(&my, g.y, n, m, 1, g.ldy, m * g.ldy, 32, P == 3));
+    if (g.z != nullptr) LIN_TRY(make_map(&mz, g.z, n, m, 1, g.ldz, m * g.ldz, 32, P == 3));
+    if (g.residual != nullptr) LIN_TRY(make_map(&mr, g.residual, n, m, 1, g.ldr, m * g.ldr, 32, P == 3));
+  }
+  constexpr int smem = LinearTiles<P>::kSmem;
+  LIN_TRY(ensure_dynamic_smem(linear_gemm_kernel<MODE, P>, smem));
+  const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(tiles, num_sms / 2));
+  LIN_TRY(launch_kernel(linear_gemm_kernel<MODE, P>, dim3(grid), dim3(kGemmThreads), smem, s, 2u, ma, mb, my, mz, mr, g));
+  if (g.sum == nullptr) return cudaSuccess;
+  const int64_t blocks = std::min<int64_t>((m * ((n + 3) / 4) + 255) / 256, int64_t{num_sms} * 16);
+  return launch_kernel(linear_finish_kernel<E, MODE == kForward>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0u, g);
+}
+
+template <typename E>
+Operand<E> operand(const void* p, int64_t ld, int64_t rows, int64_t cols, int64_t padded, uint16_t* out, int num_sms) {
+  Operand<E> o = {static_cast<const E*>(p), ld, rows, cols, padded, on16(p, ld, sizeof(E)), out, 0};
+  if (out != nullptr) o.blocks = static_cast<unsigned>(std::min<int64_t>((rows * (padded / 8) + 255) / 256, int64_t{num_sms} * 32));
+  return o;
+}
+
+template <typename E>
+cudaError_t forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int P = sizeof(E) == 2 ? 1 : 3;
+  const Layout l = layout(a.rows, a.in, a.out, P == 1, MPC_LINEAR_FORWARD, on16(a.x, 0, 1) ? a.ldx : 0, on16(a.w, 0, 1) ? a.ldw : 0, 0);
+  char* ws = static_cast<char*>(a.ws);
+  Prepare<E> f = {};
+  if (l.pack_x) f.x = operand<E>(a.x, a.ldx, a.rows, a.in, l.Kp, reinterpret_cast<uint16_t*>(ws + l.x), num_sms);
+  if (l.pack_w) f.w = operand<E>(a.w, a.ldw, a.out, a.in, l.Kp, reinterpret_cast<uint16_t*>(ws + l.w), num_sms);
+  if (f.x.blocks + f.w.blocks > 0)
+    LIN_TRY(launch_kernel(linear_prepare_kernel<E, P>, dim3(f.x.blocks + f.w.blocks), dim3(256), 0, s, 0u, f));
+  LinearGemm g = {};
+  g.bias = a.bias;
+  g.bias_wide = on16(a.bias, 0, 1);
+  g.residual = a.residual;
+  g.ldr = a.ldr;
+  g.y = a.y;
+  g.ldy = a.ldy;
+  g.z = a.z;
+  g.ldz = a.ldz;
+  g.act = a.act;
+  g.drop = make_drop(a.p, a.seed, a.step);
+  g.spin_limit = a.spin_limit;
+  g.status = a.status;
+  const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
+  const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
+  return product<kForward, E>(g, x, w, a.rows, a.out, a.in, l.forward, reinterpret_cast<float*>(ws + l.sum), l.Np, num_sms, s);
+}
+
+template <typename E>
+cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int P = sizeof(E) == 2 ? 1 : 3;
+  const Layout l = layout(a.rows, a.in, a.out, P == 1, MPC_LINEAR_BACKWARD, on16(a.x, 0, 1) ? a.ldx : 0,
+                          on16(a.w, 0, 1) ? a.ldw : 0, on16(a.dy, 0, 1) ? a.lddy : 0);
+  char* ws = static_cast<char*>(a.ws);
+  float* part = reinterpret_cast<float*>(ws + l.part);
+  const bool products = a.dx != nullptr || a.dw != nullptr;
+  Prepare<E> f = {};
+  f.drop = make_drop(a.p, a.seed, a.step);
+  f.act = a.act;
+  f.z = static_cast<const E*>(a.z_in);
+  f.ldz = a.ldz;
+  f.wide_z = on16(a.z_in, a.ldz, sizeof(E));
+  const bool make = products && (l.pack_dy || a.act != MPC_ACT_NONE || f.drop.level > 0);
+  f.dy = operand<E>(a.dy, a.lddy, a.rows, a.out, l.Np, make ? reinterpret_cast<uint16_t*>(ws + l.dz) : nullptr, num_sms);
+  f.part = a.dbias != nullptr ? part : nullptr;
+  const int64_t chunks = (a.rows + kDzRows - 1) / kDzRows, cols = (a.out + 255) / 256;
+  if (chunks * cols > 0x3fffffff) return cudaErrorInvalidValue;
+  f.dz_cols = static_cast<unsigned>(cols);
+  f.dy.blocks = make || a.dbias != nullptr ? static_cast<unsigned>(chunks * cols) : 0;
+  if (l.pack_x && a.dw != nullptr) f.x = operand<E>(a.x, a.ldx, a.rows, a.in, l.Kp, reinterpret_cast<uint16_t*>(ws + l.x), num_sms);
+  if (l.pack_w && a.dx != nullptr) f.w = operand<E>(a.w, a.ldw, a.out, a.in, l.Kp, reinterpret_cast<uint16_t*>(ws + l.w), num_sms);
+  const unsigned blocks = f.dy.blocks + f.x.blocks + f.w.blocks;
+  if (blocks > 0) LIN_TRY(launch_kernel(linear_prepare_kernel<E, P>, dim3(blocks), dim3(256), 0, s, 0u, f));
+  if (a.dbias != nullptr)
+    LIN_TRY(launch_kernel(linear_dbias_kernel<E>, dim3(static_cast<unsigned>((a.out + 31) / 32)), dim3(256), 0, s, 0u,
+                          static_cast<const float*>(part), chunks, a.out, f.drop.scale, static_cast<E*>(a.dbias)));
+  LinearGemm g = {};
+  g.drop = f.drop;
+  g.spin_limit = a.spin_limit;
+  g.status = a.status;
+  float* sum = reinterpret_cast<float*>(ws + l.sum);
+  const Matrix dz = {make ? ws + l.dz : a.dy, a.rows, a.out, make ? l.Np : a.lddy};
+  if (a.dx != nullptr) {
+    const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
+    g.y = a.dx;
+    g.ldy = a.lddx;
+    LIN_TRY(product<kDx, E>(g, dz, w, a.rows, a.in, a.out, l.dx, sum, l.Kp, num_sms, s));
+  }
+  if (a.dw != nullptr) {
+    const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
+    g.y = a.dw;
+    g.ldy = a.lddw;
+    LIN_TRY(product<kDw, E>(g, dz, x, a.out, a.in, a.rows, l.dw, sum, l.Kp, num_sms, s));
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
 
-size_t linear_workspace_bytes(int64_t rows, int64_t, int64_t out, int bf16, int pass, int64_t, int64_t, int64_t) {
-  if (pass == MPC_LINEAR_FORWARD) return 0;
-  return up(rows * out * (bf16 ? 2 : 4)) + up((rows + 255) / 256 * out * 4);
+size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, int pass, int64_t ldx, int64_t ldw, int64_t lddy) {
+  return layout(rows, in, out, bf16 != 0, pass, ldx, ldw, lddy).total;
 }
-cudaError_t launch_linear_forward(const LinearArgs& a, int, cudaStream_t s) {
-  return a.bf16 ? forward<__nv_bfloat16>(a, s) : forward<float>(a, s);
+cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
+  return a.bf16 ? forward<__nv_bfloat16>(a, num_sms, s) : forward<float>(a, num_sms, s);
 }
-cudaError_t launch_linear_backward(const LinearArgs& a, int, cudaStream_t s) {
-  return a.bf16 ? backward<__nv_bfloat16>(a, s) : backward<float>(a, s);
+cudaError_t launch_linear_backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
+  return a.bf16 ? backward<__nv_bfloat16>(a, num_sms, s) : backward<float>(a, num_sms, s);
 }
 
 }  // namespace mpc

@@ -115,43 +115,6 @@ __global__ void __launch_bounds__(kScan)
   }
 }
 
-template <typename E>
-__device__ __forceinline__ void planes_of(E x, uint16_t (&p)[3]);
-template <>
-__device__ __forceinline__ void planes_of<float>(float x, uint16_t (&p)[3]) { split(x, p); }
-template <>
-__device__ __forceinline__ void planes_of<__nv_bfloat16>(__nv_bfloat16 x, uint16_t (&p)[3]) {
-  p[0] = __bfloat16_as_ushort(x);
-}
-
-// Eight elements from p on; those from `left` on are zero.
-template <typename E>
-__device__ __forceinline__ void load8(const E* p, int left, bool wide, E (&x)[8]) {
-  if (wide && left >= 8) {
-    uint4 u[sizeof(E) / 2];
-#pragma unroll
-    for (int k = 0; k < static_cast<int>(sizeof(E)) / 2; ++k) u[k] = reinterpret_cast<const uint4*>(p)[k];
-    memcpy(x, u, sizeof(x));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = j < left ? p[j] : E(0.0f);
-  }
-}
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-template <int P>
-__device__ __forceinline__ void store_planes8(uint16_t* out, int64_t plane, const uint16_t (&p)[8][3]) {
-#pragma unroll
-  for (int k = 0; k < P; ++k) {
-    uint4 u;
-    u.x = p[0][k] | static_cast<uint32_t>(p[1][k]) << 16;
-    u.y = p[2][k] | static_cast<uint32_t>(p[3][k]) << 16;
-    u.z = p[4][k] | static_cast<uint32_t>(p[5][k]) << 16;
-    u.w = p[6][k] | static_cast<uint32_t>(p[7][k]) << 16;
-    *reinterpret_cast<uint4*>(out + k * plane) = u;
-  }
-}
 // Eight values of packed planes.
 template <int P>
 __device__ __forceinline__ void load_planes8(const uint16_t* in, int64_t plane, float (&x)[8]) {
@@ -664,9 +627,6 @@ __global__ void __launch_bounds__(256)
 // ---------------------------------------------------------------------------
 // Workspace and launches
 // ---------------------------------------------------------------------------
-size_t up(size_t x) { return (x + 255) / 256 * 256; }
-int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-
 // The coefficients of a piece take 1 GiB at most (0.4 % of the memory; a shorter
 // vocabulary piece makes smaller products and more launches).
 constexpr int64_t kPieceBytes = int64_t{1} << 30;
@@ -689,40 +649,7 @@ struct Layout {
   int64_t piece, padded, Dp, ldc;
 };
 
-// Widths of tiles, and parts of K for dh, by an estimate of the products' time in
-// cycles: waves of tiles over the SM pairs, a K block of a tile bound by its copies
-// from L2 (about 60 bytes a cycle an SM: in bf16 546 cycles for 256 columns, 410
-// for 128, 341 for 64) or its products (512, 256, 128; in fp32 six times as many on
-// three times the bytes), an epilogue a tile, and for each part its sums written
-// and read once more.
-constexpr int kPairs = 76;  // of the 152 SMs
-constexpr int kMaxSplits = 32;
-
-struct Plan {
-  int tile_n, splits;
-};
-
-Plan plan_tiles(int64_t m, int64_t n, int64_t blocks, int planes, int narrowest, int most_splits) {
-  Plan best = {kN, 1};
-  double least = 1e300;
-  const int64_t mt = (m + kPair - 1) / kPair;
-  for (int tn = kN; tn >= narrowest; tn /= 2) {
-    const int64_t nt = (n + tn - 1) / tn;
-    const double copies = planes * (kBytesA + tn / 2 * kK * 2) / 60.0, products = (planes == 1 ? 2.0 : 12.0) * tn;
-    const double step = std::max(copies, products), end = 1000.0 + 3000.0 * tn / kN;
-    for (int s = 1; s <= most_splits && s <= std::max<int64_t>(blocks, 1); ++s) {
-      const int64_t waves = (mt * nt * s + kPairs - 1) / kPairs;
-      const double sums = s > 1 ? static_cast<double>(s) * m * n * 8.0 / 3500.0 : 0.0;
-      const double cost = waves * (((blocks + s - 1) / s) * step + end) + sums;
-      if (cost < 0.98 * least) {
-        least = cost;
-        best = Plan{tn, s};
-      }
-    }
-  }
-  return best;
-}
-
+constexpr int kMaxSplits = 32;  // parts of K for dh
 // dw in parts needs its sums and one more pass, for a vocabulary of few tiles.
 constexpr int kMostDwSplits = 16;
 Plan plan_dw(int64_t T, int64_t D, int64_t piece, int planes) {
@@ -784,39 +711,6 @@ Layout layout(int64_t T, int64_t D, int64_t V, bool bf16, int pass, int64_t piec
   }
   l.total = at;
   return l;
-}
-
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encoder() {
-  static EncodeFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeFn>(p);
-  }();
-  return fn;
-}
-
-// A map over [planes][rows][cols] bf16 with rows ld elements apart, read in boxes
-// of 64 columns x box_rows rows; what lies outside reads as zero.
-cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int planes, int64_t ld,
-                     int64_t plane, int box_rows) {
-  const cuuint64_t size[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
-                              static_cast<cuuint64_t>(planes)};
-  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(plane) * 2};
-  const cuuint32_t box[3] = {kK, static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
-  const EncodeFn fn = encoder();
-  if (fn == nullptr) return cudaErrorNotSupported;
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), size, stride, box, step,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
-             ? cudaSuccess
-             : cudaErrorInvalidValue;
 }
 
 template <int MODE, int PLANES>

@@ -2,25 +2,13 @@
 // tensor cores, with the softmax in their epilogues.
 #pragma once
 
-#include <cuda_bf16.h>
-
-#include "tcgen05.cuh"
+#include "gemm_tiles.cuh"
 
 namespace mpc {
 namespace {
 
-constexpr int kM = 128;        // rows of a CTA's output tile (lanes of tensor memory)
-constexpr int kPair = 2 * kM;  // rows of a CTA pair's output tile
-constexpr int kN = 256;        // columns of an output tile
-constexpr int kK = 64;         // K elements of a stage: 128 bytes, one swizzle row
 constexpr int kStages = 6;    // of one plane; fp32 has kStages / 3 of three
-constexpr int kBytesA = kM * kK * 2;
-constexpr int kBytesB = kN / 2 * kK * 2;
-constexpr int kStageBytes = kBytesA + kBytesB;
-constexpr int kEpiWarps = 8;
 constexpr int kStoreBytes = 4096;  // of an epilogue warp's stores of c
-constexpr int kGemmThreads = (2 + kEpiWarps) * 32;
-constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
 constexpr int kRun = 16;       // sorted tokens whose target gradients one CTA sums
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -30,23 +18,6 @@ struct Header {
   float mean;  // 1 / valid (0 when none counts)
   int redo;    // some token's exponentials are formed again (see kExp)
 };
-
-// ---------------------------------------------------------------------------
-// Operands in bf16 planes.  A bf16 tensor is one plane.  An fp32 x is the sum of
-// three, x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1) (24 bits), and a
-// product of two fp32 tensors the sum of the plane products i + j <= 2, six of
-// them: what is left out is below 2^-24 of a term.  One kernel so serves both
-// types, an fp32 product being a bf16 one with six times the K steps.
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ void split(float x, uint16_t (&p)[3]) {
-  const __nv_bfloat16 a = __float2bfloat16_rn(x);
-  const float r = fsub(x, __bfloat162float(a));
-  const __nv_bfloat16 b = __float2bfloat16_rn(r);
-  const __nv_bfloat16 c = __float2bfloat16_rn(fsub(r, __bfloat162float(b)));
-  p[0] = __bfloat16_as_ushort(a);
-  p[1] = __bfloat16_as_ushort(b);
-  p[2] = __bfloat16_as_ushort(c);
-}
 
 // ---------------------------------------------------------------------------
 // The matrix products: C[m][n] = sum_k A[m][k] B[n][k] in 256 x 256 tiles.
@@ -139,17 +110,6 @@ struct Gemm {
   unsigned* status;
 };
 
-// Plane pair of a product, smallest products first.
-template <int PLANES>
-__device__ __forceinline__ void term_planes(int t, int* a, int* b) {
-  if (PLANES == 1) {
-    *a = *b = 0;
-  } else {  // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0), two bits each
-    *a = (0x052 >> (2 * t)) & 3;
-    *b = (0x118 >> (2 * t)) & 3;
-  }
-}
-
 // What an epilogue needs of its row, loaded before the tile is waited for.
 struct Row {
   int target;
@@ -205,13 +165,6 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-  uint32_t u;
-  memcpy(&u, &p, 4);
-  return u;
-}
-
 // A warp's 32 rows of a half tile as bf16 planes of the coefficients, by tensor-map
 // stores of 64 columns from its 4 KB of shared memory: a row's 16-byte groups lie
 // swizzled, so the lanes' writes meet in no bank, and HBM gets whole lines (one
@@ -472,12 +425,6 @@ __device__ __forceinline__ bool skipped(const Gemm& g, const Tile& t) {
   return MODE == kExp && g.redo != nullptr && g.redo[t.m0 / kPair] == 0;
 }
 
-// Columns of a tile that the product forms: a multiple of 16.  Each CTA of the
-// pair holds half of them as rows of B.
-__device__ __forceinline__ int tile_cols(const Gemm& g, int cols, int n0) {
-  return min((cols - n0 + 15) / 16 * 16, g.tile_n);
-}
-
 template <int MODE, int PLANES>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     ce_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -534,7 +481,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       for (int i = pair; i < total && ok; i += pairs) {
         const Tile t = tile_of<MODE>(g, s, i);
         if (skipped<MODE>(g, t)) continue;
-        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g, cols, t.n0) / 2);
+        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(cols, t.n0, g.tile_n) / 2);
         for (int kb = t.k0; kb < t.k1; ++kb, ++it) {
           const int st = it % stages;
           ok = mbar_wait_bounded(&empty[st], (it / stages & 1) ^ 1, g.spin_limit, g.status);
@@ -583,7 +530,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       for (int i = pair; i < total && ok; i += pairs) {
         const Tile t = tile_of<MODE>(g, s, i);
         if (skipped<MODE>(g, t)) continue;
-        const uint32_t idesc = mma_desc(kPair, tile_cols(g, cols, t.n0), A_MN, B_MN);
+        const uint32_t idesc = mma_desc(kPair, tile_cols(cols, t.n0, g.tile_n), A_MN, B_MN);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
           ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
           tc_fence_after();

@@ -55,6 +55,14 @@ def test_sizes(mpc, M, K, N, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("act,residual", [(None, True), ("gelu", True), ("silu", False)])
+@pytest.mark.parametrize("M,K,N", [(4128, 520, 2056), (3001, 331, 3203), (1030, 2100, 4104), (130, 4500, 96)])
+def test_many_tiles(mpc, M, K, N, act, residual, kind):
+    """More tiles than the SMs take at once, whole and ragged, and long sums."""
+    check(mpc, *make(M, M, K, N, forms.KINDS[kind], True, residual), act=act, p=0.1, seed=5)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("act", [None, "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("bias,residual,p", [(False, False, 0.0), (True, False, 0.0), (False, True, 0.5), (True, True, 0.25)])
 @pytest.mark.parametrize("M,K,N", [(5, 40, 72), (150, 136, 200), (131, 99, 143)])
