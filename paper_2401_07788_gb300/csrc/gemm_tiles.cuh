@@ -152,18 +152,17 @@ EncodeFn encoder() {
   return fn;
 }
 
-// A map over [planes][rows][cols] bf16 (or fp32) with rows ld elements apart, in boxes
-// of 128 bytes x box_rows rows; what lies outside reads as zero and is not written.
+// A map over [planes][rows][cols] bf16 with rows ld elements apart, in boxes
+// of 64 columns x box_rows rows; what lies outside reads as zero and is not written.
 cudaError_t make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int planes, int64_t ld,
-                     int64_t plane, int box_rows, bool fp32 = false) {
-  const int size_of = fp32 ? 4 : 2;
+                     int64_t plane, int box_rows) {
   const cuuint64_t size[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
                               static_cast<cuuint64_t>(planes)};
-  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld) * size_of, static_cast<cuuint64_t>(plane) * size_of};
-  const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / size_of), static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
+  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(plane) * 2};
+  const cuuint32_t box[3] = {kK, static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
   const EncodeFn fn = encoder();
   if (fn == nullptr) return cudaErrorNotSupported;
-  return fn(map, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), size, stride, box, step,
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), size, stride, box, step,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? cudaSuccess

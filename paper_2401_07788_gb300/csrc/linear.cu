@@ -180,22 +180,28 @@ __global__ void __launch_bounds__(256) linear_dbias_kernel(const float* part, in
   }
 }
 
-// The parts of a product cut along K, four columns a thread, and what its epilogue would have done.
+// The tiles that were formed in parts of K, four columns a thread, and what the epilogue would have
+// done.
 template <typename E, bool FORWARD>
 __global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) {
   pdl_begin();
   pdl_end();
-  const int groups = (g.n + 3) / 4;
+  const int rest = g.m_tiles * g.n_tiles - g.whole, groups = g.tile_n / 4;
+  const int64_t part = static_cast<int64_t>(rest) * kPair * g.tile_n;
   const uint64_t seed = FORWARD && g.drop.level > 0 ? drop_seed(g.drop) : 0;
-  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(g.m) * groups;
+  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(rest) * kPair * groups;
        q += gridDim.x * int64_t{256}) {
-    const int64_t m = q / groups;
-    const int n = static_cast<int>(q - m * groups) * 4, left = min(g.n - n, 4);
-    const float* from = g.sum + m * g.lds + n;
+    const int row = static_cast<int>(q / groups), col = static_cast<int>(q - static_cast<int64_t>(row) * groups) * 4;
+    int m0, n0;
+    place_tile(g, g.whole + row / kPair, &m0, &n0);
+    const int64_t m = m0 + row % kPair;
+    const int n = n0 + col, left = min(g.n - n, 4);
+    if (m >= g.m || left <= 0) continue;
+    const float* from = g.sum + static_cast<int64_t>(row) * g.tile_n + col;
     float4 s = *reinterpret_cast<const float4*>(from);
 #pragma unroll 4
     for (int p = 1; p < g.splits; ++p) {
-      const float4 a = *reinterpret_cast<const float4*>(from + p * g.sum_split);
+      const float4 a = *reinterpret_cast<const float4*>(from + p * part);
       s = make_float4(fadd(s.x, a.x), fadd(s.y, a.y), fadd(s.z, a.z), fadd(s.w, a.w));
     }
     float v[4] = {s.x, s.y, s.z, s.w};
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) 
         for (int j = 0; j < 4; ++j)
           if (j < left) v[j] = fadd(as_float(static_cast<const E*>(g.residual)[m * g.ldr + n + j]), v[j]);
       }
-    } else {
+    } else if (g.drop.level > 0) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = fmul(v[j], g.drop.scale);
     }
@@ -226,13 +232,57 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) 
 // ---------------------------------------------------------------------------
 // Workspace and launches
 // ---------------------------------------------------------------------------
+// Tile width and parts of K.  All pairs of SMs form whole tiles as long as there is one for each
+// of them; what is left over can be cut into parts along K, which then fill the pairs once
+// more, at the price of their sums, written and read, and of a launch.  Estimated in cycles:
+// a K block of a tile takes its products (512 for 256 columns in bf16, six times that in
+// fp32) or its copies from L2 (about 55 bytes a cycle an SM) and a little more; what is
+// exposed at the ends is the first copies and the last tile's epilogue.
+struct Cut {
+  int tile_n, splits;
+  int64_t whole;  // tiles in one piece
+};
 constexpr int kMostSplits = 32;
+
+Cut cut_tiles(int64_t m, int64_t n, int64_t blocks, int planes) {
+  Cut best = {kN, 1, 0};
+  double least = 1e300;
+  const int64_t mt = (m + kPair - 1) / kPair;
+  for (int tn = kN; tn >= 64; tn -= 64) {
+    const int64_t nt = (n + tn - 1) / tn, tiles = mt * nt, full = tiles / kPairs * kPairs, rest = tiles - full;
+    const double copies = planes * (kBytesA + tn / 2 * kK * 2) / 55.0, products = (planes == 1 ? 2.0 : 12.0) * tn;
+    const double step = std::max(copies, products) + 20.0, end = 3000.0 + 4000.0 * tn / kN;
+    const double tile = std::max(blocks * step, 3000.0 * tn / kN);  // or its epilogue
+    for (int s = 1; s <= kMostSplits && s <= blocks; ++s) {
+      if (s > 1 && rest == 0) break;
+      double cost = tiles / kPairs * tile + end;
+      if (s == 1) {
+        cost += rest > 0 ? tile : 0.0;
+      } else {
+        const int64_t waves = (rest * s + kPairs - 1) / kPairs;
+        cost += waves * (((blocks + s - 1) / s) * step + 500.0) + 3000.0 +
+                static_cast<double>(rest) * s * kPair * tn * 8.0 / 3500.0;
+      }
+      if (cost < 0.98 * least) {
+        least = cost;
+        best = Cut{tn, s, s == 1 ? tiles : full};
+      }
+    }
+  }
+  return best;
+}
+// Bytes of the sums.
+size_t cut_bytes(const Cut& c, int64_t m, int64_t n) {
+  if (c.splits == 1) return 0;
+  const int64_t tiles = (m + kPair - 1) / kPair * ((n + c.tile_n - 1) / c.tile_n);
+  return static_cast<size_t>((tiles - c.whole) * c.splits) * kPair * c.tile_n * 4;
+}
 
 struct Layout {
   size_t x, w, dz, part, sum, total;
   bool pack_x, pack_w, pack_dy;  // dy: where nothing else makes a dz of it
   int64_t Kp, Np;
-  Plan forward, dx, dw;
+  Cut forward, dx, dw;
 };
 
 Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_t ldx, int64_t ldw, int64_t lddy) {
@@ -251,16 +301,15 @@ Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_
   l.pack_dy = !bf16 || lddy < out || lddy % 8 != 0;
   l.x = take(l.pack_x ? static_cast<size_t>(planes) * rows * l.Kp * 2 : 0);
   l.w = take(l.pack_w ? static_cast<size_t>(planes) * out * l.Kp * 2 : 0);
-  auto sums = [](const Plan& p, int64_t m, int64_t ld) { return p.splits > 1 ? static_cast<size_t>(p.splits) * m * ld * 4 : 0; };
   if (pass == MPC_LINEAR_FORWARD) {
-    l.forward = plan_tiles(rows, out, (in + kK - 1) / kK, planes, 64, kMostSplits);
-    l.sum = take(sums(l.forward, rows, l.Np));
+    l.forward = cut_tiles(rows, out, (in + kK - 1) / kK, planes);
+    l.sum = take(cut_bytes(l.forward, rows, out));
   } else {
     l.dz = take(static_cast<size_t>(planes) * rows * l.Np * 2);
     l.part = take((rows + kDzRows - 1) / kDzRows * out * 4);
-    l.dx = plan_tiles(rows, in, (out + kK - 1) / kK, planes, 64, kMostSplits);
-    l.dw = plan_tiles(out, in, (rows + kK - 1) / kK, planes, 64, kMostSplits);
-    l.sum = take(std::max(sums(l.dx, rows, l.Kp), sums(l.dw, out, l.Kp)));  // dx's are read before dw's are written
+    l.dx = cut_tiles(rows, in, (out + kK - 1) / kK, planes);
+    l.dw = cut_tiles(out, in, (rows + kK - 1) / kK, planes);
+    l.sum = take(std::max(cut_bytes(l.dx, rows, in), cut_bytes(l.dw, out, in)));  // dx's are read before dw's are written
   }
   l.total = at;
   return l;
@@ -281,40 +330,41 @@ struct Matrix {
 };
 
 template <int MODE, typename E>
-cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, int64_t n, int64_t k, const Plan& plan,
-                    float* sum, int64_t lds, int num_sms, cudaStream_t s) {
-  constexpr int P = sizeof(E) == 2 ? 1 : 3;
+cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, int64_t n, int64_t k, const Cut& cut,
+                    float* sum, int num_sms, cudaStream_t s) {
+  constexpr int P = sizeof(E) == 2 ? 1 : 3, size = static_cast<int>(sizeof(E));
+  const int64_t mt = (m + kPair - 1) / kPair, nt = (n + cut.tile_n - 1) / cut.tile_n;
+  const int64_t rest = mt * nt - cut.whole, units = cut.whole + rest * cut.splits;
+  if (units > 0x7fffffff - num_sms || rest * kPair > 0x7fffffff) return cudaErrorInvalidValue;
   g.m = static_cast<int>(m);
   g.n = static_cast<int>(n);
   g.blocks = static_cast<int>((k + kK - 1) / kK);
-  g.tile_n = plan.tile_n;
-  g.splits = plan.splits;
-  const int64_t mt = (m + kPair - 1) / kPair, nt = (n + plan.tile_n - 1) / plan.tile_n, tiles = mt * nt * plan.splits;
-  if (tiles > 0x7fffffff - num_sms) return cudaErrorInvalidValue;
   g.m_tiles = static_cast<int>(mt);
   g.n_tiles = static_cast<int>(nt);
+  g.whole = static_cast<int>(cut.whole);
+  g.splits = cut.splits;
+  g.tile_n = cut.tile_n;
   g.group = 8;
   g.chunk = P == 1 ? 128 : 2;
-  g.sum = plan.splits > 1 ? sum : nullptr;
-  g.lds = lds;
-  g.sum_split = m * lds;
-  const int size = static_cast<int>(sizeof(E));
-  g.mapped = on16(g.y, g.ldy, size) && (g.z == nullptr || on16(g.z, g.ldz, size)) &&
-             (g.residual == nullptr || on16(g.residual, g.ldr, size));
-  CUtensorMap ma, mb, my = {}, mz = {}, mr = {};
+  g.sum = sum;
+  auto on = [&](uintptr_t bytes) {
+    auto fits = [&](const void* q, int64_t ld) {
+      return q == nullptr || (reinterpret_cast<uintptr_t>(q) % bytes == 0 && ld * size % static_cast<int64_t>(bytes) == 0);
+    };
+    return fits(g.y, g.ldy) && fits(g.z, g.ldz) && fits(g.residual, g.ldr);
+  };
+  g.wide = on(32) ? 2 : on(16) ? 1 : 0;
+  CUtensorMap ma, mb;
   LIN_TRY(make_map(&ma, a.p, a.cols, a.rows, P, a.ld, a.rows * a.ld, MODE == kDw ? kK : kM));
-  LIN_TRY(make_map(&mb, b.p, b.cols, b.rows, P, b.ld, b.rows * b.ld, MODE == kForward ? plan.tile_n / 2 : kK));
-  if (g.mapped && g.sum == nullptr) {
-    LIN_TRY(make_map(&my, g.y, n, m, 1, g.ldy, m * g.ldy, 32, P == 3));
-    if (g.z != nullptr) LIN_TRY(make_map(&mz, g.z, n, m, 1, g.ldz, m * g.ldz, 32, P == 3));
-    if (g.residual != nullptr) LIN_TRY(make_map(&mr, g.residual, n, m, 1, g.ldr, m * g.ldr, 32, P == 3));
-  }
+  LIN_TRY(make_map(&mb, b.p, b.cols, b.rows, P, b.ld, b.rows * b.ld, MODE == kForward ? cut.tile_n / 2 : kK));
+  const bool one = P == 1 && g.blocks <= g.chunk;
+  const auto kernel = one ? linear_gemm_kernel<MODE, P, P == 1> : linear_gemm_kernel<MODE, P, false>;
   constexpr int smem = LinearTiles<P>::kSmem;
-  LIN_TRY(ensure_dynamic_smem(linear_gemm_kernel<MODE, P>, smem));
-  const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(tiles, num_sms / 2));
-  LIN_TRY(launch_kernel(linear_gemm_kernel<MODE, P>, dim3(grid), dim3(kGemmThreads), smem, s, 2u, ma, mb, my, mz, mr, g));
-  if (g.sum == nullptr) return cudaSuccess;
-  const int64_t blocks = std::min<int64_t>((m * ((n + 3) / 4) + 255) / 256, int64_t{num_sms} * 16);
+  LIN_TRY(ensure_dynamic_smem(kernel, smem));
+  const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(units, num_sms / 2));
+  LIN_TRY(launch_kernel(kernel, dim3(grid), dim3(kLinearThreads), smem, s, 2u, ma, mb, g));
+  if (rest == 0) return cudaSuccess;
+  const int64_t blocks = std::min<int64_t>(rest * (kPair / 4) * cut.tile_n / 256, int64_t{num_sms} * 16);
   return launch_kernel(linear_finish_kernel<E, MODE == kForward>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0u, g);
 }
 
@@ -350,7 +400,7 @@ cudaError_t forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   g.status = a.status;
   const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
   const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
-  return product<kForward, E>(g, x, w, a.rows, a.out, a.in, l.forward, reinterpret_cast<float*>(ws + l.sum), l.Np, num_sms, s);
+  return product<kForward, E>(g, x, w, a.rows, a.out, a.in, l.forward, reinterpret_cast<float*>(ws + l.sum), num_sms, s);
 }
 
 template <typename E>
@@ -391,13 +441,13 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
     const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
     g.y = a.dx;
     g.ldy = a.lddx;
-    LIN_TRY(product<kDx, E>(g, dz, w, a.rows, a.in, a.out, l.dx, sum, l.Kp, num_sms, s));
+    LIN_TRY(product<kDx, E>(g, dz, w, a.rows, a.in, a.out, l.dx, sum, num_sms, s));
   }
   if (a.dw != nullptr) {
     const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
     g.y = a.dw;
     g.ldy = a.lddw;
-    LIN_TRY(product<kDw, E>(g, dz, x, a.out, a.in, a.rows, l.dw, sum, l.Kp, num_sms, s));
+    LIN_TRY(product<kDw, E>(g, dz, x, a.out, a.in, a.rows, l.dw, sum, num_sms, s));
   }
   return cudaSuccess;
 }

@@ -15,12 +15,15 @@ namespace {
 // kDx       A = dz [rows][out], B = w^T [in][out]   (B read as it is: rows of 64 entries of `in`)
 // kDw       A = dz^T [out][rows], B = x^T [in][rows]  (both read as they are)
 //
-// Warp 0 copies operand tiles through tensor maps, one thread of the first CTA's warp 1
-// issues the products of both CTAs, eight warps a CTA take the finished tile from tensor
-// memory, which holds two accumulators: a tile's epilogue runs under the next one's
-// products.  bf16: five stages of 32 KB a CTA and two 4 KB boxes an epilogue warp for what
-// it loads and stores (32 rows of 128 bytes, by tensor maps); fp32: two stages of three
-// planes, which serve six plane products, and one box.
+// Warp 0 copies operand tiles through tensor maps (six stages of 32 KB a CTA; fp32: two of
+// three planes, which serve six plane products), one thread of the first CTA's warp 1 issues
+// the products of both CTAs, sixteen warps a CTA take the finished tile from tensor memory, 32
+// rows by 64 columns each.  Tensor memory holds two accumulators: a tile's epilogue runs
+// under the next one's products, and has to be no longer than those.  What it takes is
+// latency: the matrix units and the copies leave little of shared memory's bandwidth, so results
+// go from registers to global memory, 64 bytes a lane, and four warps a scheduler hide the
+// exponentials of one another (8192 x 1024 x 4096 with gelu_tanh: eight warps that hand their rows
+// through shared memory take 89 us).
 //
 // An accumulator truncates as it adds (1.7e-7 of a large value a step of 16 at most), so it
 // sums `chunk` K blocks, and the epilogue adds the chunks in fp32 rounded to nearest: 2
@@ -31,12 +34,13 @@ enum LinearMode { kForward, kDx, kDw };
 struct LinearGemm {
   int m, n;            // of C
   int blocks;          // K blocks of 64
-  int m_tiles, n_tiles, splits;
+  int m_tiles, n_tiles;
+  int whole;           // tiles formed in one piece; the others, the last ones, in `splits` parts of K
+  int splits;
   int group;           // row tiles that run together over all columns
   int tile_n, chunk;
-  float* sum;          // parts of K (else nullptr): [split][m][lds]
-  int64_t lds, sum_split;
-  int mapped;          // y, z and residual go through tensor maps
+  float* sum;          // [split][tiles in parts][256][tile_n]
+  int wide;            // y, z and residual have rows on 16 bytes (1), on 32 (2)
   const void* bias;
   int bias_wide;
   const void* residual;
@@ -51,80 +55,181 @@ struct LinearGemm {
   unsigned* status;
 };
 
+constexpr int kLinearEpi = 16;                      // epilogue warps
+constexpr int kLinearThreads = (2 + kLinearEpi) * 32;
+constexpr int kLinearCols = kN / (kLinearEpi / 4);  // columns of one of them
+constexpr int kLinearBox = 2048;                    // 32 rows of 64 bytes, where rows lie on no 16 bytes
+
 template <int PLANES>
 struct LinearTiles {
-  static constexpr int kStages = PLANES == 1 ? 5 : 2;
-  static constexpr int kBoxes = PLANES == 1 ? 2 : 1;  // of an epilogue warp
-  static constexpr int kBoxBytes = 4096;
-  static constexpr int kSmem = kStages * PLANES * kStageBytes + kEpiWarps * kBoxes * kBoxBytes + 1024;
+  static constexpr int kStages = 6 / PLANES;
+  static constexpr int kSmem = kStages * PLANES * kStageBytes + kLinearEpi * kLinearBox + 1024;
 };
 
 struct LinearTile {
-  int m0, n0, split, k0, k1;  // K blocks [k0, k1)
+  int m0, n0, k0, k1;  // K blocks [k0, k1)
+  int slot;            // of the sums, -1: a whole tile
 };
 // The tiles that run at the same time, one a pair, are `group` row tiles by as many column
 // tiles: of 76 pairs, 8 x 9.5 read 18 strips of operands where one row tile after the
 // other over all of a large x would read it from HBM once a wave.
-__device__ __forceinline__ LinearTile linear_tile(const LinearGemm& g, int i) {
-  LinearTile t;
-  const int per_split = g.m_tiles * g.n_tiles;
-  t.split = i / per_split;
-  i -= t.split * per_split;
+__device__ __forceinline__ void place_tile(const LinearGemm& g, int i, int* m0, int* n0) {
   const int band = g.group * g.n_tiles, b = i / band, first = b * g.group;
   const int rows = min(g.group, g.m_tiles - first);
   i -= b * band;
-  t.m0 = (first + i % rows) * kPair;
-  t.n0 = i / rows * g.tile_n;
-  t.k0 = static_cast<int>(static_cast<int64_t>(g.blocks) * t.split / g.splits);
-  t.k1 = static_cast<int>(static_cast<int64_t>(g.blocks) * (t.split + 1) / g.splits);
+  *m0 = (first + i % rows) * kPair;
+  *n0 = i / rows * g.tile_n;
+}
+__device__ __forceinline__ int linear_units(const LinearGemm& g) {
+  return g.whole + (g.m_tiles * g.n_tiles - g.whole) * g.splits;
+}
+__device__ __forceinline__ LinearTile linear_tile(const LinearGemm& g, int i) {
+  LinearTile t;
+  if (i < g.whole) {
+    t.slot = -1;
+    t.k0 = 0;
+    t.k1 = g.blocks;
+  } else {
+    const int rest = g.m_tiles * g.n_tiles - g.whole;
+    t.slot = i - g.whole;
+    const int split = t.slot / rest;
+    i = g.whole + t.slot - split * rest;
+    t.k0 = static_cast<int>(static_cast<int64_t>(g.blocks) * split / g.splits);
+    t.k1 = static_cast<int>(static_cast<int64_t>(g.blocks) * (split + 1) / g.splits);
+  }
+  place_tile(g, i, &t.m0, &t.n0);
   return t;
 }
 
-// A lane's 128 bytes of a box of 32 rows, 16-byte groups swizzled as the tensor maps do.
+// 32 columns of a lane's row, from `p` on, of which `left` exist; rows on 16 (or 32) bytes.
 template <typename T>
-__device__ __forceinline__ void box_put(uint8_t* box, const float* v) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void store_wide(T* p, int left, bool wider, const float (&v)[32]) {
+  constexpr int V = kVec<T>;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    float f[kVec<T>];
+  for (int c = 0; c < 32 / V; c += 2) {
+    float f[2][V];
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) f[i] = v[c * kVec<T> + i];
-    *reinterpret_cast<uint4*>(box + lane * 128 + ((c ^ (lane & 7)) * 16)) = pack16(f);
+    for (int i = 0; i < 2 * V; ++i) f[i / V][i % V] = v[c * V + i];
+    const uint4 a = pack16(f[0]), b = pack16(f[1]);
+    if (wider && left >= (c + 2) * V) {
+      const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      st_v8(p + c * V, u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (left >= (c + e + 1) * V) {
+          *reinterpret_cast<uint4*>(p + (c + e) * V) = e == 0 ? a : b;
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i)
+            if ((c + e) * V + i < left) put(p + (c + e) * V + i, f[e][i]);
+        }
+      }
+    }
+  }
+}
+// The residual's bytes, asked for before they are wanted.
+template <typename T>
+struct Ahead {
+  uint4 u[32 / kVec<T>];
+};
+template <typename T>
+__device__ __forceinline__ void load_wide(const T* p, int left, Ahead<T>& a) {
+  constexpr int V = kVec<T>;
+#pragma unroll
+  for (int c = 0; c < 32 / V; ++c) {
+    if (left >= (c + 1) * V) {
+      a.u[c] = *reinterpret_cast<const uint4*>(p + c * V);
+    } else {
+      float f[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] = c * V + i < left ? as_float(p[c * V + i]) : 0.0f;
+      a.u[c] = pack16(f);
+    }
   }
 }
 template <typename T>
-__device__ __forceinline__ void box_add(const uint8_t* box, float* v) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void add_ahead(const Ahead<T>& a, float (&v)[32]) {
+  constexpr int V = kVec<T>;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    float f[kVec<T>];
-    unpack16(*reinterpret_cast<const uint4*>(box + lane * 128 + ((c ^ (lane & 7)) * 16)), f);
+  for (int c = 0; c < 32 / V; ++c) {
+    float f[V];
+    unpack16(a.u[c], f);
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) v[c * kVec<T> + i] = fadd(f[i], v[c * kVec<T> + i]);
+    for (int i = 0; i < V; ++i) v[c * V + i] = fadd(f[i], v[c * V + i]);
   }
 }
+
+// The same where rows lie on no 16 bytes, by way of a warp's 2 KB of shared memory, so that
+// neighbouring lanes take neighbouring entries: 64 bytes of 32 rows at a time, a row's
+// words swizzled by its number.
 template <typename T>
-__device__ __forceinline__ T* box_at(uint8_t* box, int row, int col) {
-  const int at = col * static_cast<int>(sizeof(T));
-  return reinterpret_cast<T*>(box + row * 128 + (((at >> 4) ^ (row & 7)) << 4) + (at & 15));
+__device__ __forceinline__ uint32_t* box_word(uint8_t* box, int row, int word) {
+  return reinterpret_cast<uint32_t*>(box) + row * 16 + (word ^ (row & 15));
 }
-// A box to or from rows that tensor maps do not reach: neighbouring lanes neighbouring entries.
 template <typename T, bool LOAD>
-__device__ __forceinline__ void box_rows(uint8_t* box, T* p, int64_t ld, int rows, int cols) {
-  constexpr int W = 128 / sizeof(T);
+__device__ __forceinline__ void box_rows(uint8_t* box, T* p, int64_t ld, int rows, int left) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
+  if (sizeof(T) == 2) {
 #pragma unroll 8
-  for (int r = 0; r < 32; ++r) {
-#pragma unroll
-    for (int c = lane; c < W; c += 32) {
-      if (r < rows && c < cols) {
-        if (LOAD) *box_at<T>(box, r, c) = p[r * ld + c];
-        else p[r * ld + c] = *box_at<T>(box, r, c);
+    for (int r = 0; r < 32; ++r) {
+      uint16_t* at = reinterpret_cast<uint16_t*>(box_word<T>(box, r, lane / 2)) + (lane & 1);
+      uint16_t* out = reinterpret_cast<uint16_t*>(p) + r * ld + lane;
+      if (r < rows && lane < left) {
+        if (LOAD) *at = *out;
+        else *out = *at;
+      }
+    }
+  } else {
+#pragma unroll 8
+    for (int i = 0; i < 16; ++i) {
+      const int r = 2 * i + (lane >> 4), c = lane & 15;
+      uint32_t* at = box_word<T>(box, r, c);
+      uint32_t* out = reinterpret_cast<uint32_t*>(p) + r * ld + c;
+      if (r < rows && c < left) {
+        if (LOAD) *at = *out;
+        else *out = *at;
       }
     }
   }
   __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void store_any(uint8_t* box, T* p, int64_t ld, int rows, int left, const float (&v)[32]) {
+  constexpr int E = 64 / sizeof(T);  // entries of 64 bytes
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 0; h < 32; h += E) {
+    if (h < left) {
+#pragma unroll
+      for (int w = 0; w < 16; ++w)
+        *box_word<T>(box, lane, w) = sizeof(T) == 2 ? pack2(v[(2 * w) % 32], v[(2 * w + 1) % 32]) : __float_as_uint(v[(h + w) % 32]);
+      box_rows<T, false>(box, p + h, ld, rows, left - h);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void add_any(uint8_t* box, const T* p, int64_t ld, int rows, int left, float (&v)[32]) {
+  constexpr int E = 64 / sizeof(T);
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 0; h < 32; h += E) {
+    if (h < left) {
+      box_rows<T, true>(box, const_cast<T*>(p) + h, ld, rows, left - h);
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const uint32_t u = *box_word<T>(box, lane, w);
+        if (sizeof(T) == 2) {
+          v[(2 * w) % 32] = fadd(__uint_as_float(u << 16), v[(2 * w) % 32]);
+          v[(2 * w + 1) % 32] = fadd(__uint_as_float(u & 0xffff0000u), v[(2 * w + 1) % 32]);
+        } else {
+          v[(h + w) % 32] = fadd(__uint_as_float(u), v[(h + w) % 32]);
+        }
+      }
+      __syncwarp();
+    }
+  }
 }
 
 template <int W, bool FAST>
@@ -177,122 +282,64 @@ __device__ __forceinline__ void add_bias(const T* bias, bool wide, int left, flo
   }
 }
 
-// What an epilogue warp keeps of its boxes between tiles.
-template <int PLANES>
-struct Boxes {
-  uint8_t* box;        // [kBoxes][4 KB]
-  uint64_t* loaded;    // [kBoxes]
-  uint32_t phase;      // bit b: parity of the next load into box b
-  uint32_t flying;     // bit b: a load into box b has not been waited for
-  uint32_t turn;       // of stores that take the boxes in turn
-};
-// The next box to store from, without a residual: the last store from it has been read.
-template <int PLANES>
-__device__ __forceinline__ uint8_t* next_box(Boxes<PLANES>& b) {
-  constexpr int kBoxes = LinearTiles<PLANES>::kBoxes;
-  if ((threadIdx.x & 31) == 0) {
-    if (kBoxes == 1) bulk_wait_read();
-    else bulk_wait_read_but_one();
-  }
-  __syncwarp();
-  return b.box + (b.turn++ & (kBoxes - 1)) * LinearTiles<PLANES>::kBoxBytes;
-}
-
-// One lane's row of a half tile: x[j] = C[m][n0 + j], j < 128.  m0: row of lane 0.
+// What is done to 32 columns of an epilogue warp's 32 rows, from row m0 and column n on, a row a
+// lane: v[j] = C[m0 + lane][n + j].
 template <int MODE, int PLANES>
-__device__ __forceinline__ bool linear_epilogue(const LinearGemm& g, const LinearTile& t, int m0, int n0, uint64_t seed,
-                                                float (&x)[kHalf], Boxes<PLANES>& b, const CUtensorMap* map_y,
-                                                const CUtensorMap* map_z, const CUtensorMap* map_r) {
+__device__ __forceinline__ void linear_piece(const LinearGemm& g, int m0, int n, uint64_t seed, float (&v)[32], uint8_t* box) {
   using T = typename std::conditional<PLANES == 1, __nv_bfloat16, float>::type;
-  constexpr int W = 128 / sizeof(T), kBoxes = LinearTiles<PLANES>::kBoxes;
-  const int lane = threadIdx.x & 31, m = m0 + lane;
-  if (m0 >= g.m) return true;
-  if (g.sum != nullptr) {
-    if (m >= g.m) return true;
-    float* out = g.sum + t.split * g.sum_split + m * g.lds + n0;
-    const int cols = min(static_cast<int>(g.lds) - n0, g.tile_n);
-#pragma unroll
-    for (int j = 0; j < kHalf; j += 8) {
-      if (j < cols) {
-        uint32_t u[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(x[j + q]);
-        st_v8(out + j, u);
-      }
+  const int lane = threadIdx.x & 31, m = m0 + lane, rows = min(g.m - m0, 32), left = g.n - n;
+  auto store = [&](void* base, int64_t ld) {
+    T* p = static_cast<T*>(base) + n;
+    if (g.wide == 0) store_any<T>(box, p + m0 * ld, ld, rows, left, v);
+    else if (lane < rows) store_wide<T>(p + m * ld, left, g.wide == 2, v);
+  };
+  if (MODE == kForward) {
+    const T* r = static_cast<const T*>(g.residual) + n;
+    Ahead<T> ahead;
+    if (g.residual != nullptr && g.wide != 0) load_wide<T>(r + min(m, g.m - 1) * g.ldr, left, ahead);
+    if (g.bias != nullptr) add_bias<T, 32>(static_cast<const T*>(g.bias) + n, g.bias_wide, left, v);
+    if (g.z != nullptr) store(g.z, g.ldz);
+    apply_act<32, PLANES == 1>(g.act, v);
+    if (g.drop.level > 0) apply_drop<32>(g.drop, seed, static_cast<uint64_t>(m) * g.n + n, v);
+    if (g.residual != nullptr) {
+      if (g.wide != 0) add_ahead<T>(ahead, v);
+      else add_any<T>(box, r + m0 * g.ldr, g.ldr, rows, left, v);
     }
-    return true;
+  } else if (g.drop.level > 0) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = fmul(v[j], g.drop.scale);
   }
-  const int rows = min(g.m - m0, 32);
-#pragma unroll
-  for (int h = 0; h < kHalf / W; ++h) {
-    const int n = n0 + h * W, left = g.n - n;
-    if (left <= 0 || h * W >= g.tile_n) continue;
-    const int at = h & (kBoxes - 1);  // the box of the residual, where y takes its place
-    uint8_t* box = b.box + at * LinearTiles<PLANES>::kBoxBytes;
-    float* v = x + h * W;
-    if (MODE == kForward) {
-      if (g.bias != nullptr) add_bias<T, W>(static_cast<const T*>(g.bias) + n, g.bias_wide, left, v);
-      if (g.z != nullptr) {
-        uint8_t* zbox = next_box<PLANES>(b);
-        box_put<T>(zbox, v);
-        if (g.mapped) {
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) tensor_s2g(map_z, n, m0, 0, zbox);
-        } else {
-          box_rows<T, false>(zbox, static_cast<T*>(g.z) + m0 * g.ldz + n, g.ldz, rows, left);
-        }
-      }
-      apply_act<W, PLANES == 1>(g.act, v);
-      if (g.drop.level > 0) apply_drop<W>(g.drop, seed, static_cast<uint64_t>(m) * g.n + n, v);
-      if (g.residual != nullptr) {
-        if (g.mapped) {
-          if (!(b.flying >> at & 1)) {
-            if (lane == 0) {
-              bulk_wait_read();
-              mbar_arrive_expect_tx(&b.loaded[at], LinearTiles<PLANES>::kBoxBytes);
-              tensor_g2s_own(box, map_r, n, m0, 0, smem_addr(&b.loaded[at]));
-            }
-            b.flying |= 1u << at;
-          }
-          const bool ok = mbar_wait_bounded(&b.loaded[at], b.phase >> at & 1, g.spin_limit, g.status);
-          if (!__all_sync(kFull, ok)) return false;
-          b.phase ^= 1u << at;
-          b.flying &= ~(1u << at);
-        } else {
-          box_rows<T, true>(box, const_cast<T*>(static_cast<const T*>(g.residual)) + m0 * g.ldr + n, g.ldr, rows, left);
-        }
-        box_add<T>(box, v);
-      } else {
-        box = next_box<PLANES>(b);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < W; ++j) v[j] = fmul(v[j], g.drop.scale);
-      box = next_box<PLANES>(b);
-    }
-    box_put<T>(box, v);
-    if (g.mapped) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) tensor_s2g(map_y, n, m0, 0, box);
-    } else {
-      box_rows<T, false>(box, static_cast<T*>(g.y) + m0 * g.ldy + n, g.ldy, rows, left);
-    }
-  }
-  return true;
+  store(g.y, g.ldy);
 }
 
-template <int MODE, int PLANES>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+// The same 32 columns of a tile in parts: into its slot of the sums.
+__device__ __forceinline__ void sum_piece(const LinearGemm& g, int slot, int row, int col, const float (&v)[32]) {
+  float* out = g.sum + (static_cast<int64_t>(slot) * kPair + row) * g.tile_n + col;
+#pragma unroll
+  for (int j = 0; j < 32; j += 8) {
+    uint32_t u[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) u[q] = __float_as_uint(v[j + q]);
+    st_v8(out + j, u);
+  }
+}
+
+__device__ __forceinline__ void landed(float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) asm volatile("" : "+f"(v[j]));  // nothing uses v before the wait
+}
+
+// ONE: a tile has one chunk, so the epilogue takes 32 columns at a time from tensor memory, the next
+// ones on their way; else it keeps 128 columns in registers and adds the chunks.
+template <int MODE, int PLANES, bool ONE>
+__global__ void __launch_bounds__(kLinearThreads, 1)
     linear_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                       const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
-                       const __grid_constant__ CUtensorMap map_r, const __grid_constant__ LinearGemm g) {
+                       const __grid_constant__ LinearGemm g) {
   constexpr bool A_MN = MODE == kDw, B_MN = MODE != kForward;
-  constexpr int stages = LinearTiles<PLANES>::kStages, kBoxes = LinearTiles<PLANES>::kBoxes;
+  constexpr int stages = LinearTiles<PLANES>::kStages;
   extern __shared__ uint8_t raw[];
   // full and taken are used in the first CTA, for both; empty and done in each
-  __shared__ uint64_t full[stages], empty[stages], done[2], taken[2], drain, loaded[kEpiWarps * kBoxes];
+  __shared__ uint64_t full[stages], empty[stages], done[2], taken[2], drain;
   __shared__ uint32_t tmem;
   uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -304,9 +351,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&done[i], 1);
-      mbar_init(&taken[i], 2 * kEpiWarps);
+      mbar_init(&taken[i], 2 * kLinearEpi);
     }
-    for (int i = 0; i < kEpiWarps * kBoxes; ++i) mbar_init(&loaded[i], 1);
     mbar_init(&drain, 1);
     fence_mbar_init();
     prefetch_map(&map_a);
@@ -319,7 +365,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc_fence_after();
   const uint32_t acc = tmem;
   pdl_begin();
-  const int total = g.m_tiles * g.n_tiles * g.splits;
+  pdl_end();
+  const int total = linear_units(g);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (warp == 0) {
@@ -330,18 +377,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
       const int b_blocks = (g.tile_n / 2 + 63) / 64;
       const uint32_t bytes = 2 * PLANES * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
+      const uint32_t full0 = dsmem_addr(full, 0);
+      uint32_t st = 0, parity = 1;  // of the stage's `empty` to wait for
       for (int i = pair; i < total && ok; i += pairs) {
         const LinearTile t = linear_tile(g, i);
         const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g.n, t.n0, g.tile_n) / 2);
         for (int kb = t.k0; kb < t.k1; ++kb, ++it) {
-          const int st = it % stages;
-          ok = mbar_wait_bounded(&empty[st], (it / stages & 1) ^ 1, g.spin_limit, g.status);
+          ok = mbar_wait_bounded(&empty[st], parity, g.spin_limit, g.status);
           if (!ok) break;
-          const uint32_t bar = dsmem_addr(&full[st], 0);
+          const uint32_t bar = full0 + st * 8;
           if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
+          uint8_t* stage = stage0 + st * (PLANES * kStageBytes);
+          if (++st == stages) {
+            st = 0;
+            parity ^= 1;
+          }
 #pragma unroll
           for (int p = 0; p < PLANES; ++p) {
-            uint8_t* a = stage0 + (st * PLANES + p) * kStageBytes;
+            uint8_t* a = stage + p * kStageBytes;
             uint8_t* b = a + kBytesA;
             if (A_MN) {
 #pragma unroll
@@ -375,10 +428,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      uint32_t it = 0, n = 0;
+      const uint32_t base = smem_addr(stage0);
+      const uint64_t a0 = A_MN ? smem_desc(base, kK * 128, 1024) : smem_desc(base, 16, 1024);
+      const uint64_t b0 = B_MN ? smem_desc(base + kBytesA, kK * 128, 1024) : smem_desc(base + kBytesA, 16, 1024);
+      // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
+      constexpr uint64_t kStepA = (A_MN ? 2048 : 32) >> 4, kStepB = (B_MN ? 2048 : 32) >> 4;
+      uint32_t st = 0, parity = 0, n = 0;
       bool ok = true;
+      LinearTile next = linear_tile(g, pair);
       for (int i = pair; i < total && ok; i += pairs) {
-        const LinearTile t = linear_tile(g, i);
+        const LinearTile t = next;
         const uint32_t idesc = mma_desc(kPair, tile_cols(g.n, t.n0, g.tile_n), A_MN, B_MN);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
           ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
@@ -386,27 +445,28 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           const uint32_t d = acc + (n & 1) * kN;
           bool fresh = true;
           const int steps = min(g.chunk, t.k1 - c);
-          for (int k = 0; k < steps; ++k, ++it) {
-            const int st = it % stages;
-            ok = mbar_wait_bounded(&full[st], it / stages & 1, g.spin_limit, g.status);
+          for (int k = 0; k < steps; ++k) {
+            ok = mbar_wait_bounded(&full[st], parity, g.spin_limit, g.status);
             if (!ok) break;
+            const uint32_t now = st;
+            if (++st == stages) {
+              st = 0;
+              parity ^= 1;
+            }
             tc_fence_after();
-            const uint32_t base = smem_addr(stage0 + st * PLANES * kStageBytes);
+            const uint64_t as = a0 + now * (PLANES * kStageBytes >> 4), bs = b0 + now * (PLANES * kStageBytes >> 4);
 #pragma unroll
             for (int term = 0; term < (PLANES == 1 ? 1 : 6); ++term) {
               int pa, pb;
               term_planes<PLANES>(term, &pa, &pb);
-              const uint32_t a = base + pa * kStageBytes, b = base + pb * kStageBytes + kBytesA;
 #pragma unroll
               for (int q = 0; q < kK / 16; ++q) {
-                // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
-                const uint64_t da = A_MN ? smem_desc(a + q * 2048, kK * 128, 1024) : smem_desc(a + q * 32, 16, 1024);
-                const uint64_t db = B_MN ? smem_desc(b + q * 2048, kK * 128, 1024) : smem_desc(b + q * 32, 16, 1024);
-                mma_bf16(d, da, db, idesc, fresh);
+                mma_bf16(d, as + pa * (kStageBytes >> 4) + q * kStepA, bs + pb * (kStageBytes >> 4) + q * kStepB, idesc, fresh);
                 fresh = false;
               }
             }
-            mma_commit_pair(&empty[st]);
+            mma_commit_pair(&empty[now]);
+            if (c + k == t.k0) next = linear_tile(g, min(i + pairs, total - 1));  // while these products run
           }
           if (ok) mma_commit_pair(&done[n & 1]);
         }
@@ -417,78 +477,82 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
     }
   } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int quad = warp & 3, first = ((warp - 2) >> 2) * kLinearCols;  // its lanes and columns of the tile
     const uint64_t seed = MODE == kForward && g.drop.level > 0 ? drop_seed(g.drop) : 0;
-    Boxes<PLANES> boxes = {stage0 + stages * PLANES * kStageBytes + (warp - 2) * kBoxes * LinearTiles<PLANES>::kBoxBytes,
-                           loaded + (warp - 2) * kBoxes, 0u, 0u, 0u};
-    constexpr int W = 64 * PLANES / (PLANES == 1 ? 1 : 6);  // columns of a box: 64 or 32
-    if (MODE == kForward && lane == 0) fence_proxy_async_all();  // a residual that earlier kernels wrote
+    uint8_t* box = stage0 + stages * PLANES * kStageBytes + (warp - 2) * kLinearBox;
+    constexpr int kPieces = kLinearCols / 32;
     uint32_t n = 0;
-    bool ok = true;
     for (int i = pair; i < total; i += pairs) {
       const LinearTile t = linear_tile(g, i);
-      const int m0 = t.m0 + rank * kM + quad * 32, n0 = t.n0 + half * kHalf;
-      // the residual's first boxes come while the products run
-      if (MODE == kForward && g.residual != nullptr && g.z == nullptr && g.mapped && g.sum == nullptr && m0 < g.m &&
-          half * kHalf < g.tile_n) {
-        if (lane == 0) bulk_wait_read();
-#pragma unroll
-        for (int q = 0; q < kBoxes; ++q) {
-          if (n0 + q * W < g.n && half * kHalf + q * W < g.tile_n) {
-            if (lane == 0) {
-              mbar_arrive_expect_tx(&boxes.loaded[q], LinearTiles<PLANES>::kBoxBytes);
-              tensor_g2s_own(boxes.box + q * LinearTiles<PLANES>::kBoxBytes, &map_r, n0 + q * W, m0, 0,
-                             smem_addr(&boxes.loaded[q]));
-            }
-            boxes.flying |= 1u << q;
-          }
-        }
-      }
-      float x[kHalf];
-      for (int c = t.k0; c < t.k1; c += g.chunk, ++n) {
+      const int m0 = t.m0 + rank * kM + quad * 32, n0 = t.n0 + first;
+      // pieces of 32 columns that this warp takes
+      const int width = min(g.n - n0, g.tile_n - first);
+      const int pieces = m0 < g.m && width > 0 ? min((width + 31) / 32, kPieces) : 0;
+      const uint32_t columns = first + (static_cast<uint32_t>(quad * 32) << 16);
+      const int row = rank * kM + quad * 32 + lane;
+      auto out = [&](int q, float (&v)[32]) {
+        if (t.slot >= 0) sum_piece(g, t.slot, row, first + 32 * q, v);
+        else linear_piece<MODE, PLANES>(g, m0, n0 + 32 * q, seed, v, box);
+      };
+      bool ok = true;
+      if (ONE) {
         ok = mbar_wait_bounded(&done[n & 1], n / 2 & 1, g.spin_limit, g.status);
         ok = __all_sync(kFull, ok);
         if (!ok) break;
         tc_fence_after();
-        if (half * kHalf >= g.tile_n) {  // a narrow tile: the first four warps take it
-          if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
-          continue;
-        }
-        const uint32_t at = acc + (n & 1) * kN + half * kHalf + (static_cast<uint32_t>(quad * 32) << 16);
-        if (c == t.k0) {
+        const uint32_t at = acc + (n & 1) * kN + columns;
 #pragma unroll
-          for (int q = 0; q < kHalf; q += 32) tmem_ld32(at + q, x + q);
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < kHalf; ++j) asm volatile("" : "+f"(x[j]));  // nothing uses x before the wait
-        } else {
-#pragma unroll
-          for (int q = 0; q < kHalf; q += 64) {
-            float y[64];
-            tmem_ld32(at + q, y);
-            tmem_ld32(at + q + 32, y + 32);
+        for (int q = 0; q < kPieces; ++q) {
+          float v[32];
+          if (q < pieces) {
+            tmem_ld32(at + 32 * q, v);
             tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 64; ++j) {
-              asm volatile("" : "+f"(y[j]));
-              x[q + j] = fadd(x[q + j], y[j]);
-            }
+            landed(v);
           }
+          if (q + 1 == max(pieces, 1)) {  // its columns are in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+          }
+          if (q < pieces) out(q, v);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+        ++n;
+      } else {
+        float x[kPieces][32];
+        for (int c = t.k0; c < t.k1; c += g.chunk, ++n) {
+          ok = mbar_wait_bounded(&done[n & 1], n / 2 & 1, g.spin_limit, g.status);
+          ok = __all_sync(kFull, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t at = acc + (n & 1) * kN + columns;
+          if (pieces > 0) {
+            if (c == t.k0) {
+#pragma unroll
+              for (int q = 0; q < kPieces; ++q) tmem_ld32(at + 32 * q, x[q]);
+              tmem_wait_ld();
+#pragma unroll
+              for (int q = 0; q < kPieces; ++q) landed(x[q]);
+            } else {
+#pragma unroll
+              for (int q = 0; q < kPieces; ++q) {
+                float y[32];
+                tmem_ld32(at + 32 * q, y);
+                tmem_wait_ld();
+                landed(y);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[q][j] = fadd(x[q][j], y[j]);
+              }
+            }
+            tc_fence_before();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q)
+          if (q < pieces) out(q, x[q]);
       }
-      if (!ok) break;
-      if (half * kHalf >= g.tile_n) continue;
-      ok = linear_epilogue<MODE, PLANES>(g, t, m0, n0, seed, x, boxes, &map_y, &map_z, &map_r);
-      if (!ok) break;
-    }
-    // no copy of this warp is in flight when it leaves
-    if (lane == 0) {
-      for (int q = 0; q < kBoxes; ++q)
-        if (boxes.flying >> q & 1) mbar_wait_bounded(&boxes.loaded[q], boxes.phase >> q & 1, kDrainPolls, g.status);
-      bulk_wait();
     }
   }
   __syncwarp();

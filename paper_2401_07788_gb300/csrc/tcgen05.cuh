@@ -24,14 +24,6 @@ __device__ __forceinline__ void tensor_g2s(void* dst, const CUtensorMap* map, in
       "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
-// The same on a barrier of this CTA, whose copies are its own.
-__device__ __forceinline__ void tensor_g2s_own(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_addr(dst)),
-      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
 // A box from this CTA's shared memory to global memory, in a bulk group of the thread.
 __device__ __forceinline__ void tensor_s2g(const CUtensorMap* map, int x, int y, int z, const void* src) {
   asm volatile(
@@ -42,9 +34,6 @@ __device__ __forceinline__ void tensor_s2g(const CUtensorMap* map, int x, int y,
 }
 // The thread's groups have read their shared memory; have finished.
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read_but_one() {  // but the latest
-  asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-}
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
