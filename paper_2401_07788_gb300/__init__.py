@@ -144,9 +144,10 @@ def _ptr(t: torch.Tensor | None):
     return None if t is None else _VP(t.data_ptr())
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return _VP(s.cuda_stream)
+def _stream(stream) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _launch(call, device, stream, *args) -> None:
@@ -677,30 +678,46 @@ def _step(step, device):
     return None if step is None else _vector(step, 1, torch.int64, "step", device).data_ptr()
 
 
-def _like(t, rows: int, cols: int, of, name: str, stream):
-    """An output matrix of the type and device of `of`: the caller's, checked, or a new one."""
+# The calls below are made once a layer and token, where the host's time is what counts: an operand is
+# looked at once, in the order of what it mostly is (dense, of the first one's type and device),
+# and goes through the checks that name what is wrong with it only otherwise.
+
+def _ld(t, name: str, rows: int, cols: int, of, index: int) -> int:
+    """The row distance of a matrix of this shape, of the type and device of `of`."""
+    if isinstance(t, torch.Tensor) and t.dtype is of.dtype and t.get_device() == index and t.shape == (rows, cols) \
+            and t.is_contiguous():
+        return cols
+    ld = _matrix(t, name, cols, of)
+    if t.shape[0] != rows:
+        raise MpcError(1, "%s must have %d rows" % (name, rows))
+    return ld
+
+
+def _like(t, rows: int, cols: int, of, name: str, index: int, stream):
+    """An output matrix of the type and device of `of`: the caller's, checked, or a new one; its row distance."""
     if t is None:
         t = torch.empty((rows, cols), dtype=of.dtype, device=of.device)
         if stream is not None:
             t.record_stream(stream)
         return t, cols
-    ld = _matrix(t, name, cols, of)
-    if t.shape[0] != rows:
-        raise MpcError(1, "%s must have %d rows" % (name, rows))
-    return t, ld
+    return t, _ld(t, name, rows, cols, of, index)
 
 
-def _rows_like(t, name: str, of):
-    """The row distance of an input matrix with the shape, type and device of `of` (0 for None)."""
-    if t is None:
-        return 0
-    if t.shape != of.shape:
-        raise MpcError(1, "%s must have the shape %s" % (name, tuple(of.shape)))
-    return _matrix(t, name, of.shape[1], of)
+def _vector_like(t, n: int, of, name: str, index: int):
+    """The address of a dense tensor of n entries, of the type and device of `of`."""
+    if isinstance(t, torch.Tensor) and t.dtype is of.dtype and t.get_device() == index and t.shape == (n,) \
+            and t.is_contiguous():
+        return t.data_ptr()
+    return _vector(t, n, of.dtype, name, of.device).data_ptr()
 
 
-def _vector_like(t, n: int, of, name: str):
-    return None if t is None else _vector(t, n, of.dtype, name, of.device).data_ptr()
+def _call(fn, of, index: int, stream, *args) -> None:
+    if stream is None and index == torch._C._cuda_getDevice():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+        if status:
+            _check(status)
+    else:
+        _launch(fn, of.device, stream, *args)
 
 
 def mpc_dropout(x, p: float, seed: int = 0, residual=None, step=None, y=None, stream=None):
@@ -708,43 +725,46 @@ def mpc_dropout(x, p: float, seed: int = 0, residual=None, step=None, y=None, st
     residual contiguous, of one shape.  No mask is stored: the same ``seed`` (plus ``step``, an int64 device
     tensor of one entry) makes the same one, so the gradient of x is this call on the gradient of y."""
     kind = _dtype(x, "x")
+    index = x.get_device()
     _cuda(x, x.dtype, "x")
     for name, t in (("residual", residual), ("y", y)):
         if t is not None:
             _cuda(t, x.dtype, name)
-            if t.shape != x.shape or t.device != x.device:
+            if t.shape != x.shape or t.get_device() != index:
                 raise MpcError(1, "%s must have the shape and device of x" % name)
     if y is None:
         y = torch.empty_like(x)
         _on(stream, y)
-    _launch(lib().mpc_dropout, x.device, stream, x.data_ptr(), _address(residual), x.numel(), kind, p, seed & _SEEDS,
-            _step(step, x.device), y.data_ptr())
+    _call(lib().mpc_dropout, x, index, stream, x.data_ptr(), None if residual is None else residual.data_ptr(), x.numel(),
+          kind, p, seed & _SEEDS, None if step is None else _step(step, x.device), y.data_ptr())
     return y
 
 
 def _norm_args(x, weight, residual, h, rstd, stream):
     ldx = _matrix(x, "x")
     rows, D = x.shape
+    index = x.get_device()
     if D == 0:
         raise MpcError(1, "the rows of x must hold at least one entry")
-    w = _vector_like(weight, D, x, "weight")
-    ldr = _rows_like(residual, "residual", x)
-    ldh = ldx
+    w = _vector_like(weight, D, x, "weight", index)
+    ldr = ldh = 0
     if residual is not None:
-        h, ldh = _like(h, rows, D, x, "h", stream)
+        ldr = _ld(residual, "residual", rows, D, x, index)
+        h, ldh = _like(h, rows, D, x, "h", index, stream)
     elif h is not None:
         raise MpcError(1, "h is the sum with a residual; without one it is x")
     rstd = _vector_or_new(rstd, rows, "rstd", x.device, stream)
-    return rows, D, ldx, w, ldr, h, ldh, rstd
+    return rows, D, index, ldx, w, None if residual is None else residual.data_ptr(), ldr, h, \
+        None if h is None else h.data_ptr(), ldh, rstd
 
 
 def mpc_rms_norm_forward(x, weight, eps: float = 1e-6, residual=None, y=None, h=None, rstd=None, stream=None):
     """Root-mean-square norm of the rows of x [R, D], after the residual's addition where there is one.
     Returns (y, h, rstd): h = x + residual in the type of x (x itself without a residual), rstd [R] fp32."""
-    rows, D, ldx, w, ldr, h, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
-    y, ldy = _like(y, rows, D, x, "y", stream)
-    _launch(lib().mpc_rms_norm_forward, x.device, stream, x.data_ptr(), ldx, _address(residual), ldr, w, rows, D,
-            _DTYPES[x.dtype], eps, y.data_ptr(), ldy, _address(h), ldh, rstd.data_ptr())
+    rows, D, index, ldx, w, r, ldr, h, hp, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    y, ldy = _like(y, rows, D, x, "y", index, stream)
+    _call(lib().mpc_rms_norm_forward, x, index, stream, x.data_ptr(), ldx, r, ldr, w, rows, D, _DTYPES[x.dtype], eps,
+          y.data_ptr(), ldy, hp, ldh, rstd.data_ptr())
     return y, x if h is None else h, rstd
 
 
@@ -752,17 +772,17 @@ def mpc_rms_norm_quant(x, weight, eps: float = 1e-6, residual=None, codes=None, 
                        rstd=None, stream=None):
     """The same norm with its output as an 8-bit quantisation payload for mpc_quant_decompress.  Returns
     (codes [R, W] int32 of uint32 words, scale [R], minv [R], h, rstd)."""
-    rows, D, ldx, w, ldr, h, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    rows, D, index, ldx, w, r, ldr, h, hp, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
     W = (D + 15) // 16 * 4
     if codes is None:
         codes = torch.empty((rows, W), dtype=torch.int32, device=x.device)
         _on(stream, codes)
-    _vector(codes, rows * W, torch.int32, "codes", x.device)
+    else:
+        _vector(codes, rows * W, torch.int32, "codes", x.device)
     scale = _vector_or_new(scale, rows, "scale", x.device, stream)
     minv = _vector_or_new(minv, rows, "minv", x.device, stream)
-    _launch(lib().mpc_rms_norm_quant, x.device, stream, x.data_ptr(), ldx, _address(residual), ldr, w, rows, D,
-            _DTYPES[x.dtype], eps, codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), _address(h), ldh,
-            rstd.data_ptr())
+    _call(lib().mpc_rms_norm_quant, x, index, stream, x.data_ptr(), ldx, r, ldr, w, rows, D, _DTYPES[x.dtype], eps,
+          codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), hp, ldh, rstd.data_ptr())
     return codes, scale, minv, x if h is None else h, rstd
 
 
@@ -776,14 +796,16 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
     reaches h by other ways; dx is that of x and of residual alike.  ``need_weight`` False leaves dweight out."""
     ldh = _matrix(h, "h")
     rows, D = h.shape
+    index = h.get_device()
     if D == 0:
         raise MpcError(1, "the rows of h must hold at least one entry")
-    lddy, lddh = _rows_like(dy, "dy", h), _rows_like(dh, "dh", h)
-    w = _vector_like(weight, D, h, "weight")
+    lddy = _ld(dy, "dy", rows, D, h, index)
+    lddh = 0 if dh is None else _ld(dh, "dh", rows, D, h, index)
+    w = _vector_like(weight, D, h, "weight", index)
     _vector(rstd, rows, torch.float32, "rstd", h.device)
-    dx, lddx = _like(dx, rows, D, h, "dx", stream)
+    dx, lddx = _like(dx, rows, D, h, "dx", index, stream)
     if dweight is not None:
-        _vector(dweight, D, h.dtype, "dweight", h.device)
+        _vector_like(dweight, D, h, "dweight", index)
     elif need_weight:
         dweight = torch.empty(D, dtype=h.dtype, device=h.device)
         _on(stream, dweight)
@@ -791,8 +813,8 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
     ws, wsb = _workspace(mpc_rms_norm_workspace_bytes(rows, D), ws, h.device)
     if given is None:
         _on(stream, ws)
-    _launch(lib().mpc_rms_norm_backward, h.device, stream, dy.data_ptr(), lddy, h.data_ptr(), ldh, w, rstd.data_ptr(),
-            _address(dh), lddh, rows, D, _DTYPES[h.dtype], dx.data_ptr(), lddx, _address(dweight), _address(ws), wsb)
+    _call(lib().mpc_rms_norm_backward, h, index, stream, dy.data_ptr(), lddy, h.data_ptr(), ldh, w, rstd.data_ptr(),
+          _address(dh), lddh, rows, D, _DTYPES[h.dtype], dx.data_ptr(), lddx, _address(dweight), _address(ws), wsb)
     return dx, dweight
 
 
@@ -805,16 +827,30 @@ def mpc_linear_workspace_bytes(rows: int, inputs: int, outputs: int, dtype=torch
                                                 outputs if lddy is None else lddy))
 
 
-def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, device, stream):
-    need = lib().mpc_linear_workspace_bytes(
-        rows, K, N, kind, backward, 0 if x is None or x.data_ptr() % 16 else ldx,
-        0 if w is None or w.data_ptr() % 16 else ldw, 0 if dy is None or dy.data_ptr() % 16 else lddy)
+def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, of, stream):
+    """(ws, its address, its bytes); x, w, dy: addresses."""
     if ws is None:
+        need = lib().mpc_linear_workspace_bytes(rows, K, N, kind, backward, 0 if x & 15 else ldx, 0 if w & 15 else ldw,
+                                                0 if dy & 15 else lddy)
         if need == 0:
-            return None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-        _on(stream, ws)
-    return ws, ws.numel() * ws.element_size()
+            return None, None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=of.device)
+        if stream is not None:
+            ws.record_stream(stream)
+        return ws, ws.data_ptr(), need
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _linear_args(x, w):
+    ldx = _matrix(x, "x")
+    rows, K = x.shape
+    index = x.get_device()
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        _matrix(w, "w", K, x)
+    N = w.shape[0]
+    if K == 0 or N == 0:
+        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
+    return rows, K, N, index, ldx, _ld(w, "w", N, K, x, index), _DTYPES[x.dtype]
 
 
 def mpc_linear_forward(x, w, bias=None, residual=None, act: str | None = None, p: float = 0.0, seed: int = 0,
@@ -822,23 +858,19 @@ def mpc_linear_forward(x, w, bias=None, residual=None, act: str | None = None, p
     """residual + drop(act(x @ w.T + bias)) for x [R, K], w [N, K].  Returns (y [R, N], z): z holds the values
     before the activation, for the backward call, with ``keep`` (else None).  act: None, "relu", "gelu",
     "gelu_tanh" or "silu"; p, seed and step as for mpc_dropout."""
-    ldx = _matrix(x, "x")
-    rows, K = x.shape
-    ldw = _matrix(w, "w", K, x)
-    N = w.shape[0]
-    if K == 0 or N == 0:
-        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
-    kind, code = _DTYPES[x.dtype], _act(act)
-    b = _vector_like(bias, N, x, "bias")
-    y, ldy = _like(y, rows, N, x, "y", stream)
-    ldr = _rows_like(residual, "residual", y)
-    ldz = 0
+    rows, K, N, index, ldx, ldw, kind = _linear_args(x, w)
+    code = _act(act)
+    b = None if bias is None else _vector_like(bias, N, x, "bias", index)
+    r, ldr = (None, 0) if residual is None else (residual.data_ptr(), _ld(residual, "residual", rows, N, x, index))
+    y, ldy = _like(y, rows, N, x, "y", index, stream)
+    zp, ldz = None, 0
     if keep or z is not None:
-        z, ldz = _like(z, rows, N, x, "z", stream)
-    ws, wsb = _linear_ws(rows, K, N, kind, 0, x, ldx, w, ldw, None, 0, ws, x.device, stream)
-    _launch(lib().mpc_linear_forward, x.device, stream, x.data_ptr(), ldx, w.data_ptr(), ldw, b, _address(residual),
-            ldr, rows, K, N, kind, code, p, seed & _SEEDS, _step(step, x.device), y.data_ptr(), ldy, _address(z), ldz,
-            _address(ws), wsb)
+        z, ldz = _like(z, rows, N, x, "z", index, stream)
+        zp = z.data_ptr()
+    xp, wp = x.data_ptr(), w.data_ptr()
+    ws, wsp, wsb = _linear_ws(rows, K, N, kind, 0, xp, ldx, wp, ldw, 0, 0, ws, x, stream)
+    _call(lib().mpc_linear_forward, x, index, stream, xp, ldx, wp, ldw, b, r, ldr, rows, K, N, kind, code, p, seed & _SEEDS,
+          None if step is None else _step(step, x.device), y.data_ptr(), ldy, zp, ldz, wsp, wsb)
     return y, z
 
 
@@ -847,33 +879,29 @@ def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0
     """The gradient of mpc_linear_forward, with its z where it has an activation and its p, seed and step:
     (dx [R, K], dw [N, K], db [N]); ``need`` says which are formed (the others are None).  The gradient of the
     residual is dy.  dy, x, w: all three are given, whatever is formed."""
-    ldx = _matrix(x, "x")
-    rows, K = x.shape
-    ldw = _matrix(w, "w", K, x)
-    N = w.shape[0]
-    if K == 0 or N == 0:
-        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
-    kind, code = _DTYPES[x.dtype], _act(act)
-    lddy = _matrix(dy, "dy", N, x)
-    if dy.shape[0] != rows:
-        raise MpcError(1, "dy must have %d rows" % rows)
-    if code and z is None:
-        raise MpcError(1, "the gradient of an activation needs z (keep=True in the forward call)")
-    ldz = _rows_like(z, "z", dy)
+    rows, K, N, index, ldx, ldw, kind = _linear_args(x, w)
+    code = _act(act)
+    lddy = _ld(dy, "dy", rows, N, x, index)
+    zp, ldz = None, 0
+    if code:
+        if z is None:
+            raise MpcError(1, "the gradient of an activation needs z (keep=True in the forward call)")
+        zp, ldz = z.data_ptr(), _ld(z, "z", rows, N, x, index)
     lddx = lddw = 0
     if dx is not None or need[0]:
-        dx, lddx = _like(dx, rows, K, x, "dx", stream)
+        dx, lddx = _like(dx, rows, K, x, "dx", index, stream)
     if dw is not None or need[1]:
-        dw, lddw = _like(dw, N, K, x, "dw", stream)
+        dw, lddw = _like(dw, N, K, x, "dw", index, stream)
     if db is not None:
-        _vector(db, N, x.dtype, "db", x.device)
+        _vector_like(db, N, x, "db", index)
     elif need[2]:
         db = torch.empty(N, dtype=x.dtype, device=x.device)
         _on(stream, db)
-    ws, wsb = _linear_ws(rows, K, N, kind, 1, x, ldx, w, ldw, dy, lddy, ws, x.device, stream)
-    _launch(lib().mpc_linear_backward, x.device, stream, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw,
-            _address(z), ldz, rows, K, N, kind, code, p, seed & _SEEDS, _step(step, x.device), _address(dx), lddx,
-            _address(dw), lddw, _address(db), _address(ws), wsb)
+    xp, wp, dyp = x.data_ptr(), w.data_ptr(), dy.data_ptr()
+    ws, wsp, wsb = _linear_ws(rows, K, N, kind, 1, xp, ldx, wp, ldw, dyp, lddy, ws, x, stream)
+    _call(lib().mpc_linear_backward, x, index, stream, dyp, lddy, xp, ldx, wp, ldw, zp, ldz, rows, K, N, kind, code, p,
+          seed & _SEEDS, None if step is None else _step(step, x.device), _address(dx), lddx, _address(dw), lddw, _address(db),
+          wsp, wsb)
     return dx, dw, db
 
 
