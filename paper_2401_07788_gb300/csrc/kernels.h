@@ -241,5 +241,8 @@ size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, i
                               int64_t ldw, int64_t lddy);
 cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_linear_backward(const LinearArgs& a, int num_sms, cudaStream_t s);
+// The forward pass of a few rows (linear_few.cu); ldx, ldw: 0 for an operand off 16 bytes.
+bool linear_few_fits(int64_t rows, int64_t in, int bf16, int64_t ldx, int64_t ldw);
+cudaError_t launch_linear_few(const LinearArgs& a, int num_sms, cudaStream_t s);
 
 }  // namespace mpc

@@ -455,9 +455,12 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
 }  // namespace
 
 size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, int pass, int64_t ldx, int64_t ldw, int64_t lddy) {
+  if (pass == MPC_LINEAR_FORWARD && linear_few_fits(rows, in, bf16, ldx, ldw)) return 0;
   return layout(rows, in, out, bf16 != 0, pass, ldx, ldw, lddy).total;
 }
 cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
+  if (linear_few_fits(a.rows, a.in, a.bf16, on16(a.x, 0, 1) ? a.ldx : 0, on16(a.w, 0, 1) ? a.ldw : 0))
+    return launch_linear_few(a, num_sms, s);
   return a.bf16 ? forward<__nv_bfloat16>(a, num_sms, s) : forward<float>(a, num_sms, s);
 }
 cudaError_t launch_linear_backward(const LinearArgs& a, int num_sms, cudaStream_t s) {

@@ -55,6 +55,19 @@ def test_sizes(mpc, M, K, N, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("K,N", [(8, 5), (24, 16), (40, 33), (264, 31), (1000, 12001), (2056, 100), (74, 90), (75, 91)])
+@pytest.mark.parametrize("M", [1, 4, 7, 8, 9, 16, 20, 32, 33, 64, 65])
+def test_few_rows(mpc, M, K, N, kind):
+    x, w, b, r, _ = make(M + K, M, K, N, forms.KINDS[kind])
+    for act, p, bias, residual in (("silu", 0.0, b, None), (None, 0.3, None, r)):
+        mask = forms.kept(2, M * N, p).view(M, N).cuda() if p else None
+        y, z = mpc.mpc_linear_forward(x, w, bias, residual, act=act, p=p, seed=2, keep=True)
+        want, zw = forms.linear(x, w, bias, residual, act, mask)
+        forms.close(y, want, forms.linear_bound(x, w, bias, residual, act, mask, want, x.dtype), "y")
+        forms.close(z, zw, forms.linear_bound(x, w, bias, None, None, None, zw, x.dtype), "z")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("act,residual", [(None, True), ("gelu", True), ("silu", False)])
 @pytest.mark.parametrize("M,K,N", [(4128, 520, 2056), (3001, 331, 3203), (1030, 2100, 4104), (130, 4500, 96)])
 def test_many_tiles(mpc, M, K, N, act, residual, kind):
