@@ -47,11 +47,11 @@ __device__ __forceinline__ uint4 pack16(const float (&x)[8]) {
 
 // ---------------------------------------------------------------------------
 // Activations and their derivatives, with one exponential each:
-//   Phi(z) = erfc(-z / sqrt 2) / 2,           gelu = z Phi,  gelu' = Phi + z phi(z)
+//   Phi(z) = (1 + erf(z / sqrt 2)) / 2,          gelu = z Phi,  gelu' = Phi + z phi(z)
 //   s = 1 / (1 + exp(-v)),                     silu = z s(z)
 //   (1 + tanh(v / 2)) / 2 = s(v),              gelu_tanh = z s(2 sqrt(2/pi) (z + 0.044715 z^3))
 // For bf16 results the exponential and the quotient are the approximate ones (2 ulp),
-// and erfc is formula 7.1.26 of Abramowitz and Stegun (1.5e-7 off at most).
+// and 1 - erf is formula 7.1.26 of Abramowitz and Stegun (1.5e-7 off at most).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float exp_of(float x, bool fast) { return fast ? __expf(x) : expf(x); }
 __device__ __forceinline__ float over(float a, float b, bool fast) { return fast ? __fdividef(a, b) : fdiv(a, b); }
@@ -61,7 +61,7 @@ __device__ __forceinline__ float sigmoid(float v, bool fast) {
 }
 // Phi(z), with e = exp(-z^2 / 2).
 __device__ __forceinline__ float normal_cdf(float z, float e, bool fast) {
-  if (!fast) return fmul(0.5f, erfcf(fmul(z, -0.70710678118654752f)));
+  if (!fast) return fmul(0.5f, fadd(1.0f, erff(fmul(z, 0.70710678118654752f))));  // 6e-8 off at most
   const float t = __fdividef(1.0f, __fmaf_rn(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
   float q = __fmaf_rn(t, 1.061405429f, -1.453152027f);
   q = __fmaf_rn(t, q, 1.421413741f);

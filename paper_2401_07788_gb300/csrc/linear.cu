@@ -33,7 +33,13 @@ struct Operand {
   unsigned blocks;
 };
 
-constexpr int kDzRows = 128;  // rows of a CTA's part of dz: 8 threads a column group, 16 rows each
+// Rows of a CTA's part of dz, of 256 columns: up to 128 (8 threads a column group, 16 rows each),
+// fewer where that would leave SMs without work (1000 x 2051 in fp32 with gelu took 34 us).
+int64_t dz_rows(int64_t rows, int64_t out) {
+  int64_t r = 128;
+  while (r > 8 && (rows + r - 1) / r * ((out + 255) / 256) < 608) r /= 2;
+  return r;
+}
 
 template <typename E>
 struct Prepare {
@@ -42,7 +48,8 @@ struct Prepare {
   int64_t ldz;
   int wide_z, act;
   Drop drop;
-  float* part;             // column sums of every kDzRows rows, or nullptr
+  float* part;             // column sums of every dz_rows rows, or nullptr
+  int dz_rows;
   unsigned dz_cols;        // CTAs along the columns
 };
 
@@ -68,8 +75,8 @@ __device__ __forceinline__ void make_dz(unsigned block, const Prepare<E>& f) {
   const Operand<E>& o = f.dy;
   const int tc = threadIdx.x & 31, tr = threadIdx.x >> 5;
   const int c = static_cast<int>(block % f.dz_cols) * 256 + tc * 8;
-  const int64_t chunk = block / f.dz_cols, first = chunk * kDzRows;
-  const int64_t end = min64(o.rows, first + kDzRows);
+  const int64_t chunk = block / f.dz_cols, first = chunk * f.dz_rows;
+  const int64_t end = min64(o.rows, first + f.dz_rows);
   const int left = static_cast<int>(o.cols - c);
   const uint64_t seed = f.drop.level > 0 ? drop_seed(f.drop) : 0;
   float sum[8] = {};
@@ -306,7 +313,7 @@ Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_
     l.sum = take(cut_bytes(l.forward, rows, out));
   } else {
     l.dz = take(static_cast<size_t>(planes) * rows * l.Np * 2);
-    l.part = take((rows + kDzRows - 1) / kDzRows * out * 4);
+    l.part = take((rows + dz_rows(rows, out) - 1) / dz_rows(rows, out) * out * 4);
     l.dx = cut_tiles(rows, in, (out + kK - 1) / kK, planes);
     l.dw = cut_tiles(out, in, (rows + kK - 1) / kK, planes);
     l.sum = take(std::max(cut_bytes(l.dx, rows, in), cut_bytes(l.dw, out, in)));  // dx's are read before dw's are written
@@ -420,7 +427,8 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   const bool make = products && (l.pack_dy || a.act != MPC_ACT_NONE || f.drop.level > 0);
   f.dy = operand<E>(a.dy, a.lddy, a.rows, a.out, l.Np, make ? reinterpret_cast<uint16_t*>(ws + l.dz) : nullptr, num_sms);
   f.part = a.dbias != nullptr ? part : nullptr;
-  const int64_t chunks = (a.rows + kDzRows - 1) / kDzRows, cols = (a.out + 255) / 256;
+  f.dz_rows = static_cast<int>(dz_rows(a.rows, a.out));
+  const int64_t chunks = (a.rows + f.dz_rows - 1) / f.dz_rows, cols = (a.out + 255) / 256;
   if (chunks * cols > 0x3fffffff) return cudaErrorInvalidValue;
   f.dz_cols = static_cast<unsigned>(cols);
   f.dy.blocks = make || a.dbias != nullptr ? static_cast<unsigned>(chunks * cols) : 0;

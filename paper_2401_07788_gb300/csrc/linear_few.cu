@@ -8,9 +8,9 @@
 // a launch to add them cost more than the pass itself (24 x 4096 x 4096 in bf16: 17 + 4.5
 // us; 5.0 us is what 33.5 MB of w take).
 //
-// bf16 rows on 16 bytes, up to 64 rows of x: linear_few_mma_kernel.  A CTA of eight
-// warps takes 16 or 32 rows of w, its warps a stretch of K each.  A lane reads 16 bytes of a row of w
-// and 16 of a row of x and feeds them to warp-level products as they lie: the sum over K
+// bf16 rows on 16 bytes, up to 64 rows of x: linear_few_mma_kernel.  A CTA of four or eight
+// warps takes 16 or 32 rows of w, its warps a stretch of K each.  A lane reads 32 (or 16) bytes of a row
+// of w and as many of a row of x and feeds them to warp-level products as they lie: the sum over K
 // may run in any order, so the k that a lane of the fragment stands for is that of its own
 // bytes, the same in both operands.  The warps' sums are added in shared memory in a
 // fixed order, and every thread finishes some of the CTA's results.
@@ -52,11 +52,28 @@ __device__ __forceinline__ void warp_product(float (&d)[4], uint32_t a0, uint32_
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-constexpr int kMmaWarps = 8;
-constexpr int kMmaK = 32;  // k of a step: 16 bytes of four lanes
+// B bytes of a lane: k of a step.
+template <int B>
+struct Bytes {
+  uint32_t u[B / 4];
+};
+template <int B>
+__device__ __forceinline__ void load_bytes(Bytes<B>& v, const void* p, bool there) {
+  if (!there) {
+#pragma unroll
+    for (int i = 0; i < B / 4; ++i) v.u[i] = 0;
+  } else if constexpr (B == 32) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v.u[0]), "=r"(v.u[1]), "=r"(v.u[2]), "=r"(v.u[3]), "=r"(v.u[4]), "=r"(v.u[5]), "=r"(v.u[6]), "=r"(v.u[7])
+                 : "l"(p));
+  } else {
+    const uint4 x = *static_cast<const uint4*>(p);
+    v.u[0] = x.x, v.u[1] = x.y, v.u[2] = x.z, v.u[3] = x.w;
+  }
+}
 
-// NT: groups of 8 rows of x; RT: groups of 16 rows of w.
-template <int NT, int RT>
+// NT: groups of 8 rows of x; RT: groups of 16 rows of w; B: bytes of an access.
+template <int NT, int RT, int B, int kMmaWarps>
 __global__ void __launch_bounds__(kMmaWarps * 32) linear_few_mma_kernel(const Few f) {
   constexpr int kRows = 16 * RT, kTokens = 8 * NT;
   __shared__ float sums[kMmaWarps][kRows][kTokens + 1];
@@ -75,32 +92,38 @@ __global__ void __launch_bounds__(kMmaWarps * 32) linear_few_mma_kernel(const Fe
   for (int r = 0; r < 2 * RT; ++r) wr[r] = w + min64(n0 + r * 8 + i, a.out - 1) * a.ldw;
 #pragma unroll
   for (int r = 0; r < NT; ++r) xr[r] = x + static_cast<int64_t>(min(r * 8 + i, M - 1)) * a.ldx;
-  const int steps = (K + kMmaK - 1) / kMmaK;
+  constexpr int kEach = B / 2, kStep = 4 * kEach;  // k of a lane, of a step
+  const int steps = (K + kStep - 1) / kStep;
   const int first = static_cast<int>(static_cast<int64_t>(steps) * warp / kMmaWarps);
   const int last = static_cast<int>(static_cast<int64_t>(steps) * (warp + 1) / kMmaWarps);
   float d[RT][NT][4] = {};
-  constexpr int kAhead = NT * RT <= 4 ? 4 : 2;  // steps whose loads are in flight
+  // a ring of steps whose loads are in flight
+  constexpr int kLoads = (2 * RT + NT) * (B / 16), kAhead = kLoads <= 3 ? 8 : kLoads <= 6 ? 4 : kLoads <= 12 ? 2 : 1;
+  Bytes<B> wa[kAhead][2 * RT], xb[kAhead][NT];
+  auto load = [&](int u, int s) {
+    const int k = s * kStep + j * kEach;  // K is a multiple of kEach: all of a lane's exist, or none
+    const bool there = s < last && k < K;
+#pragma unroll
+    for (int r = 0; r < 2 * RT; ++r) load_bytes<B>(wa[u][r], wr[r] + k, there);
+#pragma unroll
+    for (int r = 0; r < NT; ++r) load_bytes<B>(xb[u][r], xr[r] + k, there);
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) load(u, first + u);
   for (int s = first; s < last; s += kAhead) {
-    uint4 wa[kAhead][2 * RT], xb[kAhead][NT];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int k = (s + u) * kMmaK + j * 8;  // K is a multiple of 8: all of a lane's 8 exist, or none
-      const bool there = s + u < last && k < K;
-#pragma unroll
-      for (int r = 0; r < 2 * RT; ++r) wa[u][r] = there ? *reinterpret_cast<const uint4*>(wr[r] + k) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int r = 0; r < NT; ++r) xb[u][r] = there ? *reinterpret_cast<const uint4*>(xr[r] + k) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const uint4 lo = wa[u][2 * r], hi = wa[u][2 * r + 1], b = xb[u][t];
-          warp_product(d[r][t], lo.x, hi.x, lo.y, hi.y, b.x, b.y);
-          warp_product(d[r][t], lo.z, hi.z, lo.w, hi.w, b.z, b.w);
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int q = 0; q < B / 4; q += 2) {
+            const uint32_t *lo = wa[u][2 * r].u + q, *hi = wa[u][2 * r + 1].u + q, *b = xb[u][t].u + q;
+            warp_product(d[r][t], lo[0], hi[0], lo[1], hi[1], b[0], b[1]);
+          }
+      load(u, s + u + kAhead);
+    }
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r)
@@ -134,11 +157,12 @@ __device__ __forceinline__ void few_load(const T* p, float (&v)[W]) {
   }
 }
 
-constexpr int kFmaRows = 4;  // of w a warp
 
-// M rows of x; accesses of W elements, of which K is a multiple.
+// M rows of x; accesses of W elements, of which K is a multiple. A warp takes four
+// rows of w: x is read once for all of them.
 template <typename T, int M, int W>
 __global__ void __launch_bounds__(128) linear_few_kernel(const Few f) {
+  constexpr int kFmaRows = 4;
   pdl_begin();
   pdl_end();
   const LinearArgs& a = f.a;
@@ -197,22 +221,39 @@ __global__ void __launch_bounds__(128) linear_few_kernel(const Few f) {
       if (lane == r * M + m && m < rows && n0 + r < a.out) finish_one<T>(f, seed, m, n0 + r, acc[r][m]);
 }
 
-template <int NT>
+template <int NT, int RT, int B, int WARPS>
+cudaError_t launch_mma(const Few& f, cudaStream_t s) {
+  const unsigned grid = static_cast<unsigned>((f.a.out + 16 * RT - 1) / (16 * RT));
+  return launch_kernel(linear_few_mma_kernel<NT, RT, B, WARPS>, dim3(grid), dim3(WARPS * 32), 0, s, 0u, f);
+}
+// 32 rows of w a CTA read x half as often, where enough CTAs are left and the loads in flight
+// fit the registers; eight warps along K where a warp's stretch stays long and little of x is
+// read (1 x 4096 x 4096 in bf16 7.1 us, with four 7.7; 24 x 4096 x 4096 12.6 and 10.9).
+template <int NT, int B>
 cudaError_t launch_mma(const Few& f, int num_sms, cudaStream_t s) {
-  // 32 rows of w a CTA read x half as often; 16 where those would leave SMs without work
-  const bool wide = NT <= 4 && f.a.out >= int64_t{32} * 2 * num_sms;
-  const int64_t rows = wide ? 32 : 16;
-  const unsigned grid = static_cast<unsigned>((f.a.out + rows - 1) / rows);
-  if constexpr (NT <= 4) {
-    if (wide) return launch_kernel(linear_few_mma_kernel<NT, 2>, dim3(grid), dim3(kMmaWarps * 32), 0, s, 0u, f);
+  if constexpr (NT <= 2) {
+    const bool wide = f.a.out >= int64_t{32} * 2 * num_sms;
+    if (NT == 1 && f.a.in >= 2048)
+      return wide ? launch_mma<NT, 2, B, 8>(f, s) : launch_mma<NT, 1, B, 8>(f, s);
+    if (wide) return launch_mma<NT, 2, B, 4>(f, s);
   }
-  return launch_kernel(linear_few_mma_kernel<NT, 1>, dim3(grid), dim3(kMmaWarps * 32), 0, s, 0u, f);
+  return launch_mma<NT, 1, B, 4>(f, s);
+}
+template <int B>
+cudaError_t launch_mma(const Few& f, int num_sms, cudaStream_t s) {
+  switch ((f.a.rows + 7) / 8) {
+    case 1: return launch_mma<1, B>(f, num_sms, s);
+    case 2: return launch_mma<2, B>(f, num_sms, s);
+    case 3: return launch_mma<3, B>(f, num_sms, s);
+    case 4: return launch_mma<4, B>(f, num_sms, s);
+    default: return launch_mma<8, B>(f, num_sms, s);
+  }
 }
 
 template <typename T, int W>
 cudaError_t launch_fma(const Few& f, cudaStream_t s) {
-  const unsigned grid = static_cast<unsigned>((f.a.out + 4 * kFmaRows - 1) / (4 * kFmaRows));
-  const int64_t m = f.a.rows;
+  const int64_t m = f.a.rows, each = 16;
+  const unsigned grid = static_cast<unsigned>((f.a.out + each - 1) / each);
   auto* kernel = m <= 1 ? linear_few_kernel<T, 1, W> : m <= 2 ? linear_few_kernel<T, 2, W> : m <= 4 ? linear_few_kernel<T, 4, W>
                                                                                          : linear_few_kernel<T, 8, W>;
   return launch_kernel(kernel, dim3(grid), dim3(128), 0, s, 0u, f);
@@ -233,15 +274,8 @@ cudaError_t launch_linear_few(const LinearArgs& a, int num_sms, cudaStream_t s) 
              static_cast<uintptr_t>(a.ldw * size) | static_cast<uintptr_t>(a.in * size)) % bytes) == 0;
   };
   if (a.bf16) {
-    if (on(16)) {
-      switch ((a.rows + 7) / 8) {
-        case 1: return launch_mma<1>(f, num_sms, s);
-        case 2: return launch_mma<2>(f, num_sms, s);
-        case 3: return launch_mma<3>(f, num_sms, s);
-        case 4: return launch_mma<4>(f, num_sms, s);
-        default: return launch_mma<8>(f, num_sms, s);
-      }
-    }
+    if (on(32)) return launch_mma<32>(f, num_sms, s);
+    if (on(16)) return launch_mma<16>(f, num_sms, s);
     return on(4) ? launch_fma<__nv_bfloat16, 2>(f, s) : launch_fma<__nv_bfloat16, 1>(f, s);
   }
   return on(16) ? launch_fma<float, 4>(f, s) : launch_fma<float, 1>(f, s);

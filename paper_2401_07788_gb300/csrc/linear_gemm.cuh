@@ -15,10 +15,10 @@ namespace {
 // kDx       A = dz [rows][out], B = w^T [in][out]   (B read as it is: rows of 64 entries of `in`)
 // kDw       A = dz^T [out][rows], B = x^T [in][rows]  (both read as they are)
 //
-// Warp 0 copies operand tiles through tensor maps (six stages of 32 KB a CTA; fp32: two of
-// three planes, which serve six plane products), one thread of the first CTA's warp 1 issues
+// Warp 0 copies operand tiles through tensor maps (six stages of 32 KB a CTA, of one
+// plane; fp32's three planes of a K block serve six plane products, and are given back one by one), one thread of the first CTA's warp 1 issues
 // the products of both CTAs, sixteen warps a CTA take the finished tile from tensor memory, 32
-// rows by 64 columns each.  Tensor memory holds two accumulators: a tile's epilogue runs
+// rows by twice 32 columns each.  Tensor memory holds two accumulators: a tile's epilogue runs
 // under the next one's products, and has to be no longer than those.  What it takes is
 // latency: the matrix units and the copies leave little of shared memory's bandwidth, so results
 // go from registers to global memory, 64 bytes a lane, and four warps a scheduler hide the
@@ -57,13 +57,12 @@ struct LinearGemm {
 
 constexpr int kLinearEpi = 16;                      // epilogue warps
 constexpr int kLinearThreads = (2 + kLinearEpi) * 32;
-constexpr int kLinearCols = kN / (kLinearEpi / 4);  // columns of one of them
 constexpr int kLinearBox = 2048;                    // 32 rows of 64 bytes, where rows lie on no 16 bytes
 
 template <int PLANES>
 struct LinearTiles {
-  static constexpr int kStages = 6 / PLANES;
-  static constexpr int kSmem = kStages * PLANES * kStageBytes + kLinearEpi * kLinearBox + 1024;
+  static constexpr int kStages = 6;  // of one plane of both operands
+  static constexpr int kSmem = kStages * kStageBytes + kLinearEpi * kLinearBox + 1024;
 };
 
 struct LinearTile {
@@ -157,6 +156,24 @@ __device__ __forceinline__ void add_ahead(const Ahead<T>& a, float (&v)[32]) {
     unpack16(a.u[c], f);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[c * V + i] = fadd(f[i], v[c * V + i]);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void add_wide(const T* p, int left, float (&v)[32]) {
+  constexpr int V = kVec<T>;
+#pragma unroll
+  for (int c = 0; c < 32 / V; ++c) {
+    if (left >= (c + 1) * V) {
+      float f[V];
+      unpack16(*reinterpret_cast<const uint4*>(p + c * V), f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[c * V + i] = fadd(f[i], v[c * V + i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c * V + i < left) v[c * V + i] = fadd(as_float(p[c * V + i]), v[c * V + i]);
+    }
   }
 }
 
@@ -295,14 +312,15 @@ __device__ __forceinline__ void linear_piece(const LinearGemm& g, int m0, int n,
   };
   if (MODE == kForward) {
     const T* r = static_cast<const T*>(g.residual) + n;
-    Ahead<T> ahead;
-    if (g.residual != nullptr && g.wide != 0) load_wide<T>(r + min(m, g.m - 1) * g.ldr, left, ahead);
+    Ahead<T> ahead;  // fp32: no registers are left for it
+    if (PLANES == 1 && g.residual != nullptr && g.wide != 0) load_wide<T>(r + min(m, g.m - 1) * g.ldr, left, ahead);
     if (g.bias != nullptr) add_bias<T, 32>(static_cast<const T*>(g.bias) + n, g.bias_wide, left, v);
     if (g.z != nullptr) store(g.z, g.ldz);
     apply_act<32, PLANES == 1>(g.act, v);
     if (g.drop.level > 0) apply_drop<32>(g.drop, seed, static_cast<uint64_t>(m) * g.n + n, v);
     if (g.residual != nullptr) {
-      if (g.wide != 0) add_ahead<T>(ahead, v);
+      if (PLANES == 1 && g.wide != 0) add_ahead<T>(ahead, v);
+      else if (g.wide != 0) add_wide<T>(r + min(m, g.m - 1) * g.ldr, left, v);
       else add_any<T>(box, r + m0 * g.ldr, g.ldr, rows, left, v);
     }
   } else if (g.drop.level > 0) {
@@ -330,7 +348,7 @@ __device__ __forceinline__ void landed(float (&v)[32]) {
 }
 
 // ONE: a tile has one chunk, so the epilogue takes 32 columns at a time from tensor memory, the next
-// ones on their way; else it keeps 128 columns in registers and adds the chunks.
+// ones on their way; else it keeps its 64 in registers and adds the chunks.
 template <int MODE, int PLANES, bool ONE>
 __global__ void __launch_bounds__(kLinearThreads, 1)
     linear_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -361,9 +379,8 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
   cluster_sync();  // both CTAs have started: the allocation is the pair's
   if (warp == 1) tmem_alloc(&tmem, 512);
   tc_fence_before();
-  cluster_sync();
+  cluster_sync();  // both have their tensor memory
   tc_fence_after();
-  const uint32_t acc = tmem;
   pdl_begin();
   pdl_end();
   const int total = linear_units(g);
@@ -376,37 +393,38 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
       bool ok = true;
       // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
       const int b_blocks = (g.tile_n / 2 + 63) / 64;
-      const uint32_t bytes = 2 * PLANES * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
+      const uint32_t bytes = 2 * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
       const uint32_t full0 = dsmem_addr(full, 0);
       uint32_t st = 0, parity = 1;  // of the stage's `empty` to wait for
       for (int i = pair; i < total && ok; i += pairs) {
         const LinearTile t = linear_tile(g, i);
         const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g.n, t.n0, g.tile_n) / 2);
-        for (int kb = t.k0; kb < t.k1; ++kb, ++it) {
+        int kb = t.k0, p = PLANES - 1;  // planes in the order in which they are given back
+        for (int left = (t.k1 - t.k0) * PLANES; left > 0; --left, ++it) {
           ok = mbar_wait_bounded(&empty[st], parity, g.spin_limit, g.status);
           if (!ok) break;
           const uint32_t bar = full0 + st * 8;
           if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
-          uint8_t* stage = stage0 + st * (PLANES * kStageBytes);
+          uint8_t* a = stage0 + st * kStageBytes;
+          uint8_t* b = a + kBytesA;
           if (++st == stages) {
             st = 0;
             parity ^= 1;
           }
+          if (A_MN) {
 #pragma unroll
-          for (int p = 0; p < PLANES; ++p) {
-            uint8_t* a = stage + p * kStageBytes;
-            uint8_t* b = a + kBytesA;
-            if (A_MN) {
-#pragma unroll
-              for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, p, bar);
-            } else {
-              tensor_g2s(a, &map_a, kb * kK, m0, p, bar);
-            }
-            if (B_MN) {
-              for (int q = 0; q < b_blocks; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, kb * kK, p, bar);
-            } else {
-              tensor_g2s(b, &map_b, kb * kK, n0, p, bar);
-            }
+            for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, p, bar);
+          } else {
+            tensor_g2s(a, &map_a, kb * kK, m0, p, bar);
+          }
+          if (B_MN) {
+            for (int q = 0; q < b_blocks; ++q) tensor_g2s(b + q * kK * 128, &map_b, n0 + q * 64, kb * kK, p, bar);
+          } else {
+            tensor_g2s(b, &map_b, kb * kK, n0, p, bar);
+          }
+          if (PLANES == 1 || --p < 0) {
+            p = PLANES - 1;
+            ++kb;
           }
         }
       }
@@ -428,7 +446,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      const uint32_t base = smem_addr(stage0);
+      const uint32_t base = smem_addr(stage0), acc = tmem;
       const uint64_t a0 = A_MN ? smem_desc(base, kK * 128, 1024) : smem_desc(base, 16, 1024);
       const uint64_t b0 = B_MN ? smem_desc(base + kBytesA, kK * 128, 1024) : smem_desc(base + kBytesA, 16, 1024);
       // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
@@ -446,26 +464,31 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
           bool fresh = true;
           const int steps = min(g.chunk, t.k1 - c);
           for (int k = 0; k < steps; ++k) {
-            ok = mbar_wait_bounded(&full[st], parity, g.spin_limit, g.status);
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) ok = ok && mbar_wait_bounded(&full[st + p], parity, g.spin_limit, g.status);
             if (!ok) break;
             const uint32_t now = st;
-            if (++st == stages) {
+            st += PLANES;
+            if (st == stages) {
               st = 0;
               parity ^= 1;
             }
             tc_fence_after();
-            const uint64_t as = a0 + now * (PLANES * kStageBytes >> 4), bs = b0 + now * (PLANES * kStageBytes >> 4);
 #pragma unroll
             for (int term = 0; term < (PLANES == 1 ? 1 : 6); ++term) {
               int pa, pb;
               term_planes<PLANES>(term, &pa, &pb);
+              const uint64_t as = a0 + (now + PLANES - 1 - pa) * (kStageBytes >> 4), bs = b0 + (now + PLANES - 1 - pb) * (kStageBytes >> 4);
 #pragma unroll
               for (int q = 0; q < kK / 16; ++q) {
-                mma_bf16(d, as + pa * (kStageBytes >> 4) + q * kStepA, bs + pb * (kStageBytes >> 4) + q * kStepB, idesc, fresh);
+                mma_bf16(d, as + q * kStepA, bs + q * kStepB, idesc, fresh);
                 fresh = false;
               }
+              // a plane is given back after its last product
+              if (PLANES == 1 || term == 5) mma_commit_pair(&empty[now + PLANES - 1]);
+              else if (term == 1) mma_commit_pair(&empty[now]);
+              else if (term == 4) mma_commit_pair(&empty[now + 1]);
             }
-            mma_commit_pair(&empty[now]);
             if (c + k == t.k0) next = linear_tile(g, min(i + pairs, total - 1));  // while these products run
           }
           if (ok) mma_commit_pair(&done[n & 1]);
@@ -477,17 +500,19 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
       mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
     }
   } else {
-    const int quad = warp & 3, first = ((warp - 2) >> 2) * kLinearCols;  // its lanes and columns of the tile
+    // its lanes of tensor memory, and the first of its pieces of 32 columns: 64 columns of a
+    // wide tile (a lane writes whole lines), one piece of a narrow one
+    const int quad = warp & 3, first = ((warp - 2) >> 2) * (g.tile_n > 128 ? 64 : 32);
+    const uint32_t acc = tmem;
     const uint64_t seed = MODE == kForward && g.drop.level > 0 ? drop_seed(g.drop) : 0;
-    uint8_t* box = stage0 + stages * PLANES * kStageBytes + (warp - 2) * kLinearBox;
-    constexpr int kPieces = kLinearCols / 32;
+    uint8_t* box = stage0 + stages * kStageBytes + (warp - 2) * kLinearBox;
+    constexpr int kPieces = 2;
     uint32_t n = 0;
     for (int i = pair; i < total; i += pairs) {
       const LinearTile t = linear_tile(g, i);
       const int m0 = t.m0 + rank * kM + quad * 32, n0 = t.n0 + first;
-      // pieces of 32 columns that this warp takes
       const int width = min(g.n - n0, g.tile_n - first);
-      const int pieces = m0 < g.m && width > 0 ? min((width + 31) / 32, kPieces) : 0;
+      const int pieces = m0 < g.m && width > 0 ? min((width + 31) / 32, g.tile_n > 128 ? 2 : 1) : 0;
       const uint32_t columns = first + (static_cast<uint32_t>(quad * 32) << 16);
       const int row = rank * kM + quad * 32 + lane;
       auto out = [&](int q, float (&v)[32]) {
@@ -534,13 +559,15 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
               for (int q = 0; q < kPieces; ++q) landed(x[q]);
             } else {
 #pragma unroll
-              for (int q = 0; q < kPieces; ++q) {
-                float y[32];
-                tmem_ld32(at + 32 * q, y);
+              for (int q = 0; q < 2 * kPieces; ++q) {
+                float y[16];
+                tmem_ld16(at + 16 * q, y);
                 tmem_wait_ld();
-                landed(y);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) x[q][j] = fadd(x[q][j], y[j]);
+                for (int j = 0; j < 16; ++j) {
+                  asm volatile("" : "+f"(y[j]));
+                  x[q / 2][q % 2 * 16 + j] = fadd(x[q / 2][q % 2 * 16 + j], y[j]);
+                }
               }
             }
             tc_fence_before();
@@ -561,7 +588,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
   cluster_sync();  // nothing signals or reads the other CTA's shared memory any more
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(acc, 512);
+    tmem_dealloc(tmem, 512);
   }
 }
 

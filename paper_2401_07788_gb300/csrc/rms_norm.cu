@@ -103,7 +103,7 @@ __device__ __forceinline__ Stats reduce_row(Stats s, bool extremes, Stats* share
 #pragma unroll
   for (int o = (NT < 32 ? NT : 32) / 2; o > 0; o >>= 1) s = merge(s, shuffled(s, o, extremes), extremes);
   if (NT > 32) {
-    constexpr int W = NT / 32;
+    constexpr int W = NT < 32 ? 1 : NT / 32;
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) shared[warp] = s;
     __syncthreads();
@@ -254,37 +254,104 @@ __global__ void __launch_bounds__(kLongBlock) rms_long_kernel(const RmsNormArgs 
 }
 
 // ---------------------------------------------------------------------------
-// Gradient.  Rows in registers as above; a CTA takes every gridDim.x-th set of rows and
-// keeps its sums of dw in registers, which leave as one row of `part`.
+// Gradient.  A CTA an SM takes every gridDim.x-th set of rows and keeps its sums of dw in
+// registers, which leave as one row of `part`.  A thread holds 32 bytes of each tensor's row and
+// asks for those of the next set before it works on this one: what bounds the pass is the bytes
+// in flight (16384 x 4096 in bf16, four tensors: 124 us without that).
 // ---------------------------------------------------------------------------
 constexpr int kBackBlock = 512;
 constexpr int kParts = 304;  // most rows of `part`
+template <typename T>
+constexpr int kBackEach = 32 / static_cast<int>(sizeof(T));
+template <typename T>
+constexpr int64_t kBackLongest = kBackEach<T> * 1024;
+
+template <typename T, int NT, bool WIDE>
+struct Raw {
+  static constexpr int E = kBackEach<T>, V = kVec<T>;
+  uint4 u[2];
+  __device__ __forceinline__ void load(const T* p, int t, int D) {
+    if (WIDE) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int col = (c * NT + t) * V;
+        u[c] = col < D ? *reinterpret_cast<const uint4*>(p + col) : make_uint4(0, 0, 0, 0);
+      }
+    } else {
+      T e[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) e[j] = j * NT + t < D ? p[j * NT + t] : T(0.0f);
+      memcpy(u, e, 32);
+    }
+  }
+  __device__ __forceinline__ void floats(float (&v)[E]) const {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float f[V];
+      unpack16(u[c], f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[c * V + i] = f[i];
+    }
+  }
+  __device__ __forceinline__ void store(T* p, int t, int D, const float (&v)[E]) const {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float f[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] = v[c * V + i];
+      if (WIDE) {
+        const int col = (c * NT + t) * V;
+        if (col < D) *reinterpret_cast<uint4*>(p + col) = pack16(f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if ((c * V + i) * NT + t < D) put(p + (c * V + i) * NT + t, f[i]);
+      }
+    }
+  }
+};
 
 template <typename T, int NT, bool WIDE>
 __global__ void __launch_bounds__(NT < kBackBlock ? kBackBlock : NT, 1) rms_backward_kernel(const RmsNormArgs a, float* part) {
   constexpr int kThreads = NT < kBackBlock ? kBackBlock : NT;
-  constexpr int kRows = kThreads / NT;
+  constexpr int kRows = kThreads / NT, E = kBackEach<T>;
+  using R = Raw<T, NT, WIDE>;
   __shared__ Stats shared[2][kThreads / 32];
   extern __shared__ float sums[];  // [kRows][D] when kRows > 1
   pdl_begin();
   pdl_end();
   const int t = threadIdx.x % NT, D = static_cast<int>(a.D);
-  float w[kEach], dw[kEach];
-  load_row<T, NT, WIDE>(static_cast<const T*>(a.weight), t, D, w);
+  R wr, h, dy, dh;
+  float dw[E];
+  wr.load(static_cast<const T*>(a.weight), t, D);
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) dw[j] = 0.0f;
+  for (int j = 0; j < E; ++j) dw[j] = 0.0f;
+  const int64_t apart = static_cast<int64_t>(gridDim.x) * kRows;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / NT;
+  float rstd = 0.0f;
+  auto ask = [&](int64_t r) {  // a row that does not exist is one of zeros
+    const bool live = r < a.rows;
+    const int width = live ? D : 0;
+    h.load(static_cast<const T*>(a.x) + r * a.ldx, t, width);
+    dy.load(static_cast<const T*>(a.dy) + r * a.lddy, t, width);
+    if (a.dh != nullptr) dh.load(static_cast<const T*>(a.dh) + r * a.lddh, t, width);
+    rstd = live ? a.rstd_in[r] : 0.0f;
+  };
+  ask(row);
   int turn = 0;
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows, turn ^= 1) {
-    const int64_t row = first + threadIdx.x / NT;
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += apart, row += apart, turn ^= 1) {
     const bool live = row < a.rows;
-    float n[kEach], g[kEach];
-    load_row<T, NT, WIDE>(static_cast<const T*>(a.x) + row * a.ldx, t, live ? D : 0, n);
-    load_row<T, NT, WIDE>(static_cast<const T*>(a.dy) + row * a.lddy, t, live ? D : 0, g);
-    const float rstd = live ? a.rstd_in[row] : 0.0f;
+    float n[E], g[E], w[E];
+    const float mine = rstd;
+    const R dh_now = dh;
+    h.floats(n);
+    dy.floats(g);
+    wr.floats(w);
+    ask(row + apart);
     float dot[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      n[j] = fmul(n[j], rstd);
+    for (int j = 0; j < E; ++j) {
+      n[j] = fmul(n[j], mine);
       dw[j] = __fmaf_rn(g[j], n[j], dw[j]);
       g[j] = fmul(g[j], w[j]);
       dot[j & 3] = __fmaf_rn(g[j], n[j], dot[j & 3]);
@@ -293,31 +360,25 @@ __global__ void __launch_bounds__(NT < kBackBlock ? kBackBlock : NT, 1) rms_back
     s = reduce_row<NT>(s, false, shared[turn]);
     const float c = fdiv(s.sum, static_cast<float>(D));
     if (live) {
-      float dh[kEach];
-      if (a.dh != nullptr) load_row<T, NT, WIDE>(static_cast<const T*>(a.dh) + row * a.lddh, t, D, dh);
+      float add[E];
+      if (a.dh != nullptr) dh_now.floats(add);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        g[j] = fmul(rstd, __fmaf_rn(-c, n[j], g[j]));
-        if (a.dh != nullptr) g[j] = fadd(g[j], dh[j]);
+      for (int j = 0; j < E; ++j) {
+        g[j] = fmul(mine, __fmaf_rn(-c, n[j], g[j]));
+        if (a.dh != nullptr) g[j] = fadd(g[j], add[j]);
       }
-      store_row<T, NT, WIDE>(static_cast<T*>(a.dx) + row * a.lddx, t, D, g);
+      h.store(static_cast<T*>(a.dx) + row * a.lddx, t, D, g);
     }
   }
   if (part == nullptr) return;
   float* out = part + static_cast<int64_t>(blockIdx.x) * D;
-  if (kRows == 1) {
+  float* mine = kRows == 1 ? out : sums + threadIdx.x / NT * D;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int col = column<T, NT, WIDE>(t, j);
-      if (col < D) out[col] = dw[j];
-    }
-  } else {
-    float* mine = sums + threadIdx.x / NT * D;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int col = column<T, NT, WIDE>(t, j);
-      if (col < D) mine[col] = dw[j];
-    }
+  for (int j = 0; j < E; ++j) {
+    const int col = column<T, NT, WIDE>(t, j);
+    if (col < D) mine[col] = dw[j];
+  }
+  if (kRows > 1) {
     __syncthreads();
     for (int i = threadIdx.x; i < D; i += kThreads) {
       float v = sums[i];
@@ -410,14 +471,14 @@ cudaError_t launch_rows_backward(const RmsNormArgs& a, float* part, int* parts, 
 }
 
 // Threads of a row: as few as hold it.
-template <typename T, bool WIDE, typename F>
+template <int EACH, typename F>
 cudaError_t with_threads(int64_t D, F f) {
-  if (D <= 8 * kEach) return f(std::integral_constant<int, 8>());
-  if (D <= 32 * kEach) return f(std::integral_constant<int, 32>());
-  if (D <= 64 * kEach) return f(std::integral_constant<int, 64>());
-  if (D <= 128 * kEach) return f(std::integral_constant<int, 128>());
-  if (D <= 256 * kEach) return f(std::integral_constant<int, 256>());
-  if (D <= 512 * kEach) return f(std::integral_constant<int, 512>());
+  if (D <= 8 * EACH) return f(std::integral_constant<int, 8>());
+  if (D <= 32 * EACH) return f(std::integral_constant<int, 32>());
+  if (D <= 64 * EACH) return f(std::integral_constant<int, 64>());
+  if (D <= 128 * EACH) return f(std::integral_constant<int, 128>());
+  if (D <= 256 * EACH) return f(std::integral_constant<int, 256>());
+  if (D <= 512 * EACH) return f(std::integral_constant<int, 512>());
   return f(std::integral_constant<int, 1024>());
 }
 
@@ -430,8 +491,8 @@ cudaError_t run_forward(const RmsNormArgs& a, cudaStream_t s) {
   const bool wide = a.D % V == 0 && rows_wide(a.x, a.ldx, V) && rows_wide(a.residual, a.ldr, V) &&
                     rows_wide(a.weight, 0, V) && rows_wide(a.y, a.ldy, V) && rows_wide(a.h, a.ldh, V);
   if (wide)
-    return with_threads<T, true>(a.D, [&](auto nt) { return launch_rows<T, decltype(nt)::value, true>(a, s); });
-  return with_threads<T, false>(a.D, [&](auto nt) { return launch_rows<T, decltype(nt)::value, false>(a, s); });
+    return with_threads<kEach>(a.D, [&](auto nt) { return launch_rows<T, decltype(nt)::value, true>(a, s); });
+  return with_threads<kEach>(a.D, [&](auto nt) { return launch_rows<T, decltype(nt)::value, false>(a, s); });
 }
 
 template <typename T>
@@ -440,7 +501,7 @@ cudaError_t run_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s) {
   float* part = a.dweight == nullptr ? nullptr : static_cast<float*>(a.ws);
   int parts = 0;
   cudaError_t e;
-  if (a.D > kLongest) {
+  if (a.D > kBackLongest<T>) {
     float* dot = static_cast<float*>(a.ws) + static_cast<int64_t>(kParts) * a.D;
     e = launch_kernel(rms_long_dot_kernel<T>, dim3(static_cast<unsigned>(a.rows)), dim3(kLongBlock), 0, s, 0u, a, dot);
     if (e != cudaSuccess) return e;
@@ -451,9 +512,9 @@ cudaError_t run_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s) {
     const bool wide = a.D % V == 0 && rows_wide(a.x, a.ldx, V) && rows_wide(a.dy, a.lddy, V) &&
                       rows_wide(a.dh, a.lddh, V) && rows_wide(a.weight, 0, V) && rows_wide(a.dx, a.lddx, V);
     if (wide)
-      e = with_threads<T, true>(a.D, [&](auto nt) { return launch_rows_backward<T, decltype(nt)::value, true>(a, part, &parts, num_sms, s); });
+      e = with_threads<kBackEach<T>>(a.D, [&](auto nt) { return launch_rows_backward<T, decltype(nt)::value, true>(a, part, &parts, num_sms, s); });
     else
-      e = with_threads<T, false>(a.D, [&](auto nt) { return launch_rows_backward<T, decltype(nt)::value, false>(a, part, &parts, num_sms, s); });
+      e = with_threads<kBackEach<T>>(a.D, [&](auto nt) { return launch_rows_backward<T, decltype(nt)::value, false>(a, part, &parts, num_sms, s); });
   }
   if (e != cudaSuccess || part == nullptr) return e;
   return launch_kernel(rms_dweight_kernel<T>, dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(512), 0, s, 0u,
@@ -464,7 +525,7 @@ cudaError_t run_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s) {
 
 size_t rms_norm_workspace_bytes(int64_t rows, int64_t D) {
   const int64_t parts = std::min<int64_t>(rows, kParts);
-  return static_cast<size_t>(D > kLongest ? (kParts * D + rows) * 4 : parts * D * 4);
+  return static_cast<size_t>(D > kBackLongest<float> ? (kParts * D + rows) * 4 : parts * D * 4);  // either type's
 }
 
 cudaError_t launch_rms_norm(const RmsNormArgs& a, int, cudaStream_t s) {
