@@ -380,8 +380,8 @@ def mpc_quant_decompress(codes, scale, minv, row_len: int, bits: int, y=None, st
     if y is None:
         y = torch.empty((R, row_len), dtype=torch.float32, device=scale.device)
     _cuda(y, torch.float32, "y")
-    _check(lib().mpc_quant_decompress(_ptr(codes), _ptr(scale), _ptr(minv), R, row_len, bits,
-                                      _ptr(y), _stream(stream)))
+    _check(lib().mpc_quant_decompress(codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), R, row_len, bits,
+                                      y.data_ptr(), _stream(stream)))
     return y
 
 
@@ -693,6 +693,19 @@ def _ld(t, name: str, rows: int, cols: int, of, index: int) -> int:
     return ld
 
 
+def _operand(x, name: str):
+    """(rows, columns, row distance, device index) of the matrix that the other operands go by."""
+    if isinstance(x, torch.Tensor) and x.dtype in _DTYPES and x.dim() == 2 and x.is_contiguous():
+        index = x.get_device()
+        rows, cols = x.shape
+        if index >= 0 and cols > 0:
+            return rows, cols, cols, index
+    ld = _matrix(x, name)
+    if x.shape[1] == 0:
+        raise MpcError(1, "the rows of %s must hold at least one entry" % name)
+    return x.shape[0], x.shape[1], ld, x.get_device()
+
+
 def _like(t, rows: int, cols: int, of, name: str, index: int, stream):
     """An output matrix of the type and device of `of`: the caller's, checked, or a new one; its row distance."""
     if t is None:
@@ -726,53 +739,51 @@ def mpc_dropout(x, p: float, seed: int = 0, residual=None, step=None, y=None, st
     tensor of one entry) makes the same one, so the gradient of x is this call on the gradient of y."""
     kind = _dtype(x, "x")
     index = x.get_device()
-    _cuda(x, x.dtype, "x")
-    for name, t in (("residual", residual), ("y", y)):
-        if t is not None:
+    for name, t in (("x", x), ("residual", residual), ("y", y)):
+        if t is not None and not (isinstance(t, torch.Tensor) and t.dtype is x.dtype and t.get_device() == index
+                                  and t.shape == x.shape and t.is_contiguous()):
             _cuda(t, x.dtype, name)
-            if t.shape != x.shape or t.get_device() != index:
-                raise MpcError(1, "%s must have the shape and device of x" % name)
+            raise MpcError(1, "%s must have the shape and device of x" % name)
     if y is None:
         y = torch.empty_like(x)
-        _on(stream, y)
+        if stream is not None:
+            y.record_stream(stream)
     _call(lib().mpc_dropout, x, index, stream, x.data_ptr(), None if residual is None else residual.data_ptr(), x.numel(),
           kind, p, seed & _SEEDS, None if step is None else _step(step, x.device), y.data_ptr())
     return y
 
 
-def _norm_args(x, weight, residual, h, rstd, stream):
-    ldx = _matrix(x, "x")
-    rows, D = x.shape
-    index = x.get_device()
-    if D == 0:
-        raise MpcError(1, "the rows of x must hold at least one entry")
-    w = _vector_like(weight, D, x, "weight", index)
-    ldr = ldh = 0
-    if residual is not None:
-        ldr = _ld(residual, "residual", rows, D, x, index)
-        h, ldh = _like(h, rows, D, x, "h", index, stream)
-    elif h is not None:
-        raise MpcError(1, "h is the sum with a residual; without one it is x")
-    rstd = _vector_or_new(rstd, rows, "rstd", x.device, stream)
-    return rows, D, index, ldx, w, None if residual is None else residual.data_ptr(), ldr, h, \
-        None if h is None else h.data_ptr(), ldh, rstd
+def _summed(x, rows: int, D: int, index: int, residual, h, stream):
+    """(residual's address and row distance, h, its address and row distance) of a norm's call."""
+    if residual is None:
+        if h is not None:
+            raise MpcError(1, "h is the sum with a residual; without one it is x")
+        return None, 0, x, None, 0
+    ldr = _ld(residual, "residual", rows, D, x, index)
+    h, ldh = _like(h, rows, D, x, "h", index, stream)
+    return residual.data_ptr(), ldr, h, h.data_ptr(), ldh
 
 
 def mpc_rms_norm_forward(x, weight, eps: float = 1e-6, residual=None, y=None, h=None, rstd=None, stream=None):
     """Root-mean-square norm of the rows of x [R, D], after the residual's addition where there is one.
     Returns (y, h, rstd): h = x + residual in the type of x (x itself without a residual), rstd [R] fp32."""
-    rows, D, index, ldx, w, r, ldr, h, hp, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    rows, D, ldx, index = _operand(x, "x")
+    w = _vector_like(weight, D, x, "weight", index)
+    r, ldr, h, hp, ldh = _summed(x, rows, D, index, residual, h, stream)
     y, ldy = _like(y, rows, D, x, "y", index, stream)
+    rstd = _vector_or_new(rstd, rows, "rstd", x.device, stream)
     _call(lib().mpc_rms_norm_forward, x, index, stream, x.data_ptr(), ldx, r, ldr, w, rows, D, _DTYPES[x.dtype], eps,
           y.data_ptr(), ldy, hp, ldh, rstd.data_ptr())
-    return y, x if h is None else h, rstd
+    return y, h, rstd
 
 
 def mpc_rms_norm_quant(x, weight, eps: float = 1e-6, residual=None, codes=None, scale=None, minv=None, h=None,
                        rstd=None, stream=None):
     """The same norm with its output as an 8-bit quantisation payload for mpc_quant_decompress.  Returns
     (codes [R, W] int32 of uint32 words, scale [R], minv [R], h, rstd)."""
-    rows, D, index, ldx, w, r, ldr, h, hp, ldh, rstd = _norm_args(x, weight, residual, h, rstd, stream)
+    rows, D, ldx, index = _operand(x, "x")
+    w = _vector_like(weight, D, x, "weight", index)
+    r, ldr, h, hp, ldh = _summed(x, rows, D, index, residual, h, stream)
     W = (D + 15) // 16 * 4
     if codes is None:
         codes = torch.empty((rows, W), dtype=torch.int32, device=x.device)
@@ -781,9 +792,10 @@ def mpc_rms_norm_quant(x, weight, eps: float = 1e-6, residual=None, codes=None, 
         _vector(codes, rows * W, torch.int32, "codes", x.device)
     scale = _vector_or_new(scale, rows, "scale", x.device, stream)
     minv = _vector_or_new(minv, rows, "minv", x.device, stream)
+    rstd = _vector_or_new(rstd, rows, "rstd", x.device, stream)
     _call(lib().mpc_rms_norm_quant, x, index, stream, x.data_ptr(), ldx, r, ldr, w, rows, D, _DTYPES[x.dtype], eps,
           codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), hp, ldh, rstd.data_ptr())
-    return codes, scale, minv, x if h is None else h, rstd
+    return codes, scale, minv, h, rstd
 
 
 def mpc_rms_norm_workspace_bytes(rows: int, row_len: int) -> int:
@@ -794,11 +806,7 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
                           stream=None):
     """The gradient of mpc_rms_norm_forward from its h and rstd: (dx, dweight).  ``dh`` is the gradient that
     reaches h by other ways; dx is that of x and of residual alike.  ``need_weight`` False leaves dweight out."""
-    ldh = _matrix(h, "h")
-    rows, D = h.shape
-    index = h.get_device()
-    if D == 0:
-        raise MpcError(1, "the rows of h must hold at least one entry")
+    rows, D, ldh, index = _operand(h, "h")
     lddy = _ld(dy, "dy", rows, D, h, index)
     lddh = 0 if dh is None else _ld(dh, "dh", rows, D, h, index)
     w = _vector_like(weight, D, h, "weight", index)
@@ -842,14 +850,11 @@ def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, of, str
 
 
 def _linear_args(x, w):
-    ldx = _matrix(x, "x")
-    rows, K = x.shape
-    index = x.get_device()
-    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+    rows, K, ldx, index = _operand(x, "x")
+    N = w.shape[0] if isinstance(w, torch.Tensor) and w.dim() == 2 else 0
+    if N == 0:
         _matrix(w, "w", K, x)
-    N = w.shape[0]
-    if K == 0 or N == 0:
-        raise MpcError(1, "x [R, K] and w [N, K] must have K >= 1 and N >= 1")
+        raise MpcError(1, "w [N, K] must have N >= 1")
     return rows, K, N, index, ldx, _ld(w, "w", N, K, x, index), _DTYPES[x.dtype]
 
 
