@@ -259,7 +259,7 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t blocks, int planes) {
     const int64_t nt = (n + tn - 1) / tn, tiles = mt * nt, full = tiles / kPairs * kPairs, rest = tiles - full;
     const double copies = planes * (kBytesA + tn / 2 * kK * 2) / 55.0, products = (planes == 1 ? 2.0 : 12.0) * tn;
     const double step = std::max(copies, products) + 20.0, end = 3000.0 + 4000.0 * tn / kN;
-    const double tile = std::max(blocks * step, 3000.0 * tn / kN);  // or its epilogue
+    const double tile = std::max(blocks * step, 2500.0 + 3500.0 * tn / kN);  // or its epilogue
     for (int s = 1; s <= kMostSplits && s <= blocks; ++s) {
       if (s > 1 && rest == 0) break;
       double cost = tiles / kPairs * tile + end;
@@ -351,7 +351,11 @@ cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, i
   g.whole = static_cast<int>(cut.whole);
   g.splits = cut.splits;
   g.tile_n = cut.tile_n;
-  g.group = 8;
+  g.group = static_cast<int>(std::min<int64_t>(8, mt));
+  const int64_t over = mt % g.group;
+  g.band = divisor(static_cast<uint32_t>(g.group * nt));
+  g.rows = divisor(static_cast<uint32_t>(g.group));
+  g.last_rows = divisor(static_cast<uint32_t>(over > 0 ? over : g.group));
   g.chunk = P == 1 ? 128 : 2;
   g.sum = sum;
   auto on = [&](uintptr_t bytes) {

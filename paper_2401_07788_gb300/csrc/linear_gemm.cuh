@@ -31,6 +31,24 @@ namespace {
 // ---------------------------------------------------------------------------
 enum LinearMode { kForward, kDx, kDw };
 
+// Quotient and remainder by a divisor that the host knows (a division takes 40 instructions, three of
+// them a tile and warp).
+struct Divisor {
+  uint32_t d, inverse;  // floor(2^32 / d): its quotient is at most one too small
+  __device__ __forceinline__ uint32_t of(uint32_t i, uint32_t* rest) const {
+    uint32_t q = __umulhi(i, inverse), r = i - q * d;
+    if (r >= d) {
+      ++q;
+      r -= d;
+    }
+    *rest = r;
+    return q;
+  }
+};
+inline Divisor divisor(uint32_t d) {
+  return Divisor{d, d == 1 ? 0xffffffffu : static_cast<uint32_t>((uint64_t{1} << 32) / d)};
+}
+
 struct LinearGemm {
   int m, n;            // of C
   int blocks;          // K blocks of 64
@@ -38,6 +56,7 @@ struct LinearGemm {
   int whole;           // tiles formed in one piece; the others, the last ones, in `splits` parts of K
   int splits;
   int group;           // row tiles that run together over all columns
+  Divisor band, rows, last_rows;  // by the tiles of a group, its row tiles, those of the last group
   int tile_n, chunk;
   float* sum;          // [split][tiles in parts][256][tile_n]
   int wide;            // y, z and residual have rows on 16 bytes (1), on 32 (2)
@@ -73,11 +92,11 @@ struct LinearTile {
 // tiles: of 76 pairs, 8 x 9.5 read 18 strips of operands where one row tile after the
 // other over all of a large x would read it from HBM once a wave.
 __device__ __forceinline__ void place_tile(const LinearGemm& g, int i, int* m0, int* n0) {
-  const int band = g.group * g.n_tiles, b = i / band, first = b * g.group;
-  const int rows = min(g.group, g.m_tiles - first);
-  i -= b * band;
-  *m0 = (first + i % rows) * kPair;
-  *n0 = i / rows * g.tile_n;
+  uint32_t in, row;
+  const uint32_t first = g.band.of(i, &in) * g.group;
+  const uint32_t col = (first + g.group <= static_cast<uint32_t>(g.m_tiles) ? g.rows : g.last_rows).of(in, &row);
+  *m0 = static_cast<int>(first + row) * kPair;
+  *n0 = static_cast<int>(col) * g.tile_n;
 }
 __device__ __forceinline__ int linear_units(const LinearGemm& g) {
   return g.whole + (g.m_tiles * g.n_tiles - g.whole) * g.splits;
@@ -537,7 +556,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
           if (q + 1 == max(pieces, 1)) {  // its columns are in registers
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+            if (lane == 0) mbar_arrive_relaxed(dsmem_addr(&taken[n & 1], 0));
           }
           if (q < pieces) out(q, v);
         }
@@ -573,7 +592,7 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
             tc_fence_before();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(dsmem_addr(&taken[n & 1], 0));
+          if (lane == 0) mbar_arrive_relaxed(dsmem_addr(&taken[n & 1], 0));
         }
         if (!ok) break;
 #pragma unroll
