@@ -50,11 +50,14 @@ __device__ __forceinline__ float fdiv(float a, float b) { return __fdiv_rn(a, b)
 
 // splitmix64 (Steele, Lea & Flood, OOPSLA 2014) at counter c: the finaliser
 // applied to seed + (c + 1) * golden-ratio increment.
-__device__ __forceinline__ uint64_t splitmix64_at(uint64_t seed, uint64_t c) {
-  uint64_t z = seed + (c + 1u) * 0x9E3779B97F4A7C15ull;
+constexpr uint64_t kSplitmixStep = 0x9E3779B97F4A7C15ull;
+__device__ __forceinline__ uint64_t splitmix64_of(uint64_t z) {
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
   z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
   return z ^ (z >> 31);
+}
+__device__ __forceinline__ uint64_t splitmix64_at(uint64_t seed, uint64_t c) {
+  return splitmix64_of(seed + (c + 1u) * kSplitmixStep);
 }
 
 // Magnitude key of a float: its bit pattern without the sign.  For

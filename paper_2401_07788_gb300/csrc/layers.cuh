@@ -53,31 +53,45 @@ __device__ __forceinline__ uint4 pack16(const float (&x)[8]) {
 // For bf16 results the exponential and the quotient are the approximate ones (2 ulp),
 // and 1 - erf is formula 7.1.26 of Abramowitz and Stegun (1.5e-7 off at most).
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float exp_of(float x, bool fast) { return fast ? __expf(x) : expf(x); }
-__device__ __forceinline__ float over(float a, float b, bool fast) { return fast ? __fdividef(a, b) : fdiv(a, b); }
-__device__ __forceinline__ float sigmoid(float v, bool fast) {
-  // __fdividef(1, d) is 0 from d = 2^126 on, where s is below any sum's last digit
-  return over(1.0f, fadd(1.0f, exp_of(-v, fast)), fast);
+// 2^x and 1 / x, approximate (2 ulp), subnormal numbers as 0: one instruction each.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-// Phi(z), with e = exp(-z^2 / 2).
-__device__ __forceinline__ float normal_cdf(float z, float e, bool fast) {
-  if (!fast) return fmul(0.5f, fadd(1.0f, erff(fmul(z, 0.70710678118654752f))));  // 6e-8 off at most
-  const float t = __fdividef(1.0f, __fmaf_rn(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
-  float q = __fmaf_rn(t, 1.061405429f, -1.453152027f);
-  q = __fmaf_rn(t, q, 1.421413741f);
-  q = __fmaf_rn(t, q, -0.284496736f);
-  q = __fmaf_rn(t, q, 0.254829592f);
-  q = fmul(fmul(fmul(0.5f, t), q), e);  // Phi(-|z|)
+__device__ __forceinline__ float inverse_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+// s(v); fast: from -v log2 e.
+__device__ __forceinline__ float sigmoid(float v) { return fdiv(1.0f, fadd(1.0f, expf(-v))); }
+__device__ __forceinline__ float sigmoid_fast(float minus_log2) { return inverse_fast(fadd(1.0f, exp2_fast(minus_log2))); }
+// Phi(z); fast: with e = exp(-z^2 / 2).
+__device__ __forceinline__ float normal_cdf(float z) { return fmul(0.5f, fadd(1.0f, erff(fmul(z, 0.70710678118654752f)))); }  // 6e-8 off at most
+__device__ __forceinline__ float normal_cdf_fast(float z, float e) {
+  const float t = inverse_fast(__fmaf_rn(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.0f));
+  float q = __fmaf_rn(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  q = __fmaf_rn(t, q, 0.5f * 1.421413741f);
+  q = __fmaf_rn(t, q, 0.5f * -0.284496736f);
+  q = __fmaf_rn(t, q, 0.5f * 0.254829592f);
+  q = fmul(fmul(t, q), e);  // Phi(-|z|)
   return z < 0.0f ? q : fsub(1.0f, q);
 }
+__device__ __forceinline__ float bell_fast(float z) { return exp2_fast(fmul(fmul(z, z), -0.5f * kLog2E)); }
 constexpr float kTanhIn = 1.5957691216057308f;  // 2 sqrt(2/pi)
 template <bool FAST>
 __device__ __forceinline__ float act_value(int act, float z) {
   switch (act) {
     case MPC_ACT_RELU: return z > 0.0f ? z : z != z ? z : 0.0f;
-    case MPC_ACT_GELU: return fmul(z, normal_cdf(z, FAST ? __expf(fmul(fmul(z, z), -0.5f)) : 0.0f, FAST));
-    case MPC_ACT_GELU_TANH: return fmul(z, sigmoid(fmul(fmul(z, kTanhIn), __fmaf_rn(fmul(z, z), 0.044715f, 1.0f)), FAST));
-    case MPC_ACT_SILU: return fmul(z, sigmoid(z, FAST));
+    case MPC_ACT_GELU: return fmul(z, FAST ? normal_cdf_fast(z, bell_fast(z)) : normal_cdf(z));
+    case MPC_ACT_GELU_TANH: {
+      const float zz = fmul(z, z);
+      if (FAST) return fmul(z, sigmoid_fast(fmul(z, __fmaf_rn(zz, -kTanhIn * kLog2E * 0.044715f, -kTanhIn * kLog2E))));
+      return fmul(z, sigmoid(fmul(fmul(z, kTanhIn), __fmaf_rn(zz, 0.044715f, 1.0f))));
+    }
+    case MPC_ACT_SILU: return fmul(z, FAST ? sigmoid_fast(fmul(z, -kLog2E)) : sigmoid(z));
     default: return z;
   }
 }
@@ -87,18 +101,19 @@ __device__ __forceinline__ float act_slope(int act, float z) {
   switch (act) {
     case MPC_ACT_RELU: return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
     case MPC_ACT_GELU: {
-      const float e = exp_of(fmul(fmul(z, z), -0.5f), FAST);
-      return __fmaf_rn(fmul(z, 0.3989422804014327f), e, normal_cdf(z, e, FAST));
+      const float e = FAST ? bell_fast(z) : expf(fmul(fmul(z, z), -0.5f));
+      return __fmaf_rn(fmul(z, 0.3989422804014327f), e, FAST ? normal_cdf_fast(z, e) : normal_cdf(z));
     }
     case MPC_ACT_GELU_TANH: {
       const float zz = fmul(z, z);
-      const float s = sigmoid(fmul(fmul(z, kTanhIn), __fmaf_rn(zz, 0.044715f, 1.0f)), FAST);
+      const float s = FAST ? sigmoid_fast(fmul(z, __fmaf_rn(zz, -kTanhIn * kLog2E * 0.044715f, -kTanhIn * kLog2E)))
+                           : sigmoid(fmul(fmul(z, kTanhIn), __fmaf_rn(zz, 0.044715f, 1.0f)));
       // s + z s (1 - s) dv/dz
-      const float dv = fmul(kTanhIn, __fmaf_rn(zz, 3.0f * 0.044715f, 1.0f));
+      const float dv = __fmaf_rn(zz, kTanhIn * 3.0f * 0.044715f, kTanhIn);
       return __fmaf_rn(fmul(z, dv), fmul(s, fsub(1.0f, s)), s);
     }
     case MPC_ACT_SILU: {
-      const float s = sigmoid(z, FAST);
+      const float s = FAST ? sigmoid_fast(fmul(z, -kLog2E)) : sigmoid(z);
       return fmul(s, __fmaf_rn(z, fsub(1.0f, s), 1.0f));
     }
     default: return 1.0f;
@@ -126,6 +141,12 @@ inline Drop make_drop(double p, uint64_t seed, const int64_t* step) {
 __device__ __forceinline__ uint64_t drop_seed(const Drop& d) {
   return d.seed + (d.step != nullptr ? static_cast<uint64_t>(*d.step) : 0ull);
 }
+// Draws of neighbouring counters: the state of one is the last one's plus a constant.
+struct Draws {
+  uint64_t state;
+  __device__ __forceinline__ Draws(uint64_t seed, uint64_t counter) : state(seed + counter * kSplitmixStep) {}
+  __device__ __forceinline__ uint64_t next() { return splitmix64_of(state += kSplitmixStep); }
+};
 // Whether part q (0..3) of a draw keeps its entry.
 __device__ __forceinline__ bool kept(uint64_t z, int q, uint32_t level) {
   const uint32_t w = static_cast<uint32_t>(q < 2 ? z : z >> 32);

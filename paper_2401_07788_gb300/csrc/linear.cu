@@ -92,11 +92,12 @@ __device__ __forceinline__ void make_dz(unsigned block, const Prepare<E>& f) {
       if (f.drop.level > 0) {
         const uint64_t at = static_cast<uint64_t>(r) * o.cols + c;
         const int off = static_cast<int>(at & 3) * 16;
-        uint64_t d = splitmix64_at(seed, at >> 2);
+        Draws draws(seed, at >> 2);
+        uint64_t d = draws.next();
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint64_t use = d;
-          if (off != 0 || q == 0) d = splitmix64_at(seed, (at >> 2) + q + 1);
+          if (off != 0 || q == 0) d = draws.next();
           if (off != 0) use = (use >> off) | (d << (64 - off));
 #pragma unroll
           for (int k = 0; k < 4; ++k)

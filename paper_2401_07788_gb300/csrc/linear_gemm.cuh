@@ -289,11 +289,12 @@ __device__ __forceinline__ void apply_act(int act, float* v) {
 template <int W>
 __device__ __forceinline__ void apply_drop(const Drop& d, uint64_t seed, uint64_t first, float* v) {
   const int off = static_cast<int>(first & 3) * 16;
-  uint64_t z = splitmix64_at(seed, first >> 2);
+  Draws draws(seed, first >> 2);
+  uint64_t z = draws.next();
 #pragma unroll
   for (int q = 0; q < W / 4; ++q) {
     uint64_t use = z;
-    if (off != 0 || q + 1 < W / 4) z = splitmix64_at(seed, (first >> 2) + q + 1);
+    if (off != 0 || q + 1 < W / 4) z = draws.next();
     if (off != 0) use = (use >> off) | (z << (64 - off));
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[4 * q + k] = kept(use, k, d.level) ? fmul(v[4 * q + k], d.scale) : 0.0f;
@@ -321,7 +322,9 @@ __device__ __forceinline__ void add_bias(const T* bias, bool wide, int left, flo
 // What is done to 32 columns of an epilogue warp's 32 rows, from row m0 and column n on, a row a
 // lane: v[j] = C[m0 + lane][n + j].
 template <int MODE, int PLANES>
-__device__ __forceinline__ void linear_piece(const LinearGemm& g, int m0, int n, uint64_t seed, float (&v)[32], uint8_t* box) {
+__device__ __forceinline__ void linear_piece(const LinearGemm& g, int m0, int n, uint64_t seed, float (&v)[32],
+                                             const Ahead<typename std::conditional<PLANES == 1, __nv_bfloat16, float>::type>& ahead,
+                                             uint8_t* box) {
   using T = typename std::conditional<PLANES == 1, __nv_bfloat16, float>::type;
   const int lane = threadIdx.x & 31, m = m0 + lane, rows = min(g.m - m0, 32), left = g.n - n;
   auto store = [&](void* base, int64_t ld) {
@@ -331,8 +334,6 @@ __device__ __forceinline__ void linear_piece(const LinearGemm& g, int m0, int n,
   };
   if (MODE == kForward) {
     const T* r = static_cast<const T*>(g.residual) + n;
-    Ahead<T> ahead;  // fp32: no registers are left for it
-    if (PLANES == 1 && g.residual != nullptr && g.wide != 0) load_wide<T>(r + min(m, g.m - 1) * g.ldr, left, ahead);
     if (g.bias != nullptr) add_bias<T, 32>(static_cast<const T*>(g.bias) + n, g.bias_wide, left, v);
     if (g.z != nullptr) store(g.z, g.ldz);
     apply_act<32, PLANES == 1>(g.act, v);
@@ -534,9 +535,18 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
       const int pieces = m0 < g.m && width > 0 ? min((width + 31) / 32, g.tile_n > 128 ? 2 : 1) : 0;
       const uint32_t columns = first + (static_cast<uint32_t>(quad * 32) << 16);
       const int row = rank * kM + quad * 32 + lane;
+      // the residual's bytes come while the products run (fp32: no registers are left for them)
+      using T = typename std::conditional<PLANES == 1, __nv_bfloat16, float>::type;
+      Ahead<T> ahead[kPieces];
+      if (MODE == kForward && PLANES == 1 && g.residual != nullptr && g.wide != 0 && t.slot < 0) {
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q)
+          if (q < pieces)
+            load_wide<T>(static_cast<const T*>(g.residual) + min(m0 + lane, g.m - 1) * g.ldr + n0 + 32 * q, g.n - n0 - 32 * q, ahead[q]);
+      }
       auto out = [&](int q, float (&v)[32]) {
         if (t.slot >= 0) sum_piece(g, t.slot, row, first + 32 * q, v);
-        else linear_piece<MODE, PLANES>(g, m0, n0 + 32 * q, seed, v, box);
+        else linear_piece<MODE, PLANES>(g, m0, n0 + 32 * q, seed, v, ahead[q], box);
       };
       bool ok = true;
       if (ONE) {
