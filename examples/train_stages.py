@@ -1,13 +1,14 @@
 """A small language model trained in pipeline stages with compressed boundaries (one GPU).
 
 The model is cut into stages; after each but the last a CompressionBoundary sends the compressed
-activation forward and the compressed gradient back.  The last stage's loss is the linear cross
+activation forward and the compressed gradient back.  The layers are the library's: norms, and linear
+layers whose activation, dropout and residual are part of their products.  The last stage's loss is the linear cross
 entropy over the vocabulary, without its logits, and every stage takes its own AdamW step with
 clipping by the gradient norm.  The data are synthetic: a random walk over the vocabulary in which
 each word has a few likely successors, with some positions padded (target -100).
 
     python examples/train_stages.py [--steps 200] [--vocab 50257] [--width 256] [--stages 3]
-        [--state-bits 8] [--topk 20]
+        [--state-bits 8] [--topk 20] [--dropout 0.0]
 """
 
 import argparse
@@ -25,12 +26,12 @@ import paper_2401_07788_gb300 as mpc  # noqa: E402
 class Stage(torch.nn.Module):
     """Embedding (first stage only), then residual blocks of a causal average and an MLP."""
 
-    def __init__(self, width, blocks, vocab=None):
+    def __init__(self, width, blocks, vocab=None, dropout=0.0):
         super().__init__()
         self.embed = None if vocab is None else torch.nn.Embedding(vocab, width)
-        self.norms = torch.nn.ModuleList(torch.nn.LayerNorm(width) for _ in range(blocks))
-        self.mix = torch.nn.ModuleList(torch.nn.Linear(2 * width, 2 * width) for _ in range(blocks))
-        self.out = torch.nn.ModuleList(torch.nn.Linear(2 * width, width) for _ in range(blocks))
+        self.norms = torch.nn.ModuleList(mpc.RMSNorm(width) for _ in range(blocks))
+        self.mix = torch.nn.ModuleList(mpc.Linear(2 * width, 2 * width, act="gelu") for _ in range(blocks))
+        self.out = torch.nn.ModuleList(mpc.Linear(2 * width, width, p=dropout) for _ in range(blocks))
 
     def forward(self, x):
         if self.embed is not None:
@@ -39,7 +40,7 @@ class Stage(torch.nn.Module):
             y = norm(x)
             count = torch.arange(1, y.shape[1] + 1, device=y.device, dtype=y.dtype)[:, None]
             y = torch.cat([y, y.cumsum(1) / count], dim=-1)
-            x = x + out(torch.nn.functional.gelu(mix(y)))
+            x = out(mix(y), residual=x)
         return x
 
 
@@ -60,10 +61,10 @@ def batches(vocab, batch, length, seed, device):
 
 
 def train(steps=200, vocab=50257, width=256, stages=3, blocks=2, batch=16, length=64, topk=20, state_bits=8,
-          lr=2e-3, seed=0, log=print):
+          lr=2e-3, seed=0, dropout=0.0, log=print):
     device = torch.device("cuda")
     torch.manual_seed(seed)
-    parts = [Stage(width, blocks, vocab if i == 0 else None).to(device) for i in range(stages)]
+    parts = [Stage(width, blocks, vocab if i == 0 else None, dropout).to(device) for i in range(stages)]
     body = mpc.with_boundaries(parts, lambda i: mpc.CompressionBoundary(
         mpc.TopK(topk, feedback="ef21"), mpc.Quant(8), rows="last"))
     head = mpc.LinearCrossEntropy(width, vocab, device=device)
@@ -99,4 +100,5 @@ if __name__ == "__main__":
     for name, value in (("steps", 200), ("vocab", 50257), ("width", 256), ("stages", 3), ("topk", 20),
                         ("state-bits", 8)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--dropout", type=float, default=0.0)
     train(**vars(ap.parse_args()))

@@ -89,21 +89,6 @@ __device__ __forceinline__ void make_dz(unsigned block, const Prepare<E>& f) {
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = to_float(x[j]);
-      if (f.drop.level > 0) {
-        const uint64_t at = static_cast<uint64_t>(r) * o.cols + c;
-        const int off = static_cast<int>(at & 3) * 16;
-        Draws draws(seed, at >> 2);
-        uint64_t d = draws.next();
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint64_t use = d;
-          if (off != 0 || q == 0) d = draws.next();
-          if (off != 0) use = (use >> off) | (d << (64 - off));
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (!kept(use, k, f.drop.level)) v[4 * q + k] = 0.0f;
-        }
-      }
       if (f.act != MPC_ACT_NONE) {
 #define MPC_EACH(A) \
   case A:           \
@@ -121,6 +106,21 @@ __device__ __forceinline__ void make_dz(unsigned block, const Prepare<E>& f) {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             if (j >= left) v[j] = 0.0f;
+        }
+      }
+      if (f.drop.level > 0) {  // last: what z holds in a dropped place reaches nothing
+        const uint64_t at = static_cast<uint64_t>(r) * o.cols + c;
+        const int off = static_cast<int>(at & 3) * 16;
+        Draws draws(seed, at >> 2);
+        uint64_t d = draws.next();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint64_t use = d;
+          if (off != 0 || q == 0) d = draws.next();
+          if (off != 0) use = (use >> off) | (d << (64 - off));
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (!kept(use, k, f.drop.level)) v[4 * q + k] = 0.0f;
         }
       }
 #pragma unroll

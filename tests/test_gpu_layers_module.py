@@ -243,3 +243,21 @@ def test_copies_of_a_module(mpc):
     want = a(x)
     assert torch.equal(b(x), want) and torch.equal(c(x), want)
     assert set(a.state_dict()) == {"weight", "bias"}
+
+
+def test_the_example_runs_on_the_layers(mpc):
+    """A few steps of the training example with dropout: finite losses, and every layer gets a gradient."""
+    import importlib.util
+    import os
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    spec = importlib.util.spec_from_file_location("train_stages", os.path.join(root, "examples", "train_stages.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.train(steps=3, vocab=200, width=64, stages=2, blocks=1, batch=4, length=32, dropout=0.1, log=None)
+    assert bool(losses.isfinite().all())
+    stage = example.Stage(64, 2, dropout=0.1).cuda()
+    x = torch.randn(2, 16, 64, device="cuda", requires_grad=True)
+    stage(x).sum().backward()
+    for p in (x, *stage.parameters()):
+        assert p.grad is not None and bool(p.grad.isfinite().all()) and p.grad.abs().sum() > 0

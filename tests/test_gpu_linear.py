@@ -178,6 +178,73 @@ def test_nan_stays_in_its_row(mpc, M, kind):
     assert not nan[torch.arange(M) != 1].any()
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_nan_in_dropped_places_of_the_gradient(mpc, kind):
+    """NaN of z and dy where dropout drops reaches nothing; elsewhere it reaches its row of dx and its column of db."""
+    M, K, N = 40, 64, 72
+    x, w, _, _, dy = make(19, M, K, N, forms.KINDS[kind])
+    _, z = mpc.mpc_linear_forward(x, w, act="silu", p=0.5, seed=6, keep=True)
+    clean = mpc.mpc_linear_backward(dy, x, w, z, act="silu", p=0.5, seed=6)
+    gone = forms.kept(6, M * N, 0.5).view(M, N).cuda() == 0
+    z[gone], dy[gone] = float("nan"), float("nan")
+    for a, c in zip(clean, mpc.mpc_linear_backward(dy, x, w, z, act="silu", p=0.5, seed=6)):
+        assert torch.equal(a, c)
+    row, col = (~gone).nonzero()[0].tolist()
+    z[row, col] = float("nan")
+    dx, _, db = mpc.mpc_linear_backward(dy, x, w, z, act="silu", p=0.5, seed=6)
+    assert dx[row].isnan().all() and db[col].isnan()
+    assert not dx[torch.arange(M) != row].isnan().any() and not db[torch.arange(N) != col].isnan().any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("limit", [1, 2, 20])
+def test_waits_of_one_and_a_few_tries(mpc, kind, limit):
+    """Whichever wait gives up first, the kernels return with nothing in flight: the status says so, and the calls
+    after that are as before."""
+    x, w, b, r, dy = make(20, 600, 1160, 1400, forms.KINDS[kind])
+
+    def calls():
+        y, z = mpc.mpc_linear_forward(x, w, b, r, act="gelu", p=0.1, seed=2, keep=True)
+        return (y, *mpc.mpc_linear_backward(dy, x, w, z, act="gelu", p=0.1, seed=2))
+
+    before = calls()
+    assert mpc.mpc_get_status() == 0
+    mpc.mpc_set_knob(mpc.MPC_KNOB_SPIN_LIMIT, limit)
+    try:
+        calls()
+        assert mpc.mpc_get_status() in (0, 5)
+    finally:
+        mpc.mpc_set_knob(mpc.MPC_KNOB_SPIN_LIMIT, 1 << 20)
+    assert mpc.mpc_get_status() == 0
+    for a, c in zip(before, calls()):
+        assert torch.equal(a, c)
+    assert mpc.mpc_get_status() == 0
+
+
+def test_two_streams_at_once(mpc):
+    """Calls on two streams, each with a workspace of its own, give what they give one after the other."""
+    sets = [make(30 + i, 700, 900, 1100, torch.float32) for i in range(2)]
+    want = [mpc.mpc_linear_backward(s[4], s[0], s[1]) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [mpc.mpc_linear_backward(s[4], s[0], s[1], stream=st) for s, st in zip(sets, streams)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, c) for a, c in zip(g, w))
+
+
+def test_pdl_knob_changes_nothing(mpc):
+    args = make(22, 520, 600, 700, torch.bfloat16)
+    first = check(mpc, *args, act="silu", p=0.1, seed=1)
+    mpc.mpc_set_knob(mpc.MPC_KNOB_PDL, 0)
+    try:
+        for a, c in zip(first, check(mpc, *args, act="silu", p=0.1, seed=1)):
+            assert torch.equal(a, c)
+    finally:
+        mpc.mpc_set_knob(mpc.MPC_KNOB_PDL, 1)
+
+
 def test_everything_dropped(mpc):
     x, w, b, r, dy = make(15, 40, 64, 48, torch.float32)
     y, _ = mpc.mpc_linear_forward(x, w, b, r, p=1.0, seed=3)
