@@ -374,8 +374,8 @@ __device__ __forceinline__ void landed(float (&v)[32]) {
   for (int j = 0; j < 32; ++j) asm volatile("" : "+f"(v[j]));  // nothing uses v before the wait
 }
 
-// ONE: a tile has one chunk, so the epilogue takes 32 columns at a time from tensor memory, the next
-// ones on their way; else it keeps its 64 in registers and adds the chunks.
+// ONE: a tile has one chunk, and the epilogue takes 32 columns at a time from tensor memory; else it
+// keeps its 64 in registers and adds the chunks.
 template <int MODE, int PLANES, bool ONE>
 __global__ void __launch_bounds__(kLinearThreads, 1)
     linear_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,

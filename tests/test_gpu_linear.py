@@ -76,6 +76,13 @@ def test_many_tiles(mpc, M, K, N, act, residual, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(9000, 2064, 2576), (2576, 9000, 2064), (70, 9001, 130)])
+def test_sums_of_several_chunks(mpc, M, K, N, kind):
+    """More K blocks than one accumulator of the matrix units sums, in whole tiles and in tiles cut along K."""
+    check(mpc, *make(M, M, K, N, forms.KINDS[kind]), act="gelu_tanh", p=0.1, seed=7)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("act", [None, "gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("bias,residual,p", [(False, False, 0.0), (True, False, 0.0), (False, True, 0.5), (True, True, 0.25)])
 @pytest.mark.parametrize("M,K,N", [(5, 40, 72), (150, 136, 200), (131, 99, 143)])
