@@ -174,37 +174,46 @@ __global__ void __launch_bounds__(256) linear_prepare_kernel(const Prepare<E> f)
 
 // db from the column sums: 32 columns a CTA, 8 rows of threads.
 template <typename E>
-__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* part, int64_t parts, int64_t out, float scale, E* db) {
+struct Bias {
+  const float* part;
+  int64_t parts, out;
+  float scale;
+  E* db;
+  unsigned blocks;
+};
+template <typename E>
+__device__ __forceinline__ void sum_bias(unsigned block, const Bias<E>& b) {
   __shared__ float sums[8][33];
-  pdl_begin();
-  pdl_end();
-  const int64_t col = blockIdx.x * int64_t{32} + (threadIdx.x & 31);
+  const int64_t col = block * int64_t{32} + (threadIdx.x & 31);
   const int r = threadIdx.x >> 5;
   float v = 0.0f;
-  if (col < out) {
-#pragma unroll 4
-    for (int64_t p = r; p < parts; p += 8) v = fadd(v, part[p * out + col]);
+  if (col < b.out) {
+#pragma unroll 8
+    for (int64_t p = r; p < b.parts; p += 8) v = fadd(v, b.part[p * b.out + col]);
   }
   sums[r][threadIdx.x & 31] = v;
   __syncthreads();
-  if (r == 0 && col < out) {
+  if (r == 0 && col < b.out) {
 #pragma unroll
     for (int p = 1; p < 8; ++p) v = fadd(v, sums[p][threadIdx.x]);
-    put(db + col, fmul(v, scale));
+    put(b.db + col, fmul(v, b.scale));
   }
 }
 
 // The tiles that were formed in parts of K, four columns a thread, and what the epilogue would have
 // done.
+struct Finish {
+  LinearGemm g;
+  unsigned blocks;  // 0: every tile was whole
+};
 template <typename E, bool FORWARD>
-__global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) {
-  pdl_begin();
-  pdl_end();
+__device__ __forceinline__ void finish_tiles(unsigned block, const Finish& f) {
+  const LinearGemm& g = f.g;
   const int rest = g.m_tiles * g.n_tiles - g.whole, groups = g.tile_n / 4;
   const int64_t part = static_cast<int64_t>(rest) * kPair * g.tile_n;
   const uint64_t seed = FORWARD && g.drop.level > 0 ? drop_seed(g.drop) : 0;
-  for (int64_t q = blockIdx.x * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(rest) * kPair * groups;
-       q += gridDim.x * int64_t{256}) {
+  for (int64_t q = block * int64_t{256} + threadIdx.x; q < static_cast<int64_t>(rest) * kPair * groups;
+       q += f.blocks * int64_t{256}) {
     const int row = static_cast<int>(q / groups), col = static_cast<int>(q - static_cast<int64_t>(row) * groups) * 4;
     int m0, n0;
     place_tile(g, g.whole + row / kPair, &m0, &n0);
@@ -243,6 +252,27 @@ __global__ void __launch_bounds__(256) linear_finish_kernel(const LinearGemm g) 
   }
 }
 
+// One launch for what a call has left to add: db, and the tiles in parts of its products.
+template <typename E, bool FORWARD>
+__global__ void __launch_bounds__(256) linear_finish_kernel(const Bias<E> bias, const Finish a, const Finish b) {
+  pdl_begin();
+  pdl_end();
+  unsigned block = blockIdx.x;
+  if (block < bias.blocks) {
+    sum_bias<E>(block, bias);
+    return;
+  }
+  block -= bias.blocks;
+  if (block < a.blocks) finish_tiles<E, FORWARD>(block, a);
+  else finish_tiles<E, FORWARD>(block - a.blocks, b);
+}
+template <typename E, bool FORWARD>
+cudaError_t launch_finish(const Bias<E>& bias, const Finish& a, const Finish& b, cudaStream_t s) {
+  const unsigned blocks = bias.blocks + a.blocks + b.blocks;
+  if (blocks == 0) return cudaSuccess;
+  return launch_kernel(linear_finish_kernel<E, FORWARD>, dim3(blocks), dim3(256), 0, s, 0u, bias, a, b);
+}
+
 // ---------------------------------------------------------------------------
 // Workspace and launches
 // ---------------------------------------------------------------------------
@@ -258,7 +288,7 @@ struct Cut {
 };
 constexpr int kMostSplits = 32;
 
-Cut cut_tiles(int64_t m, int64_t n, int64_t blocks, int planes) {
+Cut best_cut(int64_t m, int64_t n, int64_t blocks, int planes) {
   Cut best = {kN, 1, 0};
   double least = 1e300;
   const int64_t mt = (m + kPair - 1) / kPair;
@@ -285,6 +315,22 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t blocks, int planes) {
   }
   return best;
 }
+// The estimate weighs up to 128 candidates, and a call asks for it three times (for the size of its
+// workspace, to check that, and to launch): 15 us of the host for a backward call.  So each thread
+// keeps the answers for the sizes it asked for last.
+Cut cut_tiles(int64_t m, int64_t n, int64_t blocks, int planes) {
+  struct Known {
+    int64_t m, n, blocks;
+    int planes;
+    Cut cut;
+  };
+  static thread_local Known known[32] = {};
+  const uint64_t key = static_cast<uint64_t>(m) * 0x9E3779B97F4A7C15ull ^ static_cast<uint64_t>(n) * 0xBF58476D1CE4E5B9ull ^
+                       static_cast<uint64_t>(blocks * 4 + planes) * 0x94D049BB133111EBull;
+  Known& k = known[key >> 59];
+  if (k.m != m || k.n != n || k.blocks != blocks || k.planes != planes) k = Known{m, n, blocks, planes, best_cut(m, n, blocks, planes)};
+  return k.cut;
+}
 // Bytes of the sums.
 size_t cut_bytes(const Cut& c, int64_t m, int64_t n) {
   if (c.splits == 1) return 0;
@@ -293,7 +339,7 @@ size_t cut_bytes(const Cut& c, int64_t m, int64_t n) {
 }
 
 struct Layout {
-  size_t x, w, dz, part, sum, total;
+  size_t x, w, dz, part, sum, dw_sum, total;
   bool pack_x, pack_w, pack_dy;  // dy: where nothing else makes a dz of it
   int64_t Kp, Np;
   Cut forward, dx, dw;
@@ -323,7 +369,8 @@ Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_
     l.part = take((rows + dz_rows(rows, out) - 1) / dz_rows(rows, out) * out * 4);
     l.dx = cut_tiles(rows, in, (out + kK - 1) / kK, planes);
     l.dw = cut_tiles(out, in, (rows + kK - 1) / kK, planes);
-    l.sum = take(std::max(cut_bytes(l.dx, rows, in), cut_bytes(l.dw, out, in)));  // dx's are read before dw's are written
+    l.sum = take(cut_bytes(l.dx, rows, in));
+    l.dw_sum = take(cut_bytes(l.dw, out, in));
   }
   l.total = at;
   return l;
@@ -345,7 +392,7 @@ struct Matrix {
 
 template <int MODE, typename E>
 cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, int64_t n, int64_t k, const Cut& cut,
-                    float* sum, int num_sms, cudaStream_t s) {
+                    float* sum, int num_sms, cudaStream_t s, Finish* finish) {
   constexpr int P = sizeof(E) == 2 ? 1 : 3, size = static_cast<int>(sizeof(E));
   const int64_t mt = (m + kPair - 1) / kPair, nt = (n + cut.tile_n - 1) / cut.tile_n;
   const int64_t rest = mt * nt - cut.whole, units = cut.whole + rest * cut.splits;
@@ -381,9 +428,9 @@ cudaError_t product(LinearGemm g, const Matrix& a, const Matrix& b, int64_t m, i
   LIN_TRY(ensure_dynamic_smem(kernel, smem));
   const unsigned grid = static_cast<unsigned>(2 * std::min<int64_t>(units, num_sms / 2));
   LIN_TRY(launch_kernel(kernel, dim3(grid), dim3(kLinearThreads), smem, s, 2u, ma, mb, g));
-  if (rest == 0) return cudaSuccess;
-  const int64_t blocks = std::min<int64_t>(rest * (kPair / 4) * cut.tile_n / 256, int64_t{num_sms} * 16);
-  return launch_kernel(linear_finish_kernel<E, MODE == kForward>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, 0u, g);
+  finish->g = g;
+  finish->blocks = static_cast<unsigned>(std::min<int64_t>(rest * (kPair / 4) * cut.tile_n / 256, int64_t{num_sms} * 16));
+  return cudaSuccess;
 }
 
 template <typename E>
@@ -418,7 +465,9 @@ cudaError_t forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   g.status = a.status;
   const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
   const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
-  return product<kForward, E>(g, x, w, a.rows, a.out, a.in, l.forward, reinterpret_cast<float*>(ws + l.sum), num_sms, s);
+  Finish finish = {};
+  LIN_TRY(product<kForward, E>(g, x, w, a.rows, a.out, a.in, l.forward, reinterpret_cast<float*>(ws + l.sum), num_sms, s, &finish));
+  return launch_finish<E, true>(Bias<E>{}, finish, Finish{}, s);
 }
 
 template <typename E>
@@ -447,9 +496,10 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   if (l.pack_w && a.dx != nullptr) f.w = operand<E>(a.w, a.ldw, a.out, a.in, l.Kp, reinterpret_cast<uint16_t*>(ws + l.w), num_sms);
   const unsigned blocks = f.dy.blocks + f.x.blocks + f.w.blocks;
   if (blocks > 0) LIN_TRY(launch_kernel(linear_prepare_kernel<E, P>, dim3(blocks), dim3(256), 0, s, 0u, f));
+  Bias<E> bias = {};
   if (a.dbias != nullptr)
-    LIN_TRY(launch_kernel(linear_dbias_kernel<E>, dim3(static_cast<unsigned>((a.out + 31) / 32)), dim3(256), 0, s, 0u,
-                          static_cast<const float*>(part), chunks, a.out, f.drop.scale, static_cast<E*>(a.dbias)));
+    bias = {part, chunks, a.out, f.drop.scale, static_cast<E*>(a.dbias), static_cast<unsigned>((a.out + 31) / 32)};
+  Finish dx = {}, dw = {};
   LinearGemm g = {};
   g.drop = f.drop;
   g.spin_limit = a.spin_limit;
@@ -460,15 +510,15 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
     const Matrix w = {l.pack_w ? ws + l.w : a.w, a.out, a.in, l.pack_w ? l.Kp : a.ldw};
     g.y = a.dx;
     g.ldy = a.lddx;
-    LIN_TRY(product<kDx, E>(g, dz, w, a.rows, a.in, a.out, l.dx, sum, num_sms, s));
+    LIN_TRY(product<kDx, E>(g, dz, w, a.rows, a.in, a.out, l.dx, sum, num_sms, s, &dx));
   }
   if (a.dw != nullptr) {
     const Matrix x = {l.pack_x ? ws + l.x : a.x, a.rows, a.in, l.pack_x ? l.Kp : a.ldx};
     g.y = a.dw;
     g.ldy = a.lddw;
-    LIN_TRY(product<kDw, E>(g, dz, x, a.out, a.in, a.rows, l.dw, sum, num_sms, s));
+    LIN_TRY(product<kDw, E>(g, dz, x, a.out, a.in, a.rows, l.dw, reinterpret_cast<float*>(ws + l.dw_sum), num_sms, s, &dw));
   }
-  return cudaSuccess;
+  return launch_finish<E, false>(bias, dx, dw, s);
 }
 
 }  // namespace
