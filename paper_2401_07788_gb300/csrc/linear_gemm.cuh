@@ -387,8 +387,8 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
   __shared__ uint64_t full[stages], empty[stages], done[2], taken[2], drain;
   __shared__ uint32_t tmem;
   uint8_t* stage0 = raw + (1024 - (smem_addr(raw) & 1023)) % 1024;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = static_cast<int>(cluster_rank());
+  const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = blockIdx.x & 1;
   if (threadIdx.x == 0) {
     for (int i = 0; i < stages; ++i) {
       mbar_init(&full[i], 1);
@@ -414,30 +414,27 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (warp == 0) {
-    if (lane == 0) {
-      fence_proxy_async_all();  // operands that earlier kernels wrote
-      uint32_t it = 0;
-      bool ok = true;
-      // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
-      const int b_blocks = (g.tile_n / 2 + 63) / 64;
-      const uint32_t bytes = 2 * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
-      const uint32_t full0 = dsmem_addr(full, 0);
-      uint32_t st = 0, parity = 1;  // of the stage's `empty` to wait for
-      for (int i = pair; i < total && ok; i += pairs) {
-        const LinearTile t = linear_tile(g, i);
-        const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g.n, t.n0, g.tile_n) / 2);
-        int kb = t.k0, p = PLANES - 1;  // planes in the order in which they are given back
-        for (int left = (t.k1 - t.k0) * PLANES; left > 0; --left, ++it) {
-          ok = mbar_wait_bounded(&empty[st], parity, g.spin_limit, g.status);
-          if (!ok) break;
-          const uint32_t bar = full0 + st * 8;
+    const bool leader = elect_one();
+    fence_proxy_async_all();  // operands that earlier kernels wrote
+    uint32_t it = 0;
+    bool ok = true;
+    // a CTA's rows of B in a stage: half the tile's, in blocks of 64 where they are columns
+    const int b_blocks = (g.tile_n / 2 + 63) / 64;
+    const uint32_t bytes = 2 * (kBytesA + (B_MN ? b_blocks * kK * 128 : g.tile_n / 2 * kK * 2));
+    const uint32_t full0 = dsmem_addr(full, 0);
+    uint32_t st = 0, parity = 1;  // of the stage's `empty` to wait for
+    for (int i = pair; i < total && ok; i += pairs) {
+      const LinearTile t = linear_tile(g, i);
+      const int m0 = t.m0 + rank * kM, n0 = t.n0 + rank * (tile_cols(g.n, t.n0, g.tile_n) / 2);
+      int kb = t.k0, p = PLANES - 1;  // planes in the order in which they are given back
+      for (int left = (t.k1 - t.k0) * PLANES; left > 0; --left, ++it) {
+        ok = __all_sync(kFull, mbar_wait_bounded(&empty[st], parity, g.spin_limit, g.status));
+        if (!ok) break;
+        const uint32_t bar = full0 + st * 8;
+        uint8_t* a = stage0 + st * kStageBytes;
+        uint8_t* b = a + kBytesA;
+        if (leader) {
           if (rank == 0) mbar_arrive_expect_tx(&full[st], bytes);
-          uint8_t* a = stage0 + st * kStageBytes;
-          uint8_t* b = a + kBytesA;
-          if (++st == stages) {
-            st = 0;
-            parity ^= 1;
-          }
           if (A_MN) {
 #pragma unroll
             for (int q = 0; q < kM / 64; ++q) tensor_g2s(a + q * kK * 128, &map_a, m0 + q * 64, kb * kK, p, bar);
@@ -449,16 +446,23 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
           } else {
             tensor_g2s(b, &map_b, kb * kK, n0, p, bar);
           }
-          if (PLANES == 1 || --p < 0) {
-            p = PLANES - 1;
-            ++kb;
-          }
+        }
+        __syncwarp();
+        if (++st == stages) {
+          st = 0;
+          parity ^= 1;
+        }
+        if (PLANES == 1 || --p < 0) {
+          p = PLANES - 1;
+          ++kb;
         }
       }
-      // Copies in flight must land before either CTA leaves (the cluster barrier
-      // below).  The first CTA's barriers count both CTAs' copies.  The second CTA knows
-      // its own by the products that read them, which have not been formed where the
-      // first one gave up: then it gives them a millisecond.
+    }
+    // Copies in flight must land before either CTA leaves (the cluster barrier
+    // below).  The first CTA's barriers count both CTAs' copies.  The second CTA knows
+    // its own by the products that read them, which have not been formed where the
+    // first one gave up: then it gives them a millisecond.
+    if (lane == 0) {
       if (rank == 0) {
         for (uint32_t i = it > stages ? it - stages : 0; i < it; ++i)
           mbar_wait_bounded(&full[i % stages], i / stages & 1, kDrainPolls, g.status);
@@ -472,8 +476,9 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      const uint32_t base = smem_addr(stage0), acc = tmem;
+    if (rank == 0) {
+      const bool leader = elect_one();
+      const uint32_t base = smem_addr(stage0), acc = __shfl_sync(kFull, tmem, 0);
       const uint64_t a0 = A_MN ? smem_desc(base, kK * 128, 1024) : smem_desc(base, 16, 1024);
       const uint64_t b0 = B_MN ? smem_desc(base + kBytesA, kK * 128, 1024) : smem_desc(base + kBytesA, 16, 1024);
       // 16 K-elements on: 32 bytes along a row, or 16 rows of 128 bytes
@@ -485,46 +490,50 @@ __global__ void __launch_bounds__(kLinearThreads, 1)
         const LinearTile t = next;
         const uint32_t idesc = mma_desc(kPair, tile_cols(g.n, t.n0, g.tile_n), A_MN, B_MN);
         for (int c = t.k0; c < t.k1 && ok; c += g.chunk, ++n) {
-          ok = mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status);
+          ok = __all_sync(kFull, mbar_wait_bounded(&taken[n & 1], (n / 2 & 1) ^ 1, g.spin_limit, g.status));
           tc_fence_after();
           const uint32_t d = acc + (n & 1) * kN;
-          bool fresh = true;
           const int steps = min(g.chunk, t.k1 - c);
           for (int k = 0; k < steps; ++k) {
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) ok = ok && mbar_wait_bounded(&full[st + p], parity, g.spin_limit, g.status);
+            for (int p = 0; p < PLANES; ++p)
+              ok = ok && __all_sync(kFull, mbar_wait_bounded(&full[st + p], parity, g.spin_limit, g.status));
             if (!ok) break;
-            const uint32_t now = st;
+            tc_fence_after();
+            const uint64_t as = a0 + st * (kStageBytes >> 4), bs = b0 + st * (kStageBytes >> 4);
+            if (leader) {
+#pragma unroll
+              for (int term = 0; term < (PLANES == 1 ? 1 : 6); ++term) {
+                int pa, pb;
+                term_planes<PLANES>(term, &pa, &pb);
+#pragma unroll
+                for (int q = 0; q < kK / 16; ++q)
+                  mma_bf16(d, as + (PLANES - 1 - pa) * (kStageBytes >> 4) + q * kStepA,
+                           bs + (PLANES - 1 - pb) * (kStageBytes >> 4) + q * kStepB, idesc, term == 0 && q == 0 && k == 0);
+                // a plane is given back after its last product
+                if (PLANES == 1 || term == 5) mma_commit_pair(&empty[st + PLANES - 1]);
+                else if (term == 1) mma_commit_pair(&empty[st]);
+                else if (term == 4) mma_commit_pair(&empty[st + 1]);
+              }
+              if (k + 1 == steps) mma_commit_pair(&done[n & 1]);
+            }
+            __syncwarp();
             st += PLANES;
             if (st == stages) {
               st = 0;
               parity ^= 1;
             }
-            tc_fence_after();
-#pragma unroll
-            for (int term = 0; term < (PLANES == 1 ? 1 : 6); ++term) {
-              int pa, pb;
-              term_planes<PLANES>(term, &pa, &pb);
-              const uint64_t as = a0 + (now + PLANES - 1 - pa) * (kStageBytes >> 4), bs = b0 + (now + PLANES - 1 - pb) * (kStageBytes >> 4);
-#pragma unroll
-              for (int q = 0; q < kK / 16; ++q) {
-                mma_bf16(d, as + q * kStepA, bs + q * kStepB, idesc, fresh);
-                fresh = false;
-              }
-              // a plane is given back after its last product
-              if (PLANES == 1 || term == 5) mma_commit_pair(&empty[now + PLANES - 1]);
-              else if (term == 1) mma_commit_pair(&empty[now]);
-              else if (term == 4) mma_commit_pair(&empty[now + 1]);
-            }
             if (c + k == t.k0) next = linear_tile(g, min(i + pairs, total - 1));  // while these products run
           }
-          if (ok) mma_commit_pair(&done[n & 1]);
         }
       }
       // products in flight must end before the tensor memory and the stages are given
       // back, also where an epilogue that gave up no longer waits for them
-      mma_commit(&drain);
-      mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
+      if (leader) {
+        mma_commit(&drain);
+        mbar_wait_bounded(&drain, 0, kDrainPolls, g.status);
+      }
+      __syncwarp();
     }
   } else {
     // its lanes of tensor memory, and the first of its pieces of 32 columns: 64 columns of a

@@ -135,6 +135,14 @@ __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// One lane of a converged warp.  The other lanes run the same loop around what it issues, so that its
+// operands are the warp's and lie in uniform registers, where these instructions want them.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t mine;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(mine));
+  return mine != 0;
+}
+
 // 32-byte store (address 32-byte aligned).
 __device__ __forceinline__ void st_v8(void* p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
