@@ -15,10 +15,9 @@
 // Dropout's factor stays out of dz: it scales the fp32 sums of dx, dw and db, so a dz without an
 // activation is dy's own bits.
 //
-// What bounds it: the products.  Measured on one GB300: 8192^3 in bf16 588 us (1.87 PFLOP/s;
-// cuBLAS 545), 4096^3 in fp32 454 us (six plane products, 1.82 PFLOP/s); training 8192 x 4096 x
-// 1024 with dropout and residual 170 us, 16384 x 4096 x 16384 with gelu_tanh 4.46 ms (1.48
-// PFLOP/s of its 6 M N K operations, the two passes over z and dz in between).
+// What bounds it: the products.  Measured on one GB300: 8192^3 in bf16 558 us (1.97 PFLOP/s;
+// cuBLAS 546), 4096^3 in fp32 454 us (six plane products, 1.82 PFLOP/s); training 8192 x 4096 x
+// 1024 with dropout and residual 150 us, 1000 x 777 x 2051 in fp32 with gelu 96.
 #include <algorithm>
 
 #include "launch_util.h"

@@ -17,20 +17,24 @@ namespace {
 //
 // Warp 0 copies operand tiles through tensor maps, six stages of 32 KB a CTA, each of one
 // plane (fp32's three planes of a K block serve six plane products and are given back
-// one by one: 4096^3 took 566 us with two stages of three planes, 454 so).  One thread of the first
-// CTA's warp 1 issues the products of both CTAs; sixteen warps a CTA take the finished tile from
+// one by one: 4096^3 took 566 us with two stages of three planes, 454 so).  One lane of the first
+// CTA's warp 1 issues the products of both CTAs.  What these two warps do for a K block has to take less
+// than the products' 512 cycles, and they wait for every instruction: so all lanes run their loops,
+// which keeps the operands of copies and products in uniform registers, and one of them issues
+// (8192^3 in bf16 593 us with one lane in the loops, 558 so).  Sixteen warps a CTA take the finished tile from
 // tensor memory, 32 rows by twice 32 columns each.  Tensor memory holds two accumulators: a
 // tile's epilogue runs under the next one's products, and should take no longer than those
-// (512 cycles a K block; 590 to 640 are reached).
+// (512 cycles a K block; 560 to 590 are reached).
 //
 // What an epilogue takes is latency.  The matrix units and the copies leave little of shared
 // memory's bandwidth, so results go from registers to global memory, 64 bytes a lane, and four
 // warps a scheduler hide the exponentials of one another; its arrival for the accumulator is a
 // relaxed one (a release waits for the stores: 2000 cycles a tile).  Cycles a 256 x 256 tile: 3700
 // for z alone, 8000 with gelu_tanh, 8800 with dropout.  Measured in bf16 (one GB300, boxes differ
-// by 3 %): 8192 x 1024 x 4096 48 us, with gelu_tanh 58, with dropout and residual 79 (cuBLAS
-// without any of it 37); 8192^3 588 us (545); 2000 x 4096 x 8192 91 to 97 (73), whose 256 tiles
-// are 3.4 waves of the 76 pairs.
+// by 3 %): 8192 x 1024 x 4096 44 us, with gelu_tanh and bias 58 to 65 (cuBLAS without any of it 37);
+// 8192^3 558 us (546); 2000 x 4096 x 8192 81 to 87 (72), whose 256 tiles are 3.4 waves of the 76
+// pairs.  Eight stages of 24 KB for tiles of 128 columns were 2 to 3 % slower: their addresses
+// are no constants of the loops.
 //
 // An accumulator truncates as it adds (1.7e-7 of a large value a step of 16 at most), so it
 // sums `chunk` K blocks, and the epilogue adds the chunks in fp32 rounded to nearest: 2
