@@ -9,8 +9,8 @@
 // along K, because whole ones would leave SMs without work, linear_finish_kernel adds the parts and
 // does it there.  A few rows go another way (linear_few.cu).
 //
-// Rounded to fewer bits in bf16: z as it is kept for the backward pass (2^-9 of it, which
-// moves act' by less than half as much), and dz for the two products (an error of the size of
+// Rounded to fewer bits in bf16: z as it is kept for the backward pass (up to 2^-8 of it, which
+// moves act' by 0.8 of that at most), and dz for the two products (an error of the size of
 // the result's own rounding: dx and dw are 2.4e-3 off 64 bits, where one rounding makes 1.7e-3).
 // Dropout's factor stays out of dz: it scales the fp32 sums of dx, dw and db, so a dz without an
 // activation is dy's own bits.
@@ -199,6 +199,12 @@ __device__ __forceinline__ void sum_bias(unsigned block, const Bias<E>& b) {
   }
 }
 
+// Four entries that start at a multiple of four of a row on 16 bytes.
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&v)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+}
+
 // The tiles that were formed in parts of K, four columns a thread, and what the epilogue would have
 // done.
 struct Finish {
@@ -227,13 +233,19 @@ __device__ __forceinline__ void finish_tiles(unsigned block, const Finish& f) {
       s = make_float4(fadd(s.x, a.x), fadd(s.y, a.y), fadd(s.z, a.z), fadd(s.w, a.w));
     }
     float v[4] = {s.x, s.y, s.z, s.w};
-    if (FORWARD) {
-      if (g.bias != nullptr) add_bias<E, 4>(static_cast<const E*>(g.bias) + n, false, left, v);
-      if (g.z != nullptr) {
+    auto store = [&](void* base, int64_t ld) {
+      E* p = static_cast<E*>(base) + m * ld + n;
+      if (g.wide != 0 && left == 4) {
+        store4(p, v);
+      } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (j < left) put(static_cast<E*>(g.z) + m * g.ldz + n + j, v[j]);
+          if (j < left) put(p + j, v[j]);
       }
+    };
+    if (FORWARD) {
+      if (g.bias != nullptr) add_bias<E, 4>(static_cast<const E*>(g.bias) + n, false, left, v);
+      if (g.z != nullptr) store(g.z, g.ldz);
       apply_act<4, sizeof(E) == 2>(g.act, v);
       if (g.drop.level > 0) apply_drop<4>(g.drop, seed, static_cast<uint64_t>(m) * g.n + n, v);
       if (g.residual != nullptr) {
@@ -245,9 +257,7 @@ __device__ __forceinline__ void finish_tiles(unsigned block, const Finish& f) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = fmul(v[j], g.drop.scale);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < left) put(static_cast<E*>(g.y) + m * g.ldy + n + j, v[j]);
+    store(g.y, g.ldy);
   }
 }
 
