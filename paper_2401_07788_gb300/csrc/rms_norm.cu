@@ -11,6 +11,11 @@
 // row; so codes come from u's extremes, in the same reduction as the sum of squares,
 // and rstd goes to scale and minimum.  Codes then depend on no rounding of rstd.
 //
+// Rounded to fewer bits in bf16: h, which the gradient reads as the forward pass left it (the residual
+// stream, kept anyway).  This loses precision against a gradient from the fp32 sum x + r: dw of
+// 16384 x 4096 is 2.2e-3 to 2.3e-3 off 64 bits, with its own rounding alone 1.5e-3 to 1.6e-3.  An h in fp32
+// would be written and read at twice the bytes; the sum made again would read x and r for h.
+//
 // What bounds it: HBM where rows are wide and aligned.  16384 x 4096 in bf16 with residual: forward
 // 80 us (6.7 TB/s), gradient 96 us (5.6 TB/s) and 5 us for dw's parts; 8192 x 768 in fp32 to 8 bits
 // 14 us (6.1 TB/s).  Rows on odd addresses are read entry by entry and wait for latency:
