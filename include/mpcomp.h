@@ -466,7 +466,7 @@ mpc_status mpc_rms_norm_forward(const void* x, int64_t ldx, const void* residual
  *   n = h rstd;   dx = dh + rstd (weight dy - n mean(weight dy n));
  *   dweight = sum over rows of dy n.
  * A bf16 h is the rounded sum x + residual, and its rounding (up to 2^-8 of an entry)
- * reaches dx and dweight: dweight is then about 1.4 times as far off as its own
+ * reaches dx and dweight: dweight is then 1.2 to 1.6 times as far off as its own
  * rounding to bf16 alone would leave it.
  *   dy, dh, dx  [rows][row_len] of `type`, rows lddy, lddh, lddx apart; `dh`, the
  *           gradient that reaches h by other ways (along the residual stream), may

@@ -806,7 +806,7 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
                           stream=None):
     """The gradient of mpc_rms_norm_forward from its h and rstd: (dx, dweight).  ``dh`` is the gradient that
     reaches h by other ways; dx is that of x and of residual alike.  ``need_weight`` False leaves dweight out.
-    The rounding of a bf16 h (x + residual) reaches dweight: about 1.4 times its own rounding's error."""
+    The rounding of a bf16 h (x + residual) reaches dweight: 1.2 to 1.6 times its own rounding's error."""
     rows, D, ldh, index = _operand(h, "h")
     lddy = _ld(dy, "dy", rows, D, h, index)
     lddh = 0 if dh is None else _ld(dh, "dh", rows, D, h, index)
