@@ -11,14 +11,23 @@ addition.  A block of a stage that normalises before its layers:
   as an 8-bit payload and read back, in fp32.
 
 Dropout: masks are made from a seed where they are used and never stored.  A module's seed is
-``(seed << 32) + step``, with ``step`` the number of its training calls.  A captured graph repeats the host's
-numbers at every replay, so a module refuses to be captured unless it is given a device counter
-(``step=tensor``, int64, one entry) that the program advances between steps, after the backward pass.
+``(seed << 32) + calls``, with ``calls`` the number of its training calls.  Each of these also draws a number
+from torch's CPU generator (5 us).  Recomputation (``torch.utils.checkpoint``) puts that generator back for the
+pass that it repeats, so a number that a module drew before marks a repeated call, which takes the earlier
+one's mask; so does any other program that puts the generator back.  A call inside a backward pass whose number
+is not known (recomputation that leaves the generator alone, or more than ``remembered`` calls later) is
+refused.
+
+A captured graph repeats the host's numbers at every replay, so a module refuses to be captured unless it is
+given a device counter (``step=tensor``, int64, one entry) that the program advances between steps, after the
+backward pass.
 
 None of the gradients here can be differentiated again: asking for it raises.
 """
 
 from __future__ import annotations
+
+import collections
 
 import torch
 
@@ -169,7 +178,12 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, bits: int | None = Non
 # ---------------------------------------------------------------------------------------
 
 class _Seeded(torch.nn.Module):
-    """The dropout seeds of a module: (seed << 32) + the number of its training calls, or the device counter."""
+    """The dropout seeds of a module: (seed << 32) + the number of its training calls, or the device counter.
+
+    ``_known`` holds the seeds of the last calls by the numbers that they drew from torch's CPU generator
+    (about 200 bytes each)."""
+
+    remembered = 4096
 
     def _seeded(self, p, seed, step):
         if not 0.0 <= p <= 1.0:
@@ -177,6 +191,14 @@ class _Seeded(torch.nn.Module):
         self.p = float(p)
         self.seed = int(torch.randint(1 << 31, ()) if seed is None else seed)
         self.step, self.calls = step, 0
+        self._known = collections.OrderedDict()
+
+    def __getstate__(self):
+        # what only passes in flight need is not copied
+        return self.__dict__ | {"_known": collections.OrderedDict()}
+
+    def __setstate__(self, state):
+        super().__setstate__({"_known": collections.OrderedDict()} | state)
 
     def _draw(self, device):
         """(p, seed, step) of one call."""
@@ -185,8 +207,17 @@ class _Seeded(torch.nn.Module):
         if self.step is None:
             if device.type == "cuda" and torch.cuda.is_current_stream_capturing():
                 raise MpcError(1, "a captured dropout needs a device counter: every replay would repeat its mask")
-            self.calls += 1
-            return self.p, (self.seed << 32) + self.calls, None
+            drawn = int(torch.randint(1 << 62, (), device="cpu"))
+            seed = self._known.get(drawn)
+            if seed is None:
+                if torch._C._current_graph_task_id() != -1:  # in a backward pass
+                    raise MpcError(1, "a dropout that is recomputed needs torch's CPU generator as it was at the first "
+                                      "call (preserve_rng_state), and no more than %d other calls since" % self.remembered)
+                self.calls += 1
+                seed = self._known[drawn] = (self.seed << 32) + self.calls
+                if len(self._known) > self.remembered:
+                    self._known.popitem(last=False)
+            return self.p, seed, None
         return self.p, self.seed << 32, self.step
 
 

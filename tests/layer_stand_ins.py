@@ -1,0 +1,37 @@
+"""The calls that the stage's layers make, in plain torch on the CPU: what a function or a module does around them
+(seeds, saved tensors, which calls it makes) is tested without a GPU."""
+
+import torch
+
+import layer_forms as forms
+
+
+def _mask(seed, step, p, shape):
+    if not p:
+        return None
+    seed = seed + (0 if step is None else int(step))
+    n = shape[0] * shape[1] if len(shape) == 2 else torch.Size(shape).numel()
+    return forms.kept(seed, n, p).view(shape)
+
+
+def linear_forward(x, w, bias=None, residual=None, act=None, p=0.0, seed=0, step=None, keep=False):
+    with torch.no_grad():
+        y, z = forms.linear(x, w, bias, residual, act, _mask(seed, step, p, (x.shape[0], w.shape[0])))
+    return y.to(x.dtype), z.to(x.dtype) if keep else None
+
+
+def linear_backward(dy, x, w, z=None, act=None, p=0.0, seed=0, step=None, need=(True, True, True), dx=None):
+    with torch.enable_grad():
+        grads = forms.linear_grads(dy, x, w, z, act, _mask(seed, step, p, dy.shape))[:3]
+    return tuple(g.to(x.dtype) if wanted else None for g, wanted in zip(grads, need))
+
+
+def dropout(x, p, seed=0, residual=None, step=None):
+    with torch.no_grad():
+        y = x if not p else x * _mask(seed, step, p, x.shape).to(x.dtype)
+        return y.clone() if residual is None else y + residual
+
+
+def install(monkeypatch, layers):
+    for name, call in (("mpc_linear_forward", linear_forward), ("mpc_linear_backward", linear_backward), ("mpc_dropout", dropout)):
+        monkeypatch.setattr(layers, name, call)
