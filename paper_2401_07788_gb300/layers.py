@@ -22,7 +22,8 @@ A captured graph repeats the host's numbers at every replay, so a module refuses
 given a device counter (``step=tensor``, int64, one entry) that the program advances between steps, after the
 backward pass.
 
-None of the gradients here can be differentiated again: asking for it raises.
+None of the gradients here can be differentiated again, and there are no forward-mode derivatives: asking for
+either raises.
 """
 
 from __future__ import annotations
@@ -30,6 +31,7 @@ from __future__ import annotations
 import collections
 
 import torch
+from torch.autograd import forward_ad
 
 from . import (MpcError, mpc_dropout, mpc_linear_backward, mpc_linear_forward, mpc_quant_decompress,
                mpc_rms_norm_backward, mpc_rms_norm_forward, mpc_rms_norm_quant)
@@ -56,6 +58,14 @@ def _final(grads, *sources):
         return tuple(grads)
     sources = [s for s in sources if s is not None]
     return tuple(None if g is None else _Final.apply(g, *sources) for g in grads)
+
+
+def _differentiated(*operands) -> bool:
+    """Whether a call has to go through its autograd function: one of its operands takes a gradient, or has a tangent
+    (the functions refuse forward mode; the plain call would lose the tangent)."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in operands):
+        return True
+    return forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in operands)
 
 
 def _rows(t):
@@ -98,7 +108,7 @@ def linear(x, w, bias=None, residual=None, act: str | None = None, p: float = 0.
             raise MpcError(1, "residual must have the shape %s" % (tuple(shape),))
         residual = _rows(residual)
     rows, w, bias = _rows(x), _rows(w), _whole(bias)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (rows, w, bias, residual)):
+    if _differentiated(rows, w, bias, residual):
         y = _LinearFn.apply(rows, w, bias, residual, act, p, seed, step)
     else:
         y, _ = mpc_linear_forward(rows, w, bias, residual, act=act, p=p, seed=seed, step=step)
@@ -128,7 +138,7 @@ def dropout(x, p: float, seed: int = 0, residual=None, step=None):
     x, residual = x.contiguous(), _whole(residual)
     if residual is not None and residual.shape != x.shape:
         raise MpcError(1, "residual must have the shape %s" % (tuple(x.shape),))
-    if torch.is_grad_enabled() and (x.requires_grad or (residual is not None and residual.requires_grad)):
+    if _differentiated(x, residual):
         return _DropoutFn.apply(x, residual, p, seed, step)
     return mpc_dropout(x, p, seed, residual=residual, step=step)
 
