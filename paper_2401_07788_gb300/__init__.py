@@ -18,6 +18,7 @@ import operator
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 from ._build import LIB_PATH
 
@@ -164,6 +165,14 @@ def _launch(call, device, stream, *args) -> None:
     else:
         with torch.cuda.device(device):
             _check(call(*args, raw))
+
+
+def _differentiated(*operands) -> bool:
+    """Whether a call has to go through its autograd function: one of its operands takes a gradient, or has a tangent
+    (the functions refuse forward mode; a plain call would lose the tangent)."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in operands):
+        return True
+    return forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in operands)
 
 
 def _cuda(t: torch.Tensor, dtype: torch.dtype, name: str) -> torch.Tensor:

@@ -31,10 +31,9 @@ from __future__ import annotations
 import collections
 
 import torch
-from torch.autograd import forward_ad
 
-from . import (MpcError, mpc_dropout, mpc_linear_backward, mpc_linear_forward, mpc_quant_decompress,
-               mpc_rms_norm_backward, mpc_rms_norm_forward, mpc_rms_norm_quant)
+from . import (MpcError, _differentiated, mpc_dropout, mpc_linear_backward, mpc_linear_forward,
+               mpc_quant_decompress, mpc_rms_norm_backward, mpc_rms_norm_forward, mpc_rms_norm_quant)
 
 __all__ = ["Dropout", "Linear", "RMSNorm", "dropout", "linear", "rms_norm"]
 
@@ -58,14 +57,6 @@ def _final(grads, *sources):
         return tuple(grads)
     sources = [s for s in sources if s is not None]
     return tuple(None if g is None else _Final.apply(g, *sources) for g in grads)
-
-
-def _differentiated(*operands) -> bool:
-    """Whether a call has to go through its autograd function: one of its operands takes a gradient, or has a tangent
-    (the functions refuse forward mode; the plain call would lose the tangent)."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in operands):
-        return True
-    return forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in operands)
 
 
 def _rows(t):

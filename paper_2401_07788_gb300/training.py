@@ -19,7 +19,7 @@ import operator
 import numpy as np
 import torch
 
-from . import (MpcError, _data_ptr, _dtype, _numel, _vectors, mpc_adamw_step, mpc_grad_norm,
+from . import (MpcError, _data_ptr, _differentiated, _dtype, _numel, _vectors, mpc_adamw_step, mpc_grad_norm,
                mpc_linear_ce_backward, mpc_linear_ce_forward, mpc_linear_ce_train)
 
 __all__ = ["AdamW", "AdamWPlan", "LinearCrossEntropy", "linear_cross_entropy"]
@@ -119,7 +119,7 @@ def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str
     """Softmax cross entropy of the logits h @ w.T, h [..., D], w [V, D], targets [...] (int64).
     ``reduction``: "mean" over the tokens that count, "sum", or "none" (a loss for each token, 0
     where the target is ``ignore_index``).  A target outside [0, V) does not count either, and is reported
-    by ``mpc_get_status``.  There is no second derivative: asking for one raises.
+    by ``mpc_get_status``.  There is no second derivative and no forward-mode one: asking for them raises.
 
     The loss by itself keeps no logits.  The gradient of a mean does for the length of its call, as
     exponentials (2 bytes each in bf16, 6 in fp32, 4 GiB at most), and then forms them once.
@@ -130,7 +130,7 @@ def linear_cross_entropy(h, w, targets, ignore_index: int = -100, reduction: str
         raise ValueError("reduction must be mean, sum or none")
     rows, y = _rows_apart(h.reshape(-1, h.shape[-1])), targets.reshape(-1).contiguous()
     w = _rows_apart(w)
-    grad = torch.is_grad_enabled() and (h.requires_grad or w.requires_grad)
+    grad = _differentiated(h, w)
     if reduction == "mean":
         if grad:
             return _LinearCeMeanFn.apply(rows, w, y, ignore_index, piece)
