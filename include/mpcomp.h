@@ -490,7 +490,9 @@ mpc_status mpc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
  * round to nearest), bit for bit, and
  *   scale = scale(u) rstd,   minv = min(u) rstd
  * (a row's rstd scales its range and its values alike, so the codes do not depend on
- * it).  codes [rows][W], W = mpc_quant_codes_words(1, row_len, 8), 16-byte aligned.
+ * it).  A row with a NaN in u has the scale and minimum NaN, so all of it is read back as
+ * NaN, and its codes are not specified.
+ *   codes [rows][W], W = mpc_quant_codes_words(1, row_len, 8), 16-byte aligned.
  * The other arguments are those of mpc_rms_norm_forward. */
 mpc_status mpc_rms_norm_quant(const void* x, int64_t ldx, const void* residual, int64_t ldr,
                               const void* weight, int64_t rows, int64_t row_len, mpc_dtype type,

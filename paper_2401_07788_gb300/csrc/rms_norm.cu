@@ -87,14 +87,28 @@ __device__ __forceinline__ void store_row(T* p, int t, int D, const float (&v)[k
   }
 }
 
+// Extremes that a NaN takes over: a row with a NaN in u then has the scale and minimum NaN, as the
+// quantiser's, whose keys order NaN beyond infinity (fminf and fmaxf would drop it, and the receiver read
+// a finite value).
+__device__ __forceinline__ float least(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float most(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 struct Stats {
   float sum, lo, hi;
 };
 __device__ __forceinline__ Stats merge(const Stats& a, const Stats& b, bool extremes) {
   Stats r = {fadd(a.sum, b.sum), a.lo, a.hi};
   if (extremes) {
-    r.lo = fminf(a.lo, b.lo);
-    r.hi = fmaxf(a.hi, b.hi);
+    r.lo = least(a.lo, b.lo);
+    r.hi = most(a.hi, b.hi);
   }
   return r;
 }
@@ -127,7 +141,7 @@ __device__ __forceinline__ Stats reduce_row(Stats s, bool extremes, Stats* share
 }
 
 // scale and code step of a row of u, as the quantiser's (quant.cu): a range that is 0 or
-// infinite, or whose inverse is, sends codes 0 and scale 0.
+// infinite, or whose inverse is, sends codes 0 and scale 0; one that is NaN the scale NaN.
 struct Code {
   float lo, inv, scale;
 };
@@ -178,8 +192,8 @@ __global__ void __launch_bounds__(NT < kBlock ? kBlock : NT) rms_row_kernel(cons
     for (int j = 0; j < kEach; ++j) {
       const float u = fmul(h[j], w[j]);
       if (column<T, NT, WIDE>(t, j) < D) {
-        s.lo = fminf(s.lo, u);
-        s.hi = fmaxf(s.hi, u);
+        s.lo = least(s.lo, u);
+        s.hi = most(s.hi, u);
       }
     }
   }
@@ -236,8 +250,8 @@ __global__ void __launch_bounds__(kLongBlock) rms_long_kernel(const RmsNormArgs 
     s.sum = __fmaf_rn(h, h, s.sum);
     if (CODES) {
       const float u = fmul(h, as_float(w[i]));
-      s.lo = fminf(s.lo, u);
-      s.hi = fmaxf(s.hi, u);
+      s.lo = least(s.lo, u);
+      s.hi = most(s.hi, u);
     }
   }
   s = reduce_row<kLongBlock>(s, CODES, shared);
