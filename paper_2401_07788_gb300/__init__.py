@@ -6,7 +6,9 @@ Each ``mpc_*`` function here has the name of the C entry point it calls (declare
 ``include/mpcomp.h``) and only marshals arguments: it checks that tensors are contiguous
 CUDA tensors of the right dtype, allocates outputs and workspaces with PyTorch when the
 caller does not pass them, and passes raw device pointers and the current CUDA stream to
-the library.  Every operator runs in the library's kernels; there is no fallback.  If
+the library.  With ``stream=`` a call runs on that stream, and what it allocates is that stream's: the
+caller orders the stream behind what makes the inputs, and what uses the outputs behind the
+stream.  Every operator runs in the library's kernels; there is no fallback.  If
 ``libmpcomp.so`` has not been built, the first call raises ``MpcError``.
 """
 
@@ -192,11 +194,24 @@ def _rows_cols(x: torch.Tensor) -> tuple[int, int]:
     return (x.numel() // L if L else 0), L
 
 
-def _workspace(nbytes: int, ws, device) -> tuple:
+def _new(shape, dtype: torch.dtype, device, stream, out: bool = True) -> torch.Tensor:
+    """Memory that a call makes for itself.  On a stream of the caller's choice it is that stream's memory: a block of the
+    current stream's may still be read or written by work that is queued there, which the other stream does
+    not wait for.  An output is noted as the current stream's too, so that freeing it waits for its uses there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if out:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(nbytes: int, ws, device, stream) -> tuple:
     if nbytes == 0:
         return ws, (0 if ws is None else ws.numel() * ws.element_size())
     if ws is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        ws = _new(nbytes, torch.uint8, device, stream, out=False)
     return ws, ws.numel() * ws.element_size()
 
 
@@ -208,12 +223,12 @@ def mpc_topk_workspace_bytes(rows: int, row_len: int, k: int) -> int:
     return int(lib().mpc_topk_workspace_bytes(rows, row_len, k))
 
 
-def _topk_outputs(x, k, vals, idx):
+def _topk_outputs(x, k, vals, idx, stream):
     R, L = _rows_cols(x)
     if vals is None:
-        vals = torch.empty((R, k), dtype=torch.float32, device=x.device)
+        vals = _new((R, k), torch.float32, x.device, stream)
     if idx is None:
-        idx = torch.empty((R, k), dtype=torch.int32, device=x.device)
+        idx = _new((R, k), torch.int32, x.device, stream)
     _cuda(vals, torch.float32, "vals")
     _cuda(idx, torch.int32, "idx")
     if vals.numel() != R * k or idx.numel() != R * k:
@@ -224,8 +239,8 @@ def _topk_outputs(x, k, vals, idx):
 def mpc_topk_compress(x, k: int, vals=None, idx=None, ws=None, stream=None):
     """TopK per row of x (last dimension = row).  Returns (vals [R,k], idx [R,k])."""
     _cuda(x, torch.float32, "x")
-    R, L, vals, idx = _topk_outputs(x, k, vals, idx)
-    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device)
+    R, L, vals, idx = _topk_outputs(x, k, vals, idx, stream)
+    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device, stream)
     _check(lib().mpc_topk_compress(_ptr(x), R, L, k, _ptr(vals), _ptr(idx), _ptr(ws), wsb,
                                    _stream(stream)))
     return vals, idx
@@ -237,8 +252,8 @@ def mpc_ef_topk_compress(x, err, k: int, vals=None, idx=None, ws=None, stream=No
     _cuda(err, torch.float32, "err")
     if err.shape != x.shape:
         raise MpcError(1, "err must have the shape of x")
-    R, L, vals, idx = _topk_outputs(x, k, vals, idx)
-    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device)
+    R, L, vals, idx = _topk_outputs(x, k, vals, idx, stream)
+    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device, stream)
     _check(lib().mpc_ef_topk_compress(_ptr(x), _ptr(err), R, L, k, _ptr(vals), _ptr(idx),
                                       _ptr(ws), wsb, _stream(stream)))
     return vals, idx
@@ -254,8 +269,8 @@ def mpc_efmix_topk_compress(x, err, k: int, vals=None, idx=None, ws=None, stream
     _cuda(err, torch.float32, "err")
     if err.shape != x.shape:
         raise MpcError(1, "err must have the shape of x")
-    R, L, vals, idx = _topk_outputs(x, k, vals, idx)
-    ws, wsb = _workspace(mpc_efmix_workspace_bytes(R, L, k) if R else 0, ws, x.device)
+    R, L, vals, idx = _topk_outputs(x, k, vals, idx, stream)
+    ws, wsb = _workspace(mpc_efmix_workspace_bytes(R, L, k) if R else 0, ws, x.device, stream)
     _check(lib().mpc_efmix_topk_compress(_ptr(x), _ptr(err), R, L, k, _ptr(vals), _ptr(idx),
                                          _ptr(ws), wsb, _stream(stream)))
     return vals, idx
@@ -267,8 +282,8 @@ def mpc_ef21_topk_compress(x, g, k: int, vals=None, idx=None, ws=None, stream=No
     _cuda(g, torch.float32, "g")
     if g.shape != x.shape:
         raise MpcError(1, "g must have the shape of x")
-    R, L, vals, idx = _topk_outputs(x, k, vals, idx)
-    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device)
+    R, L, vals, idx = _topk_outputs(x, k, vals, idx, stream)
+    ws, wsb = _workspace(mpc_topk_workspace_bytes(R, L, k) if R else 0, ws, x.device, stream)
     _check(lib().mpc_ef21_topk_compress(_ptr(x), _ptr(g), R, L, k, _ptr(vals), _ptr(idx),
                                         _ptr(ws), wsb, _stream(stream)))
     return vals, idx
@@ -280,7 +295,7 @@ def mpc_topk_decompress(vals, idx, row_len: int, y=None, stream=None):
     _cuda(idx, torch.int32, "idx")
     R, k = _rows_cols(vals)
     if y is None:
-        y = torch.empty((R, row_len), dtype=torch.float32, device=vals.device)
+        y = _new((R, row_len), torch.float32, vals.device, stream)
     _cuda(y, torch.float32, "y")
     _check(lib().mpc_topk_decompress(_ptr(vals), _ptr(idx), R, row_len, k, _ptr(y),
                                      _stream(stream)))
@@ -296,7 +311,7 @@ def mpc_topk_gather(g, idx, vals=None, stream=None):
     if Ri != R:
         raise MpcError(1, "idx must have one row per row of g")
     if vals is None:
-        vals = torch.empty((R, k), dtype=torch.float32, device=g.device)
+        vals = _new((R, k), torch.float32, g.device, stream)
     _cuda(vals, torch.float32, "vals")
     _check(lib().mpc_topk_gather(_ptr(g), R, L, _ptr(idx), k, _ptr(vals), _stream(stream)))
     return vals
@@ -319,9 +334,9 @@ def mpc_aqsgd_compress(x, buf, sample_ids, k: int, vals=None, idx=None, ws=None,
         raise MpcError(1, "x.shape[0] must equal the number of sample ids")
     R = n_ids * rps
     if vals is None:
-        vals = torch.empty((R, k), dtype=torch.float32, device=x.device)
+        vals = _new((R, k), torch.float32, x.device, stream)
     if idx is None:
-        idx = torch.empty((R, k), dtype=torch.int32, device=x.device)
+        idx = _new((R, k), torch.int32, x.device, stream)
     _cuda(vals, torch.float32, "vals")
     _cuda(idx, torch.int32, "idx")
     _check(lib().mpc_aqsgd_compress(_ptr(x), _ptr(buf), S, _ptr(sample_ids), n_ids, rps, L, k,
@@ -366,15 +381,15 @@ def mpc_quant_compress(x, bits: int, stochastic: bool = False, seed: int = 0, co
         raise MpcError(1, "bits=%d is not supported" % bits)
     W = words // R if R else 0
     if codes is None:
-        codes = torch.empty((R, W), dtype=torch.int32, device=x.device)
+        codes = _new((R, W), torch.int32, x.device, stream)
     if scale is None:
-        scale = torch.empty(R, dtype=torch.float32, device=x.device)
+        scale = _new(R, torch.float32, x.device, stream)
     if minv is None:
-        minv = torch.empty(R, dtype=torch.float32, device=x.device)
+        minv = _new(R, torch.float32, x.device, stream)
     _cuda(codes, torch.int32, "codes")
     _cuda(scale, torch.float32, "scale")
     _cuda(minv, torch.float32, "minv")
-    ws, wsb = _workspace(mpc_quant_workspace_bytes(R, L, bits) if R else 0, ws, x.device)
+    ws, wsb = _workspace(mpc_quant_workspace_bytes(R, L, bits) if R else 0, ws, x.device, stream)
     _check(lib().mpc_quant_compress(_ptr(x), R, L, bits, 1 if stochastic else 0,
                                     seed & 0xFFFFFFFFFFFFFFFF, _ptr(codes), _ptr(scale),
                                     _ptr(minv), _ptr(ws), wsb, _stream(stream)))
@@ -387,7 +402,7 @@ def mpc_quant_decompress(codes, scale, minv, row_len: int, bits: int, y=None, st
     _cuda(minv, torch.float32, "minv")
     R = scale.numel()
     if y is None:
-        y = torch.empty((R, row_len), dtype=torch.float32, device=scale.device)
+        y = _new((R, row_len), torch.float32, scale.device, stream)
     _cuda(y, torch.float32, "y")
     _check(lib().mpc_quant_decompress(codes.data_ptr(), scale.data_ptr(), minv.data_ptr(), R, row_len, bits,
                                       y.data_ptr(), _stream(stream)))
@@ -425,16 +440,16 @@ def mpc_aqsgd_quant_compress(x, buf, sample_ids, bits: int, stochastic: bool = F
         raise MpcError(1, "bits=%d is not supported" % bits)
     W = words // R if R else 0
     if codes is None:
-        codes = torch.empty((R, W), dtype=torch.int32, device=x.device)
+        codes = _new((R, W), torch.int32, x.device, stream)
     if scale is None:
-        scale = torch.empty(R, dtype=torch.float32, device=x.device)
+        scale = _new(R, torch.float32, x.device, stream)
     if minv is None:
-        minv = torch.empty(R, dtype=torch.float32, device=x.device)
+        minv = _new(R, torch.float32, x.device, stream)
     _cuda(codes, torch.int32, "codes")
     _cuda(scale, torch.float32, "scale")
     _cuda(minv, torch.float32, "minv")
     need = mpc_aqsgd_quant_workspace_bytes(n_ids, rps, L, bits) if R else 0
-    ws, wsb = _workspace(need, ws, x.device)
+    ws, wsb = _workspace(need, ws, x.device, stream)
     _check(lib().mpc_aqsgd_quant_compress(_ptr(x), _ptr(buf), S, _ptr(sample_ids), n_ids, rps,
                                           L, bits, 1 if stochastic else 0,
                                           seed & 0xFFFFFFFFFFFFFFFF, _ptr(codes), _ptr(scale),
@@ -492,14 +507,6 @@ def _address(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-def _on(stream, *tensors):
-    """Tells the allocator that a call on `stream` uses what was allocated for it here."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-
-
 def _vector(t, n: int, dtype: torch.dtype, name: str, device):
     _cuda(t, dtype, name)
     if t.numel() != n or t.device != device:
@@ -532,9 +539,7 @@ def _vector_or_new(t, n: int, name: str, device, stream):
     """An fp32 output of n entries: the caller's, checked, or a new one."""
     if t is not None:
         return _vector(t, n, torch.float32, name, device)
-    t = torch.empty(n, dtype=torch.float32, device=device)
-    _on(stream, t)
-    return t
+    return torch.empty(n, dtype=torch.float32, device=device) if stream is None else _new(n, torch.float32, device, stream)
 
 
 def mpc_linear_ce_workspace_bytes(tokens: int, hidden: int, vocab: int, dtype=torch.float32,
@@ -555,10 +560,7 @@ def _linear_ce_args(h, w, targets, grad, piece, ws, stream):
     _vector(targets, T, torch.int64, "targets", h.device)
     need = mpc_linear_ce_workspace_bytes(T, D, V, h.dtype, grad, piece,
                                          0 if w.data_ptr() % 16 else ldw)
-    given = ws
-    ws, wsb = _workspace(need, ws, h.device)
-    if given is None:
-        _on(stream, ws)
+    ws, wsb = _workspace(need, ws, h.device, stream)
     return T, D, V, ldh, ldw, ws, wsb
 
 
@@ -578,8 +580,7 @@ def _linear_ce_grads(h, w, dh, dw, stream):
     out = []
     for name, t, of in (("dh", dh, h), ("dw", dw, w)):
         if t is None:
-            t = torch.empty(of.shape, dtype=of.dtype, device=of.device)
-            _on(stream, t)
+            t = _new(of.shape, of.dtype, of.device, stream)
             out += [t, of.shape[1]]
         else:
             if t.shape != of.shape:
@@ -657,10 +658,10 @@ def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
     norm = _vector_or_new(norm, 1, "norm", plan.device, stream)
     if ws is None:
         if plan.norm_ws is None:
-            plan.norm_ws = torch.empty(mpc_grad_norm_workspace_bytes(plan.count), dtype=torch.uint8,
-                                       device=plan.device)
+            plan.norm_ws = _new(mpc_grad_norm_workspace_bytes(plan.count), torch.uint8, plan.device, stream)
         ws = plan.norm_ws
-        _on(stream, ws)
+        if stream is not None:
+            ws.record_stream(stream)
     wsb = ws.numel() * ws.element_size()
     _launch(lib().mpc_grad_norm, plan.device, stream, plan.table, plan.count, plan.grad_type, norm.data_ptr(),
             _address(ws), wsb)
@@ -718,10 +719,9 @@ def _operand(x, name: str):
 def _like(t, rows: int, cols: int, of, name: str, index: int, stream):
     """An output matrix of the type and device of `of`: the caller's, checked, or a new one; its row distance."""
     if t is None:
-        t = torch.empty((rows, cols), dtype=of.dtype, device=of.device)
-        if stream is not None:
-            t.record_stream(stream)
-        return t, cols
+        if stream is None:
+            return torch.empty((rows, cols), dtype=of.dtype, device=of.device), cols
+        return _new((rows, cols), of.dtype, of.device, stream), cols
     return t, _ld(t, name, rows, cols, of, index)
 
 
@@ -754,9 +754,7 @@ def mpc_dropout(x, p: float, seed: int = 0, residual=None, step=None, y=None, st
             _cuda(t, x.dtype, name)
             raise MpcError(1, "%s must have the shape and device of x" % name)
     if y is None:
-        y = torch.empty_like(x)
-        if stream is not None:
-            y.record_stream(stream)
+        y = torch.empty_like(x) if stream is None else _new(x.shape, x.dtype, x.device, stream)
     _call(lib().mpc_dropout, x, index, stream, x.data_ptr(), None if residual is None else residual.data_ptr(), x.numel(),
           kind, p, seed & _SEEDS, None if step is None else _step(step, x.device), y.data_ptr())
     return y
@@ -795,8 +793,7 @@ def mpc_rms_norm_quant(x, weight, eps: float = 1e-6, residual=None, codes=None, 
     r, ldr, h, hp, ldh = _summed(x, rows, D, index, residual, h, stream)
     W = (D + 15) // 16 * 4
     if codes is None:
-        codes = torch.empty((rows, W), dtype=torch.int32, device=x.device)
-        _on(stream, codes)
+        codes = _new((rows, W), torch.int32, x.device, stream)
     else:
         _vector(codes, rows * W, torch.int32, "codes", x.device)
     scale = _vector_or_new(scale, rows, "scale", x.device, stream)
@@ -825,12 +822,8 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
     if dweight is not None:
         _vector_like(dweight, D, h, "dweight", index)
     elif need_weight:
-        dweight = torch.empty(D, dtype=h.dtype, device=h.device)
-        _on(stream, dweight)
-    given = ws
-    ws, wsb = _workspace(mpc_rms_norm_workspace_bytes(rows, D), ws, h.device)
-    if given is None:
-        _on(stream, ws)
+        dweight = _new(D, h.dtype, h.device, stream)
+    ws, wsb = _workspace(mpc_rms_norm_workspace_bytes(rows, D), ws, h.device, stream)
     _call(lib().mpc_rms_norm_backward, h, index, stream, dy.data_ptr(), lddy, h.data_ptr(), ldh, w, rstd.data_ptr(),
           _address(dh), lddh, rows, D, _DTYPES[h.dtype], dx.data_ptr(), lddx, _address(dweight), _address(ws), wsb)
     return dx, dweight
@@ -852,9 +845,8 @@ def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, of, str
                                                 0 if dy & 15 else lddy)
         if need == 0:
             return None, None, 0
-        ws = torch.empty(need, dtype=torch.uint8, device=of.device)
-        if stream is not None:
-            ws.record_stream(stream)
+        ws = torch.empty(need, dtype=torch.uint8, device=of.device) if stream is None else \
+            _new(need, torch.uint8, of.device, stream, out=False)
         return ws, ws.data_ptr(), need
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
@@ -910,8 +902,7 @@ def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0
     if db is not None:
         _vector_like(db, N, x, "db", index)
     elif need[2]:
-        db = torch.empty(N, dtype=x.dtype, device=x.device)
-        _on(stream, db)
+        db = _new(N, x.dtype, x.device, stream)
     xp, wp, dyp = x.data_ptr(), w.data_ptr(), dy.data_ptr()
     ws, wsp, wsb = _linear_ws(rows, K, N, kind, 1, xp, ldx, wp, ldw, dyp, lddy, ws, x, stream)
     _call(lib().mpc_linear_backward, x, index, stream, dyp, lddy, xp, ldx, wp, ldw, zp, ldz, rows, K, N, kind, code, p,
