@@ -208,11 +208,18 @@ def _new(shape, dtype: torch.dtype, device, stream, out: bool = True) -> torch.T
 
 
 def _workspace(nbytes: int, ws, device, stream) -> tuple:
+    if ws is not None:
+        return ws, _given(ws, device)
     if nbytes == 0:
-        return ws, (0 if ws is None else ws.numel() * ws.element_size())
-    if ws is None:
-        ws = _new(nbytes, torch.uint8, device, stream, out=False)
-    return ws, ws.numel() * ws.element_size()
+        return None, 0
+    return _new(nbytes, torch.uint8, device, stream, out=False), nbytes
+
+
+def _given(ws, device) -> int:
+    """The bytes of a workspace of the caller's: its address and size are all that the library sees."""
+    if not isinstance(ws, torch.Tensor) or not ws.is_cuda or ws.device != device or not ws.is_contiguous():
+        raise MpcError(1, "ws must be a contiguous tensor on %s" % device)
+    return ws.numel() * ws.element_size()
 
 
 # ---------------------------------------------------------------------------------------
@@ -339,9 +346,9 @@ def mpc_aqsgd_compress(x, buf, sample_ids, k: int, vals=None, idx=None, ws=None,
         idx = _new((R, k), torch.int32, x.device, stream)
     _cuda(vals, torch.float32, "vals")
     _cuda(idx, torch.int32, "idx")
+    ws, wsb = _workspace(0, ws, x.device, stream)
     _check(lib().mpc_aqsgd_compress(_ptr(x), _ptr(buf), S, _ptr(sample_ids), n_ids, rps, L, k,
-                                    _ptr(vals), _ptr(idx), _ptr(ws), 0 if ws is None else
-                                    ws.numel() * ws.element_size(), _stream(stream)))
+                                    _ptr(vals), _ptr(idx), _ptr(ws), wsb, _stream(stream)))
     return vals, idx
 
 
@@ -662,7 +669,7 @@ def mpc_grad_norm(plan, norm=None, ws=None, stream=None):
         ws = plan.norm_ws
         if stream is not None:
             ws.record_stream(stream)
-    wsb = ws.numel() * ws.element_size()
+    wsb = _given(ws, plan.device)
     _launch(lib().mpc_grad_norm, plan.device, stream, plan.table, plan.count, plan.grad_type, norm.data_ptr(),
             _address(ws), wsb)
     return norm
@@ -848,7 +855,8 @@ def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, of, str
         ws = torch.empty(need, dtype=torch.uint8, device=of.device) if stream is None else \
             _new(need, torch.uint8, of.device, stream, out=False)
         return ws, ws.data_ptr(), need
-    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+    size = _given(ws, of.device)
+    return ws, ws.data_ptr(), size
 
 
 def _linear_args(x, w):
