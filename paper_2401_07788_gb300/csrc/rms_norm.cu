@@ -527,10 +527,10 @@ cudaError_t run_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s) {
   int parts = 0;
   cudaError_t e;
   if (a.D > kBackLongest<T>) {
-    float* dot = static_cast<float*>(a.ws) + static_cast<int64_t>(kParts) * a.D;
+    parts = static_cast<int>(std::min<int64_t>(a.rows, kParts));
+    float* dot = static_cast<float*>(a.ws) + parts * a.D;
     e = launch_kernel(rms_long_dot_kernel<T>, dim3(static_cast<unsigned>(a.rows)), dim3(kLongBlock), 0, s, 0u, a, dot);
     if (e != cudaSuccess) return e;
-    parts = static_cast<int>(std::min<int64_t>(a.rows, kParts));
     e = launch_kernel(rms_long_backward_kernel<T>, dim3(static_cast<unsigned>((a.D + 255) / 256), parts), dim3(256), 0, s, 0u, a,
                       static_cast<const float*>(dot), part);
   } else {
@@ -550,7 +550,7 @@ cudaError_t run_backward(const RmsNormArgs& a, int num_sms, cudaStream_t s) {
 
 size_t rms_norm_workspace_bytes(int64_t rows, int64_t D) {
   const int64_t parts = std::min<int64_t>(rows, kParts);
-  return static_cast<size_t>(D > kBackLongest<float> ? (kParts * D + rows) * 4 : parts * D * 4);  // either type's
+  return static_cast<size_t>(parts * D + (D > kBackLongest<float> ? rows : 0)) * 4;  // either type's
 }
 
 cudaError_t launch_rms_norm(const RmsNormArgs& a, int, cudaStream_t s) {
