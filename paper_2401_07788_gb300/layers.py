@@ -154,8 +154,15 @@ class _RmsNormFn(torch.autograd.Function):
         need = ctx.needs_input_grad
         if dy is None:  # only h was used
             return dh, dh if need[1] else None, None, None, None
-        dx, dw = mpc_rms_norm_backward(_rows(dy.detach().to(h.dtype)), h, weight, rstd,
-                                       dh=None if dh is None else _rows(dh.detach()), need_weight=need[2])
+        more = None if dh is None else _rows(dh.detach())
+        if dy.dtype != h.dtype:
+            # what bf16 rows sent was read back in fp32: its gradient is used as it is, on fp32 copies of the bf16
+            # operands, and the results are rounded once
+            more = None if more is None else more.float()
+            dx, dw = mpc_rms_norm_backward(_rows(dy.detach()), h.float(), weight.float(), rstd, dh=more, need_weight=need[2])
+            dx, dw = dx.to(h.dtype), None if dw is None else dw.to(h.dtype)
+        else:
+            dx, dw = mpc_rms_norm_backward(_rows(dy.detach()), h, weight, rstd, dh=more, need_weight=need[2])
         dx, dw = _final((dx, dw), h, weight, dy, dh)
         return dx if need[0] else None, dx if need[1] else None, dw, None, None
 
