@@ -318,7 +318,8 @@ typedef enum { MPC_CE_FORWARD = 0, MPC_CE_BACKWARD = 1, MPC_CE_TRAIN = 2 } mpc_c
  * Products are summed in fp32 and fp32 inputs are not rounded to a narrower
  * type.  A NaN logit makes its token's loss and lse NaN.  (An fp32 infinity, or a
  * magnitude from 2^128 - 2^119 on, makes the logits that it meets NaN where the
- * matrix units form them.)  tokens = 0 is a no-op.  Requires 1 <= hidden <= 2^24, 1 <= vocab <=
+ * matrix units form them; there an fp32 entry keeps its bits down to 2^-133, so that one
+ * below 2^-110 is rounded, by 2^-134 at most.)  tokens = 0 is a no-op.  Requires 1 <= hidden <= 2^24, 1 <= vocab <=
  * 2^30, tokens <= 2^30. */
 size_t mpc_linear_ce_workspace_bytes(int64_t tokens, int64_t hidden, int64_t vocab, mpc_dtype type,
                                      mpc_ce_pass pass, int64_t piece, int64_t ldw);
@@ -523,8 +524,9 @@ typedef enum { MPC_LINEAR_FORWARD = 0, MPC_LINEAR_BACKWARD = 1 } mpc_linear_pass
  *       bf16 terms.
  * Products are summed in fp32 and fp32 inputs are not rounded to a narrower type;
  * what is added to them is added in fp32 and rounded once.  (An fp32 infinity, or a
- * magnitude from 2^128 - 2^119 on, may make the products that it meets NaN.)  y may be
- * residual, with the same row distance.  rows = 0 is a no-op.  Requires
+ * magnitude from 2^128 - 2^119 on, may make the products that it meets NaN; and an fp32
+ * entry keeps its bits down to 2^-133, so that one below 2^-110 is rounded, by 2^-134 at
+ * most.)  y may be residual, with the same row distance.  rows = 0 is a no-op.  Requires
  * 1 <= in, out <= 2^24, rows <= 2^30. */
 size_t mpc_linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, mpc_dtype type,
                                   mpc_linear_pass pass, int64_t ldx, int64_t ldw, int64_t lddy);

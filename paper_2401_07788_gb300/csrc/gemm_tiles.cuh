@@ -23,7 +23,8 @@ constexpr int kHalf = kN / 2;  // columns an epilogue warp takes
 
 // ---------------------------------------------------------------------------
 // Operands in bf16 planes.  A bf16 tensor is one plane.  An fp32 x is the sum of
-// three, x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1) (24 bits), and a
+// three, x0 = bf16(x), x1 = bf16(x - x0), x2 = bf16(x - x0 - x1) (24 bits, down
+// to bf16's smallest number 2^-133, which entries below 2^-110 reach), and a
 // product of two fp32 tensors the sum of the plane products i + j <= 2, six of
 // them: what is left out is below 2^-24 of a term.  One kernel so serves both
 // types, an fp32 product being a bf16 one with six times the K steps.
