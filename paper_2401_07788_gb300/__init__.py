@@ -893,10 +893,19 @@ def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0
                         need=(True, True, True), dx=None, dw=None, db=None, ws=None, stream=None):
     """The gradient of mpc_linear_forward, with its z where it has an activation and its p, seed and step:
     (dx [R, K], dw [N, K], db [N]); ``need`` says which are formed (the others are None).  The gradient of the
-    residual is dy.  dy, x, w: all three are given, whatever is formed."""
-    rows, K, N, index, ldx, ldw, kind = _linear_args(x, w)
+    residual is dy.  dy and w are given whatever is formed, x for dw."""
     code = _act(act)
-    lddy = _ld(dy, "dy", rows, N, x, index)
+    if x is not None or dw is not None or need[1]:
+        rows, K, N, index, ldx, ldw, kind = _linear_args(x, w)
+        lddy, xp = _ld(dy, "dy", rows, N, x, index), x.data_ptr()
+    else:
+        rows, N, lddy, index = _operand(dy, "dy")
+        x, xp, kind = dy, 0, _DTYPES[dy.dtype]
+        _matrix(w, "w", like=dy)
+        K = ldx = w.shape[1]
+        ldw = _ld(w, "w", N, K, dy, index)
+        if K == 0:
+            raise MpcError(1, "the rows of w must hold at least one entry")
     zp, ldz = None, 0
     if code:
         if z is None:
@@ -911,7 +920,7 @@ def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0
         _vector_like(db, N, x, "db", index)
     elif need[2]:
         db = _new(N, x.dtype, x.device, stream)
-    xp, wp, dyp = x.data_ptr(), w.data_ptr(), dy.data_ptr()
+    wp, dyp = w.data_ptr(), dy.data_ptr()
     ws, wsp, wsb = _linear_ws(rows, K, N, kind, 1, xp, ldx, wp, ldw, dyp, lddy, ws, x, stream)
     _call(lib().mpc_linear_backward, x, index, stream, dyp, lddy, xp, ldx, wp, ldw, zp, ldz, rows, K, N, kind, code, p,
           seed & _SEEDS, None if step is None else _step(step, x.device), _address(dx), lddx, _address(dw), lddw, _address(db),

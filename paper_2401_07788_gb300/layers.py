@@ -74,7 +74,8 @@ class _LinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, residual, act, p, seed, step):
         y, z = mpc_linear_forward(x, w, bias, residual, act=act, p=p, seed=seed, step=step, keep=act is not None)
-        ctx.save_for_backward(x, w, z, step)
+        # x: for dw, and to hang the gradients on it where they depend on it by z
+        ctx.save_for_backward(x if ctx.needs_input_grad[1] or act is not None else None, w, z, step)
         ctx.call = act, p, seed
         return y
 

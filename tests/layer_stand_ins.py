@@ -21,6 +21,8 @@ def linear_forward(x, w, bias=None, residual=None, act=None, p=0.0, seed=0, step
 
 
 def linear_backward(dy, x, w, z=None, act=None, p=0.0, seed=0, step=None, need=(True, True, True), dx=None):
+    assert x is not None or not need[1]
+    x = dy.new_zeros(dy.shape[0], w.shape[1]) if x is None else x
     with torch.enable_grad():
         grads = forms.linear_grads(dy, x, w, z, act, _mask(seed, step, p, dy.shape))[:3]
     return tuple(g.to(x.dtype) if wanted else None for g, wanted in zip(grads, need))
