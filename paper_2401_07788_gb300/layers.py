@@ -74,20 +74,21 @@ class _LinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, residual, act, p, seed, step):
         y, z = mpc_linear_forward(x, w, bias, residual, act=act, p=p, seed=seed, step=step, keep=act is not None)
-        # x: for dw, and to hang the gradients on it where they depend on it by z
-        ctx.save_for_backward(x if ctx.needs_input_grad[1] or act is not None else None, w, z, step)
+        # x: for dw; x and bias also to hang the gradients on them where they depend on them by z
+        ctx.save_for_backward(x if ctx.needs_input_grad[1] or act is not None else None, w, z, step,
+                              None if act is None else bias)
         ctx.call = act, p, seed
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, w, z, step = ctx.saved_tensors
+        x, w, z, step, bias = ctx.saved_tensors
         act, p, seed = ctx.call
         need = ctx.needs_input_grad
         grads = None, None, None
         if any(need[:3]):
             grads = mpc_linear_backward(_rows(dy.detach()), x, w, z, act=act, p=p, seed=seed, step=step, need=need[:3])
-        return (*_final(grads, x, w, dy), dy if need[3] else None, None, None, None, None)
+        return (*_final(grads, x, w, bias, dy), dy if need[3] else None, None, None, None, None)
 
 
 def linear(x, w, bias=None, residual=None, act: str | None = None, p: float = 0.0, seed: int = 0, step=None):
