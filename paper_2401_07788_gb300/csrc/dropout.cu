@@ -4,7 +4,8 @@
 // What bounds it: HBM.  A draw (20 instructions) serves four entries, so an entry of bf16 costs 9
 // instructions of the 23 that an SM has for the 4 bytes it moves.  Four 16-byte groups a thread
 // keep enough bytes in flight.  Measured: 16384 x 4096 in fp32 with residual 107 us, without 75
-// (7.5 and 7.2 TB/s: the last 120 MB are still in L2), both 190.6 us among others (7.04 TB/s).
+// (7.5 and 7.2 TB/s: the last 120 MB are still in L2), both 190.6 us among others (7.04 TB/s); in bf16
+// 57 us and 40 (7.0 and 6.8 TB/s).
 #include "launch_util.h"
 #include "layers.cuh"
 

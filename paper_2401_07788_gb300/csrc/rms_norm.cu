@@ -18,8 +18,10 @@
 // would be written and read at twice the bytes; the sum made again would read x and r for h.
 //
 // What bounds it: HBM where rows are wide and aligned.  16384 x 4096 in bf16 with residual: forward
-// 80 us (6.7 TB/s), gradient 96 us (5.6 TB/s) and 5 us for dw's parts; 8192 x 768 in fp32 to 8 bits
-// 14 us (6.1 TB/s).  Rows on odd addresses are read entry by entry and wait for latency:
+// 80 us (6.7 TB/s), gradient 96 us (5.6 TB/s) and 5 us for dw's parts; in fp32 153 us (7.0 TB/s) and 163
+// with dw's parts (6.6 TB/s); 8192 x 768 in fp32 to 8 bits 14 us (6.1 TB/s).  Rows beyond 16384 entries are
+// read entry by entry also where they are aligned: 600 x 20000 in bf16 18 us (2.7 TB/s), gradient 50 us (1.4
+// TB/s).  Rows on odd addresses are read entry by entry and wait for latency:
 // 3001 x 2051 in bf16 to 8 bits 21 us, 0.9 TB/s.
 #include <algorithm>
 

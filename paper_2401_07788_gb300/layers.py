@@ -8,11 +8,12 @@ addition.  A block of a stage that normalises before its layers:
 * ``linear`` / ``Linear``, ``dropout`` / ``Dropout``, ``rms_norm`` / ``RMSNorm``: functions with their
   gradients, and modules on them.  Each makes the ``mpc_*`` calls of its name; these check their arguments.
 * ``RMSNorm(..., bits=8)`` is also the end of a stage whose boundary lies behind the norm: its output is sent
-  as an 8-bit payload and read back, in fp32.
+  as an 8-bit payload and read back, in fp32.  It is no ``CompressionBoundary``: it sends 8 bits in ``eval()`` as in
+  training, and its gradient goes back as it is (``CompressionBoundary(None, Quant(8))`` behind it compresses that).
 
 Dropout: masks are made from a seed where they are used and never stored.  A module's seed is
 ``(seed << 32) + calls``, with ``calls`` the number of its training calls.  Each of these also draws a number
-from torch's CPU generator (5 us).  Recomputation (``torch.utils.checkpoint``) puts that generator back for the
+from torch's CPU generator (4 us).  Recomputation (``torch.utils.checkpoint``) puts that generator back for the
 pass that it repeats, so a number that a module drew before marks a repeated call, which takes the earlier
 one's mask; so does any other program that puts the generator back.  A call inside a backward pass whose number
 is not known (recomputation that leaves the generator alone, or more than ``remembered`` calls later) is
@@ -20,7 +21,13 @@ refused.
 
 A captured graph repeats the host's numbers at every replay, so a module refuses to be captured unless it is
 given a device counter (``step=tensor``, int64, one entry) that the program advances between steps, after the
-backward pass.
+backward pass.  All calls between two advances take one mask: with several micro-batches a step, advance it
+after each one's backward pass.
+
+When masks repeat: a copy of a module (``copy.deepcopy``, a pickle) has its seed and count, so it drops the same places
+at its next call; layers cloned from one another want seeds of their own (``layer.seed = ...``).  A copy's device counter
+is a copy too, which the program has to advance.  ``calls`` is in no state dict: a run that resumes with a given seed
+sets it (``layer.calls = ...``), or its first masks are those of the first run.
 
 None of the gradients here can be differentiated again, and there are no forward-mode derivatives: asking for
 either raises.
@@ -268,7 +275,8 @@ class Linear(_Seeded):
 
 
 class RMSNorm(torch.nn.Module):
-    """A weight [width] of ones; forward(x) is the norm, forward(x, residual) the pair (norm, x + residual)."""
+    """A weight [width] of ones; forward(x) is the norm, forward(x, residual) the pair (norm, x + residual).  ``bits`` 8: the
+    norm by way of its 8-bit payload, in fp32, in training and in ``eval()`` alike."""
 
     def __init__(self, width: int, eps: float = 1e-6, bits: int | None = None, device=None, dtype=None):
         super().__init__()
