@@ -17,7 +17,7 @@
 //
 // What bounds it: the products.  Measured on one GB300: 8192^3 in bf16 558 us (1.97 PFLOP/s;
 // cuBLAS 546), 4096^3 in fp32 454 us (six plane products, 1.82 PFLOP/s); training 8192 x 4096 x
-// 1024 with dropout and residual 146 to 159 us over several boxes, 1000 x 777 x 2051 in fp32 with gelu 96.  fp32 of 9 to
+// 1024 with dropout and residual 146 to 159 us over several GPUs, 1000 x 777 x 2051 in fp32 with gelu 96.  fp32 of 9 to
 // 100 rows splits all of w in every call: 9 x 4096 x 4096 69 us, 64 rows 71, 100 rows 73 (8 rows in linear_few.cu 36).
 #include <algorithm>
 

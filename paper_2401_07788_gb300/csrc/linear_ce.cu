@@ -30,7 +30,7 @@
 // NaN: a logit that is NaN makes its token's loss, lse and gradients NaN.  An fp32
 // infinity in h or w becomes NaN in its planes.
 //
-// What bounds it: the matrix units (linear_ce_gemm.cuh).  Measured over several boxes:
+// What bounds it: the matrix units (linear_ce_gemm.cuh).  Measured over several GPUs:
 // 8192 tokens (a tenth ignored) x 768 x 50257 in bf16 1.20 to 1.26 ms, of which the
 // three products 1.08 ms (the gradient from lse where all count 1.14, the loss 0.38);
 // 8192 x 4096 x 131072 16.2 to 17.9 ms, 1.47 to 1.63 PFLOP/s of the 6 T D V operations;

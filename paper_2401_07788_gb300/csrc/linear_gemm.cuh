@@ -32,7 +32,7 @@ namespace {
 // relaxed one (a release waits for the stores: 2000 cycles a tile).  8192 x 64 x 8192 in bf16, 14 waves of
 // tiles with one K block: 42 us for z alone, 63 with gelu_tanh, 74 with dropout, 100 with both: 5800, 8800, 10300
 // and 13900 cycles a tile; no pipe is busy half of the time (with gelu_tanh the one of the special functions 19 %, with
-// dropout that of integers 48 %).  Measured in bf16 (one GB300, boxes differ
+// dropout that of integers 48 %).  Measured in bf16 (one GB300 each, they differ
 // by 3 %): 8192 x 1024 x 4096 44 us, with gelu_tanh and bias 58 to 65 (cuBLAS without any of it 37);
 // 8192^3 558 us (546); 2000 x 4096 x 8192 81 to 87 (72), whose 256 tiles are 3.4 waves of the 76
 // pairs.  Eight stages of 24 KB for tiles of 128 columns were 2 to 3 % slower: their addresses
