@@ -507,8 +507,11 @@ typedef enum {
     MPC_ACT_NONE = 0, MPC_ACT_RELU = 1, MPC_ACT_GELU = 2, MPC_ACT_GELU_TANH = 3, MPC_ACT_SILU = 4
 } mpc_act;
 
-/* The call that a linear layer's workspace is for. */
-typedef enum { MPC_LINEAR_FORWARD = 0, MPC_LINEAR_BACKWARD = 1 } mpc_linear_pass;
+/* The call that a linear layer's workspace is for.  MPC_LINEAR_BACKWARD_PLAIN: a gradient without
+ * activation and with p = 0, whose dz is dy itself; less room where a bf16 dy is read in place. */
+typedef enum {
+    MPC_LINEAR_FORWARD = 0, MPC_LINEAR_BACKWARD = 1, MPC_LINEAR_BACKWARD_PLAIN = 2
+} mpc_linear_pass;
 
 /* Linear layer with bias, activation, dropout and residual in one call:
  *   z = x w^T + bias;   y = residual + drop(act(z)).
@@ -544,7 +547,8 @@ mpc_status mpc_linear_forward(const void* x, int64_t ldx, const void* w, int64_t
  *   [rows][in], dw [out][in] and dbias [out] of `type`, out: each may be NULL, and is
  *   not formed then.  x is not read without dw, w not without dx.
  *   ws  workspace of ws_bytes >= mpc_linear_workspace_bytes(rows, in, out, type,
- *       MPC_LINEAR_BACKWARD, ldx, ldw, lddy), 256-byte aligned.
+ *       MPC_LINEAR_BACKWARD, ldx, ldw, lddy), or MPC_LINEAR_BACKWARD_PLAIN where that is the
+ *       call, 256-byte aligned.
  * Sums run in fp32 in a fixed order: results repeat bit for bit on one device.
  * rows = 0 writes dw = 0 and dbias = 0. */
 mpc_status mpc_linear_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,

@@ -837,18 +837,19 @@ def mpc_rms_norm_backward(dy, h, weight, rstd, dh=None, dx=None, dweight=None, n
 
 
 def mpc_linear_workspace_bytes(rows: int, inputs: int, outputs: int, dtype=torch.float32, backward: bool = False,
-                               ldx: int | None = None, ldw: int | None = None, lddy: int | None = None) -> int:
+                               ldx: int | None = None, ldw: int | None = None, lddy: int | None = None,
+                               plain: bool = False) -> int:
     """Bytes of workspace; ldx, ldw, lddy: the distances of the rows of x, w and dy (dense when None, 0 for an
-    operand that is not 16-byte aligned)."""
-    return int(lib().mpc_linear_workspace_bytes(rows, inputs, outputs, _DTYPES[dtype], int(backward),
+    operand that is not 16-byte aligned); ``plain``: of a backward call without activation and with p = 0."""
+    return int(lib().mpc_linear_workspace_bytes(rows, inputs, outputs, _DTYPES[dtype], (2 if plain else 1) if backward else 0,
                                                 inputs if ldx is None else ldx, inputs if ldw is None else ldw,
                                                 outputs if lddy is None else lddy))
 
 
-def _linear_ws(rows, K, N, kind, backward, x, ldx, w, ldw, dy, lddy, ws, of, stream):
-    """(ws, its address, its bytes); x, w, dy: addresses."""
+def _linear_ws(rows, K, N, kind, which, x, ldx, w, ldw, dy, lddy, ws, of, stream):
+    """(ws, its address, its bytes); which: 0 forward, 1 backward, 2 backward where dz is dy; x, w, dy: addresses."""
     if ws is None:
-        need = lib().mpc_linear_workspace_bytes(rows, K, N, kind, backward, 0 if x & 15 else ldx, 0 if w & 15 else ldw,
+        need = lib().mpc_linear_workspace_bytes(rows, K, N, kind, which, 0 if x & 15 else ldx, 0 if w & 15 else ldw,
                                                 0 if dy & 15 else lddy)
         if need == 0:
             return None, None, 0
@@ -921,7 +922,7 @@ def mpc_linear_backward(dy, x, w, z=None, act: str | None = None, p: float = 0.0
     elif need[2]:
         db = _new(N, x.dtype, x.device, stream)
     wp, dyp = w.data_ptr(), dy.data_ptr()
-    ws, wsp, wsb = _linear_ws(rows, K, N, kind, 1, xp, ldx, wp, ldw, dyp, lddy, ws, x, stream)
+    ws, wsp, wsb = _linear_ws(rows, K, N, kind, 1 if code or p else 2, xp, ldx, wp, ldw, dyp, lddy, ws, x, stream)
     _call(lib().mpc_linear_backward, x, index, stream, dyp, lddy, xp, ldx, wp, ldw, zp, ldz, rows, K, N, kind, code, p,
           seed & _SEEDS, None if step is None else _step(step, x.device), _address(dx), lddx, _address(dw), lddw, _address(db),
           wsp, wsb)

@@ -1021,7 +1021,7 @@ mpc_status mpc_rms_norm_backward(const void* dy, int64_t lddy, const void* h, in
 
 size_t mpc_linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, mpc_dtype type, mpc_linear_pass pass,
                                   int64_t ldx, int64_t ldw, int64_t lddy) {
-  if (rows == 0 || !linear_sizes_ok(rows, in, out) || pass < MPC_LINEAR_FORWARD || pass > MPC_LINEAR_BACKWARD) return 0;
+  if (rows == 0 || !linear_sizes_ok(rows, in, out) || pass < MPC_LINEAR_FORWARD || pass > MPC_LINEAR_BACKWARD_PLAIN) return 0;
   return mpc::linear_workspace_bytes(rows, in, out, type == MPC_BF16, pass, ldx, ldw, lddy);
 }
 
@@ -1118,7 +1118,7 @@ mpc_status mpc_linear_backward(const void* dy, int64_t lddy, const void* x, int6
   }
   if (act != MPC_ACT_NONE) MPC_TRY(check_rows(z, rows, out, ldz, type, "z"));
   MPC_TRY(check_ws(ws, ws_bytes,
-                   mpc::linear_workspace_bytes(rows, in, out, a.bf16, MPC_LINEAR_BACKWARD, ld_in_place(x, ldx),
+                   mpc::linear_workspace_bytes(rows, in, out, a.bf16, mpc::linear_backward_pass(a), ld_in_place(x, ldx),
                                                ld_in_place(w, ldw), ld_in_place(dy, lddy)), 256));
   Device d;
   MPC_TRY(current_device(&d));

@@ -239,6 +239,8 @@ struct LinearArgs {
 };
 size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, int pass, int64_t ldx,
                               int64_t ldw, int64_t lddy);
+// The pass of a backward call's workspace: MPC_LINEAR_BACKWARD_PLAIN where dz is drop(dy) act'(z) = dy.
+int linear_backward_pass(const LinearArgs& a);
 cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_linear_backward(const LinearArgs& a, int num_sms, cudaStream_t s);
 // The forward pass of a few rows (linear_few.cu); ldx, ldw: 0 for an operand off 16 bytes.

@@ -375,7 +375,8 @@ Layout layout(int64_t rows, int64_t in, int64_t out, bool bf16, int pass, int64_
     l.forward = cut_tiles(rows, out, (in + kK - 1) / kK, planes);
     l.sum = take(cut_bytes(l.forward, rows, out));
   } else {
-    l.dz = take(static_cast<size_t>(planes) * rows * l.Np * 2);
+    // plain: dz is dy itself where it is read in place
+    l.dz = take(pass == MPC_LINEAR_BACKWARD_PLAIN && !l.pack_dy ? 0 : static_cast<size_t>(planes) * rows * l.Np * 2);
     l.part = take((rows + dz_rows(rows, out) - 1) / dz_rows(rows, out) * out * 4);
     l.dx = cut_tiles(rows, in, (out + kK - 1) / kK, planes);
     l.dw = cut_tiles(out, in, (rows + kK - 1) / kK, planes);
@@ -483,7 +484,7 @@ cudaError_t forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
 template <typename E>
 cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   constexpr int P = sizeof(E) == 2 ? 1 : 3;
-  const Layout l = layout(a.rows, a.in, a.out, P == 1, MPC_LINEAR_BACKWARD, on16(a.x, 0, 1) ? a.ldx : 0,
+  const Layout l = layout(a.rows, a.in, a.out, P == 1, linear_backward_pass(a), on16(a.x, 0, 1) ? a.ldx : 0,
                           on16(a.w, 0, 1) ? a.ldw : 0, on16(a.dy, 0, 1) ? a.lddy : 0);
   char* ws = static_cast<char*>(a.ws);
   float* part = reinterpret_cast<float*>(ws + l.part);
@@ -494,7 +495,7 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   f.z = static_cast<const E*>(a.z_in);
   f.ldz = a.ldz;
   f.wide_z = on16(a.z_in, a.ldz, sizeof(E));
-  const bool make = products && (l.pack_dy || a.act != MPC_ACT_NONE || f.drop.level > 0);
+  const bool make = products && (l.pack_dy || linear_backward_pass(a) == MPC_LINEAR_BACKWARD);
   f.dy = operand<E>(a.dy, a.lddy, a.rows, a.out, l.Np, make ? reinterpret_cast<uint16_t*>(ws + l.dz) : nullptr, num_sms);
   f.part = a.dbias != nullptr ? part : nullptr;
   f.dz_rows = static_cast<int>(dz_rows(a.rows, a.out));
@@ -536,6 +537,9 @@ cudaError_t backward(const LinearArgs& a, int num_sms, cudaStream_t s) {
 size_t linear_workspace_bytes(int64_t rows, int64_t in, int64_t out, int bf16, int pass, int64_t ldx, int64_t ldw, int64_t lddy) {
   if (pass == MPC_LINEAR_FORWARD && linear_few_fits(rows, in, bf16, ldx, ldw)) return 0;
   return layout(rows, in, out, bf16 != 0, pass, ldx, ldw, lddy).total;
+}
+int linear_backward_pass(const LinearArgs& a) {
+  return a.act == MPC_ACT_NONE && make_drop(a.p, 0, nullptr).level == 0 ? MPC_LINEAR_BACKWARD_PLAIN : MPC_LINEAR_BACKWARD;
 }
 cudaError_t launch_linear_forward(const LinearArgs& a, int num_sms, cudaStream_t s) {
   if (linear_few_fits(a.rows, a.in, a.bf16, on16(a.x, 0, 1) ? a.ldx : 0, on16(a.w, 0, 1) ? a.ldw : 0))
